@@ -329,8 +329,57 @@ DODO_API int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_
                         const void* locV, const int32_t* loc_off, const int32_t* loc_len, const int32_t* loc_pos0,
                         int loc_rows, int B, void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Nugget cache held in 4 bits.  dodo_gather_kv_q4 is dodo_gather_kv into such a cache: the same tables, append and
+ * bookkeeping, the selected rows quantised on the way.  A row of one head is cut into groups of DODO_Q4_GROUP features;
+ * with lo and hi a group's least and largest value
+ *   m = the largest bf16 number <= lo,   s = the least bf16 number with 15 s >= hi - m,
+ *   c_i = (x_i - m) / s rounded to the nearest whole number, ties to even (0 where s = 0),
+ * and feature i stands for m + c_i s, at most s / 2 from x_i.  The result is unique.  A group that holds a NaN or an
+ * infinity, or whose span overflows fp32, is stored as NaN (all of its features read back as NaN).
+ *   cache_q4    [device] bytes [cache_off[B], H, 2, dh / 2], 16-byte aligned: the codes of a row's K, then of its V;
+ *               feature 2 i in the low half of byte i
+ *   cache_scale [device] uint32 [cache_off[B], H, 2, dh / DODO_Q4_GROUP], 16-byte aligned: s in the low 16 bits of a
+ *               group's word, m in the high 16
+ *   everything else as in dodo_gather_kv
+ * A row takes H * 160 bytes at head size 128 (dodo_gather_kv: H * 512 in bf16).  Supported: dh in {64, 128}.
+ */
+enum { DODO_Q4_GROUP = 32 };
+DODO_API int dodo_gather_kv_q4(dodo_ctx* ctx, const void* K, const void* V, int dtype, int H, int dh,
+                      const int32_t* seq_off, const int32_t* idx, const int32_t* nug_off, const int32_t* pos_base, int B,
+                      void* cache_q4, uint32_t* cache_scale, int32_t* cache_pos, const int32_t* cache_off,
+                      int32_t* cache_len, void* stream);
+
+/*
+ * The rows in use of a 4-bit cache as rows of `dtype`: row r of sequence b's region, r < cache_len[b], is written to row
+ * cache_off[b] + r of K and of V (m + c s, rounded once to fp32 and once more to bf16); other rows are left as they were.
+ * K, V with cache_pos, cache_off and cache_len are then a nugget cache as dodo_attend reads it.
+ *   K, V  [device] [cache_off[B], H, dh] in `dtype`, 16-byte aligned
+ */
+DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32_t* cache_scale, int H, int dh,
+                      const int32_t* cache_off, const int32_t* cache_len, int B, int dtype, void* K, void* V, void* stream);
+
+/*
+ * dodo_attend over a 4-bit nugget cache (local tokens, queries and outputs in `dtype`): the keys and values of cached
+ * rows are those that the codes stand for, fp32 arithmetic, one rounding of O.  A block of queries whose longest part has
+ * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale > 0) runs on the tensor cores when the
+ * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
+ * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
+ * call takes the streaming kernel.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache
+ * by other means than dodo_gather_kv_q4 calls dodo_cache_written.
+ *   cache_rows  cache_off[B] of the calls that the workspace is meant for
+ *   everything else as in dodo_attend and dodo_gather_kv_q4
+ * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.
+ */
+DODO_API size_t dodo_attend_q4_workspace_bytes(const dodo_ctx* ctx, int H, int dh, int cache_rows);
+DODO_API int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H,
+                   int dh, float sm_scale, const void* cache_q4, const uint32_t* cache_scale, const int32_t* cache_pos,
+                   const int32_t* cache_off, const int32_t* cache_len, const void* locK, const void* locV,
+                   const int32_t* loc_off, const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, void* O,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Tells the context that a nugget cache was written by something other than its own dodo_gather_kv*
- * calls (see "Stream order" above): the next dodo_attend reads no cache row ahead of its dependency
+ * calls or dodo_gather_kv_q4 (see "Stream order" above): the next dodo_attend or dodo_attend_q4 reads no cache row ahead of its dependency
  * wait.  Host-side flag only; nothing is launched. */
 DODO_API int dodo_cache_written(dodo_ctx* ctx);
 

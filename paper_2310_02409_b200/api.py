@@ -20,6 +20,7 @@ FORCE_LAST = 1
 ACT_IDENTITY, ACT_RELU, ACT_GELU_TANH = 0, 1, 2
 TUNE_ATTEND_TARGET_BLOCKS, TUNE_DENSE_MIN_QUERIES, TUNE_DENSE_BALANCE = 1, 3, 4
 DEV_WAIT_TIMEOUT, DEV_BAD_INDEX = 1, 2
+Q4_GROUP = 32
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_CUDA = 0, -1, -2, -3, -4
 
 # every symbol include/dodo.h declares: name -> (restype, argtypes)
@@ -52,6 +53,11 @@ SIGNATURES = {
                          _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "dodo_attend_indexed": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                  _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "dodo_gather_kv_q4": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dodo_expand_kv_q4": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _i, _i, _vp, _vp, _vp]),
+    "dodo_attend_q4_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
+    "dodo_attend_q4": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                            _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "dodo_host_arena_bytes": (_sz, [_vp, _i, _i, _i, _i, _i, _i, _i, _i, _i]),
     "dodo_compress_decode_host": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _vp, _i, _f,
                                        _vp, _vp, _sz, _vp]),
@@ -97,6 +103,25 @@ def _dev(t: torch.Tensor | None):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("device arguments must be contiguous CUDA tensors")
     return t.data_ptr()
+
+
+def _on(device: torch.device, shapes: dict, dtypes: dict):
+    """Raises unless every named tensor (None: skipped) lies on ``device``, dense, with its shape and dtype."""
+    for name, (t, shape) in shapes.items():
+        if t is None:
+            continue
+        if t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor on {device}")
+        if t.dtype != dtypes[name]:
+            raise TypeError(f"{name} must be {dtypes[name]}, is {t.dtype}")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+
+
+def _len_array(cache_len) -> np.ndarray:
+    if not (isinstance(cache_len, np.ndarray) and cache_len.dtype == np.int32 and cache_len.flags.c_contiguous):
+        raise TypeError("cache_len must be a contiguous int32 numpy array (updated in place)")
+    return cache_len
 
 
 def _host_i32(a) -> np.ndarray | None:
@@ -294,6 +319,79 @@ class Dodo:
                                           _dev(cacheK), _dev(cacheV), _dev(cache_pos), _hp(co), _hp(cl),
                                           _dev(locK), _dev(locV), _hp(lo), _hp(ll), _hp(lp), loc_rows,
                                           len(qo) - 1, _dev(O), _dev(lse), _dev(workspace), ws_bytes, _stream()))
+
+    # -- the 4-bit nugget cache ----------------------------------------------------------------------
+    def _q4_cache(self, cache_q4, cache_scale, H, dh, more=(), dtypes=None):
+        rows = cache_q4.shape[0]
+        shapes = {"cache_q4": (cache_q4, (rows, H, 2, dh // 2)), "cache_scale": (cache_scale, (rows, H, 2, dh // Q4_GROUP)), **dict(more)}
+        _on(self.device, shapes, {"cache_q4": torch.uint8, "cache_scale": torch.int32, **(dtypes or {})})
+        return rows
+
+    def _regions(self, rows, off, lens=None, what="cache_off"):
+        if len(off) and int(off[-1]) > rows:
+            raise ValueError(f"{what} ends at row {int(off[-1])} of an array of {rows}")
+        if lens is not None and len(lens) < len(off) - 1:
+            raise ValueError(f"{len(off) - 1} regions, {len(lens)} lengths")
+
+    def gather_kv_q4(self, K, V, seq_off, idx, nug_off, pos_base, cache_q4, cache_scale, cache_pos, cache_off, cache_len):
+        """``dodo_gather_kv_q4``: append the selected rows to a 4-bit cache (``cache_q4`` uint8 [rows, H, 2, dh/2],
+        ``cache_scale`` int32 [rows, H, 2, dh/32]); ``cache_len`` (int32 numpy array) is updated in place."""
+        so, no, pb, co = _host_i32(seq_off), _host_i32(nug_off), _host_i32(pos_base), _host_i32(cache_off)
+        H, dh = K.shape[-2], K.shape[-1]
+        code = _dtype_code(K)
+        rows = self._q4_cache(cache_q4, cache_scale, H, dh,
+                              {"K": (K, None), "V": (V, K.shape), "idx": (idx, None), "cache_pos": (cache_pos, None)},
+                              {"K": K.dtype, "V": K.dtype, "idx": torch.int32, "cache_pos": torch.int32})
+        B = len(so) - 1
+        self._regions(K.shape[0], so, None, "seq_off")
+        self._regions(idx.numel(), no, None, "nug_off")
+        self._regions(min(rows, cache_pos.numel()), co, _len_array(cache_len))
+        if not (len(no) == len(co) == B + 1 and len(pb) >= B):
+            raise ValueError("seq_off, nug_off, pos_base and cache_off must describe the same number of sequences")
+        self._check(self._lib.dodo_gather_kv_q4(self._ctx, K.data_ptr(), V.data_ptr(), code, H, dh, _hp(so), idx.data_ptr(), _hp(no),
+                                                _hp(pb), B, cache_q4.data_ptr(), cache_scale.data_ptr(), cache_pos.data_ptr(), _hp(co),
+                                                _hp(cache_len), _stream()))
+
+    def expand_kv_q4(self, cache_q4, cache_scale, cache_off, cache_len, K, V):
+        """``dodo_expand_kv_q4``: the rows in use of a 4-bit cache as rows of K and V (their dtype, the cache's row layout)."""
+        co, cl = _host_i32(cache_off), _host_i32(cache_len)
+        H, dh = K.shape[-2], K.shape[-1]
+        code = _dtype_code(K)
+        rows = self._q4_cache(cache_q4, cache_scale, H, dh, {"K": (K, None), "V": (V, K.shape)}, {"K": K.dtype, "V": K.dtype})
+        self._regions(min(rows, K.shape[0]), co, cl)
+        self._check(self._lib.dodo_expand_kv_q4(self._ctx, cache_q4.data_ptr(), cache_scale.data_ptr(), H, dh, _hp(co), _hp(cl),
+                                                len(co) - 1, code, K.data_ptr(), V.data_ptr(), _stream()))
+
+    def attend_q4_workspace_bytes(self, H: int, dh: int, cache_rows: int) -> int:
+        return int(self._lib.dodo_attend_q4_workspace_bytes(self._ctx, int(H), int(dh), int(cache_rows)))
+
+    def attend_q4(self, Q, q_off, q_pos0, sm_scale, cache_q4, cache_scale, cache_pos, cache_off, cache_len,
+                  locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):
+        """``dodo_attend_q4``: ``attend`` over a 4-bit nugget cache and uncompressed local tokens."""
+        qo, qp = _host_i32(q_off), _host_i32(q_pos0)
+        co, cl = _host_i32(cache_off), _host_i32(cache_len)
+        lo, ll, lp = _host_i32(loc_off), _host_i32(loc_len), _host_i32(loc_pos0)
+        H, dh = Q.shape[-2], Q.shape[-1]
+        code, B, dt = _dtype_code(Q), len(qo) - 1, Q.dtype
+        loc_rows = 0 if locK is None else locK.shape[0]
+        more = {"Q": (Q, None), "O": (O, Q.shape), "lse": (lse, Q.shape[:2]), "locK": (locK, None), "locV": (locV, locK.shape if locK is not None else None),
+                "cache_pos": (cache_pos, None), "workspace": (workspace, None)}
+        types = {"Q": dt, "O": dt, "lse": torch.float32, "locK": dt, "locV": dt, "cache_pos": torch.int32,
+                 "workspace": workspace.dtype if workspace is not None else None}
+        if cache_q4 is not None:
+            self._regions(min(self._q4_cache(cache_q4, cache_scale, H, dh, more, types), cache_pos.numel()), co, cl)
+            if len(co) != B + 1:
+                raise ValueError("cache_off and q_off must describe the same number of sequences")
+        else:
+            _on(self.device, more, types)
+        self._regions(Q.shape[0], qo, qp, "q_off")
+        if locK is not None and not (len(lo) >= B and len(ll) >= B and len(lp) >= B and tuple(locK.shape[1:]) == (H, dh)):
+            raise ValueError("loc_off, loc_len and loc_pos0 must have one entry a sequence, locK and locV [rows, H, dh]")
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._check(self._lib.dodo_attend_q4(self._ctx, Q.data_ptr(), _hp(qo), _hp(qp), code, H, dh, float(sm_scale), ptr(cache_q4),
+                                             ptr(cache_scale), ptr(cache_pos), _hp(co), _hp(cl), ptr(locK), ptr(locV), _hp(lo), _hp(ll),
+                                             _hp(lp), loc_rows, B, O.data_ptr(), ptr(lse), ptr(workspace), ws_bytes, _stream()))
 
     def attend_indexed(self, Q, q_off, q_pos0, sm_scale, K, V, seq_off, idx, nug_off, pos_base,
                        locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):

@@ -345,10 +345,12 @@ int dodo_score_select(dodo_ctx* ctx, const void* X, int dtype, int d, const void
     return DODO_OK;
 }
 
-// Checks shared by the two gather entry points (everything but the K/V pointers).  row_bytes is set.
-static int gather_check(dodo_ctx* ctx, int dtype, int H, int dh, const int32_t* seq_off, const int32_t* nug_off,
-                        const int32_t* pos_base, int B, const int32_t* cache_off, const int32_t* cache_len,
-                        size_t* row_bytes) {
+}  // extern "C"
+
+// Checks shared by the gather entry points (everything but the K/V pointers).  row_bytes is set.
+int dodo_check_gather(dodo_ctx* ctx, int dtype, int H, int dh, const int32_t* seq_off, const int32_t* nug_off,
+                      const int32_t* pos_base, int B, const int32_t* cache_off, const int32_t* cache_len,
+                      size_t* row_bytes) {
     if (B < 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "B = %d is negative", B);
     if (!valid_dtype(dtype)) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "dtype %d", dtype);
     if (H <= 0 || dh <= 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "H = %d, dh = %d", H, dh);
@@ -367,8 +369,8 @@ static int gather_check(dodo_ctx* ctx, int dtype, int H, int dh, const int32_t* 
     return DODO_OK;
 }
 
-static void gather_group(GatherGroup& g, int b0, int B, const int32_t* seq_off, const int32_t* nug_off,
-                         const int32_t* pos_base, const int32_t* cache_off, const int32_t* cache_len) {
+void dodo_fill_gather_group(GatherGroup& g, int b0, int B, const int32_t* seq_off, const int32_t* nug_off,
+                            const int32_t* pos_base, const int32_t* cache_off, const int32_t* cache_len) {
     g.nseq = B - b0 < DODO_GROUP ? B - b0 : DODO_GROUP;
     for (int i = 0; i < g.nseq; ++i) {
         const int b = b0 + i;
@@ -381,13 +383,15 @@ static void gather_group(GatherGroup& g, int b0, int B, const int32_t* seq_off, 
     g.idx0[g.nseq] = nug_off[b0 + g.nseq];
 }
 
+extern "C" {
+
 int dodo_gather_kv(dodo_ctx* ctx, const void* K, const void* V, int dtype, int H, int dh,
                    const int32_t* seq_off, const int32_t* idx, const int32_t* nug_off,
                    const int32_t* pos_base, int B, void* cacheK, void* cacheV, int32_t* cache_pos,
                    const int32_t* cache_off, int32_t* cache_len, void* stream) {
     if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
     size_t row_bytes = 0;
-    const int rc0 = gather_check(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
+    const int rc0 = dodo_check_gather(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
     if (rc0 != DODO_OK) return rc0;
     if (nug_off[B] > 0) {
         if (K == nullptr || V == nullptr || idx == nullptr || cacheK == nullptr || cacheV == nullptr || cache_pos == nullptr)
@@ -397,7 +401,7 @@ int dodo_gather_kv(dodo_ctx* ctx, const void* K, const void* V, int dtype, int H
     }
     for (int b0 = 0; b0 < B; b0 += DODO_GROUP) {
         GatherGroup g;
-        gather_group(g, b0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
+        dodo_fill_gather_group(g, b0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
         ctx->cache_clean = false;   // the next attend must not read cache rows ahead of its dependency wait
         const int rc = dodo_launch_gather(ctx, K, V, row_bytes, idx, g, cacheK, cacheV, cache_pos, ctx->dev_status,
                                           static_cast<cudaStream_t>(stream));
@@ -417,7 +421,7 @@ int dodo_compress(dodo_ctx* ctx, const void* X, int dtype, int d, const void* w,
     rc = check_select_args(ctx, seq_off, nug_off, B, flags, idx);
     if (rc != DODO_OK) return rc;
     size_t row_bytes = 0;
-    rc = gather_check(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
+    rc = dodo_check_gather(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
     if (rc != DODO_OK) return rc;
     if (nug_off[B] > 0) {
         if (K == nullptr || V == nullptr || cacheK == nullptr || cacheV == nullptr || cache_pos == nullptr)
@@ -433,7 +437,7 @@ int dodo_compress(dodo_ctx* ctx, const void* X, int dtype, int d, const void* w,
         ScoreSelectGroup sg;
         fill_score_group(sg, seq_off, nug_off, 0, B);
         GatherGroup gg;
-        gather_group(gg, 0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
+        dodo_fill_gather_group(gg, 0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         rc = dodo_launch_score(ctx, X, dtype, d, w, bias, sg, 1, flags, scores, idx, ctx->tickets,
                                ctx->compress_state + DODO_FLAG_STRIDE, st);
@@ -458,7 +462,7 @@ int dodo_gather_kv_layers(dodo_ctx* ctx, int L, const void* const* K, const void
     if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
     if (L < 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "L = %d is negative", L);
     size_t row_bytes = 0;
-    const int rc0 = gather_check(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
+    const int rc0 = dodo_check_gather(ctx, dtype, H, dh, seq_off, nug_off, pos_base, B, cache_off, cache_len, &row_bytes);
     if (rc0 != DODO_OK) return rc0;
     if (L == 0) return DODO_OK;   // no layer: nothing is appended, cache_len stays
     if (nug_off[B] > 0) {
@@ -472,7 +476,7 @@ int dodo_gather_kv_layers(dodo_ctx* ctx, int L, const void* const* K, const void
         }
         for (int b0 = 0; b0 < B; b0 += DODO_GROUP) {
             GatherGroup g;
-            gather_group(g, b0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
+            dodo_fill_gather_group(g, b0, B, seq_off, nug_off, pos_base, cache_off, cache_len);
             for (int l0 = 0; l0 < L; l0 += DODO_LAYER_GROUP) {
                 GatherLayers lay;
                 lay.n = L - l0 < DODO_LAYER_GROUP ? L - l0 : DODO_LAYER_GROUP;
@@ -551,32 +555,26 @@ size_t dodo_attend_workspace_bytes(const dodo_ctx* ctx, int dh) {
     return stream_bytes > dense_bytes ? stream_bytes : dense_bytes;
 }
 
-int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0,
-                int dtype, int H, int dh, float sm_scale,
-                const void* cacheK, const void* cacheV, const int32_t* cache_pos,
-                const int32_t* cache_off, const int32_t* cache_len,
-                const void* locK, const void* locV, const int32_t* loc_off,
-                const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B,
-                void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
+}  // extern "C"
+
+int dodo_check_attend_queries(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H, int dh, int B) {
     if (B < 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "B = %d is negative", B);
     if (!valid_dtype(dtype)) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "dtype %d", dtype);
     if (dh != 64 && dh != 128) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "head size %d (supported: 64, 128)", dh);
     if (H <= 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "H = %d", H);
     if (!valid_offsets(q_off, B)) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "q_off must start at 0 and be non-decreasing");
     if (B > 0 && q_pos0 == nullptr) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "q_pos0 must not be NULL");
-    if (q_off[B] == 0) return DODO_OK;
-    if (Q == nullptr || O == nullptr || !dodo_aligned16(Q) || !dodo_aligned16(O))
-        return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "Q and O must be non-NULL and 16-byte aligned");
+    return DODO_OK;
+}
 
-    // key segments
-    bool any_cache = false, any_local = false;
+int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_t* cache_len, const int32_t* loc_off,
+                           const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, bool* any_cache, bool* any_local) {
     if (cache_len != nullptr) {
         if (!valid_offsets(cache_off, B)) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "cache_off must start at 0 and be non-decreasing");
         for (int b = 0; b < B; ++b) {
             if (cache_len[b] < 0 || cache_len[b] > cache_off[b + 1] - cache_off[b])
                 return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "sequence %d: cache_len %d outside its region", b, cache_len[b]);
-            any_cache = any_cache || cache_len[b] > 0;
+            *any_cache = *any_cache || cache_len[b] > 0;
         }
     }
     if (loc_len != nullptr) {
@@ -586,10 +584,40 @@ int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_
                 if (loc_off == nullptr || loc_pos0 == nullptr) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "loc_off and loc_pos0 must not be NULL");
                 if (loc_off[b] < 0 || static_cast<int64_t>(loc_off[b]) + loc_len[b] > loc_rows)
                     return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "sequence %d: local rows [%d, %d) outside loc_rows = %d", b, loc_off[b], loc_off[b] + loc_len[b], loc_rows);
-                any_local = true;
+                *any_local = true;
             }
         }
     }
+    return DODO_OK;
+}
+
+// A call's work is launched on the caller's current device, so that has to be the context's.
+int dodo_check_device(dodo_ctx* ctx) {
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "cudaGetDevice");
+    if (dev != ctx->device)
+        return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "the current device is %d, the context belongs to device %d", dev, ctx->device);
+    return DODO_OK;
+}
+
+extern "C" {
+
+int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0,
+                int dtype, int H, int dh, float sm_scale,
+                const void* cacheK, const void* cacheV, const int32_t* cache_pos,
+                const int32_t* cache_off, const int32_t* cache_len,
+                const void* locK, const void* locV, const int32_t* loc_off,
+                const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B,
+                void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
+    bool any_cache = false, any_local = false;
+    int rc = dodo_check_attend_queries(ctx, q_off, q_pos0, dtype, H, dh, B);
+    if (rc != DODO_OK || q_off[B] == 0) return rc;
+    if (Q == nullptr || O == nullptr || !dodo_aligned16(Q) || !dodo_aligned16(O))
+        return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "Q and O must be non-NULL and 16-byte aligned");
+    rc = dodo_check_attend_keys(ctx, cache_off, cache_len, loc_off, loc_len, loc_pos0, loc_rows, B, &any_cache, &any_local);
+    if (rc != DODO_OK) return rc;
     if (any_cache && (cacheK == nullptr || cacheV == nullptr || cache_pos == nullptr || !dodo_aligned16(cacheK) || !dodo_aligned16(cacheV)))
         return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "cacheK, cacheV, cache_pos must be non-NULL, K/V 16-byte aligned");
     if (any_local && (locK == nullptr || locV == nullptr || !dodo_aligned16(locK) || !dodo_aligned16(locV)))
@@ -609,7 +637,6 @@ int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_
     const AttendMaps maps = {any_cache ? cacheK : nullptr, any_cache ? cacheV : nullptr,
                              any_local ? locK : nullptr, any_local ? locV : nullptr};
     DenseMaps dmaps;
-    int rc = DODO_OK;
     if (dense) {
         plan.qt = dodo_dense_tile_queries();
         tot.split = false;

@@ -106,6 +106,12 @@ struct GatherGroup {
     int pos_base[DODO_GROUP];
 };
 
+// argument checks and launch tables shared by the entry points that append to a cache
+int dodo_check_gather(dodo_ctx* ctx, int dtype, int H, int dh, const int32_t* seq_off, const int32_t* nug_off,
+                      const int32_t* pos_base, int B, const int32_t* cache_off, const int32_t* cache_len, size_t* row_bytes);
+void dodo_fill_gather_group(GatherGroup& g, int b0, int B, const int32_t* seq_off, const int32_t* nug_off,
+                            const int32_t* pos_base, const int32_t* cache_off, const int32_t* cache_len);
+
 int dodo_launch_gather(dodo_ctx* ctx, const void* K, const void* V, size_t row_bytes,
                        const int32_t* idx, const GatherGroup& g, void* cacheK, void* cacheV,
                        int32_t* cache_pos, int* dev_status, cudaStream_t st);
@@ -144,7 +150,26 @@ struct PoolGroup {
 int dodo_launch_pool(dodo_ctx* ctx, const void* K, const void* V, int dtype, size_t row_bytes, int r, const PoolGroup& g,
                      void* cacheK, void* cacheV, int32_t* cache_pos, cudaStream_t st);
 
+// ---- 4-bit nugget cache -------------------------------------------------------------------------
+// gather into it: as dodo_launch_gather, the rows quantised on the way (format: see dodo_gather_kv_q4 in dodo.h)
+int dodo_launch_gather_q4(dodo_ctx* ctx, const void* K, const void* V, int dtype, int H, int dh, const int32_t* idx,
+                          const GatherGroup& g, void* cache_q4, uint32_t* cache_scale, int32_t* cache_pos, int* dev_status,
+                          cudaStream_t st);
+struct ExpandGroup {
+    int nseq;
+    int out0[DODO_GROUP + 1];   // prefix of rows per sequence
+    int row0[DODO_GROUP];       // first cache row of the sequence
+};
+int dodo_launch_expand_q4(dodo_ctx* ctx, const void* cache_q4, const uint32_t* cache_scale, int H, int dh, int dtype,
+                          const ExpandGroup& g, void* K, void* V, cudaStream_t st);
+
 // ---- attend -----------------------------------------------------------------------------------
+// argument checks shared by the attend entry points; any_cache / any_local are set where a segment has rows
+int dodo_check_attend_queries(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H, int dh, int B);
+int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_t* cache_len, const int32_t* loc_off,
+                           const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, bool* any_cache, bool* any_local);
+int dodo_check_device(dodo_ctx* ctx);
+
 struct AttendSeq {
     int q_row0;     // first query row
     int tq;         // query tokens
@@ -226,6 +251,11 @@ struct DenseGather {
 int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps,
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
+// The streaming kernel over a 4-bit cache: launch as above, the cache as codes and group words
+int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const AttendPlan& plan,
+                          const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale,
+                          const int32_t* cache_pos, const void* locK, const void* locV, void* O, float* lse,
+                          float* partials, int* tickets, bool early_cache, cudaStream_t st);
 int dodo_attend_tile_keys(int dtype, int dh);
 int dodo_attend_max_qt(int dtype, int dh);
 int dodo_attend_max_cluster();   // most chunks of one (query tile, head) that can merge inside a cluster

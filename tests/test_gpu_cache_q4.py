@@ -1,0 +1,397 @@
+"""The 4-bit nugget cache on the GPU: append and expansion bit for bit against the format's definition in 64 bits, attention over
+it against the plain form over the values the codes stand for."""
+import numpy as np
+import pytest
+import torch
+
+import plain64
+from paper_2310_02409_b200 import api, inputs
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _cuda(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def _cache(rows, H, dh, fill=0x5a):
+    return (torch.full((rows, H, 2, dh // 2), fill, dtype=torch.uint8, device="cuda"),
+            torch.full((rows, H, 2, dh // 32), 0x12345678, dtype=torch.int32, device="cuda"),
+            torch.full((rows,), -7, dtype=torch.int32, device="cuda"))
+
+
+def _hard_rows(H, dh, dtype):
+    """Rows whose groups are what the format finds hard, in the storage type."""
+    rs = np.random.RandomState(5)
+    rows = []
+    rows.append(np.zeros((H, dh)))                                            # s = 0
+    rows.append(np.full((H, dh), -1.7))                                       # constant (fp32: not a bf16 number)
+    rows.append(np.tile(np.arange(32) * 0.5 - 8.0, H * dh // 32))             # many values exactly on borders
+    rows.append(np.tile(np.concatenate([[-1.5, 13.5], np.tile([1e-10, -1e-10, 0.0, 1e-30, -1e-30], 6)]), H * dh // 32))  # borders decided far below fp32
+    rows.append(rs.standard_normal(H * dh) * 1e-40)                           # subnormal
+    rows.append(rs.standard_normal(H * dh) * 1e37)
+    rows.append(rs.standard_normal(H * dh) * 10.0 ** rs.randint(-30, 30, H * dh))
+    rows.append(np.tile(np.concatenate([[0.0, 15.0], np.arange(30) / 2.0]), H * dh // 32))   # every half step
+    rows.append(np.where(rs.randint(0, 200, H * dh) == 0, np.nan, rs.standard_normal(H * dh)))
+    rows.append(np.where(rs.randint(0, 200, H * dh) == 0, np.inf, rs.standard_normal(H * dh)))
+    rows.append(np.where(rs.randint(0, 200, H * dh) == 0, -np.inf, rs.standard_normal(H * dh)))
+    rows.append(np.where(np.arange(H * dh) % 32 == 3, 3.3e38, -3.3e38) * (np.arange(H * dh) % 64 < 32))   # span overflows
+    x = np.stack([np.asarray(r).reshape(H, dh) for r in rows])
+    return torch.from_numpy(x).to(torch.float32).to(dtype)
+
+
+@pytest.mark.parametrize("dtype,H,dh", [(BF, 32, 128), (F32, 4, 64), (BF, 3, 64), (F32, 5, 128), (BF, 1, 64), (F32, 1, 128)])
+def test_gather_q4_is_the_format_bit_for_bit(dodo, dtype, H, dh):
+    lens, ks, used = [40, 0, 300, 1, 64], [17, 0, 31, 1, 64], [3, 0, 0, 1, 2]
+    seq_off, nug_off = inputs.offsets(lens), inputs.offsets(ks)
+    cache_off = inputs.offsets([k + u + 2 for k, u in zip(ks, used)])
+    N, rows = int(seq_off[-1]), int(cache_off[-1])
+    K = inputs.randn((N, H, dh), "q4", H, dh, "K", dtype=dtype)
+    V = inputs.randn((N, H, dh), "q4", H, dh, "V", std=3.0, dtype=dtype)
+    hard = _hard_rows(H, dh, dtype)
+    K[40:40 + len(hard)] = hard
+    V[340:340 + 1] = hard[6:7]
+    V[341:341 + len(hard)] = hard
+    rs = np.random.RandomState(1)
+    idx = [np.sort(rs.permutation(n)[:k]).astype(np.int32) for n, k in zip(lens, ks)]
+    idx[2] = np.arange(31, dtype=np.int32)                    # the hard rows are selected
+    idx = np.concatenate(idx)
+    pos_base = np.array([5, 6, 700, 8, 9], np.int32)
+    q4, sc, pos = _cache(rows, H, dh)
+    before = [t.cpu().numpy().copy() for t in (q4, sc, pos)]
+    clen = np.asarray(used, np.int32)
+    dodo.gather_kv_q4(K.cuda(), V.cuda(), seq_off, _cuda(idx), nug_off, pos_base, q4, sc, pos, cache_off, clen)
+    torch.cuda.synchronize()
+    assert clen.tolist() == [k + u for k, u in zip(ks, used)]
+    got = [t.cpu().numpy() for t in (q4, sc, pos)]
+    want = [b.copy() for b in before]
+    for b in range(5):
+        rows_b = seq_off[b] + idx[nug_off[b]:nug_off[b + 1]]
+        at = slice(int(cache_off[b]) + used[b], int(cache_off[b]) + used[b] + ks[b])
+        for kv, X in enumerate((K, V)):
+            c, w = plain64.pack(*plain64.quantise(X.float().numpy()[rows_b]))
+            want[0][at, :, kv], want[1][at, :, kv] = c, w
+        want[2][at] = pos_base[b] + idx[nug_off[b]:nug_off[b + 1]]
+    for name, g, w in zip(("steps", "codes", "positions"), (got[1], got[0], got[2]), (want[1], want[0], want[2])):
+        off = np.argwhere(g != w)
+        assert len(off) == 0, (name, len(off), off[:4].tolist(), g[tuple(off[0])], w[tuple(off[0])])
+    # what the codes stand for is at most half a step from the row
+    c, s, m = plain64.quantise(K.float().numpy()[:40])
+    v = plain64.values(*plain64.pack(c, s, m))
+    assert np.all(np.abs(v - K.float().numpy()[:40]) <= np.repeat(s, 32, -1) * 0.5 * (1 + 1e-12))
+
+    # expansion: one rounding to fp32, for bf16 one more; rows that are not in use stay
+    Ke, Ve = torch.full((rows, H, dh), 9.0, dtype=dtype, device="cuda"), torch.full((rows, H, dh), -9.0, dtype=dtype, device="cuda")
+    dodo.expand_kv_q4(q4, sc, cache_off, clen, Ke, Ve)
+    torch.cuda.synchronize()
+    live = np.zeros(rows, bool)
+    for b in range(5):
+        live[cache_off[b]:cache_off[b] + clen[b]] = True
+    for kv, (E, fill) in enumerate(((Ke, 9.0), (Ve, -9.0))):
+        with np.errstate(over="ignore", invalid="ignore"):
+            ref = torch.from_numpy(plain64.values(got[0][:, :, kv], got[1][:, :, kv]).astype(np.float32)).to(dtype)
+        assert torch.equal(torch.isnan(E.cpu()[live]), torch.isnan(ref[live]))
+        assert torch.equal(torch.nan_to_num(E.cpu()[live].float()), torch.nan_to_num(ref[live].float()))
+        assert bool((E.cpu()[~live].float() == fill).all())
+    assert dodo.device_status() == 0
+
+
+def test_gather_q4_appends_many_sequences_and_matches_gather(dodo):
+    # 70 sequences: two launch groups; the cache equals quantising what dodo_gather_kv stores
+    H, dh, B = 2, 64, 70
+    rs = np.random.RandomState(3)
+    lens = [int(x) for x in rs.randint(0, 40, B)]
+    ks = [n // 3 for n in lens]
+    seq_off, nug_off, cache_off = inputs.offsets(lens), inputs.offsets(ks), inputs.offsets([2 * k for k in ks])
+    K, V = (inputs.randn((int(seq_off[-1]), H, dh), "q4many", n, dtype=BF).cuda() for n in "KV")
+    idx = _cuda(np.concatenate([np.sort(rs.permutation(n)[:k]) for n, k in zip(lens, ks)]).astype(np.int32))
+    rows = int(cache_off[-1])
+    q4, sc, pos = _cache(rows, H, dh)
+    cK, cV = torch.zeros((rows, H, dh), dtype=BF, device="cuda"), torch.zeros((rows, H, dh), dtype=BF, device="cuda")
+    cpos = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    cl4, cl = np.zeros(B, np.int32), np.zeros(B, np.int32)
+    for base in (0, 1000):
+        pb = np.full(B, base, np.int32)
+        dodo.gather_kv_q4(K, V, seq_off, idx, nug_off, pb, q4, sc, pos, cache_off, cl4)
+        dodo.gather_kv(K, V, seq_off, idx, nug_off, pb, cK, cV, cpos, cache_off, cl)
+    torch.cuda.synchronize()
+    assert np.array_equal(cl4, cl) and torch.equal(pos, cpos)
+    for kv, X in enumerate((cK, cV)):
+        c, w = plain64.pack(*plain64.quantise(X.float().cpu().numpy()))
+        assert np.array_equal(q4.cpu().numpy()[:, :, kv], c) and np.array_equal(sc.cpu().numpy()[:, :, kv], w)
+
+
+def test_gather_q4_bad_index_is_reported_not_followed(libdodo):
+    ctx = api.Dodo(0)
+    H, dh = 2, 64
+    K = torch.ones((10, H, dh), device="cuda")
+    q4, sc, pos = _cache(4, H, dh)
+    b4, bs = q4.clone(), sc.clone()
+    clen = np.zeros(1, np.int32)
+    ctx.gather_kv_q4(K, K, [0, 10], _cuda(np.array([0, -1, 10, 9], np.int32)), [0, 4], [0], q4, sc, pos, [0, 4], clen)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == api.DEV_BAD_INDEX
+    assert torch.equal(q4[1:3], b4[1:3]) and torch.equal(sc[1:3], bs[1:3]) and pos.tolist() == [0, -7, -7, 9]
+    ctx.reset()
+    assert ctx.device_status() == 0
+    ctx.close()
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2):
+    """A ragged batch over a 4-bit cache; row regions have slack rows that hold NaN groups, the local array NaN rows."""
+    rs = np.random.RandomState(inputs.seed_for(tag) % 2 ** 32)
+    B = len(tqs)
+    p = dict(B=B, H=H, dh=dh, dtype=dtype, scale=dh ** -0.5)
+    p["q_off"], p["cache_off"] = inputs.offsets(tqs), inputs.offsets([c + slack for c in clens])
+    p["clen"], p["llen"] = np.asarray(clens, np.int32), np.asarray(llens, np.int32)
+    p["loc_off"] = inputs.offsets([n + slack for n in llens])[:-1].copy()
+    rows, lrows = int(p["cache_off"][-1]), int(sum(n + slack for n in llens))
+    span = [5 * c + 3 for c in clens]
+    p["loc_pos0"] = np.asarray(span, np.int32)
+    p["q_pos0"] = np.asarray([s // 2 - 2 if inside else s + n - t for s, n, t in zip(span, llens, tqs)], np.int32)
+    cpos = np.full(rows, 0, np.int32)
+    kv = [rs.standard_normal((rows, H, dh)), 2.0 * rs.standard_normal((rows, H, dh))]
+    packed = [plain64.pack(*plain64.quantise(np.asarray(torch.from_numpy(x).float().to(dtype).float().numpy()))) for x in kv]
+    codes, words = np.stack([packed[0][0], packed[1][0]], 2), np.stack([packed[0][1], packed[1][1]], 2)
+    loc = [torch.from_numpy(rs.standard_normal((lrows, H, dh))).to(dtype) for _ in range(2)]
+    live_l = np.zeros(lrows, bool)
+    for b in range(B):
+        c0 = int(p["cache_off"][b])
+        cpos[c0:c0 + clens[b]] = np.sort(rs.permutation(span[b])[:clens[b]])
+        words[c0 + clens[b]:int(p["cache_off"][b + 1])] = 0x7fc07fc0
+        live_l[p["loc_off"][b]:p["loc_off"][b] + llens[b]] = True
+    for t in loc:
+        t[torch.from_numpy(~live_l)] = float("nan")
+    p["codes"], p["words"], p["cpos"], p["loc"] = codes, words, cpos, loc
+    p["Q"] = torch.from_numpy(rs.standard_normal((int(p["q_off"][-1]), H, dh))).to(dtype)
+    return p
+
+
+def _run_q4(dodo, p, workspace=None, lse=True, stream=None):
+    d = dict(O=torch.full(p["Q"].shape, float("nan"), dtype=p["dtype"], device="cuda"),
+             lse=torch.full(p["Q"].shape[:2], float("nan"), device="cuda") if lse else None)
+    if workspace is None:
+        workspace = torch.empty(dodo.attend_q4_workspace_bytes(p["H"], p["dh"], p["codes"].shape[0]), dtype=torch.uint8, device="cuda")
+    dodo.attend_q4(p["Q"].cuda(), p["q_off"], p["q_pos0"], p["scale"], _cuda(p["codes"]), _cuda(p["words"]), _cuda(p["cpos"]),
+                   p["cache_off"], p["clen"], p["loc"][0].cuda(), p["loc"][1].cuda(), p["loc_off"], p["llen"], p["loc_pos0"],
+                   d["O"], d["lse"], workspace)
+    torch.cuda.synchronize()
+    return d["O"], d["lse"]
+
+
+def _reference(p, rounded=False):
+    """O, lse and the bounds on their errors, sequence by sequence."""
+    K, V = plain64.values(p["codes"][:, :, 0], p["words"][:, :, 0]), plain64.values(p["codes"][:, :, 1], p["words"][:, :, 1])
+    low = np.repeat((p["words"][:, :, 0].view(np.uint32) & 0xffff0000).astype(np.uint32).view(np.float32).astype(np.float64), 32, -1)
+    Q, lK, lV = _f64(p["Q"]), _f64(p["loc"][0]), _f64(p["loc"][1])
+    O, lse, tO, tL = np.zeros(Q.shape), np.zeros(Q.shape[:2]), np.zeros(Q.shape), np.zeros(Q.shape[:2])
+    half = plain64.HALF["bf16" if p["dtype"] == BF else "f32"]
+    for b in range(p["B"]):
+        q, c = slice(int(p["q_off"][b]), int(p["q_off"][b + 1])), slice(int(p["cache_off"][b]), int(p["cache_off"][b]) + int(p["clen"][b]))
+        l = slice(int(p["loc_off"][b]), int(p["loc_off"][b]) + int(p["llen"][b]))
+        k, v = np.concatenate([K[c], lK[l]]), np.concatenate([V[c], lV[l]])
+        kpos = np.concatenate([p["cpos"][c], p["loc_pos0"][b] + np.arange(p["llen"][b])])
+        qpos = p["q_pos0"][b] + np.arange(q.stop - q.start)
+        O[q], lse[q] = plain64.attend(Q[q], qpos, p["scale"], k, v, kpos)
+        if not len(k) or q.stop == q.start:
+            continue
+        d = plain64.logit_bound(Q[q], k, p["scale"], p["dh"], np.concatenate([low[c], np.zeros_like(lK[l])]))
+        extra = 0.0
+        if rounded:     # keys and values rounded to bf16, weights rounded to bf16: each off by at most 2^-8 of itself
+            d += 2.0 ** -8 * abs(p["scale"]) * max(float(np.max(np.abs(Q[q][:, h]) @ np.abs(k[:, h]).T)) for h in range(p["H"]))
+            extra = 2.0 ** -8 + 2.0 ** -8
+        w = 2.0 * d + extra + 2.0 ** -20 + len(k) * 2.0 ** -24     # relative error of a weight: its logit's, the exponential's, the sum's
+        tO[q] = half * np.abs(O[q]) + w * np.max(np.abs(v))
+        tL[q] = d + 2.0 ** -20 + len(k) * 2.0 ** -24 + 2.0 ** -22 * np.abs(np.where(np.isfinite(lse[q]), lse[q], 0.0))
+    return O, lse, tO, tL
+
+
+def _check(p, O, lse, rounded=False):
+    rO, rL, tO, tL = _reference(p, rounded)
+    gO = _f64(O)
+    assert np.all(np.isfinite(gO))
+    assert np.all(np.abs(gO - rO) <= tO), float(np.max(np.abs(gO - rO) - tO))
+    if lse is not None:
+        gL = _f64(lse)
+        empty = np.isneginf(rL)
+        assert np.array_equal(np.isneginf(gL), empty)
+        assert np.all(np.abs(gL[~empty] - rL[~empty]) <= tL[~empty])
+        assert np.all(gO[empty] == 0.0)
+
+
+SHAPES = [
+    # dtype, H, dh, query tokens, cached rows, local rows
+    (BF, 32, 128, [1] * 8, [205] * 8, [64] * 8),
+    (BF, 2, 128, [1, 1, 1, 1, 1], [0, 1, 63, 129, 1000], [1, 0, 65, 7, 130]),
+    (F32, 3, 64, [1, 1, 1], [700, 5, 0], [64, 1, 33]),
+    (F32, 2, 128, [2, 1, 2], [33, 300, 64], [2, 9, 70]),
+    (BF, 3, 64, [3, 4, 1, 0, 2], [257, 31, 8, 40, 0], [5, 4, 1, 3, 66]),
+    (F32, 4, 64, [16], [52], [16]),
+    (BF, 1, 128, [7], [4097], [100]),
+    (BF, 40, 128, [1], [3277], [64]),
+    (BF, 5, 64, [13, 31], [100, 900], [31, 40]),
+]
+
+
+@pytest.mark.parametrize("inside", [False, True])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_attend_q4_against_plain(dodo, case, inside):
+    dtype, H, dh, tqs, cl, ll = SHAPES[case]
+    p = _problem(("q4a", case, inside), dtype, H, dh, tqs, cl, ll, inside)
+    O, lse = _run_q4(dodo, p)
+    _check(p, O, lse)
+    O2, lse2 = _run_q4(dodo, p)                      # bit for bit the same again
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    O3, _ = _run_q4(dodo, p, lse=False)
+    assert torch.equal(O, O3)
+    assert dodo.device_status() == 0
+
+
+def test_attend_q4_split_targets(libdodo):
+    ctx = api.Dodo(0)
+    p = _problem("q4split", BF, 3, 128, [1, 1, 2], [2000, 37, 500], [70, 0, 3])
+    for target in (1, 7, 64, 4096):
+        ctx.set_tuning(api.TUNE_ATTEND_TARGET_BLOCKS, target)
+        _check(p, *_run_q4(ctx, p))
+    ctx.close()
+
+
+def test_attend_q4_masked_nan_rows_do_not_count(dodo):
+    # cached rows ahead of the queries hold NaN, in the middle of the list and at its end
+    p = _problem("q4nan", BF, 2, 128, [1, 2], [300, 90], [5, 2], inside=True)
+    for b in range(2):
+        c0, n = int(p["cache_off"][b]), int(p["clen"][b])
+        hidden = c0 + np.flatnonzero(p["cpos"][c0:c0 + n] > p["q_pos0"][b] + 1)
+        assert len(hidden) > 10
+        p["words"][hidden] = np.array(0x7fc07fc0, np.uint32).view(np.int32)
+    for t in p["loc"]:
+        t.fill_(float("nan"))
+    O, lse = _run_q4(dodo, p)
+    q = dict(p)
+    q["words"] = np.where(p["words"] == 0x7fc07fc0, 0, p["words"])
+    q["loc"] = [torch.zeros_like(t) for t in p["loc"]]
+    _check(q, O, lse)
+
+
+def test_attend_q4_visible_nan_shows(dodo):
+    p = _problem("q4vis", F32, 2, 64, [1], [40], [3])
+    p["words"][7, 1, 0] = 0x7fc07fc0
+    O, lse = _run_q4(dodo, p)
+    assert bool(torch.isnan(O[0, 1]).all()) and bool(torch.isnan(lse[0, 1]))
+    assert bool(torch.isfinite(O[0, 0]).all())
+
+
+@pytest.mark.parametrize("inside", [False, True])
+def test_attend_q4_query_block_on_tensor_cores(dodo, inside):
+    p = _problem(("q4block", inside), BF, 3, 128, [130, 32, 1], [333, 64, 0], [200, 40, 70], inside)
+    rows = p["codes"].shape[0]
+    need = dodo.attend_q4_workspace_bytes(3, 128, rows)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    O, lse = _run_q4(dodo, p, ws)
+    _check(p, O, lse, rounded=True)
+    # one byte less: the streaming kernel, whose values are not rounded
+    Os, ls = _run_q4(dodo, p, ws[:need - 1])
+    _check(p, Os, ls)
+
+
+def test_attend_q4_without_cache_or_locals(dodo):
+    p = _problem("q4none", BF, 2, 128, [1, 3], [50, 9], [0, 0])
+    _check(p, *_run_q4(dodo, p))
+    # no cache at all: equal to the plain form over the local tokens
+    p = _problem("q4noc", F32, 2, 64, [1, 2], [0, 0], [9, 70], slack=0)
+    O = torch.empty(p["Q"].shape, device="cuda")
+    lse = torch.empty(p["Q"].shape[:2], device="cuda")
+    dodo.attend_q4(p["Q"].cuda(), p["q_off"], p["q_pos0"], p["scale"], None, None, None, None, None, p["loc"][0].cuda(),
+                   p["loc"][1].cuda(), p["loc_off"], p["llen"], p["loc_pos0"], O, lse, None)
+    torch.cuda.synchronize()
+    _check(p, O, lse)
+
+
+def test_q4_cache_as_a_server_uses_it(dodo, oracle):
+    """Compress, append to the 4-bit cache, decode; append more; decode; in a captured graph and on another stream."""
+    H, dh, d, r = 4, 128, 512, 10
+    B, n = 3, [300, 77, 512]
+    seq_off = inputs.offsets(n)
+    ks = [dodo.num_nuggets(m, r) for m in n]
+    nug_off, cache_off = inputs.offsets(ks), inputs.offsets([2 * k for k in ks])
+    X = inputs.randn((int(seq_off[-1]), d), "q4srv", "X", dtype=BF).cuda()
+    w = inputs.randn((d,), "q4srv", "w", std=d ** -0.5, dtype=BF).cuda()
+    K, V = (inputs.randn((int(seq_off[-1]), H, dh), "q4srv", k, dtype=BF).cuda() for k in "KV")
+    lK, lV = (inputs.randn((B * 8, H, dh), "q4srv", "l" + k, dtype=BF).cuda() for k in "KV")
+    Q = inputs.randn((B, H, dh), "q4srv", "Q", dtype=BF).cuda()
+    scores, idx = torch.empty(int(seq_off[-1]), device="cuda"), torch.empty(int(nug_off[-1]), dtype=torch.int32, device="cuda")
+    rows = int(cache_off[-1])
+    ws = torch.empty(dodo.attend_q4_workspace_bytes(H, dh, rows), dtype=torch.uint8, device="cuda")
+
+    def steps(q4, sc, pos, outs):
+        clen = np.zeros(B, np.int32)
+        for part in range(2):
+            dodo.score_select(X, w, 0.0, seq_off, nug_off, 0, scores, idx)
+            dodo.gather_kv_q4(K, V, seq_off, idx, nug_off, np.full(B, 1000 * part, np.int32), q4, sc, pos, cache_off, clen)
+            for step in range(2):
+                dodo.attend_q4(Q, np.arange(B + 1), np.full(B, 5000 + step, np.int32), dh ** -0.5, q4, sc, pos, cache_off, clen, lK, lV,
+                               8 * np.arange(B), np.full(B, 8), np.full(B, 4995), outs[2 * part + step], None, ws)
+        return clen
+
+    def fresh():
+        return _cache(rows, H, dh, 0), [torch.full(Q.shape, float("nan"), dtype=BF, device="cuda") for _ in range(4)]
+
+    (q4, sc, pos), outs = fresh()
+    clen = steps(q4, sc, pos, outs)
+    torch.cuda.synchronize()
+    assert clen.tolist() == [2 * k for k in ks]
+    for b in range(B):
+        for part in range(2):
+            sel = idx[nug_off[b]:nug_off[b + 1]].long() + int(seq_off[b])
+            at = slice(int(cache_off[b]) + part * ks[b], int(cache_off[b]) + (part + 1) * ks[b])
+            for kv, T in enumerate((K, V)):
+                c, wd = plain64.pack(*plain64.quantise(T[sel].float().cpu().numpy()))
+                assert np.array_equal(q4[at, :, kv].cpu().numpy(), c) and np.array_equal(sc[at, :, kv].cpu().numpy(), wd)
+    for part in range(2):
+        for step in range(2):
+            p = dict(B=B, H=H, dh=dh, dtype=BF, scale=dh ** -0.5, q_off=np.arange(B + 1), q_pos0=np.full(B, 5000 + step), Q=Q.cpu(),
+                     codes=q4.cpu().numpy(), words=sc.cpu().numpy(), cpos=pos.cpu().numpy(), cache_off=cache_off,
+                     clen=np.asarray([(part + 1) * k for k in ks]), loc=[lK.cpu(), lV.cpu()], loc_off=8 * np.arange(B),
+                     llen=np.full(B, 8), loc_pos0=np.full(B, 4995))
+            _check(p, outs[2 * part + step], None)
+
+    # captured, replayed twice (the append is part of the graph), on a stream of its own
+    (g4, gs, gp), gouts = fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        steps(g4, gs, gp, gouts)
+    for _ in range(2):
+        for t in gouts:
+            t.fill_(float("nan"))
+        g4.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(g4, q4) and torch.equal(gs, sc) and torch.equal(gp, pos)
+        assert all(torch.equal(a, b) for a, b in zip(gouts, outs))
+    assert dodo.device_status() == 0
+
+
+def test_q4_binding_refuses_wrong_tensors(dodo):
+    q4, sc, pos = _cache(4, 2, 64)
+    K = torch.zeros((4, 2, 64), device="cuda")
+    idx = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = lambda **k: {**dict(K=K, V=K, seq_off=[0, 4], idx=idx, nug_off=[0, 1], pos_base=[0], cache_q4=q4, cache_scale=sc,  # noqa: E731
+                               cache_pos=pos, cache_off=[0, 4], cache_len=np.zeros(1, np.int32)), **k}
+    for bad, kind in ((dict(V=K.bfloat16()), TypeError), (dict(idx=idx.long()), TypeError), (dict(cache_q4=q4.int()), TypeError),
+                      (dict(cache_scale=sc[:, :, :, :1]), ValueError), (dict(K=K.cpu()), ValueError), (dict(V=K[:3]), ValueError),
+                      (dict(seq_off=[0, 5]), ValueError), (dict(nug_off=[0, 2]), ValueError), (dict(cache_off=[0, 5]), ValueError),
+                      (dict(cache_len=[0]), TypeError), (dict(K=K.transpose(0, 1)), ValueError), (dict(pos_base=[]), ValueError)):
+        with pytest.raises(kind):
+            dodo.gather_kv_q4(**args(**bad))
+    with pytest.raises(api.DodoError) as e:
+        dodo.gather_kv_q4(**args(cache_len=np.full(1, 4, np.int32)))
+    assert e.value.status == api.ERR_CAPACITY
