@@ -330,6 +330,38 @@ DODO_API int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_
                         int loc_rows, int B, void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Gradient of dodo_attend (training; the paper's Eq. 3/4/9/13 differentiated, its scores by Eq. 16-18).  With the forward
+ * call's tables, inputs, O and lse, and the gradient dO that arrives at O, for every visible (query i, key j) of a head
+ *   x = sm_scale q_i.k_j,  P = exp(x - lse_i),  D_i = sum(dO_i * O_i),  dS = P (dO_i.v_j - D_i)
+ *   dQ_i = sm_scale sum_j dS k_j,   dK_j = sm_scale sum_i dS q_i,   dV_j = sum_i P dO_i
+ *   dscore_j = sum over queries and heads of dS, for nuggets: the straight-through gradient of their scores
+ *              (Eq. 18 adds s_j - StopGrad(s_j) to every logit x of nugget j)
+ * fp32 arithmetic, one rounding of each result to `dtype`; on the tensor cores P and dS are rounded to bf16 on the way.
+ *   O, lse      [device] what dodo_attend wrote for these inputs (lse is required)
+ *   dO          [device] [q_off[B], H, dh] in `dtype`, 16-byte aligned
+ *   dQ          [device] like Q, written
+ *   dcacheK/V   [device] like cacheK/V: rows in use (r < cache_len[b] of each region) are written, others left as they were
+ *   dlocK/V     [device] like locK/V: the rows of the sequences' windows are written, others left as they were.  Windows
+ *               must not share rows (DODO_ERR_INVALID_ARG)
+ *   dscore      [device] float[cache_off[B]], rows in use written; or NULL
+ *   workspace   [device] at least dodo_attend_backward_workspace_bytes(ctx, q_off[B], H, dh, cache_off[B]) bytes, 16-byte
+ *               aligned
+ *   everything else as in dodo_attend
+ * Written rows are overwritten, not added to; keys that no query sees and queries that see no key get zeros.  Outputs must
+ * not overlap inputs or each other.  Results repeat bit for bit.  A nugget's gradient is that of the cache row:
+ * the row of K and V that it was gathered from has the same one.  Queries, O and dO must be finite; a row of K or V that a
+ * query does not see does not reach that query's gradient, whatever it holds.
+ * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.
+ */
+DODO_API size_t dodo_attend_backward_workspace_bytes(const dodo_ctx* ctx, int q_rows, int H, int dh, int cache_rows);
+DODO_API int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H,
+                         int dh, float sm_scale, const void* cacheK, const void* cacheV, const int32_t* cache_pos,
+                         const int32_t* cache_off, const int32_t* cache_len, const void* locK, const void* locV,
+                         const int32_t* loc_off, const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B,
+                         const void* O, const float* lse, const void* dO, void* dQ, void* dcacheK, void* dcacheV,
+                         void* dlocK, void* dlocV, float* dscore, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Nugget cache held in 4 bits.  dodo_gather_kv_q4 is dodo_gather_kv into such a cache: the same tables, append and
  * bookkeeping, the selected rows quantised on the way.  A row of one head is cut into groups of DODO_Q4_GROUP features;
  * with lo and hi a group's least and largest value

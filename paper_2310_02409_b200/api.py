@@ -53,6 +53,9 @@ SIGNATURES = {
                          _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "dodo_attend_indexed": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                  _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "dodo_attend_backward_workspace_bytes": (_sz, [_vp, _i, _i, _i, _i]),
+    "dodo_attend_backward": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i,
+                                  _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dodo_gather_kv_q4": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
     "dodo_expand_kv_q4": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _i, _i, _vp, _vp, _vp]),
     "dodo_attend_q4_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
@@ -319,6 +322,43 @@ class Dodo:
                                           _dev(cacheK), _dev(cacheV), _dev(cache_pos), _hp(co), _hp(cl),
                                           _dev(locK), _dev(locV), _hp(lo), _hp(ll), _hp(lp), loc_rows,
                                           len(qo) - 1, _dev(O), _dev(lse), _dev(workspace), ws_bytes, _stream()))
+
+    # -- the gradient of attend --------------------------------------------------------------------
+    def attend_backward_workspace_bytes(self, q_rows: int, H: int, dh: int, cache_rows: int) -> int:
+        return int(self._lib.dodo_attend_backward_workspace_bytes(self._ctx, int(q_rows), int(H), int(dh), int(cache_rows)))
+
+    def attend_backward(self, Q, q_off, q_pos0, sm_scale, cacheK, cacheV, cache_pos, cache_off, cache_len,
+                        locK, locV, loc_off, loc_len, loc_pos0, O, lse, dO, dQ, dcacheK, dcacheV, dlocK, dlocV, dscore, workspace):
+        """``dodo_attend_backward``: gradients of ``attend`` from its inputs, ``O``, ``lse`` and ``dO``; ``dscore`` (float, one
+        entry a cache row) may be None, and the cache's or the local tokens' tensors where the call has none."""
+        qo, qp = _host_i32(q_off), _host_i32(q_pos0)
+        co, cl = _host_i32(cache_off), _host_i32(cache_len)
+        lo, ll, lp = _host_i32(loc_off), _host_i32(loc_len), _host_i32(loc_pos0)
+        H, dh = Q.shape[-2], Q.shape[-1]
+        code, B, dt = _dtype_code(Q), len(qo) - 1, Q.dtype
+        loc_rows = 0 if locK is None else locK.shape[0]
+        like = lambda t: None if t is None else t.shape  # noqa: E731
+        _on(self.device, {"Q": (Q, None), "O": (O, Q.shape), "dO": (dO, Q.shape), "dQ": (dQ, Q.shape), "lse": (lse, Q.shape[:2]),
+                          "cacheK": (cacheK, None), "cacheV": (cacheV, like(cacheK)), "dcacheK": (dcacheK, like(cacheK)),
+                          "dcacheV": (dcacheV, like(cacheK)), "cache_pos": (cache_pos, None), "locK": (locK, None),
+                          "locV": (locV, like(locK)), "dlocK": (dlocK, like(locK)), "dlocV": (dlocV, like(locK)),
+                          "dscore": (dscore, None), "workspace": (workspace, None)},
+            {**{n: dt for n in ("Q", "O", "dO", "dQ", "cacheK", "cacheV", "dcacheK", "dcacheV", "locK", "locV", "dlocK", "dlocV")},
+             "lse": torch.float32, "dscore": torch.float32, "cache_pos": torch.int32, "workspace": workspace.dtype})
+        self._regions(Q.shape[0], qo, qp, "q_off")
+        if cacheK is not None:
+            rows = min(cacheK.shape[0], cache_pos.numel(), cacheK.shape[0] if dscore is None else dscore.numel())
+            self._regions(rows, co, cl)
+            if len(co) != B + 1 or tuple(cacheK.shape[1:]) != (H, dh):
+                raise ValueError("cache_off must describe the same sequences as q_off, cacheK and cacheV [rows, H, dh]")
+        if locK is not None and not (len(lo) >= B and len(ll) >= B and len(lp) >= B and tuple(locK.shape[1:]) == (H, dh)):
+            raise ValueError("loc_off, loc_len and loc_pos0 must have one entry a sequence, locK and locV [rows, H, dh]")
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._check(self._lib.dodo_attend_backward(
+            self._ctx, ptr(Q), _hp(qo), _hp(qp), code, H, dh, float(sm_scale), ptr(cacheK), ptr(cacheV), ptr(cache_pos), _hp(co),
+            _hp(cl), ptr(locK), ptr(locV), _hp(lo), _hp(ll), _hp(lp), loc_rows, B, ptr(O), ptr(lse), ptr(dO), ptr(dQ), ptr(dcacheK),
+            ptr(dcacheV), ptr(dlocK), ptr(dlocV), ptr(dscore), ptr(workspace), workspace.numel() * workspace.element_size(),
+            _stream()))
 
     # -- the 4-bit nugget cache ----------------------------------------------------------------------
     def _q4_cache(self, cache_q4, cache_scale, H, dh, more=(), dtypes=None):

@@ -1,0 +1,560 @@
+// Gradient of attention over [nugget cache ; local tokens].  With x = scale q.k (the softmax's argument) on visible
+// (query, key) pairs, and the forward's output O and log-sum-exp at hand,
+//   P = exp(x - lse),  D = sum(dO * O) per query,  dP = dO . V,  dS = P (dP - D)
+//   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dscore_j = sum over queries and heads of dS_j
+// The probabilities are recomputed, nothing of size queries x keys is stored.  dscore is the straight-through gradient
+// (Eq. 16-18): the paper adds s_j - StopGrad(s_j) to every logit of nugget j, so what reaches its score is the sum of
+// the gradients at its logits.  Every output row is summed by one owner in a fixed order (no atomics): results repeat
+// bit for bit.
+//
+// Two kernels here, a third (bf16, head size 128, blocks of queries) on the tensor cores in attend_backward_dense.cu:
+//   backward_stream_kernel  up to four queries per sequence (single-token steps).  All traffic, no reuse: one pass reads
+//       K and V once, writes dK and dV once and sums dQ, the queries and their dQ in registers.
+//   backward_tile_kernel    everything else (fp32, head size 64): key blocks and query blocks side by side in one launch,
+//       64 keys x 32 queries at a time in shared memory, fp32 FMAs on register tiles.
+#include "dodo_internal.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T> __device__ __forceinline__ uint4 pack16(const float* f);
+template <> __device__ __forceinline__ uint4 pack16<float>(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
+    return make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
+}
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                       __uint_as_float(v.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(two_bf16(v.x, v.y), two_bf16(v.z, v.w));
+}
+// a query's statistic: log-sum-exp in base 2, +inf (every weight comes out 0) where the query sees nothing
+__device__ __forceinline__ float lse_base2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// One more of `n` arrivals on a counter that is zero between launches; true for the last, which finds the others' writes
+// visible.  All threads of the block call it.
+__device__ __forceinline__ bool last_arrival(int* counter, int n, int* flag) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int t = atomicAdd(counter, 1);
+        *flag = t == n - 1;
+        if (t == n - 1) *counter = 0;
+    }
+    __syncthreads();
+    const bool last = *flag != 0;
+    if (last) __threadfence();
+    __syncthreads();
+    return last;
+}
+
+// Gradient of the scores of cache rows [row, row + n): the heads' sums added up in head order by the last head to arrive.
+__device__ __forceinline__ void finish_scores(const BackwardArrays& a, int H, int row, int n, int* counter, int* flag) {
+    if (!last_arrival(counter, H, flag)) return;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        float s = 0.f;
+        for (int h = 0; h < H; ++h) s += __ldcg(a.score_part + static_cast<size_t>(h) * a.score_rows + row + i);
+        a.dscore[row + i] = s;
+    }
+}
+
+// =============================================== up to four queries =====================================================
+template <typename T, int DH, int QT, int U>
+__global__ void __launch_bounds__(kThreads)
+backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
+    constexpr int E = Vec16<T>::kElems, LPR = DH / E, NB = kThreads / LPR;
+    __shared__ float red[NB][DH + 4];
+    __shared__ int s_flag;
+    const int tid = threadIdx.x, bundle = tid / LPR, lig = tid % LPR;
+    int b = 0;
+    for (int i = 1; i < g.nseq; ++i) b += g.seq[i].kv0 <= static_cast<int>(blockIdx.x) ? 1 : 0;
+    const BackwardSeq sq = g.seq[b];
+    const int r = static_cast<int>(blockIdx.x) - sq.kv0;
+    const int chunk = r % sq.nchunk, h = r / sq.nchunk;
+    const int n_keys = sq.c_len + sq.l_len;
+    const int k0 = min(n_keys, chunk * sq.ctiles * NB), k1 = min(n_keys, k0 + sq.ctiles * NB);
+    const size_t row_elems = static_cast<size_t>(H) * DH;
+    const size_t col = static_cast<size_t>(h) * DH + lig * E;
+    dodo_grid_dependency_sync();
+
+    float q[QT][E], go[QT][E], dq[QT][E], lse2[QT], delta[QT];
+    int qpos[QT];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        float o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[i][e] = go[i][e] = o[e] = dq[i][e] = 0.f;
+        lse2[i] = INFINITY;
+        qpos[i] = static_cast<int>(0x80000000);
+        if (i < sq.tq) {
+            const size_t at = static_cast<size_t>(sq.q_row0 + i) * row_elems + col;
+            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.Q) + at), q[i]);
+            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.dO) + at), go[i]);
+            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.O) + at), o);
+            lse2[i] = lse_base2(a.lse[static_cast<size_t>(sq.q_row0 + i) * H + h]);
+            qpos[i] = sq.q_pos0 + i;
+        }
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) d = fmaf(go[i][e], o[e], d);
+#pragma unroll
+        for (int s = LPR / 2; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
+        delta[i] = d;
+    }
+    const float scale2 = scale * kLog2e;
+
+    uint4 kv[U], vv[U];
+    int kpos[U];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = base + u * NB + bundle;
+            kv[u] = vv[u] = make_uint4(0, 0, 0, 0);
+            kpos[u] = 0x7fffffff;
+            if (j < k1) {
+                const bool cached = j < sq.c_len;
+                const int row = cached ? sq.c_row0 + j : sq.l_row0 + (j - sq.c_len);
+                const size_t at = static_cast<size_t>(row) * row_elems + col;
+                kv[u] = ld_stream16(static_cast<const T*>(cached ? a.cK : a.lK) + at);
+                vv[u] = ld_stream16(static_cast<const T*>(cached ? a.cV : a.lV) + at);
+                kpos[u] = cached ? __ldg(a.cache_pos + row) : sq.l_pos0 + (j - sq.c_len);
+            }
+        }
+    };
+    load(k0);
+    for (int base = k0; base < k1; base += NB * U) {
+        uint4 kc[U], vc[U];
+        int pc[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) { kc[u] = kv[u]; vc[u] = vv[u]; pc[u] = kpos[u]; }
+        load(base + NB * U);
+        // logits and dP of the batch; the sums over a row's lanes for all keys and queries together
+        float s[QT][U], t[QT][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float k[E], v[E];
+            Vec16<T>::unpack(kc[u], k);
+            Vec16<T>::unpack(vc[u], v);
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                float2 x = make_float2(0.f, 0.f), y = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    x = __ffma2_rn(make_float2(q[i][e], q[i][e + 1]), make_float2(k[e], k[e + 1]), x);
+                    y = __ffma2_rn(make_float2(go[i][e], go[i][e + 1]), make_float2(v[e], v[e + 1]), y);
+                }
+                s[i][u] = x.x + x.y;
+                t[i][u] = y.x + y.y;
+            }
+        }
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    s[i][u] += __shfl_xor_sync(0xffffffffu, s[i][u], o);
+                    t[i][u] += __shfl_xor_sync(0xffffffffu, t[i][u], o);
+                }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = base + u * NB + bundle;
+            float k[E], dk[E], dv[E], ds_sum = 0.f;
+            Vec16<T>::unpack(kc[u], k);
+#pragma unroll
+            for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                const bool see = pc[u] <= qpos[i];       // a masked key takes no part, whatever its row holds
+                const float p = see ? ex2_approx(fmaf(s[i][u], scale2, -lse2[i])) : 0.f;
+                const float ds = see ? p * (t[i][u] - delta[i]) : 0.f;
+                ds_sum += ds;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    dk[e] = fmaf(ds, q[i][e], dk[e]);
+                    dv[e] = fmaf(p, go[i][e], dv[e]);
+                    dq[i][e] = see ? fmaf(ds, k[e], dq[i][e]) : dq[i][e];
+                }
+            }
+            if (j < k1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) dk[e] *= scale;
+                const bool cached = j < sq.c_len;
+                const int row = cached ? sq.c_row0 + j : sq.l_row0 + (j - sq.c_len);
+                const size_t at = static_cast<size_t>(row) * row_elems + col;
+                *reinterpret_cast<uint4*>(static_cast<T*>(cached ? a.dcK : a.dlK) + at) = pack16<T>(dk);
+                *reinterpret_cast<uint4*>(static_cast<T*>(cached ? a.dcV : a.dlV) + at) = pack16<T>(dv);
+                if (cached && a.dscore != nullptr && lig == 0) a.score_part[static_cast<size_t>(h) * a.score_rows + row] = ds_sum;
+            }
+        }
+    }
+
+    // ---- dQ: the bundles' sums, then the chunks' --------------------------------------------------------------
+#pragma unroll 1
+    for (int i = 0; i < QT; ++i) {
+        if (i >= sq.tq) break;
+        float mine[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            mine[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < QT; ++k) mine[e] = k == i ? dq[k][e] : mine[e];
+            red[bundle][lig * E + e] = mine[e];
+        }
+        __syncthreads();
+        if (tid < DH) {
+            float sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) sum += red[n][tid];
+            if (sq.nchunk == 1) {
+                const float v = sum * scale;
+                T* out = static_cast<T*>(a.dQ) + static_cast<size_t>(sq.q_row0 + i) * row_elems + static_cast<size_t>(h) * DH + tid;
+                if constexpr (sizeof(T) == 4) *out = v; else *out = __float2bfloat16_rn(v);
+            } else {
+                a.dq_part[(static_cast<size_t>(sq.part0 + h * sq.nchunk + chunk) * QT + i) * DH + tid] = sum;
+            }
+        }
+        __syncthreads();
+    }
+    // cache rows of this chunk: their score gradients, once every head has been here
+    const int c1 = min(sq.c_len, k1);
+    if (a.dscore != nullptr && k0 < c1) finish_scores(a, H, sq.c_row0 + k0, c1 - k0, a.tickets + sq.stick0 + chunk, &s_flag);
+    if (sq.nchunk > 1 && sq.tq > 0 && last_arrival(a.tickets + sq.qtick0 + h, sq.nchunk, &s_flag)) {
+        for (int i = tid; i < sq.tq * DH; i += kThreads) {
+            float sum = 0.f;
+            for (int c = 0; c < sq.nchunk; ++c)
+                sum += __ldcg(a.dq_part + (static_cast<size_t>(sq.part0 + h * sq.nchunk + c) * QT + i / DH) * DH + i % DH);
+            const float v = sum * scale;
+            T* out = static_cast<T*>(a.dQ) + static_cast<size_t>(sq.q_row0 + i / DH) * row_elems + static_cast<size_t>(h) * DH + i % DH;
+            if constexpr (sizeof(T) == 4) *out = v; else *out = __float2bfloat16_rn(v);
+        }
+    }
+}
+
+// =============================================== statistics =============================================================
+// (log-sum-exp in base 2, sum of dO * O) of every query, one row per head so that a tile's entries are contiguous; entries
+// behind a sequence's last query, up to a multiple of 64, are (+inf, 0): such a column's weights come out 0.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, int DH) {
+    constexpr int E = Vec16<T>::kElems;
+    const int lpr = DH / E;                             // lanes per row: 8, 16 or 32
+    const int per_block = kThreads / lpr;
+    const long long unit = static_cast<long long>(blockIdx.x) * per_block + threadIdx.x / lpr;   // (entry, head), heads fastest
+    const int entry = static_cast<int>(unit / H), h = static_cast<int>(unit % H), lig = threadIdx.x % lpr;
+    int b = 0;
+    for (int i = 1; i < g.nseq; ++i) b += g.seq[i].stat0 <= entry ? 1 : 0;
+    const int q = entry - g.seq[b].stat0;
+    dodo_grid_dependency_sync();
+    const bool live = entry < g.stat_rows && q < g.seq[b].tq;
+    float d = 0.f;
+    const size_t row = static_cast<size_t>(g.seq[b].q_row0 + q) * H + h;
+    if (live) {
+        float x[E], y[E];
+        Vec16<T>::unpack(ld_stream16(static_cast<const T*>(a.dO) + row * DH + lig * E), x);
+        Vec16<T>::unpack(ld_stream16(static_cast<const T*>(a.O) + row * DH + lig * E), y);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d = fmaf(x[e], y[e], d);
+    }
+    for (int s = lpr / 2; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
+    if (entry < g.stat_rows && lig == 0)
+        a.stats[static_cast<size_t>(h) * g.stat_rows + entry] = live ? make_float2(lse_base2(a.lse[row]), d) : make_float2(INFINITY, 0.f);
+}
+
+// =============================================== fp32 tiles ==============================================================
+constexpr int TK = 64, TQ = 32;     // keys and queries of a tile
+constexpr int LDP = TK + 4;         // row of the weight tiles
+
+template <int DH> struct TileSmem {
+    static constexpr int LD = DH + 4;   // rows 4 banks apart: eight rows' 16-byte pieces cover all banks
+    float K[TK][LD], V[TK][LD], Q[TQ][LD], G[TQ][LD];
+    float P[TQ][LDP], S[TQ][LDP];       // weights and dS, [query][key]
+    float2 stat[TQ];
+    int kpos[TK];
+    int flag;
+};
+
+template <typename T, int DH>
+__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const T* src, size_t row_elems, int row0, int rows, int n) {
+    constexpr int V4 = DH / 4;
+    for (int i = threadIdx.x; i < n * V4; i += kThreads) {
+        const int r = i / V4, c = i % V4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows) v = load4(src + static_cast<size_t>(row0 + r) * row_elems + 4 * c);
+        *reinterpret_cast<float4*>(&dst[r][4 * c]) = v;
+    }
+}
+// dot products of a 4-key x 2-query register tile, over all features, of (K, Q) and (V, dO)
+template <int DH>
+__device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0, float scale2) {
+    const int tk = threadIdx.x % 16, tq = threadIdx.x / 16;     // keys tk + 16 i, queries tq + 16 i
+    float s[4][2], t[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) s[i][j] = t[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DH; c += 4) {
+        float4 k[4], v[4], q[2], o[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            k[i] = *reinterpret_cast<const float4*>(&sm.K[tk + 16 * i][c]);
+            v[i] = *reinterpret_cast<const float4*>(&sm.V[tk + 16 * i][c]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            q[j] = *reinterpret_cast<const float4*>(&sm.Q[tq + 16 * j][c]);
+            o[j] = *reinterpret_cast<const float4*>(&sm.G[tq + 16 * j][c]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[i][j] = fmaf(k[i].x, q[j].x, fmaf(k[i].y, q[j].y, fmaf(k[i].z, q[j].z, fmaf(k[i].w, q[j].w, s[i][j]))));
+                t[i][j] = fmaf(v[i].x, o[j].x, fmaf(v[i].y, o[j].y, fmaf(v[i].z, o[j].z, fmaf(v[i].w, o[j].w, t[i][j]))));
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int key = tk + 16 * i, q = tq + 16 * j;
+            const bool see = q < nq && sm.kpos[key] <= qpos0 + q;
+            const float2 st = sm.stat[q];
+            const float p = see ? ex2_approx(fmaf(s[i][j], scale2, -st.x)) : 0.f;
+            sm.P[q][key] = p;
+            sm.S[q][key] = see ? p * (t[i][j] - st.y) : 0.f;
+        }
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads)
+backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    TileSmem<DH>& sm = *reinterpret_cast<TileSmem<DH>*>(raw);
+    const int tid = threadIdx.x;
+    const size_t row_elems = static_cast<size_t>(H) * DH;
+    const float scale2 = scale * kLog2e;
+    // query blocks first: they are the longer ones
+    const bool own_queries = static_cast<int>(blockIdx.x) < g.q_blocks;
+    const int bid = static_cast<int>(blockIdx.x) - (own_queries ? 0 : g.q_blocks);
+    int b = 0;
+    for (int i = 1; i < g.nseq; ++i) b += (own_queries ? g.seq[i].q0 : g.seq[i].kv0) <= bid ? 1 : 0;
+    const BackwardSeq sq = g.seq[b];
+    const int tx = tid % 16, ty = tid / 16;
+    constexpr int ND = DH / 64;       // a thread owns 4 consecutive features in each run of 64
+    dodo_grid_dependency_sync();
+
+    if (!own_queries) {
+        const int r = bid - sq.kv0;
+        const int h = r % H, tile = r / H;
+        const int nt_c = (sq.c_len + TK - 1) / TK;
+        const bool cached = tile < nt_c;
+        const int first = (cached ? tile : tile - nt_c) * TK;
+        const int rows = min(TK, (cached ? sq.c_len : sq.l_len) - first);
+        const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
+        const T* gk = static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH;
+        const T* gv = static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH;
+        load_rows<T, DH>(sm.K, gk, row_elems, row0, rows, TK);
+        load_rows<T, DH>(sm.V, gv, row_elems, row0, rows, TK);
+        if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
+        float dk[4][4 * ND], dv[4][4 * ND], score[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            score[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4 * ND; ++e) dk[i][e] = dv[i][e] = 0.f;
+        }
+        // queries from the first one that can see a key of a local tile
+        const int q_start = cached ? 0 : max(0, sq.l_pos0 + first - sq.q_pos0) / TQ * TQ;
+        for (int q0 = q_start; q0 < sq.tq; q0 += TQ) {
+            const int nq = min(TQ, sq.tq - q0);
+            __syncthreads();
+            load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+            load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+            if (tid < TQ) sm.stat[tid] = __ldg(a.stats + static_cast<size_t>(h) * g.stat_rows + sq.stat0 + q0 + tid);
+            __syncthreads();
+            tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
+            __syncthreads();
+#pragma unroll 2
+            for (int q = 0; q < TQ; ++q) {
+                const float4 p = *reinterpret_cast<const float4*>(&sm.P[q][4 * ty]), s = *reinterpret_cast<const float4*>(&sm.S[q][4 * ty]);
+                const float pa[4] = {p.x, p.y, p.z, p.w}, sa[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) score[i] += sa[i];
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const float4 o = *reinterpret_cast<const float4*>(&sm.G[q][64 * d + 4 * tx]);
+                    const float4 x = *reinterpret_cast<const float4*>(&sm.Q[q][64 * d + 4 * tx]);
+                    const float oa[4] = {o.x, o.y, o.z, o.w}, xa[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            dv[i][4 * d + e] = fmaf(pa[i], oa[e], dv[i][4 * d + e]);
+                            dk[i][4 * d + e] = fmaf(sa[i], xa[e], dk[i][4 * d + e]);
+                        }
+                }
+            }
+        }
+        T* ok = static_cast<T*>(cached ? a.dcK : a.dlK) + static_cast<size_t>(h) * DH;
+        T* ov = static_cast<T*>(cached ? a.dcV : a.dlV) + static_cast<size_t>(h) * DH;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = 4 * ty + i;
+            if (key >= rows) continue;
+            const size_t at = static_cast<size_t>(row0 + key) * row_elems;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                store4(ok + at + 64 * d + 4 * tx, make_float4(dk[i][4 * d] * scale, dk[i][4 * d + 1] * scale, dk[i][4 * d + 2] * scale, dk[i][4 * d + 3] * scale));
+                store4(ov + at + 64 * d + 4 * tx, make_float4(dv[i][4 * d], dv[i][4 * d + 1], dv[i][4 * d + 2], dv[i][4 * d + 3]));
+            }
+            if (cached && a.dscore != nullptr && tx == 0) a.score_part[static_cast<size_t>(h) * a.score_rows + row0 + key] = score[i];
+        }
+        if (cached && a.dscore != nullptr) finish_scores(a, H, row0, rows, a.tickets + sq.stick0 + tile, &sm.flag);
+        return;
+    }
+
+    // ---- a query tile (or a chunk of its key list) -------------------------------------------------------------------
+    int r = bid - sq.q0;
+    const int chunk = r % sq.nchunk; r /= sq.nchunk;
+    const int h = r % H, qt = r / H;
+    const int q0 = qt * TQ, nq = min(TQ, sq.tq - q0);
+    const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q0 + nq - sq.l_pos0));
+    const int nt_c = (sq.c_len + TK - 1) / TK, nt = nt_c + (l_vis + TK - 1) / TK;
+    const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
+    load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+    load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+    if (tid < TQ) sm.stat[tid] = __ldg(a.stats + static_cast<size_t>(h) * g.stat_rows + sq.stat0 + q0 + tid);
+    float dq[2][4 * ND];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4 * ND; ++e) dq[i][e] = 0.f;
+    for (int t = t0; t < t1; ++t) {
+        const bool cached = t < nt_c;
+        const int first = (cached ? t : t - nt_c) * TK;
+        const int rows = min(TK, (cached ? sq.c_len : l_vis) - first);
+        const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
+        __syncthreads();
+        load_rows<T, DH>(sm.K, static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows, TK);
+        load_rows<T, DH>(sm.V, static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows, TK);
+        if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
+        __syncthreads();
+        tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
+        __syncthreads();
+#pragma unroll 4
+        for (int k = 0; k < TK; ++k) {
+            const float s0 = sm.S[ty][k], s1 = sm.S[ty + 16][k];
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const float4 x = *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]);
+                const float xa[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    // a key that some queries of the tile do not see may hold anything: its dS is exactly 0 there
+                    dq[0][4 * d + e] = s0 != 0.f ? fmaf(s0, xa[e], dq[0][4 * d + e]) : dq[0][4 * d + e];
+                    dq[1][4 * d + e] = s1 != 0.f ? fmaf(s1, xa[e], dq[1][4 * d + e]) : dq[1][4 * d + e];
+                }
+            }
+        }
+    }
+    T* out = static_cast<T*>(a.dQ) + static_cast<size_t>(sq.q_row0 + q0) * row_elems + static_cast<size_t>(h) * DH;
+    const size_t part = static_cast<size_t>(sq.part0 + (qt * H + h) * sq.nchunk);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int q = ty + 16 * i;
+        if (q >= nq) continue;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const float4 v = make_float4(dq[i][4 * d], dq[i][4 * d + 1], dq[i][4 * d + 2], dq[i][4 * d + 3]);
+            if (sq.nchunk == 1) store4(out + q * row_elems + 64 * d + 4 * tx, make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale));
+            else store4(a.dq_part + ((part + chunk) * TQ + q) * DH + 64 * d + 4 * tx, v);
+        }
+    }
+    if (sq.nchunk == 1 || !last_arrival(a.tickets + sq.qtick0 + qt * H + h, sq.nchunk, &sm.flag)) return;
+    for (int i = tid; i < nq * (DH / 4); i += kThreads) {
+        const int q = i / (DH / 4), c = 4 * (i % (DH / 4));
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int n = 0; n < sq.nchunk; ++n) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(a.dq_part + ((part + n) * TQ + q) * DH + c));
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        store4(out + q * row_elems + c, make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale));
+    }
+}
+
+template <typename T, int DH>
+int launch_stream(dodo_ctx* ctx, int H, float scale, int max_tq, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
+    const dim3 grid(static_cast<unsigned>(g.kv_blocks)), block(kThreads);
+    const cudaError_t e = max_tq <= 1 ? dodo_launch_dependent(backward_stream_kernel<T, DH, 1, 4>, grid, block, 0, st, a, g, H, scale)
+                        : max_tq <= 2 ? dodo_launch_dependent(backward_stream_kernel<T, DH, 2, 2>, grid, block, 0, st, a, g, H, scale)
+                                      : dodo_launch_dependent(backward_stream_kernel<T, DH, 4, 2>, grid, block, 0, st, a, g, H, scale);
+    return dodo_check_cuda(ctx, e, "attend gradient launch");
+}
+
+template <typename T, int DH>
+int launch_tile(dodo_ctx* ctx, int slot, int H, float scale, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
+    auto kern = backward_tile_kernel<T, DH>;
+    const size_t smem = sizeof(TileSmem<DH>);
+    if (!ctx->backward_attr_set[slot]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient shared-memory attribute");
+        ctx->backward_attr_set[slot] = true;
+    }
+    return dodo_check_cuda(ctx, dodo_launch_dependent(kern, dim3(static_cast<unsigned>(g.q_blocks + g.kv_blocks)), dim3(kThreads), smem, st, a, g, H, scale),
+                           "attend gradient launch");
+}
+
+}  // namespace
+
+BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh) {
+    const int bundles = kThreads / (dh * static_cast<int>(dodo_elem_bytes(dtype)) / 16);
+    if (variant == DODO_BWD_STREAM) return {bundles, 4, bundles};
+    return {TK, TQ, TK};
+}
+
+int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, int max_tq, const BackwardGroup& g,
+                                const BackwardArrays& a, cudaStream_t st) {
+    if (g.kv_blocks == 0) return DODO_OK;
+    if (dtype == DODO_BF16 && dh == 128) return launch_stream<__nv_bfloat16, 128>(ctx, H, sm_scale, max_tq, g, a, st);
+    if (dtype == DODO_BF16) return launch_stream<__nv_bfloat16, 64>(ctx, H, sm_scale, max_tq, g, a, st);
+    if (dh == 128) return launch_stream<float, 128>(ctx, H, sm_scale, max_tq, g, a, st);
+    return launch_stream<float, 64>(ctx, H, sm_scale, max_tq, g, a, st);
+}
+
+int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
+    if (g.stat_rows == 0) return DODO_OK;
+    const int per_block = kThreads / (dh * static_cast<int>(dodo_elem_bytes(dtype)) / 16);
+    const long long units = static_cast<long long>(g.stat_rows) * H;
+    const dim3 grid(static_cast<unsigned>((units + per_block - 1) / per_block)), block(kThreads);
+    const cudaError_t e = dtype == DODO_BF16 ? dodo_launch_dependent(backward_stats_kernel<__nv_bfloat16>, grid, block, 0, st, a, g, H, dh)
+                                             : dodo_launch_dependent(backward_stats_kernel<float>, grid, block, 0, st, a, g, H, dh);
+    return dodo_check_cuda(ctx, e, "attend gradient statistics launch");
+}
+
+int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a,
+                              cudaStream_t st) {
+    if (g.q_blocks + g.kv_blocks == 0) return DODO_OK;
+    if (dtype == DODO_BF16 && dh == 128) return launch_tile<__nv_bfloat16, 128>(ctx, 0, H, sm_scale, g, a, st);
+    if (dtype == DODO_BF16) return launch_tile<__nv_bfloat16, 64>(ctx, 1, H, sm_scale, g, a, st);
+    if (dh == 128) return launch_tile<float, 128>(ctx, 2, H, sm_scale, g, a, st);
+    return launch_tile<float, 64>(ctx, 3, H, sm_scale, g, a, st);
+}

@@ -34,6 +34,7 @@ struct dodo_ctx {
     struct MapEntry { const void* base; int rows, width, box_rows; CUtensorMap map; } map_cache[16];
     int map_next;               // round-robin replacement
     bool dense_attr_set[4];     // shared-memory attribute of the four forms of the tensor-core kernel
+    bool backward_attr_set[6];  // ... and of the kernels of attend's gradient
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
     int select_key_cap;
@@ -258,6 +259,51 @@ int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scal
                           float* partials, int* tickets, bool early_cache, cudaStream_t st);
 int dodo_attend_tile_keys(int dtype, int dh);
 int dodo_attend_max_qt(int dtype, int dh);
+
+// ---- gradient of attend ---------------------------------------------------------------------------
+// Per-sequence tables of one launch.  Key blocks own key rows (their dK, dV and score gradients), query blocks own query
+// rows (their dQ) and may share a query tile by cutting its key list into chunks.
+struct BackwardSeq {
+    int q_row0, tq, q_pos0;
+    int c_row0, c_len;
+    int l_row0, l_len, l_pos0;
+    int stat0;      // first entry of the sequence in a head's row of statistics (a multiple of 64)
+    int kv0;        // first key block
+    int q0;         // first query block
+    int nchunk;     // chunks of a (query tile, head)'s key list
+    int ctiles;     // key tiles per chunk
+    int part0;      // first partial tile of the sequence's query tiles
+    int qtick0;     // first arrival counter of its (query tile, head) units
+    int stick0;     // first arrival counter of its key tiles (score gradients, one arrival per head)
+};
+struct BackwardGroup {
+    int nseq;
+    int kv_blocks, q_blocks;
+    int stat_rows;                  // entries of a head's row of statistics
+    BackwardSeq seq[DODO_GROUP];
+};
+struct BackwardArrays {
+    const void *Q, *O, *dO;
+    const void *cK, *cV, *lK, *lV;
+    const int32_t* cache_pos;
+    const float* lse;
+    void *dQ, *dcK, *dcV, *dlK, *dlV;
+    float* dscore;                  // or NULL
+    float2* stats;                  // [H][stat_rows]: (log-sum-exp in base 2, or +inf where nothing is visible; sum of dO * O)
+    float* score_part;              // [H][score_rows]
+    float* dq_part;                 // partial tiles of dQ
+    int score_rows;
+    int* tickets;
+};
+enum { DODO_BWD_STREAM = 0, DODO_BWD_TILE = 1, DODO_BWD_DENSE = 2 };
+// tile sizes the planner needs: keys per key block, queries per query tile, keys per step of a query block
+struct BackwardTiles { int keys, queries, step; };
+BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh);
+int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, int max_tq, const BackwardGroup& g,
+                                const BackwardArrays& a, cudaStream_t st);
+int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st);
+int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g,
+                              const BackwardArrays& a, cudaStream_t st);
 int dodo_attend_max_cluster();   // most chunks of one (query tile, head) that can merge inside a cluster
 // Table for AttendPlan::cluster_cap of the kernel that serves (dtype, dh, qt), from the occupancy calculator
 // (cached in the context); NULL if that kernel is not built.

@@ -99,3 +99,27 @@ def logit_bound(Q, K, scale, dh, low=None):
     a = np.abs(K) if low is None else np.abs(K) + 2.0 * np.abs(low)
     size = abs(scale) * max(float(np.max(np.abs(Q[:, h]) @ a[:, h].T)) for h in range(Q.shape[1]))
     return (dh + 16) * 2.0 ** -24 * size
+
+
+def backward_with_bounds(Q, q_pos, scale, K, V, k_pos, O, lse, dO, half, weight_half=0.0):
+    """attend_backward and how far each result may be off.  fp32 operations, each off by at most 2^-24 of what it adds up (2^-23
+    allowed, for accumulators that cut); results rounded once (half); P and dS rounded on the way where weight_half > 0."""
+    dQ, dK, dV, dx, P, dS = attend_backward(Q, q_pos, scale, K, V, k_pos, O, lse, dO)
+    T, n, dh, u = Q.shape[0], K.shape[0], Q.shape[2], 2.0 ** -23
+    if T == 0 or n == 0:
+        return (dQ, dK, dV, dx), (np.zeros_like(dQ), np.zeros_like(dK), np.zeros_like(dV), np.zeros_like(dx))
+    eins = np.einsum
+    size_x = abs(scale) * eins("thd,khd->htk", np.abs(Q), np.abs(K))
+    fin = np.where(np.isfinite(lse), np.abs(lse), 0.0).T[:, :, None]
+    ex = (dh + 8) * u * size_x + 4 * u * (size_x + fin) + 2.0 ** -21                 # relative error of P
+    dP = eins("thd,khd->htk", dO, V) - eins("thd,thd->ht", dO, O)[:, :, None]
+    ed = (dh + 8) * u * (eins("thd,khd->htk", np.abs(dO), np.abs(V)) + eins("thd,thd->ht", np.abs(dO), np.abs(O))[:, :, None])
+    eP = P * (ex + weight_half)
+    eS = P * (ex * np.abs(dP) + (1.0 + ex) * ed)
+    eSr = eS + weight_half * (np.abs(dS) + eS)                                       # as the products see it
+    aS, sc = np.abs(dS), abs(scale)
+    tQ = half * np.abs(dQ) + sc * ((1 + half) * eins("htk,khd->thd", eSr, np.abs(K)) + (n + 8) * u * eins("htk,khd->thd", aS, np.abs(K)))
+    tK = half * np.abs(dK) + sc * ((1 + half) * eins("htk,thd->khd", eSr, np.abs(Q)) + (T + 8) * u * eins("htk,thd->khd", aS, np.abs(Q)))
+    tV = half * np.abs(dV) + (1 + half) * eins("htk,thd->khd", eP, np.abs(dO)) + (T + 8) * u * eins("htk,thd->khd", P, np.abs(dO))
+    tx = eS.sum((0, 1)) + (T * Q.shape[1] + 8) * u * aS.sum((0, 1))
+    return (dQ, dK, dV, dx), (tQ, tK, tV, tx)

@@ -1,0 +1,332 @@
+"""attend's gradient on the GPU against the formula in 64 bits, with bounds from the number of operations, and as a training step
+uses it: behind the forward call, in a captured graph, with rows and regions that are not its own left alone."""
+import numpy as np
+import pytest
+import torch
+
+import plain64
+from paper_2310_02409_b200 import api, inputs
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _cuda(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2, scale=None, std=1.0, nan_slack=True):
+    """A ragged batch with slack rows (NaN) behind every region; O and lse come from dodo_attend (see forward)."""
+    rs = np.random.RandomState(inputs.seed_for(tag) % 2 ** 32)
+    B = len(tqs)
+    p = dict(B=B, H=H, dh=dh, dtype=dtype, scale=dh ** -0.5 if scale is None else scale)
+    p["q_off"], p["cache_off"] = inputs.offsets(tqs), inputs.offsets([c + slack for c in clens])
+    p["clen"], p["llen"] = np.asarray(clens, np.int32), np.asarray(llens, np.int32)
+    p["loc_off"] = inputs.offsets([n + slack for n in llens])[:-1].copy()
+    rows, lrows = int(p["cache_off"][-1]), int(sum(n + slack for n in llens))
+    span = [5 * c + 3 for c in clens]
+    p["loc_pos0"] = np.asarray(span, np.int32)
+    p["q_pos0"] = np.asarray([max(0, s // 2 - t // 2 - 1) if inside else s + n - t for s, n, t in zip(span, llens, tqs)], np.int32)
+    draw = lambda r: torch.from_numpy(std * rs.standard_normal((r, H, dh))).to(dtype)  # noqa: E731
+    p["cK"], p["cV"], p["lK"], p["lV"] = draw(rows), draw(rows), draw(lrows), draw(lrows)
+    p["Q"], p["dO"] = draw(int(p["q_off"][-1])), draw(int(p["q_off"][-1]))
+    p["cpos"] = np.zeros(rows, np.int32)
+    p["live_c"], p["live_l"] = np.zeros(rows, bool), np.zeros(lrows, bool)
+    for b in range(B):
+        c0 = int(p["cache_off"][b])
+        p["cpos"][c0:c0 + clens[b]] = np.sort(rs.permutation(span[b])[:clens[b]])
+        p["live_c"][c0:c0 + clens[b]] = True
+        p["live_l"][p["loc_off"][b]:p["loc_off"][b] + llens[b]] = True
+    if nan_slack:
+        for n, live in (("cK", "live_c"), ("cV", "live_c"), ("lK", "live_l"), ("lV", "live_l")):
+            p[n][torch.from_numpy(~p[live])] = float("nan")
+    return p
+
+
+def forward(dodo, p):
+    d = {n: p[n].cuda() for n in ("Q", "cK", "cV", "lK", "lV", "dO")}
+    d["cpos"] = _cuda(p["cpos"])
+    d["O"] = torch.zeros_like(d["Q"])
+    d["lse"] = torch.full(d["Q"].shape[:2], -float("inf"), device="cuda")
+    ws = torch.empty(dodo.attend_workspace_bytes(p["dh"]), dtype=torch.uint8, device="cuda")
+    dodo.attend(d["Q"], p["q_off"], p["q_pos0"], p["scale"], d["cK"], d["cV"], d["cpos"], p["cache_off"], p["clen"], d["lK"], d["lV"],
+                p["loc_off"], p["llen"], p["loc_pos0"], d["O"], d["lse"], ws)
+    return d
+
+
+def buffers(d, fill=7.0):
+    out = {n: torch.full_like(d[s], fill) for n, s in (("dQ", "Q"), ("dcK", "cK"), ("dcV", "cV"), ("dlK", "lK"), ("dlV", "lV"))}
+    out["dscore"] = torch.full((d["cK"].shape[0],), fill, device="cuda")
+    return out
+
+
+def backward(dodo, p, d, out=None, scores=True, ws=None):
+    out = buffers(d) if out is None else out
+    if ws is None:
+        n = dodo.attend_backward_workspace_bytes(d["Q"].shape[0], p["H"], p["dh"], int(p["cache_off"][-1]))
+        ws = torch.full((n + 256,), 0xff, dtype=torch.uint8, device="cuda")      # (NaN in every format)
+        guard = ws[n:]
+        ws = ws[:n]
+    else:
+        guard = None
+    dodo.attend_backward(d["Q"], p["q_off"], p["q_pos0"], p["scale"], d["cK"], d["cV"], d["cpos"], p["cache_off"], p["clen"], d["lK"],
+                         d["lV"], p["loc_off"], p["llen"], p["loc_pos0"], d["O"], d["lse"], d["dO"], out["dQ"], out["dcK"], out["dcV"],
+                         out["dlK"], out["dlV"], out["dscore"] if scores else None, ws)
+    if guard is not None:
+        assert bool((guard == 0xff).all())
+    return out
+
+
+def check(p, d, out, dense=False, fill=7.0, scores=True):
+    half = plain64.HALF["bf16" if p["dtype"] == BF else "f32"]
+    Q, O, dO, lse = (_f64(d[n]) for n in ("Q", "O", "dO", "lse"))
+    cK, cV, lK, lV = (_f64(p[n]) for n in ("cK", "cV", "lK", "lV"))
+    got = {n: _f64(t) for n, t in out.items()}
+    worst = {}
+    for b in range(p["B"]):
+        q = slice(int(p["q_off"][b]), int(p["q_off"][b + 1]))
+        c = slice(int(p["cache_off"][b]), int(p["cache_off"][b]) + int(p["clen"][b]))
+        l = slice(int(p["loc_off"][b]), int(p["loc_off"][b]) + int(p["llen"][b]))
+        n = c.stop - c.start
+        k, v = np.concatenate([cK[c], lK[l]]), np.concatenate([cV[c], lV[l]])
+        kpos = np.concatenate([p["cpos"][c], p["loc_pos0"][b] + np.arange(p["llen"][b])])
+        ref, tol = plain64.backward_with_bounds(Q[q], p["q_pos0"][b] + np.arange(q.stop - q.start), p["scale"], k, v, kpos, O[q], lse[q],
+                                                dO[q], half, plain64.HALF["bf16"] if dense else 0.0)
+        pairs = [("dQ", got["dQ"][q], ref[0], tol[0]), ("dcK", got["dcK"][c], ref[1][:n], tol[1][:n]), ("dlK", got["dlK"][l], ref[1][n:], tol[1][n:]),
+                 ("dcV", got["dcV"][c], ref[2][:n], tol[2][:n]), ("dlV", got["dlV"][l], ref[2][n:], tol[2][n:])]
+        if scores:
+            pairs.append(("dscore", got["dscore"][c], ref[3][:n], tol[3][:n]))
+        for name, g, r, t in pairs:
+            assert np.all(np.isfinite(g)), (name, b)
+            bad = np.abs(g - r) > t + 1e-30
+            assert not bad.any(), (name, b, int(bad.sum()), np.argwhere(bad)[:3].tolist(), float(np.max(np.abs(g - r) - t)))
+            if r.size:
+                worst[name] = max(worst.get(name, 0.0), float(np.linalg.norm(g - r) / max(1e-30, np.linalg.norm(r))))
+    # rows that belong to nobody keep what they held
+    assert np.all(got["dcK"][~p["live_c"]] == fill) and np.all(got["dcV"][~p["live_c"]] == fill)
+    assert np.all(got["dlK"][~p["live_l"]] == fill) and np.all(got["dlV"][~p["live_l"]] == fill)
+    assert np.all(got["dscore"][~p["live_c"] if scores else slice(None)] == fill)
+    return worst
+
+
+SHAPES = [
+    # dtype, H, dh, query tokens, cached rows, local rows
+    (BF, 4, 128, [1] * 8, [205] * 8, [64] * 8),
+    (BF, 2, 128, [1, 1, 0, 1, 1], [0, 1, 50, 129, 1000], [1, 0, 3, 7, 130]),
+    (F32, 3, 64, [1, 1, 1], [700, 5, 0], [64, 1, 33]),
+    (F32, 2, 128, [2, 1, 2], [33, 300, 64], [2, 9, 70]),
+    (BF, 3, 64, [3, 4, 1, 0, 2], [257, 31, 8, 40, 0], [5, 4, 1, 3, 66]),
+    (F32, 4, 64, [16], [52], [16]),
+    (F32, 2, 128, [33, 5, 64], [70, 0, 129], [40, 5, 64]),
+    (BF, 2, 64, [7, 100, 0, 31], [300, 64, 20, 1], [7, 130, 9, 31]),
+    (F32, 1, 64, [65], [2000], [65]),
+]
+
+
+@pytest.mark.parametrize("inside", [False, True])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_gradient_against_plain(dodo, errlog, case, inside):
+    dtype, H, dh, tqs, cl, ll = SHAPES[case]
+    p = problem(("bwd", case, inside), dtype, H, dh, tqs, cl, ll, inside)
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    worst = check(p, d, out)
+    errlog.add(f"attend_backward {SHAPES[case]} {inside}", **{"rel_" + n: v for n, v in worst.items()})
+    again = backward(dodo, p, d)                                  # bit for bit the same again, with and without scores
+    bare = backward(dodo, p, d, scores=False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n].nan_to_num(5.0), again[n].nan_to_num(5.0)) for n in out)
+    assert all(torch.equal(out[n], bare[n]) for n in out if n != "dscore") and bool((bare["dscore"] == 7.0).all())
+    assert dodo.device_status() == 0
+
+
+def test_gradient_of_many_sequences(dodo):
+    # 70 sequences: two launch groups share the workspace
+    rs = np.random.RandomState(2)
+    for most in (1, 9):
+        tqs, cl, ll = rs.randint(0, most + 1, 70), rs.randint(0, 90, 70), rs.randint(0, 40, 70)
+        p = problem(("bwdmany", most), F32, 2, 64, tqs.tolist(), cl.tolist(), ll.tolist())
+        d = forward(dodo, p)
+        out = backward(dodo, p, d)
+        torch.cuda.synchronize()
+        check(p, d, out)
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 1), (F32, 64, 20), (BF, 128, 3), (BF, 64, 40)])
+def test_gradient_negative_and_zero_scale(dodo, dtype, dh, tq):
+    for scale in (-0.1, 0.0):
+        p = problem(("bwdscale", dh, tq, scale), dtype, 2, dh, [tq], [100], [tq + 3], scale=scale)
+        d = forward(dodo, p)
+        out = backward(dodo, p, d)
+        torch.cuda.synchronize()
+        check(p, d, out)
+
+
+@pytest.mark.parametrize("dtype,H,dh,tq", [(F32, 2, 64, 2), (F32, 2, 128, 40), (BF, 2, 64, 70), (BF, 2, 128, 4)])
+def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
+    """Nuggets ahead of every query, and local tokens behind it, hold NaN and infinities: their own gradients are 0, nobody
+    else's changes; queries before the first key get 0."""
+    p = problem(("bwdnan", dh, tq), dtype, H, dh, [tq, tq], [200, 90], [tq, 5], inside=True)
+    p["q_pos0"][1] = -tq                       # sees nothing at all
+    d = forward(dodo, p)
+    clean = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    check(p, d, clean)
+    bad = dict(p)
+    for b in range(2):
+        c0, n = int(p["cache_off"][b]), int(p["clen"][b])
+        hidden = torch.from_numpy(c0 + np.flatnonzero(p["cpos"][c0:c0 + n] > p["q_pos0"][b] + tq - 1))
+        assert len(hidden) > 10
+        for name, v in (("cK", float("nan")), ("cV", float("inf"))):
+            bad[name] = bad[name].clone()
+            bad[name][hidden] = v
+    for name in ("lK", "lV"):
+        bad[name] = torch.full_like(p[name], float("-inf"))
+    db = {**d, **{n: bad[n].cuda() for n in ("cK", "cV", "lK", "lV")}}
+    out = backward(dodo, bad, db)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n], clean[n]) for n in out)
+    assert bool((out["dQ"][tq:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 24), (BF, 64, 40)])
+def test_gradient_partly_visible_nan_key(dodo, dtype, dh, tq):
+    """A key that only later queries see holds NaN: earlier queries' dQ is untouched."""
+    p = problem(("bwdpart", dh, tq), dtype, 1, dh, [tq], [0], [tq], slack=0)
+    d = forward(dodo, p)
+    clean = backward(dodo, p, d)
+    d2 = dict(d)
+    d2["lK"] = d["lK"].clone()
+    d2["lK"][tq - 1] = float("nan")            # the last query's own token
+    out = backward(dodo, p, d2)
+    torch.cuda.synchronize()
+    assert torch.equal(out["dQ"][:tq - 1], clean["dQ"][:tq - 1])
+    assert bool(torch.isnan(out["dQ"][tq - 1]).all())
+
+
+def test_gradient_against_differences(dodo):
+    # the whole step by differences of the plain forward: dQ, dK, dV of the fp32 kernels
+    p = problem("bwddiff", F32, 2, 64, [6], [20], [6], slack=0)
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    Q, dO = _f64(p["Q"]), _f64(p["dO"])
+    kpos = np.concatenate([p["cpos"], p["loc_pos0"][0] + np.arange(6)])
+    K, V = np.concatenate([_f64(p["cK"]), _f64(p["lK"])]), np.concatenate([_f64(p["cV"]), _f64(p["lV"])])
+    qpos = p["q_pos0"][0] + np.arange(6)
+    loss = lambda a: float(np.sum(plain64.attend(a[0], qpos, p["scale"], a[1], a[2], kpos)[0] * dO))  # noqa: E731
+    got = [_f64(out["dQ"]), np.concatenate([_f64(out["dcK"]), _f64(out["dlK"])]), np.concatenate([_f64(out["dcV"]), _f64(out["dlV"])])]
+    rs, e = np.random.RandomState(4), 1e-5
+    for which in range(3):
+        for _ in range(25):
+            a, b = [Q.copy(), K.copy(), V.copy()], [Q.copy(), K.copy(), V.copy()]
+            i = tuple(rs.randint(0, s) for s in a[which].shape)
+            a[which][i] += e
+            b[which][i] -= e
+            # central differences: cut-off of order e^2, 64-bit cancellation of order 1e-16 |loss| / e; fp32 results about 1e-5
+            assert abs((loss(a) - loss(b)) / (2 * e) - got[which][i]) < 1e-4
+
+
+@pytest.mark.parametrize("dtype,H,dh,tqs", [(F32, 2, 64, [1, 2]), (F32, 2, 64, [20, 3]), (BF, 2, 128, [2, 1]), (BF, 2, 128, [40, 65])])
+def test_gradient_captured_and_replayed(dodo, dtype, H, dh, tqs):
+    """Forward and gradient of two problems in one graph on a stream of its own, with a shared workspace, replayed on new data."""
+    ps = [problem(("bwdgraph", i, dh, tqs[0]), dtype, H, dh, tqs, [150, 60], [tqs[0] + 3, tqs[1]], inside=bool(i)) for i in range(2)]
+    ws = torch.empty(max(dodo.attend_backward_workspace_bytes(int(p["q_off"][-1]), H, dh, int(p["cache_off"][-1])) for p in ps),
+                     dtype=torch.uint8, device="cuda")
+    ds = [forward(dodo, p) for p in ps]
+    eager = [backward(dodo, p, d, ws=ws) for p, d in zip(ps, ds)]
+    torch.cuda.synchronize()
+    outs = [buffers(d) for d in ds]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for p, d, o in zip(ps, ds, outs):
+            backward(dodo, p, d, o, ws=ws)
+    for t in ds:
+        t["dO"].mul_(2.0)                      # exact in either type: every gradient doubles
+    for _ in range(2):
+        for o in outs:
+            for t in o.values():
+                t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, o, e in zip(ps, outs, eager):
+            for n in e:
+                live = p["live_c"] if n in ("dcK", "dcV", "dscore") else p["live_l"] if n in ("dlK", "dlV") else np.ones(o[n].shape[0], bool)
+                live = torch.from_numpy(live).cuda()
+                assert torch.equal(o[n][live], 2.0 * e[n][live]), n
+                assert bool((o[n][~live] == 7.0).all())
+
+
+def test_gradient_without_a_segment_or_queries(dodo):
+    p = problem("bwdseg", F32, 2, 64, [3, 9], [40, 20], [0, 0], slack=0)
+    d = forward(dodo, p)
+    out = buffers(d)
+    ws = torch.empty(dodo.attend_backward_workspace_bytes(12, 2, 64, 60), dtype=torch.uint8, device="cuda")
+    dodo.attend_backward(d["Q"], p["q_off"], p["q_pos0"], p["scale"], d["cK"], d["cV"], d["cpos"], p["cache_off"], p["clen"], None, None, None,
+                         None, None, d["O"], d["lse"], d["dO"], out["dQ"], out["dcK"], out["dcV"], None, None, out["dscore"], ws)
+    torch.cuda.synchronize()
+    check(p, d, out)
+    # no queries: the keys' gradients are zeros
+    z = np.zeros(3, np.int32)
+    empty = torch.empty((0, 2, 64), device="cuda")
+    dodo.attend_backward(empty, z, p["q_pos0"], p["scale"], d["cK"], d["cV"], d["cpos"], p["cache_off"], p["clen"], None, None, None, None,
+                         None, empty, torch.empty((0, 2), device="cuda"), empty, empty, out["dcK"], out["dcV"], None, None, out["dscore"], ws)
+    torch.cuda.synchronize()
+    assert not out["dcK"].any() and not out["dcV"].any() and not out["dscore"].any()
+
+
+def test_training_step_of_the_scorer(dodo, oracle):
+    """Score, select, gather, attend, gradient, and from the nuggets' score gradients the Scorer's (dw = sum dscore_j x_j): the
+    whole against the formula in 64 bits on the rows that the GPU selected."""
+    n, dm, H, dh, r, tq = 300, 256, 4, 64, 10, 16
+    X = inputs.randn((n, dm), "bwdtrain", "X")
+    w = inputs.randn((dm,), "bwdtrain", "w", std=dm ** -0.5)
+    K, V = (inputs.randn((n, H, dh), "bwdtrain", k) for k in "KV")
+    Q, lK, lV, dO = (inputs.randn((tq, H, dh), "bwdtrain", k) for k in ("Q", "lK", "lV", "dO"))
+    k = dodo.num_nuggets(n, r)
+    scores, idx = torch.empty(n, device="cuda"), torch.empty(k, dtype=torch.int32, device="cuda")
+    cK, cV = torch.zeros((k, H, dh), device="cuda"), torch.zeros((k, H, dh), device="cuda")
+    cpos, clen = torch.zeros(k, dtype=torch.int32, device="cuda"), np.zeros(1, np.int32)
+    dodo.compress(X.cuda(), w.cuda(), 0.0, K.cuda(), V.cuda(), [0, n], [0, k], [0], 0, scores, idx, cK, cV, cpos, [0, k], clen)
+    p = dict(B=1, H=H, dh=dh, dtype=F32, scale=dh ** -0.5, q_off=np.array([0, tq], np.int32), q_pos0=np.array([n], np.int32),
+             cache_off=np.array([0, k], np.int32), clen=clen, loc_off=np.array([0], np.int32), llen=np.array([tq], np.int32),
+             loc_pos0=np.array([n], np.int32), cK=cK.cpu(), cV=cV.cpu(), lK=lK, lV=lV, Q=Q, dO=dO, cpos=cpos.cpu().numpy(),
+             live_c=np.ones(k, bool), live_l=np.ones(tq, bool))
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    dw = X.cuda()[idx.long()].T @ out["dscore"]
+    torch.cuda.synchronize()
+    check(p, d, out)
+    i = idx.cpu().numpy()
+    assert np.array_equal(i, oracle.select(scores.cpu().numpy(), k))
+    ref = plain64.attend_backward(_f64(Q), n + np.arange(tq), p["scale"], np.concatenate([_f64(K)[i], _f64(lK)]),
+                                  np.concatenate([_f64(V)[i], _f64(lV)]), np.concatenate([i, n + np.arange(tq)]), _f64(d["O"]), _f64(d["lse"]), _f64(dO))
+    ref_dw = _f64(X)[i].T @ ref[3][:k]
+    assert np.linalg.norm(_f64(dw) - ref_dw) <= 1e-5 * np.linalg.norm(ref_dw) + 1e-6
+
+
+def test_backward_binding_refuses_wrong_tensors(dodo):
+    p = problem("bwdref", F32, 2, 64, [3], [8], [3], slack=0)
+    d = forward(dodo, p)
+    out = buffers(d)
+    ws = torch.empty(dodo.attend_backward_workspace_bytes(3, 2, 64, 8), dtype=torch.uint8, device="cuda")
+    base = dict(Q=d["Q"], q_off=p["q_off"], q_pos0=p["q_pos0"], sm_scale=p["scale"], cacheK=d["cK"], cacheV=d["cV"], cache_pos=d["cpos"],
+                cache_off=p["cache_off"], cache_len=p["clen"], locK=d["lK"], locV=d["lV"], loc_off=p["loc_off"], loc_len=p["llen"],
+                loc_pos0=p["loc_pos0"], O=d["O"], lse=d["lse"], dO=d["dO"], dQ=out["dQ"], dcacheK=out["dcK"], dcacheV=out["dcV"],
+                dlocK=out["dlK"], dlocV=out["dlV"], dscore=out["dscore"], workspace=ws)
+    for bad, kind in ((dict(dO=d["dO"].bfloat16()), TypeError), (dict(lse=d["lse"].double()), TypeError), (dict(dQ=out["dQ"][:2]), ValueError),
+                      (dict(dcacheV=out["dcV"].cpu()), ValueError), (dict(dscore=out["dscore"][:7]), ValueError), (dict(q_off=[0, 4]), ValueError),
+                      (dict(cacheK=d["cK"].transpose(0, 1)), ValueError), (dict(cache_off=[0, 9]), ValueError), (dict(loc_len=[]), ValueError),
+                      (dict(dlocK=out["dlK"].bfloat16()), TypeError), (dict(O=d["O"].transpose(1, 2)), ValueError)):
+        with pytest.raises(kind):
+            dodo.attend_backward(**{**base, **bad})
+    with pytest.raises(api.DodoError) as e:
+        dodo.attend_backward(**{**base, "workspace": ws[:-16]})
+    assert e.value.status == api.ERR_CAPACITY

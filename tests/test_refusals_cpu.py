@@ -93,3 +93,28 @@ def test_attend_q4_workspace_grows_with_the_cache(ctx):
     a, b = (lib.dodo_attend_q4_workspace_bytes(c, 2, 128, rows) for rows in (0, 100))
     assert b - a == 2 * 100 * 2 * 128 * 2
     assert lib.dodo_attend_q4_workspace_bytes(c, 0, 128, 1) == 0 and lib.dodo_attend_q4_workspace_bytes(c, 2, 128, -1) == 0
+
+
+def _backward(**k):
+    return {**dict(Q=P, q_off=_i32(0, 1, 2), q_pos0=_i32(9, 9), dtype=1, H=2, dh=64, sm_scale=0.125, cacheK=P, cacheV=P, pos=P,
+                   cache_off=_i32(0, 2, 4), cache_len=_i32(1, 2), locK=P, locV=P, loc_off=_i32(0, 3), loc_len=_i32(3, 1), loc_pos0=_i32(0, 0),
+                   loc_rows=4, B=2, O=P, lse=P, dO=P, dQ=P, dcacheK=P, dcacheV=P, dlocK=P, dlocV=P, dscore=P, workspace=P,
+                   workspace_bytes=1 << 16, stream=None), **k}
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(B=-1), BAD), (dict(dtype=7), UNSUP), (dict(dh=96), UNSUP), (dict(H=0), BAD), (dict(Q=None), BAD), (dict(O=None), BAD), (dict(lse=None), BAD),
+    (dict(dO=P + 8), BAD), (dict(dQ=None), BAD), (dict(q_pos0=None), BAD), (dict(q_off=_i32(0, 2, 1)), BAD), (dict(cacheK=None), BAD),
+    (dict(cacheV=P + 4), BAD), (dict(pos=None), BAD), (dict(dcacheK=None), BAD), (dict(dcacheV=P + 8), BAD), (dict(cache_len=_i32(3, 0)), BAD),
+    (dict(cache_off=None), BAD), (dict(loc_len=_i32(-1, 0)), BAD), (dict(loc_off=None), BAD), (dict(dlocK=None), BAD), (dict(dlocV=P + 8), BAD),
+    (dict(loc_off=_i32(0, 2)), BAD), (dict(loc_off=_i32(1, 0), loc_len=_i32(2, 2)), BAD),       # windows that share a row
+    (dict(workspace=None), CAP), (dict(workspace=P + 8), CAP), (dict(workspace_bytes=64), CAP),
+])
+def test_attend_backward_refuses(ctx, change, status):
+    assert _call(ctx, "dodo_attend_backward", **_backward(**change)) == status
+
+
+def test_attend_backward_of_nothing_is_nothing(ctx):
+    nothing = dict(q_off=_i32(0, 0, 0), cache_len=None, loc_len=None, Q=None, O=None, lse=None, dO=None, dQ=None, workspace=None)
+    assert _call(ctx, "dodo_attend_backward", **_backward(**nothing)) == 0
+    assert _call(ctx, "dodo_attend_backward", **_backward(B=0, q_off=_i32(0), q_pos0=None, cache_len=None, loc_len=None)) == 0
