@@ -17,8 +17,8 @@ struct Layout { size_t stats, scores, parts, total; };
 Layout layout(const dodo_ctx* ctx, int q_rows, int H, int cache_rows) {
     Layout l;
     l.stats = 0;
-    l.scores = round256(static_cast<size_t>(H) * (static_cast<size_t>(q_rows) + DODO_GROUP * kStatAlign) * sizeof(float2));
-    l.parts = l.scores + round256(static_cast<size_t>(H) * cache_rows * sizeof(float));
+    l.scores = round256(static_cast<size_t>(H) * (static_cast<size_t>(q_rows) + DODO_GROUP * kStatAlign) * 2 * sizeof(float));
+    l.parts = l.scores + round256(static_cast<size_t>(H) * 2 * cache_rows * sizeof(float));
     l.total = l.parts + static_cast<size_t>(2) * ctx->num_sms * kPartFloats * sizeof(float);
     return l;
 }
@@ -100,7 +100,7 @@ int plan_group(dodo_ctx* ctx, const AttendShape& s, int variant, int b0, int nb,
         g.seq[i].stick0 = static_cast<int>(qticks + sticks);
         sticks += variant == DODO_BWD_STREAM ? g.seq[i].nchunk : ceil_div(g.seq[i].c_len, t.keys);
     }
-    if (qticks + sticks > DODO_NUM_TICKETS)
+    if (qticks + sticks > DODO_NUM_TICKETS - 1)      // (the last counter hands out the tensor-core kernel's units)
         return dodo_fail(ctx, DODO_ERR_CAPACITY, "too many key tiles and split query tiles (%lld) in one group of sequences", static_cast<long long>(qticks + sticks));
     if (kv + qb > 0x7fffffff || stat > 0x7fffffff)
         return dodo_fail(ctx, DODO_ERR_CAPACITY, "too many thread blocks (%lld)", static_cast<long long>(kv + qb));
@@ -148,14 +148,14 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
 
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
-    const int variant = max_tq <= kStreamQueries ? DODO_BWD_STREAM : DODO_BWD_TILE;
+    const int variant = max_tq <= kStreamQueries ? DODO_BWD_STREAM : dtype == DODO_BF16 && dh == 128 ? DODO_BWD_DENSE : DODO_BWD_TILE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     BackwardArrays a;
     a.Q = Q; a.O = O; a.dO = dO; a.cK = cacheK; a.cV = cacheV; a.lK = locK; a.lV = locV;
     a.cache_pos = cache_pos; a.lse = lse;
     a.dQ = dQ; a.dcK = dcacheK; a.dcV = dcacheV; a.dlK = dlocK; a.dlV = dlocV;
     a.dscore = any_cache ? dscore : nullptr;
-    a.stats = reinterpret_cast<float2*>(ws + lay.stats);
+    a.stats = reinterpret_cast<float*>(ws + lay.stats);
     a.score_part = reinterpret_cast<float*>(ws + lay.scores);
     a.dq_part = reinterpret_cast<float*>(ws + lay.parts);
     a.score_rows = any_cache ? cache_off[B] : 0;
@@ -173,7 +173,10 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
                 rc = dodo_launch_backward_stream(ctx, dtype, H, dh, sm_scale, max_tq, g, a, st);
             } else {
                 rc = dodo_launch_backward_stats(ctx, dtype, H, dh, g, a, st);
-                if (rc == DODO_OK) rc = dodo_launch_backward_tile(ctx, dtype, H, dh, sm_scale, g, a, st);
+                if (rc == DODO_OK)
+                    rc = variant == DODO_BWD_TILE ? dodo_launch_backward_tile(ctx, dtype, H, dh, sm_scale, g, a, st)
+                                                  : dodo_launch_backward_dense(ctx, H, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
+                                                                               ctx->tickets + DODO_NUM_TICKETS - 1, st);
             }
             if (rc != DODO_OK) return rc;
         }

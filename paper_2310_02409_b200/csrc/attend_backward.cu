@@ -45,8 +45,8 @@ __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<f
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
     *reinterpret_cast<uint2*>(p) = make_uint2(two_bf16(v.x, v.y), two_bf16(v.z, v.w));
 }
-// a query's statistic: log-sum-exp in base 2, +inf (every weight comes out 0) where the query sees nothing
-__device__ __forceinline__ float lse_base2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// a query's statistic: minus the log-sum-exp in base 2, -inf (every weight comes out 0) where the query sees nothing
+__device__ __forceinline__ float minus_lse2(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
 
 // One more of `n` arrivals on a counter that is zero between launches; true for the last, which finds the others' writes
 // visible.  All threads of the block call it.
@@ -94,21 +94,21 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
     const size_t col = static_cast<size_t>(h) * DH + lig * E;
     dodo_grid_dependency_sync();
 
-    float q[QT][E], go[QT][E], dq[QT][E], lse2[QT], delta[QT];
+    float q[QT][E], go[QT][E], dq[QT][E], nlse[QT], delta[QT];
     int qpos[QT];
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
         float o[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) q[i][e] = go[i][e] = o[e] = dq[i][e] = 0.f;
-        lse2[i] = INFINITY;
+        nlse[i] = -INFINITY;
         qpos[i] = static_cast<int>(0x80000000);
         if (i < sq.tq) {
             const size_t at = static_cast<size_t>(sq.q_row0 + i) * row_elems + col;
             Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.Q) + at), q[i]);
             Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.dO) + at), go[i]);
             Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.O) + at), o);
-            lse2[i] = lse_base2(a.lse[static_cast<size_t>(sq.q_row0 + i) * H + h]);
+            nlse[i] = minus_lse2(a.lse[static_cast<size_t>(sq.q_row0 + i) * H + h]);
             qpos[i] = sq.q_pos0 + i;
         }
         float d = 0.f;
@@ -183,7 +183,7 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
 #pragma unroll
             for (int i = 0; i < QT; ++i) {
                 const bool see = pc[u] <= qpos[i];       // a masked key takes no part, whatever its row holds
-                const float p = see ? ex2_approx(fmaf(s[i][u], scale2, -lse2[i])) : 0.f;
+                const float p = see ? ex2_approx(fmaf(s[i][u], scale2, nlse[i])) : 0.f;
                 const float ds = see ? p * (t[i][u] - delta[i]) : 0.f;
                 ds_sum += ds;
 #pragma unroll
@@ -249,8 +249,8 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
 }
 
 // =============================================== statistics =============================================================
-// (log-sum-exp in base 2, sum of dO * O) of every query, one row per head so that a tile's entries are contiguous; entries
-// behind a sequence's last query, up to a multiple of 64, are (+inf, 0): such a column's weights come out 0.
+// -(log-sum-exp in base 2) and -(sum of dO * O) of every query, one row per head so that a tile's entries are contiguous;
+// entries behind a sequence's last query, up to a multiple of 64, are -inf and 0: such a column's weights come out 0.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, int DH) {
@@ -274,8 +274,11 @@ backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGr
         for (int e = 0; e < E; ++e) d = fmaf(x[e], y[e], d);
     }
     for (int s = lpr / 2; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
-    if (entry < g.stat_rows && lig == 0)
-        a.stats[static_cast<size_t>(h) * g.stat_rows + entry] = live ? make_float2(lse_base2(a.lse[row]), d) : make_float2(INFINITY, 0.f);
+    if (entry < g.stat_rows && lig == 0) {
+        float* s = a.stats + (static_cast<size_t>(h) * g.stat_rows + (entry & ~63)) * 2 + (entry & 63);
+        s[0] = live ? minus_lse2(a.lse[row]) : -INFINITY;
+        s[64] = live ? -d : 0.f;
+    }
 }
 
 // =============================================== fp32 tiles ==============================================================
@@ -290,6 +293,14 @@ template <int DH> struct TileSmem {
     int kpos[TK];
     int flag;
 };
+
+// statistics of queries [q0, q0 + TQ) of a sequence
+__device__ __forceinline__ void load_stats(float2* dst, const BackwardArrays& a, const BackwardGroup& g, int h, int entry0) {
+    if (threadIdx.x >= TQ) return;
+    const int e = entry0 + static_cast<int>(threadIdx.x);
+    const float* s = a.stats + (static_cast<size_t>(h) * g.stat_rows + (e & ~63)) * 2 + (e & 63);
+    dst[threadIdx.x] = make_float2(__ldg(s), __ldg(s + 64));
+}
 
 template <typename T, int DH>
 __device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const T* src, size_t row_elems, int row0, int rows, int n) {
@@ -338,9 +349,9 @@ __device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0
             const int key = tk + 16 * i, q = tq + 16 * j;
             const bool see = q < nq && sm.kpos[key] <= qpos0 + q;
             const float2 st = sm.stat[q];
-            const float p = see ? ex2_approx(fmaf(s[i][j], scale2, -st.x)) : 0.f;
+            const float p = see ? ex2_approx(fmaf(s[i][j], scale2, st.x)) : 0.f;
             sm.P[q][key] = p;
-            sm.S[q][key] = see ? p * (t[i][j] - st.y) : 0.f;
+            sm.S[q][key] = see ? p * (t[i][j] + st.y) : 0.f;
         }
 }
 
@@ -389,7 +400,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
             __syncthreads();
             load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
             load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-            if (tid < TQ) sm.stat[tid] = __ldg(a.stats + static_cast<size_t>(h) * g.stat_rows + sq.stat0 + q0 + tid);
+            load_stats(sm.stat, a, g, h, sq.stat0 + q0);
             __syncthreads();
             tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
             __syncthreads();
@@ -442,7 +453,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
     load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
     load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-    if (tid < TQ) sm.stat[tid] = __ldg(a.stats + static_cast<size_t>(h) * g.stat_rows + sq.stat0 + q0 + tid);
+    load_stats(sm.stat, a, g, h, sq.stat0 + q0);
     float dq[2][4 * ND];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -528,6 +539,7 @@ int launch_tile(dodo_ctx* ctx, int slot, int H, float scale, const BackwardGroup
 BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh) {
     const int bundles = kThreads / (dh * static_cast<int>(dodo_elem_bytes(dtype)) / 16);
     if (variant == DODO_BWD_STREAM) return {bundles, 4, bundles};
+    if (variant == DODO_BWD_DENSE) return dodo_backward_dense_tiles();
     return {TK, TQ, TK};
 }
 

@@ -145,6 +145,49 @@ def test_gradient_against_plain(dodo, errlog, case, inside):
     assert dodo.device_status() == 0
 
 
+DENSE = [
+    # H, query tokens, cached rows, local rows (bf16, head size 128, more than four queries: tensor cores)
+    (2, [64], [128], [64]),
+    (1, [5], [1], [5]),
+    (2, [128], [0], [128]),
+    (3, [16, 200, 0, 1], [70, 333, 129, 0], [16, 230, 9, 65]),
+    (2, [256], [717], [320]),
+    (1, [512], [130], [512]),
+    (4, [33, 7], [2000, 64], [40, 7]),
+    (32, [130] * 3, [205] * 3, [194] * 3),
+    (1, [65, 127, 129], [63, 64, 65], [65, 191, 129]),
+]
+
+
+@pytest.mark.parametrize("inside", [False, True])
+@pytest.mark.parametrize("case", range(len(DENSE)))
+def test_gradient_on_tensor_cores(dodo, errlog, case, inside):
+    H, tqs, cl, ll = DENSE[case]
+    p = problem(("bwdtc", case, inside), BF, H, 128, tqs, cl, ll, inside)
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    assert dodo.device_status() == 0
+    worst = check(p, d, out, dense=True)
+    errlog.add(f"attend_backward tensor cores {DENSE[case]} {inside}", **{"rel_tc_" + n: v for n, v in worst.items()})
+    again = backward(dodo, p, d)
+    bare = backward(dodo, p, d, scores=False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n], again[n]) for n in out)
+    assert all(torch.equal(out[n], bare[n]) for n in out if n != "dscore") and bool((bare["dscore"] == 7.0).all())
+
+
+def test_gradient_on_tensor_cores_many_sequences(dodo):
+    rs = np.random.RandomState(12)
+    tqs, cl, ll = rs.randint(0, 90, 67), rs.randint(0, 200, 67), rs.randint(0, 100, 67)
+    p = problem("bwdtcmany", BF, 2, 128, tqs.tolist(), cl.tolist(), ll.tolist())
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    check(p, d, out, dense=True)
+    assert dodo.device_status() == 0
+
+
 def test_gradient_of_many_sequences(dodo):
     # 70 sequences: two launch groups share the workspace
     rs = np.random.RandomState(2)
@@ -157,17 +200,17 @@ def test_gradient_of_many_sequences(dodo):
         check(p, d, out)
 
 
-@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 1), (F32, 64, 20), (BF, 128, 3), (BF, 64, 40)])
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 1), (F32, 64, 20), (BF, 128, 3), (BF, 64, 40), (BF, 128, 40)])
 def test_gradient_negative_and_zero_scale(dodo, dtype, dh, tq):
     for scale in (-0.1, 0.0):
         p = problem(("bwdscale", dh, tq, scale), dtype, 2, dh, [tq], [100], [tq + 3], scale=scale)
         d = forward(dodo, p)
         out = backward(dodo, p, d)
         torch.cuda.synchronize()
-        check(p, d, out)
+        check(p, d, out, dense=dtype == BF and dh == 128 and tq > 4)
 
 
-@pytest.mark.parametrize("dtype,H,dh,tq", [(F32, 2, 64, 2), (F32, 2, 128, 40), (BF, 2, 64, 70), (BF, 2, 128, 4)])
+@pytest.mark.parametrize("dtype,H,dh,tq", [(F32, 2, 64, 2), (F32, 2, 128, 40), (BF, 2, 64, 70), (BF, 2, 128, 4), (BF, 2, 128, 70)])
 def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
     """Nuggets ahead of every query, and local tokens behind it, hold NaN and infinities: their own gradients are 0, nobody
     else's changes; queries before the first key get 0."""
@@ -176,7 +219,7 @@ def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
     d = forward(dodo, p)
     clean = backward(dodo, p, d)
     torch.cuda.synchronize()
-    check(p, d, clean)
+    check(p, d, clean, dense=dtype == BF and dh == 128 and tq > 4)
     bad = dict(p)
     for b in range(2):
         c0, n = int(p["cache_off"][b]), int(p["clen"][b])
@@ -194,7 +237,7 @@ def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
     assert bool((out["dQ"][tq:] == 0).all())
 
 
-@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 24), (BF, 64, 40)])
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 24), (BF, 64, 40), (BF, 128, 100)])
 def test_gradient_partly_visible_nan_key(dodo, dtype, dh, tq):
     """A key that only later queries see holds NaN: earlier queries' dQ is untouched."""
     p = problem(("bwdpart", dh, tq), dtype, 1, dh, [tq], [0], [tq], slack=0)
