@@ -108,23 +108,36 @@ def _dev(t: torch.Tensor | None):
     return t.data_ptr()
 
 
-def _on(device: torch.device, shapes: dict, dtypes: dict):
-    """Raises unless every named tensor (None: skipped) lies on ``device``, dense, with its shape and dtype."""
-    for name, (t, shape) in shapes.items():
-        if t is None:
-            continue
-        if t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous tensor on {device}")
-        if t.dtype != dtypes[name]:
-            raise TypeError(f"{name} must be {dtypes[name]}, is {t.dtype}")
-        if shape is not None and t.shape != shape:
-            raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+_I32 = np.dtype(np.int32)
 
 
-def _len_array(cache_len) -> np.ndarray:
-    if not (isinstance(cache_len, np.ndarray) and cache_len.dtype == np.int32 and cache_len.flags.c_contiguous):
-        raise TypeError("cache_len must be a contiguous int32 numpy array (updated in place)")
-    return cache_len
+def _table(a) -> bytes | None:
+    """A host table as the bytes of an int32 array: a read-only pointer argument without the cost of ``ndarray.ctypes``."""
+    if a is None:
+        return None
+    if type(a) is not np.ndarray or a.dtype is not _I32:
+        a = np.asarray(a, dtype=np.int32)
+    return a.tobytes()
+
+
+def _in_place(a) -> int:
+    """Address of an int32 table that the call updates."""
+    if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.flags.c_contiguous and a.flags.writeable):
+        raise TypeError("cache_len must be a contiguous, writeable int32 numpy array (updated in place)")
+    return ctypes.addressof(ctypes.c_char.from_buffer(a)) if a.size else 0
+
+
+def _bound(table: bytes | None, sequences: int, rows: int, what: str):
+    """Raises unless an offset table describes ``sequences`` regions inside ``rows`` rows."""
+    if table is None or len(table) != 4 * (sequences + 1):
+        raise ValueError(f"{what} must have {sequences + 1} entries")
+    if int.from_bytes(table[-4:], "little", signed=True) > rows:
+        raise ValueError(f"{what} ends behind row {rows}, the last of its array")
+
+
+def _entries(table: bytes | None, sequences: int, what: str):
+    if table is None or len(table) < 4 * sequences:
+        raise ValueError(f"{what} must have {sequences} entries")
 
 
 def _host_i32(a) -> np.ndarray | None:
@@ -154,6 +167,7 @@ class Dodo:
             self._ctx = None
             raise DodoError(rc, msg)
         self.device = torch.device("cuda", device)
+        self._index = int(device)
 
     def close(self):
         if getattr(self, "_ctx", None):
@@ -323,6 +337,27 @@ class Dodo:
                                           _dev(locK), _dev(locV), _hp(lo), _hp(ll), _hp(lp), loc_rows,
                                           len(qo) - 1, _dev(O), _dev(lse), _dev(workspace), ws_bytes, _stream()))
 
+    # -- checks of the methods below ------------------------------------------------------------------
+    def _ptr(self, t, dtype, numel, name):
+        """Address of a dense tensor on this context's device with its dtype and (None: any) number of elements."""
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
+        if t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor on {self.device}")
+        if numel is not None and t.numel() != numel:
+            raise ValueError(f"{name} must have {numel} elements, has {t.numel()} (shape {tuple(t.shape)})")
+        return t.data_ptr()
+
+    def _workspace(self, t):
+        if t is None:
+            return None, 0
+        return self._ptr(t, t.dtype, None, "workspace"), t.numel() * t.element_size()
+
+    def _heads(self, t, name):
+        if t.dim() != 3:
+            raise ValueError(f"{name} must have shape [rows, H, dh], has {tuple(t.shape)}")
+        return t.shape
+
     # -- the gradient of attend --------------------------------------------------------------------
     def attend_backward_workspace_bytes(self, q_rows: int, H: int, dh: int, cache_rows: int) -> int:
         return int(self._lib.dodo_attend_backward_workspace_bytes(self._ctx, int(q_rows), int(H), int(dh), int(cache_rows)))
@@ -331,76 +366,76 @@ class Dodo:
                         locK, locV, loc_off, loc_len, loc_pos0, O, lse, dO, dQ, dcacheK, dcacheV, dlocK, dlocV, dscore, workspace):
         """``dodo_attend_backward``: gradients of ``attend`` from its inputs, ``O``, ``lse`` and ``dO``; ``dscore`` (float, one
         entry a cache row) may be None, and the cache's or the local tokens' tensors where the call has none."""
-        qo, qp = _host_i32(q_off), _host_i32(q_pos0)
-        co, cl = _host_i32(cache_off), _host_i32(cache_len)
-        lo, ll, lp = _host_i32(loc_off), _host_i32(loc_len), _host_i32(loc_pos0)
-        H, dh = Q.shape[-2], Q.shape[-1]
-        code, B, dt = _dtype_code(Q), len(qo) - 1, Q.dtype
-        loc_rows = 0 if locK is None else locK.shape[0]
-        like = lambda t: None if t is None else t.shape  # noqa: E731
-        _on(self.device, {"Q": (Q, None), "O": (O, Q.shape), "dO": (dO, Q.shape), "dQ": (dQ, Q.shape), "lse": (lse, Q.shape[:2]),
-                          "cacheK": (cacheK, None), "cacheV": (cacheV, like(cacheK)), "dcacheK": (dcacheK, like(cacheK)),
-                          "dcacheV": (dcacheV, like(cacheK)), "cache_pos": (cache_pos, None), "locK": (locK, None),
-                          "locV": (locV, like(locK)), "dlocK": (dlocK, like(locK)), "dlocV": (dlocV, like(locK)),
-                          "dscore": (dscore, None), "workspace": (workspace, None)},
-            {**{n: dt for n in ("Q", "O", "dO", "dQ", "cacheK", "cacheV", "dcacheK", "dcacheV", "locK", "locV", "dlocK", "dlocV")},
-             "lse": torch.float32, "dscore": torch.float32, "cache_pos": torch.int32, "workspace": workspace.dtype})
-        self._regions(Q.shape[0], qo, qp, "q_off")
+        qo, qp = _table(q_off), _table(q_pos0)
+        co, cl = _table(cache_off), _table(cache_len)
+        lo, ll, lp = _table(loc_off), _table(loc_len), _table(loc_pos0)
+        rows_q, H, dh = self._heads(Q, "Q")
+        code, B, dt, row = _dtype_code(Q), len(qo) // 4 - 1, Q.dtype, H * dh
+        _bound(qo, B, rows_q, "q_off")
+        _entries(qp, B, "q_pos0")
+        n, ptr = rows_q * row, self._ptr
+        q, o, g, dq = ptr(Q, dt, n, "Q"), ptr(O, dt, n, "O"), ptr(dO, dt, n, "dO"), ptr(dQ, dt, n, "dQ")
+        ls = ptr(lse, torch.float32, rows_q * H, "lse")
+        ck = cv = dk = dv = pos = ds = None
         if cacheK is not None:
-            rows = min(cacheK.shape[0], cache_pos.numel(), cacheK.shape[0] if dscore is None else dscore.numel())
-            self._regions(rows, co, cl)
-            if len(co) != B + 1 or tuple(cacheK.shape[1:]) != (H, dh):
-                raise ValueError("cache_off must describe the same sequences as q_off, cacheK and cacheV [rows, H, dh]")
-        if locK is not None and not (len(lo) >= B and len(ll) >= B and len(lp) >= B and tuple(locK.shape[1:]) == (H, dh)):
-            raise ValueError("loc_off, loc_len and loc_pos0 must have one entry a sequence, locK and locV [rows, H, dh]")
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+            rows = self._heads(cacheK, "cacheK")[0]
+            n = rows * row
+            ck, cv = ptr(cacheK, dt, n, "cacheK"), ptr(cacheV, dt, n, "cacheV")
+            dk, dv = ptr(dcacheK, dt, n, "dcacheK"), ptr(dcacheV, dt, n, "dcacheV")
+            pos = ptr(cache_pos, torch.int32, None, "cache_pos")
+            rows = min(rows, cache_pos.numel())
+            if dscore is not None:
+                ds = ptr(dscore, torch.float32, None, "dscore")
+                rows = min(rows, dscore.numel())
+            _bound(co, B, rows, "cache_off")
+            _entries(cl, B, "cache_len")
+        lk = lv = dlk = dlv = None
+        loc_rows = 0
+        if locK is not None:
+            loc_rows = self._heads(locK, "locK")[0]
+            n = loc_rows * row
+            lk, lv = ptr(locK, dt, n, "locK"), ptr(locV, dt, n, "locV")
+            dlk, dlv = ptr(dlocK, dt, n, "dlocK"), ptr(dlocV, dt, n, "dlocV")
+            _entries(lo, B, "loc_off")
+            _entries(ll, B, "loc_len")
+            _entries(lp, B, "loc_pos0")
+        w, ws_bytes = self._workspace(workspace)
         self._check(self._lib.dodo_attend_backward(
-            self._ctx, ptr(Q), _hp(qo), _hp(qp), code, H, dh, float(sm_scale), ptr(cacheK), ptr(cacheV), ptr(cache_pos), _hp(co),
-            _hp(cl), ptr(locK), ptr(locV), _hp(lo), _hp(ll), _hp(lp), loc_rows, B, ptr(O), ptr(lse), ptr(dO), ptr(dQ), ptr(dcacheK),
-            ptr(dcacheV), ptr(dlocK), ptr(dlocV), ptr(dscore), ptr(workspace), workspace.numel() * workspace.element_size(),
-            _stream()))
+            self._ctx, q, qo, qp, code, H, dh, sm_scale, ck, cv, pos, co, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls, g, dq, dk, dv,
+            dlk, dlv, ds, w, ws_bytes, _stream()))
 
     # -- the 4-bit nugget cache ----------------------------------------------------------------------
-    def _q4_cache(self, cache_q4, cache_scale, H, dh, more=(), dtypes=None):
+    def _q4_cache(self, cache_q4, cache_scale, H, dh):
         rows = cache_q4.shape[0]
-        shapes = {"cache_q4": (cache_q4, (rows, H, 2, dh // 2)), "cache_scale": (cache_scale, (rows, H, 2, dh // Q4_GROUP)), **dict(more)}
-        _on(self.device, shapes, {"cache_q4": torch.uint8, "cache_scale": torch.int32, **(dtypes or {})})
-        return rows
-
-    def _regions(self, rows, off, lens=None, what="cache_off"):
-        if len(off) and int(off[-1]) > rows:
-            raise ValueError(f"{what} ends at row {int(off[-1])} of an array of {rows}")
-        if lens is not None and len(lens) < len(off) - 1:
-            raise ValueError(f"{len(off) - 1} regions, {len(lens)} lengths")
+        return rows, self._ptr(cache_q4, torch.uint8, rows * H * dh, "cache_q4"), self._ptr(cache_scale, torch.int32, rows * H * (dh // 16), "cache_scale")
 
     def gather_kv_q4(self, K, V, seq_off, idx, nug_off, pos_base, cache_q4, cache_scale, cache_pos, cache_off, cache_len):
         """``dodo_gather_kv_q4``: append the selected rows to a 4-bit cache (``cache_q4`` uint8 [rows, H, 2, dh/2],
         ``cache_scale`` int32 [rows, H, 2, dh/32]); ``cache_len`` (int32 numpy array) is updated in place."""
-        so, no, pb, co = _host_i32(seq_off), _host_i32(nug_off), _host_i32(pos_base), _host_i32(cache_off)
-        H, dh = K.shape[-2], K.shape[-1]
-        code = _dtype_code(K)
-        rows = self._q4_cache(cache_q4, cache_scale, H, dh,
-                              {"K": (K, None), "V": (V, K.shape), "idx": (idx, None), "cache_pos": (cache_pos, None)},
-                              {"K": K.dtype, "V": K.dtype, "idx": torch.int32, "cache_pos": torch.int32})
-        B = len(so) - 1
-        self._regions(K.shape[0], so, None, "seq_off")
-        self._regions(idx.numel(), no, None, "nug_off")
-        self._regions(min(rows, cache_pos.numel()), co, _len_array(cache_len))
-        if not (len(no) == len(co) == B + 1 and len(pb) >= B):
-            raise ValueError("seq_off, nug_off, pos_base and cache_off must describe the same number of sequences")
-        self._check(self._lib.dodo_gather_kv_q4(self._ctx, K.data_ptr(), V.data_ptr(), code, H, dh, _hp(so), idx.data_ptr(), _hp(no),
-                                                _hp(pb), B, cache_q4.data_ptr(), cache_scale.data_ptr(), cache_pos.data_ptr(), _hp(co),
-                                                _hp(cache_len), _stream()))
+        so, no, pb, co, cl = _table(seq_off), _table(nug_off), _table(pos_base), _table(cache_off), _in_place(cache_len)
+        tokens, H, dh = self._heads(K, "K")
+        code, dt, B, ptr = _dtype_code(K), K.dtype, len(so) // 4 - 1, self._ptr
+        rows, q4, sc = self._q4_cache(cache_q4, cache_scale, H, dh)
+        k, v = ptr(K, dt, None, "K"), ptr(V, dt, K.numel(), "V")
+        ix, pos = ptr(idx, torch.int32, None, "idx"), ptr(cache_pos, torch.int32, None, "cache_pos")
+        _bound(so, B, tokens, "seq_off")
+        _bound(no, B, idx.numel(), "nug_off")
+        _bound(co, B, min(rows, cache_pos.numel()), "cache_off")
+        _entries(pb, B, "pos_base")
+        if cache_len.size < B:
+            raise ValueError(f"cache_len must have {B} entries")
+        self._check(self._lib.dodo_gather_kv_q4(self._ctx, k, v, code, H, dh, so, ix, no, pb, B, q4, sc, pos, co, cl, _stream()))
 
     def expand_kv_q4(self, cache_q4, cache_scale, cache_off, cache_len, K, V):
         """``dodo_expand_kv_q4``: the rows in use of a 4-bit cache as rows of K and V (their dtype, the cache's row layout)."""
-        co, cl = _host_i32(cache_off), _host_i32(cache_len)
-        H, dh = K.shape[-2], K.shape[-1]
-        code = _dtype_code(K)
-        rows = self._q4_cache(cache_q4, cache_scale, H, dh, {"K": (K, None), "V": (V, K.shape)}, {"K": K.dtype, "V": K.dtype})
-        self._regions(min(rows, K.shape[0]), co, cl)
-        self._check(self._lib.dodo_expand_kv_q4(self._ctx, cache_q4.data_ptr(), cache_scale.data_ptr(), H, dh, _hp(co), _hp(cl),
-                                                len(co) - 1, code, K.data_ptr(), V.data_ptr(), _stream()))
+        co, cl = _table(cache_off), _table(cache_len)
+        rows_k, H, dh = self._heads(K, "K")
+        code, dt, B = _dtype_code(K), K.dtype, len(co) // 4 - 1
+        rows, q4, sc = self._q4_cache(cache_q4, cache_scale, H, dh)
+        k, v = self._ptr(K, dt, None, "K"), self._ptr(V, dt, K.numel(), "V")
+        _bound(co, B, min(rows, rows_k), "cache_off")
+        _entries(cl, B, "cache_len")
+        self._check(self._lib.dodo_expand_kv_q4(self._ctx, q4, sc, H, dh, co, cl, B, code, k, v, _stream()))
 
     def attend_q4_workspace_bytes(self, H: int, dh: int, cache_rows: int) -> int:
         return int(self._lib.dodo_attend_q4_workspace_bytes(self._ctx, int(H), int(dh), int(cache_rows)))
@@ -408,30 +443,31 @@ class Dodo:
     def attend_q4(self, Q, q_off, q_pos0, sm_scale, cache_q4, cache_scale, cache_pos, cache_off, cache_len,
                   locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):
         """``dodo_attend_q4``: ``attend`` over a 4-bit nugget cache and uncompressed local tokens."""
-        qo, qp = _host_i32(q_off), _host_i32(q_pos0)
-        co, cl = _host_i32(cache_off), _host_i32(cache_len)
-        lo, ll, lp = _host_i32(loc_off), _host_i32(loc_len), _host_i32(loc_pos0)
-        H, dh = Q.shape[-2], Q.shape[-1]
-        code, B, dt = _dtype_code(Q), len(qo) - 1, Q.dtype
-        loc_rows = 0 if locK is None else locK.shape[0]
-        more = {"Q": (Q, None), "O": (O, Q.shape), "lse": (lse, Q.shape[:2]), "locK": (locK, None), "locV": (locV, locK.shape if locK is not None else None),
-                "cache_pos": (cache_pos, None), "workspace": (workspace, None)}
-        types = {"Q": dt, "O": dt, "lse": torch.float32, "locK": dt, "locV": dt, "cache_pos": torch.int32,
-                 "workspace": workspace.dtype if workspace is not None else None}
+        qo, qp = _table(q_off), _table(q_pos0)
+        co, cl = _table(cache_off), _table(cache_len)
+        lo, ll, lp = _table(loc_off), _table(loc_len), _table(loc_pos0)
+        rows_q, H, dh = self._heads(Q, "Q")
+        code, B, dt, ptr = _dtype_code(Q), len(qo) // 4 - 1, Q.dtype, self._ptr
+        _bound(qo, B, rows_q, "q_off")
+        _entries(qp, B, "q_pos0")
+        q, o = ptr(Q, dt, None, "Q"), ptr(O, dt, Q.numel(), "O")
+        ls = None if lse is None else ptr(lse, torch.float32, rows_q * H, "lse")
+        q4 = sc = pos = lk = lv = None
         if cache_q4 is not None:
-            self._regions(min(self._q4_cache(cache_q4, cache_scale, H, dh, more, types), cache_pos.numel()), co, cl)
-            if len(co) != B + 1:
-                raise ValueError("cache_off and q_off must describe the same number of sequences")
-        else:
-            _on(self.device, more, types)
-        self._regions(Q.shape[0], qo, qp, "q_off")
-        if locK is not None and not (len(lo) >= B and len(ll) >= B and len(lp) >= B and tuple(locK.shape[1:]) == (H, dh)):
-            raise ValueError("loc_off, loc_len and loc_pos0 must have one entry a sequence, locK and locV [rows, H, dh]")
-        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self._check(self._lib.dodo_attend_q4(self._ctx, Q.data_ptr(), _hp(qo), _hp(qp), code, H, dh, float(sm_scale), ptr(cache_q4),
-                                             ptr(cache_scale), ptr(cache_pos), _hp(co), _hp(cl), ptr(locK), ptr(locV), _hp(lo), _hp(ll),
-                                             _hp(lp), loc_rows, B, O.data_ptr(), ptr(lse), ptr(workspace), ws_bytes, _stream()))
+            rows, q4, sc = self._q4_cache(cache_q4, cache_scale, H, dh)
+            pos = ptr(cache_pos, torch.int32, None, "cache_pos")
+            _bound(co, B, min(rows, cache_pos.numel()), "cache_off")
+            _entries(cl, B, "cache_len")
+        loc_rows = 0
+        if locK is not None:
+            loc_rows = self._heads(locK, "locK")[0]
+            lk, lv = ptr(locK, dt, loc_rows * H * dh, "locK"), ptr(locV, dt, loc_rows * H * dh, "locV")
+            _entries(lo, B, "loc_off")
+            _entries(ll, B, "loc_len")
+            _entries(lp, B, "loc_pos0")
+        w, ws_bytes = self._workspace(workspace)
+        self._check(self._lib.dodo_attend_q4(self._ctx, q, qo, qp, code, H, dh, sm_scale, q4, sc, pos, co, cl, lk, lv, lo, ll, lp, loc_rows,
+                                             B, o, ls, w, ws_bytes, _stream()))
 
     def attend_indexed(self, Q, q_off, q_pos0, sm_scale, K, V, seq_off, idx, nug_off, pos_base,
                        locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):

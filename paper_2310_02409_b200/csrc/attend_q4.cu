@@ -65,7 +65,7 @@ struct Q4Source {
 
 // FPL: features per lane (32 or 16); LPR = DH / FPL lanes share a key.
 template <typename T, int DH, int QT, int FPL, int U>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, QT == 1 ? 2 : 1)
 attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_constant__ AttendGroup g,
                  const int32_t* __restrict__ cache_pos, int H, float scale_log2, int TK, T* __restrict__ O,
                  float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets, int early_cache) {
@@ -467,7 +467,7 @@ template <typename T, int DH>
 int launch_qt(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src,
               const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
     switch (qt) {
-        case 1: return launch_t<T, DH, 1, 32, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
+        case 1: return launch_t<T, DH, 1, 16, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
         case 2: return launch_t<T, DH, 2, 16, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
         case 4: return launch_t<T, DH, 4, 16, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
         default: break;

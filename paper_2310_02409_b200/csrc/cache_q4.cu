@@ -87,21 +87,28 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t& word) {
     const float s = step_of(t, e);
     word = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
     if (s == 0.f) return 0u;
-    // Codes by a reciprocal: (x - m) / s comes out within 3e-6 of the true quotient (at most 15), so a fraction that is
-    // more than 1e-4 away from one half decides the rounding; any other (2e-4 of the features, and steps whose reciprocal
-    // overflows) is decided exactly.
-    const float inv = __fdiv_rn(1.f, s);
+    // Codes by a reciprocal: f = (x - m) / s comes out within 3e-6 of the true quotient (at most 15), so k = round(f - 1/2) is
+    // the whole number below it or one of its two neighbours' border lies within 3e-6; either way the code is k or k + 1, by
+    // which side of the border (k + 1/2) s the difference lies on.  The border is exact in fp32 (5 + 8 bits); where the
+    // difference equals it, what its rounding lost decides, or the even code if nothing was (bf16 rows, whose values lie on
+    // a coarse grid, meet that in about one octet in fifty).  Steps whose reciprocal overflows go through code_of.
+    const float inv = __fdiv_rn(1.f, s), half = 0.5f * s;
     constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: adding it rounds to whole numbers, in the low mantissa bits
     uint32_t codes = 0u;
-    bool sure = true;
 #pragma unroll
     for (int i = 0; i < kOctet; ++i) {
-        const float f = __fmul_rn(__fsub_rn(x[i], m), inv);
-        const float g = __fadd_rn(f, kMagic);
-        sure = sure && fabsf(__fsub_rn(f, __fsub_rn(g, kMagic))) < 0.4999f;
-        codes |= (__float_as_uint(g) & 15u) << (4 * i);
+        const float d = __fsub_rn(x[i], m);
+        const float r = __fadd_rn(__fmaf_rn(d, inv, -0.5f), kMagic);
+        const float border = __fmaf_rn(__fsub_rn(r, kMagic), s, half);
+        bool up = d > border;
+        if (d == border) {
+            float t2, e2;
+            two_diff(x[i], m, t2, e2);
+            up = e2 > 0.f || (e2 == 0.f && (__float_as_uint(r) & 1u) != 0u);
+        }
+        codes |= ((__float_as_uint(r) & 15u) + (up ? 1u : 0u)) << (4 * i);
     }
-    if (!sure) {
+    if (s < 1e-36f) {
         codes = 0u;
 #pragma unroll 1
         for (int i = 0; i < kOctet; ++i) codes |= static_cast<uint32_t>(code_of(x[i], m, s)) << (4 * i);
