@@ -6,7 +6,7 @@
 //   c_i = (x_i - m) / s rounded to the nearest whole number, ties to even (0 where s = 0),
 // and feature i stands for m + c_i s.  Both roundings go outwards, so every x_i lies in [m, m + 15 s], no code is
 // clamped and the error is at most s / 2 for every feature.  The codes are defined on real numbers; the kernel finds
-// them in fp32 and decides the few that lie next to a border exactly (see code_of).  A group that holds a NaN or an
+// them in fp32 and decides the few that lie on a border exactly (see quantise).  A group that holds a NaN or an
 // infinity, or whose span overflows, is stored as NaN: all of its features read back as NaN.
 // Storage: a (row, head) owns dh bytes of codes, K's dh / 2 then V's (feature 2i in the low half of byte i), which is
 // one 128-byte line at head size 128, and 2 dh / 32 words, K's then V's, with s in the low and m in the high 16 bits.
@@ -15,8 +15,9 @@
 namespace {
 
 constexpr int kThreads = 128;
+constexpr int kGatherThreads = 256;
 constexpr int kGroup = DODO_Q4_GROUP;
-constexpr int kOctet = 8;                       // features per thread and step: one word of codes
+constexpr int kOctet = 8;                       // features per word of codes
 constexpr float kFinite = 3.4028234663852886e38f;
 
 __device__ __forceinline__ float cut_bf16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }   // towards 0
@@ -30,10 +31,10 @@ __device__ __forceinline__ void two_diff(float a, float b, float& t, float& e) {
     const float z = __fsub_rn(t, a);
     e = __fadd_rn(__fsub_rn(a, __fsub_rn(t, z)), __fsub_rn(-b, z));
 }
-// Least bf16 s with 15 s >= t + e.  The quotient is off by at most a few units of fp32, so its bf16 cut is s or one
-// or two steps below; 15 s is exact (8 + 4 bits).
+// Least bf16 s with 15 s >= t + e.  The quotient is off by a few units of fp32, so its bf16 cut is s or one or two steps
+// below; 15 s is exact (8 + 4 bits).
 __device__ __forceinline__ float step_of(float t, float e) {
-    float s = cut_bf16(__fdiv_rn(t, 15.f));
+    float s = cut_bf16(__fmul_rn(t, 1.f / 15.f));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const float p = __fmul_rn(15.f, s);
@@ -54,77 +55,113 @@ __device__ __noinline__ int code_of(float x, float m, float s) {
     return min(max(c, 0), 15);
 }
 
-template <typename T> __device__ __forceinline__ void load_octet(const unsigned char* p, uint4* v);
-template <> __device__ __forceinline__ void load_octet<__nv_bfloat16>(const unsigned char* p, uint4* v) { v[0] = ld_stream16(p); }
-template <> __device__ __forceinline__ void load_octet<float>(const unsigned char* p, uint4* v) {
-    v[0] = ld_stream16(p);
-    v[1] = ld_stream16(p + 16);
+__device__ __forceinline__ float min3(float a, float b, float c) {   // (a NaN stays one)
+    float d;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 32 bytes, streaming
+__device__ __forceinline__ void load32(const void* p, uint32_t* v) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
+}
+// the storage words of a group as floats
+template <typename T> __device__ __forceinline__ void widen(const uint32_t* raw, float* x);
+template <> __device__ __forceinline__ void widen<float>(const uint32_t* raw, float* x) {
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) x[i] = __uint_as_float(raw[i]);
+}
+template <> __device__ __forceinline__ void widen<__nv_bfloat16>(const uint32_t* raw, float* x) {
+#pragma unroll
+    for (int i = 0; i < kGroup / 2; ++i) {
+        x[2 * i] = __uint_as_float(raw[i] << 16);
+        x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+    }
 }
 
-// Quantise one octet; the four lanes of a quad hold one group.  All lanes of the warp take part.
-__device__ __forceinline__ uint32_t quantise(const float* x, uint32_t& word) {
-    float lo = x[0], hi = x[0];
-    bool fine = fabsf(x[0]) <= kFinite;
+// Codes (four words) and group word of 32 features; kWide: they have more than the 8 significant bits of bf16.
+template <bool kWide>
+__device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* codes) {
+    float lo = min3(x[0], x[0], x[1]), hi = max3(x[0], x[0], x[1]);
 #pragma unroll
-    for (int i = 1; i < kOctet; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        fine = fine && fabsf(x[i]) <= kFinite;
-    }
-    if (!fine) hi = INFINITY;   // poisons the span
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    for (int i = 2; i < kGroup; i += 2) {
+        lo = min3(lo, x[i], x[i + 1]);
+        hi = max3(hi, x[i], x[i + 1]);
     }
     const float m = bf16_down(lo);
     float t, e;
     two_diff(hi, m, t, e);
-    if (!(t <= kFinite)) {
-        word = 0x00007fc0u;     // step NaN
-        return 0u;
-    }
-    const float s = step_of(t, e);
-    word = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
-    if (s == 0.f) return 0u;
-    // Codes by a reciprocal: f = (x - m) / s comes out within 3e-6 of the true quotient (at most 15), so k = round(f - 1/2) is
-    // the whole number below it or one of its two neighbours' border lies within 3e-6; either way the code is k or k + 1, by
-    // which side of the border (k + 1/2) s the difference lies on.  The border is exact in fp32 (5 + 8 bits); where the
-    // difference equals it, what its rounding lost decides, or the even code if nothing was (bf16 rows, whose values lie on
-    // a coarse grid, meet that in about one octet in fifty).  Steps whose reciprocal overflows go through code_of.
-    const float inv = __fdiv_rn(1.f, s), half = 0.5f * s;
-    constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: adding it rounds to whole numbers, in the low mantissa bits
-    uint32_t codes = 0u;
 #pragma unroll
-    for (int i = 0; i < kOctet; ++i) {
-        const float d = __fsub_rn(x[i], m);
-        const float r = __fadd_rn(__fmaf_rn(d, inv, -0.5f), kMagic);
-        const float border = __fmaf_rn(__fsub_rn(r, kMagic), s, half);
-        bool up = d > border;
-        if (d == border) {
-            float t2, e2;
-            two_diff(x[i], m, t2, e2);
-            up = e2 > 0.f || (e2 == 0.f && (__float_as_uint(r) & 1u) != 0u);
+    for (int w = 0; w < 4; ++w) codes[w] = 0u;
+    if (!(t <= kFinite)) return 0x00007fc0u;     // NaN, an infinity or too wide a span: step NaN
+    const float s = step_of(t, e);
+    const uint32_t word = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
+    // Codes by a reciprocal.  k = round((x - m) / s - 1/2), off by far less than one half, so the code is k or k + 1, by the
+    // side of the border (k + 1/2) s that d = x - m lies on; the border is exact in fp32 (5 + 8 bits).  At the border the even
+    // code wins: there d >= border is asked for odd k, which on the bits of non-negative floats is d + 1 > border.  k sits in
+    // the low bits of r = k + 1.5 * 2^23; the words are summed with those bits' constant part and freed of it at the end.
+    const float inv = rcp_approx(s), half = 0.5f * s;
+    constexpr float kMagic = 12582912.f;
+    constexpr uint32_t kMagicBits = 0x4b400000u;
+    bool met = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t c = 0u - kMagicBits * 0x11111111u;
+#pragma unroll
+        for (int i = 0; i < kOctet; ++i) {
+            const float d = __fsub_rn(x[w * kOctet + i], m);
+            const float r = __fadd_rn(__fmaf_rn(d, inv, -0.5f), kMagic);
+            const float border = __fmaf_rn(__fsub_rn(r, kMagic), s, half);
+            const uint32_t rb = __float_as_uint(r);
+            c += rb << (4 * i);
+            if (__float_as_uint(d) + (rb & 1u) > __float_as_uint(border)) c += 1u << (4 * i);
+            if (kWide) met = met || d == border;
         }
-        codes |= ((__float_as_uint(r) & 15u) + (up ? 1u : 0u)) << (4 * i);
+        codes[w] = c;
     }
-    if (s < 1e-36f) {
-        codes = 0u;
-#pragma unroll 1
-        for (int i = 0; i < kOctet; ++i) codes |= static_cast<uint32_t>(code_of(x[i], m, s)) << (4 * i);
+    // What rounding took from d matters only at a border.  bf16 values of exponents at most 15 apart subtract exactly, so for
+    // bf16 rows d is inexact only where |x| < 2^-14 |m|, when d is within 2^-14 of -m and a border has to be as near, or where
+    // |m| < 2^-14 |x| (1.3e-4 is above 2 * 2^-14).  fp32 rows look at every feature.  Such groups, and steps without a reciprocal in range, go through code_of.
+    const float z = -m * inv, zk = z - floorf(z) - 0.5f;
+    bool exactly = s < 1e-36f || (kWide ? met : m != 0.f && fabsf(m) < 1.3e-4f * fabsf(hi));
+    if (!kWide && fabsf(zk) < 2e-3f) {
+        const float small = 1.3e-4f * fabsf(m);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) exactly = exactly || (fabsf(x[i]) < small && x[i] != 0.f);
     }
-    return codes;
+    if (exactly) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            codes[w] = 0u;
+            if (s > 0.f) {       // (s = 0: a constant group)
+#pragma unroll
+                for (int i = 0; i < kOctet; ++i) codes[w] |= static_cast<uint32_t>(code_of(x[w * kOctet + i], m, s)) << (4 * i);
+            }
+        }
+    }
+    return word;
 }
 
-// One block per nugget: 8 features a thread and step, kUnroll steps' loads of both rows in flight.  Bound by HBM: it reads
-// the two rows and writes 80 (dh 128) of their 256 bytes a head.
+// One block per nugget.  A thread takes whole groups of 32 features (bf16: 64 bytes in two 32-byte loads), so a group's
+// extremes, step and reciprocal cost it no exchange and are found once; kUnroll groups' loads are in flight together.  Bound by
+// instruction issue (about 13 per feature) ahead of HBM: it reads two rows and writes 80 (dh 128) of their 256 bytes a head.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kGatherThreads, 4)
 gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __restrict__ V, int H, int dh,
                  const int32_t* __restrict__ idx, const __grid_constant__ GatherGroup g, unsigned char* __restrict__ cache_q4,
                  uint32_t* __restrict__ cache_scale, int32_t* __restrict__ cache_pos, int* __restrict__ dev_status) {
-    constexpr int kVecs = kOctet / Vec16<T>::kElems;    // 16-byte loads per octet
-    constexpr int kUnroll = 4 / kVecs;
+    constexpr int kWords = kGroup * static_cast<int>(sizeof(T)) / 4;    // storage words of a group
+    constexpr int kUnroll = 1;
     const int j = g.idx0[0] + static_cast<int>(blockIdx.x);
     int lo = 0, hi = g.nseq;
     while (hi - lo > 1) {
@@ -138,42 +175,36 @@ gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __res
         if (threadIdx.x == 0) atomicOr(dev_status, DODO_DEV_BAD_INDEX);
         return;
     }
-    const int octets = H * dh / kOctet, per_head = dh / kOctet;
+    const int per_head = dh / kGroup, groups = H * per_head;     // of K; as many of V
     const size_t src = (static_cast<size_t>(g.src_row0[b]) + static_cast<size_t>(token)) * static_cast<size_t>(H) * dh * sizeof(T);
     const int dst_row = g.dst_row0[b] + (j - g.idx0[b]);
-    uint32_t* const q4 = reinterpret_cast<uint32_t*>(cache_q4 + static_cast<size_t>(dst_row) * H * dh);
-    uint32_t* const sc = cache_scale + static_cast<size_t>(dst_row) * H * (2 * dh / kGroup);
+    uint4* const q4 = reinterpret_cast<uint4*>(cache_q4 + static_cast<size_t>(dst_row) * H * dh);
+    uint32_t* const sc = cache_scale + static_cast<size_t>(dst_row) * (2 * groups);
     if (threadIdx.x == 0) cache_pos[dst_row] = g.pos_base[b] + token;
 
-    for (int c0 = 0; c0 < octets; c0 += kUnroll * kThreads) {
-        uint4 raw[2][kUnroll][kVecs];
+    for (int i0 = 0; i0 < 2 * groups; i0 += kUnroll * kGatherThreads) {
+        uint32_t raw[kUnroll][kWords];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int c = c0 + u * kThreads + static_cast<int>(threadIdx.x);
+            const int i = i0 + u * kGatherThreads + static_cast<int>(threadIdx.x);
+            if (i < 2 * groups) {
+                const unsigned char* p = (i < groups ? K + src : V + src) + static_cast<size_t>(i < groups ? i : i - groups) * (kWords * 4);
 #pragma unroll
-            for (int e = 0; e < kVecs; ++e) raw[0][u][e] = raw[1][u][e] = make_uint4(0, 0, 0, 0);
-            if (c < octets) {
-                const size_t at = src + static_cast<size_t>(c) * kOctet * sizeof(T);
-                load_octet<T>(K + at, raw[0][u]);
-                load_octet<T>(V + at, raw[1][u]);
+                for (int w = 0; w < kWords; w += 8) load32(p + 4 * w, raw[u] + w);
             }
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int c = c0 + u * kThreads + static_cast<int>(threadIdx.x);
-            const int h = c / per_head, w = c - h * per_head;   // head and word within the head's K (or V) codes
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                float x[kOctet];
-#pragma unroll
-                for (int e = 0; e < kVecs; ++e) Vec16<T>::unpack(raw[kv][u][e], x + e * Vec16<T>::kElems);
-                uint32_t word;
-                const uint32_t codes = quantise(x, word);
-                if (c < octets) {
-                    q4[h * (dh / 4) + kv * (dh / 8) + w] = codes;
-                    if ((w & 3) == 0) sc[(h * 2 + kv) * (dh / kGroup) + w / 4] = word;
-                }
-            }
+            const int i = i0 + u * kGatherThreads + static_cast<int>(threadIdx.x);
+            if (i >= 2 * groups) break;
+            float x[kGroup];
+            widen<T>(raw[u], x);
+            uint32_t codes[4];
+            const uint32_t word = quantise<sizeof(T) == 4>(x, codes);
+            const int kv = i < groups ? 0 : 1, c = i - kv * groups, h = c / per_head;
+            const int at = (h * 2 + kv) * per_head + (c - h * per_head);
+            q4[at] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+            sc[at] = word;
         }
     }
 }
@@ -247,7 +278,7 @@ int dodo_launch_gather_q4(dodo_ctx* ctx, const void* K, const void* V, int dtype
     const unsigned char* k = static_cast<const unsigned char*>(K);
     const unsigned char* v = static_cast<const unsigned char*>(V);
     unsigned char* q4 = static_cast<unsigned char*>(cache_q4);
-    const dim3 grid(static_cast<unsigned>(total)), block(kThreads);
+    const dim3 grid(static_cast<unsigned>(total)), block(kGatherThreads);
     const cudaError_t e = dtype == DODO_BF16
         ? dodo_launch_dependent(gather_q4_kernel<__nv_bfloat16>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status)
         : dodo_launch_dependent(gather_q4_kernel<float>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status);
