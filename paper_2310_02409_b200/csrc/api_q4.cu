@@ -156,7 +156,7 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     if (cap_status != cudaStreamCaptureStatusActive) cap_id = 0;
     for (int gi = 0; gi < ngroups && rc == DODO_OK; ++gi) {
         const bool early = ctx->cache_clean && ctx->clean_capture_id == cap_id;
-        rc = dodo_launch_attend_q4(ctx, dtype, H, dh, sm_scale, plan, groups[gi], Q, cache_q4, cache_scale, cache_pos, locK, locV, O, lse,
+        rc = dodo_launch_attend_q4(ctx, dtype, H, dh, sm_scale, plan, groups[gi], Q, cache_q4, cache_scale, cache_rows, cache_pos, locK, locV, O, lse,
                                    static_cast<float*>(workspace), ctx->tickets, early, st);
         if (rc == DODO_OK) {
             ctx->cache_clean = true;

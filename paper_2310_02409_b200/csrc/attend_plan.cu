@@ -18,17 +18,18 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
-// [rows, H*dh] bf16 tensor, box of 64 elements x box_rows rows, 128-byte swizzle
-int encode_sw128(void* fn, CUtensorMap* map, const void* base, int width, int rows, int box_rows, char* err,
-                 size_t err_len) {
+// [rows, width] tensor of bf16 (box of 64 elements x box_rows rows, 128-byte swizzle) or bytes (box of box_width)
+enum MapKind { kBf16 = 0, kBytes32 = 1, kBytes128 = 2 };
+int encode_rows(void* fn, CUtensorMap* map, const void* base, int kind, int width, int rows, int box_rows, char* err,
+                size_t err_len) {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {dims[0] * 2};
-    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
+    const cuuint64_t strides[1] = {dims[0] * (kind == kBf16 ? 2 : 1)};
+    const cuuint32_t box[2] = {kind == kBf16 ? 64u : kind == kBytes32 ? 32u : 128u, static_cast<cuuint32_t>(box_rows)};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult r = reinterpret_cast<EncodeTiledFn>(fn)(
-        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        map, kind == kBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, kind == kBytes32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         if (err != nullptr && err_len > 0) snprintf(err, err_len, "cuTensorMapEncodeTiled failed with %d", static_cast<int>(r));
         return DODO_ERR_CUDA;
@@ -38,28 +39,35 @@ int encode_sw128(void* fn, CUtensorMap* map, const void* base, int width, int ro
 }  // namespace
 
 namespace {
-// encode_sw128 through the context's small cache: serving loops pass the same buffers call after call
-int cached_sw128(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_rows, char* err,
-                 size_t err_len) {
+// encode_rows through the context's small cache: serving loops pass the same buffers call after call
+int cached_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int kind, int width, int rows, int box_rows, char* err,
+                size_t err_len) {
     const int n = static_cast<int>(sizeof ctx->map_cache / sizeof ctx->map_cache[0]);
     for (int i = 0; i < n; ++i) {
         const dodo_ctx::MapEntry& e = ctx->map_cache[i];
-        if (e.base == base && e.rows == rows && e.width == width && e.box_rows == box_rows && base != nullptr) {
+        if (e.base == base && e.rows == rows && e.width == width && e.box_rows == box_rows && e.kind == kind && base != nullptr) {
             *map = e.map;
             return DODO_OK;
         }
     }
-    const int rc = encode_sw128(ctx->encode_tiled, map, base, width, rows, box_rows, err, err_len);
+    const int rc = encode_rows(ctx->encode_tiled, map, base, kind, width, rows, box_rows, err, err_len);
     if (rc != DODO_OK) return rc;
     dodo_ctx::MapEntry& e = ctx->map_cache[ctx->map_next];
     ctx->map_next = (ctx->map_next + 1) % n;
-    e.base = base; e.rows = rows; e.width = width; e.box_rows = box_rows; e.map = *map;
+    e.base = base; e.rows = rows; e.width = width; e.box_rows = box_rows; e.kind = kind; e.map = *map;
     return DODO_OK;
+}
+int cached_sw128(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_rows, char* err,
+                 size_t err_len) {
+    return cached_rows(ctx, map, base, kBf16, width, rows, box_rows, err, err_len);
 }
 }  // namespace
 
 int dodo_encode_bf16_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_rows) {
     return cached_sw128(ctx, map, base, width, rows, box_rows, ctx->err, sizeof ctx->err);
+}
+int dodo_encode_byte_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_width, int box_rows) {
+    return cached_rows(ctx, map, base, box_width == 32 ? kBytes32 : kBytes128, width, rows, box_rows, ctx->err, sizeof ctx->err);
 }
 
 int dodo_dense_encode_maps(dodo_ctx* ctx, const AttendShape& s, const void* Q, int q_rows, const void* cacheK,

@@ -12,6 +12,7 @@
 // takes the 2^23 off, and the weight 16^i is folded into the query feature (for K) and divided out of the accumulator at
 // the end (for V), both powers of two and exact.  That is 2.1 instructions per code and product.
 #include "dodo_internal.cuh"
+#include "sm100_ptx.cuh"
 #include <type_traits>
 
 namespace {
@@ -55,6 +56,60 @@ template <> __device__ __forceinline__ Codes<2> load_codes<2>(const uint32_t* p)
     Codes<2> c;
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(c.w[0]), "=r"(c.w[1]) : "l"(p));
     return c;
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ void write_out(T* O, float* lse, size_t orow, int dim, float M, float L, float o) {
+    store_out(O + orow * DH + dim, L != 0.f ? o / L : 0.f);   // (a NaN sum stays one)
+    if (lse != nullptr && dim == 0) lse[orow] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+// The last chunk of a (query tile, head) to arrive merges the partials of all of them by log-sum-exp; nobody waits.
+template <typename T, int DH>
+__device__ __forceinline__ void merge_chunks(const AttendSeq& sq, int H, int qtile, int h, int q_first, int nq,
+                                             int nchunk, const float* partials, int* tickets, int* flag, T* O, float* lse) {
+    constexpr int RED = DH + 2;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int* tk = tickets + sq.tick0 + qtile * H + h;
+        const int t = atomicAdd(tk, 1);
+        *flag = t == nchunk - 1;
+        if (t == nchunk - 1) *tk = 0;  // leave the counter clean for the next launch
+    }
+    __syncthreads();
+    if (*flag == 0) return;
+    __threadfence();
+    for (int i = threadIdx.x; i < nq * DH; i += kThreads) {
+        const int q2 = i / DH, dim = i % DH;
+        const float* pr = partials + (static_cast<size_t>(sq.part0) + (static_cast<size_t>(q_first + q2) * H + h) * nchunk) * RED;
+        float M = kNeg, L = 0.f, o = 0.f;
+        for (int c0 = 0; c0 < nchunk; c0 += 8) {   // eight chunks' loads in flight together
+            float mv[8], lv[8], ov[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const bool live = c0 + u < nchunk;
+                const float* pc = pr + static_cast<size_t>(live ? c0 + u : 0) * RED;
+                mv[u] = live ? __ldcg(pc + DH) : kNeg;
+                lv[u] = live ? __ldcg(pc + DH + 1) : 0.f;
+                ov[u] = live ? __ldcg(pc + dim) : 0.f;
+            }
+            float M_new = M;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) M_new = fmaxf(M_new, mv[u]);
+            const float corr = ex2_approx(M - M_new);
+            M = M_new;
+            L *= corr;
+            o *= corr;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float wgt = ex2_approx(mv[u] - M);
+                L = fmaf(lv[u], wgt, L);
+                o = fmaf(ov[u], wgt, o);
+            }
+        }
+        write_out<T, DH>(O, lse, static_cast<size_t>(sq.q_row0 + q_first + q2) * H + h, dim, M, L, o);
+    }
 }
 
 struct Q4Source {
@@ -380,11 +435,6 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
     __syncthreads();
 
     const int qrow0 = sq.q_row0 + q_first;
-    auto write_out = [&](int q2, int dim, float M, float L, float o) {
-        const size_t orow = static_cast<size_t>(qrow0 + q2) * H + h;
-        store_out(O + orow * DH + dim, L != 0.f ? o / L : 0.f);   // (a NaN sum stays one)
-        if (lse != nullptr && dim == 0) lse[orow] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
-    };
     for (int i = tid; i < QT * DH; i += kThreads) {
         const int q2 = i / DH, dim = i % DH;
         if (q2 >= nq) continue;
@@ -399,7 +449,7 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
             o = fmaf(red[w][q2][dim], wgt, o);
         }
         if (nchunk == 1) {
-            write_out(q2, dim, M, L, o);
+            write_out<T, DH>(O, lse, static_cast<size_t>(qrow0 + q2) * H + h, dim, M, L, o);
         } else {
             float* pr = partials + (static_cast<size_t>(sq.part0) + (static_cast<size_t>(q_first + q2) * H + h) * nchunk + chunk) * RED;
             pr[dim] = o;
@@ -408,49 +458,437 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
     }
     if (nchunk == 1) return;
 
-    // ---- the last chunk to arrive merges the partials of its (query tile, head); nobody waits ----------------------------
-    __threadfence();
-    __syncthreads();
+    merge_chunks<T, DH>(sq, H, qtile, h, q_first, nq, nchunk, partials, tickets, &s_flag, O, lse);
+}
+
+// ---- one bf16 query per sequence, head size 128 --------------------------------------------------------------------------
+// The kernel above spends 40 warp instructions per cached key and head, most of them on turning codes into floats and
+// multiplying them one by one.  Here the warp-level matrix instruction takes the codes nearly as they lie in memory: a pair of
+// nibbles masked out of a word, read as two bf16 numbers, is c 2^-133 (low nibble of a byte) or 16 c 2^-133 (high nibble) exactly,
+// since bf16 bit patterns below 256 are the multiples of 2^-133; so five instructions (four masks, one shift) make eight codes
+// into operands.  Scale: the other operand carries a power of two, the products stay in the normal range of fp32.
+//   Q.K   A = 16 keys x 16 features of codes, B = the query in up to four columns, column n holding only the features of group n
+//         (lane quad t owns group t's features, so a column's lanes are zero elsewhere): one accumulator gathers the four groups'
+//         sums of q c apart, exact products summed in fp32; steps and minima enter afterwards.
+//   P.V   A = 16 features x 16 keys (words of two keys interleaved by byte permutation), B = p s per key: column n holds group
+//         n & 3, its bf16 value for n < 4 and what that rounding left for n >= 4, so that p s keeps 16 bits.  Of the accumulators a
+//         row's own group is used, the rest is ignored.
+// That is about 14 instructions and one matrix instruction (8.4 cycles of a scheduler's pipe, measured) per key and head.
+// Rows come through shared memory: a ninth warp brings 128 keys at a time (their codes and group words of this head, 20 KB) with two
+// tensor copies into a ring of four stages, so that up to 160 KB per SM are on their way whatever the consumers do; loads into
+// registers a tile or two ahead left HBM at 2.5 TB/s.
+constexpr int kQExp = 64;        // the query is shifted to a largest feature near 2^64
+constexpr int kBackExp = 64;     // ... undone in two steps, the first of 2^64
+constexpr int kPExp = 40;        // power of two on p s
+
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+struct TokenMaps { CUtensorMap q4, scale; };   // boxes of 128 and 32 bytes x kRound rows
+constexpr int kRound = 16 * kWarps;            // keys of a stage: 16 per warp
+constexpr int kTokenStages = 4;
+constexpr int kCodeBytes = kRound * 128, kStageBytes = kCodeBytes + kRound * 32;
+constexpr int kTokenThreads = kThreads + 32;
+
+__global__ void __launch_bounds__(kTokenThreads, 2)
+attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant__ TokenMaps maps, const Q4Source src,
+                       const __grid_constant__ AttendGroup g, const int32_t* __restrict__ cache_pos, int H, float scale_log2,
+                       __nv_bfloat16* __restrict__ O, float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets,
+                       int early_cache, int* __restrict__ dev_status) {
+    using namespace sm100;
+    constexpr int DH = 128, RED = DH + 2;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ float red[2 * kWarps][RED];                 // a warp's cached keys, its local keys
+    __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
+    __shared__ int s_flag;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r = lane >> 2, t = lane & 3;                 // fragment row (key, feature word or column) and quad lane
+    const int bid = static_cast<int>(blockIdx.x);
+    int b;
+    if (g.uniform_ctas > 0) {
+        b = bid / g.uniform_ctas;
+    } else {
+        b = 0;
+#pragma unroll 8
+        for (int i = 1; i < DODO_GROUP; ++i) b += (i < g.nseq && g.cta0[i] <= bid) ? 1 : 0;
+    }
+    const AttendSeq sq = g.seq[b];
+    const int r0 = bid - g.cta0[b];
+    const int nchunk = sq.nchunk, chunk = r0 % nchunk, h = r0 / nchunk;    // one query: H units of nchunk blocks
+    const int qpos = sq.q_pos0;
+    const int l_vis = max(0, min(sq.l_len, qpos - sq.l_pos0 + 1));
+    const int nt_c = (sq.c_len + kRound - 1) / kRound;                     // (the planner's tile is kRound keys)
+    const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
+    const int c_begin = min(sq.c_len, t_begin * kRound), c_end = min(sq.c_len, t_end * kRound);
+    const int l_begin = min(l_vis, max(0, t_begin - nt_c) * kRound), l_end = min(l_vis, max(0, t_end - nt_c) * kRound);
+    const int n_c = c_end - c_begin, n_l = l_end - l_begin;
+    const int c_row = sq.c_row0 + c_begin, l_row = sq.l_row0 + l_begin;
+    const int rounds = (n_c + kRound - 1) / kRound;
+
     if (tid == 0) {
-        int* tk = tickets + sq.tick0 + qtile * H + h;
-        const int t = atomicAdd(tk, 1);
-        s_flag = (t == nchunk - 1);
-        if (s_flag) *tk = 0;  // leave the counter clean for the next launch
+        for (int i = 0; i < kTokenStages; ++i) { mbar_init(&bar_full[i], 1); mbar_init(&bar_free[i], kWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    if (!s_flag) return;
-    __threadfence();
-    for (int i = tid; i < QT * DH; i += kThreads) {
-        const int q2 = i / DH, dim = i % DH;
-        if (q2 >= nq) continue;
-        const float* pr = partials + (static_cast<size_t>(sq.part0) + (static_cast<size_t>(q_first + q2) * H + h) * nchunk) * RED;
-        float M = kNeg, L = 0.f, o = 0.f;
-        for (int c0 = 0; c0 < nchunk; c0 += 8) {   // eight chunks' loads in flight together
-            float mv[8], lv[8], ov[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const bool live = c0 + u < nchunk;
-                const float* pc = pr + static_cast<size_t>(live ? c0 + u : 0) * RED;
-                mv[u] = live ? __ldcg(pc + DH) : kNeg;
-                lv[u] = live ? __ldcg(pc + DH + 1) : 0.f;
-                ov[u] = live ? __ldcg(pc + dim) : 0.f;
+    bool ok = true;
+    if (warp == kWarps) {
+        // ---- producer.  Ahead of the dependency wait (see attend.cu) it copies only when nothing in flight writes a cache -----------
+        if (lane == 0) {
+            auto load_round = [&](int i) {
+                const int st = i % kTokenStages;
+                const uint32_t dst = ring + st * kStageBytes;
+                mbar_expect_tx(&bar_full[st], kStageBytes);
+                tma_load_2d(dst, &maps.q4, h * 128, c_row + i * kRound, &bar_full[st]);
+                tma_load_2d(dst + kCodeBytes, &maps.scale, h * 32, c_row + i * kRound, &bar_full[st]);
+            };
+            const int ahead = min(rounds, kTokenStages);
+            if (early_cache)
+                for (int i = 0; i < ahead; ++i) load_round(i);
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            if (!early_cache)
+                for (int i = 0; i < ahead; ++i) load_round(i);
+            int done = ahead;
+            for (int i = kTokenStages; i < rounds; ++i) {
+                const int st = i % kTokenStages;
+                if (!mbar_wait(&bar_free[st], static_cast<uint32_t>(i / kTokenStages - 1) & 1u)) { ok = false; break; }
+                load_round(i);
+                done = i + 1;
             }
-            float M_new = M;
+            // leave no copy in flight behind (when consumers have given up)
+            for (int i = max(0, done - kTokenStages); i < done; ++i) ok = mbar_wait(&bar_full[i % kTokenStages], static_cast<uint32_t>(i / kTokenStages) & 1u) && ok;
+            if (!ok) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+        }
+    } else {
+    auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
+        for (int i = tid; i < rows * 2; i += kThreads)
+            asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(base + (static_cast<size_t>(row + i / 2) * H + h) * DH) + (i % 2) * 128));
+    };
+    hint_rows(Q, sq.q_row0, 1);
+    hint_rows(static_cast<const __nv_bfloat16*>(src.lK), l_row, min(n_l, kHintKeys));
+    hint_rows(static_cast<const __nv_bfloat16*>(src.lV), l_row, min(n_l, kHintKeys));
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // a warp's tile of a stage: keys 16 warp + ..., in the swizzled rows of 128 bytes (16-byte piece p of row j lies at p ^ (j & 7))
+    struct Tile { uint4 k[2]; uint32_t v[8]; uint2 ks[2], vs[2]; int pos[2]; };
+    const int key0 = 16 * warp;
+    const uint32_t k_at = static_cast<uint32_t>((key0 + r) * 128 + ((t ^ r) << 4));             // row r; row r + 8 is 1024 bytes on
+    const uint32_t s_at = static_cast<uint32_t>(kCodeBytes + (key0 + r) * 32 + (t & 1) * 8);    // row r + 8: 256 bytes on
+    uint32_t v_at[2][2];                                                                        // rows 2 t, 2 t + 1; words r, r + 8
 #pragma unroll
-            for (int u = 0; u < 8; ++u) M_new = fmaxf(M_new, mv[u]);
-            const float corr = ex2_approx(M - M_new);
-            M = M_new;
-            L *= corr;
-            o *= corr;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float wgt = ex2_approx(mv[u] - M);
-                L = fmaf(lv[u], wgt, L);
-                o = fmaf(ov[u], wgt, o);
+        for (int w = 0; w < 2; ++w) {
+            const int row = 2 * t + i, piece = 4 + 2 * w + (r >> 2);
+            v_at[i][w] = static_cast<uint32_t>((key0 + row) * 128 + ((piece ^ row) << 4) + (r & 3) * 4);
+        }
+    auto positions = [&](int i, int* pos) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int j = i * kRound + key0 + r + 8 * e;
+            pos[e] = j < n_c ? __ldg(cache_pos + c_row + j) : 0x7fffffff;
+        }
+    };
+    auto lds32 = [](uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; };
+    auto lds64 = [](uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; };
+    auto lds128 = [](uint32_t a) {
+        uint4 v;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+        return v;
+    };
+    auto read_tile = [&](int st, Tile& x) {
+        const uint32_t base = ring + st * kStageBytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {       // keys r and r + 8: group t's codes of K, words of K groups and V groups 2 (t & 1) + {0, 1}
+            x.k[i] = lds128(base + k_at + 1024u * i);
+            x.ks[i] = lds64(base + s_at + 256u * i);
+            x.vs[i] = lds64(base + s_at + 256u * i + 16u);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {       // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: words r and r + 8 of V's codes
+            x.v[2 * i] = lds32(base + v_at[i & 1][0] + 1024u * (i >> 1));
+            x.v[2 * i + 1] = lds32(base + v_at[i & 1][1] + 1024u * (i >> 1));
+        }
+    };
+
+    // ---- the query as B fragments: lane (n = r, t) holds column n, nonzero where n = t: group t's features -------------------
+    const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0) * H + h) * DH;
+    uint32_t qb[4][2][2];
+    float qsum[2], q_back;      // sums of q over groups 2 (t & 1) + {0, 1}, lanes t < 2; the second step back
+    {
+        float f[32], top = 0.f, mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 32 * t + 8 * i), f + 8 * i);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { top = fmaxf(top, fabsf(f[i])); mine += f[i]; }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // exponent of the largest feature (a query below 2^-62 is shifted less), as powers of two put together bit by bit
+        const int e = max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62);
+        const float shift = __uint_as_float(static_cast<uint32_t>(kQExp - e + 127) << 23);
+        q_back = __uint_as_float(static_cast<uint32_t>(min(133 - kQExp - kBackExp + e + 127, 255)) << 23);
+        const float at0 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2), at1 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2 + 1);
+        qsum[0] = t < 2 ? at0 : 0.f;
+        qsum[1] = t < 2 ? at1 : 0.f;
+        const float s1 = r == t ? shift : 0.f, s16 = s1 * 0.0625f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float* w = f + 8 * i;
+            qb[i][0][0] = two_bf16(w[0] * s1, w[4] * s1);
+            qb[i][0][1] = two_bf16(w[1] * s16, w[5] * s16);
+            qb[i][1][0] = two_bf16(w[2] * s1, w[6] * s1);
+            qb[i][1][1] = two_bf16(w[3] * s16, w[7] * s16);
+        }
+    }
+
+    constexpr float kBack = 18446744073709551616.f;            // 2^kBackExp
+    constexpr float kPScale = 1099511627776.f;                 // 2^kPExp
+    float m = kNeg, l = 0.f, accm[2] = {0.f, 0.f};             // the maximum is the warp's; l and accm are a lane's own rows'
+    float acc[8][4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
+
+    auto reduce = [&](const Tile& x) {
+        // ---- logits of keys r and r + 8 ----------------------------------------------------------------------------
+        float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};     // two accumulators: half the chain
+        const uint32_t ka[4] = {x.k[0].x, x.k[0].y, x.k[0].z, x.k[0].w}, kb[4] = {x.k[1].x, x.k[1].y, x.k[1].z, x.k[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t ha = ka[i] >> 8, hb = kb[i] >> 8;
+            mma16816(d0, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u, qb[i][0][0], qb[i][0][1]);
+            mma16816(d1, ha & 0x000f000fu, hb & 0x000f000fu, ha & 0x00f000f0u, hb & 0x00f000f0u, qb[i][1][0], qb[i][1][1]);
+        }
+        float s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float y0 = ((d0[2 * i] + d1[2 * i]) * kBack) * q_back, y1 = ((d0[2 * i + 1] + d1[2 * i + 1]) * kBack) * q_back;
+            const float st0 = __uint_as_float(x.ks[i].x << 16), lo0 = __uint_as_float(x.ks[i].x & 0xffff0000u);
+            const float st1 = __uint_as_float(x.ks[i].y << 16), lo1 = __uint_as_float(x.ks[i].y & 0xffff0000u);
+            s[i] = fmaf(st0, y0, lo0 * qsum[0]) + fmaf(st1, y1, lo1 * qsum[1]);      // (lanes t >= 2: columns 4 to 7, all zero)
+            s[i] += __shfl_xor_sync(0xffffffffu, s[i], 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = __shfl_sync(0xffffffffu, s[i], lane & ~3) * scale_log2;
+            if (x.pos[i] > qpos) s[i] = kNeg;
+        }
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (top > m + 8.f) {     // the reference moves only when it pays: weights stay below 2^8
+            const float corr = ex2_approx(m - top);
+            m = top;
+            l *= corr;
+            accm[0] *= corr; accm[1] *= corr;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] *= corr;
+        }
+        // ---- weights; p s of this lane's keys and V groups, rounded to bf16 (lanes t >= 2) or what rounding left (t < 2) ---------
+        uint32_t pw[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool see = x.pos[i] <= qpos;                   // a masked key takes no part, whatever its words hold
+            const float p = see ? ex2_approx(s[i] - m) : 0.f;
+            l += p;
+            const float st0 = __uint_as_float(x.vs[i].x << 16), lo0 = __uint_as_float(x.vs[i].x & 0xffff0000u);
+            const float st1 = __uint_as_float(x.vs[i].y << 16), lo1 = __uint_as_float(x.vs[i].y & 0xffff0000u);
+            const float pp = p * kPScale;
+            float a0 = see ? pp * st0 : 0.f, a1 = see ? pp * st1 : 0.f;
+            accm[0] = see ? fmaf(p, lo0, accm[0]) : accm[0];
+            accm[1] = see ? fmaf(p, lo1, accm[1]) : accm[1];
+            const uint32_t w = two_bf16(a0, a1);
+            a0 -= __uint_as_float(w << 16);
+            a1 -= __uint_as_float(w & 0xffff0000u);
+            pw[i] = t < 2 ? two_bf16(a0, a1) : w;
+        }
+        // B fragments: column n = r is group n & 3, rounded part for n < 4; keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+        const int from = (r < 4 ? 2 : 0) + ((r & 3) >> 1);
+        const uint32_t pick = (r & 1) != 0 ? 0x7632u : 0x5410u;
+        const uint32_t b0 = __byte_perm(__shfl_sync(0xffffffffu, pw[0], 8 * t + from), __shfl_sync(0xffffffffu, pw[0], 8 * t + 4 + from), pick);
+        const uint32_t b1 = __byte_perm(__shfl_sync(0xffffffffu, pw[1], 8 * t + from), __shfl_sync(0xffffffffu, pw[1], 8 * t + 4 + from), pick);
+        // ---- P V: nibble j of words r (rows r) and r + 8 (rows r + 8), keys interleaved ---------------------------------------------
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint32_t sel = hf == 0 ? 0x5410u : 0x7632u;
+            const uint32_t wa = __byte_perm(x.v[0], x.v[2], sel), wb = __byte_perm(x.v[1], x.v[3], sel);
+            const uint32_t wc = __byte_perm(x.v[4], x.v[6], sel), wd = __byte_perm(x.v[5], x.v[7], sel);
+            mma16816(acc[4 * hf], wa & 0x000f000fu, wb & 0x000f000fu, wc & 0x000f000fu, wd & 0x000f000fu, b0, b1);
+            mma16816(acc[4 * hf + 1], wa & 0x00f000f0u, wb & 0x00f000f0u, wc & 0x00f000f0u, wd & 0x00f000f0u, b0, b1);
+            const uint32_t ha = wa >> 8, hb = wb >> 8, hc = wc >> 8, hd = wd >> 8;
+            mma16816(acc[4 * hf + 2], ha & 0x000f000fu, hb & 0x000f000fu, hc & 0x000f000fu, hd & 0x000f000fu, b0, b1);
+            mma16816(acc[4 * hf + 3], ha & 0x00f000f0u, hb & 0x00f000f0u, hc & 0x00f000f0u, hd & 0x00f000f0u, b0, b1);
+        }
+    };
+    int next_pos[2];
+    positions(0, next_pos);
+    for (int i = 0; i < rounds; ++i) {
+        const int st = i % kTokenStages;
+        Tile x;
+        x.pos[0] = next_pos[0];
+        x.pos[1] = next_pos[1];
+        if (i + 1 < rounds) positions(i + 1, next_pos);
+        if (__all_sync(0xffffffffu, mbar_wait(&bar_full[st], static_cast<uint32_t>(i / kTokenStages) & 1u)) == 0) { ok = false; break; }
+        if (i * kRound + key0 < n_c) {      // (a warp past the chunk's end has nothing here)
+            read_tile(st, x);
+            reduce(x);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar_free[st]);
+    }
+    if (!ok && lane == 0) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+
+    // ---- the warp's record of its cached keys ----------------------------------------------------------------------------------
+    {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            l += __shfl_xor_sync(0xffffffffu, l, o);
+            accm[0] += __shfl_xor_sync(0xffffffffu, accm[0], o);
+            accm[1] += __shfl_xor_sync(0xffffffffu, accm[1], o);
+        }
+        constexpr int kExp = 133 - kPExp;                          // 93: codes come out as c 2^-133 p s 2^40
+        const float back = __uint_as_float(static_cast<uint32_t>(kExp + 127) << 23);
+        const bool second = r >= 4;                                // of the two groups in this lane's accumulator columns
+        const float bias = second ? accm[1] : accm[0];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // lanes t even hold rows r (groups 0, 1), odd ones rows r + 8 (groups 2, 3); t and t + 2 the two parts of p s
+            float v = (t & 1) == 0 ? (second ? acc[j][1] : acc[j][0]) : (second ? acc[j][3] : acc[j][2]);
+            v += __shfl_xor_sync(0xffffffffu, v, 2);
+            v = fmaf(v * ((j & 1) != 0 ? 0.0625f : 1.f), back, bias);
+            if (t < 2) red[warp][8 * (r + 8 * t) + j] = v;
+        }
+        if (lane == 0) { red[warp][DH] = m; red[warp][DH + 1] = l; }
+    }
+
+    // ---- local keys: eight lanes a key, 16 features a lane, two keys a bundle and round ---------------------------------------------
+    {
+        constexpr int UL = 2, NB = kThreads / 8;
+        const int bundle = tid >> 3, lig = tid & 7;
+        float2 q2[8], a2[8];
+        {
+            float f[16];
+            Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 16 * lig), f);
+            Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 16 * lig + 8), f + 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q2[i] = make_float2(f[2 * i] * scale_log2, f[2 * i + 1] * scale_log2);
+                a2[i] = make_float2(0.f, 0.f);
             }
         }
-        write_out(q2, dim, M, L, o);
+        float ml = kNeg, ll = 0.f;
+        for (int base = 0; base < n_l; base += NB * UL) {
+            uint4 kv[UL][2], vv[UL][2];
+            float s[UL];
+            bool see[UL];
+#pragma unroll
+            for (int u = 0; u < UL; ++u) {
+                const int j = base + u * NB + bundle;
+                see[u] = j < n_l;                               // (rows past the query's own position are not in the window)
+                kv[u][0] = kv[u][1] = vv[u][0] = vv[u][1] = make_uint4(0, 0, 0, 0);
+                if (see[u]) {
+                    const size_t at = (static_cast<size_t>(l_row + j) * H + h) * DH + 16 * lig;
+                    const uint4* pk = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(src.lK) + at);
+                    const uint4* pv = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(src.lV) + at);
+                    kv[u][0] = __ldg(pk); kv[u][1] = __ldg(pk + 1);
+                    vv[u][0] = __ldg(pv); vv[u][1] = __ldg(pv + 1);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < UL; ++u) {
+                float f[16];
+                Vec16<__nv_bfloat16>::unpack(kv[u][0], f);
+                Vec16<__nv_bfloat16>::unpack(kv[u][1], f + 8);
+                float2 d = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d = __ffma2_rn(q2[i], make_float2(f[2 * i], f[2 * i + 1]), d);
+                s[u] = d.x + d.y;
+            }
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+                for (int u = 0; u < UL; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+            float m_new = ml;
+#pragma unroll
+            for (int u = 0; u < UL; ++u) {
+                if (!see[u]) s[u] = kNeg;
+                m_new = fmaxf(m_new, s[u]);
+            }
+            const float corr = ex2_approx(ml - m_new);
+            ml = m_new;
+            ll *= corr;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a2[i] = __fmul2_rn(a2[i], make_float2(corr, corr));
+#pragma unroll
+            for (int u = 0; u < UL; ++u) {
+                const float p = see[u] ? ex2_approx(s[u] - m_new) : 0.f;
+                ll += p;
+                float f[16];
+                Vec16<__nv_bfloat16>::unpack(vv[u][0], f);
+                Vec16<__nv_bfloat16>::unpack(vv[u][1], f + 8);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a2[i] = __ffma2_rn(make_float2(p, p), make_float2(f[2 * i], f[2 * i + 1]), a2[i]);
+            }
+        }
+        // the warp's four bundles: halving exchanges over lane bits 3 and 4
+        float M = fmaxf(ml, __shfl_xor_sync(0xffffffffu, ml, 8));
+        M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
+        const float f = ex2_approx(ml - M);
+        ll *= f;
+        ll += __shfl_xor_sync(0xffffffffu, ll, 8);
+        ll += __shfl_xor_sync(0xffffffffu, ll, 16);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { v[2 * i] = a2[i].x * f; v[2 * i + 1] = a2[i].y * f; }
+        const bool up8 = (lane & 8) != 0, up16 = (lane & 16) != 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float give = up8 ? v[i] : v[8 + i], keep = up8 ? v[8 + i] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float give = up16 ? v[i] : v[4 + i], keep = up16 ? v[4 + i] : v[i];
+            red[kWarps + warp][16 * lig + (up8 ? 8 : 0) + (up16 ? 4 : 0) + i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+        }
+        if (lane == 0) { red[kWarps + warp][DH] = M; red[kWarps + warp][DH + 1] = ll; }
     }
+    }       // (consumers)
+    __syncthreads();
+    if (tid < DH) {
+        float M = kNeg;
+#pragma unroll
+        for (int w = 0; w < 2 * kWarps; ++w) M = fmaxf(M, red[w][DH]);
+        float L = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < 2 * kWarps; ++w) {
+            const float wgt = ex2_approx(red[w][DH] - M);
+            L = fmaf(red[w][DH + 1], wgt, L);
+            o = fmaf(red[w][tid], wgt, o);
+        }
+        if (nchunk == 1) {
+            write_out<__nv_bfloat16, DH>(O, lse, static_cast<size_t>(sq.q_row0) * H + h, tid, M, L, o);
+        } else {
+            float* pr = partials + (static_cast<size_t>(sq.part0) + static_cast<size_t>(h) * nchunk + chunk) * RED;
+            pr[tid] = o;
+            if (tid == 0) { pr[DH] = M; pr[DH + 1] = L; }
+        }
+    }
+    if (nchunk == 1) return;
+    merge_chunks<__nv_bfloat16, DH>(sq, H, 0, h, 0, 1, nchunk, partials, tickets, &s_flag, O, lse);
 }
 
 template <typename T, int DH, int QT, int FPL, int U>
@@ -475,14 +913,37 @@ int launch_qt(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: query tile %d is not built", qt);
 }
 
+int launch_token(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const void* Q, const Q4Source& src, int cache_rows,
+                 const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
+    TokenMaps maps;
+    memset(&maps, 0, sizeof maps);
+    if (cache_rows > 0) {
+        int rc = dodo_encode_byte_rows(ctx, &maps.q4, src.q4, H * 128, cache_rows, 128, kRound);
+        if (rc == DODO_OK) rc = dodo_encode_byte_rows(ctx, &maps.scale, src.scale, H * 32, cache_rows, 32, kRound);
+        if (rc != DODO_OK) return rc;
+    }
+    const size_t smem = static_cast<size_t>(kTokenStages) * kStageBytes + 1024;
+    if (!ctx->q4_attr_set) {
+        const cudaError_t e = cudaFuncSetAttribute(attend_q4_token_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "4-bit attend shared-memory attribute");
+        ctx->q4_attr_set = true;
+    }
+    return dodo_check_cuda(ctx, dodo_launch_dependent(attend_q4_token_kernel, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kTokenThreads), smem, st,
+                                                      static_cast<const __nv_bfloat16*>(Q), maps, src, g, cache_pos, H, sm_scale * 1.4426950408889634f,
+                                                      static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
+                           "4-bit attend launch");
+}
+
 }  // namespace
 
 int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const AttendPlan& plan,
-                          const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale,
+                          const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale, int cache_rows,
                           const int32_t* cache_pos, const void* locK, const void* locV, void* O, float* lse,
                           float* partials, int* tickets, bool early_cache, cudaStream_t st) {
     if (g.cta0[g.nseq] == 0) return DODO_OK;
     const Q4Source src = {static_cast<const uint32_t*>(cache_q4), cache_scale, locK, locV};
+    if (dtype == DODO_BF16 && dh == 128 && plan.qt == 1)     // (plan.qt 1: no sequence has more than one query)
+        return launch_token(ctx, H, sm_scale, g, Q, src, cache_rows, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_BF16 && dh == 128)
         return launch_qt<__nv_bfloat16, 128>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_BF16 && dh == 64)

@@ -31,9 +31,10 @@ struct dodo_ctx {
     int dense_balance;          // 0 auto, 1 always, 2 never, 3 always but not in step: key tiles balanced over the resident blocks
     void* encode_tiled;         // cuTensorMapEncodeTiled, fetched through the runtime
     // recently encoded tensor maps (a map depends only on these host values, so reuse is exact)
-    struct MapEntry { const void* base; int rows, width, box_rows; CUtensorMap map; } map_cache[16];
+    struct MapEntry { const void* base; int rows, width, box_rows, kind; CUtensorMap map; } map_cache[16];
     int map_next;               // round-robin replacement
     bool dense_attr_set[4];     // shared-memory attribute of the four forms of the tensor-core kernel
+    bool q4_attr_set;           // ... and of the 4-bit single-query kernel
     bool backward_attr_set[6];  // ... and of the kernels of attend's gradient
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
@@ -84,6 +85,8 @@ int dodo_score_mlp_reduce_rows();          // rows per block of the fused reduct
 int dodo_score_mlp_fused_max_tokens();     // longer sequences are selected by a launch of their own
 // tensor map of a [rows, width] bf16 row-major array: box of 64 elements x box_rows rows, 128-byte swizzle (cached)
 int dodo_encode_bf16_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_rows);
+// ... of a [rows, width] byte array: box of box_width (32: no swizzle, 128: 128-byte swizzle) bytes x box_rows rows (cached)
+int dodo_encode_byte_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_width, int box_rows);
 
 // ---- threshold selection ----------------------------------------------------------------------
 struct ThresholdGroup {
@@ -252,9 +255,9 @@ struct DenseGather {
 int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps,
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
-// The streaming kernel over a 4-bit cache: launch as above, the cache as codes and group words
+// The streaming kernels over a 4-bit cache: launch as above, the cache (cache_rows rows) as codes and group words
 int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const AttendPlan& plan,
-                          const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale,
+                          const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale, int cache_rows,
                           const int32_t* cache_pos, const void* locK, const void* locV, void* O, float* lse,
                           float* partials, int* tickets, bool early_cache, cudaStream_t st);
 int dodo_attend_tile_keys(int dtype, int dh);
