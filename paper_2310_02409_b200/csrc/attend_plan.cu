@@ -109,6 +109,7 @@ void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& p
         tot.work += qtiles * s.H * seq_tiles(s, b, TK);
     }
     tot.target = target_ctas;
+    tot.min_chunk = 1;
     // split the keys only while there are too few (query tile, head) units to fill the device
     tot.split = tot.units < tot.target && tot.work > tot.units;
 }
@@ -131,8 +132,8 @@ void dodo_attend_plan_group(const AttendShape& s, const AttendPlan& plan, Attend
         if (tot.split && tiles > 1) {
             // share of the target proportional to this sequence's work, rounded
             int64_t want = (static_cast<int64_t>(tiles) * tot.target + tot.work / 2) / tot.work;
+            if (want > tiles / tot.min_chunk) want = tiles / tot.min_chunk;
             if (want < 1) want = 1;
-            if (want > tiles) want = tiles;
             const int ct = static_cast<int>((tiles + want - 1) / want);
             nchunk = (tiles + ct - 1) / ct;
         }

@@ -474,11 +474,13 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
 //         n & 3, its bf16 value for n < 4 and what that rounding left for n >= 4, so that p s keeps 16 bits.  Of the accumulators a
 //         row's own group is used, the rest is ignored.
 // That is about 14 instructions and one matrix instruction (8.4 cycles of a scheduler's pipe, measured) per key and head.
-// Rows come through shared memory: a ninth warp brings 128 keys at a time (their codes and group words of this head, 20 KB) with two
-// tensor copies into a ring of four stages, so that up to 160 KB per SM are on their way whatever the consumers do; loads into
-// registers a tile or two ahead left HBM at 2.5 TB/s.
+// Rows come through shared memory: a fifth warp brings 64 keys at a time (their codes and group words of this head, 10 KB) with two
+// tensor copies into a ring of four stages, so that 120 KB per SM are on their way whatever the consumers do; loads into
+// registers a tile or two ahead left HBM at 2.5 TB/s.  Four consumers and three blocks per SM: with more warps a block two blocks
+// fit, registers are rounded down to 96 (five warps on one scheduler) and a ragged batch balances worse (16 sequences, 52 to 3277
+// rows: 25.4 against 28.4 us).  What bounds it is instruction issue next to HBM: the same kernel without the arithmetic takes 20 us
+// for 16,384 rows of 40 heads (5.4 TB/s) where this takes 25.
 constexpr int kQExp = 64;        // the query is shifted to a largest feature near 2^64
-constexpr int kBackExp = 64;     // ... undone in two steps, the first of 2^64
 constexpr int kPExp = 40;        // power of two on p s
 
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -491,20 +493,21 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
 }
 
 struct TokenMaps { CUtensorMap q4, scale; };   // boxes of 128 and 32 bytes x kRound rows
-constexpr int kRound = 16 * kWarps;            // keys of a stage: 16 per warp
-constexpr int kTokenStages = 4;
-constexpr int kCodeBytes = kRound * 128, kStageBytes = kCodeBytes + kRound * 32;
-constexpr int kTokenThreads = kThreads + 32;
+constexpr int kTokenWarps = 4;                // consumers; one more warp brings the rows
+constexpr int kConsumers = 32 * kTokenWarps, kTokenThreads = kConsumers + 32;
+constexpr int kRound = 16 * kTokenWarps;       // keys of a stage: 16 per warp
+constexpr int kTokenStages = 4, kTokenBlocks = 3;
+constexpr int kCodeBytes = kRound * 128, kStageBytes = (kCodeBytes + kRound * 32 + 1023) / 1024 * 1024;
 
-__global__ void __launch_bounds__(kTokenThreads, 2)
+__global__ void __launch_bounds__(kTokenThreads, kTokenBlocks)
 attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant__ TokenMaps maps, const Q4Source src,
-                       const __grid_constant__ AttendGroup g, const int32_t* __restrict__ cache_pos, int H, float scale_log2,
+                       const __grid_constant__ AttendGroup g, const int32_t* __restrict__ cache_pos, int H, float scale_log2, int TK,
                        __nv_bfloat16* __restrict__ O, float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets,
                        int early_cache, int* __restrict__ dev_status) {
     using namespace sm100;
     constexpr int DH = 128, RED = DH + 2;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ float red[2 * kWarps][RED];                 // a warp's cached keys, its local keys
+    __shared__ float red[2 * kTokenWarps][RED];                 // a warp's cached keys, its local keys
     __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
     __shared__ int s_flag;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -525,28 +528,28 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     const int nchunk = sq.nchunk, chunk = r0 % nchunk, h = r0 / nchunk;    // one query: H units of nchunk blocks
     const int qpos = sq.q_pos0;
     const int l_vis = max(0, min(sq.l_len, qpos - sq.l_pos0 + 1));
-    const int nt_c = (sq.c_len + kRound - 1) / kRound;                     // (the planner's tile is kRound keys)
+    const int nt_c = (sq.c_len + TK - 1) / TK;                             // planning tiles of TK keys
     const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
-    const int c_begin = min(sq.c_len, t_begin * kRound), c_end = min(sq.c_len, t_end * kRound);
-    const int l_begin = min(l_vis, max(0, t_begin - nt_c) * kRound), l_end = min(l_vis, max(0, t_end - nt_c) * kRound);
+    const int c_begin = min(sq.c_len, t_begin * TK), c_end = min(sq.c_len, t_end * TK);
+    const int l_begin = min(l_vis, max(0, t_begin - nt_c) * TK), l_end = min(l_vis, max(0, t_end - nt_c) * TK);
     const int n_c = c_end - c_begin, n_l = l_end - l_begin;
     const int c_row = sq.c_row0 + c_begin, l_row = sq.l_row0 + l_begin;
     const int rounds = (n_c + kRound - 1) / kRound;
 
     if (tid == 0) {
-        for (int i = 0; i < kTokenStages; ++i) { mbar_init(&bar_full[i], 1); mbar_init(&bar_free[i], kWarps); }
+        for (int i = 0; i < kTokenStages; ++i) { mbar_init(&bar_full[i], 1); mbar_init(&bar_free[i], kTokenWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
     bool ok = true;
-    if (warp == kWarps) {
+    if (warp == kTokenWarps) {
         // ---- producer.  Ahead of the dependency wait (see attend.cu) it copies only when nothing in flight writes a cache -----------
         if (lane == 0) {
             auto load_round = [&](int i) {
                 const int st = i % kTokenStages;
                 const uint32_t dst = ring + st * kStageBytes;
-                mbar_expect_tx(&bar_full[st], kStageBytes);
+                mbar_expect_tx(&bar_full[st], kCodeBytes + kRound * 32);
                 tma_load_2d(dst, &maps.q4, h * 128, c_row + i * kRound, &bar_full[st]);
                 tma_load_2d(dst + kCodeBytes, &maps.scale, h * 32, c_row + i * kRound, &bar_full[st]);
             };
@@ -570,7 +573,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
         }
     } else {
     auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
-        for (int i = tid; i < rows * 2; i += kThreads)
+        for (int i = tid; i < rows * 2; i += kConsumers)
             asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(base + (static_cast<size_t>(row + i / 2) * H + h) * DH) + (i % 2) * 128));
     };
     hint_rows(Q, sq.q_row0, 1);
@@ -580,7 +583,6 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // a warp's tile of a stage: keys 16 warp + ..., in the swizzled rows of 128 bytes (16-byte piece p of row j lies at p ^ (j & 7))
-    struct Tile { uint4 k[2]; uint32_t v[8]; uint2 ks[2], vs[2]; int pos[2]; };
     const int key0 = 16 * warp;
     const uint32_t k_at = static_cast<uint32_t>((key0 + r) * 128 + ((t ^ r) << 4));             // row r; row r + 8 is 1024 bytes on
     const uint32_t s_at = static_cast<uint32_t>(kCodeBytes + (key0 + r) * 32 + (t & 1) * 8);    // row r + 8: 256 bytes on
@@ -606,25 +608,10 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
         return v;
     };
-    auto read_tile = [&](int st, Tile& x) {
-        const uint32_t base = ring + st * kStageBytes;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {       // keys r and r + 8: group t's codes of K, words of K groups and V groups 2 (t & 1) + {0, 1}
-            x.k[i] = lds128(base + k_at + 1024u * i);
-            x.ks[i] = lds64(base + s_at + 256u * i);
-            x.vs[i] = lds64(base + s_at + 256u * i + 16u);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {       // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: words r and r + 8 of V's codes
-            x.v[2 * i] = lds32(base + v_at[i & 1][0] + 1024u * (i >> 1));
-            x.v[2 * i + 1] = lds32(base + v_at[i & 1][1] + 1024u * (i >> 1));
-        }
-    };
-
     // ---- the query as B fragments: lane (n = r, t) holds column n, nonzero where n = t: group t's features -------------------
     const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0) * H + h) * DH;
     uint32_t qb[4][2][2];
-    float qsum[2], q_back;      // sums of q over groups 2 (t & 1) + {0, 1}, lanes t < 2; the second step back
+    float qsum[2], q_back;      // sums of q over groups 2 (t & 1) + {0, 1}, lanes t < 2; what undoes the shifts, with the softmax scale
     {
         float f[32], top = 0.f, mine = 0.f;
 #pragma unroll
@@ -633,13 +620,14 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
         for (int i = 0; i < 32; ++i) { top = fmaxf(top, fabsf(f[i])); mine += f[i]; }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // exponent of the largest feature (a query below 2^-62 is shifted less), as powers of two put together bit by bit
-        const int e = max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62);
+        // exponent of the largest feature, as powers of two put together bit by bit; a query outside 2^-62 .. 2^57 is shifted less
+        // or more, so that both powers stay normal numbers (its products still fit: codes end at 15, q at 2^128 2^7)
+        const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62), 57);
         const float shift = __uint_as_float(static_cast<uint32_t>(kQExp - e + 127) << 23);
-        q_back = __uint_as_float(static_cast<uint32_t>(min(133 - kQExp - kBackExp + e + 127, 255)) << 23);
+        q_back = __uint_as_float(static_cast<uint32_t>(133 - kQExp + e + 127) << 23) * scale_log2;
         const float at0 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2), at1 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2 + 1);
-        qsum[0] = t < 2 ? at0 : 0.f;
-        qsum[1] = t < 2 ? at1 : 0.f;
+        qsum[0] = t < 2 ? at0 * scale_log2 : 0.f;
+        qsum[1] = t < 2 ? at1 * scale_log2 : 0.f;
         const float s1 = r == t ? shift : 0.f, s16 = s1 * 0.0625f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -651,8 +639,9 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
         }
     }
 
-    constexpr float kBack = 18446744073709551616.f;            // 2^kBackExp
     constexpr float kPScale = 1099511627776.f;                 // 2^kPExp
+    const int from = 8 * t + (r < 4 ? 2 : 0) + ((r & 3) >> 1);     // lane that holds the p s of key 2 t for column r
+    const uint32_t pick = (r & 1) != 0 ? 0x7632u : 0x5410u;
     float m = kNeg, l = 0.f, accm[2] = {0.f, 0.f};             // the maximum is the warp's; l and accm are a lane's own rows'
     float acc[8][4];
 #pragma unroll
@@ -660,31 +649,47 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
 
-    auto reduce = [&](const Tile& x) {
+    // N stages at once (one tile of 16 keys of each): their chains of shuffles and matrix instructions overlap
+    auto reduce = [&](auto count, auto all_seen, const int* stage, const int (*pos)[2]) {
+        constexpr int N = decltype(count)::value;
+        constexpr bool kAll = decltype(all_seen)::value;           // every key of the tiles is visible: no selects
+        uint32_t base[N];
+        float s[N][2];
         // ---- logits of keys r and r + 8 ----------------------------------------------------------------------------
-        float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};     // two accumulators: half the chain
-        const uint32_t ka[4] = {x.k[0].x, x.k[0].y, x.k[0].z, x.k[0].w}, kb[4] = {x.k[1].x, x.k[1].y, x.k[1].z, x.k[1].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t ha = ka[i] >> 8, hb = kb[i] >> 8;
-            mma16816(d0, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u, qb[i][0][0], qb[i][0][1]);
-            mma16816(d1, ha & 0x000f000fu, hb & 0x000f000fu, ha & 0x00f000f0u, hb & 0x00f000f0u, qb[i][1][0], qb[i][1][1]);
-        }
-        float s[2];
+        for (int n = 0; n < N; ++n) {
+            base[n] = ring + stage[n] * kStageBytes;
+            const uint4 k0 = lds128(base[n] + k_at), k1 = lds128(base[n] + k_at + 1024u);        // group t's codes
+            const uint2 w0 = lds64(base[n] + s_at), w1 = lds64(base[n] + s_at + 256u);           // words of groups 2 (t & 1) + {0, 1}
+            const uint32_t ka[4] = {k0.x, k0.y, k0.z, k0.w}, kb[4] = {k1.x, k1.y, k1.z, k1.w};
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float y0 = ((d0[2 * i] + d1[2 * i]) * kBack) * q_back, y1 = ((d0[2 * i + 1] + d1[2 * i + 1]) * kBack) * q_back;
-            const float st0 = __uint_as_float(x.ks[i].x << 16), lo0 = __uint_as_float(x.ks[i].x & 0xffff0000u);
-            const float st1 = __uint_as_float(x.ks[i].y << 16), lo1 = __uint_as_float(x.ks[i].y & 0xffff0000u);
-            s[i] = fmaf(st0, y0, lo0 * qsum[0]) + fmaf(st1, y1, lo1 * qsum[1]);      // (lanes t >= 2: columns 4 to 7, all zero)
-            s[i] += __shfl_xor_sync(0xffffffffu, s[i], 1);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t ha = ka[i] >> 8, hb = kb[i] >> 8;
+                mma16816(d, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u, qb[i][0][0], qb[i][0][1]);
+                mma16816(d, ha & 0x000f000fu, hb & 0x000f000fu, ha & 0x00f000f0u, hb & 0x00f000f0u, qb[i][1][0], qb[i][1][1]);
+            }
+            const uint2 w[2] = {w0, w1};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {      // (lanes t >= 2: columns 4 to 7, all zero)
+                const float a0 = fmaf(d[2 * i] * q_back, __uint_as_float(w[i].x << 16), __uint_as_float(w[i].x & 0xffff0000u) * qsum[0]);
+                const float a1 = fmaf(d[2 * i + 1] * q_back, __uint_as_float(w[i].y << 16), __uint_as_float(w[i].y & 0xffff0000u) * qsum[1]);
+                s[n][i] = a0 + a1;
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            s[i] = __shfl_sync(0xffffffffu, s[i], lane & ~3) * scale_log2;
-            if (x.pos[i] > qpos) s[i] = kNeg;
-        }
-        float top = fmaxf(s[0], s[1]);
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[n][i] += __shfl_xor_sync(0xffffffffu, s[n][i], 1);
+        float top = kNeg;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s[n][i] = __shfl_sync(0xffffffffu, s[n][i], lane & ~3);
+                if (!kAll) s[n][i] = pos[n][i] <= qpos ? s[n][i] : kNeg;
+                top = fmaxf(top, s[n][i]);
+            }
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         if (top > m + 8.f) {     // the reference moves only when it pays: weights stay below 2^8
@@ -698,56 +703,77 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
                 for (int e = 0; e < 4; ++e) acc[j][e] *= corr;
         }
         // ---- weights; p s of this lane's keys and V groups, rounded to bf16 (lanes t >= 2) or what rounding left (t < 2) ---------
-        uint32_t pw[2];
+        uint32_t pw[N][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const bool see = x.pos[i] <= qpos;                   // a masked key takes no part, whatever its words hold
-            const float p = see ? ex2_approx(s[i] - m) : 0.f;
-            l += p;
-            const float st0 = __uint_as_float(x.vs[i].x << 16), lo0 = __uint_as_float(x.vs[i].x & 0xffff0000u);
-            const float st1 = __uint_as_float(x.vs[i].y << 16), lo1 = __uint_as_float(x.vs[i].y & 0xffff0000u);
-            const float pp = p * kPScale;
-            float a0 = see ? pp * st0 : 0.f, a1 = see ? pp * st1 : 0.f;
-            accm[0] = see ? fmaf(p, lo0, accm[0]) : accm[0];
-            accm[1] = see ? fmaf(p, lo1, accm[1]) : accm[1];
-            const uint32_t w = two_bf16(a0, a1);
-            a0 -= __uint_as_float(w << 16);
-            a1 -= __uint_as_float(w & 0xffff0000u);
-            pw[i] = t < 2 ? two_bf16(a0, a1) : w;
-        }
-        // B fragments: column n = r is group n & 3, rounded part for n < 4; keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
-        const int from = (r < 4 ? 2 : 0) + ((r & 3) >> 1);
-        const uint32_t pick = (r & 1) != 0 ? 0x7632u : 0x5410u;
-        const uint32_t b0 = __byte_perm(__shfl_sync(0xffffffffu, pw[0], 8 * t + from), __shfl_sync(0xffffffffu, pw[0], 8 * t + 4 + from), pick);
-        const uint32_t b1 = __byte_perm(__shfl_sync(0xffffffffu, pw[1], 8 * t + from), __shfl_sync(0xffffffffu, pw[1], 8 * t + 4 + from), pick);
-        // ---- P V: nibble j of words r (rows r) and r + 8 (rows r + 8), keys interleaved ---------------------------------------------
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t sel = hf == 0 ? 0x5410u : 0x7632u;
-            const uint32_t wa = __byte_perm(x.v[0], x.v[2], sel), wb = __byte_perm(x.v[1], x.v[3], sel);
-            const uint32_t wc = __byte_perm(x.v[4], x.v[6], sel), wd = __byte_perm(x.v[5], x.v[7], sel);
-            mma16816(acc[4 * hf], wa & 0x000f000fu, wb & 0x000f000fu, wc & 0x000f000fu, wd & 0x000f000fu, b0, b1);
-            mma16816(acc[4 * hf + 1], wa & 0x00f000f0u, wb & 0x00f000f0u, wc & 0x00f000f0u, wd & 0x00f000f0u, b0, b1);
-            const uint32_t ha = wa >> 8, hb = wb >> 8, hc = wc >> 8, hd = wd >> 8;
-            mma16816(acc[4 * hf + 2], ha & 0x000f000fu, hb & 0x000f000fu, hc & 0x000f000fu, hd & 0x000f000fu, b0, b1);
-            mma16816(acc[4 * hf + 3], ha & 0x00f000f0u, hb & 0x00f000f0u, hc & 0x00f000f0u, hd & 0x00f000f0u, b0, b1);
+            for (int i = 0; i < 2; ++i) {
+                const uint2 w = lds64(base[n] + s_at + 16u + 256u * i);
+                const bool see = kAll || pos[n][i] <= qpos;         // a masked key takes no part, whatever its words hold
+                const float p = see ? ex2_approx(s[n][i] - m) : 0.f;
+                l += p;
+                const float pp = p * kPScale, lo0 = __uint_as_float(w.x & 0xffff0000u), lo1 = __uint_as_float(w.y & 0xffff0000u);
+                float a0 = pp * __uint_as_float(w.x << 16), a1 = pp * __uint_as_float(w.y << 16);
+                if (!kAll) { a0 = see ? a0 : 0.f; a1 = see ? a1 : 0.f; }
+                accm[0] = see ? fmaf(p, lo0, accm[0]) : accm[0];
+                accm[1] = see ? fmaf(p, lo1, accm[1]) : accm[1];
+                const uint32_t u = two_bf16(a0, a1);
+                a0 -= __uint_as_float(u << 16);
+                a1 -= __uint_as_float(u & 0xffff0000u);
+                pw[n][i] = t < 2 ? two_bf16(a0, a1) : u;
+            }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            // B fragments: column r is group r & 3, rounded part for r < 4; keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+            const uint32_t b0 = __byte_perm(__shfl_sync(0xffffffffu, pw[n][0], from), __shfl_sync(0xffffffffu, pw[n][0], from + 4), pick);
+            const uint32_t b1 = __byte_perm(__shfl_sync(0xffffffffu, pw[n][1], from), __shfl_sync(0xffffffffu, pw[n][1], from + 4), pick);
+            uint32_t v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {       // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: words r and r + 8 of V's codes
+                v[2 * i] = lds32(base[n] + v_at[i & 1][0] + 1024u * (i >> 1));
+                v[2 * i + 1] = lds32(base[n] + v_at[i & 1][1] + 1024u * (i >> 1));
+            }
+            // ---- P V: nibble j of words r (rows r) and r + 8 (rows r + 8), keys interleaved -----------------------------------------
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint32_t sel = hf == 0 ? 0x5410u : 0x7632u;
+                const uint32_t wa = __byte_perm(v[0], v[2], sel), wb = __byte_perm(v[1], v[3], sel);
+                const uint32_t wc = __byte_perm(v[4], v[6], sel), wd = __byte_perm(v[5], v[7], sel);
+                mma16816(acc[4 * hf], wa & 0x000f000fu, wb & 0x000f000fu, wc & 0x000f000fu, wd & 0x000f000fu, b0, b1);
+                mma16816(acc[4 * hf + 1], wa & 0x00f000f0u, wb & 0x00f000f0u, wc & 0x00f000f0u, wd & 0x00f000f0u, b0, b1);
+                const uint32_t ha = wa >> 8, hb = wb >> 8, hc = wc >> 8, hd = wd >> 8;
+                mma16816(acc[4 * hf + 2], ha & 0x000f000fu, hb & 0x000f000fu, hc & 0x000f000fu, hd & 0x000f000fu, b0, b1);
+                mma16816(acc[4 * hf + 3], ha & 0x00f000f0u, hb & 0x00f000f0u, hc & 0x00f000f0u, hd & 0x00f000f0u, b0, b1);
+            }
         }
     };
-    int next_pos[2];
-    positions(0, next_pos);
-    for (int i = 0; i < rounds; ++i) {
-        const int st = i % kTokenStages;
-        Tile x;
-        x.pos[0] = next_pos[0];
-        x.pos[1] = next_pos[1];
-        if (i + 1 < rounds) positions(i + 1, next_pos);
-        if (__all_sync(0xffffffffu, mbar_wait(&bar_full[st], static_cast<uint32_t>(i / kTokenStages) & 1u)) == 0) { ok = false; break; }
-        if (i * kRound + key0 < n_c) {      // (a warp past the chunk's end has nothing here)
-            read_tile(st, x);
-            reduce(x);
+    const int mine = n_c > key0 ? (n_c - key0 + kRound - 1) / kRound : 0;      // stages that hold keys of this warp's
+    int pos[2][2], next_pos[2][2];
+    positions(0, next_pos[0]);
+    positions(1, next_pos[1]);
+    for (int i = 0; i < rounds; i += 2) {
+        const int st[2] = {i % kTokenStages, (i + 1) % kTokenStages};
+#pragma unroll
+        for (int n = 0; n < 2; ++n) { pos[n][0] = next_pos[n][0]; pos[n][1] = next_pos[n][1]; }
+        if (i + 2 < rounds) { positions(i + 2, next_pos[0]); positions(i + 3, next_pos[1]); }
+        const bool two = i + 1 < rounds;
+        bool came = mbar_wait(&bar_full[st[0]], static_cast<uint32_t>(i / kTokenStages) & 1u);
+        if (two) came = mbar_wait(&bar_full[st[1]], static_cast<uint32_t>((i + 1) / kTokenStages) & 1u) && came;
+        if (__all_sync(0xffffffffu, came) == 0) { ok = false; break; }
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        if (i + 1 < mine) {
+            const bool all = max(max(pos[0][0], pos[0][1]), max(pos[1][0], pos[1][1])) <= qpos;
+            if (__all_sync(0xffffffffu, all)) reduce(Two(), std::true_type(), st, pos);
+            else reduce(Two(), std::false_type(), st, pos);
+        } else if (i < mine) {
+            reduce(One(), std::false_type(), st, pos);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar_free[st]);
+        if (lane == 0) {
+            mbar_arrive(&bar_free[st[0]]);
+            if (two) mbar_arrive(&bar_free[st[1]]);
+        }
     }
     if (!ok && lane == 0) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
 
@@ -776,7 +802,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 
     // ---- local keys: eight lanes a key, 16 features a lane, two keys a bundle and round ---------------------------------------------
     {
-        constexpr int UL = 2, NB = kThreads / 8;
+        constexpr int UL = 2, NB = kConsumers / 8;
         const int bundle = tid >> 3, lig = tid & 7;
         float2 q2[8], a2[8];
         {
@@ -862,19 +888,19 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float give = up16 ? v[i] : v[4 + i], keep = up16 ? v[4 + i] : v[i];
-            red[kWarps + warp][16 * lig + (up8 ? 8 : 0) + (up16 ? 4 : 0) + i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+            red[kTokenWarps + warp][16 * lig + (up8 ? 8 : 0) + (up16 ? 4 : 0) + i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
         }
-        if (lane == 0) { red[kWarps + warp][DH] = M; red[kWarps + warp][DH + 1] = ll; }
+        if (lane == 0) { red[kTokenWarps + warp][DH] = M; red[kTokenWarps + warp][DH + 1] = ll; }
     }
     }       // (consumers)
     __syncthreads();
     if (tid < DH) {
         float M = kNeg;
 #pragma unroll
-        for (int w = 0; w < 2 * kWarps; ++w) M = fmaxf(M, red[w][DH]);
+        for (int w = 0; w < 2 * kTokenWarps; ++w) M = fmaxf(M, red[w][DH]);
         float L = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < 2 * kWarps; ++w) {
+        for (int w = 0; w < 2 * kTokenWarps; ++w) {
             const float wgt = ex2_approx(red[w][DH] - M);
             L = fmaf(red[w][DH + 1], wgt, L);
             o = fmaf(red[w][tid], wgt, o);
@@ -930,7 +956,7 @@ int launch_token(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, con
     }
     return dodo_check_cuda(ctx, dodo_launch_dependent(attend_q4_token_kernel, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kTokenThreads), smem, st,
                                                       static_cast<const __nv_bfloat16*>(Q), maps, src, g, cache_pos, H, sm_scale * 1.4426950408889634f,
-                                                      static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
+                                                      dodo_attend_tile_keys(DODO_BF16, 128), static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
                            "4-bit attend launch");
 }
 

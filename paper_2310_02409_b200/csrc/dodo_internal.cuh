@@ -226,6 +226,7 @@ struct AttendShape {
 struct AttendTotals {
     int64_t units, work, target;   // (query tile, head) units; units x key tiles; block target
     bool split;
+    int min_chunk;                 // key tiles a chunk has at least
     int64_t part_rows, tick_rows;  // running totals over launch groups
 };
 void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& plan, AttendTotals& tot);
