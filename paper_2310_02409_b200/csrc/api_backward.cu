@@ -18,7 +18,7 @@ Layout layout(const dodo_ctx* ctx, int q_rows, int H, int cache_rows) {
     Layout l;
     l.stats = 0;
     l.scores = round256(static_cast<size_t>(H) * (static_cast<size_t>(q_rows) + DODO_GROUP * kStatAlign) * 2 * sizeof(float));
-    l.parts = l.scores + round256(static_cast<size_t>(H) * 2 * cache_rows * sizeof(float));
+    l.parts = l.scores + round256(static_cast<size_t>(H) * 4 * cache_rows * sizeof(float));
     l.total = l.parts + static_cast<size_t>(2) * ctx->num_sms * kPartFloats * sizeof(float);
     return l;
 }

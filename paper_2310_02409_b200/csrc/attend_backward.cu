@@ -281,6 +281,29 @@ backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGr
     }
 }
 
+// =============================================== score gradients =========================================================
+// dscore of 32 cache rows per block: a warp adds up every eighth of the parts, then the warps' sums are added in warp order.
+__global__ void __launch_bounds__(kThreads)
+backward_scores_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int parts) {
+    __shared__ float sums[kThreads / 32][32];
+    const int b = blockIdx.y, row = static_cast<int>(blockIdx.x) * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+    if (static_cast<int>(blockIdx.x) * 32 >= g.seq[b].c_len) return;
+    dodo_grid_dependency_sync();
+    float s = 0.f;
+    if (row < g.seq[b].c_len) {
+        const float* p = a.score_part + g.seq[b].c_row0 + row;
+#pragma unroll 8
+        for (int i = warp; i < parts; i += kThreads / 32) s += __ldcg(p + static_cast<size_t>(i) * a.score_rows);
+    }
+    sums[warp][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (warp == 0 && row < g.seq[b].c_len) {
+#pragma unroll
+        for (int w = 1; w < kThreads / 32; ++w) s += sums[w][threadIdx.x];
+        a.dscore[g.seq[b].c_row0 + row] = s;
+    }
+}
+
 // =============================================== fp32 tiles ==============================================================
 constexpr int TK = 64, TQ = 32;     // keys and queries of a tile
 constexpr int LDP = TK + 4;         // row of the weight tiles
@@ -560,6 +583,15 @@ int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const Ba
     const cudaError_t e = dtype == DODO_BF16 ? dodo_launch_dependent(backward_stats_kernel<__nv_bfloat16>, grid, block, 0, st, a, g, H, dh)
                                              : dodo_launch_dependent(backward_stats_kernel<float>, grid, block, 0, st, a, g, H, dh);
     return dodo_check_cuda(ctx, e, "attend gradient statistics launch");
+}
+
+int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const BackwardArrays& a, int parts, cudaStream_t st) {
+    int most = 0;
+    for (int i = 0; i < g.nseq; ++i) most = most > g.seq[i].c_len ? most : g.seq[i].c_len;
+    if (a.dscore == nullptr || most == 0) return DODO_OK;
+    return dodo_check_cuda(ctx, dodo_launch_dependent(backward_scores_kernel, dim3(static_cast<unsigned>((most + 31) / 32), static_cast<unsigned>(g.nseq)),
+                                                      dim3(kThreads), 0, st, a, g, parts),
+                           "attend gradient score launch");
 }
 
 int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a,

@@ -16,13 +16,21 @@
 //
 // One persistent block per SM draws units from a counter, query units first (they are the longer ones).  Roles, each
 // waiting only for what it consumes:
-//   producer (warp 10)  draws units, brings the stationary pair (two buffers: the next unit's loads overlap this one's end)
-//       and the streamed tiles (three stages) with plain TMA tensor copies, 128-byte swizzle
-//   issuer of S, T (warp 8)   into one of two score buffers of TMEM, up to two tiles ahead of the weights
-//   issuer of the accumulating products (warp 9)
-//   weights (warps 0-7; two threads per row, 32 columns each)  P and dS from S, T and the statistics; at a unit's end the
-//       accumulators out of TMEM
-// TMEM columns: [0,128) dK or dQ, [128,256) dV, then per score buffer 64 of S and 64 of T.
+//   producer (a warp)  draws units and brings the stationary pairs and the streamed tiles with plain TMA tensor copies, 128-byte
+//       swizzle, into seven 32 KB slots: a stationary pair takes two, a tile one.  Slots go back as tiles are consumed, so up
+//       to five tiles are on their way (a load takes about 2000 cycles, a tile's whole stay about 6000).
+//   issuer of S, then T (a warp)  into a score buffer of TMEM, up to two tiles ahead of the weights
+//   weights (16 warps; four threads per row, 16 columns each)  P from S while T is still computed, then dS
+//   issuer of the accumulating products (a warp)  P dO as soon as P is published, dS Q (dS K) behind it
+//   a unit's end  the weights' threads move the accumulators through the slots of the unit's own stationary pair, from where a
+//       warp of its own stores them with tensor copies (64 rows at a time; rows of a box that reaches behind the segment are
+//       stored directly).  Row by row from registers a warp's store touches 32 lines: 5000 cycles a unit.  The weights of the
+//       next unit's first tile come before that, so that the tensor pipe has work meanwhile.
+// What sets the tile period is a score buffer's round (S, P, T, dS, accumulation: about 3500 cycles): key units have two
+// buffers; query units, which need no dV, a third one in its place.
+// TMEM columns: [0,128) dK or dQ, [128,256) dV or score buffer 2, [256,384) and [384,512) score buffers 0 and 1; a score buffer is
+// 64 columns of S and 64 of T.
+// The heads' score gradients are added up by a kernel of their own (a fence and a ticket per unit cost microseconds each).
 // Every wait is bounded; a role whose wait runs out reports it and leaves, and so do the others in turn.
 #include "dodo_internal.cuh"
 #include "sm100_ptx.cuh"
@@ -34,23 +42,41 @@ using namespace sm100;
 constexpr int DH = 128;
 constexpr int BM = 128;                 // rows of a unit
 constexpr int BN = 64;                  // rows of a streamed tile
-constexpr int kWeightThreads = 256;
-constexpr int kThreads = kWeightThreads + 96;
-constexpr int kStages = 3;
-constexpr int kSlots = 4;               // units announced ahead
-constexpr int kXHalf = BM * 128;        // 64 features of a stationary tile
-constexpr int kXTile = 2 * kXHalf;
-constexpr int kYHalf = BN * 128;
-constexpr int kYTile = 2 * kYHalf;
+constexpr int kWeightWarps = 16, kWeightThreads = 32 * kWeightWarps;
+constexpr int kProducer = kWeightWarps, kIssueScore = kProducer + 1, kIssueAcc = kProducer + 2, kStore = kProducer + 3;
+constexpr int kThreads = 32 * (kWeightWarps + 4);
+constexpr int kSlots = 7, kSlotBytes = 32 * 1024;     // X1 or X2 of a unit, or Y1 and Y2 of a tile
+constexpr int kMostTiles = kSlots - 2;                // tiles on their way: a pair is always resident beside them
+constexpr int kRing = 8;                              // tiles' barriers (more than kMostTiles)
+constexpr int kAhead = 4;                             // units announced ahead
+constexpr int kXHalf = BM * 128;                      // 64 features of a stationary tile
+constexpr int kYHalf = BN * 128, kYTile = 2 * kYHalf;
 constexpr int kStatBytes = BN * 8;
-constexpr int kOffX = 0;                                   // [buffer][X1, X2]
-constexpr int kOffY = kOffX + 2 * 2 * kXTile;              // [stage][Y1, Y2]
-constexpr int kOffStat = kOffY + kStages * 2 * kYTile;     // [stage][64 x -lse, 64 x -D]
-constexpr int kSmemBytes = kOffStat + kStages * kStatBytes;
+static_assert(2 * kXHalf == kSlotBytes && 2 * kYTile == kSlotBytes, "slots");
+constexpr int kOffStat = kSlots * kSlotBytes;         // [kMostTiles][64 x -lse, 64 x -D]
+constexpr int kOffSync = kOffStat + kMostTiles * kStatBytes;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColAcc2 = 128, kColScore = 256;        // + buffer * 128; T at + 64
+constexpr uint32_t kColAcc2 = 128;
+__device__ __forceinline__ uint32_t score_col(int buffer) { return buffer == 2 ? 128u : 256u + 128u * buffer; }   // S; T at + 64
 
-struct BackwardMaps { CUtensorMap Q, dO, cK, cV, lK, lV; };   // boxes of 64 elements x 64 rows, 128-byte swizzle
+// barriers and the small tables behind them, at the end of the block's shared memory (all of it is dynamic, so that it starts
+// at a 1024-byte boundary without padding: there is none to spare)
+struct Sync {
+    uint64_t x[2], xdone[2], staged[2];                  // a unit's pair: here, its slots free again, its results staged in them
+    uint64_t y[kRing], yfree[kRing];                     // a tile: here, consumed
+    uint64_t s[3], t[3], p[3], d[3], a[3];               // a score buffer: S, T, P, dS there; consumed
+    uint64_t done, epi, meet, unit[kAhead], unit_free[kAhead];
+    int x_slot[2];           // slots of a unit's pair (first | second << 8), units with tiles counted
+    int y_slot[kRing];       // a tile's slot
+    int release[kRing];      // producer: slots that come back with a tile
+    int unit_id[kAhead];
+    uint32_t tmem;
+    int last;
+};
+constexpr int kSmemBytes = kOffSync + 512;
+static_assert(sizeof(Sync) <= 512 && kSmemBytes <= 227 * 1024, "shared memory");
+
+struct BackwardMaps { CUtensorMap Q, dO, cK, cV, lK, lV, dQ, dcK, dcV, dlK, dlV; };   // boxes of 64 elements x 64 rows, 128-byte swizzle
 
 __device__ __forceinline__ float ex2_approx(float x) {
     float y;
@@ -64,6 +90,40 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+// 16 columns each of the warp's 32 TMEM lanes at two addresses (early-clobber outputs: the second address is read after the
+// first load has been issued)
+__device__ __forceinline__ void tmem_ld16_pair(uint32_t a, uint32_t b, uint32_t* x, uint32_t* y) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=&r"(x[0]), "=&r"(x[1]), "=&r"(x[2]), "=&r"(x[3]), "=&r"(x[4]), "=&r"(x[5]), "=&r"(x[6]), "=&r"(x[7]),
+          "=&r"(x[8]), "=&r"(x[9]), "=&r"(x[10]), "=&r"(x[11]), "=&r"(x[12]), "=&r"(x[13]), "=&r"(x[14]), "=&r"(x[15]),
+          "=&r"(y[0]), "=&r"(y[1]), "=&r"(y[2]), "=&r"(y[3]), "=&r"(y[4]), "=&r"(y[5]), "=&r"(y[6]), "=&r"(y[7]),
+          "=&r"(y[8]), "=&r"(y[9]), "=&r"(y[10]), "=&r"(y[11]), "=&r"(y[12]), "=&r"(y[13]), "=&r"(y[14]), "=&r"(y[15])
+        : "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t a, const uint32_t* v) {     // (the caller waits)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* x) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]),
+          "=r"(x[8]), "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+        : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 // a wait by a whole warp: all lanes see the same outcome
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; }
@@ -137,187 +197,399 @@ __device__ __forceinline__ uint32_t finite2(uint32_t v) {
     return v;
 }
 
+// The score buffers' order, which every role follows by itself: a key unit's tiles alternate between two buffers, a query unit's
+// go round three; a buffer's barriers complete once per use, that of P once per use by a key unit.
+struct Buffers {
+    int cur = 1;
+    uint32_t parity = 0u, used = 0u, key_parity = 0u;       // of the next use; whether there was one; of the next by a key unit
+    __device__ __forceinline__ void next(bool keys) { cur = keys ? (cur == 0 ? 1 : 0) : (cur == 2 ? 0 : cur + 1); }
+    __device__ __forceinline__ uint32_t phase() const { return (parity >> cur) & 1u; }
+    __device__ __forceinline__ bool again() const { return ((used >> cur) & 1u) != 0u; }
+    __device__ __forceinline__ uint32_t key_phase() const { return (key_parity >> cur) & 1u; }
+    __device__ __forceinline__ void use(bool keys) {
+        parity ^= 1u << cur;
+        used |= 1u << cur;
+        if (keys) key_parity ^= 1u << cur;
+    }
+};
+
 __global__ void __launch_bounds__(kThreads, 1)
 backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_constant__ BackwardGroup g, const BackwardArrays a, int H,
                       float scale, int* __restrict__ next_unit, int* __restrict__ dev_status) {
-    extern __shared__ unsigned char smem_raw[];
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    __shared__ __align__(8) uint64_t bar_x[2], bar_xfree[2], bar_y[kStages], bar_yfree[kStages], bar_s[2], bar_p[2], bar_a[2], bar_epi,
-        bar_u[kSlots], bar_ufree[kSlots], bar_w;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int s_unit[kSlots];
-    __shared__ int s_flag;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    Sync& sy = *reinterpret_cast<Sync*>(smem + kOffSync);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int total = g.q_blocks + g.kv_blocks;
+    if ((base & 1023u) != 0u) {      // (the swizzle counts on it; a block's dynamic shared memory starts there when there is no other)
+        if (tid == 0) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+        return;
+    }
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&bar_x[i], 1); mbar_init(&bar_xfree[i], 1); mbar_init(&bar_s[i], 1); mbar_init(&bar_a[i], 1);
-            mbar_init(&bar_p[i], kWeightThreads / 32);
+        for (int i = 0; i < 2; ++i) { mbar_init(&sy.x[i], 1); mbar_init(&sy.xdone[i], 1); mbar_init(&sy.staged[i], kWeightWarps); }
+        for (int i = 0; i < kRing; ++i) { mbar_init(&sy.y[i], 1); mbar_init(&sy.yfree[i], 1); }
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(&sy.s[i], 1); mbar_init(&sy.t[i], 1); mbar_init(&sy.a[i], 1);
+            mbar_init(&sy.p[i], kWeightWarps); mbar_init(&sy.d[i], kWeightWarps);
         }
-        for (int i = 0; i < kStages; ++i) { mbar_init(&bar_y[i], 1); mbar_init(&bar_yfree[i], 1); }
-        for (int i = 0; i < kSlots; ++i) { mbar_init(&bar_u[i], 1); mbar_init(&bar_ufree[i], 2 + kWeightThreads / 32); }
-        mbar_init(&bar_epi, kWeightThreads / 32);
-        mbar_init(&bar_w, kWeightThreads / 32);
+        for (int i = 0; i < kAhead; ++i) { mbar_init(&sy.unit[i], 1); mbar_init(&sy.unit_free[i], 3 + kWeightWarps); }
+        mbar_init(&sy.done, 1);
+        mbar_init(&sy.epi, kWeightWarps);
+        mbar_init(&sy.meet, kWeightWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sy.tmem)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sy.tmem);
     // (launched in plain stream order: everything before this kernel on the stream has completed)
 
-    // the unit announced as number k, or -1 past the last (and when the announcement does not come)
+    auto shared_int = [](const int& v) { return *reinterpret_cast<const volatile int*>(&v); };
+    // the unit announced as number k to a whole warp: -1 past the last, -2 when the announcement does not come
     auto unit_number = [&](int k) {
-        if (!mbar_wait(&bar_u[k % kSlots], static_cast<uint32_t>(k / kSlots) & 1u)) return -2;
-        return *reinterpret_cast<volatile int*>(&s_unit[k % kSlots]);
+        if (!warp_wait(&sy.unit[k % kAhead], static_cast<uint32_t>(k / kAhead) & 1u)) return -2;
+        return shared_int(sy.unit_id[k % kAhead]);
+    };
+    auto unit_read = [&](int k) {       // ... has been read by all lanes of the warp
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sy.unit_free[k % kAhead]);
     };
 
+    // Barriers' phases: tile m (counted over all units of the block) uses ring entry m % kRing, the x-th unit with tiles pair
+    // entry x & 1, score buffers as Buffers says.  Nobody can fall two phases behind: a ring entry is used again only after its
+    // tile's accumulation, which everyone's part in the tile precedes; likewise score buffers; a pair entry only after the
+    // results of the unit before in it have been stored.
     bool ok = true;
-    if (warp == 10) {
-        // ================================= producer =================================
+    if (warp == kProducer) {
         if (lane == 0) {
-            int m = 0, x = 0;       // streamed tiles and units with tiles so far
+            unsigned free_slots = (1u << kSlots) - 1u;
+            int m = 0, freed = 0, x = 0, xfreed = 0;       // tiles issued, consumed; units with tiles begun, stored
+            unsigned pair_slots[2] = {0u, 0u};             // slots of the units begun and not stored
+            auto pair_back = [&]() { free_slots |= (xfreed & 1) ? pair_slots[1] : pair_slots[0]; ++xfreed; };
+            auto take_slot = [&]() {
+                for (int i = 0; free_slots == 0u; ++i) {   // a tile consumed or a unit stored, whichever comes first
+                    if (freed < m && mbar_try_wait(&sy.yfree[freed % kRing], static_cast<uint32_t>(freed / kRing) & 1u)) {
+                        free_slots |= static_cast<unsigned>(sy.release[freed % kRing]);
+                        ++freed;
+                    } else if (xfreed < x && mbar_try_wait(&sy.xdone[xfreed & 1], static_cast<uint32_t>(xfreed >> 1) & 1u)) {
+                        pair_back();
+                    } else if (i >= kWaitPolls) {
+                        ok = false;
+                        return 0;
+                    }
+                }
+                const int s = __ffs(static_cast<int>(free_slots)) - 1;
+                free_slots &= ~(1u << s);
+                return s;
+            };
             for (int k = 0; ok; ++k) {
-                const int slot = k % kSlots;
-                if (k >= kSlots && !mbar_wait(&bar_ufree[slot], static_cast<uint32_t>(k / kSlots - 1) & 1u)) { ok = false; break; }
+                const int entry = k % kAhead;
+                if (k >= kAhead && !mbar_wait(&sy.unit_free[entry], static_cast<uint32_t>(k / kAhead - 1) & 1u)) { ok = false; break; }
                 const int drawn = atomicAdd(next_unit, 1);
                 if (drawn == total + static_cast<int>(gridDim.x) - 1) *next_unit = 0;   // every block draws one past the end: the last puts the counter back
                 const int id = drawn < total ? drawn : -1;
-                *reinterpret_cast<volatile int*>(&s_unit[slot]) = id;
-                mbar_arrive(&bar_u[slot]);
+                *reinterpret_cast<volatile int*>(&sy.unit_id[entry]) = id;
+                mbar_arrive(&sy.unit[entry]);
                 if (id < 0) break;
                 const Unit u = unit_of(g, H, id);
                 if (u.n == 0) continue;
                 const BackwardSeq& sq = g.seq[u.i];
-                const int xb = x & 1, col = u.h * DH;
-                if (x >= 2 && !mbar_wait(&bar_xfree[xb], static_cast<uint32_t>(x / 2 - 1) & 1u)) { ok = false; break; }
-                const CUtensorMap* x1 = !u.keys ? &maps.Q : u.cached ? &maps.cK : &maps.lK;
-                const CUtensorMap* x2 = !u.keys ? &maps.dO : u.cached ? &maps.cV : &maps.lV;
-                mbar_expect_tx(&bar_x[xb], 2 * kXTile);
+                const int col = u.h * DH, xe = x & 1;
+                while (xfreed < x - 1) {      // (the unit that had this entry has been stored)
+                    if (!mbar_wait(&sy.xdone[xfreed & 1], static_cast<uint32_t>(xfreed >> 1) & 1u)) { ok = false; break; }
+                    pair_back();
+                }
+                if (!ok) break;
+                const int x1 = take_slot();
+                if (!ok) break;
+                const int x2 = take_slot();
+                if (!ok) break;
+                if (xe == 0) pair_slots[0] = (1u << x1) | (1u << x2); else pair_slots[1] = (1u << x1) | (1u << x2);
+                sy.x_slot[xe] = x1 | (x2 << 8);
+                const CUtensorMap* m1 = !u.keys ? &maps.Q : u.cached ? &maps.cK : &maps.lK;
+                const CUtensorMap* m2 = !u.keys ? &maps.dO : u.cached ? &maps.cV : &maps.lV;
+                mbar_expect_tx(&sy.x[xe], 2 * kSlotBytes);
                 for (int part = 0; part < 4; ++part) {      // (64 features, 64 rows) at a time
-                    const uint32_t dst = base + kOffX + xb * 2 * kXTile + (part >> 1) * kXHalf + (part & 1) * (64 * 128);
-                    tma_load_2d(dst, x1, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &bar_x[xb]);
-                    tma_load_2d(dst + kXTile, x2, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &bar_x[xb]);
+                    const uint32_t at = base + (part >> 1) * kXHalf + (part & 1) * (64 * 128);
+                    tma_load_2d(at + x1 * kSlotBytes, m1, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &sy.x[xe]);
+                    tma_load_2d(at + x2 * kSlotBytes, m2, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &sy.x[xe]);
                 }
                 ++x;
                 for (int j = 0; j < u.n; ++j, ++m) {
-                    const int st = m % kStages;
-                    if (m >= kStages && !mbar_wait(&bar_yfree[st], static_cast<uint32_t>(m / kStages - 1) & 1u)) { ok = false; break; }
+                    const int slot = take_slot(), e = m % kRing;
+                    if (!ok) break;
                     const Tile t = tile_of(sq, u, u.t0 + j);
                     const CUtensorMap* y1 = u.keys ? &maps.Q : t.cached ? &maps.cK : &maps.lK;
                     const CUtensorMap* y2 = u.keys ? &maps.dO : t.cached ? &maps.cV : &maps.lV;
-                    const uint32_t dst = base + kOffY + st * 2 * kYTile;
-                    mbar_expect_tx(&bar_y[st], 2 * kYTile + (u.keys ? kStatBytes : 0));
-                    tma_load_2d(dst, y1, col, t.row0, &bar_y[st]);
-                    tma_load_2d(dst + kYHalf, y1, col + 64, t.row0, &bar_y[st]);
-                    tma_load_2d(dst + kYTile, y2, col, t.row0, &bar_y[st]);
-                    tma_load_2d(dst + kYTile + kYHalf, y2, col + 64, t.row0, &bar_y[st]);
+                    const uint32_t dst = base + slot * kSlotBytes;
+                    sy.y_slot[e] = slot;
+                    sy.release[e] = 1 << slot;
+                    mbar_expect_tx(&sy.y[e], kSlotBytes + (u.keys ? kStatBytes : 0));
+                    tma_load_2d(dst, y1, col, t.row0, &sy.y[e]);
+                    tma_load_2d(dst + kYHalf, y1, col + 64, t.row0, &sy.y[e]);
+                    tma_load_2d(dst + kYTile, y2, col, t.row0, &sy.y[e]);
+                    tma_load_2d(dst + kYTile + kYHalf, y2, col + 64, t.row0, &sy.y[e]);
                     if (u.keys)
-                        bulk_load(base + kOffStat + st * kStatBytes, a.stats + (static_cast<size_t>(u.h) * g.stat_rows + sq.stat0 + t.first) * 2,
-                                  kStatBytes, &bar_y[st]);
+                        bulk_load(base + kOffStat + (m % kMostTiles) * kStatBytes,
+                                  a.stats + (static_cast<size_t>(u.h) * g.stat_rows + sq.stat0 + t.first) * 2, kStatBytes, &sy.y[e]);
                 }
             }
             if (!ok) {       // leave no copy in flight behind
-                for (int i = max(0, m - kStages); i < m; ++i) mbar_wait(&bar_y[i % kStages], static_cast<uint32_t>(i / kStages) & 1u);
-                for (int i = max(0, x - 2); i < x; ++i) mbar_wait(&bar_x[i & 1], static_cast<uint32_t>(i / 2) & 1u);
+                for (int i = max(0, m - kMostTiles); i < m; ++i) mbar_wait(&sy.y[i % kRing], static_cast<uint32_t>(i / kRing) & 1u);
+                for (int i = max(0, x - 2); i < x; ++i) mbar_wait(&sy.x[i & 1], static_cast<uint32_t>(i / 2) & 1u);
             }
         }
-    } else if (warp == 8) {
-        // ================================= S = X1 Y1^T, T = X2 Y2^T =================================
-        if (lane == 0) {
-            int m = 0, x = 0;
-            for (int k = 0; ok; ++k) {
-                const int id = unit_number(k);
-                if (id < 0) { ok = id == -1; break; }
-                const Unit u = unit_of(g, H, id);
-                mbar_arrive(&bar_ufree[k % kSlots]);
-                if (u.n == 0) continue;
-                const int xb = x & 1;
-                if (!mbar_wait(&bar_x[xb], static_cast<uint32_t>(x / 2) & 1u)) { ok = false; break; }
-                const uint64_t a1 = desc_kmajor(base + kOffX + xb * 2 * kXTile), a2 = desc_kmajor(base + kOffX + xb * 2 * kXTile + kXTile);
-                const uint32_t idesc = idesc_bf16(BN, false);
-                for (int j = 0; j < u.n; ++j, ++m) {
-                    const int b = m & 1, st = m % kStages;
-                    if (m >= 2 && !mbar_wait(&bar_a[b], static_cast<uint32_t>((m - 2) >> 1) & 1u)) { ok = false; break; }   // P, dS of two tiles ago consumed
-                    if (!mbar_wait(&bar_y[st], static_cast<uint32_t>(m / kStages) & 1u)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint64_t b1 = desc_kmajor(base + kOffY + st * 2 * kYTile), b2 = desc_kmajor(base + kOffY + st * 2 * kYTile + kYTile);
-                    const uint32_t d = tmem + kColScore + b * 128;
+    } else if (warp == kIssueScore) {
+        // ---- S = X1 Y1^T, T = X2 Y2^T (a whole warp with an elected lane per instruction: descriptors stay in uniform registers)
+        const uint32_t idesc = idesc_bf16(BN, false);
+        Buffers buf;
+        int m = 0, x = 0;
+        for (int k = 0; ok; ++k) {
+            const int id = __reduce_max_sync(0xffffffffu, unit_number(k));
+            if (id < 0) { ok = id == -1; break; }
+            unit_read(k);
+            const int n = __reduce_max_sync(0xffffffffu, unit_of(g, H, id).n);
+            const bool keys = id >= g.q_blocks;
+            if (n == 0) continue;
+            if (!warp_wait(&sy.x[x & 1], static_cast<uint32_t>(x / 2) & 1u)) { ok = false; break; }
+            const int xs = __reduce_max_sync(0xffffffffu, shared_int(sy.x_slot[x & 1]));
+            const uint64_t a1 = desc_kmajor(base + (xs & 255) * kSlotBytes), a2 = desc_kmajor(base + (xs >> 8) * kSlotBytes);
+            for (int j = 0; j < n; ++j, ++m) {
+                const int e = m % kRing;
+                buf.next(keys);
+                if (buf.again() && !warp_wait(&sy.a[buf.cur], buf.phase() ^ 1u)) { ok = false; break; }    // the P and dS before have been consumed
+                if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
+                const int ys = __reduce_max_sync(0xffffffffu, shared_int(sy.y_slot[e]));
+                tc_fence_after();
+                const uint64_t b1 = desc_kmajor(base + ys * kSlotBytes), b2 = desc_kmajor(base + ys * kSlotBytes + kYTile);
+                const uint32_t d = tmem + score_col(buf.cur);
+                if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < DH / 16; ++i)
                         mma_bf16(d, a1 + static_cast<uint64_t>(((i / 4) * kXHalf + (i % 4) * 32) >> 4),
                                  b1 + static_cast<uint64_t>(((i / 4) * kYHalf + (i % 4) * 32) >> 4), idesc, i > 0);
+                    mma_commit(&sy.s[buf.cur]);
 #pragma unroll
                     for (int i = 0; i < DH / 16; ++i)
                         mma_bf16(d + 64, a2 + static_cast<uint64_t>(((i / 4) * kXHalf + (i % 4) * 32) >> 4),
                                  b2 + static_cast<uint64_t>(((i / 4) * kYHalf + (i % 4) * 32) >> 4), idesc, i > 0);
-                    mma_commit(&bar_s[b]);
+                    mma_commit(&sy.t[buf.cur]);
                 }
-                if (ok) mma_commit(&bar_xfree[xb]);
-                ++x;
+                __syncwarp();
+                buf.use(keys);
             }
+            ++x;
         }
-    } else if (warp == 9) {
-        // ================================= acc1 += dS Y1, acc2 += P Y2 =================================
-        if (lane == 0) {
-            int m = 0, x = 0;
-            for (int k = 0; ok; ++k) {
-                const int id = unit_number(k);
-                if (id < 0) { ok = id == -1; break; }
-                const Unit u = unit_of(g, H, id);
-                mbar_arrive(&bar_ufree[k % kSlots]);
-                if (u.n == 0) continue;
-                if (x >= 1 && !mbar_wait(&bar_epi, static_cast<uint32_t>(x - 1) & 1u)) { ok = false; break; }   // the last unit's accumulators are out
-                const uint32_t idesc = idesc_bf16(DH, true);
-                for (int j = 0; j < u.n; ++j, ++m) {
-                    const int b = m & 1, st = m % kStages;
-                    if (!mbar_wait(&bar_p[b], static_cast<uint32_t>(m >> 1) & 1u)) { ok = false; break; }
-                    if (!mbar_wait(&bar_y[st], static_cast<uint32_t>(m / kStages) & 1u)) { ok = false; break; }
+    } else if (warp == kIssueAcc) {
+        // ---- acc2 += P Y2, acc1 += dS Y1 -------------------------------------------------------------------------------------
+        const uint32_t idesc = idesc_bf16(DH, true);
+        Buffers buf;
+        int m = 0, x = 0;
+        for (int k = 0; ok; ++k) {
+            const int id = __reduce_max_sync(0xffffffffu, unit_number(k));
+            if (id < 0) { ok = id == -1; break; }
+            unit_read(k);
+            const int n = __reduce_max_sync(0xffffffffu, unit_of(g, H, id).n);
+            const bool keys = id >= g.q_blocks;
+            if (n == 0) continue;
+            if (x >= 1 && !warp_wait(&sy.epi, static_cast<uint32_t>(x - 1) & 1u)) { ok = false; break; }   // the last unit's accumulators are out
+            for (int j = 0; j < n; ++j, ++m) {
+                const int e = m % kRing;
+                buf.next(keys);
+                const uint32_t p = tmem + score_col(buf.cur);
+                if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
+                const int ys = __reduce_max_sync(0xffffffffu, shared_int(sy.y_slot[e]));
+                const uint64_t y1 = desc_mnmajor(base + ys * kSlotBytes, kYHalf), y2 = desc_mnmajor(base + ys * kSlotBytes + kYTile, kYHalf);
+                // (16 rows of Y = 8 columns of pairs, at the first 8 of the 16 score columns they came from)
+                if (keys) {
+                    if (!warp_wait(&sy.p[buf.cur], buf.key_phase())) { ok = false; break; }
                     tc_fence_after();
-                    const uint64_t y1 = desc_mnmajor(base + kOffY + st * 2 * kYTile, kYHalf), y2 = desc_mnmajor(base + kOffY + st * 2 * kYTile + kYTile, kYHalf);
-                    const uint32_t p = tmem + kColScore + b * 128;
-                    // (16 rows of Y = 8 columns of pairs; a row's two threads keep to their own half of the S and T columns)
-                    if (u.keys) {
+                    if (elect_one()) {
 #pragma unroll
                         for (int i = 0; i < BN / 16; ++i)
-                            mma_bf16_ts(tmem + kColAcc2, p + (i / 2) * 32 + (i % 2) * 8, y2 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
+                            mma_bf16_ts(tmem + kColAcc2, p + i * 16, y2 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
                     }
+                    __syncwarp();
+                }
+                if (!warp_wait(&sy.d[buf.cur], buf.phase())) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < BN / 16; ++i)
-                        mma_bf16_ts(tmem, p + 64 + (i / 2) * 32 + (i % 2) * 8, y1 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
-                    mma_commit(&bar_a[b]);
-                    mma_commit(&bar_yfree[st]);
+                        mma_bf16_ts(tmem, p + 64 + i * 16, y1 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
+                    mma_commit(&sy.a[buf.cur]);
+                    mma_commit(&sy.yfree[e]);
+                    if (j == n - 1) mma_commit(&sy.done);
                 }
+                __syncwarp();
+                buf.use(keys);
+            }
+            ++x;
+        }
+    } else if (warp == kStore) {
+        // ---- results staged in the pair's slots go out, 64 rows of 64 features at a time -----------------------------------------
+        if (lane == 0) {
+            int x = 0;
+            for (int k = 0; ok; ++k) {
+                if (!mbar_wait(&sy.unit[k % kAhead], static_cast<uint32_t>(k / kAhead) & 1u)) { ok = false; break; }
+                const int id = shared_int(sy.unit_id[k % kAhead]);
+                if (id < 0) break;
+                mbar_arrive(&sy.unit_free[k % kAhead]);
+                const Unit u = unit_of(g, H, id);
+                if (u.n == 0) continue;
+                const int xe = x & 1;
+                if (!mbar_wait(&sy.staged[xe], static_cast<uint32_t>(x >> 1) & 1u)) { ok = false; break; }
+                if (u.keys || g.seq[u.i].nchunk == 1) {
+                    const int xs = shared_int(sy.x_slot[xe]);
+                    const CUtensorMap* o1 = !u.keys ? &maps.dQ : u.cached ? &maps.dcK : &maps.dlK;
+                    const CUtensorMap* o2 = u.cached ? &maps.dcV : &maps.dlV;
+                    for (int box = 0; box < u.rows / 64; ++box)
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t at = base + c * kXHalf + box * (64 * 128);
+                            tma_store_2d(o1, u.h * DH + c * 64, u.row0 + box * 64, at + (xs & 255) * kSlotBytes);
+                            if (u.keys) tma_store_2d(o2, u.h * DH + c * 64, u.row0 + box * 64, at + (xs >> 8) * kSlotBytes);
+                        }
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
+                mbar_arrive(&sy.xdone[xe]);
                 ++x;
             }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     } else {
-        // ================================= weights =================================
-        const int row = tid & (BM - 1), half = tid >> 7;
+        // ---- weights -----------------------------------------------------------------------------------------------------------
+        const int row = tid & (BM - 1), part = tid >> 7;        // 16 of a tile's columns, 32 of the accumulators'
         const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const float scale2 = scale * 1.4426950408889634f;
         const float2 c2 = make_float2(scale2, scale2);
-        int m = 0;
+        Buffers buf;
+        int m = 0, x = 0;
         uint32_t turn = 0;
-        // the eight warps meet (a barrier with a bounded wait: a warp that has left must not hold the others)
+        // the 16 warps meet (a barrier with a bounded wait: a warp that has left must not hold the others)
         auto meet = [&]() {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bar_w);
-            if (!warp_wait(&bar_w, turn & 1u)) ok = false;
+            if (lane == 0) mbar_arrive(&sy.meet);
+            if (!warp_wait(&sy.meet, turn & 1u)) ok = false;
             ++turn;
         };
+        // ---- the end of a unit: a thread takes 32 of its row's 128 columns of the accumulators ---------------------------------------
+        auto finish = [&](const Unit& u, float score) {
+            const BackwardSeq& sq = g.seq[u.i];
+            const bool live = row < u.rows;
+            const size_t at = (static_cast<size_t>(u.row0 + row) * H + u.h) * DH + part * 32;
+            if (live && u.keys && u.cached && a.dscore != nullptr)
+                a.score_part[(static_cast<size_t>(u.h) * 4 + part) * a.score_rows + u.row0 + row] = score;
+            uint32_t v[32];
+            auto pack8 = [&](int e, float f) {
+                return make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
+                                  pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
+                                  pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
+                                  pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
+            };
+            auto direct = [&](void* dst, float f) {
+                uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(dst) + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = pack8(e, f);
+            };
+            void* const o1 = u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ;
+            void* const o2 = u.cached ? a.dcV : a.dlV;
+            const bool cut = !u.keys && sq.nchunk > 1;
+            if (u.n == 0 && !cut) {       // nothing was summed: zeros
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = 0u;
+                if (live) {
+                    direct(o1, 1.f);
+                    if (u.keys) direct(o2, 1.f);
+                }
+                return;
+            }
+            const size_t unit0 = cut ? static_cast<size_t>(sq.part0 + (u.qt * H + u.h) * sq.nchunk) : 0u;
+            float* const mine = a.dq_part + (unit0 + u.chunk) * (BM * DH) + (part * 32) * BM + row;
+            if (u.n > 0) {
+                if (!warp_wait(&sy.done, static_cast<uint32_t>(x) & 1u)) { ok = false; return; }
+                tc_fence_after();
+                const int xs = shared_int(sy.x_slot[x & 1]);
+                const bool boxed = (row | 63) < u.rows;       // all 64 rows of the row's box are live
+                // where the thread's four 16-byte pieces go in a swizzled half of 64 features
+                unsigned char* const stage = smem + (part >> 1) * kXHalf + row * 128;
+                const int piece0 = (part & 1) * 4;
+                tmem_ld32(tmem + part * 32 + lane_sel, v);
+                if (cut) {                // unnormalised partials [feature][row], so that a warp's lanes write consecutive floats
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mine[e * BM] = __uint_as_float(v[e]);
+                } else if (boxed) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint4*>(stage + (xs & 255) * kSlotBytes + (((piece0 + e) ^ (row & 7)) << 4)) = pack8(e, scale);
+                } else if (live) {
+                    direct(o1, scale);
+                }
+                if (u.keys) {
+                    tmem_ld32(tmem + kColAcc2 + part * 32 + lane_sel, v);
+                    if (boxed) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<uint4*>(stage + (xs >> 8) * kSlotBytes + (((piece0 + e) ^ (row & 7)) << 4)) = pack8(e, 1.f);
+                    } else if (live) {
+                        direct(o2, 1.f);
+                    }
+                }
+                tc_fence_before();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sy.epi);
+                    mbar_arrive(&sy.staged[x & 1]);
+                }
+                ++x;
+            } else {                      // an empty chunk's partial
+#pragma unroll
+                for (int e = 0; e < 32; ++e) mine[e * BM] = 0.f;
+            }
+            if (!cut) return;
+            // ---- the last chunk of a query tile to arrive adds up all of them, in chunk order
+            __threadfence();
+            meet();
+            if (ok && tid == 0) {
+                int* counter = a.tickets + sq.qtick0 + u.qt * H + u.h;
+                const int t = atomicAdd(counter, 1);
+                *reinterpret_cast<volatile int*>(&sy.last) = t == sq.nchunk - 1;
+                if (t == sq.nchunk - 1) *counter = 0;
+            }
+            if (ok) meet();
+            if (!ok) return;
+            if (shared_int(sy.last)) {
+                __threadfence();
+                float o[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                for (int n = 0; n < sq.nchunk; ++n) {
+                    const float* src = a.dq_part + (unit0 + n) * (BM * DH) + (part * 32) * BM + row;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] += __ldcg(src + e * BM);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(o[e]);
+                if (live) direct(a.dQ, scale);
+            }
+            meet();     // `last` is free again
+        };
+
+        Unit before;                      // the unit whose accumulators are still to be taken
+        float before_score = 0.f;
+        bool pending = false;
         for (int k = 0; ok; ++k) {
-            const int id = __shfl_sync(0xffffffffu, unit_number(k), 0);
+            const int id = unit_number(k);
             if (id < 0) { ok = id == -1; break; }
+            unit_read(k);
             const Unit u = unit_of(g, H, id);
-            if (lane == 0) mbar_arrive(&bar_ufree[k % kSlots]);
             const BackwardSeq& sq = g.seq[u.i];
             const bool live = row < u.rows;
             float2 score2 = make_float2(0.f, 0.f);
@@ -339,198 +611,139 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             // key unit: a tile needs the position test if its first query lies behind some key of this warp's rows; query
             // unit: if some key of the tile lies behind some query of the warp's rows
             const int edge = u.keys ? __reduce_max_sync(0xffffffffu, my_pos) : __reduce_min_sync(0xffffffffu, my_pos);
-            // query unit: positions of a tile's columns, one a lane for the thread's half, fetched a tile ahead
+            // query unit: positions of the thread's 16 columns of a tile, one a lane (lanes 16 to 31 repeat them), fetched a tile ahead
             auto column_pos = [&](int t) {
                 const Tile s = tile_of(sq, u, t);
-                const int c = half * 32 + lane;
+                const int c = part * 16 + (lane & 15);
                 if (c >= s.rows) return 0x7fffffff;
                 return s.cached ? __ldg(a.cache_pos + s.row0 + c) : sq.l_pos0 + s.first + c;
             };
             int next_pos = !u.keys && u.n > 0 ? column_pos(u.t0) : 0;
 
-            for (int j = 0; j < u.n && ok; ++j, ++m) {
-                const int b = m & 1, st = m % kStages;
+            for (int j = 0; j < u.n; ++j, ++m) {
+                const int e = m % kRing;
+                buf.next(u.keys);
+                const int b = buf.cur;
                 const Tile t = tile_of(sq, u, u.t0 + j);
-                const int cpos = next_pos;
-                if (!u.keys && j + 1 < u.n) next_pos = column_pos(u.t0 + j + 1);
-                if (!warp_wait(&bar_s[b], static_cast<uint32_t>(m >> 1) & 1u)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t ts = tmem + kColScore + b * 128 + half * 32 + lane_sel;
-                uint32_t sv[32], tv[32];
-                tmem_ld32(ts, sv);
-                tmem_ld32(ts + 64, tv);
-                uint32_t pp[16], pd[16];
+                const uint32_t ts = tmem + score_col(b) + part * 16 + lane_sel;
+                // (this warp sees the tile's own barrier too: the statistics came with it, and rows may have to be cleared)
+                if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
+                if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
+                uint32_t sv[16], pk[8];
                 if (u.keys) {
-                    if (!warp_wait(&bar_y[st], static_cast<uint32_t>(m / kStages) & 1u)) { ok = false; break; }   // the statistics came with the tile
-                    const float4* nl = reinterpret_cast<const float4*>(base_ptr + kOffStat + st * kStatBytes) + half * 8;
+                    const float4* nl = reinterpret_cast<const float4*>(smem + kOffStat + (m % kMostTiles) * kStatBytes) + part * 4;
                     const float4* nd = nl + 16;
                     const int q0 = sq.q_pos0 + t.first;
                     const bool test = edge > q0 || t.rows < BN;
-                    const int c_lo = my_pos - q0 - half * 32, c_hi = t.rows - half * 32;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float4 l4 = nl[c], d4 = nd[c];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int i = 4 * c + 2 * e;
-                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2,
-                                                        e == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
-                            float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                            float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(tv[i]), __uint_as_float(tv[i + 1])),
-                                                               e == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
-                            if (test) {
-                                if (i < c_lo || i >= c_hi) p.x = d.x = 0.f;
-                                if (i + 1 < c_lo || i + 1 >= c_hi) p.y = d.y = 0.f;
-                            }
-                            score2 = __fadd2_rn(score2, d);
-                            pp[i / 2] = pack_bf16(p.x, p.y);
-                            pd[i / 2] = pack_bf16(d.x, d.y);
-                        }
-                    }
-                    tmem_st16(ts, pp);
-                    if (t.rows < BN) {   // rows behind the sequence's queries must not reach the products
-                        unsigned char* y = base_ptr + kOffY + st * 2 * kYTile;
+                    const int c_lo = my_pos - q0 - part * 16, c_hi = t.rows - part * 16;
+                    if (t.rows < BN) {   // rows behind the sequence's queries must not reach the products (both score products done with them)
+                        if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
+                        unsigned char* y = smem + shared_int(sy.y_slot[e]) * kSlotBytes;
                         for (int i = tid; i < (BN - t.rows) * 32; i += kWeightThreads) {     // 32 x 16 bytes per row of the pair
                             const int r = t.rows + i / 32, piece = i % 32;
                             *reinterpret_cast<uint4*>(y + (piece >> 4) * kYTile + ((piece >> 3) & 1) * kYHalf + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
+                    tc_fence_after();
+                    tmem_ld16(ts, sv);
+                    float2 p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 l4 = nl[i / 2];
+                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2,
+                                                    (i & 1) == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
+                        p[i] = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+                    }
+                    if (test) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
+                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pk[i] = pack_bf16(p[i].x, p[i].y);
+                    tmem_st8(ts, pk);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sy.p[b]);
+                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
+                    tc_fence_after();
+                    tmem_ld16(ts + 64, sv);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 d4 = nd[i / 2];
+                        p[i] = __fmul2_rn(p[i], __fadd2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])),
+                                                          (i & 1) == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
+                    }
+                    if (test) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
+                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        score2 = __fadd2_rn(score2, p[i]);
+                        pk[i] = pack_bf16(p[i].x, p[i].y);
+                    }
                 } else {
+                    const int cpos = next_pos;
+                    if (j + 1 < u.n) next_pos = column_pos(u.t0 + j + 1);
+                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
+                    tc_fence_after();
+                    uint32_t tv[16];
+                    tmem_ld16_pair(ts, ts + 64, sv, tv);
                     const int far = __reduce_max_sync(0xffffffffu, cpos);
                     const bool test = far > edge;
                     const float2 l2 = make_float2(nlse, nlse), d2 = make_float2(ndelta, ndelta);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, l2);
-                        const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, l2);
+                        const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
                         float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(tv[i]), __uint_as_float(tv[i + 1])), d2));
                         if (test) {
                             if (__shfl_sync(0xffffffffu, cpos, i) > my_pos) d.x = 0.f;
                             if (__shfl_sync(0xffffffffu, cpos, i + 1) > my_pos) d.y = 0.f;
                         }
-                        pd[i / 2] = pack_bf16(d.x, d.y);
+                        pk[i / 2] = pack_bf16(d.x, d.y);
                     }
                     // Keys that some query of the tile does not see, and rows behind the segment: dS is 0 there, but 0 times
                     // what the row holds need not be.  Rows behind the segment are zeroed, NaN and infinities of the others
-                    // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 8 rows of its half.
+                    // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 4 rows of its 16 columns'.
                     if (far > sq.q_pos0 + u.first) {
-                        const int r = half * 32 + (warp & 3) * 8 + (lane >> 2), part = lane & 3;
-                        uint4* y = reinterpret_cast<uint4*>(base_ptr + kOffY + st * 2 * kYTile + (part >> 1) * kYHalf + r * 128 + (part & 1) * 64);
-                        // (the copies' writes are visible to threads that have seen their barrier)
-                        if (!warp_wait(&bar_y[st], static_cast<uint32_t>(m / kStages) & 1u)) { ok = false; break; }
+                        const int r = part * 16 + (warp & 3) * 4 + (lane >> 3), piece = lane & 7;
+                        uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece >> 2) * kYHalf + r * 128 + (piece & 3) * 32);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            uint4 v = y[e];
-                            y[e] = r >= t.rows ? make_uint4(0, 0, 0, 0) : make_uint4(finite2(v.x), finite2(v.y), finite2(v.z), finite2(v.w));
+                        for (int i = 0; i < 2; ++i) {
+                            const uint4 w = y[i];
+                            y[i] = r >= t.rows ? make_uint4(0, 0, 0, 0) : make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                 }
-                tmem_st16(ts + 64, pd);
+                tmem_st8(ts + 64, pk);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bar_p[b]);
+                if (lane == 0) mbar_arrive(&sy.d[b]);
+                buf.use(u.keys);
+                if (j == 0 && pending) {      // (the unit before: its last accumulation has had this tile's time to complete)
+                    pending = false;
+                    finish(before, before_score);
+                    if (!ok) break;
+                }
             }
             if (!ok) break;
-
-            // ---- the unit's accumulators --------------------------------------------------------------------------
-            if (u.n > 0) {
-                if (!warp_wait(&bar_a[(m - 1) & 1], static_cast<uint32_t>((m - 1) >> 1) & 1u)) { ok = false; break; }
-                tc_fence_after();
-            }
-            const size_t at = (static_cast<size_t>(u.row0 + row) * H + u.h) * DH + half * 64;
-            auto take = [&](uint32_t col, uint32_t* v) {      // 32 columns of the thread's row; zeros where nothing was summed
-                if (u.n > 0) {
-                    tmem_ld32(tmem + col + lane_sel, v);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = 0u;
-                }
-            };
-            auto write_rows = [&](uint32_t col, void* dst, float f) {
-#pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
-                    take(col + half * 64 + c * 32, v);
-                    if (live) {
-                        uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(dst) + at + c * 32);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[e] = make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
-                                              pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
-                                              pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
-                                              pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
-                    }
-                }
-            };
-            const bool cut = !u.keys && sq.nchunk > 1;
-            const int unit0 = u.keys ? 0 : sq.part0 + (u.qt * H + u.h) * sq.nchunk;
-            if (cut) {       // [feature][row], so that a warp's lanes write consecutive floats
-                float* dst = a.dq_part + static_cast<size_t>(unit0 + u.chunk) * (BM * DH) + (half * 64) * BM + row;
-#pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
-                    take(half * 64 + c * 32, v);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) dst[(c * 32 + e) * BM] = __uint_as_float(v[e]);
-                }
-            } else {
-                write_rows(0, u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ, scale);
-                if (u.keys) write_rows(kColAcc2, u.cached ? a.dcV : a.dlV, 1.f);
-            }
-            if (u.n > 0) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar_epi);
-            }
-            // ---- what several units share: the heads' score gradients, the chunks' dQ; the last to arrive adds up -----
-            const bool scores = u.keys && u.cached && a.dscore != nullptr;
-            if (scores || cut) {
-                if (scores && live) a.score_part[(static_cast<size_t>(u.h) * 2 + half) * a.score_rows + u.row0 + row] = score2.x + score2.y;
-                __threadfence();
-                meet();
-                if (ok && tid == 0) {
-                    int* counter = scores ? a.tickets + sq.stick0 + u.first / BM : a.tickets + sq.qtick0 + u.qt * H + u.h;
-                    const int want = scores ? H : sq.nchunk;
-                    const int t = atomicAdd(counter, 1);
-                    s_flag = t == want - 1;
-                    if (t == want - 1) *counter = 0;
-                }
-                if (ok) meet();
-                if (!ok) break;
-                if (s_flag) {
-                    __threadfence();
-                    if (scores) {
-                        if (half == 0 && live) {
-                            float s = 0.f;
-                            for (int h = 0; h < 2 * H; ++h) s += __ldcg(a.score_part + static_cast<size_t>(h) * a.score_rows + u.row0 + row);
-                            a.dscore[u.row0 + row] = s;
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int c = 0; c < 2; ++c) {
-                            float o[32];
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                            for (int n = 0; n < sq.nchunk; ++n) {
-                                const float* src = a.dq_part + static_cast<size_t>(unit0 + n) * (BM * DH) + (half * 64 + c * 32) * BM + row;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] += __ldcg(src + e * BM);
-                            }
-                            if (live) {
-                                uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dQ) + at + c * 32);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    dst[e] = make_uint4(pack_bf16(o[8 * e] * scale, o[8 * e + 1] * scale), pack_bf16(o[8 * e + 2] * scale, o[8 * e + 3] * scale),
-                                                        pack_bf16(o[8 * e + 4] * scale, o[8 * e + 5] * scale), pack_bf16(o[8 * e + 6] * scale, o[8 * e + 7] * scale));
-                            }
-                        }
-                    }
-                }
-                meet();     // s_flag is free again
-            }
+            if (pending) finish(before, before_score);       // (a unit without tiles came between)
+            pending = ok;
+            before = u;
+            before_score = score2.x + score2.y;
         }
+        if (ok && pending) finish(before, before_score);
     }
     if (!ok) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
     tc_fence_before();
@@ -549,14 +762,16 @@ int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const Backw
     if (total == 0) return DODO_OK;
     BackwardMaps maps;
     memset(&maps, 0, sizeof maps);
-    struct { CUtensorMap* map; const void* base; int rows; } todo[6] = {{&maps.Q, a.Q, q_rows}, {&maps.dO, a.dO, q_rows}, {&maps.cK, a.cK, cache_rows},
-                                                                        {&maps.cV, a.cV, cache_rows}, {&maps.lK, a.lK, loc_rows}, {&maps.lV, a.lV, loc_rows}};
+    struct { CUtensorMap* map; const void* base; int rows; } todo[11] = {
+        {&maps.Q, a.Q, q_rows},        {&maps.dO, a.dO, q_rows},        {&maps.dQ, a.dQ, q_rows},        {&maps.cK, a.cK, cache_rows},
+        {&maps.cV, a.cV, cache_rows},  {&maps.dcK, a.dcK, cache_rows},  {&maps.dcV, a.dcV, cache_rows},  {&maps.lK, a.lK, loc_rows},
+        {&maps.lV, a.lV, loc_rows},    {&maps.dlK, a.dlK, loc_rows},    {&maps.dlV, a.dlV, loc_rows}};
     for (auto& t : todo) {
         if (t.rows == 0) continue;
         const int rc = dodo_encode_bf16_rows(ctx, t.map, t.base, H * DH, t.rows, BN);
         if (rc != DODO_OK) return rc;
     }
-    const size_t smem = static_cast<size_t>(kSmemBytes) + 1024;
+    const size_t smem = static_cast<size_t>(kSmemBytes);
     if (!ctx->backward_attr_set[4]) {
         const cudaError_t e = cudaFuncSetAttribute(backward_dense_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient shared-memory attribute");
@@ -564,5 +779,7 @@ int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const Backw
     }
     const int grid = total < ctx->num_sms ? total : ctx->num_sms;
     backward_dense_kernel<<<grid, kThreads, smem, st>>>(maps, g, a, H, sm_scale, next_unit, ctx->dev_status);
-    return dodo_check_cuda(ctx, cudaGetLastError(), "attend gradient launch");
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient launch");
+    return dodo_launch_backward_scores(ctx, g, a, 4 * H, st);
 }

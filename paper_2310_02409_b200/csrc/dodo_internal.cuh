@@ -296,7 +296,7 @@ struct BackwardArrays {
     // statistics, per head and run of 64 entries: 64 x -(log-sum-exp in base 2), -inf where nothing is visible, then
     // 64 x -(sum of dO * O).  One address per entry and head: entry e's first is stats + (h * stat_rows + e / 64 * 64) * 2 + e % 64
     float* stats;
-    float* score_part;              // [H][score_rows], tensor-core kernel: [2 H][score_rows]
+    float* score_part;              // [H][score_rows], tensor-core kernel: [4 H][score_rows]
     float* dq_part;                 // partial tiles of dQ
     int score_rows;
     int* tickets;
@@ -312,6 +312,8 @@ int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const Ba
 BackwardTiles dodo_backward_dense_tiles();
 int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
                                int cache_rows, int loc_rows, int* next_unit, cudaStream_t st);
+// dscore of the group's cache rows: the sum of `parts` rows of score_part, in order
+int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const BackwardArrays& a, int parts, cudaStream_t st);
 int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g,
                               const BackwardArrays& a, cudaStream_t st);
 int dodo_attend_max_cluster();   // most chunks of one (query tile, head) that can merge inside a cluster
