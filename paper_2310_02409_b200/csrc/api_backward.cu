@@ -18,7 +18,7 @@ Layout layout(const dodo_ctx* ctx, int q_rows, int H, int cache_rows) {
     Layout l;
     l.stats = 0;
     l.scores = round256(static_cast<size_t>(H) * (static_cast<size_t>(q_rows) + DODO_GROUP * kStatAlign) * 2 * sizeof(float));
-    l.parts = l.scores + round256(static_cast<size_t>(H) * 4 * cache_rows * sizeof(float));
+    l.parts = l.scores + round256(static_cast<size_t>(H) * 2 * cache_rows * sizeof(float));
     l.total = l.parts + static_cast<size_t>(2) * ctx->num_sms * kPartFloats * sizeof(float);
     return l;
 }
@@ -171,12 +171,13 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
             if (pass == 0) continue;
             if (variant == DODO_BWD_STREAM) {
                 rc = dodo_launch_backward_stream(ctx, dtype, H, dh, sm_scale, max_tq, g, a, st);
+            } else if (variant == DODO_BWD_TILE) {
+                rc = dodo_launch_backward_tile(ctx, dtype, H, dh, sm_scale, g, a, st);
             } else {
                 rc = dodo_launch_backward_stats(ctx, dtype, H, dh, g, a, st);
                 if (rc == DODO_OK)
-                    rc = variant == DODO_BWD_TILE ? dodo_launch_backward_tile(ctx, dtype, H, dh, sm_scale, g, a, st)
-                                                  : dodo_launch_backward_dense(ctx, H, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
-                                                                               ctx->tickets + DODO_NUM_TICKETS - 1, st);
+                    rc = dodo_launch_backward_dense(ctx, H, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
+                                                    ctx->tickets + DODO_NUM_TICKETS - 1, st);
             }
             if (rc != DODO_OK) return rc;
         }

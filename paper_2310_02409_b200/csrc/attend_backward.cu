@@ -249,6 +249,7 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
 }
 
 // =============================================== statistics =============================================================
+// (for the tensor-core kernel, whose statistics travel with its tiles; the others make their own)
 // -(log-sum-exp in base 2) and -(sum of dO * O) of every query, one row per head so that a tile's entries are contiguous;
 // entries behind a sequence's last query, up to a multiple of 64, are -inf and 0: such a column's weights come out 0.
 template <typename T>
@@ -317,12 +318,23 @@ template <int DH> struct TileSmem {
     int flag;
 };
 
-// statistics of queries [q0, q0 + TQ) of a sequence
-__device__ __forceinline__ void load_stats(float2* dst, const BackwardArrays& a, const BackwardGroup& g, int h, int entry0) {
-    if (threadIdx.x >= TQ) return;
-    const int e = entry0 + static_cast<int>(threadIdx.x);
-    const float* s = a.stats + (static_cast<size_t>(h) * g.stat_rows + (e & ~63)) * 2 + (e & 63);
-    dst[threadIdx.x] = make_float2(__ldg(s), __ldg(s + 64));
+// statistics of queries [q0, q0 + nq) of a sequence and head: eight threads a query
+template <typename T, int DH>
+__device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a, int H, int h, int row0, int nq) {
+    const int q = threadIdx.x / 8, part = threadIdx.x % 8;
+    float d = 0.f;
+    const size_t row = static_cast<size_t>(row0 + q) * H + h;
+    if (q < nq) {
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) {
+            const float4 x = load4(static_cast<const T*>(a.dO) + row * DH + 4 * (part + 8 * i));
+            const float4 y = load4(static_cast<const T*>(a.O) + row * DH + 4 * (part + 8 * i));
+            d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
+        }
+    }
+#pragma unroll
+    for (int s = 4; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
+    if (part == 0) dst[q] = q < nq ? make_float2(minus_lse2(__ldg(a.lse + row)), -d) : make_float2(-INFINITY, 0.f);
 }
 
 template <typename T, int DH>
@@ -423,7 +435,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
             __syncthreads();
             load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
             load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-            load_stats(sm.stat, a, g, h, sq.stat0 + q0);
+            tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
             __syncthreads();
             tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
             __syncthreads();
@@ -476,7 +488,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
     load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
     load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-    load_stats(sm.stat, a, g, h, sq.stat0 + q0);
+    tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
     float dq[2][4 * ND];
 #pragma unroll
     for (int i = 0; i < 2; ++i)

@@ -20,12 +20,13 @@
 //       swizzle, into seven 32 KB slots: a stationary pair takes two, a tile one.  Slots go back as tiles are consumed, so up
 //       to five tiles are on their way (a load takes about 2000 cycles, a tile's whole stay about 6000).
 //   issuer of S, then T (a warp)  into a score buffer of TMEM, up to two tiles ahead of the weights
-//   weights (16 warps; four threads per row, 16 columns each)  P from S while T is still computed, then dS
+//   weights (8 warps; two threads per row, 32 columns each)  P from S while T is still computed, then dS.  (16 warps spend
+//       as long on a tile, be it 16 columns a thread or two tiles at a time: what a warp does per tile besides counts.)
 //   issuer of the accumulating products (a warp)  P dO as soon as P is published, dS Q (dS K) behind it
-//   a unit's end  the weights' threads move the accumulators through the slots of the unit's own stationary pair, from where a
-//       warp of its own stores them with tensor copies (64 rows at a time; rows of a box that reaches behind the segment are
-//       stored directly).  Row by row from registers a warp's store touches 32 lines: 5000 cycles a unit.  The weights of the
-//       next unit's first tile come before that, so that the tensor pipe has work meanwhile.
+//   a unit's end (4 warps; a thread per row)  moves the accumulators through the slots of the unit's own stationary pair, from
+//       where another warp stores them with tensor copies (64 rows at a time; rows of a box that reaches behind the segment are
+//       stored directly).  Row by row from registers a warp's store touches 32 lines, 5000 cycles a unit, and done by the
+//       weights' warps the end of a unit stood in the way of the next one's tiles.
 // What sets the tile period is a score buffer's round (S, P, T, dS, accumulation: about 3500 cycles): key units have two
 // buffers; query units, which need no dV, a third one in its place.
 // TMEM columns: [0,128) dK or dQ, [128,256) dV or score buffer 2, [256,384) and [384,512) score buffers 0 and 1; a score buffer is
@@ -42,9 +43,9 @@ using namespace sm100;
 constexpr int DH = 128;
 constexpr int BM = 128;                 // rows of a unit
 constexpr int BN = 64;                  // rows of a streamed tile
-constexpr int kWeightWarps = 16, kWeightThreads = 32 * kWeightWarps;
-constexpr int kProducer = kWeightWarps, kIssueScore = kProducer + 1, kIssueAcc = kProducer + 2, kStore = kProducer + 3;
-constexpr int kThreads = 32 * (kWeightWarps + 4);
+constexpr int kWeightWarps = 8, kEndWarps = 4;
+constexpr int kProducer = kWeightWarps + kEndWarps, kIssueScore = kProducer + 1, kIssueAcc = kProducer + 2, kStore = kProducer + 3;
+constexpr int kThreads = 32 * (kStore + 1);
 constexpr int kSlots = 7, kSlotBytes = 32 * 1024;     // X1 or X2 of a unit, or Y1 and Y2 of a tile
 constexpr int kMostTiles = kSlots - 2;                // tiles on their way: a pair is always resident beside them
 constexpr int kRing = 8;                              // tiles' barriers (more than kMostTiles)
@@ -227,16 +228,16 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) { mbar_init(&sy.x[i], 1); mbar_init(&sy.xdone[i], 1); mbar_init(&sy.staged[i], kWeightWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sy.x[i], 1); mbar_init(&sy.xdone[i], 1); mbar_init(&sy.staged[i], kEndWarps); }
         for (int i = 0; i < kRing; ++i) { mbar_init(&sy.y[i], 1); mbar_init(&sy.yfree[i], 1); }
         for (int i = 0; i < 3; ++i) {
             mbar_init(&sy.s[i], 1); mbar_init(&sy.t[i], 1); mbar_init(&sy.a[i], 1);
             mbar_init(&sy.p[i], kWeightWarps); mbar_init(&sy.d[i], kWeightWarps);
         }
-        for (int i = 0; i < kAhead; ++i) { mbar_init(&sy.unit[i], 1); mbar_init(&sy.unit_free[i], 3 + kWeightWarps); }
+        for (int i = 0; i < kAhead; ++i) { mbar_init(&sy.unit[i], 1); mbar_init(&sy.unit_free[i], 3 + kWeightWarps + kEndWarps); }
         mbar_init(&sy.done, 1);
-        mbar_init(&sy.epi, kWeightWarps);
-        mbar_init(&sy.meet, kWeightWarps);
+        mbar_init(&sy.epi, kEndWarps);
+        mbar_init(&sy.meet, kEndWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -406,7 +407,8 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                 const int ys = __reduce_max_sync(0xffffffffu, shared_int(sy.y_slot[e]));
                 const uint64_t y1 = desc_mnmajor(base + ys * kSlotBytes, kYHalf), y2 = desc_mnmajor(base + ys * kSlotBytes + kYTile, kYHalf);
-                // (16 rows of Y = 8 columns of pairs, at the first 8 of the 16 score columns they came from)
+                // (16 rows of Y = 8 columns of pairs, at the first 8 of the 16 score columns they came from: each chunk of 16
+                // columns is read before it is written over)
                 if (keys) {
                     if (!warp_wait(&sy.p[buf.cur], buf.key_phase())) { ok = false; break; }
                     tc_fence_after();
@@ -463,128 +465,14 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             }
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
-    } else {
+    } else if (warp < kWeightWarps) {
         // ---- weights -----------------------------------------------------------------------------------------------------------
-        const int row = tid & (BM - 1), part = tid >> 7;        // 16 of a tile's columns, 32 of the accumulators'
+        const int row = tid & (BM - 1), half = tid >> 7;        // 32 of a tile's columns
         const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const float scale2 = scale * 1.4426950408889634f;
         const float2 c2 = make_float2(scale2, scale2);
         Buffers buf;
-        int m = 0, x = 0;
-        uint32_t turn = 0;
-        // the 16 warps meet (a barrier with a bounded wait: a warp that has left must not hold the others)
-        auto meet = [&]() {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sy.meet);
-            if (!warp_wait(&sy.meet, turn & 1u)) ok = false;
-            ++turn;
-        };
-        // ---- the end of a unit: a thread takes 32 of its row's 128 columns of the accumulators ---------------------------------------
-        auto finish = [&](const Unit& u, float score) {
-            const BackwardSeq& sq = g.seq[u.i];
-            const bool live = row < u.rows;
-            const size_t at = (static_cast<size_t>(u.row0 + row) * H + u.h) * DH + part * 32;
-            if (live && u.keys && u.cached && a.dscore != nullptr)
-                a.score_part[(static_cast<size_t>(u.h) * 4 + part) * a.score_rows + u.row0 + row] = score;
-            uint32_t v[32];
-            auto pack8 = [&](int e, float f) {
-                return make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
-                                  pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
-                                  pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
-                                  pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
-            };
-            auto direct = [&](void* dst, float f) {
-                uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(dst) + at);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = pack8(e, f);
-            };
-            void* const o1 = u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ;
-            void* const o2 = u.cached ? a.dcV : a.dlV;
-            const bool cut = !u.keys && sq.nchunk > 1;
-            if (u.n == 0 && !cut) {       // nothing was summed: zeros
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = 0u;
-                if (live) {
-                    direct(o1, 1.f);
-                    if (u.keys) direct(o2, 1.f);
-                }
-                return;
-            }
-            const size_t unit0 = cut ? static_cast<size_t>(sq.part0 + (u.qt * H + u.h) * sq.nchunk) : 0u;
-            float* const mine = a.dq_part + (unit0 + u.chunk) * (BM * DH) + (part * 32) * BM + row;
-            if (u.n > 0) {
-                if (!warp_wait(&sy.done, static_cast<uint32_t>(x) & 1u)) { ok = false; return; }
-                tc_fence_after();
-                const int xs = shared_int(sy.x_slot[x & 1]);
-                const bool boxed = (row | 63) < u.rows;       // all 64 rows of the row's box are live
-                // where the thread's four 16-byte pieces go in a swizzled half of 64 features
-                unsigned char* const stage = smem + (part >> 1) * kXHalf + row * 128;
-                const int piece0 = (part & 1) * 4;
-                tmem_ld32(tmem + part * 32 + lane_sel, v);
-                if (cut) {                // unnormalised partials [feature][row], so that a warp's lanes write consecutive floats
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) mine[e * BM] = __uint_as_float(v[e]);
-                } else if (boxed) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint4*>(stage + (xs & 255) * kSlotBytes + (((piece0 + e) ^ (row & 7)) << 4)) = pack8(e, scale);
-                } else if (live) {
-                    direct(o1, scale);
-                }
-                if (u.keys) {
-                    tmem_ld32(tmem + kColAcc2 + part * 32 + lane_sel, v);
-                    if (boxed) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            *reinterpret_cast<uint4*>(stage + (xs >> 8) * kSlotBytes + (((piece0 + e) ^ (row & 7)) << 4)) = pack8(e, 1.f);
-                    } else if (live) {
-                        direct(o2, 1.f);
-                    }
-                }
-                tc_fence_before();
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sy.epi);
-                    mbar_arrive(&sy.staged[x & 1]);
-                }
-                ++x;
-            } else {                      // an empty chunk's partial
-#pragma unroll
-                for (int e = 0; e < 32; ++e) mine[e * BM] = 0.f;
-            }
-            if (!cut) return;
-            // ---- the last chunk of a query tile to arrive adds up all of them, in chunk order
-            __threadfence();
-            meet();
-            if (ok && tid == 0) {
-                int* counter = a.tickets + sq.qtick0 + u.qt * H + u.h;
-                const int t = atomicAdd(counter, 1);
-                *reinterpret_cast<volatile int*>(&sy.last) = t == sq.nchunk - 1;
-                if (t == sq.nchunk - 1) *counter = 0;
-            }
-            if (ok) meet();
-            if (!ok) return;
-            if (shared_int(sy.last)) {
-                __threadfence();
-                float o[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                for (int n = 0; n < sq.nchunk; ++n) {
-                    const float* src = a.dq_part + (unit0 + n) * (BM * DH) + (part * 32) * BM + row;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] += __ldcg(src + e * BM);
-                }
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(o[e]);
-                if (live) direct(a.dQ, scale);
-            }
-            meet();     // `last` is free again
-        };
-
-        Unit before;                      // the unit whose accumulators are still to be taken
-        float before_score = 0.f;
-        bool pending = false;
+        int m = 0;
         for (int k = 0; ok; ++k) {
             const int id = unit_number(k);
             if (id < 0) { ok = id == -1; break; }
@@ -611,139 +499,241 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             // key unit: a tile needs the position test if its first query lies behind some key of this warp's rows; query
             // unit: if some key of the tile lies behind some query of the warp's rows
             const int edge = u.keys ? __reduce_max_sync(0xffffffffu, my_pos) : __reduce_min_sync(0xffffffffu, my_pos);
-            // query unit: positions of the thread's 16 columns of a tile, one a lane (lanes 16 to 31 repeat them), fetched a tile ahead
+            // query unit: positions of the thread's 32 columns of a tile, one a lane, fetched a tile ahead
             auto column_pos = [&](int t) {
                 const Tile s = tile_of(sq, u, t);
-                const int c = part * 16 + (lane & 15);
+                const int c = half * 32 + lane;
                 if (c >= s.rows) return 0x7fffffff;
                 return s.cached ? __ldg(a.cache_pos + s.row0 + c) : sq.l_pos0 + s.first + c;
             };
-            int next_pos = !u.keys && u.n > 0 ? column_pos(u.t0) : 0;
+            int next_pos = 0;
+            if (!u.keys && u.n > 0) next_pos = column_pos(u.t0);
+
 
             for (int j = 0; j < u.n; ++j, ++m) {
-                const int e = m % kRing;
                 buf.next(u.keys);
-                const int b = buf.cur;
-                const Tile t = tile_of(sq, u, u.t0 + j);
-                const uint32_t ts = tmem + score_col(b) + part * 16 + lane_sel;
+                const int e = m % kRing, b = buf.cur;
+                const uint32_t ts = tmem + score_col(b) + half * 32 + lane_sel;
+                uint32_t sv[16], pk[8];
+                if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
                 // (this warp sees the tile's own barrier too: the statistics came with it, and rows may have to be cleared)
                 if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
-                if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
-                uint32_t sv[16], pk[8];
                 if (u.keys) {
-                    const float4* nl = reinterpret_cast<const float4*>(smem + kOffStat + (m % kMostTiles) * kStatBytes) + part * 4;
+                    const float4* nl = reinterpret_cast<const float4*>(smem + kOffStat + (m % kMostTiles) * kStatBytes) + half * 8;
                     const float4* nd = nl + 16;
-                    const int q0 = sq.q_pos0 + t.first;
-                    const bool test = edge > q0 || t.rows < BN;
-                    const int c_lo = my_pos - q0 - part * 16, c_hi = t.rows - part * 16;
-                    if (t.rows < BN) {   // rows behind the sequence's queries must not reach the products (both score products done with them)
+                    const int first = (u.t0 + j) * BN, rows = min(BN, sq.tq - first), q0 = sq.q_pos0 + first;
+                    const bool test = edge > q0 || rows < BN;
+                    const int c_lo = my_pos - q0 - half * 32, c_hi = rows - half * 32;
+                    if (rows < BN) {   // rows behind the sequence's queries must not reach the products (both score products done with them)
                         if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                         unsigned char* y = smem + shared_int(sy.y_slot[e]) * kSlotBytes;
-                        for (int i = tid; i < (BN - t.rows) * 32; i += kWeightThreads) {     // 32 x 16 bytes per row of the pair
-                            const int r = t.rows + i / 32, piece = i % 32;
+                        for (int i = tid; i < (BN - rows) * 32; i += 32 * kWeightWarps) {     // 32 x 16 bytes per row of the pair
+                            const int r = rows + i / 32, piece = i % 32;
                             *reinterpret_cast<uint4*>(y + (piece >> 4) * kYTile + ((piece >> 3) & 1) * kYHalf + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     tc_fence_after();
-                    tmem_ld16(ts, sv);
-                    float2 p[8];
+                    float2 p[16];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 l4 = nl[i / 2];
-                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2,
-                                                    (i & 1) == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
-                        p[i] = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-                    }
-                    if (test) {
+                    for (int c = 0; c < 2; ++c) {       // 16 columns at a time
+                        tmem_ld16(ts + 16 * c, sv);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
-                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                            const float4 l4 = nl[4 * c + i / 2];
+                            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2,
+                                                        (i & 1) == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
+                            p[8 * c + i] = make_float2(ex2_approx(z.x), ex2_approx(z.y));
                         }
-                    }
+                        if (test) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) pk[i] = pack_bf16(p[i].x, p[i].y);
-                    tmem_st8(ts, pk);
+                            for (int i = 8 * c; i < 8 * c + 8; ++i) {
+                                if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
+                                if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) pk[i] = pack_bf16(p[8 * c + i].x, p[8 * c + i].y);
+                        tmem_st8(ts + 16 * c, pk);
+                    }
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sy.p[b]);
                     if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                     tc_fence_after();
-                    tmem_ld16(ts + 64, sv);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 d4 = nd[i / 2];
-                        p[i] = __fmul2_rn(p[i], __fadd2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])),
-                                                          (i & 1) == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
-                    }
-                    if (test) {
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_ld16(ts + 64 + 16 * c, sv);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
-                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                            const float4 d4 = nd[4 * c + i / 2];
+                            float2 d = __fmul2_rn(p[8 * c + i], __fadd2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])),
+                                                                          (i & 1) == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
+                            if (test) {         // (0 times a NaN of a masked pair)
+                                const int col = 16 * c + 2 * i;
+                                if (col < c_lo || col >= c_hi) d.x = 0.f;
+                                if (col + 1 < c_lo || col + 1 >= c_hi) d.y = 0.f;
+                            }
+                            score2 = __fadd2_rn(score2, d);
+                            pk[i] = pack_bf16(d.x, d.y);
                         }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        score2 = __fadd2_rn(score2, p[i]);
-                        pk[i] = pack_bf16(p[i].x, p[i].y);
+                        tmem_st8(ts + 64 + 16 * c, pk);
                     }
                 } else {
                     const int cpos = next_pos;
                     if (j + 1 < u.n) next_pos = column_pos(u.t0 + j + 1);
-                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
-                    tc_fence_after();
-                    uint32_t tv[16];
-                    tmem_ld16_pair(ts, ts + 64, sv, tv);
                     const int far = __reduce_max_sync(0xffffffffu, cpos);
                     const bool test = far > edge;
                     const float2 l2 = make_float2(nlse, nlse), d2 = make_float2(ndelta, ndelta);
+                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
+                    tc_fence_after();
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, l2);
-                        const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-                        float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(tv[i]), __uint_as_float(tv[i + 1])), d2));
-                        if (test) {
-                            if (__shfl_sync(0xffffffffu, cpos, i) > my_pos) d.x = 0.f;
-                            if (__shfl_sync(0xffffffffu, cpos, i + 1) > my_pos) d.y = 0.f;
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t tv[16];
+                        tmem_ld16_pair(ts + 16 * c, ts + 64 + 16 * c, sv, tv);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, l2);
+                            const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
+                            float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(tv[i]), __uint_as_float(tv[i + 1])), d2));
+                            if (test) {
+                                if (__shfl_sync(0xffffffffu, cpos, 16 * c + i) > my_pos) d.x = 0.f;
+                                if (__shfl_sync(0xffffffffu, cpos, 16 * c + i + 1) > my_pos) d.y = 0.f;
+                            }
+                            pk[i / 2] = pack_bf16(d.x, d.y);
                         }
-                        pk[i / 2] = pack_bf16(d.x, d.y);
+                        tmem_st8(ts + 64 + 16 * c, pk);
                     }
                     // Keys that some query of the tile does not see, and rows behind the segment: dS is 0 there, but 0 times
                     // what the row holds need not be.  Rows behind the segment are zeroed, NaN and infinities of the others
-                    // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 4 rows of its 16 columns'.
+                    // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 8 rows of its half.
                     if (far > sq.q_pos0 + u.first) {
-                        const int r = part * 16 + (warp & 3) * 4 + (lane >> 3), piece = lane & 7;
-                        uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece >> 2) * kYHalf + r * 128 + (piece & 3) * 32);
+                        const int rows = tile_of(sq, u, u.t0 + j).rows;
+                        const int r = half * 32 + (warp & 3) * 8 + (lane >> 2), piece = lane & 3;
+                        uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece >> 1) * kYHalf + r * 128 + (piece & 1) * 64);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             const uint4 w = y[i];
-                            y[i] = r >= t.rows ? make_uint4(0, 0, 0, 0) : make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
+                            y[i] = r >= rows ? make_uint4(0, 0, 0, 0) : make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                 }
-                tmem_st8(ts + 64, pk);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.d[b]);
                 buf.use(u.keys);
-                if (j == 0 && pending) {      // (the unit before: its last accumulation has had this tile's time to complete)
-                    pending = false;
-                    finish(before, before_score);
-                    if (!ok) break;
-                }
             }
             if (!ok) break;
-            if (pending) finish(before, before_score);       // (a unit without tiles came between)
-            pending = ok;
-            before = u;
-            before_score = score2.x + score2.y;
+            if (live && u.keys && u.cached && a.dscore != nullptr)
+                a.score_part[(static_cast<size_t>(u.h) * 2 + half) * a.score_rows + u.row0 + row] = score2.x + score2.y;
         }
-        if (ok && pending) finish(before, before_score);
+    } else {
+        // ---- the end of a unit: a thread takes its row of the accumulators, 32 columns at a time -------------------------------------
+        const int row = tid & (BM - 1);
+        const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        int x = 0;
+        uint32_t turn = 0;
+        // the four warps meet (a barrier with a bounded wait: a warp that has left must not hold the others)
+        auto meet = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sy.meet);
+            if (!warp_wait(&sy.meet, turn & 1u)) ok = false;
+            ++turn;
+        };
+        for (int k = 0; ok; ++k) {
+            const int id = unit_number(k);
+            if (id < 0) { ok = id == -1; break; }
+            unit_read(k);
+            const Unit u = unit_of(g, H, id);
+            const BackwardSeq& sq = g.seq[u.i];
+            const bool live = row < u.rows;
+            const size_t at = (static_cast<size_t>(u.row0 + row) * H + u.h) * DH;
+            const bool cut = !u.keys && sq.nchunk > 1;
+            const size_t unit0 = cut ? static_cast<size_t>(sq.part0 + (u.qt * H + u.h) * sq.nchunk) : 0u;
+            float* const mine = a.dq_part + (unit0 + u.chunk) * (BM * DH) + row;     // [feature][row]: a warp's lanes write consecutive floats
+            void* const out[2] = {u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ, u.cached ? a.dcV : a.dlV};
+            const int outs = u.keys ? 2 : 1;
+            if (u.n > 0) {
+                if (!warp_wait(&sy.done, static_cast<uint32_t>(x) & 1u)) { ok = false; break; }
+                tc_fence_after();
+                const int xs = shared_int(sy.x_slot[x & 1]);
+                const bool boxed = (row | 63) < u.rows;       // all 64 rows of the row's box are live
+                for (int o = 0; o < outs; ++o) {
+                    const float f = o == 0 ? scale : 1.f;
+                    unsigned char* const stage = smem + ((xs >> (8 * o)) & 255) * kSlotBytes + row * 128;     // swizzled halves of 64 features
+                    __nv_bfloat16* const direct = static_cast<__nv_bfloat16*>(out[o]) + at;
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32(tmem + o * kColAcc2 + c * 32 + lane_sel, v);
+                        if (cut) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * BM] = __uint_as_float(v[e]);
+                            continue;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint4 q = make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
+                                                       pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
+                                                       pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
+                                                       pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
+                            if (boxed) *reinterpret_cast<uint4*>(stage + (c >> 1) * kXHalf + ((((c & 1) * 4 + e) ^ (row & 7)) << 4)) = q;
+                            else if (live) *reinterpret_cast<uint4*>(direct + c * 32 + 8 * e) = q;
+                        }
+                    }
+                }
+                tc_fence_before();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sy.epi);
+                    mbar_arrive(&sy.staged[x & 1]);
+                }
+                ++x;
+            } else if (cut) {             // an empty chunk's partial
+                for (int e = 0; e < DH; ++e) mine[e * BM] = 0.f;
+            } else if (live) {            // nothing was summed: zeros
+                for (int o = 0; o < outs; ++o)
+                    for (int e = 0; e < DH / 8; ++e) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out[o]) + at + 8 * e) = make_uint4(0, 0, 0, 0);
+            }
+            if (!cut) continue;
+            // ---- the last chunk of a query tile to arrive adds up all of them, in chunk order
+            __threadfence();
+            meet();
+            if (ok && tid == 32 * kWeightWarps) {
+                int* counter = a.tickets + sq.qtick0 + u.qt * H + u.h;
+                const int t = atomicAdd(counter, 1);
+                *reinterpret_cast<volatile int*>(&sy.last) = t == sq.nchunk - 1;
+                if (t == sq.nchunk - 1) *counter = 0;
+            }
+            if (ok) meet();
+            if (!ok) break;
+            if (shared_int(sy.last)) {
+                __threadfence();
+#pragma unroll 1
+                for (int c = 0; c < DH / 16; ++c) {
+                    float o[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+                    for (int n = 0; n < sq.nchunk; ++n) {
+                        const float* src = a.dq_part + (unit0 + n) * (BM * DH) + (c * 16) * BM + row;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] += __ldcg(src + e * BM);
+                    }
+                    if (live) {
+                        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dQ) + at + c * 16);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            dst[e] = make_uint4(pack_bf16(o[8 * e] * scale, o[8 * e + 1] * scale), pack_bf16(o[8 * e + 2] * scale, o[8 * e + 3] * scale),
+                                                pack_bf16(o[8 * e + 4] * scale, o[8 * e + 5] * scale), pack_bf16(o[8 * e + 6] * scale, o[8 * e + 7] * scale));
+                    }
+                }
+            }
+            meet();     // `last` is free again
+        }
     }
     if (!ok) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
     tc_fence_before();
@@ -781,5 +771,5 @@ int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const Backw
     backward_dense_kernel<<<grid, kThreads, smem, st>>>(maps, g, a, H, sm_scale, next_unit, ctx->dev_status);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient launch");
-    return dodo_launch_backward_scores(ctx, g, a, 4 * H, st);
+    return dodo_launch_backward_scores(ctx, g, a, 2 * H, st);
 }

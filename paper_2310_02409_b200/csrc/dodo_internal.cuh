@@ -296,7 +296,7 @@ struct BackwardArrays {
     // statistics, per head and run of 64 entries: 64 x -(log-sum-exp in base 2), -inf where nothing is visible, then
     // 64 x -(sum of dO * O).  One address per entry and head: entry e's first is stats + (h * stat_rows + e / 64 * 64) * 2 + e % 64
     float* stats;
-    float* score_part;              // [H][score_rows], tensor-core kernel: [4 H][score_rows]
+    float* score_part;              // [H][score_rows], tensor-core kernel: [2 H][score_rows]
     float* dq_part;                 // partial tiles of dQ
     int score_rows;
     int* tickets;
