@@ -92,30 +92,39 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
-// 16 columns each of the warp's 32 TMEM lanes at two addresses (early-clobber outputs: the second address is read after the
-// first load has been issued)
-__device__ __forceinline__ void tmem_ld16_pair(uint32_t a, uint32_t b, uint32_t* x, uint32_t* y) {
+// 32 columns of the warp's 32 TMEM lanes; the caller waits (tmem_wait_ld) before it uses them
+__device__ __forceinline__ void tmem_ld32_async(uint32_t a, uint32_t* v) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=&r"(x[0]), "=&r"(x[1]), "=&r"(x[2]), "=&r"(x[3]), "=&r"(x[4]), "=&r"(x[5]), "=&r"(x[6]), "=&r"(x[7]),
-          "=&r"(x[8]), "=&r"(x[9]), "=&r"(x[10]), "=&r"(x[11]), "=&r"(x[12]), "=&r"(x[13]), "=&r"(x[14]), "=&r"(x[15]),
-          "=&r"(y[0]), "=&r"(y[1]), "=&r"(y[2]), "=&r"(y[3]), "=&r"(y[4]), "=&r"(y[5]), "=&r"(y[6]), "=&r"(y[7]),
-          "=&r"(y[8]), "=&r"(y[9]), "=&r"(y[10]), "=&r"(y[11]), "=&r"(y[12]), "=&r"(y[13]), "=&r"(y[14]), "=&r"(y[15])
-        : "r"(a), "r"(b) : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t a, const uint32_t* v) {     // (the caller waits)
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* x) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]),
-          "=r"(x[8]), "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(a) : "memory");
+}
+// (the values pass through, so that nothing that uses them moves ahead of the wait)
+__device__ __forceinline__ void tmem_wait_ld(uint32_t* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+          "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+          "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+          "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
+}
+__device__ __forceinline__ void tmem_st16_async(uint32_t a, const uint32_t* v) {     // (the caller waits)
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+// a wait that may take long, by a warp that nobody is in a hurry for: sleeps between polls, which otherwise take issue slots
+__device__ __forceinline__ bool slow_wait(uint64_t* bar, uint32_t parity) {
+    for (int i = 0; i < kWaitPolls / 16; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        __nanosleep(128);
+    }
+    return false;
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
@@ -407,15 +416,14 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                 const int ys = __reduce_max_sync(0xffffffffu, shared_int(sy.y_slot[e]));
                 const uint64_t y1 = desc_mnmajor(base + ys * kSlotBytes, kYHalf), y2 = desc_mnmajor(base + ys * kSlotBytes + kYTile, kYHalf);
-                // (16 rows of Y = 8 columns of pairs, at the first 8 of the 16 score columns they came from: each chunk of 16
-                // columns is read before it is written over)
+                // (16 rows of Y = 8 columns of pairs; a row's two threads keep to their own half of the S and T columns)
                 if (keys) {
                     if (!warp_wait(&sy.p[buf.cur], buf.key_phase())) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
                         for (int i = 0; i < BN / 16; ++i)
-                            mma_bf16_ts(tmem + kColAcc2, p + i * 16, y2 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
+                            mma_bf16_ts(tmem + kColAcc2, p + (i / 2) * 32 + (i % 2) * 8, y2 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
                     }
                     __syncwarp();
                 }
@@ -424,7 +432,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < BN / 16; ++i)
-                        mma_bf16_ts(tmem, p + 64 + i * 16, y1 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
+                        mma_bf16_ts(tmem, p + 64 + (i / 2) * 32 + (i % 2) * 8, y1 + static_cast<uint64_t>((i * 2048) >> 4), idesc, j > 0 || i > 0);
                     mma_commit(&sy.a[buf.cur]);
                     mma_commit(&sy.yfree[e]);
                     if (j == n - 1) mma_commit(&sy.done);
@@ -446,7 +454,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 const Unit u = unit_of(g, H, id);
                 if (u.n == 0) continue;
                 const int xe = x & 1;
-                if (!mbar_wait(&sy.staged[xe], static_cast<uint32_t>(x >> 1) & 1u)) { ok = false; break; }
+                if (!slow_wait(&sy.staged[xe], static_cast<uint32_t>(x >> 1) & 1u)) { ok = false; break; }
                 if (u.keys || g.seq[u.i].nchunk == 1) {
                     const int xs = shared_int(sy.x_slot[xe]);
                     const CUtensorMap* o1 = !u.keys ? &maps.dQ : u.cached ? &maps.dcK : &maps.dlK;
@@ -514,7 +522,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 buf.next(u.keys);
                 const int e = m % kRing, b = buf.cur;
                 const uint32_t ts = tmem + score_col(b) + half * 32 + lane_sel;
-                uint32_t sv[16], pk[8];
+                uint32_t sv[32], pk[16];
                 if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
                 // (this warp sees the tile's own barrier too: the statistics came with it, and rows may have to be cleared)
                 if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
@@ -534,51 +542,51 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     tc_fence_after();
+                    tmem_ld32_async(ts, sv);
+                    tmem_wait_ld(sv);
                     float2 p[16];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {       // 16 columns at a time
-                        tmem_ld16(ts + 16 * c, sv);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 l4 = nl[4 * c + i / 2];
-                            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2,
-                                                        (i & 1) == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
-                            p[8 * c + i] = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-                        }
-                        if (test) {
-#pragma unroll
-                            for (int i = 8 * c; i < 8 * c + 8; ++i) {
-                                if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
-                                if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) pk[i] = pack_bf16(p[8 * c + i].x, p[8 * c + i].y);
-                        tmem_st8(ts + 16 * c, pk);
+                    for (int i = 0; i < 16; ++i) {
+                        const float4 l4 = nl[i / 2];
+                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2,
+                                                    (i & 1) == 0 ? make_float2(l4.x, l4.y) : make_float2(l4.z, l4.w));
+                        p[i] = make_float2(ex2_approx(z.x), ex2_approx(z.y));
                     }
+                    if (test) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
+                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(p[i].x, p[i].y);
+                    tmem_st16_async(ts, pk);
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sy.p[b]);
                     if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                     tc_fence_after();
+                    tmem_ld32_async(ts + 64, sv);
+                    tmem_wait_ld(sv);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        tmem_ld16(ts + 64 + 16 * c, sv);
+                    for (int i = 0; i < 16; ++i) {
+                        const float4 d4 = nd[i / 2];
+                        p[i] = __fmul2_rn(p[i], __fadd2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])),
+                                                          (i & 1) == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
+                    }
+                    if (test) {         // (0 times a NaN of a masked pair)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 d4 = nd[4 * c + i / 2];
-                            float2 d = __fmul2_rn(p[8 * c + i], __fadd2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])),
-                                                                          (i & 1) == 0 ? make_float2(d4.x, d4.y) : make_float2(d4.z, d4.w)));
-                            if (test) {         // (0 times a NaN of a masked pair)
-                                const int col = 16 * c + 2 * i;
-                                if (col < c_lo || col >= c_hi) d.x = 0.f;
-                                if (col + 1 < c_lo || col + 1 >= c_hi) d.y = 0.f;
-                            }
-                            score2 = __fadd2_rn(score2, d);
-                            pk[i] = pack_bf16(d.x, d.y);
+                        for (int i = 0; i < 16; ++i) {
+                            if (2 * i < c_lo || 2 * i >= c_hi) p[i].x = 0.f;
+                            if (2 * i + 1 < c_lo || 2 * i + 1 >= c_hi) p[i].y = 0.f;
                         }
-                        tmem_st8(ts + 64 + 16 * c, pk);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        score2 = __fadd2_rn(score2, p[i]);
+                        pk[i] = pack_bf16(p[i].x, p[i].y);
                     }
                 } else {
                     const int cpos = next_pos;
@@ -588,23 +596,27 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     const float2 l2 = make_float2(nlse, nlse), d2 = make_float2(ndelta, ndelta);
                     if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                     tc_fence_after();
+                    uint32_t tv[32];
+                    tmem_ld32_async(ts, sv);
+                    tmem_ld32_async(ts + 64, tv);
+                    tmem_wait_ld(sv);
+                    tmem_wait_ld(tv);
+                    float2 d[16];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t tv[16];
-                        tmem_ld16_pair(ts + 16 * c, ts + 64 + 16 * c, sv, tv);
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, l2);
-                            const float2 p = make_float2(ex2_approx(z.x), ex2_approx(z.y));
-                            float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(tv[i]), __uint_as_float(tv[i + 1])), d2));
-                            if (test) {
-                                if (__shfl_sync(0xffffffffu, cpos, 16 * c + i) > my_pos) d.x = 0.f;
-                                if (__shfl_sync(0xffffffffu, cpos, 16 * c + i + 1) > my_pos) d.y = 0.f;
-                            }
-                            pk[i / 2] = pack_bf16(d.x, d.y);
-                        }
-                        tmem_st8(ts + 64 + 16 * c, pk);
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 z = __ffma2_rn(make_float2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), c2, l2);
+                        d[i] = __fmul2_rn(make_float2(ex2_approx(z.x), ex2_approx(z.y)),
+                                          __fadd2_rn(make_float2(__uint_as_float(tv[2 * i]), __uint_as_float(tv[2 * i + 1])), d2));
                     }
+                    if (test) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (__shfl_sync(0xffffffffu, cpos, 2 * i) > my_pos) d[i].x = 0.f;
+                            if (__shfl_sync(0xffffffffu, cpos, 2 * i + 1) > my_pos) d[i].y = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(d[i].x, d[i].y);
                     // Keys that some query of the tile does not see, and rows behind the segment: dS is 0 there, but 0 times
                     // what the row holds need not be.  Rows behind the segment are zeroed, NaN and infinities of the others
                     // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 8 rows of its half.
@@ -620,6 +632,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                 }
+                tmem_st16_async(ts + 64, pk);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
@@ -657,7 +670,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             void* const out[2] = {u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ, u.cached ? a.dcV : a.dlV};
             const int outs = u.keys ? 2 : 1;
             if (u.n > 0) {
-                if (!warp_wait(&sy.done, static_cast<uint32_t>(x) & 1u)) { ok = false; break; }
+                if (__all_sync(0xffffffffu, slow_wait(&sy.done, static_cast<uint32_t>(x) & 1u)) == 0) { ok = false; break; }
                 tc_fence_after();
                 const int xs = shared_int(sy.x_slot[x & 1]);
                 const bool boxed = (row | 63) < u.rows;       // all 64 rows of the row's box are live
