@@ -289,9 +289,11 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         ++freed;
                     } else if (xfreed < x && mbar_try_wait(&sy.xdone[xfreed & 1], static_cast<uint32_t>(xfreed >> 1) & 1u)) {
                         pair_back();
-                    } else if (i >= kWaitPolls) {
+                    } else if (i >= kWaitPolls / 16) {
                         ok = false;
                         return 0;
+                    } else {
+                        __nanosleep(32);
                     }
                 }
                 const int s = __ffs(static_cast<int>(free_slots)) - 1;
@@ -523,10 +525,10 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 const int e = m % kRing, b = buf.cur;
                 const uint32_t ts = tmem + score_col(b) + half * 32 + lane_sel;
                 uint32_t sv[32], pk[16];
-                if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
-                // (this warp sees the tile's own barrier too: the statistics came with it, and rows may have to be cleared)
-                if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                 if (u.keys) {
+                    if (!warp_wait(&sy.s[b], buf.phase())) { ok = false; break; }
+                    // (this warp sees the tile's own barrier too: the statistics came with it, and rows may have to be cleared)
+                    if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                     const float4* nl = reinterpret_cast<const float4*>(smem + kOffStat + (m % kMostTiles) * kStatBytes) + half * 8;
                     const float4* nd = nl + 16;
                     const int first = (u.t0 + j) * BN, rows = min(BN, sq.tq - first), q0 = sq.q_pos0 + first;
@@ -594,7 +596,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     const int far = __reduce_max_sync(0xffffffffu, cpos);
                     const bool test = far > edge;
                     const float2 l2 = make_float2(nlse, nlse), d2 = make_float2(ndelta, ndelta);
-                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
+                    if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }     // (T is issued behind S by the same thread)
                     tc_fence_after();
                     uint32_t tv[32];
                     tmem_ld32_async(ts, sv);
@@ -621,6 +623,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     // what the row holds need not be.  Rows behind the segment are zeroed, NaN and infinities of the others
                     // replaced by 0 (a query that sees such a key has a NaN in dS).  Each warp takes 8 rows of its half.
                     if (far > sq.q_pos0 + u.first) {
+                        if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                         const int rows = tile_of(sq, u, u.t0 + j).rows;
                         const int r = half * 32 + (warp & 3) * 8 + (lane >> 2), piece = lane & 3;
                         uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece >> 1) * kYHalf + r * 128 + (piece & 1) * 64);
