@@ -66,7 +66,7 @@ struct Sync {
     uint64_t x[2], xdone[2], staged[2];                  // a unit's pair: here, its slots free again, its results staged in them
     uint64_t y[kRing], yfree[kRing];                     // a tile: here, consumed
     uint64_t s[3], t[3], p[3], d[3], a[3];               // a score buffer: S, T, P, dS there; consumed
-    uint64_t done, epi, meet, unit[kAhead], unit_free[kAhead];
+    uint64_t done, epi[2], meet, unit[kAhead], unit_free[kAhead];     // accumulators: complete; read out (each of the two)
     int x_slot[2];           // slots of a unit's pair (first | second << 8), units with tiles counted
     int y_slot[kRing];       // a tile's slot
     int release[kRing];      // producer: slots that come back with a tile
@@ -245,7 +245,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
         }
         for (int i = 0; i < kAhead; ++i) { mbar_init(&sy.unit[i], 1); mbar_init(&sy.unit_free[i], 3 + kWeightWarps + kEndWarps); }
         mbar_init(&sy.done, 1);
-        mbar_init(&sy.epi, kEndWarps);
+        for (int i = 0; i < 2; ++i) mbar_init(&sy.epi[i], kEndWarps);
         mbar_init(&sy.meet, kEndWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -375,12 +375,12 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             for (int j = 0; j < n; ++j, ++m) {
                 const int e = m % kRing;
                 buf.next(keys);
-                if (buf.again() && !warp_wait(&sy.a[buf.cur], buf.phase() ^ 1u)) { ok = false; break; }    // the P and dS before have been consumed
                 if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                 const int ys = __reduce_max_sync(0xffffffffu, shared_int(sy.y_slot[e]));
-                tc_fence_after();
                 const uint64_t b1 = desc_kmajor(base + ys * kSlotBytes), b2 = desc_kmajor(base + ys * kSlotBytes + kYTile);
                 const uint32_t d = tmem + score_col(buf.cur);
+                if (buf.again() && !warp_wait(&sy.a[buf.cur], buf.phase() ^ 1u)) { ok = false; break; }    // the P and dS before have been consumed
+                tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < DH / 16; ++i)
@@ -410,7 +410,6 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             const int n = __reduce_max_sync(0xffffffffu, unit_of(g, H, id).n);
             const bool keys = id >= g.q_blocks;
             if (n == 0) continue;
-            if (x >= 1 && !warp_wait(&sy.epi, static_cast<uint32_t>(x - 1) & 1u)) { ok = false; break; }   // the last unit's accumulators are out
             for (int j = 0; j < n; ++j, ++m) {
                 const int e = m % kRing;
                 buf.next(keys);
@@ -420,6 +419,8 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 const uint64_t y1 = desc_mnmajor(base + ys * kSlotBytes, kYHalf), y2 = desc_mnmajor(base + ys * kSlotBytes + kYTile, kYHalf);
                 // (16 rows of Y = 8 columns of pairs; a row's two threads keep to their own half of the S and T columns)
                 if (keys) {
+                    // (the last unit's accumulators are out; where that was a query unit, its tiles in score buffer 2 are done with)
+                    if (j == 0 && x >= 1 && !warp_wait(&sy.epi[1], static_cast<uint32_t>(x - 1) & 1u)) { ok = false; break; }
                     if (!warp_wait(&sy.p[buf.cur], buf.key_phase())) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
@@ -429,6 +430,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     }
                     __syncwarp();
                 }
+                if (j == 0 && x >= 1 && !warp_wait(&sy.epi[0], static_cast<uint32_t>(x - 1) & 1u)) { ok = false; break; }
                 if (!warp_wait(&sy.d[buf.cur], buf.phase())) { ok = false; break; }
                 tc_fence_after();
                 if (elect_one()) {
@@ -677,37 +679,48 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 tc_fence_after();
                 const int xs = shared_int(sy.x_slot[x & 1]);
                 const bool boxed = (row | 63) < u.rows;       // all 64 rows of the row's box are live
-                for (int o = 0; o < outs; ++o) {
-                    const float f = o == 0 ? scale : 1.f;
-                    unsigned char* const stage = smem + ((xs >> (8 * o)) & 255) * kSlotBytes + row * 128;     // swizzled halves of 64 features
-                    __nv_bfloat16* const direct = static_cast<__nv_bfloat16*>(out[o]) + at;
+                // dV first: its accumulation is the first of the next unit's
+                for (int o = 1; o >= 0; --o) {
+                    if (o < outs) {
+                        const float f = o == 0 ? scale : 1.f;
+                        unsigned char* const stage = smem + ((xs >> (8 * o)) & 255) * kSlotBytes + row * 128;     // swizzled halves of 64 features
+                        __nv_bfloat16* const direct = static_cast<__nv_bfloat16*>(out[o]) + at;
+                        uint32_t va[32], vb[32];
+                        auto put = [&](int c, const uint32_t* v) {
+                            if (cut) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * BM] = __uint_as_float(v[e]);
+                                return;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint4 q = make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
+                                                           pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
+                                                           pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
+                                                           pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
+                                if (boxed) *reinterpret_cast<uint4*>(stage + (c >> 1) * kXHalf + ((((c & 1) * 4 + e) ^ (row & 7)) << 4)) = q;
+                                else if (live) *reinterpret_cast<uint4*>(direct + c * 32 + 8 * e) = q;
+                            }
+                        };
+                        const uint32_t col = tmem + o * kColAcc2 + lane_sel;
+                        tmem_ld32_async(col, va);
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tmem_ld32(tmem + o * kColAcc2 + c * 32 + lane_sel, v);
-                        if (cut) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * BM] = __uint_as_float(v[e]);
-                            continue;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint4 q = make_uint4(pack_bf16(__uint_as_float(v[8 * e]) * f, __uint_as_float(v[8 * e + 1]) * f),
-                                                       pack_bf16(__uint_as_float(v[8 * e + 2]) * f, __uint_as_float(v[8 * e + 3]) * f),
-                                                       pack_bf16(__uint_as_float(v[8 * e + 4]) * f, __uint_as_float(v[8 * e + 5]) * f),
-                                                       pack_bf16(__uint_as_float(v[8 * e + 6]) * f, __uint_as_float(v[8 * e + 7]) * f));
-                            if (boxed) *reinterpret_cast<uint4*>(stage + (c >> 1) * kXHalf + ((((c & 1) * 4 + e) ^ (row & 7)) << 4)) = q;
-                            else if (live) *reinterpret_cast<uint4*>(direct + c * 32 + 8 * e) = q;
+                        for (int c = 0; c < 4; c += 2) {       // the next columns are on their way while these are put away
+                            tmem_wait_ld(va);
+                            tmem_ld32_async(col + (c + 1) * 32, vb);
+                            put(c, va);
+                            tmem_wait_ld(vb);
+                            if (c == 0) tmem_ld32_async(col + 64, va);
+                            put(c + 1, vb);
                         }
                     }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sy.epi[o]);
                 }
-                tc_fence_before();
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sy.epi);
-                    mbar_arrive(&sy.staged[x & 1]);
-                }
+                if (lane == 0) mbar_arrive(&sy.staged[x & 1]);
                 ++x;
             } else if (cut) {             // an empty chunk's partial
                 for (int e = 0; e < DH; ++e) mine[e * BM] = 0.f;
