@@ -35,9 +35,9 @@ template <> __device__ __forceinline__ uint4 pack16<float>(const float* f) {
 template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) {
     return make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
 }
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
 __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
     return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
                        __uint_as_float(v.y & 0xffff0000u));
 }
@@ -92,6 +92,20 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
     const int k0 = min(n_keys, chunk * sq.ctiles * NB), k1 = min(n_keys, k0 + sq.ctiles * NB);
     const size_t row_elems = static_cast<size_t>(H) * DH;
     const size_t col = static_cast<size_t>(h) * DH + lig * E;
+    // ahead of the dependency wait, hints to L2 for the rows of the first batches (a hint brings nothing into the SM, and L2 is
+    // where writes of the kernel before would land too)
+    if (lig % 8 == 0) {
+#pragma unroll
+        for (int u = 0; u < 2 * U; ++u) {
+            const int j = k0 + u * NB + bundle;
+            if (j < k1) {
+                const bool cached = j < sq.c_len;
+                const size_t at = static_cast<size_t>(cached ? sq.c_row0 + j : sq.l_row0 + (j - sq.c_len)) * row_elems + col;
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const T*>(cached ? a.cK : a.lK) + at));
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const T*>(cached ? a.cV : a.lV) + at));
+            }
+        }
+    }
     dodo_grid_dependency_sync();
 
     float q[QT][E], go[QT][E], dq[QT][E], nlse[QT], delta[QT];
@@ -337,14 +351,22 @@ __device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a,
     if (part == 0) dst[q] = q < nq ? make_float2(minus_lse2(__ldg(a.lse + row)), -d) : make_float2(-INFINITY, 0.f);
 }
 
-template <typename T, int DH>
-__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const T* src, size_t row_elems, int row0, int rows, int n) {
-    constexpr int V4 = DH / 4;
-    for (int i = threadIdx.x; i < n * V4; i += kThreads) {
-        const int r = i / V4, c = i % V4;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < rows) v = load4(src + static_cast<size_t>(row0 + r) * row_elems + 4 * c);
-        *reinterpret_cast<float4*>(&dst[r][4 * c]) = v;
+// N rows of a head's matrix to shared memory, those from `rows` on as zeros; all of a thread's loads are issued before its stores
+template <int N, typename T, int DH>
+__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const T* src, size_t row_elems, int row0, int rows) {
+    constexpr int V4 = DH / 4, kIter = N * V4 / kThreads;
+    static_assert(N * V4 % kThreads == 0, "whole passes");
+    float4 v[kIter];
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+        const int at = threadIdx.x + i * kThreads, r = at / V4, c = at % V4;
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows) v[i] = load4(src + static_cast<size_t>(row0 + r) * row_elems + 4 * c);
+    }
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+        const int at = threadIdx.x + i * kThreads;
+        *reinterpret_cast<float4*>(&dst[at / V4][4 * (at % V4)]) = v[i];
     }
 }
 // dot products of a 4-key x 2-query register tile, over all features, of (K, Q) and (V, dO)
@@ -418,8 +440,8 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
         const T* gk = static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH;
         const T* gv = static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH;
-        load_rows<T, DH>(sm.K, gk, row_elems, row0, rows, TK);
-        load_rows<T, DH>(sm.V, gv, row_elems, row0, rows, TK);
+        load_rows<TK, T, DH>(sm.K, gk, row_elems, row0, rows);
+        load_rows<TK, T, DH>(sm.V, gv, row_elems, row0, rows);
         if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
         float dk[4][4 * ND], dv[4][4 * ND], score[4];
 #pragma unroll
@@ -432,9 +454,9 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int q_start = cached ? 0 : max(0, sq.l_pos0 + first - sq.q_pos0) / TQ * TQ;
         for (int q0 = q_start; q0 < sq.tq; q0 += TQ) {
             const int nq = min(TQ, sq.tq - q0);
-            __syncthreads();
-            load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-            load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+            if (q0 > q_start) __syncthreads();      // (the first queries come with the keys)
+            load_rows<TQ, T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+            load_rows<TQ, T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
             tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
             __syncthreads();
             tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
@@ -486,8 +508,8 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q0 + nq - sq.l_pos0));
     const int nt_c = (sq.c_len + TK - 1) / TK, nt = nt_c + (l_vis + TK - 1) / TK;
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
-    load_rows<T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
-    load_rows<T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq, TQ);
+    load_rows<TQ, T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+    load_rows<TQ, T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
     tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
     float dq[2][4 * ND];
 #pragma unroll
@@ -499,9 +521,9 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int first = (cached ? t : t - nt_c) * TK;
         const int rows = min(TK, (cached ? sq.c_len : l_vis) - first);
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
-        __syncthreads();
-        load_rows<T, DH>(sm.K, static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows, TK);
-        load_rows<T, DH>(sm.V, static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows, TK);
+        if (t > t0) __syncthreads();
+        load_rows<TK, T, DH>(sm.K, static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
+        load_rows<TK, T, DH>(sm.V, static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
         if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
         __syncthreads();
         tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);

@@ -152,17 +152,21 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* codes) {
     return word;
 }
 
-// One block per nugget.  A thread takes whole groups of 32 features (bf16: 64 bytes in two 32-byte loads), so a group's
-// extremes, step and reciprocal cost it no exchange and are found once; kUnroll groups' loads are in flight together.  Bound by
-// instruction issue (about 13 per feature) ahead of HBM: it reads two rows and writes 80 (dh 128) of their 256 bytes a head.
+// A thread takes one group of 32 features of one nugget's K or V row (bf16: 64 bytes in two 32-byte loads), so a group's
+// extremes, step and reciprocal cost it no exchange and are found once; the groups of all nuggets are laid end to end over the
+// threads, whatever a row's length.  Bound by instruction issue (about 20 per feature; 68 % of the issue slots busy) ahead of
+// HBM: it reads two rows and writes 80 (dh 128) of their 256 bytes a head.
 template <typename T>
 __global__ void __launch_bounds__(kGatherThreads, 4)
 gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __restrict__ V, int H, int dh,
                  const int32_t* __restrict__ idx, const __grid_constant__ GatherGroup g, unsigned char* __restrict__ cache_q4,
                  uint32_t* __restrict__ cache_scale, int32_t* __restrict__ cache_pos, int* __restrict__ dev_status) {
     constexpr int kWords = kGroup * static_cast<int>(sizeof(T)) / 4;    // storage words of a group
-    constexpr int kUnroll = 1;
-    const int j = g.idx0[0] + static_cast<int>(blockIdx.x);
+    const int per_head = dh / kGroup, groups = H * per_head;            // of K; as many of V
+    const long long item = static_cast<long long>(blockIdx.x) * kGatherThreads + threadIdx.x;
+    const int slot = static_cast<int>(item / (2 * groups)), i = static_cast<int>(item - static_cast<long long>(slot) * (2 * groups));
+    const int j = g.idx0[0] + slot;
+    if (j >= g.idx0[g.nseq]) return;
     int lo = 0, hi = g.nseq;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -172,41 +176,23 @@ gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __res
     dodo_grid_dependency_sync();   // the indices come from the kernel before
     const int token = __ldg(idx + j);
     if (static_cast<unsigned>(token) >= static_cast<unsigned>(g.n[b])) {
-        if (threadIdx.x == 0) atomicOr(dev_status, DODO_DEV_BAD_INDEX);
+        if (i == 0) atomicOr(dev_status, DODO_DEV_BAD_INDEX);
         return;
     }
-    const int per_head = dh / kGroup, groups = H * per_head;     // of K; as many of V
-    const size_t src = (static_cast<size_t>(g.src_row0[b]) + static_cast<size_t>(token)) * static_cast<size_t>(H) * dh * sizeof(T);
+    const int kv = i < groups ? 0 : 1, c = i - kv * groups, h = c / per_head;
+    const size_t src = ((static_cast<size_t>(g.src_row0[b]) + static_cast<size_t>(token)) * groups + c) * (kWords * 4);
+    uint32_t raw[kWords];
+#pragma unroll
+    for (int w = 0; w < kWords; w += 8) load32((kv == 0 ? K : V) + src + 4 * w, raw + w);
     const int dst_row = g.dst_row0[b] + (j - g.idx0[b]);
-    uint4* const q4 = reinterpret_cast<uint4*>(cache_q4 + static_cast<size_t>(dst_row) * H * dh);
-    uint32_t* const sc = cache_scale + static_cast<size_t>(dst_row) * (2 * groups);
-    if (threadIdx.x == 0) cache_pos[dst_row] = g.pos_base[b] + token;
-
-    for (int i0 = 0; i0 < 2 * groups; i0 += kUnroll * kGatherThreads) {
-        uint32_t raw[kUnroll][kWords];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int i = i0 + u * kGatherThreads + static_cast<int>(threadIdx.x);
-            if (i < 2 * groups) {
-                const unsigned char* p = (i < groups ? K + src : V + src) + static_cast<size_t>(i < groups ? i : i - groups) * (kWords * 4);
-#pragma unroll
-                for (int w = 0; w < kWords; w += 8) load32(p + 4 * w, raw[u] + w);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int i = i0 + u * kGatherThreads + static_cast<int>(threadIdx.x);
-            if (i >= 2 * groups) break;
-            float x[kGroup];
-            widen<T>(raw[u], x);
-            uint32_t codes[4];
-            const uint32_t word = quantise<sizeof(T) == 4>(x, codes);
-            const int kv = i < groups ? 0 : 1, c = i - kv * groups, h = c / per_head;
-            const int at = (h * 2 + kv) * per_head + (c - h * per_head);
-            q4[at] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-            sc[at] = word;
-        }
-    }
+    if (i == 0) cache_pos[dst_row] = g.pos_base[b] + token;
+    float x[kGroup];
+    widen<T>(raw, x);
+    uint32_t codes[4];
+    const uint32_t word = quantise<sizeof(T) == 4>(x, codes);
+    const size_t at = static_cast<size_t>(dst_row) * (2 * groups) + (h * 2 + kv) * per_head + (c - h * per_head);
+    reinterpret_cast<uint4*>(cache_q4)[at] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+    cache_scale[at] = word;
 }
 
 template <typename T> __device__ __forceinline__ void store_octet(T* p, const float* x);
@@ -278,7 +264,8 @@ int dodo_launch_gather_q4(dodo_ctx* ctx, const void* K, const void* V, int dtype
     const unsigned char* k = static_cast<const unsigned char*>(K);
     const unsigned char* v = static_cast<const unsigned char*>(V);
     unsigned char* q4 = static_cast<unsigned char*>(cache_q4);
-    const dim3 grid(static_cast<unsigned>(total)), block(kGatherThreads);
+    const long long items = static_cast<long long>(total) * 2 * H * (dh / kGroup);
+    const dim3 grid(static_cast<unsigned>((items + kGatherThreads - 1) / kGatherThreads)), block(kGatherThreads);
     const cudaError_t e = dtype == DODO_BF16
         ? dodo_launch_dependent(gather_q4_kernel<__nv_bfloat16>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status)
         : dodo_launch_dependent(gather_q4_kernel<float>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status);
