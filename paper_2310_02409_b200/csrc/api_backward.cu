@@ -148,7 +148,7 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
 
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
-    const int variant = max_tq <= kStreamQueries ? DODO_BWD_STREAM : dtype == DODO_BF16 && dh == 128 ? DODO_BWD_DENSE : DODO_BWD_TILE;
+    const int variant = max_tq <= kStreamQueries ? DODO_BWD_STREAM : dtype == DODO_BF16 ? DODO_BWD_DENSE : DODO_BWD_TILE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     BackwardArrays a;
     a.Q = Q; a.O = O; a.dO = dO; a.cK = cacheK; a.cV = cacheV; a.lK = locK; a.lV = locV;
@@ -176,7 +176,7 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
             } else {
                 rc = dodo_launch_backward_stats(ctx, dtype, H, dh, g, a, st);
                 if (rc == DODO_OK)
-                    rc = dodo_launch_backward_dense(ctx, H, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
+                    rc = dodo_launch_backward_dense(ctx, H, dh, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
                                                     ctx->tickets + DODO_NUM_TICKETS - 1, st);
             }
             if (rc != DODO_OK) return rc;

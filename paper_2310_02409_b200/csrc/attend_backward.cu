@@ -7,10 +7,10 @@
 // the gradients at its logits.  Every output row is summed by one owner in a fixed order (no atomics): results repeat
 // bit for bit.
 //
-// Two kernels here, a third (bf16, head size 128, blocks of queries) on the tensor cores in attend_backward_dense.cu:
+// Two kernels here, a third (blocks of bf16 queries) on the tensor cores in attend_backward_dense.cu:
 //   backward_stream_kernel  up to four queries per sequence (single-token steps).  All traffic, no reuse: one pass reads
 //       K and V once, writes dK and dV once and sums dQ, the queries and their dQ in registers.
-//   backward_tile_kernel    everything else (fp32, head size 64): key blocks and query blocks side by side in one launch,
+//   backward_tile_kernel    fp32 blocks: key blocks and query blocks side by side in one launch,
 //       64 keys x 32 queries at a time in shared memory, fp32 FMAs on register tiles.
 #include "dodo_internal.cuh"
 
@@ -631,8 +631,6 @@ int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const Bac
 int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a,
                               cudaStream_t st) {
     if (g.q_blocks + g.kv_blocks == 0) return DODO_OK;
-    if (dtype == DODO_BF16 && dh == 128) return launch_tile<__nv_bfloat16, 128>(ctx, 0, H, sm_scale, g, a, st);
-    if (dtype == DODO_BF16) return launch_tile<__nv_bfloat16, 64>(ctx, 1, H, sm_scale, g, a, st);
     if (dh == 128) return launch_tile<float, 128>(ctx, 2, H, sm_scale, g, a, st);
     return launch_tile<float, 64>(ctx, 3, H, sm_scale, g, a, st);
 }

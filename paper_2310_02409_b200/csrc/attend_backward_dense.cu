@@ -1,4 +1,4 @@
-// Gradient of attention for blocks of bf16 queries, head size 128, on the 5th-generation tensor cores (formulas in
+// Gradient of attention for blocks of bf16 queries, head size 64 or 128, on the 5th-generation tensor cores (formulas in
 // attend_backward.cu): tcgen05.mma with TMEM accumulators, operands staged by TMA.
 //
 // Two kinds of units, both 128 rows tall (rows = TMEM lanes), stream the other side's rows in tiles of 64:
@@ -40,7 +40,6 @@ namespace {
 
 using namespace sm100;
 
-constexpr int DH = 128;
 constexpr int BM = 128;                 // rows of a unit
 constexpr int BN = 64;                  // rows of a streamed tile
 constexpr int kWeightWarps = 8, kEndWarps = 4;
@@ -51,9 +50,9 @@ constexpr int kMostTiles = kSlots - 2;                // tiles on their way: a p
 constexpr int kRing = 8;                              // tiles' barriers (more than kMostTiles)
 constexpr int kAhead = 4;                             // units announced ahead
 constexpr int kXHalf = BM * 128;                      // 64 features of a stationary tile
-constexpr int kYHalf = BN * 128, kYTile = 2 * kYHalf;
+constexpr int kYHalf = BN * 128;
 constexpr int kStatBytes = BN * 8;
-static_assert(2 * kXHalf == kSlotBytes && 2 * kYTile == kSlotBytes, "slots");
+static_assert(2 * kXHalf == kSlotBytes && 4 * kYHalf == kSlotBytes, "slots hold head size 128");
 constexpr int kOffStat = kSlots * kSlotBytes;         // [kMostTiles][64 x -lse, 64 x -D]
 constexpr int kOffSync = kOffStat + kMostTiles * kStatBytes;
 constexpr uint32_t kTmemCols = 512;
@@ -223,9 +222,12 @@ struct Buffers {
     }
 };
 
+// DH: head size; a row has kH runs of 64 features, the width of a tensor copy's box
+template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_constant__ BackwardGroup g, const BackwardArrays a, int H,
                       float scale, int* __restrict__ next_unit, int* __restrict__ dev_status) {
+    constexpr int kH = DH / 64, kYTile = kH * kYHalf;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
     Sync& sy = *reinterpret_cast<Sync*>(smem + kOffSync);
@@ -326,8 +328,8 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 sy.x_slot[xe] = x1 | (x2 << 8);
                 const CUtensorMap* m1 = !u.keys ? &maps.Q : u.cached ? &maps.cK : &maps.lK;
                 const CUtensorMap* m2 = !u.keys ? &maps.dO : u.cached ? &maps.cV : &maps.lV;
-                mbar_expect_tx(&sy.x[xe], 2 * kSlotBytes);
-                for (int part = 0; part < 4; ++part) {      // (64 features, 64 rows) at a time
+                mbar_expect_tx(&sy.x[xe], 2 * kH * kXHalf);
+                for (int part = 0; part < 2 * kH; ++part) {      // (64 features, 64 rows) at a time
                     const uint32_t at = base + (part >> 1) * kXHalf + (part & 1) * (64 * 128);
                     tma_load_2d(at + x1 * kSlotBytes, m1, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &sy.x[xe]);
                     tma_load_2d(at + x2 * kSlotBytes, m2, col + (part >> 1) * 64, u.row0 + (part & 1) * 64, &sy.x[xe]);
@@ -342,11 +344,11 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     const uint32_t dst = base + slot * kSlotBytes;
                     sy.y_slot[e] = slot;
                     sy.release[e] = 1 << slot;
-                    mbar_expect_tx(&sy.y[e], kSlotBytes + (u.keys ? kStatBytes : 0));
-                    tma_load_2d(dst, y1, col, t.row0, &sy.y[e]);
-                    tma_load_2d(dst + kYHalf, y1, col + 64, t.row0, &sy.y[e]);
-                    tma_load_2d(dst + kYTile, y2, col, t.row0, &sy.y[e]);
-                    tma_load_2d(dst + kYTile + kYHalf, y2, col + 64, t.row0, &sy.y[e]);
+                    mbar_expect_tx(&sy.y[e], 2 * kYTile + (u.keys ? kStatBytes : 0));
+                    for (int c = 0; c < kH; ++c) {
+                        tma_load_2d(dst + c * kYHalf, y1, col + 64 * c, t.row0, &sy.y[e]);
+                        tma_load_2d(dst + kYTile + c * kYHalf, y2, col + 64 * c, t.row0, &sy.y[e]);
+                    }
                     if (u.keys)
                         bulk_load(base + kOffStat + (m % kMostTiles) * kStatBytes,
                                   a.stats + (static_cast<size_t>(u.h) * g.stat_rows + sq.stat0 + t.first) * 2, kStatBytes, &sy.y[e]);
@@ -464,7 +466,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     const CUtensorMap* o1 = !u.keys ? &maps.dQ : u.cached ? &maps.dcK : &maps.dlK;
                     const CUtensorMap* o2 = u.cached ? &maps.dcV : &maps.dlV;
                     for (int box = 0; box < u.rows / 64; ++box)
-                        for (int c = 0; c < 2; ++c) {
+                        for (int c = 0; c < kH; ++c) {
                             const uint32_t at = base + c * kXHalf + box * (64 * 128);
                             tma_store_2d(o1, u.h * DH + c * 64, u.row0 + box * 64, at + (xs & 255) * kSlotBytes);
                             if (u.keys) tma_store_2d(o2, u.h * DH + c * 64, u.row0 + box * 64, at + (xs >> 8) * kSlotBytes);
@@ -539,9 +541,9 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     if (rows < BN) {   // rows behind the sequence's queries must not reach the products (both score products done with them)
                         if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                         unsigned char* y = smem + shared_int(sy.y_slot[e]) * kSlotBytes;
-                        for (int i = tid; i < (BN - rows) * 32; i += 32 * kWeightWarps) {     // 32 x 16 bytes per row of the pair
-                            const int r = rows + i / 32, piece = i % 32;
-                            *reinterpret_cast<uint4*>(y + (piece >> 4) * kYTile + ((piece >> 3) & 1) * kYHalf + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        for (int i = tid; i < (BN - rows) * 16 * kH; i += 32 * kWeightWarps) {     // 16 bytes of a row of the pair
+                            const int r = rows + i / (16 * kH), piece = i % (16 * kH);
+                            *reinterpret_cast<uint4*>(y + (piece >> 3) * kYHalf + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
@@ -628,9 +630,9 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         if (!warp_wait(&sy.y[e], static_cast<uint32_t>(m / kRing) & 1u)) { ok = false; break; }
                         const int rows = tile_of(sq, u, u.t0 + j).rows;
                         const int r = half * 32 + (warp & 3) * 8 + (lane >> 2), piece = lane & 3;
-                        uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece >> 1) * kYHalf + r * 128 + (piece & 1) * 64);
+                        uint4* y = reinterpret_cast<uint4*>(smem + shared_int(sy.y_slot[e]) * kSlotBytes + (piece * kH / 4) * kYHalf + r * 128 + (piece * kH % 4) * 32);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < 2 * kH; ++i) {
                             const uint4 w = y[i];
                             y[i] = r >= rows ? make_uint4(0, 0, 0, 0) : make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
                         }
@@ -705,12 +707,12 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         const uint32_t col = tmem + o * kColAcc2 + lane_sel;
                         tmem_ld32_async(col, va);
 #pragma unroll 1
-                        for (int c = 0; c < 4; c += 2) {       // the next columns are on their way while these are put away
+                        for (int c = 0; c < 2 * kH; c += 2) {  // the next columns are on their way while these are put away
                             tmem_wait_ld(va);
                             tmem_ld32_async(col + (c + 1) * 32, vb);
                             put(c, va);
                             tmem_wait_ld(vb);
-                            if (c == 0) tmem_ld32_async(col + 64, va);
+                            if (c + 2 < 2 * kH) tmem_ld32_async(col + 64, va);
                             put(c + 1, vb);
                         }
                     }
@@ -775,7 +777,8 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
 
 BackwardTiles dodo_backward_dense_tiles() { return {BM, BM, BN}; }
 
-int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows, int cache_rows,
+template <int DH>
+static int launch_dense(dodo_ctx* ctx, int slot, int H, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows, int cache_rows,
                                int loc_rows, int* next_unit, cudaStream_t st) {
     const int total = g.q_blocks + g.kv_blocks;
     if (total == 0) return DODO_OK;
@@ -791,14 +794,20 @@ int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const Backw
         if (rc != DODO_OK) return rc;
     }
     const size_t smem = static_cast<size_t>(kSmemBytes);
-    if (!ctx->backward_attr_set[4]) {
-        const cudaError_t e = cudaFuncSetAttribute(backward_dense_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (!ctx->backward_attr_set[slot]) {
+        const cudaError_t e = cudaFuncSetAttribute(backward_dense_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient shared-memory attribute");
-        ctx->backward_attr_set[4] = true;
+        ctx->backward_attr_set[slot] = true;
     }
     const int grid = total < ctx->num_sms ? total : ctx->num_sms;
-    backward_dense_kernel<<<grid, kThreads, smem, st>>>(maps, g, a, H, sm_scale, next_unit, ctx->dev_status);
+    backward_dense_kernel<DH><<<grid, kThreads, smem, st>>>(maps, g, a, H, sm_scale, next_unit, ctx->dev_status);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient launch");
     return dodo_launch_backward_scores(ctx, g, a, 2 * H, st);
+}
+
+int dodo_launch_backward_dense(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
+                               int cache_rows, int loc_rows, int* next_unit, cudaStream_t st) {
+    return dh == 128 ? launch_dense<128>(ctx, 4, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st)
+                     : launch_dense<64>(ctx, 5, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st);
 }

@@ -308,9 +308,9 @@ BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh);
 int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, int max_tq, const BackwardGroup& g,
                                 const BackwardArrays& a, cudaStream_t st);
 int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st);
-// Blocks of bf16 queries at head size 128, on the tensor cores.  next_unit: a device counter, zero between launches
+// Blocks of bf16 queries on the tensor cores.  next_unit: a device counter, zero between launches
 BackwardTiles dodo_backward_dense_tiles();
-int dodo_launch_backward_dense(dodo_ctx* ctx, int H, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
+int dodo_launch_backward_dense(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
                                int cache_rows, int loc_rows, int* next_unit, cudaStream_t st);
 // dscore of the group's cache rows: the sum of `parts` rows of score_part, in order
 int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const BackwardArrays& a, int parts, cudaStream_t st);
