@@ -350,7 +350,8 @@ DODO_API int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_
  * Written rows are overwritten, not added to; keys that no query sees and queries that see no key get zeros.  Outputs must
  * not overlap inputs or each other.  Results repeat bit for bit.  A nugget's gradient is that of the cache row:
  * the row of K and V that it was gathered from has the same one.  Queries, O and dO must be finite; a row of K or V that a
- * query does not see does not reach that query's gradient, whatever it holds.
+ * query does not see does not reach that query's gradient, whatever it holds.  Positions of queries and local tokens lie in
+ * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.
  * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.
  */
 DODO_API size_t dodo_attend_backward_workspace_bytes(const dodo_ctx* ctx, int q_rows, int H, int dh, int cache_rows);
@@ -398,7 +399,9 @@ DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32
  * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
  * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
  * call takes the streaming kernel.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache
- * by other means than dodo_gather_kv_q4 calls dodo_cache_written.
+ * by other means than dodo_gather_kv_q4 calls dodo_cache_written.  Positions of queries and local tokens lie in
+ * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.  Steps s of cached values stay below 2^47 (values below
+ * about 2^50 in magnitude; larger ones may come out as NaN or infinity).
  *   cache_rows  cache_off[B] of the calls that the workspace is meant for
  *   everything else as in dodo_attend and dodo_gather_kv_q4
  * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.

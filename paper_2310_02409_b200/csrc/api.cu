@@ -567,6 +567,18 @@ int dodo_check_attend_queries(dodo_ctx* ctx, const int32_t* q_off, const int32_t
     return DODO_OK;
 }
 
+int dodo_check_positions(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, const int32_t* loc_len, const int32_t* loc_pos0, int B) {
+    constexpr int64_t kMost = int64_t{1} << 30;
+    auto fits = [&](int64_t first, int64_t n) { return n <= 0 || (first >= -kMost && first + n <= kMost); };
+    for (int b = 0; b < B; ++b) {
+        if (!fits(q_pos0[b], q_off[b + 1] - q_off[b]))
+            return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "sequence %d: query positions from %d leave [-2^30, 2^30)", b, q_pos0[b]);
+        if (loc_len != nullptr && loc_pos0 != nullptr && !fits(loc_pos0[b], loc_len[b]))
+            return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "sequence %d: local positions from %d leave [-2^30, 2^30)", b, loc_pos0[b]);
+    }
+    return DODO_OK;
+}
+
 int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_t* cache_len, const int32_t* loc_off,
                            const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, bool* any_cache, bool* any_local) {
     if (cache_len != nullptr) {

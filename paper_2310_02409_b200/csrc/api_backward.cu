@@ -98,7 +98,8 @@ int plan_group(dodo_ctx* ctx, const AttendShape& s, int variant, int b0, int nb,
     }
     for (int i = 0; i < nb; ++i) {
         g.seq[i].stick0 = static_cast<int>(qticks + sticks);
-        sticks += variant == DODO_BWD_STREAM ? g.seq[i].nchunk : ceil_div(g.seq[i].c_len, t.keys);
+        // (the tensor-core kernel leaves the scores to a kernel of their own)
+        sticks += variant == DODO_BWD_STREAM ? g.seq[i].nchunk : variant == DODO_BWD_TILE ? ceil_div(g.seq[i].c_len, t.keys) : 0;
     }
     if (qticks + sticks > DODO_NUM_TICKETS - 1)      // (the last counter hands out the tensor-core kernel's units)
         return dodo_fail(ctx, DODO_ERR_CAPACITY, "too many key tiles and split query tiles (%lld) in one group of sequences", static_cast<long long>(qticks + sticks));
@@ -133,6 +134,7 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
     bool any_cache = false, any_local = false;
     rc = dodo_check_attend_keys(ctx, cache_off, cache_len, loc_off, loc_len, loc_pos0, loc_rows, B, &any_cache, &any_local);
     if (rc != DODO_OK) return rc;
+    if ((rc = dodo_check_positions(ctx, q_off, q_pos0, loc_len, loc_pos0, B)) != DODO_OK) return rc;
     if (B == 0 || (q_off[B] == 0 && !any_cache && !any_local)) return DODO_OK;
     if (q_off[B] > 0 && (!usable(Q) || !usable(O) || !usable(dO) || !usable(dQ) || lse == nullptr))
         return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "Q, O, dO, dQ and lse must be non-NULL, all but lse 16-byte aligned");
@@ -172,9 +174,9 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
             if (variant == DODO_BWD_STREAM) {
                 rc = dodo_launch_backward_stream(ctx, dtype, H, dh, sm_scale, max_tq, g, a, st);
             } else if (variant == DODO_BWD_TILE) {
-                rc = dodo_launch_backward_tile(ctx, dtype, H, dh, sm_scale, g, a, st);
+                rc = dodo_launch_backward_tile(ctx, H, dh, sm_scale, g, a, st);
             } else {
-                rc = dodo_launch_backward_stats(ctx, dtype, H, dh, g, a, st);
+                rc = dodo_launch_backward_stats(ctx, H, dh, g, a, st);
                 if (rc == DODO_OK)
                     rc = dodo_launch_backward_dense(ctx, H, dh, sm_scale, g, a, q_off[B], a.score_rows, any_local ? loc_rows : 0,
                                                     ctx->tickets + DODO_NUM_TICKETS - 1, st);

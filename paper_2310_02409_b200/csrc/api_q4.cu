@@ -98,6 +98,7 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     bool any_cache = false, any_local = false;
     rc = dodo_check_attend_keys(ctx, cache_off, cache_len, loc_off, loc_len, loc_pos0, loc_rows, B, &any_cache, &any_local);
     if (rc != DODO_OK) return rc;
+    if ((rc = dodo_check_positions(ctx, q_off, q_pos0, loc_len, loc_pos0, B)) != DODO_OK) return rc;
     if (any_cache) {
         if ((rc = check_cache_arrays(ctx, cache_q4, cache_scale)) != DODO_OK) return rc;
         if (cache_pos == nullptr) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "cache_pos must not be NULL");

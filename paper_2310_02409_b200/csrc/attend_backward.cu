@@ -36,15 +36,7 @@ template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* 
     return make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
 }
 __device__ __forceinline__ float4 load4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
-                       __uint_as_float(v.y & 0xffff0000u));
-}
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(two_bf16(v.x, v.y), two_bf16(v.z, v.w));
-}
 // a query's statistic: minus the log-sum-exp in base 2, -inf (every weight comes out 0) where the query sees nothing
 __device__ __forceinline__ float minus_lse2(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
 
@@ -266,11 +258,10 @@ backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardG
 // (for the tensor-core kernel, whose statistics travel with its tiles; the others make their own)
 // -(log-sum-exp in base 2) and -(sum of dO * O) of every query, one row per head so that a tile's entries are contiguous;
 // entries behind a sequence's last query, up to a multiple of 64, are -inf and 0: such a column's weights come out 0.
-template <typename T>
 __global__ void __launch_bounds__(kThreads)
 backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, int DH) {
-    constexpr int E = Vec16<T>::kElems;
-    const int lpr = DH / E;                             // lanes per row: 8, 16 or 32
+    constexpr int E = Vec16<__nv_bfloat16>::kElems;
+    const int lpr = DH / E;                             // lanes per row: 8 or 16
     const int per_block = kThreads / lpr;
     const long long unit = static_cast<long long>(blockIdx.x) * per_block + threadIdx.x / lpr;   // (entry, head), heads fastest
     const int entry = static_cast<int>(unit / H), h = static_cast<int>(unit % H), lig = threadIdx.x % lpr;
@@ -283,8 +274,8 @@ backward_stats_kernel(const BackwardArrays a, const __grid_constant__ BackwardGr
     const size_t row = static_cast<size_t>(g.seq[b].q_row0 + q) * H + h;
     if (live) {
         float x[E], y[E];
-        Vec16<T>::unpack(ld_stream16(static_cast<const T*>(a.dO) + row * DH + lig * E), x);
-        Vec16<T>::unpack(ld_stream16(static_cast<const T*>(a.O) + row * DH + lig * E), y);
+        Vec16<__nv_bfloat16>::unpack(ld_stream16(static_cast<const __nv_bfloat16*>(a.dO) + row * DH + lig * E), x);
+        Vec16<__nv_bfloat16>::unpack(ld_stream16(static_cast<const __nv_bfloat16*>(a.O) + row * DH + lig * E), y);
 #pragma unroll
         for (int e = 0; e < E; ++e) d = fmaf(x[e], y[e], d);
     }
@@ -333,7 +324,7 @@ template <int DH> struct TileSmem {
 };
 
 // statistics of queries [q0, q0 + nq) of a sequence and head: eight threads a query
-template <typename T, int DH>
+template <int DH>
 __device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a, int H, int h, int row0, int nq) {
     const int q = threadIdx.x / 8, part = threadIdx.x % 8;
     float d = 0.f;
@@ -341,8 +332,8 @@ __device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a,
     if (q < nq) {
 #pragma unroll
         for (int i = 0; i < DH / 32; ++i) {
-            const float4 x = load4(static_cast<const T*>(a.dO) + row * DH + 4 * (part + 8 * i));
-            const float4 y = load4(static_cast<const T*>(a.O) + row * DH + 4 * (part + 8 * i));
+            const float4 x = load4(static_cast<const float*>(a.dO) + row * DH + 4 * (part + 8 * i));
+            const float4 y = load4(static_cast<const float*>(a.O) + row * DH + 4 * (part + 8 * i));
             d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
         }
     }
@@ -352,8 +343,8 @@ __device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a,
 }
 
 // N rows of a head's matrix to shared memory, those from `rows` on as zeros; all of a thread's loads are issued before its stores
-template <int N, typename T, int DH>
-__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const T* src, size_t row_elems, int row0, int rows) {
+template <int N, int DH>
+__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const float* src, size_t row_elems, int row0, int rows) {
     constexpr int V4 = DH / 4, kIter = N * V4 / kThreads;
     static_assert(N * V4 % kThreads == 0, "whole passes");
     float4 v[kIter];
@@ -412,7 +403,7 @@ __device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0
         }
 }
 
-template <typename T, int DH>
+template <int DH>
 __global__ void __launch_bounds__(kThreads)
 backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
     extern __shared__ __align__(16) unsigned char raw[];
@@ -438,10 +429,10 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int first = (cached ? tile : tile - nt_c) * TK;
         const int rows = min(TK, (cached ? sq.c_len : sq.l_len) - first);
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
-        const T* gk = static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH;
-        const T* gv = static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH;
-        load_rows<TK, T, DH>(sm.K, gk, row_elems, row0, rows);
-        load_rows<TK, T, DH>(sm.V, gv, row_elems, row0, rows);
+        const float* gk = static_cast<const float*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH;
+        const float* gv = static_cast<const float*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH;
+        load_rows<TK, DH>(sm.K, gk, row_elems, row0, rows);
+        load_rows<TK, DH>(sm.V, gv, row_elems, row0, rows);
         if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
         float dk[4][4 * ND], dv[4][4 * ND], score[4];
 #pragma unroll
@@ -455,9 +446,9 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         for (int q0 = q_start; q0 < sq.tq; q0 += TQ) {
             const int nq = min(TQ, sq.tq - q0);
             if (q0 > q_start) __syncthreads();      // (the first queries come with the keys)
-            load_rows<TQ, T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-            load_rows<TQ, T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-            tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
+            load_rows<TQ, DH>(sm.Q, static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+            load_rows<TQ, DH>(sm.G, static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+            tile_stats<DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
             __syncthreads();
             tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
             __syncthreads();
@@ -482,8 +473,8 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
                 }
             }
         }
-        T* ok = static_cast<T*>(cached ? a.dcK : a.dlK) + static_cast<size_t>(h) * DH;
-        T* ov = static_cast<T*>(cached ? a.dcV : a.dlV) + static_cast<size_t>(h) * DH;
+        float* ok = static_cast<float*>(cached ? a.dcK : a.dlK) + static_cast<size_t>(h) * DH;
+        float* ov = static_cast<float*>(cached ? a.dcV : a.dlV) + static_cast<size_t>(h) * DH;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int key = 4 * ty + i;
@@ -508,9 +499,9 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q0 + nq - sq.l_pos0));
     const int nt_c = (sq.c_len + TK - 1) / TK, nt = nt_c + (l_vis + TK - 1) / TK;
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
-    load_rows<TQ, T, DH>(sm.Q, static_cast<const T*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-    load_rows<TQ, T, DH>(sm.G, static_cast<const T*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-    tile_stats<T, DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
+    load_rows<TQ, DH>(sm.Q, static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+    load_rows<TQ, DH>(sm.G, static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+    tile_stats<DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
     float dq[2][4 * ND];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -522,8 +513,8 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int rows = min(TK, (cached ? sq.c_len : l_vis) - first);
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
         if (t > t0) __syncthreads();
-        load_rows<TK, T, DH>(sm.K, static_cast<const T*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
-        load_rows<TK, T, DH>(sm.V, static_cast<const T*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
+        load_rows<TK, DH>(sm.K, static_cast<const float*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
+        load_rows<TK, DH>(sm.V, static_cast<const float*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
         if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
         __syncthreads();
         tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
@@ -544,7 +535,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
             }
         }
     }
-    T* out = static_cast<T*>(a.dQ) + static_cast<size_t>(sq.q_row0 + q0) * row_elems + static_cast<size_t>(h) * DH;
+    float* out = static_cast<float*>(a.dQ) + static_cast<size_t>(sq.q_row0 + q0) * row_elems + static_cast<size_t>(h) * DH;
     const size_t part = static_cast<size_t>(sq.part0 + (qt * H + h) * sq.nchunk);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -578,9 +569,9 @@ int launch_stream(dodo_ctx* ctx, int H, float scale, int max_tq, const BackwardG
     return dodo_check_cuda(ctx, e, "attend gradient launch");
 }
 
-template <typename T, int DH>
+template <int DH>
 int launch_tile(dodo_ctx* ctx, int slot, int H, float scale, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
-    auto kern = backward_tile_kernel<T, DH>;
+    auto kern = backward_tile_kernel<DH>;
     const size_t smem = sizeof(TileSmem<DH>);
     if (!ctx->backward_attr_set[slot]) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
@@ -609,13 +600,12 @@ int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float s
     return launch_stream<float, 64>(ctx, H, sm_scale, max_tq, g, a, st);
 }
 
-int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
+int dodo_launch_backward_stats(dodo_ctx* ctx, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
     if (g.stat_rows == 0) return DODO_OK;
-    const int per_block = kThreads / (dh * static_cast<int>(dodo_elem_bytes(dtype)) / 16);
+    const int per_block = kThreads / (dh / 8);
     const long long units = static_cast<long long>(g.stat_rows) * H;
-    const dim3 grid(static_cast<unsigned>((units + per_block - 1) / per_block)), block(kThreads);
-    const cudaError_t e = dtype == DODO_BF16 ? dodo_launch_dependent(backward_stats_kernel<__nv_bfloat16>, grid, block, 0, st, a, g, H, dh)
-                                             : dodo_launch_dependent(backward_stats_kernel<float>, grid, block, 0, st, a, g, H, dh);
+    const cudaError_t e = dodo_launch_dependent(backward_stats_kernel, dim3(static_cast<unsigned>((units + per_block - 1) / per_block)), dim3(kThreads), 0,
+                                                st, a, g, H, dh);
     return dodo_check_cuda(ctx, e, "attend gradient statistics launch");
 }
 
@@ -628,9 +618,9 @@ int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const Bac
                            "attend gradient score launch");
 }
 
-int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a,
+int dodo_launch_backward_tile(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a,
                               cudaStream_t st) {
     if (g.q_blocks + g.kv_blocks == 0) return DODO_OK;
-    if (dh == 128) return launch_tile<float, 128>(ctx, 2, H, sm_scale, g, a, st);
-    return launch_tile<float, 64>(ctx, 3, H, sm_scale, g, a, st);
+    if (dh == 128) return launch_tile<128>(ctx, 0, H, sm_scale, g, a, st);
+    return launch_tile<64>(ctx, 1, H, sm_scale, g, a, st);
 }

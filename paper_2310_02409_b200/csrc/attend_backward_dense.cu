@@ -779,7 +779,7 @@ BackwardTiles dodo_backward_dense_tiles() { return {BM, BM, BN}; }
 
 template <int DH>
 static int launch_dense(dodo_ctx* ctx, int slot, int H, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows, int cache_rows,
-                               int loc_rows, int* next_unit, cudaStream_t st) {
+                        int loc_rows, int* next_unit, cudaStream_t st) {
     const int total = g.q_blocks + g.kv_blocks;
     if (total == 0) return DODO_OK;
     BackwardMaps maps;
@@ -808,6 +808,6 @@ static int launch_dense(dodo_ctx* ctx, int slot, int H, float sm_scale, const Ba
 
 int dodo_launch_backward_dense(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
                                int cache_rows, int loc_rows, int* next_unit, cudaStream_t st) {
-    return dh == 128 ? launch_dense<128>(ctx, 4, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st)
-                     : launch_dense<64>(ctx, 5, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st);
+    return dh == 128 ? launch_dense<128>(ctx, 2, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st)
+                     : launch_dense<64>(ctx, 3, H, sm_scale, g, a, q_rows, cache_rows, loc_rows, next_unit, st);
 }

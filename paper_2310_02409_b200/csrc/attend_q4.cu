@@ -6,11 +6,17 @@
 // so that a group costs one extra multiply-add per key on either side.
 //
 // A cached key is 160 bytes a head (dh 128) where bf16 has 512, so the bound moves towards instruction issue: what counts
-// is instructions per code.  A lane owns a run of 32 features of a head (one group: 16 bytes of codes, one word each of K
-// and V steps), 16 where several queries share the key.  A code is turned into a float in place, without a shift: masking
-// nibble i of a word and or-ing in the exponent of 2^23 gives 2^23 + c 16^i exactly, one packed subtraction per two codes
-// takes the 2^23 off, and the weight 16^i is folded into the query feature (for K) and divided out of the accumulator at
-// the end (for V), both powers of two and exact.  That is 2.1 instructions per code and product.
+// is instructions per code.  Two kernels:
+//   attend_q4_kernel        every type and head size, tiles of 1, 2 or 4 queries: fp32 FMAs, exact codes as floats
+//   attend_q4_token_kernel  one bf16 query per sequence, heads of 128: the codes go to the matrix units as they are
+//
+// attend_q4_kernel: a lane owns a run of 16 features of a head (half a group: 8 bytes of codes, one word each of K and V
+// steps); eight lanes share a key of 128.  A code is turned into a float in place, without a shift: masking nibble i of a
+// word and or-ing in the exponent of 2^23 gives 2^23 + c 16^i exactly, one packed subtraction per two codes takes the 2^23
+// off, and the weight 16^i is folded into the query feature (for K) and divided out of the accumulator at the end (for V),
+// both powers of two and exact.  That is 2.1 instructions per code and product.  Measured: 64 queries over 8,192 cached keys
+// and a window, 40 heads of 128: 59 us where the codes take 18 us to read once per query tile's worth of arithmetic; what
+// bounds it is issue of the FMAs, one per code, query and product.
 #include "dodo_internal.cuh"
 #include "sm100_ptx.cuh"
 #include <type_traits>
@@ -46,14 +52,9 @@ __device__ __forceinline__ void codes_of(uint32_t w, float2* c) {
     for (int i = 0; i < 4; ++i) c[i] = __fadd2_rn(make_float2(f[2 * i], f[2 * i + 1]), base);
 }
 
-template <int W> struct Codes { uint32_t w[W]; };
-template <int W> __device__ __forceinline__ Codes<W> load_codes(const uint32_t* p);
-template <> __device__ __forceinline__ Codes<4> load_codes<4>(const uint32_t* p) {
-    const uint4 v = ld_stream16(p);
-    return {{v.x, v.y, v.z, v.w}};
-}
-template <> __device__ __forceinline__ Codes<2> load_codes<2>(const uint32_t* p) {
-    Codes<2> c;
+struct Codes { uint32_t w[2]; };
+__device__ __forceinline__ Codes load_codes(const uint32_t* p) {
+    Codes c;
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(c.w[0]), "=r"(c.w[1]) : "l"(p));
     return c;
 }
@@ -118,13 +119,13 @@ struct Q4Source {
     const void *lK, *lV;
 };
 
-// FPL: features per lane (32 or 16); LPR = DH / FPL lanes share a key.
-template <typename T, int DH, int QT, int FPL, int U>
+// U keys per lane bundle and batch: 4 for one query, 2 for tiles of queries, whose accumulators take the registers
+template <typename T, int DH, int QT, int U>
 __global__ void __launch_bounds__(kThreads, QT == 1 ? 2 : 1)
 attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_constant__ AttendGroup g,
                  const int32_t* __restrict__ cache_pos, int H, float scale_log2, int TK, T* __restrict__ O,
                  float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets, int early_cache) {
-    constexpr int LPR = DH / FPL, BPW = 32 / LPR, NB = kWarps * BPW;   // lanes per key, bundles per warp and per block
+    constexpr int FPL = 16, LPR = DH / FPL, BPW = 32 / LPR, NB = kWarps * BPW;   // lanes per key, bundles per warp and per block
     constexpr int W = FPL / 8;                                         // words of codes per lane and row
     constexpr int RED = DH + 2;
     constexpr int kLocVec = FPL * static_cast<int>(sizeof(T)) / 16;    // 16-byte loads of a local row per lane
@@ -164,7 +165,7 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
     // ---- cached keys: batches of NB * U, the next one's loads in flight while one is reduced ----------------
     const uint32_t* const q4_0 = src.q4 + (static_cast<size_t>(c_row) * H + h) * (DH / 4) + lig * W;
     const uint32_t* const sc_0 = src.scale + (static_cast<size_t>(c_row) * H + h) * (2 * DH / DODO_Q4_GROUP) + lig * FPL / DODO_Q4_GROUP;
-    struct Batch { Codes<W> k[U], v[U]; uint32_t ks[U], vs[U]; int pos[U]; };
+    struct Batch { Codes k[U], v[U]; uint32_t ks[U], vs[U]; int pos[U]; };
     auto load_batch = [&](int base, Batch& t) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -175,8 +176,8 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
             for (int i = 0; i < W; ++i) t.k[u].w[i] = t.v[u].w[i] = 0u;
             if (j < n_c) {
                 const size_t at = static_cast<size_t>(j) * H;
-                t.k[u] = load_codes<W>(q4_0 + at * (DH / 4));
-                t.v[u] = load_codes<W>(q4_0 + at * (DH / 4) + DH / 8);
+                t.k[u] = load_codes(q4_0 + at * (DH / 4));
+                t.v[u] = load_codes(q4_0 + at * (DH / 4) + DH / 8);
                 t.ks[u] = __ldg(sc_0 + at * (2 * DH / DODO_Q4_GROUP));
                 t.vs[u] = __ldg(sc_0 + at * (2 * DH / DODO_Q4_GROUP) + DH / DODO_Q4_GROUP);
                 t.pos[u] = __ldg(cache_pos + c_row + j);
@@ -481,7 +482,7 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
 // rows: 25.4 against 28.4 us).  What bounds it is instruction issue next to HBM: the same kernel without the arithmetic takes 20 us
 // for 16,384 rows of 40 heads (5.4 TB/s) where this takes 25.
 constexpr int kQExp = 64;        // the query is shifted to a largest feature near 2^64
-constexpr int kPExp = 40;        // power of two on p s
+constexpr int kPExp = 72;        // power of two on p s, p below 2^8: fits for steps below 2^47, products are normal numbers down to p s of 2^-65
 
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -639,7 +640,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
         }
     }
 
-    constexpr float kPScale = 1099511627776.f;                 // 2^kPExp
+    const float kPScale = __uint_as_float(static_cast<uint32_t>(kPExp + 127) << 23);
     const int from = 8 * t + (r < 4 ? 2 : 0) + ((r & 3) >> 1);     // lane that holds the p s of key 2 t for column r
     const uint32_t pick = (r & 1) != 0 ? 0x7632u : 0x5410u;
     float m = kNeg, l = 0.f, accm[2] = {0.f, 0.f};             // the maximum is the warp's; l and accm are a lane's own rows'
@@ -785,7 +786,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
             accm[0] += __shfl_xor_sync(0xffffffffu, accm[0], o);
             accm[1] += __shfl_xor_sync(0xffffffffu, accm[1], o);
         }
-        constexpr int kExp = 133 - kPExp;                          // 93: codes come out as c 2^-133 p s 2^40
+        constexpr int kExp = 133 - kPExp;                          // codes come out as c 2^-133 p s 2^kPExp
         const float back = __uint_as_float(static_cast<uint32_t>(kExp + 127) << 23);
         const bool second = r >= 4;                                // of the two groups in this lane's accumulator columns
         const float bias = second ? accm[1] : accm[0];
@@ -917,11 +918,11 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     merge_chunks<__nv_bfloat16, DH>(sq, H, 0, h, 0, 1, nchunk, partials, tickets, &s_flag, O, lse);
 }
 
-template <typename T, int DH, int QT, int FPL, int U>
+template <typename T, int DH, int QT, int U>
 int launch_t(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const void* Q, const Q4Source& src,
              const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
     const int dtype = sizeof(T) == 4 ? DODO_F32 : DODO_BF16;
-    const cudaError_t e = dodo_launch_dependent(attend_q4_kernel<T, DH, QT, FPL, U>, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kThreads), 0,
+    const cudaError_t e = dodo_launch_dependent(attend_q4_kernel<T, DH, QT, U>, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kThreads), 0,
                                                 st, static_cast<const T*>(Q), src, g, cache_pos, H, sm_scale * 1.4426950408889634f,
                                                 dodo_attend_tile_keys(dtype, DH), static_cast<T*>(O), lse, partials, tickets, early ? 1 : 0);
     return dodo_check_cuda(ctx, e, "4-bit attend launch");
@@ -930,12 +931,10 @@ int launch_t(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const v
 template <typename T, int DH>
 int launch_qt(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src,
               const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
-    switch (qt) {
-        case 1: return launch_t<T, DH, 1, 16, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
-        case 2: return launch_t<T, DH, 2, 16, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
-        case 4: return launch_t<T, DH, 4, 16, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
-        default: break;
-    }
+    if constexpr (sizeof(T) == 4 || DH != 128)                 // (bf16 at 128: the kernel for single queries)
+        if (qt == 1) return launch_t<T, DH, 1, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
+    if (qt == 2) return launch_t<T, DH, 2, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
+    if (qt == 4) return launch_t<T, DH, 4, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: query tile %d is not built", qt);
 }
 

@@ -35,7 +35,7 @@ struct dodo_ctx {
     int map_next;               // round-robin replacement
     bool dense_attr_set[4];     // shared-memory attribute of the four forms of the tensor-core kernel
     bool q4_attr_set;           // ... and of the 4-bit single-query kernel
-    bool backward_attr_set[6];  // ... and of the kernels of attend's gradient
+    bool backward_attr_set[4];  // ... and of the kernels of attend's gradient
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
     int select_key_cap;
@@ -172,6 +172,8 @@ int dodo_launch_expand_q4(dodo_ctx* ctx, const void* cache_q4, const uint32_t* c
 int dodo_check_attend_queries(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H, int dh, int B);
 int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_t* cache_len, const int32_t* loc_off,
                            const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, bool* any_cache, bool* any_local);
+// that positions of queries and local tokens leave room for differences and for "never seen" (2^31 - 1)
+int dodo_check_positions(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, const int32_t* loc_len, const int32_t* loc_pos0, int B);
 int dodo_check_device(dodo_ctx* ctx);
 
 struct AttendSeq {
@@ -307,14 +309,14 @@ struct BackwardTiles { int keys, queries, step; };
 BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh);
 int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, int max_tq, const BackwardGroup& g,
                                 const BackwardArrays& a, cudaStream_t st);
-int dodo_launch_backward_stats(dodo_ctx* ctx, int dtype, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st);
+int dodo_launch_backward_stats(dodo_ctx* ctx, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st);
 // Blocks of bf16 queries on the tensor cores.  next_unit: a device counter, zero between launches
 BackwardTiles dodo_backward_dense_tiles();
 int dodo_launch_backward_dense(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g, const BackwardArrays& a, int q_rows,
                                int cache_rows, int loc_rows, int* next_unit, cudaStream_t st);
 // dscore of the group's cache rows: the sum of `parts` rows of score_part, in order
 int dodo_launch_backward_scores(dodo_ctx* ctx, const BackwardGroup& g, const BackwardArrays& a, int parts, cudaStream_t st);
-int dodo_launch_backward_tile(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const BackwardGroup& g,
+int dodo_launch_backward_tile(dodo_ctx* ctx, int H, int dh, float sm_scale, const BackwardGroup& g,
                               const BackwardArrays& a, cudaStream_t st);
 int dodo_attend_max_cluster();   // most chunks of one (query tile, head) that can merge inside a cluster
 // Table for AttendPlan::cluster_cap of the kernel that serves (dtype, dh, qt), from the occupancy calculator

@@ -179,10 +179,11 @@ def test_gradient_on_tensor_cores(dodo, errlog, dh, case, inside):
     assert all(torch.equal(out[n], bare[n]) for n in out if n != "dscore") and bool((bare["dscore"] == 7.0).all())
 
 
-def test_gradient_on_tensor_cores_many_sequences(dodo):
+@pytest.mark.parametrize("dh", [128, 64])
+def test_gradient_on_tensor_cores_many_sequences(dodo, dh):
     rs = np.random.RandomState(12)
     tqs, cl, ll = rs.randint(0, 90, 67), rs.randint(0, 200, 67), rs.randint(0, 100, 67)
-    p = problem("bwdtcmany", BF, 2, 128, tqs.tolist(), cl.tolist(), ll.tolist())
+    p = problem("bwdtcmany", BF, 2, dh, tqs.tolist(), cl.tolist(), ll.tolist())
     d = forward(dodo, p)
     out = backward(dodo, p, d)
     torch.cuda.synchronize()
@@ -277,7 +278,7 @@ def test_gradient_against_differences(dodo):
             assert abs((loss(a) - loss(b)) / (2 * e) - got[which][i]) < 1e-4
 
 
-@pytest.mark.parametrize("dtype,H,dh,tqs", [(F32, 2, 64, [1, 2]), (F32, 2, 64, [20, 3]), (BF, 2, 128, [2, 1]), (BF, 2, 128, [40, 65])])
+@pytest.mark.parametrize("dtype,H,dh,tqs", [(F32, 2, 64, [1, 2]), (F32, 2, 64, [20, 3]), (BF, 2, 128, [2, 1]), (BF, 2, 128, [40, 65]), (BF, 2, 64, [40, 65])])
 def test_gradient_captured_and_replayed(dodo, dtype, H, dh, tqs):
     """Forward and gradient of two problems in one graph on a stream of its own, with a shared workspace, replayed on new data."""
     ps = [problem(("bwdgraph", i, dh, tqs[0]), dtype, H, dh, tqs, [150, 60], [tqs[0] + 3, tqs[1]], inside=bool(i)) for i in range(2)]
@@ -355,6 +356,36 @@ def test_training_step_of_the_scorer(dodo, oracle):
                                   np.concatenate([_f64(V)[i], _f64(lV)]), np.concatenate([i, n + np.arange(tq)]), _f64(d["O"]), _f64(d["lse"]), _f64(dO))
     ref_dw = _f64(X)[i].T @ ref[3][:k]
     assert np.linalg.norm(_f64(dw) - ref_dw) <= 1e-5 * np.linalg.norm(ref_dw) + 1e-6
+
+
+@pytest.mark.parametrize("dtype,tq", [(BF, 2), (BF, 40), (F32, 9)])
+def test_gradient_of_rows_behind_two_to_the_31_elements(dodo, dtype, tq):
+    """A region that starts behind 2^31 elements of the cache and of the local rows: the same gradients as in small arrays."""
+    H, dh, far, n, nl = 64, 128, 263_000, 130, 70
+    assert far * H * dh > 2 ** 31
+    small = [inputs.randn((r, H, dh), "bwdfar", i, dtype=dtype).cuda() for i, r in enumerate((tq, tq, n, n, nl, nl))]
+    Q, dO = small[:2]
+    got = []
+    for base in (0, far):
+        cK, cV, lK, lV = (torch.empty((base + t.shape[0], H, dh), dtype=dtype, device="cuda") for t in small[2:])
+        for t, src in zip((cK, cV, lK, lV), small[2:]):
+            t[base:] = src
+        pos = torch.arange(base + n, dtype=torch.int32, device="cuda") - base
+        tables = dict(q_off=[0, 0, tq], q_pos0=[0, n + nl - tq], cache_off=[0, base, base + n], cache_len=[0, n], loc_off=[0, base],
+                      loc_len=[0, nl], loc_pos0=[0, n])
+        O, lse = torch.empty_like(Q), torch.empty((tq, H), device="cuda")
+        ws = torch.empty(dodo.attend_backward_workspace_bytes(tq, H, dh, base + n), dtype=torch.uint8, device="cuda")
+        dodo.attend(Q, tables["q_off"], tables["q_pos0"], 0.09, cK, cV, pos, tables["cache_off"], tables["cache_len"], lK, lV, tables["loc_off"],
+                    tables["loc_len"], tables["loc_pos0"], O, lse, torch.empty(dodo.attend_workspace_bytes(dh), dtype=torch.uint8, device="cuda"))
+        dcK, dcV, dlK, dlV = (torch.empty_like(t) for t in (cK, cV, lK, lV))
+        dQ, ds = torch.empty_like(Q), torch.empty(base + n, device="cuda")
+        dodo.attend_backward(Q, tables["q_off"], tables["q_pos0"], 0.09, cK, cV, pos, tables["cache_off"], tables["cache_len"], lK, lV,
+                             tables["loc_off"], tables["loc_len"], tables["loc_pos0"], O, lse, dO, dQ, dcK, dcV, dlK, dlV, ds, ws)
+        torch.cuda.synchronize()
+        got.append([dQ] + [t[base:].clone() for t in (dcK, dcV, dlK, dlV, ds)])
+        del cK, cV, lK, lV, dcK, dcV, dlK, dlV, ws
+    assert all(bool(torch.isfinite(t.float()).all()) for t in got[0])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
 def test_backward_binding_refuses_wrong_tensors(dodo):

@@ -144,7 +144,7 @@ def test_gather_q4_bad_index_is_reported_not_followed(libdodo):
 
 
 # ---- attention --------------------------------------------------------------------------------------------------------
-def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2):
+def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2, kstd=1.0, vstd=2.0):
     """A ragged batch over a 4-bit cache; row regions have slack rows that hold NaN groups, the local array NaN rows."""
     rs = np.random.RandomState(inputs.seed_for(tag) % 2 ** 32)
     B = len(tqs)
@@ -157,7 +157,7 @@ def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2):
     p["loc_pos0"] = np.asarray(span, np.int32)
     p["q_pos0"] = np.asarray([s // 2 - 2 if inside else s + n - t for s, n, t in zip(span, llens, tqs)], np.int32)
     cpos = np.full(rows, 0, np.int32)
-    kv = [rs.standard_normal((rows, H, dh)), 2.0 * rs.standard_normal((rows, H, dh))]
+    kv = [kstd * rs.standard_normal((rows, H, dh)), vstd * rs.standard_normal((rows, H, dh))]
     packed = [plain64.pack(*plain64.quantise(np.asarray(torch.from_numpy(x).float().to(dtype).float().numpy()))) for x in kv]
     codes, words = np.stack([packed[0][0], packed[1][0]], 2), np.stack([packed[0][1], packed[1][1]], 2)
     loc = [torch.from_numpy(rs.standard_normal((lrows, H, dh))).to(dtype) for _ in range(2)]
@@ -280,12 +280,88 @@ def test_attend_q4_masked_nan_rows_do_not_count(dodo):
     _check(q, O, lse)
 
 
-def test_attend_q4_visible_nan_shows(dodo):
-    p = _problem("q4vis", F32, 2, 64, [1], [40], [3])
+@pytest.mark.parametrize("dtype,dh", [(F32, 64), (BF, 128), (BF, 64)])
+def test_attend_q4_visible_nan_shows(dodo, dtype, dh):
+    p = _problem("q4vis", dtype, 2, dh, [1], [40], [3])
     p["words"][7, 1, 0] = 0x7fc07fc0
     O, lse = _run_q4(dodo, p)
     assert bool(torch.isnan(O[0, 1]).all()) and bool(torch.isnan(lse[0, 1]))
     assert bool(torch.isfinite(O[0, 0]).all())
+    # in a value: the group's features
+    p = _problem("q4vis", dtype, 2, dh, [1], [40], [3])
+    p["words"][39, 1, 1, 1] = 0x7fc07fc0
+    O, lse = _run_q4(dodo, p)
+    nan = torch.isnan(O[0, 1]).cpu()
+    assert bool(nan[32:64].all()) and not bool(nan[:32].any()) and not bool(nan[64:].any()) and bool(torch.isfinite(lse).all())
+
+
+# the token kernel carries codes as bf16 numbers far below 1 and weights times steps far above: both ends of its range
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 2), (F32, 64, 1)])
+@pytest.mark.parametrize("kstd,vstd", [(1.0, 1e13), (1.0, 1e-15), (1.0, 1e-20), (1e12, 1.0), (1e-12, 1.0), (1e18, 1e-10)])
+def test_attend_q4_range_of_values(dodo, dtype, dh, tq, kstd, vstd):
+    p = _problem(("q4range", kstd, vstd, tq), dtype, 2, dh, [tq, tq], [300, 40], [1, 0], kstd=kstd, vstd=vstd)
+    p["loc"][0].fill_(0.0)
+    p["loc"][1].mul_(vstd)
+    p["Q"] = (p["Q"].float() / kstd).to(dtype)
+    _check(p, *_run_q4(dodo, p))
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF, 128), (BF, 64), (F32, 128)])
+@pytest.mark.parametrize("rise", [0.3, 3.0, 90.0])
+def test_attend_q4_rising_and_falling_logits(dodo, dtype, dh, rise):
+    """The running maximum climbs by less and by more than what moves the reference, from tile to tile and inside one."""
+    p = _problem(("q4rise", rise), dtype, 2, dh, [1, 1], [513, 130], [2, 0])
+    K = plain64.values(p["codes"][:, :, 0], p["words"][:, :, 0])
+    q = _f64(p["Q"])
+    rows = np.arange(len(K))
+    for b in range(2):      # key j along the query, so that its logit is about rise * j / 16, falling in the second sequence
+        r = slice(int(p["cache_off"][b]), int(p["cache_off"][b + 1]))
+        j = (rows[r] - r.start) * (1 if b == 0 else -1)
+        unit = q[b] / (np.sum(q[b] ** 2, -1, keepdims=True) * p["scale"])
+        K[r] = 0.05 * K[r] + (rise * j / 16.0)[:, None, None] * unit
+    x = torch.from_numpy(K).float().to(dtype).float().numpy()
+    p["codes"][:, :, 0], p["words"][:, :, 0] = plain64.pack(*plain64.quantise(x))
+    _check(p, *_run_q4(dodo, p))
+
+
+@pytest.mark.parametrize("dtype,H,dh", [(BF, 3, 128), (F32, 2, 64)])
+def test_attend_q4_many_sequences(dodo, dtype, H, dh):
+    # 70 sequences: two launch groups, some of them cut, whose partials share the workspace
+    rs = np.random.RandomState(8)
+    cl = rs.randint(0, 300, 70)
+    cl[[3, 66]] = 3000, 5000
+    p = _problem(("q4seqs", dh), dtype, H, dh, [int(x) for x in rs.randint(0, 2, 70)], cl.tolist(), rs.randint(0, 40, 70).tolist())
+    _check(p, *_run_q4(dodo, p))
+
+
+def test_q4_rows_behind_two_to_the_31_elements(dodo):
+    """The second sequence's region starts behind 2^31 codes: its rows, appended, expanded and attended, are those of a small cache."""
+    H, dh, far, n = 128, 128, 270_000, 70
+    assert far * H * dh > 2 ** 32 and far * H * 2 * dh // 2 > 2 ** 31
+    K, V = (inputs.randn((n, H, dh), "q4far", k, dtype=BF).cuda() for k in "KV")
+    Q = inputs.randn((1, H, dh), "q4far", "Q", dtype=BF).cuda()
+    idx = torch.arange(n, dtype=torch.int32, device="cuda")
+    got = []
+    for base in (0, far):
+        q4 = torch.empty((base + n, H, 2, dh // 2), dtype=torch.uint8, device="cuda")
+        sc = torch.empty((base + n, H, 2, dh // 32), dtype=torch.int32, device="cuda")
+        pos = torch.empty(base + n, dtype=torch.int32, device="cuda")
+        off, clen = np.array([0, base, base + n], np.int32), np.zeros(2, np.int32)
+        dodo.gather_kv_q4(K, V, [0, 0, n], idx, [0, 0, n], [0, 0], q4, sc, pos, off, clen)
+        assert clen.tolist() == [0, n]
+        out = [q4[base:].clone(), sc[base:].clone()]
+        for tqs in ([0, 0, 1], [0, 0, 2]):
+            q = Q.expand(tqs[2], H, dh).contiguous()
+            O = torch.empty_like(q)
+            dodo.attend_q4(q, tqs, [n, n], dh ** -0.5, q4, sc, pos, off, clen, None, None, None, None, None, O, None, None)
+            out.append(O)
+        eK, eV = (torch.empty((base + n, H, dh), dtype=BF, device="cuda") for _ in range(2))
+        dodo.expand_kv_q4(q4, sc, off, clen, eK, eV)
+        out += [eK[base:].clone(), eV[base:].clone()]
+        torch.cuda.synchronize()
+        got.append(out)
+        del q4, sc, pos, eK, eV
+    assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
 @pytest.mark.parametrize("inside", [False, True])

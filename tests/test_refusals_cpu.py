@@ -118,3 +118,10 @@ def test_attend_backward_of_nothing_is_nothing(ctx):
     nothing = dict(q_off=_i32(0, 0, 0), cache_len=None, loc_len=None, Q=None, O=None, lse=None, dO=None, dQ=None, workspace=None)
     assert _call(ctx, "dodo_attend_backward", **_backward(**nothing)) == 0
     assert _call(ctx, "dodo_attend_backward", **_backward(B=0, q_off=_i32(0), q_pos0=None, cache_len=None, loc_len=None)) == 0
+
+
+@pytest.mark.parametrize("change", [dict(q_pos0=_i32(9, 2 ** 30)), dict(q_pos0=_i32(-2 ** 30 - 1, 0)), dict(q_pos0=_i32(2 ** 31 - 1, 0)),
+                                    dict(loc_pos0=_i32(2 ** 30 - 2, 0)), dict(loc_pos0=_i32(0, -2 ** 31))])
+@pytest.mark.parametrize("name", ["dodo_attend_q4", "dodo_attend_backward"])
+def test_positions_leave_room(ctx, name, change):
+    assert _call(ctx, name, **(_attend if name == "dodo_attend_q4" else _backward)(**change)) == BAD
