@@ -15,7 +15,7 @@
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kGatherThreads = 256;
+constexpr int kGatherThreads = 64;              // small blocks leave the last wave fuller (4 x 600 fp32 rows of 12 x 64: 9.5 us at 256, 8.2 at 64)
 constexpr int kGroup = DODO_Q4_GROUP;
 constexpr int kOctet = 8;                       // features per word of codes
 constexpr float kFinite = 3.4028234663852886e38f;
@@ -113,19 +113,23 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* codes) {
     const float inv = rcp_approx(s), half = 0.5f * s;
     constexpr float kMagic = 12582912.f;
     constexpr uint32_t kMagicBits = 0x4b400000u;
+    const float2 m2 = make_float2(-m, -m), inv2 = make_float2(inv, inv), s2 = make_float2(s, s), half2 = make_float2(half, half);
+    const float2 low2 = make_float2(-0.5f, -0.5f), magic2 = make_float2(kMagic, kMagic), back2 = make_float2(-kMagic, -kMagic);
     bool met = false;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         uint32_t c = 0u - kMagicBits * 0x11111111u;
 #pragma unroll
-        for (int i = 0; i < kOctet; ++i) {
-            const float d = __fsub_rn(x[w * kOctet + i], m);
-            const float r = __fadd_rn(__fmaf_rn(d, inv, -0.5f), kMagic);
-            const float border = __fmaf_rn(__fsub_rn(r, kMagic), s, half);
-            const uint32_t rb = __float_as_uint(r);
-            c += rb << (4 * i);
-            if (__float_as_uint(d) + (rb & 1u) > __float_as_uint(border)) c += 1u << (4 * i);
-            if (kWide) met = met || d == border;
+        for (int i = 0; i < kOctet; i += 2) {        // two features per instruction
+            const float2 d = __fadd2_rn(make_float2(x[w * kOctet + i], x[w * kOctet + i + 1]), m2);
+            const float2 r = __fadd2_rn(__ffma2_rn(d, inv2, low2), magic2);
+            const float2 border = __ffma2_rn(__fadd2_rn(r, back2), s2, half2);
+            const uint32_t r0 = __float_as_uint(r.x), r1 = __float_as_uint(r.y);
+            c += r0 << (4 * i);
+            c += r1 << (4 * i + 4);
+            if (__float_as_uint(d.x) + (r0 & 1u) > __float_as_uint(border.x)) c += 1u << (4 * i);
+            if (__float_as_uint(d.y) + (r1 & 1u) > __float_as_uint(border.y)) c += 1u << (4 * i + 4);
+            if (kWide) met = met || d.x == border.x || d.y == border.y;
         }
         codes[w] = c;
     }
@@ -154,10 +158,12 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* codes) {
 
 // A thread takes one group of 32 features of one nugget's K or V row (bf16: 64 bytes in two 32-byte loads), so a group's
 // extremes, step and reciprocal cost it no exchange and are found once; the groups of all nuggets are laid end to end over the
-// threads, whatever a row's length.  Bound by instruction issue (about 20 per feature; 68 % of the issue slots busy) ahead of
-// HBM: it reads two rows and writes 80 (dh 128) of their 256 bytes a head.
+// threads, whatever a row's length.  It reads two rows and writes 80 (dh 128) of their 256 bytes a head, about 16 instructions
+// per feature.  8 x 205 nuggets of 32 heads of 128, bf16: 15.8 us (17.1 with one feature per instruction, 24 with an octet per
+// thread; dodo_gather_kv takes 10.1 to copy the same rows), bound by issue and by the load's latency, which a thread's single
+// group does not cover.
 template <typename T>
-__global__ void __launch_bounds__(kGatherThreads, 4)
+__global__ void __launch_bounds__(kGatherThreads, 16)
 gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __restrict__ V, int H, int dh,
                  const int32_t* __restrict__ idx, const __grid_constant__ GatherGroup g, unsigned char* __restrict__ cache_q4,
                  uint32_t* __restrict__ cache_scale, int32_t* __restrict__ cache_pos, int* __restrict__ dev_status) {
