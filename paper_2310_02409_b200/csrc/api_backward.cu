@@ -73,7 +73,7 @@ int plan_group(dodo_ctx* ctx, const AttendShape& s, int variant, int b0, int nb,
         const int steps = ceil_div(q.c_len, t.step) + ceil_div(q.l_len, t.step);
         const int qtiles = variant == DODO_BWD_STREAM ? 1 : ceil_div(q.tq, t.queries);
         int64_t n = work > 0 ? target * steps / work : 1;
-        const int most = ceil_div(steps, 4);            // chunks of four steps at least
+        const int most = ceil_div(steps, variant == DODO_BWD_TILE ? 2 : 4);    // chunks of two (fp32 tiles) or four steps at least
         if (n > most) n = most;
         if (n < 1) n = 1;
         q.ctiles = steps > 0 ? ceil_div(steps, static_cast<int>(n)) : 1;

@@ -342,69 +342,80 @@ __device__ __forceinline__ void tile_stats(float2* dst, const BackwardArrays& a,
     if (part == 0) dst[q] = q < nq ? make_float2(minus_lse2(__ldg(a.lse + row)), -d) : make_float2(-INFINITY, 0.f);
 }
 
-// N rows of a head's matrix to shared memory, those from `rows` on as zeros; all of a thread's loads are issued before its stores
-template <int N, int DH>
-__device__ __forceinline__ void load_rows(float (*dst)[DH + 4], const float* src, size_t row_elems, int row0, int rows) {
-    constexpr int V4 = DH / 4, kIter = N * V4 / kThreads;
+// N rows of a head's matrix on their way to shared memory, those from `rows` on as zeros
+template <int N, int DH> struct RowPieces {
+    static constexpr int V4 = DH / 4, kIter = N * V4 / kThreads;
     static_assert(N * V4 % kThreads == 0, "whole passes");
     float4 v[kIter];
+    __device__ __forceinline__ void fetch(const float* src, size_t row_elems, int row0, int rows) {
 #pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-        const int at = threadIdx.x + i * kThreads, r = at / V4, c = at % V4;
-        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < rows) v[i] = load4(src + static_cast<size_t>(row0 + r) * row_elems + 4 * c);
+        for (int i = 0; i < kIter; ++i) {
+            const int at = threadIdx.x + i * kThreads, r = at / V4, c = at % V4;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < rows) v[i] = load4(src + static_cast<size_t>(row0 + r) * row_elems + 4 * c);
+        }
     }
+    __device__ __forceinline__ void put(float (*dst)[DH + 4]) const {
 #pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-        const int at = threadIdx.x + i * kThreads;
-        *reinterpret_cast<float4*>(&dst[at / V4][4 * (at % V4)]) = v[i];
+        for (int i = 0; i < kIter; ++i) {
+            const int at = threadIdx.x + i * kThreads;
+            *reinterpret_cast<float4*>(&dst[at / V4][4 * (at % V4)]) = v[i];
+        }
     }
-}
-// dot products of a 4-key x 2-query register tile, over all features, of (K, Q) and (V, dO)
-template <int DH>
+};
+// weights of J x 16 queries: dot products of a 4-key x J-query register tile, over all features, of (K, Q) and (V, dO)
+template <int DH, int J>
 __device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0, float scale2) {
-    const int tk = threadIdx.x % 16, tq = threadIdx.x / 16;     // keys tk + 16 i, queries tq + 16 i
-    float s[4][2], t[4][2];
+    const int tk = threadIdx.x % 16, tq = threadIdx.x / 16;     // keys tk + 16 i, queries tq + 16 j
+    float2 s[4][J], t[4][J];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) s[i][j] = t[i][j] = 0.f;
+        for (int j = 0; j < J; ++j) s[i][j] = t[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
     for (int c = 0; c < DH; c += 4) {
-        float4 k[4], v[4], q[2], o[2];
+        float4 k[4], v[4], q[J], o[J];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             k[i] = *reinterpret_cast<const float4*>(&sm.K[tk + 16 * i][c]);
             v[i] = *reinterpret_cast<const float4*>(&sm.V[tk + 16 * i][c]);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
             q[j] = *reinterpret_cast<const float4*>(&sm.Q[tq + 16 * j][c]);
             o[j] = *reinterpret_cast<const float4*>(&sm.G[tq + 16 * j][c]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                s[i][j] = fmaf(k[i].x, q[j].x, fmaf(k[i].y, q[j].y, fmaf(k[i].z, q[j].z, fmaf(k[i].w, q[j].w, s[i][j]))));
-                t[i][j] = fmaf(v[i].x, o[j].x, fmaf(v[i].y, o[j].y, fmaf(v[i].z, o[j].z, fmaf(v[i].w, o[j].w, t[i][j]))));
+            for (int j = 0; j < J; ++j) {
+                s[i][j] = __ffma2_rn(make_float2(k[i].x, k[i].y), make_float2(q[j].x, q[j].y), s[i][j]);
+                t[i][j] = __ffma2_rn(make_float2(v[i].x, v[i].y), make_float2(o[j].x, o[j].y), t[i][j]);
+                s[i][j] = __ffma2_rn(make_float2(k[i].z, k[i].w), make_float2(q[j].z, q[j].w), s[i][j]);
+                t[i][j] = __ffma2_rn(make_float2(v[i].z, v[i].w), make_float2(o[j].z, o[j].w), t[i][j]);
             }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
             const int key = tk + 16 * i, q = tq + 16 * j;
             const bool see = q < nq && sm.kpos[key] <= qpos0 + q;
             const float2 st = sm.stat[q];
-            const float p = see ? ex2_approx(fmaf(s[i][j], scale2, st.x)) : 0.f;
+            const float p = see ? ex2_approx(fmaf(s[i][j].x + s[i][j].y, scale2, st.x)) : 0.f;
             sm.P[q][key] = p;
-            sm.S[q][key] = see ? p * (t[i][j] + st.y) : 0.f;
+            sm.S[q][key] = see ? p * (t[i][j].x + t[i][j].y + st.y) : 0.f;
         }
+}
+// (up to 16 queries: the other half of the tile is not computed; a warp whose queries are all behind the last has nothing to do)
+template <int DH>
+__device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0, float scale2) {
+    if (nq > 16) tile_weights<DH, 2>(sm, nq, qpos0, scale2);
+    else if (static_cast<int>(threadIdx.x / 32) * 2 < nq) tile_weights<DH, 1>(sm, nq, qpos0, scale2);
 }
 
 template <int DH>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
 backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
     extern __shared__ __align__(16) unsigned char raw[];
     TileSmem<DH>& sm = *reinterpret_cast<TileSmem<DH>*>(raw);
@@ -431,29 +442,43 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
         const float* gk = static_cast<const float*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH;
         const float* gv = static_cast<const float*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH;
-        load_rows<TK, DH>(sm.K, gk, row_elems, row0, rows);
-        load_rows<TK, DH>(sm.V, gv, row_elems, row0, rows);
+        {
+            RowPieces<TK, DH> k, v;
+            k.fetch(gk, row_elems, row0, rows);
+            v.fetch(gv, row_elems, row0, rows);
+            k.put(sm.K);
+            v.put(sm.V);
+        }
         if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
-        float dk[4][4 * ND], dv[4][4 * ND], score[4];
+        float2 dk[4][2 * ND], dv[4][2 * ND];
+        float score[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             score[i] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4 * ND; ++e) dk[i][e] = dv[i][e] = 0.f;
+            for (int e = 0; e < 2 * ND; ++e) dk[i][e] = dv[i][e] = make_float2(0.f, 0.f);
         }
+        RowPieces<TQ, DH> next_q, next_g;
+        auto fetch_queries = [&](int q0) {
+            const int n = min(TQ, sq.tq - q0);
+            next_q.fetch(static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, n);
+            next_g.fetch(static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, n);
+        };
         // queries from the first one that can see a key of a local tile
         const int q_start = cached ? 0 : max(0, sq.l_pos0 + first - sq.q_pos0) / TQ * TQ;
+        if (q_start < sq.tq) fetch_queries(q_start);
         for (int q0 = q_start; q0 < sq.tq; q0 += TQ) {
             const int nq = min(TQ, sq.tq - q0);
             if (q0 > q_start) __syncthreads();      // (the first queries come with the keys)
-            load_rows<TQ, DH>(sm.Q, static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-            load_rows<TQ, DH>(sm.G, static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+            next_q.put(sm.Q);
+            next_g.put(sm.G);
             tile_stats<DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
             __syncthreads();
+            if (q0 + TQ < sq.tq) fetch_queries(q0 + TQ);
             tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
             __syncthreads();
 #pragma unroll 2
-            for (int q = 0; q < TQ; ++q) {
+            for (int q = 0; q < nq; ++q) {
                 const float4 p = *reinterpret_cast<const float4*>(&sm.P[q][4 * ty]), s = *reinterpret_cast<const float4*>(&sm.S[q][4 * ty]);
                 const float pa[4] = {p.x, p.y, p.z, p.w}, sa[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
@@ -462,14 +487,14 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
                 for (int d = 0; d < ND; ++d) {
                     const float4 o = *reinterpret_cast<const float4*>(&sm.G[q][64 * d + 4 * tx]);
                     const float4 x = *reinterpret_cast<const float4*>(&sm.Q[q][64 * d + 4 * tx]);
-                    const float oa[4] = {o.x, o.y, o.z, o.w}, xa[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            dv[i][4 * d + e] = fmaf(pa[i], oa[e], dv[i][4 * d + e]);
-                            dk[i][4 * d + e] = fmaf(sa[i], xa[e], dk[i][4 * d + e]);
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 p2 = make_float2(pa[i], pa[i]), s2 = make_float2(sa[i], sa[i]);
+                        dv[i][2 * d] = __ffma2_rn(p2, make_float2(o.x, o.y), dv[i][2 * d]);
+                        dv[i][2 * d + 1] = __ffma2_rn(p2, make_float2(o.z, o.w), dv[i][2 * d + 1]);
+                        dk[i][2 * d] = __ffma2_rn(s2, make_float2(x.x, x.y), dk[i][2 * d]);
+                        dk[i][2 * d + 1] = __ffma2_rn(s2, make_float2(x.z, x.w), dk[i][2 * d + 1]);
+                    }
                 }
             }
         }
@@ -482,8 +507,8 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
             const size_t at = static_cast<size_t>(row0 + key) * row_elems;
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-                store4(ok + at + 64 * d + 4 * tx, make_float4(dk[i][4 * d] * scale, dk[i][4 * d + 1] * scale, dk[i][4 * d + 2] * scale, dk[i][4 * d + 3] * scale));
-                store4(ov + at + 64 * d + 4 * tx, make_float4(dv[i][4 * d], dv[i][4 * d + 1], dv[i][4 * d + 2], dv[i][4 * d + 3]));
+                store4(ok + at + 64 * d + 4 * tx, make_float4(dk[i][2 * d].x * scale, dk[i][2 * d].y * scale, dk[i][2 * d + 1].x * scale, dk[i][2 * d + 1].y * scale));
+                store4(ov + at + 64 * d + 4 * tx, make_float4(dv[i][2 * d].x, dv[i][2 * d].y, dv[i][2 * d + 1].x, dv[i][2 * d + 1].y));
             }
             if (cached && a.dscore != nullptr && tx == 0) a.score_part[static_cast<size_t>(h) * a.score_rows + row0 + key] = score[i];
         }
@@ -499,39 +524,65 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q0 + nq - sq.l_pos0));
     const int nt_c = (sq.c_len + TK - 1) / TK, nt = nt_c + (l_vis + TK - 1) / TK;
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
-    load_rows<TQ, DH>(sm.Q, static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
-    load_rows<TQ, DH>(sm.G, static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+    {
+        RowPieces<TQ, DH> q, g2;
+        q.fetch(static_cast<const float*>(a.Q) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+        g2.fetch(static_cast<const float*>(a.dO) + static_cast<size_t>(h) * DH, row_elems, sq.q_row0 + q0, nq);
+        q.put(sm.Q);
+        g2.put(sm.G);
+    }
     tile_stats<DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
-    float dq[2][4 * ND];
+    float2 dq[2][2 * ND];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4 * ND; ++e) dq[i][e] = 0.f;
-    for (int t = t0; t < t1; ++t) {
+        for (int e = 0; e < 2 * ND; ++e) dq[i][e] = make_float2(0.f, 0.f);
+    // the next keys are on their way while these are worked on
+    RowPieces<TK, DH> next_k, next_v;
+    int next_pos = 0;
+    auto fetch_keys = [&](int t) {
         const bool cached = t < nt_c;
         const int first = (cached ? t : t - nt_c) * TK;
         const int rows = min(TK, (cached ? sq.c_len : l_vis) - first);
         const int row0 = (cached ? sq.c_row0 : sq.l_row0) + first;
+        next_k.fetch(static_cast<const float*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
+        next_v.fetch(static_cast<const float*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
+        if (tid < TK) next_pos = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
+    };
+    if (t0 < t1) fetch_keys(t0);
+    for (int t = t0; t < t1; ++t) {
         if (t > t0) __syncthreads();
-        load_rows<TK, DH>(sm.K, static_cast<const float*>(cached ? a.cK : a.lK) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
-        load_rows<TK, DH>(sm.V, static_cast<const float*>(cached ? a.cV : a.lV) + static_cast<size_t>(h) * DH, row_elems, row0, rows);
-        if (tid < TK) sm.kpos[tid] = tid >= rows ? 0x7fffffff : cached ? __ldg(a.cache_pos + row0 + tid) : sq.l_pos0 + first + tid;
+        next_k.put(sm.K);
+        next_v.put(sm.V);
+        if (tid < TK) sm.kpos[tid] = next_pos;
         __syncthreads();
+        if (t + 1 < t1) fetch_keys(t + 1);
         tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
         __syncthreads();
+        auto add = [&](float2* acc, float w, float4 x, int d) {
+            // a key that some queries of the tile do not see may hold anything: its dS is exactly 0 there
+            if (w != 0.f) {
+                acc[2 * d] = __ffma2_rn(make_float2(w, w), make_float2(x.x, x.y), acc[2 * d]);
+                acc[2 * d + 1] = __ffma2_rn(make_float2(w, w), make_float2(x.z, x.w), acc[2 * d + 1]);
+            }
+        };
+        if (nq > 16) {
 #pragma unroll 4
-        for (int k = 0; k < TK; ++k) {
-            const float s0 = sm.S[ty][k], s1 = sm.S[ty + 16][k];
+            for (int k = 0; k < TK; ++k) {
+                const float s0 = sm.S[ty][k], s1 = sm.S[ty + 16][k];
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const float4 x = *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]);
-                const float xa[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    // a key that some queries of the tile do not see may hold anything: its dS is exactly 0 there
-                    dq[0][4 * d + e] = s0 != 0.f ? fmaf(s0, xa[e], dq[0][4 * d + e]) : dq[0][4 * d + e];
-                    dq[1][4 * d + e] = s1 != 0.f ? fmaf(s1, xa[e], dq[1][4 * d + e]) : dq[1][4 * d + e];
+                for (int d = 0; d < ND; ++d) {
+                    const float4 x = *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]);
+                    add(dq[0], s0, x, d);
+                    add(dq[1], s1, x, d);
                 }
+            }
+        } else if (ty < nq) {
+#pragma unroll 4
+            for (int k = 0; k < TK; ++k) {
+                const float s0 = sm.S[ty][k];
+#pragma unroll
+                for (int d = 0; d < ND; ++d) add(dq[0], s0, *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]), d);
             }
         }
     }
@@ -543,7 +594,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         if (q >= nq) continue;
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-            const float4 v = make_float4(dq[i][4 * d], dq[i][4 * d + 1], dq[i][4 * d + 2], dq[i][4 * d + 3]);
+            const float4 v = make_float4(dq[i][2 * d].x, dq[i][2 * d].y, dq[i][2 * d + 1].x, dq[i][2 * d + 1].y);
             if (sq.nchunk == 1) store4(out + q * row_elems + 64 * d + 4 * tx, make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale));
             else store4(a.dq_part + ((part + chunk) * TQ + q) * DH + 64 * d + 4 * tx, v);
         }
