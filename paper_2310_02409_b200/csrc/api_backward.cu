@@ -5,7 +5,6 @@
 
 namespace {
 
-constexpr int kStreamQueries = 4;      // longest query block of the streaming kernel
 constexpr int kStatAlign = 64;         // a sequence's statistics start at a multiple of this
 constexpr int kPartFloats = 128 * 128; // largest partial tile of dQ
 
@@ -150,7 +149,7 @@ int dodo_attend_backward(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
 
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
-    const int variant = max_tq <= kStreamQueries ? DODO_BWD_STREAM : dtype == DODO_BF16 ? DODO_BWD_DENSE : DODO_BWD_TILE;
+    const int variant = max_tq <= dodo_backward_stream_queries(dtype, dh) ? DODO_BWD_STREAM : dtype == DODO_BF16 ? DODO_BWD_DENSE : DODO_BWD_TILE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     BackwardArrays a;
     a.Q = Q; a.O = O; a.dO = dO; a.cK = cacheK; a.cV = cacheV; a.lK = locK; a.lV = locV;

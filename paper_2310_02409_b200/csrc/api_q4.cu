@@ -109,14 +109,11 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 
     // A block of many bf16 queries is a contraction: expand the rows in use once and attend them on the tensor cores,
-    // if the caller's workspace has room for them.  From a quarter of dodo_attend's number of queries on (8 by default): codes
-    // cost more per query than rows do.  Streaming against expanding, us, 8 queries: 35 / 21 (8 x 205 cached rows of 32 heads,
-    // 64 local), 226 / 189 (16,384 rows of 40 heads, 512 local), 118 / 48 (4 x 717 rows of 32 heads, 1280 local); 4 queries:
-    // 18 / 21, 116 / 190, 78 / 48.
+    // if the caller's workspace has room for them.
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
     const int cache_rows = any_cache ? cache_off[B] : 0;
-    if (dtype == DODO_BF16 && dh == 128 && sm_scale > 0.f && max_tq >= (ctx->dense_min_tq + 3) / 4 && workspace != nullptr &&
+    if (dtype == DODO_BF16 && dh == 128 && sm_scale > 0.f && max_tq >= ctx->dense_min_tq && workspace != nullptr &&
         dodo_aligned16(workspace) && workspace_bytes >= dodo_attend_q4_workspace_bytes(ctx, H, dh, cache_rows)) {
         const size_t head = round16(dodo_attend_workspace_bytes(ctx, dh));
         unsigned char* K = static_cast<unsigned char*>(workspace) + head;
@@ -126,18 +123,14 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
             if (rc != DODO_OK) return rc;
             ctx->cache_clean = false;
         }
-        const int min_tq = ctx->dense_min_tq;      // (shorter blocks than dodo_attend's own rule asks for, too)
-        ctx->dense_min_tq = 1;
-        rc = dodo_attend(ctx, Q, q_off, q_pos0, dtype, H, dh, sm_scale, K, V, cache_pos, cache_off, cache_len, locK, locV, loc_off, loc_len,
-                         loc_pos0, loc_rows, B, O, lse, workspace, head, stream);
-        ctx->dense_min_tq = min_tq;
-        return rc;
+        return dodo_attend(ctx, Q, q_off, q_pos0, dtype, H, dh, sm_scale, K, V, cache_pos, cache_off, cache_len, locK, locV, loc_off,
+                           loc_len, loc_pos0, loc_rows, B, O, lse, workspace, head, stream);
     }
 
     AttendShape shp = {q_off, q_pos0, cache_off, cache_len, loc_off, loc_len, loc_pos0, B, H, dh, dtype};
     AttendPlan plan;
     AttendTotals tot;
-    dodo_attend_plan_begin(shp, ctx->attend_target_ctas, plan, tot);
+    dodo_attend_plan_begin(shp, ctx->attend_target_ctas, plan, tot, dodo_attend_q4_tile_queries(dtype, dh, max_tq));
     // A sequence whose key list is longer than a block's share of the work is cut even when there are units enough for the
     // device (one long sequence of a ragged batch would outlast all others), but never into chunks of less than four tiles,
     // whose merge costs more than it saves (8 x 269 keys of 32 heads in two chunks each: 11.8 against 6.6 us).  The share is

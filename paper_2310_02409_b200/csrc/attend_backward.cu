@@ -8,7 +8,7 @@
 // bit for bit.
 //
 // Two kernels here, a third (blocks of bf16 queries) on the tensor cores in attend_backward_dense.cu:
-//   backward_stream_kernel  up to four queries per sequence (single-token steps).  All traffic, no reuse: one pass reads
+//   backward_stream_kernel  up to four queries per sequence (single-token steps), eight for fp32 rows of 128.  All traffic, no reuse: one pass reads
 //       K and V once, writes dK and dV once and sums dQ, the queries and their dQ in registers.
 //   backward_tile_kernel    fp32 blocks: key blocks and query blocks side by side in one launch,
 //       64 keys x 32 queries at a time in shared memory, fp32 FMAs on register tiles.
@@ -67,7 +67,7 @@ __device__ __forceinline__ void finish_scores(const BackwardArrays& a, int H, in
     }
 }
 
-// =============================================== up to four queries =====================================================
+// =============================================== few queries ============================================================
 template <typename T, int DH, int QT, int U>
 __global__ void __launch_bounds__(kThreads)
 backward_stream_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
@@ -614,7 +614,11 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
 template <typename T, int DH>
 int launch_stream(dodo_ctx* ctx, int H, float scale, int max_tq, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st) {
     const dim3 grid(static_cast<unsigned>(g.kv_blocks)), block(kThreads);
-    const cudaError_t e = max_tq <= 1 ? dodo_launch_dependent(backward_stream_kernel<T, DH, 1, 4>, grid, block, 0, st, a, g, H, scale)
+    cudaError_t e;
+    if constexpr (sizeof(T) == 4 && DH == 128)
+        if (max_tq > 4)
+            return dodo_check_cuda(ctx, dodo_launch_dependent(backward_stream_kernel<T, DH, 8, 2>, grid, block, 0, st, a, g, H, scale), "attend gradient launch");
+    e = max_tq <= 1 ? dodo_launch_dependent(backward_stream_kernel<T, DH, 1, 4>, grid, block, 0, st, a, g, H, scale)
                         : max_tq <= 2 ? dodo_launch_dependent(backward_stream_kernel<T, DH, 2, 2>, grid, block, 0, st, a, g, H, scale)
                                       : dodo_launch_dependent(backward_stream_kernel<T, DH, 4, 2>, grid, block, 0, st, a, g, H, scale);
     return dodo_check_cuda(ctx, e, "attend gradient launch");
@@ -635,9 +639,15 @@ int launch_tile(dodo_ctx* ctx, int slot, int H, float scale, const BackwardGroup
 
 }  // namespace
 
+// The streaming kernel beats the others up to four queries everywhere (4 queries over 8 x 269 keys of 32 heads of 128: bf16 33.5
+// against 58 us on the tensor cores, fp32 36 against 128; 4160 keys: 53 / 128, 62 / 209; head size 64: bf16 22 / 52, fp32 with 8
+// heads 12 / 18).  With eight it still does for fp32 rows of 128 (66 to 72 against 129 to 141 us; 106 to 112 against 210 to 228); at 64
+// the tiles are as fast (20 to 23 against 18 to 20), and bf16 has twice the features a lane, whose sums eight queries do not fit.
+int dodo_backward_stream_queries(int dtype, int dh) { return dtype == DODO_F32 && dh == 128 ? 8 : 4; }
+
 BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh) {
     const int bundles = kThreads / (dh * static_cast<int>(dodo_elem_bytes(dtype)) / 16);
-    if (variant == DODO_BWD_STREAM) return {bundles, 4, bundles};
+    if (variant == DODO_BWD_STREAM) return {bundles, dodo_backward_stream_queries(dtype, dh), bundles};
     if (variant == DODO_BWD_DENSE) return dodo_backward_dense_tiles();
     return {TK, TQ, TK};
 }

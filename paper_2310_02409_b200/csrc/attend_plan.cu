@@ -89,7 +89,7 @@ int dodo_dense_encode_maps(dodo_ctx* ctx, const AttendShape& s, const void* Q, i
     return DODO_OK;
 }
 
-void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& plan, AttendTotals& tot) {
+void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& plan, AttendTotals& tot, int qt) {
     const int TK = dodo_attend_tile_keys(s.dtype, s.dh);
     int max_tq = 0;
     for (int b = 0; b < s.B; ++b) {
@@ -99,6 +99,7 @@ void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& p
     plan.qt = max_tq <= 1 ? 1 : max_tq <= 2 ? 2 : max_tq <= 4 ? 4 : 8;
     const int max_qt = dodo_attend_max_qt(s.dtype, s.dh);
     if (plan.qt > max_qt) plan.qt = max_qt;
+    if (qt > 0) plan.qt = qt;
     plan.cluster_cap = nullptr;
     tot.units = tot.work = tot.part_rows = tot.tick_rows = 0;
     for (int b = 0; b < s.B; ++b) {

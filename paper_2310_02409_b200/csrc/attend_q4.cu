@@ -6,17 +6,17 @@
 // so that a group costs one extra multiply-add per key on either side.
 //
 // A cached key is 160 bytes a head (dh 128) where bf16 has 512, so the bound moves towards instruction issue: what counts
-// is instructions per code.  Two kernels:
-//   attend_q4_kernel        every type and head size, tiles of 1, 2 or 4 queries: fp32 FMAs, exact codes as floats
-//   attend_q4_token_kernel  one bf16 query per sequence, heads of 128: the codes go to the matrix units as they are
+// is instructions per code.  Three kernels:
+//   attend_q4_kernel        fp32, and bf16 at head size 64; tiles of 1, 2 or 4 queries: fp32 FMAs, exact codes as floats
+//   attend_q4_token_kernel  bf16 at head size 128, one query per sequence: the codes go to the matrix units as they are
+//   attend_q4_few_kernel    bf16 at head size 128, tiles of eight queries: likewise
 //
 // attend_q4_kernel: a lane owns a run of 16 features of a head (half a group: 8 bytes of codes, one word each of K and V
 // steps); eight lanes share a key of 128.  A code is turned into a float in place, without a shift: masking nibble i of a
 // word and or-ing in the exponent of 2^23 gives 2^23 + c 16^i exactly, one packed subtraction per two codes takes the 2^23
 // off, and the weight 16^i is folded into the query feature (for K) and divided out of the accumulator at the end (for V),
-// both powers of two and exact.  That is 2.1 instructions per code and product.  Measured: 64 queries over 8,192 cached keys
-// and a window, 40 heads of 128: 59 us where the codes take 18 us to read once per query tile's worth of arithmetic; what
-// bounds it is issue of the FMAs, one per code, query and product.
+// both powers of two and exact.  That is 2.1 instructions per code and product, and instruction issue bounds it: one bf16 query
+// over 8 x 205 cached and 64 local keys of 32 heads of 64 takes 5.2 us (four queries 12.0), fp32 of 128 8.3 (19.5).
 #include "dodo_internal.cuh"
 #include "sm100_ptx.cuh"
 #include <type_traits>
@@ -81,7 +81,7 @@ __device__ __forceinline__ void merge_chunks(const AttendSeq& sq, int H, int qti
     __syncthreads();
     if (*flag == 0) return;
     __threadfence();
-    for (int i = threadIdx.x; i < nq * DH; i += kThreads) {
+    for (int i = threadIdx.x; i < nq * DH; i += blockDim.x) {
         const int q2 = i / DH, dim = i % DH;
         const float* pr = partials + (static_cast<size_t>(sq.part0) + (static_cast<size_t>(q_first + q2) * H + h) * nchunk) * RED;
         float M = kNeg, L = 0.f, o = 0.f;
@@ -493,12 +493,52 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+__device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
+__device__ __forceinline__ uint2 lds64(uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+
 struct TokenMaps { CUtensorMap q4, scale; };   // boxes of 128 and 32 bytes x kRound rows
 constexpr int kTokenWarps = 4;                // consumers; one more warp brings the rows
 constexpr int kConsumers = 32 * kTokenWarps, kTokenThreads = kConsumers + 32;
 constexpr int kRound = 16 * kTokenWarps;       // keys of a stage: 16 per warp
 constexpr int kTokenStages = 4, kTokenBlocks = 3;
 constexpr int kCodeBytes = kRound * 128, kStageBytes = (kCodeBytes + kRound * 32 + 1023) / 1024 * 1024;
+
+// The producer's part, one thread: `rounds` stages of rows from c_row on through the ring.  Ahead of the dependency wait (see
+// attend.cu) it copies only when nothing in flight writes a cache.  False when a wait ran out.
+__device__ __forceinline__ bool bring_rows(const TokenMaps& maps, uint32_t ring, uint64_t* bar_full, uint64_t* bar_free, int h, int c_row, int rounds,
+                                           int early_cache) {
+    using namespace sm100;
+    bool ok = true;
+    auto load_round = [&](int i) {
+        const int st = i % kTokenStages;
+        const uint32_t dst = ring + st * kStageBytes;
+        mbar_expect_tx(&bar_full[st], kCodeBytes + kRound * 32);
+        tma_load_2d(dst, &maps.q4, h * 128, c_row + i * kRound, &bar_full[st]);
+        tma_load_2d(dst + kCodeBytes, &maps.scale, h * 32, c_row + i * kRound, &bar_full[st]);
+    };
+    const int ahead = min(rounds, kTokenStages);
+    if (early_cache)
+        for (int i = 0; i < ahead; ++i) load_round(i);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!early_cache)
+        for (int i = 0; i < ahead; ++i) load_round(i);
+    int done = ahead;
+    for (int i = kTokenStages; i < rounds; ++i) {
+        const int st = i % kTokenStages;
+        if (!mbar_wait(&bar_free[st], static_cast<uint32_t>(i / kTokenStages - 1) & 1u)) { ok = false; break; }
+        load_round(i);
+        done = i + 1;
+    }
+    // leave no copy in flight behind (when consumers have given up)
+    for (int i = max(0, done - kTokenStages); i < done; ++i) ok = mbar_wait(&bar_full[i % kTokenStages], static_cast<uint32_t>(i / kTokenStages) & 1u) && ok;
+    return ok;
+}
 
 __global__ void __launch_bounds__(kTokenThreads, kTokenBlocks)
 attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant__ TokenMaps maps, const Q4Source src,
@@ -545,33 +585,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     __syncthreads();
     bool ok = true;
     if (warp == kTokenWarps) {
-        // ---- producer.  Ahead of the dependency wait (see attend.cu) it copies only when nothing in flight writes a cache -----------
-        if (lane == 0) {
-            auto load_round = [&](int i) {
-                const int st = i % kTokenStages;
-                const uint32_t dst = ring + st * kStageBytes;
-                mbar_expect_tx(&bar_full[st], kCodeBytes + kRound * 32);
-                tma_load_2d(dst, &maps.q4, h * 128, c_row + i * kRound, &bar_full[st]);
-                tma_load_2d(dst + kCodeBytes, &maps.scale, h * 32, c_row + i * kRound, &bar_full[st]);
-            };
-            const int ahead = min(rounds, kTokenStages);
-            if (early_cache)
-                for (int i = 0; i < ahead; ++i) load_round(i);
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            if (!early_cache)
-                for (int i = 0; i < ahead; ++i) load_round(i);
-            int done = ahead;
-            for (int i = kTokenStages; i < rounds; ++i) {
-                const int st = i % kTokenStages;
-                if (!mbar_wait(&bar_free[st], static_cast<uint32_t>(i / kTokenStages - 1) & 1u)) { ok = false; break; }
-                load_round(i);
-                done = i + 1;
-            }
-            // leave no copy in flight behind (when consumers have given up)
-            for (int i = max(0, done - kTokenStages); i < done; ++i) ok = mbar_wait(&bar_full[i % kTokenStages], static_cast<uint32_t>(i / kTokenStages) & 1u) && ok;
-            if (!ok) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
-        }
+        if (lane == 0 && !bring_rows(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
     } else {
     auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
         for (int i = tid; i < rows * 2; i += kConsumers)
@@ -601,13 +615,6 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
             const int j = i * kRound + key0 + r + 8 * e;
             pos[e] = j < n_c ? __ldg(cache_pos + c_row + j) : 0x7fffffff;
         }
-    };
-    auto lds32 = [](uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; };
-    auto lds64 = [](uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; };
-    auto lds128 = [](uint32_t a) {
-        uint4 v;
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-        return v;
     };
     // ---- the query as B fragments: lane (n = r, t) holds column n, nonzero where n = t: group t's features -------------------
     const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0) * H + h) * DH;
@@ -918,6 +925,471 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     merge_chunks<__nv_bfloat16, DH>(sq, H, 0, h, 0, 1, nchunk, partials, tickets, &s_flag, O, lse);
 }
 
+// ---- blocks of bf16 queries, head size 128 -------------------------------------------------------------------------------
+// The same reading of codes as bf16 numbers with up to eight queries at once: the matrix instruction's eight columns are the queries.
+// What differs from the kernel above is which codes share an instruction: one group's only, since steps and minima are a group's.
+//   Q.K   lane t of a quad takes word 4 g + t of a key's codes for group g: two instructions per group, their sums over the lanes
+//         scaled by the key's step and added to the logit with m (sum of q over the group): queries are not rounded, codes are exact.
+//   P.V   rows of A = 16 of a group's 32 features, lane r taking half of word 4 g + (r & 3); columns of B = p s of the group, rounded to
+//         bf16 plus what that left (two instructions), so that p s keeps 16 bits.  The weights come out of Q.K with keys as rows and
+//         have to be columns: a transposition of two 8 x 8 matrices of bf16 halves (weights split into two halves, 16 bits).
+// Local keys take the same steps uncompressed, straight from global memory into the operands, into the same accumulators.
+// 24 matrix instructions per 16 keys whatever the number of queries, where the kernel above takes 16 for one.  1, 8, 16 queries over
+// 16,384 cached and 512 local keys of 40 heads: 34.5 (the kernel above), 52, 100 us; over 8 x 205 cached and 64 local keys of 32
+// heads 7.1, 10.9, 18.3; over 4 x 717 and 1280: 29, 37, 61.  (With fp32 FMAs eight queries took 226, 35 and 118.)  Expanding the rows
+// first and attending them on the tensor cores takes 188, 21 and 49 whatever the number, which is the better from about 32 on.
+constexpr int kFewQueries = 8;
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {       // an 8 x 8 matrix of 16-bit elements, two of row r in lane (r, t)
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ bool infinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// two floats as bf16 and what the rounding left of them
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = two_bf16(a, b);
+    lo = two_bf16(a - low_half(hi), b - high_half(hi));
+}
+
+__global__ void __launch_bounds__(kTokenThreads, kTokenBlocks)
+attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant__ TokenMaps maps, const Q4Source src,
+                     const __grid_constant__ AttendGroup g, const int32_t* __restrict__ cache_pos, int H, float scale_log2, int TK,
+                     __nv_bfloat16* __restrict__ O, float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets,
+                     int early_cache, int* __restrict__ dev_status) {
+    using namespace sm100;
+    constexpr int DH = 128, RED = DH + 2, G = DH / DODO_Q4_GROUP;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ float red[kTokenWarps][kFewQueries][RED];
+    __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
+    __shared__ int s_flag;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r = lane >> 2, t = lane & 3;                 // fragment row (key, feature or query) and quad lane
+    const int bid = static_cast<int>(blockIdx.x);
+    int b;
+    if (g.uniform_ctas > 0) {
+        b = bid / g.uniform_ctas;
+    } else {
+        b = 0;
+#pragma unroll 8
+        for (int i = 1; i < DODO_GROUP; ++i) b += (i < g.nseq && g.cta0[i] <= bid) ? 1 : 0;
+    }
+    const AttendSeq sq = g.seq[b];
+    int r0 = bid - g.cta0[b];
+    const int nchunk = sq.nchunk, chunk = r0 % nchunk;
+    r0 /= nchunk;
+    const int h = r0 % H, qtile = r0 / H;
+    const int q_first = qtile * kFewQueries, nq = min(kFewQueries, sq.tq - q_first);
+    const int qpos0 = sq.q_pos0 + q_first;
+    const int l_vis = max(0, min(sq.l_len, qpos0 + nq - sq.l_pos0));
+    const int nt_c = (sq.c_len + TK - 1) / TK;                             // planning tiles of TK keys
+    const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
+    const int c_begin = min(sq.c_len, t_begin * TK), c_end = min(sq.c_len, t_end * TK);
+    const int l_begin = min(l_vis, max(0, t_begin - nt_c) * TK), l_end = min(l_vis, max(0, t_end - nt_c) * TK);
+    const int n_c = c_end - c_begin, n_l = l_end - l_begin;
+    const int c_row = sq.c_row0 + c_begin, l_row = sq.l_row0 + l_begin, l_pos = sq.l_pos0 + l_begin;
+    const int rounds = (n_c + kRound - 1) / kRound;
+
+    if (tid == 0) {
+        for (int i = 0; i < kTokenStages; ++i) { mbar_init(&bar_full[i], 1); mbar_init(&bar_free[i], kTokenWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == kTokenWarps) {
+        if (lane == 0 && !bring_rows(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+    } else {
+        auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
+            for (int i = tid; i < rows * 2; i += kConsumers)
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(base + (static_cast<size_t>(row + i / 2) * H + h) * DH) + (i % 2) * 128));
+        };
+        hint_rows(Q, sq.q_row0 + q_first, nq);
+        hint_rows(static_cast<const __nv_bfloat16*>(src.lK), l_row, min(n_l, kHintKeys));
+        hint_rows(static_cast<const __nv_bfloat16*>(src.lV), l_row, min(n_l, kHintKeys));
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+        // a warp's tile of a stage: keys 16 warp + ..., in the swizzled rows of 128 bytes.  A stage begins at a multiple of 1024, so
+        // that piece p of row j is reached by flipping bits 4 to 6 of the address of piece j & 7.
+        const int key0 = 16 * warp;
+        const uint32_t k_at = static_cast<uint32_t>((key0 + r) * 128 + (r << 4) + t * 4);           // row r; row r + 8 is 1024 bytes on
+        const uint32_t ks_at = static_cast<uint32_t>(kCodeBytes + (key0 + r) * 32);
+        const uint32_t v_at = static_cast<uint32_t>((key0 + 2 * t) * 128 + (2 * t << 4) + (r & 3) * 4);   // row 2 t; row 2 t + 1 is 128 + 16 on
+        const uint32_t vs_at = static_cast<uint32_t>(kCodeBytes + (key0 + 2 * t) * 32 + 16);
+        const uint32_t sel = r < 4 ? 0x5410u : 0x7632u;            // half of the word whose nibbles are this lane's features
+
+        // ---- the queries as B fragments: lane (r, t) holds query r's features 8 t .. 8 t + 7 of each group
+        const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0 + q_first + min(r, nq - 1)) * H + h) * DH + 8 * t;
+        uint32_t qb[G][2][2];
+        float2 qsum[G], q_back;                 // of queries 2 t, 2 t + 1
+        {
+            float f[G][8], top = 0.f, sum[G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 32 * i), f[i]);
+                sum[i] = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (r >= nq) f[i][e] = 0.f;
+                    top = fmaxf(top, fabsf(f[i][e]));
+                    sum[i] += f[i][e];
+                }
+                sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+                sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+                sum[i] *= scale_log2;
+                qsum[i].x = __shfl_sync(0xffffffffu, sum[i], 8 * t);
+                qsum[i].y = __shfl_sync(0xffffffffu, sum[i], 8 * t + 4);
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // (shifts as in the kernel above, a query's own)
+            const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62), 57);
+            const float shift = __uint_as_float(static_cast<uint32_t>(kQExp - e + 127) << 23), s16 = shift * 0.0625f;
+            const float back = __uint_as_float(static_cast<uint32_t>(133 - kQExp + e + 127) << 23) * scale_log2;
+            q_back.x = __shfl_sync(0xffffffffu, back, 8 * t);
+            q_back.y = __shfl_sync(0xffffffffu, back, 8 * t + 4);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                qb[i][0][0] = two_bf16(f[i][0] * shift, f[i][4] * shift);
+                qb[i][0][1] = two_bf16(f[i][1] * s16, f[i][5] * s16);
+                qb[i][1][0] = two_bf16(f[i][2] * shift, f[i][6] * shift);
+                qb[i][1][1] = two_bf16(f[i][3] * s16, f[i][7] * s16);
+            }
+        }
+        const float kPScale = __uint_as_float(static_cast<uint32_t>(kPExp + 127) << 23);
+        // positions of queries 2 t, 2 t + 1; one that is not there sees nothing
+        const int qpos[2] = {2 * t < nq ? qpos0 + 2 * t : static_cast<int>(0x80000000), 2 * t + 1 < nq ? qpos0 + 2 * t + 1 : static_cast<int>(0x80000000)};
+
+        float m[2] = {kNeg, kNeg};               // of queries 2 t, 2 t + 1: the warp's
+        float2 l = make_float2(0.f, 0.f), accm[G];   // sums over a lane's own keys
+        float acc[G][2][4];                      // [group][features 0, 1 | 2, 3 of the lane's four]: even feature x queries 2 t, 2 t + 1, then the odd one
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            accm[i] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][u][e] = 0.f;
+        }
+        // logits of a tile (keys r, r + 8 x queries 2 t, 2 t + 1) to weights; moves the maxima and what has been summed so far
+        auto weigh = [&](auto all_seen, float2* s, const bool (*see)[2]) {
+            constexpr bool kAll = decltype(all_seen)::value;
+            if (!kAll) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { s[i].x = see[i][0] ? s[i].x : kNeg; s[i].y = see[i][1] ? s[i].y : kNeg; }
+            }
+            float top[2] = {fmaxf(s[0].x, s[1].x), fmaxf(s[0].y, s[1].y)};
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+                top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
+            }
+            if (top[0] > m[0] + 8.f || top[1] > m[1] + 8.f) {     // the reference moves only when it pays: weights stay below 2^8
+                float2 corr;
+                float to = top[0] > m[0] + 8.f ? top[0] : m[0];
+                corr.x = ex2_approx(m[0] - to);
+                m[0] = to;
+                to = top[1] > m[1] + 8.f ? top[1] : m[1];
+                corr.y = ex2_approx(m[1] - to);
+                m[1] = to;
+                l = __fmul2_rn(l, corr);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    accm[i] = __fmul2_rn(accm[i], corr);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][u][e] *= (e & 1) == 0 ? corr.x : corr.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s[i] = make_float2(ex2_approx(s[i].x - m[0]), ex2_approx(s[i].y - m[1]));
+                if (!kAll) { s[i].x = see[i][0] ? s[i].x : 0.f; s[i].y = see[i][1] ? s[i].y : 0.f; }
+                l = __fadd2_rn(l, s[i]);
+            }
+        };
+
+        // ---- cached keys: one tile of 16 per warp and stage -------------------------------------------------------------------
+        auto reduce = [&](auto all_seen, uint32_t base, const int* pos) {
+            constexpr bool kAll = decltype(all_seen)::value;
+            bool see[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) see[i][c] = kAll || pos[i] <= qpos[c];
+            float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            {
+                const uint4 w0 = lds128(base + ks_at), w1 = lds128(base + ks_at + 256u);
+                const uint32_t wa[4] = {w0.x, w0.y, w0.z, w0.w}, wb[4] = {w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const uint32_t at = (base + k_at) ^ (16u * i);
+                    const uint32_t ka = lds32(at), kb = lds32(at + 1024u), ha = ka >> 8, hb = kb >> 8;
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma16816(d, ka & 0x000f000fu, kb & 0x000f000fu, ka & 0x00f000f0u, kb & 0x00f000f0u, qb[i][0][0], qb[i][0][1]);
+                    mma16816(d, ha & 0x000f000fu, hb & 0x000f000fu, ha & 0x00f000f0u, hb & 0x00f000f0u, qb[i][1][0], qb[i][1][1]);
+                    s[0] = __ffma2_rn(__fmul2_rn(make_float2(d[0], d[1]), q_back), make_float2(low_half(wa[i]), low_half(wa[i])), s[0]);
+                    s[1] = __ffma2_rn(__fmul2_rn(make_float2(d[2], d[3]), q_back), make_float2(low_half(wb[i]), low_half(wb[i])), s[1]);
+                    s[0] = __ffma2_rn(qsum[i], make_float2(high_half(wa[i]), high_half(wa[i])), s[0]);
+                    s[1] = __ffma2_rn(qsum[i], make_float2(high_half(wb[i]), high_half(wb[i])), s[1]);
+                }
+            }
+            weigh(all_seen, s, see);
+            // minima of the values; a masked key takes no part, whatever its words hold
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 w = lds128(base + ks_at + 16u + 256u * i);
+                const uint32_t wv[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int n = 0; n < G; ++n) {
+                    const float2 v = __ffma2_rn(s[i], make_float2(high_half(wv[n]), high_half(wv[n])), accm[n]);
+                    accm[n].x = see[i][0] ? v.x : accm[n].x;
+                    accm[n].y = see[i][1] ? v.y : accm[n].y;
+                }
+                if (!kAll) { s[i].x = see[i][0] ? s[i].x : -1.f; s[i].y = see[i][1] ? s[i].y : -1.f; }    // (a mark for the other side)
+            }
+            // keys as columns: query r's weights of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t hi, lo;
+                split2(s[i].x, s[i].y, hi, lo);
+                hi = transpose8(hi);
+                lo = transpose8(lo);
+                p[2 * i] = low_half(hi) + low_half(lo);
+                p[2 * i + 1] = high_half(hi) + high_half(lo);
+            }
+            uint32_t wv[4][4];
+            bool hid[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hid[i] = !kAll && p[i] < 0.f;
+                p[i] *= kPScale;
+                const uint4 w = lds128(base + vs_at + 32u * (i & 1) + 256u * (i >> 1));
+                wv[i][0] = w.x; wv[i][1] = w.y; wv[i][2] = w.z; wv[i][3] = w.w;
+            }
+#pragma unroll
+            for (int n = 0; n < G; ++n) {
+                float x[4];
+                uint32_t c[4], hi[2], lo[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = p[i] * low_half(wv[i][n]);
+                    if (!kAll) x[i] = hid[i] ? 0.f : x[i];
+                    c[i] = lds32(((base + v_at + (i & 1) * 144u) ^ (64u + 16u * n)) + 1024u * (i >> 1));
+                }
+                split2(x[0], x[1], hi[0], lo[0]);
+                split2(x[2], x[3], hi[1], lo[1]);
+                uint32_t wa = __byte_perm(c[0], c[1], sel), wc = __byte_perm(c[2], c[3], sel);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    mma16816(acc[n][u], wa & 0x000f000fu, wa & 0x00f000f0u, wc & 0x000f000fu, wc & 0x00f000f0u, hi[0], hi[1]);
+                    mma16816(acc[n][u], wa & 0x000f000fu, wa & 0x00f000f0u, wc & 0x000f000fu, wc & 0x00f000f0u, lo[0], lo[1]);
+                    wa >>= 8;
+                    wc >>= 8;
+                }
+            }
+        };
+        auto positions = [&](int i, int* pos) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int j = i * kRound + key0 + r + 8 * e;
+                pos[e] = j < n_c ? __ldg(cache_pos + c_row + j) : 0x7fffffff;
+            }
+        };
+        bool ok = true;
+        const int mine = n_c > key0 ? (n_c - key0 + kRound - 1) / kRound : 0;      // stages that hold keys of this warp's
+        int next_pos[2];
+        positions(0, next_pos);
+        for (int i = 0; i < rounds; ++i) {
+            const int st = i % kTokenStages;
+            const int pos[2] = {next_pos[0], next_pos[1]};
+            if (i + 1 < rounds) positions(i + 1, next_pos);
+            if (__all_sync(0xffffffffu, mbar_wait(&bar_full[st], static_cast<uint32_t>(i / kTokenStages) & 1u)) == 0) { ok = false; break; }
+            if (i < mine) {
+                if (__all_sync(0xffffffffu, max(pos[0], pos[1]) <= qpos0)) reduce(std::true_type(), ring + st * kStageBytes, pos);
+                else reduce(std::false_type(), ring + st * kStageBytes, pos);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar_free[st]);
+        }
+        if (!ok && lane == 0) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+
+        // ---- from the codes' scale to that of plain values ------------------------------------------------------------------------
+        {
+            const float back = __uint_as_float(static_cast<uint32_t>(133 - kPExp + 127) << 23), back16 = back * 0.0625f;
+#pragma unroll
+            for (int n = 0; n < G; ++n) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    accm[n].x += __shfl_xor_sync(0xffffffffu, accm[n].x, o);
+                    accm[n].y += __shfl_xor_sync(0xffffffffu, accm[n].y, o);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[n][u][e] = fmaf(acc[n][u][e], e < 2 ? back : back16, (e & 1) == 0 ? accm[n].x : accm[n].y);
+                accm[n] = make_float2(0.f, 0.f);
+            }
+        }
+
+        // ---- local keys, 16 a warp: K and V rows as operands, pieces of them straight from global memory -----------------------------
+        if (16 * warp < n_l) {
+            uint4 qf[G];                        // query r's features 32 g + 8 t + ...
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                qf[i] = *reinterpret_cast<const uint4*>(qrow + 32 * i);
+                if (r >= nq) qf[i] = make_uint4(0, 0, 0, 0);
+            }
+            const size_t pitch = static_cast<size_t>(H) * DH;
+            const __nv_bfloat16* const lk = static_cast<const __nv_bfloat16*>(src.lK) + static_cast<size_t>(l_row) * pitch + static_cast<size_t>(h) * DH + 8 * t;
+            const __nv_bfloat16* const lv = static_cast<const __nv_bfloat16*>(src.lV) + static_cast<size_t>(l_row) * pitch + static_cast<size_t>(h) * DH + 8 * (r & 3) + 4 * (r >> 2);
+            for (int first = 16 * warp; first < n_l; first += kRound) {
+                bool see[2][2];
+                uint4 k[2][G];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int j = first + r + 8 * i;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) see[i][c] = j < n_l && l_pos + j <= qpos[c];
+#pragma unroll
+                    for (int n = 0; n < G; ++n) {
+                        k[i][n] = make_uint4(0, 0, 0, 0);
+                        if (j < n_l) k[i][n] = __ldg(reinterpret_cast<const uint4*>(lk + static_cast<size_t>(j) * pitch + 32 * n));
+                    }
+                }
+                uint2 v[4][G];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = first + 2 * t + (i & 1) + 8 * (i >> 1);
+#pragma unroll
+                    for (int n = 0; n < G; ++n) {
+                        v[i][n] = make_uint2(0, 0);
+                        if (j < n_l) v[i][n] = __ldg(reinterpret_cast<const uint2*>(lv + static_cast<size_t>(j) * pitch + 32 * n));
+                    }
+                }
+                float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                for (int n = 0; n < G; n += 2) {
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = n; e < n + 2; ++e) {
+                        mma16816(d, k[0][e].x, k[1][e].x, k[0][e].y, k[1][e].y, qf[e].x, qf[e].y);
+                        mma16816(d, k[0][e].z, k[1][e].z, k[0][e].w, k[1][e].w, qf[e].z, qf[e].w);
+                    }
+                    s[0] = __fadd2_rn(s[0], make_float2(d[0], d[1]));
+                    s[1] = __fadd2_rn(s[1], make_float2(d[2], d[3]));
+                }
+                const float2 scale2 = make_float2(scale_log2, scale_log2);
+                s[0] = __fmul2_rn(s[0], scale2);
+                s[1] = __fmul2_rn(s[1], scale2);
+                weigh(std::false_type(), s, see);
+                uint32_t hi[2], lo[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    split2(s[i].x, s[i].y, hi[i], lo[i]);
+                    hi[i] = transpose8(hi[i]);
+                    lo[i] = transpose8(lo[i]);
+                }
+                // A key behind some of the tile's queries may hold anything, and 0 times that need not be 0: if a value is not finite there,
+                // one query at a time, with the rows it does not see as zeros.
+                bool apart = false;
+                if (l_pos + min(first + 15, n_l - 1) > qpos0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int n = 0; n < G; ++n) apart = apart || infinite2(v[i][n].x) || infinite2(v[i][n].y);
+                    apart = __any_sync(0xffffffffu, apart);
+                }
+                if (!apart) {
+#pragma unroll
+                    for (int n = 0; n < G; ++n)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const uint32_t w0 = u == 0 ? v[0][n].x : v[0][n].y, w1 = u == 0 ? v[1][n].x : v[1][n].y;
+                            const uint32_t w2 = u == 0 ? v[2][n].x : v[2][n].y, w3 = u == 0 ? v[3][n].x : v[3][n].y;
+                            const uint32_t a0 = __byte_perm(w0, w1, 0x5410), a1 = __byte_perm(w0, w1, 0x7632);
+                            const uint32_t a2 = __byte_perm(w2, w3, 0x5410), a3 = __byte_perm(w2, w3, 0x7632);
+                            mma16816(acc[n][u], a0, a1, a2, a3, hi[0], hi[1]);
+                            mma16816(acc[n][u], a0, a1, a2, a3, lo[0], lo[1]);
+                        }
+                } else {
+#pragma unroll 1
+                    for (int q = 0; q < nq; ++q) {
+                        const uint32_t bh[2] = {r == q ? hi[0] : 0u, r == q ? hi[1] : 0u}, bl[2] = {r == q ? lo[0] : 0u, r == q ? lo[1] : 0u};
+                        bool sees[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sees[i] = l_pos + first + 2 * t + (i & 1) + 8 * (i >> 1) <= qpos0 + q;
+#pragma unroll
+                        for (int n = 0; n < G; ++n)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) w[i] = !sees[i] ? 0u : u == 0 ? v[i][n].x : v[i][n].y;
+                                const uint32_t a0 = __byte_perm(w[0], w[1], 0x5410), a1 = __byte_perm(w[0], w[1], 0x7632);
+                                const uint32_t a2 = __byte_perm(w[2], w[3], 0x5410), a3 = __byte_perm(w[2], w[3], 0x7632);
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma16816(d, a0, a1, a2, a3, bh[0], bh[1]);
+                                mma16816(d, a0, a1, a2, a3, bl[0], bl[1]);
+                                if (2 * t == q) { acc[n][u][0] += d[0]; acc[n][u][2] += d[2]; }
+                                if (2 * t + 1 == q) { acc[n][u][1] += d[1]; acc[n][u][3] += d[3]; }
+                            }
+                    }
+                }
+            }
+        }
+
+        // ---- the warp's record ----------------------------------------------------------------------------------------------------
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            l.x += __shfl_xor_sync(0xffffffffu, l.x, o);
+            l.y += __shfl_xor_sync(0xffffffffu, l.y, o);
+        }
+#pragma unroll
+        for (int n = 0; n < G; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    red[warp][2 * t + (e & 1)][32 * n + 8 * (r & 3) + 4 * (r >> 2) + 2 * u + (e >> 1)] = acc[n][u][e];
+        if (r == 0) {
+            red[warp][2 * t][DH] = m[0];
+            red[warp][2 * t + 1][DH] = m[1];
+            red[warp][2 * t][DH + 1] = l.x;
+            red[warp][2 * t + 1][DH + 1] = l.y;
+        }
+    }       // (consumers)
+    __syncthreads();
+    for (int i = tid; i < nq * DH; i += kTokenThreads) {
+        const int q2 = i / DH, dim = i % DH;
+        float M = kNeg;
+#pragma unroll
+        for (int w = 0; w < kTokenWarps; ++w) M = fmaxf(M, red[w][q2][DH]);
+        float L = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kTokenWarps; ++w) {
+            const float wgt = ex2_approx(red[w][q2][DH] - M);
+            L = fmaf(red[w][q2][DH + 1], wgt, L);
+            o = fmaf(red[w][q2][dim], wgt, o);
+        }
+        if (nchunk == 1) {
+            write_out<__nv_bfloat16, DH>(O, lse, static_cast<size_t>(sq.q_row0 + q_first + q2) * H + h, dim, M, L, o);
+        } else {
+            float* pr = partials + (static_cast<size_t>(sq.part0) + (static_cast<size_t>(q_first + q2) * H + h) * nchunk + chunk) * RED;
+            pr[dim] = o;
+            if (dim == 0) { pr[DH] = M; pr[DH + 1] = L; }
+        }
+    }
+    if (nchunk == 1) return;
+    merge_chunks<__nv_bfloat16, DH>(sq, H, qtile, h, q_first, nq, nchunk, partials, tickets, &s_flag, O, lse);
+}
+
 template <typename T, int DH, int QT, int U>
 int launch_t(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const void* Q, const Q4Source& src,
              const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
@@ -931,14 +1403,14 @@ int launch_t(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const v
 template <typename T, int DH>
 int launch_qt(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src,
               const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
-    if constexpr (sizeof(T) == 4 || DH != 128)                 // (bf16 at 128: the kernel for single queries)
-        if (qt == 1) return launch_t<T, DH, 1, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
+    if (qt == 1) return launch_t<T, DH, 1, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
     if (qt == 2) return launch_t<T, DH, 2, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
     if (qt == 4) return launch_t<T, DH, 4, 2>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early, st);
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: query tile %d is not built", qt);
 }
 
-int launch_token(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const void* Q, const Q4Source& src, int cache_rows,
+// the two kernels for bf16 at head size 128
+int launch_mma(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src, int cache_rows,
                  const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
     TokenMaps maps;
     memset(&maps, 0, sizeof maps);
@@ -948,12 +1420,14 @@ int launch_token(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, con
         if (rc != DODO_OK) return rc;
     }
     const size_t smem = static_cast<size_t>(kTokenStages) * kStageBytes + 1024;
-    if (!ctx->q4_attr_set) {
-        const cudaError_t e = cudaFuncSetAttribute(attend_q4_token_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    auto kern = qt == 1 ? attend_q4_token_kernel : attend_q4_few_kernel;
+    bool& set = ctx->q4_attr_set[qt == 1 ? 0 : 1];
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "4-bit attend shared-memory attribute");
-        ctx->q4_attr_set = true;
+        set = true;
     }
-    return dodo_check_cuda(ctx, dodo_launch_dependent(attend_q4_token_kernel, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kTokenThreads), smem, st,
+    return dodo_check_cuda(ctx, dodo_launch_dependent(kern, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kTokenThreads), smem, st,
                                                       static_cast<const __nv_bfloat16*>(Q), maps, src, g, cache_pos, H, sm_scale * 1.4426950408889634f,
                                                       dodo_attend_tile_keys(DODO_BF16, 128), static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
                            "4-bit attend launch");
@@ -967,10 +1441,8 @@ int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scal
                           float* partials, int* tickets, bool early_cache, cudaStream_t st) {
     if (g.cta0[g.nseq] == 0) return DODO_OK;
     const Q4Source src = {static_cast<const uint32_t*>(cache_q4), cache_scale, locK, locV};
-    if (dtype == DODO_BF16 && dh == 128 && plan.qt == 1)     // (plan.qt 1: no sequence has more than one query)
-        return launch_token(ctx, H, sm_scale, g, Q, src, cache_rows, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_BF16 && dh == 128)
-        return launch_qt<__nv_bfloat16, 128>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
+        return launch_mma(ctx, H, sm_scale, plan.qt, g, Q, src, cache_rows, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_BF16 && dh == 64)
         return launch_qt<__nv_bfloat16, 64>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_F32 && dh == 128)
@@ -979,3 +1451,5 @@ int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scal
         return launch_qt<float, 64>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: dtype %d with head size %d", dtype, dh);
 }
+
+int dodo_attend_q4_tile_queries(int dtype, int dh, int max_tq) { return dtype == DODO_BF16 && dh == 128 && max_tq > 1 ? kFewQueries : 0; }

@@ -34,7 +34,7 @@ struct dodo_ctx {
     struct MapEntry { const void* base; int rows, width, box_rows, kind; CUtensorMap map; } map_cache[16];
     int map_next;               // round-robin replacement
     bool dense_attr_set[4];     // shared-memory attribute of the four forms of the tensor-core kernel
-    bool q4_attr_set;           // ... and of the 4-bit single-query kernel
+    bool q4_attr_set[2];        // ... and of the 4-bit kernels on the warp-level matrix units
     bool backward_attr_set[4];  // ... and of the kernels of attend's gradient
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
@@ -231,7 +231,8 @@ struct AttendTotals {
     int min_chunk;                 // key tiles a chunk has at least
     int64_t part_rows, tick_rows;  // running totals over launch groups
 };
-void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& plan, AttendTotals& tot);
+// qt: queries per tile where the kernel has only one choice, 0 to go by the longest block
+void dodo_attend_plan_begin(const AttendShape& s, int target_ctas, AttendPlan& plan, AttendTotals& tot, int qt = 0);
 void dodo_attend_plan_group(const AttendShape& s, const AttendPlan& plan, AttendTotals& tot, int b0, int nb,
                             AttendGroup& g);
 // ---- dense (tensor-core) attend ----------------------------------------------------------------
@@ -259,6 +260,8 @@ int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendG
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
 // The streaming kernels over a 4-bit cache: launch as above, the cache (cache_rows rows) as codes and group words
+// queries per tile where the kernel of these types has only one choice, else 0
+int dodo_attend_q4_tile_queries(int dtype, int dh, int max_tq);
 int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const AttendPlan& plan,
                           const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale, int cache_rows,
                           const int32_t* cache_pos, const void* locK, const void* locV, void* O, float* lse,
@@ -307,6 +310,7 @@ enum { DODO_BWD_STREAM = 0, DODO_BWD_TILE = 1, DODO_BWD_DENSE = 2 };
 // tile sizes the planner needs: keys per key block, queries per query tile, keys per step of a query block
 struct BackwardTiles { int keys, queries, step; };
 BackwardTiles dodo_backward_tiles(int variant, int dtype, int dh);
+int dodo_backward_stream_queries(int dtype, int dh);     // longest query block of the streaming kernel
 int dodo_launch_backward_stream(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, int max_tq, const BackwardGroup& g,
                                 const BackwardArrays& a, cudaStream_t st);
 int dodo_launch_backward_stats(dodo_ctx* ctx, int H, int dh, const BackwardGroup& g, const BackwardArrays& a, cudaStream_t st);

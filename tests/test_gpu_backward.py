@@ -124,6 +124,9 @@ SHAPES = [
     (F32, 2, 128, [33, 5, 64], [70, 0, 129], [40, 5, 64]),
     (BF, 2, 64, [7, 100, 0, 31], [300, 64, 20, 1], [7, 130, 9, 31]),
     (F32, 1, 64, [65], [2000], [65]),
+    (F32, 3, 128, [8, 5, 0, 1], [205, 1300, 9, 64], [64, 5, 3, 1]),
+    (F32, 2, 128, [9, 16, 2], [130, 0, 700], [9, 80, 33]),
+    (F32, 3, 64, [5, 17, 8], [64, 65, 300], [70, 17, 8]),
 ]
 
 
@@ -213,7 +216,7 @@ def test_gradient_negative_and_zero_scale(dodo, dtype, dh, tq):
         check(p, d, out, dense=dtype == BF and tq > 4)
 
 
-@pytest.mark.parametrize("dtype,H,dh,tq", [(F32, 2, 64, 2), (F32, 2, 128, 40), (BF, 2, 64, 70), (BF, 2, 128, 4), (BF, 2, 128, 70)])
+@pytest.mark.parametrize("dtype,H,dh,tq", [(F32, 2, 64, 2), (F32, 2, 128, 40), (F32, 2, 128, 8), (F32, 2, 64, 12), (BF, 2, 64, 70), (BF, 2, 128, 4), (BF, 2, 128, 70)])
 def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
     """Nuggets ahead of every query, and local tokens behind it, hold NaN and infinities: their own gradients are 0, nobody
     else's changes; queries before the first key get 0."""
@@ -240,7 +243,7 @@ def test_gradient_masked_rows_may_hold_anything(dodo, dtype, H, dh, tq):
     assert bool((out["dQ"][tq:] == 0).all())
 
 
-@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 24), (BF, 64, 40), (BF, 128, 100)])
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 24), (F32, 128, 7), (F32, 64, 13), (BF, 64, 40), (BF, 128, 100)])
 def test_gradient_partly_visible_nan_key(dodo, dtype, dh, tq):
     """A key that only later queries see holds NaN: earlier queries' dQ is untouched."""
     p = problem(("bwdpart", dh, tq), dtype, 1, dh, [tq], [0], [tq], slack=0)

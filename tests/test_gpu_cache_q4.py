@@ -237,6 +237,10 @@ SHAPES = [
     (BF, 1, 128, [7], [4097], [100]),
     (BF, 40, 128, [1], [3277], [64]),
     (BF, 5, 64, [13, 31], [100, 900], [31, 40]),
+    (BF, 2, 128, [2, 3, 0, 8, 1], [700, 16, 33, 205, 1], [2, 40, 7, 64, 130]),
+    (BF, 3, 128, [9, 16, 5], [64, 1000, 0], [80, 16, 333]),
+    (BF, 1, 128, [31], [2000], [31]),
+    (BF, 2, 128, [17, 6], [0, 81], [17, 1000]),
 ]
 
 
@@ -295,8 +299,29 @@ def test_attend_q4_visible_nan_shows(dodo, dtype, dh):
     assert bool(nan[32:64].all()) and not bool(nan[:32].any()) and not bool(nan[64:].any()) and bool(torch.isfinite(lse).all())
 
 
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 5), (BF, 128, 13), (BF, 64, 3), (F32, 64, 6)])
+def test_attend_q4_partly_visible_nan_token(dodo, dtype, dh, tq):
+    """A local token, and a nugget, that only the later queries see hold NaN and infinities: earlier queries' outputs are untouched."""
+    p = _problem(("q4part", dh, tq), dtype, 2, dh, [tq], [50], [tq + 3], slack=0)
+    clean, lc = _run_q4(dodo, p)
+    for what, value in ((0, "nan"), (1, "nan"), (1, "inf")):
+        q = dict(p, loc=[t.clone() for t in p["loc"]])
+        q["loc"][what][tq + 3 - 2] = float(value)                # the last query but one's own token
+        O, lse = _run_q4(dodo, q)
+        assert torch.equal(O[:tq - 2], clean[:tq - 2]) and torch.equal(lse[:tq - 2], lc[:tq - 2])
+        assert not bool(torch.isfinite(O[tq - 2:].float()).any())
+        assert bool(torch.isfinite(lse[tq - 2:]).all()) == (what == 1)
+    q = dict(p, words=p["words"].copy(), cpos=p["cpos"].copy())
+    q["cpos"][49] = p["q_pos0"][0] + 2                           # a nugget that the first two queries do not see
+    hidden, lh = _run_q4(dodo, q)
+    q["words"][49] = 0x7fc07fc0
+    O, lse = _run_q4(dodo, q)
+    assert torch.equal(O[:2], hidden[:2]) and torch.equal(lse[:2], lh[:2])
+    assert bool(torch.isnan(O[2:]).all()) and bool(torch.isnan(lse[2:]).all())
+
+
 # the token kernel carries codes as bf16 numbers far below 1 and weights times steps far above: both ends of its range
-@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 2), (F32, 64, 1)])
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (F32, 64, 1)])
 @pytest.mark.parametrize("kstd,vstd", [(1.0, 1e13), (1.0, 1e-15), (1.0, 1e-20), (1e12, 1.0), (1e-12, 1.0), (1e18, 1e-10)])
 def test_attend_q4_range_of_values(dodo, dtype, dh, tq, kstd, vstd):
     p = _problem(("q4range", kstd, vstd, tq), dtype, 2, dh, [tq, tq], [300, 40], [1, 0], kstd=kstd, vstd=vstd)
@@ -306,31 +331,31 @@ def test_attend_q4_range_of_values(dodo, dtype, dh, tq, kstd, vstd):
     _check(p, *_run_q4(dodo, p))
 
 
-@pytest.mark.parametrize("dtype,dh", [(BF, 128), (BF, 64), (F32, 128)])
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 3), (BF, 64, 1), (F32, 128, 1)])
 @pytest.mark.parametrize("rise", [0.3, 3.0, 90.0])
-def test_attend_q4_rising_and_falling_logits(dodo, dtype, dh, rise):
+def test_attend_q4_rising_and_falling_logits(dodo, dtype, dh, tq, rise):
     """The running maximum climbs by less and by more than what moves the reference, from tile to tile and inside one."""
-    p = _problem(("q4rise", rise), dtype, 2, dh, [1, 1], [513, 130], [2, 0])
+    p = _problem(("q4rise", rise), dtype, 2, dh, [tq, tq], [513, 130], [tq + 1, 0])
     K = plain64.values(p["codes"][:, :, 0], p["words"][:, :, 0])
     q = _f64(p["Q"])
     rows = np.arange(len(K))
     for b in range(2):      # key j along the query, so that its logit is about rise * j / 16, falling in the second sequence
         r = slice(int(p["cache_off"][b]), int(p["cache_off"][b + 1]))
         j = (rows[r] - r.start) * (1 if b == 0 else -1)
-        unit = q[b] / (np.sum(q[b] ** 2, -1, keepdims=True) * p["scale"])
+        unit = q[tq * b] / (np.sum(q[tq * b] ** 2, -1, keepdims=True) * p["scale"])
         K[r] = 0.05 * K[r] + (rise * j / 16.0)[:, None, None] * unit
     x = torch.from_numpy(K).float().to(dtype).float().numpy()
     p["codes"][:, :, 0], p["words"][:, :, 0] = plain64.pack(*plain64.quantise(x))
     _check(p, *_run_q4(dodo, p))
 
 
-@pytest.mark.parametrize("dtype,H,dh", [(BF, 3, 128), (F32, 2, 64)])
-def test_attend_q4_many_sequences(dodo, dtype, H, dh):
+@pytest.mark.parametrize("dtype,H,dh,tq", [(BF, 3, 128, 1), (BF, 3, 128, 10), (F32, 2, 64, 1)])
+def test_attend_q4_many_sequences(dodo, dtype, H, dh, tq):
     # 70 sequences: two launch groups, some of them cut, whose partials share the workspace
     rs = np.random.RandomState(8)
     cl = rs.randint(0, 300, 70)
     cl[[3, 66]] = 3000, 5000
-    p = _problem(("q4seqs", dh), dtype, H, dh, [int(x) for x in rs.randint(0, 2, 70)], cl.tolist(), rs.randint(0, 40, 70).tolist())
+    p = _problem(("q4seqs", dh), dtype, H, dh, [int(x) for x in rs.randint(0, tq + 1, 70)], cl.tolist(), rs.randint(0, 40, 70).tolist())
     _check(p, *_run_q4(dodo, p))
 
 
@@ -365,8 +390,9 @@ def test_q4_rows_behind_two_to_the_31_elements(dodo):
 
 
 @pytest.mark.parametrize("inside", [False, True])
-def test_attend_q4_query_block_on_tensor_cores(dodo, inside):
-    p = _problem(("q4block", inside), BF, 3, 128, [130, 32, 1], [333, 64, 0], [200, 40, 70], inside)
+@pytest.mark.parametrize("tqs", [[130, 32, 1], [8, 1, 5]])
+def test_attend_q4_query_block_on_tensor_cores(dodo, tqs, inside):
+    p = _problem(("q4block", inside), BF, 3, 128, tqs, [333, 64, 0], [200, 40, 70], inside)
     rows = p["codes"].shape[0]
     need = dodo.attend_q4_workspace_bytes(3, 128, rows)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
