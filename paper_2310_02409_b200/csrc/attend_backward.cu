@@ -363,55 +363,78 @@ template <int N, int DH> struct RowPieces {
         }
     }
 };
-// weights of J x 16 queries: dot products of a 4-key x J-query register tile, over all features, of (K, Q) and (V, dO)
-template <int DH, int J>
-__device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0, float scale2) {
-    const int tk = threadIdx.x % 16, tq = threadIdx.x / 16;     // keys tk + 16 i, queries tq + 16 j
-    float2 s[4][J], t[4][J];
+// Dot products of a tile, 32 keys x 8 queries per warp (warp w: keys from 32 (w & 1), queries from 8 (w / 2)).  A thread sums a quarter
+// of the features for 8 keys x 4 queries, so that a load of 16 bytes feeds 21 products (with all the features of 4 x 2 pairs a thread
+// it was 5, and shared memory the bound); the four quarters are added up by exchanges that leave a lane 4 keys x 2 queries:
+// keys lane_key + 4 i, queries lane_query + 2 j.  The quarters start two pieces apart, which spreads a load over all banks.
+template <int DH>
+__device__ __forceinline__ void tile_dots(const float (*A)[DH + 4], const float (*B)[DH + 4], float (&out)[4][2]) {
+    constexpr int kPieces = DH / 16;                // 16-byte pieces of a quarter
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = lane >> 3;
+    const float* const a = A[32 * (warp & 1) + (lane >> 1 & 3)] + quarter * (DH / 4);
+    const float* const b = B[8 * (warp >> 1) + (lane & 1)] + quarter * (DH / 4);
+    // head size 128: pairs of features in packed sums; 64, where registers decide whether two blocks fit an SM: single ones
+    constexpr bool kPacked = DH == 128;
+    float2 s[8][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < J; ++j) s[i][j] = t[i][j] = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int c = 0; c < DH; c += 4) {
-        float4 k[4], v[4], q[J], o[J];
+        for (int j = 0; j < 4; ++j) s[i][j] = make_float2(0.f, 0.f);
+#pragma unroll kPacked ? 2 : 1
+    for (int c = 0; c < kPieces; ++c) {
+        const int at = 4 * ((c + 2 * quarter) & (kPieces - 1));
+        float4 x[8], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            k[i] = *reinterpret_cast<const float4*>(&sm.K[tk + 16 * i][c]);
-            v[i] = *reinterpret_cast<const float4*>(&sm.V[tk + 16 * i][c]);
-        }
+        for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float4*>(a + 4 * i * (DH + 4) + at);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            q[j] = *reinterpret_cast<const float4*>(&sm.Q[tq + 16 * j][c]);
-            o[j] = *reinterpret_cast<const float4*>(&sm.G[tq + 16 * j][c]);
-        }
+        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + 2 * j * (DH + 4) + at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                s[i][j] = __ffma2_rn(make_float2(k[i].x, k[i].y), make_float2(q[j].x, q[j].y), s[i][j]);
-                t[i][j] = __ffma2_rn(make_float2(v[i].x, v[i].y), make_float2(o[j].x, o[j].y), t[i][j]);
-                s[i][j] = __ffma2_rn(make_float2(k[i].z, k[i].w), make_float2(q[j].z, q[j].w), s[i][j]);
-                t[i][j] = __ffma2_rn(make_float2(v[i].z, v[i].w), make_float2(o[j].z, o[j].w), t[i][j]);
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (kPacked) {
+                    s[i][j] = __ffma2_rn(make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y), s[i][j]);
+                    s[i][j] = __ffma2_rn(make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w), s[i][j]);
+                } else {
+                    s[i][j].x = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j].x))));
+                }
             }
     }
+    const bool up16 = (lane & 16) != 0, up8 = (lane & 8) != 0;
+    float h[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int key = tk + 16 * i, q = tq + 16 * j;
-            const bool see = q < nq && sm.kpos[key] <= qpos0 + q;
-            const float2 st = sm.stat[q];
-            const float p = see ? ex2_approx(fmaf(s[i][j].x + s[i][j].y, scale2, st.x)) : 0.f;
-            sm.P[q][key] = p;
-            sm.S[q][key] = see ? p * (t[i][j].x + t[i][j].y + st.y) : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            const float low = s[i][j].x + s[i][j].y, high = s[i + 4][j].x + s[i + 4][j].y;
+            h[i][j] = (up16 ? high : low) + __shfl_xor_sync(0xffffffffu, up16 ? low : high, 16);
         }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            out[i][j] = (up8 ? h[i][j + 2] : h[i][j]) + __shfl_xor_sync(0xffffffffu, up8 ? h[i][j] : h[i][j + 2], 8);
 }
-// (up to 16 queries: the other half of the tile is not computed; a warp whose queries are all behind the last has nothing to do)
+// weights and dS of a tile (a warp whose queries are all behind the last has nothing to do)
 template <int DH>
 __device__ __forceinline__ void tile_weights(TileSmem<DH>& sm, int nq, int qpos0, float scale2) {
-    if (nq > 16) tile_weights<DH, 2>(sm, nq, qpos0, scale2);
-    else if (static_cast<int>(threadIdx.x / 32) * 2 < nq) tile_weights<DH, 1>(sm, nq, qpos0, scale2);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (8 * (warp >> 1) >= nq) return;
+    float s[4][2], t[4][2];
+    tile_dots<DH>(sm.K, sm.Q, s);
+    tile_dots<DH>(sm.V, sm.G, t);
+    const int key0 = 32 * (warp & 1) + (lane >> 1 & 3) + (lane >> 4) * 16, q0 = 8 * (warp >> 1) + (lane & 1) + (lane >> 3 & 1) * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int key = key0 + 4 * i, q = q0 + 2 * j;
+            const bool see = q < nq && sm.kpos[key] <= qpos0 + q;
+            const float2 st = sm.stat[q];
+            const float p = see ? ex2_approx(fmaf(s[i][j], scale2, st.x)) : 0.f;
+            sm.P[q][key] = p;
+            sm.S[q][key] = see ? p * (t[i][j] + st.y) : 0.f;
+        }
 }
 
 template <int DH>
@@ -532,11 +555,13 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         g2.put(sm.G);
     }
     tile_stats<DH>(sm.stat, a, H, h, sq.q_row0 + q0, nq);
-    float2 dq[2][2 * ND];
+    // a warp owns four queries, a lane DH / 32 consecutive features of theirs
+    const int lane = tid & 31, qw = 4 * (tid >> 5);
+    float2 dq[4][ND];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < 2 * ND; ++e) dq[i][e] = make_float2(0.f, 0.f);
+        for (int e = 0; e < ND; ++e) dq[i][e] = make_float2(0.f, 0.f);
     // the next keys are on their way while these are worked on
     RowPieces<TK, DH> next_k, next_v;
     int next_pos = 0;
@@ -559,45 +584,46 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
         if (t + 1 < t1) fetch_keys(t + 1);
         tile_weights<DH>(sm, nq, sq.q_pos0 + q0, scale2);
         __syncthreads();
-        auto add = [&](float2* acc, float w, float4 x, int d) {
-            // a key that some queries of the tile do not see may hold anything: its dS is exactly 0 there
-            if (w != 0.f) {
-                acc[2 * d] = __ffma2_rn(make_float2(w, w), make_float2(x.x, x.y), acc[2 * d]);
-                acc[2 * d + 1] = __ffma2_rn(make_float2(w, w), make_float2(x.z, x.w), acc[2 * d + 1]);
-            }
-        };
-        if (nq > 16) {
-#pragma unroll 4
-            for (int k = 0; k < TK; ++k) {
-                const float s0 = sm.S[ty][k], s1 = sm.S[ty + 16][k];
+        if (qw < nq) {
+#pragma unroll 2
+            for (int k = 0; k < TK; k += 4) {
+                float w[4][4];
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const float4 x = *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]);
-                    add(dq[0], s0, x, d);
-                    add(dq[1], s1, x, d);
+                for (int i = 0; i < 4; ++i) {
+                    const float4 u = *reinterpret_cast<const float4*>(&sm.S[qw + i][k]);
+                    w[i][0] = u.x; w[i][1] = u.y; w[i][2] = u.z; w[i][3] = u.w;
                 }
-            }
-        } else if (ty < nq) {
-#pragma unroll 4
-            for (int k = 0; k < TK; ++k) {
-                const float s0 = sm.S[ty][k];
 #pragma unroll
-                for (int d = 0; d < ND; ++d) add(dq[0], s0, *reinterpret_cast<const float4*>(&sm.K[k][64 * d + 4 * tx]), d);
+                for (int e = 0; e < 4; ++e) {
+                    float2 x[ND];
+                    const float2* const row = reinterpret_cast<const float2*>(&sm.K[k + e][2 * ND * lane]);
+                    if constexpr (ND == 2) {
+                        const float4 v = *reinterpret_cast<const float4*>(row);
+                        x[0] = make_float2(v.x, v.y);
+                        x[1] = make_float2(v.z, v.w);
+                    } else {
+                        x[0] = *row;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (w[i][e] != 0.f) {   // a key that some queries of the tile do not see may hold anything: its dS is exactly 0 there
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) dq[i][d] = __ffma2_rn(make_float2(w[i][e], w[i][e]), x[d], dq[i][d]);
+                        }
+                }
             }
         }
     }
     float* out = static_cast<float*>(a.dQ) + static_cast<size_t>(sq.q_row0 + q0) * row_elems + static_cast<size_t>(h) * DH;
     const size_t part = static_cast<size_t>(sq.part0 + (qt * H + h) * sq.nchunk);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int q = ty + 16 * i;
+    for (int i = 0; i < 4; ++i) {
+        const int q = qw + i;
         if (q >= nq) continue;
+        float* const row = (sq.nchunk == 1 ? out + q * row_elems : a.dq_part + ((part + chunk) * TQ + q) * DH) + 2 * ND * lane;
+        const float f = sq.nchunk == 1 ? scale : 1.f;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            const float4 v = make_float4(dq[i][2 * d].x, dq[i][2 * d].y, dq[i][2 * d + 1].x, dq[i][2 * d + 1].y);
-            if (sq.nchunk == 1) store4(out + q * row_elems + 64 * d + 4 * tx, make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale));
-            else store4(a.dq_part + ((part + chunk) * TQ + q) * DH + 64 * d + 4 * tx, v);
-        }
+        for (int d = 0; d < ND; ++d) *reinterpret_cast<float2*>(row + 2 * d) = make_float2(dq[i][d].x * f, dq[i][d].y * f);
     }
     if (sq.nchunk == 1 || !last_arrival(a.tickets + sq.qtick0 + qt * H + h, sq.nchunk, &sm.flag)) return;
     for (int i = tid; i < nq * (DH / 4); i += kThreads) {
