@@ -92,12 +92,11 @@ int plan_group(dodo_ctx* ctx, const AttendShape& s, int variant, int b0, int nb,
         }
         if (q.nchunk > 1) {
             parts += units * q.nchunk;
-            qticks += units;
+            if (variant != DODO_BWD_DENSE) qticks += units;       // (the tensor-core kernel leaves joins and scores to kernels of their own)
         }
     }
     for (int i = 0; i < nb; ++i) {
         g.seq[i].stick0 = static_cast<int>(qticks + sticks);
-        // (the tensor-core kernel leaves the scores to a kernel of their own)
         sticks += variant == DODO_BWD_STREAM ? g.seq[i].nchunk : variant == DODO_BWD_TILE ? ceil_div(g.seq[i].c_len, t.keys) : 0;
     }
     if (qticks + sticks > DODO_NUM_TICKETS - 1)      // (the last counter hands out the tensor-core kernel's units)

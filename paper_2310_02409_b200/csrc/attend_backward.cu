@@ -293,8 +293,8 @@ __global__ void __launch_bounds__(kThreads)
 backward_scores_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int parts) {
     __shared__ float sums[kThreads / 32][32];
     const int b = blockIdx.y, row = static_cast<int>(blockIdx.x) * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
-    if (static_cast<int>(blockIdx.x) * 32 >= g.seq[b].c_len) return;
     dodo_grid_dependency_sync();
+    if (static_cast<int>(blockIdx.x) * 32 >= g.seq[b].c_len) return;
     float s = 0.f;
     if (row < g.seq[b].c_len) {
         const float* p = a.score_part + g.seq[b].c_row0 + row;

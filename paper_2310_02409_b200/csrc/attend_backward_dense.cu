@@ -65,13 +65,12 @@ struct Sync {
     uint64_t x[2], xdone[2], staged[2];                  // a unit's pair: here, its slots free again, its results staged in them
     uint64_t y[kRing], yfree[kRing];                     // a tile: here, consumed
     uint64_t s[3], t[3], p[3], d[3], a[3];               // a score buffer: S, T, P, dS there; consumed
-    uint64_t done, epi[2], meet, unit[kAhead], unit_free[kAhead];     // accumulators: complete; read out (each of the two)
+    uint64_t done, epi[2], unit[kAhead], unit_free[kAhead];     // accumulators: complete; read out (each of the two)
     int x_slot[2];           // slots of a unit's pair (first | second << 8), units with tiles counted
     int y_slot[kRing];       // a tile's slot
     int release[kRing];      // producer: slots that come back with a tile
     int unit_id[kAhead];
     uint32_t tmem;
-    int last;
 };
 constexpr int kSmemBytes = kOffSync + 512;
 static_assert(sizeof(Sync) <= 512 && kSmemBytes <= 227 * 1024, "shared memory");
@@ -248,7 +247,6 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
         for (int i = 0; i < kAhead; ++i) { mbar_init(&sy.unit[i], 1); mbar_init(&sy.unit_free[i], 3 + kWeightWarps + kEndWarps); }
         mbar_init(&sy.done, 1);
         for (int i = 0; i < 2; ++i) mbar_init(&sy.epi[i], kEndWarps);
-        mbar_init(&sy.meet, kEndWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -655,14 +653,6 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
         const int row = tid & (BM - 1);
         const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
         int x = 0;
-        uint32_t turn = 0;
-        // the four warps meet (a barrier with a bounded wait: a warp that has left must not hold the others)
-        auto meet = [&]() {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sy.meet);
-            if (!warp_wait(&sy.meet, turn & 1u)) ok = false;
-            ++turn;
-        };
         for (int k = 0; ok; ++k) {
             const int id = unit_number(k);
             if (id < 0) { ok = id == -1; break; }
@@ -672,6 +662,7 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
             const bool live = row < u.rows;
             const size_t at = (static_cast<size_t>(u.row0 + row) * H + u.h) * DH;
             const bool cut = !u.keys && sq.nchunk > 1;
+            const bool some = (row & ~31) < u.rows;      // the warp has live rows (a short query block fills one of four)
             const size_t unit0 = cut ? static_cast<size_t>(sq.part0 + (u.qt * H + u.h) * sq.nchunk) : 0u;
             float* const mine = a.dq_part + (unit0 + u.chunk) * (BM * DH) + row;     // [feature][row]: a warp's lanes write consecutive floats
             void* const out[2] = {u.keys ? (u.cached ? a.dcK : a.dlK) : a.dQ, u.cached ? a.dcV : a.dlV};
@@ -690,8 +681,10 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                         uint32_t va[32], vb[32];
                         auto put = [&](int c, const uint32_t* v) {
                             if (cut) {
+                                if (some) {
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * BM] = __uint_as_float(v[e]);
+                                    for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * BM] = __uint_as_float(v[e]);
+                                }
                                 return;
                             }
 #pragma unroll
@@ -725,45 +718,12 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                 if (lane == 0) mbar_arrive(&sy.staged[x & 1]);
                 ++x;
             } else if (cut) {             // an empty chunk's partial
-                for (int e = 0; e < DH; ++e) mine[e * BM] = 0.f;
+                if (some)
+                    for (int e = 0; e < DH; ++e) mine[e * BM] = 0.f;
             } else if (live) {            // nothing was summed: zeros
                 for (int o = 0; o < outs; ++o)
                     for (int e = 0; e < DH / 8; ++e) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out[o]) + at + 8 * e) = make_uint4(0, 0, 0, 0);
             }
-            if (!cut) continue;
-            // ---- the last chunk of a query tile to arrive adds up all of them, in chunk order
-            __threadfence();
-            meet();
-            if (ok && tid == 32 * kWeightWarps) {
-                int* counter = a.tickets + sq.qtick0 + u.qt * H + u.h;
-                const int t = atomicAdd(counter, 1);
-                *reinterpret_cast<volatile int*>(&sy.last) = t == sq.nchunk - 1;
-                if (t == sq.nchunk - 1) *counter = 0;
-            }
-            if (ok) meet();
-            if (!ok) break;
-            if (shared_int(sy.last)) {
-                __threadfence();
-#pragma unroll 1
-                for (int c = 0; c < DH / 16; ++c) {
-                    float o[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = 0.f;
-                    for (int n = 0; n < sq.nchunk; ++n) {
-                        const float* src = a.dq_part + (unit0 + n) * (BM * DH) + (c * 16) * BM + row;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] += __ldcg(src + e * BM);
-                    }
-                    if (live) {
-                        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dQ) + at + c * 16);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            dst[e] = make_uint4(pack_bf16(o[8 * e] * scale, o[8 * e + 1] * scale), pack_bf16(o[8 * e + 2] * scale, o[8 * e + 3] * scale),
-                                                pack_bf16(o[8 * e + 4] * scale, o[8 * e + 5] * scale), pack_bf16(o[8 * e + 6] * scale, o[8 * e + 7] * scale));
-                    }
-                }
-            }
-            meet();     // `last` is free again
         }
     }
     if (!ok) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
@@ -771,6 +731,35 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
     __syncthreads();
     if (warp == 0)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// dQ of query units cut into chunks of the key list: their partial tiles added up in chunk order, 8 features of 128 queries a block.
+// (A kernel of its own: done by the last chunk's block, which has other units to go on with, it held up one block for 50 us.)
+template <int DH>
+__global__ void __launch_bounds__(BM)
+backward_join_kernel(const BackwardArrays a, const __grid_constant__ BackwardGroup g, int H, float scale) {
+    const BackwardSeq& sq = g.seq[blockIdx.z];
+    const int unit = static_cast<int>(blockIdx.x), qt = unit / H, h = unit % H, q = qt * BM + static_cast<int>(threadIdx.x), c = 8 * static_cast<int>(blockIdx.y);
+    dodo_grid_dependency_sync();
+    if (sq.nchunk == 1 || q >= sq.tq) return;
+    const float* const src = a.dq_part + static_cast<size_t>(sq.part0 + unit * sq.nchunk) * (BM * DH) + c * BM + threadIdx.x;
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int n = 0; n < sq.nchunk; n += 4) {        // four chunks' loads in flight together
+        float v[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = __ldcg(src + static_cast<size_t>(min(n + k, sq.nchunk - 1)) * (BM * DH) + e * BM);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += n + k < sq.nchunk ? v[k][e] : 0.f;
+    }
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dQ) + (static_cast<size_t>(sq.q_row0 + q) * H + h) * DH + c) =
+        make_uint4(pack_bf16(o[0] * scale, o[1] * scale), pack_bf16(o[2] * scale, o[3] * scale), pack_bf16(o[4] * scale, o[5] * scale),
+                   pack_bf16(o[6] * scale, o[7] * scale));
 }
 
 }  // namespace
@@ -801,8 +790,17 @@ static int launch_dense(dodo_ctx* ctx, int slot, int H, float sm_scale, const Ba
     }
     const int grid = total < ctx->num_sms ? total : ctx->num_sms;
     backward_dense_kernel<DH><<<grid, kThreads, smem, st>>>(maps, g, a, H, sm_scale, next_unit, ctx->dev_status);
-    const cudaError_t e = cudaGetLastError();
+    cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient launch");
+    int units = 0;      // most (query tile, head) units of a sequence whose units are cut
+    for (int i = 0; i < g.nseq; ++i) {
+        const int n = g.seq[i].nchunk > 1 ? (g.seq[i].tq + BM - 1) / BM * H : 0;
+        units = units > n ? units : n;
+    }
+    if (units > 0) {
+        e = dodo_launch_dependent(backward_join_kernel<DH>, dim3(static_cast<unsigned>(units), DH / 8, static_cast<unsigned>(g.nseq)), dim3(BM), 0, st, a, g, H, sm_scale);
+        if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "attend gradient launch");
+    }
     return dodo_launch_backward_scores(ctx, g, a, 2 * H, st);
 }
 
