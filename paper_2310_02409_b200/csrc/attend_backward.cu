@@ -666,8 +666,8 @@ int launch_tile(dodo_ctx* ctx, int slot, int H, float scale, const BackwardGroup
 }  // namespace
 
 // The streaming kernel beats the others up to four queries everywhere (4 queries over 8 x 269 keys of 32 heads of 128: bf16 33.5
-// against 58 us on the tensor cores, fp32 36 against 128; 4160 keys: 53 / 128, 62 / 209; head size 64: bf16 22 / 52, fp32 with 8
-// heads 12 / 18).  With eight it still does for fp32 rows of 128 (66 to 72 against 129 to 141 us; 106 to 112 against 210 to 228); at 64
+// against 58 us on the tensor cores, fp32 36 against 124; 4160 keys: 53 / 76, 62 / 197; head size 64: bf16 22 / 51, fp32 with 8
+// heads 12 / 18).  With eight it still does for fp32 rows of 128 (66 to 72 against 124 us; 106 to 112 against 197); at 64
 // the tiles are as fast (20 to 23 against 18 to 20), and bf16 has twice the features a lane, whose sums eight queries do not fit.
 int dodo_backward_stream_queries(int dtype, int dh) { return dtype == DODO_F32 && dh == 128 ? 8 : 4; }
 
