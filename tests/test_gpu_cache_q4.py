@@ -144,11 +144,11 @@ def test_gather_q4_bad_index_is_reported_not_followed(libdodo):
 
 
 # ---- attention --------------------------------------------------------------------------------------------------------
-def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2, kstd=1.0, vstd=2.0):
+def _problem(tag, dtype, H, dh, tqs, clens, llens, inside=False, slack=2, kstd=1.0, vstd=2.0, scale=None):
     """A ragged batch over a 4-bit cache; row regions have slack rows that hold NaN groups, the local array NaN rows."""
     rs = np.random.RandomState(inputs.seed_for(tag) % 2 ** 32)
     B = len(tqs)
-    p = dict(B=B, H=H, dh=dh, dtype=dtype, scale=dh ** -0.5)
+    p = dict(B=B, H=H, dh=dh, dtype=dtype, scale=dh ** -0.5 if scale is None else scale)
     p["q_off"], p["cache_off"] = inputs.offsets(tqs), inputs.offsets([c + slack for c in clens])
     p["clen"], p["llen"] = np.asarray(clens, np.int32), np.asarray(llens, np.int32)
     p["loc_off"] = inputs.offsets([n + slack for n in llens])[:-1].copy()
@@ -347,6 +347,13 @@ def test_attend_q4_rising_and_falling_logits(dodo, dtype, dh, tq, rise):
     x = torch.from_numpy(K).float().to(dtype).float().numpy()
     p["codes"][:, :, 0], p["words"][:, :, 0] = plain64.pack(*plain64.quantise(x))
     _check(p, *_run_q4(dodo, p))
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (BF, 128, 40), (BF, 64, 2), (F32, 128, 1)])
+def test_attend_q4_negative_and_zero_scale(dodo, dtype, dh, tq):
+    for scale in (-0.1, 0.0):
+        p = _problem(("q4scale", scale, tq), dtype, 2, dh, [tq, tq], [300, 40], [tq, tq + 3], scale=scale)
+        _check(p, *_run_q4(dodo, p))
 
 
 @pytest.mark.parametrize("dtype,H,dh,tq", [(BF, 3, 128, 1), (BF, 3, 128, 10), (F32, 2, 64, 1)])
