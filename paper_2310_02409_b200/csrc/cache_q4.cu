@@ -70,8 +70,14 @@ __device__ __forceinline__ float rcp_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 32 bytes, streaming
-__device__ __forceinline__ void load32(const void* p, uint32_t* v) {
+// 32 bytes, streaming; `whole`: p is a multiple of 32, else of 16
+__device__ __forceinline__ void load32(const unsigned char* p, uint32_t* v, bool whole) {
+    if (!whole) {
+        const uint4 a = ld_stream16(p), b = ld_stream16(p + 16);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        return;
+    }
     asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
 }
@@ -187,9 +193,10 @@ gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __res
     }
     const int kv = i < groups ? 0 : 1, c = i - kv * groups, h = c / per_head;
     const size_t src = ((static_cast<size_t>(g.src_row0[b]) + static_cast<size_t>(token)) * groups + c) * (kWords * 4);
+    const bool whole = (reinterpret_cast<uintptr_t>(kv == 0 ? K : V) & 31u) == 0u;      // (rows are multiples of 64 bytes)
     uint32_t raw[kWords];
 #pragma unroll
-    for (int w = 0; w < kWords; w += 8) load32((kv == 0 ? K : V) + src + 4 * w, raw + w);
+    for (int w = 0; w < kWords; w += 8) load32((kv == 0 ? K : V) + src + 4 * w, raw + w, whole);
     const int dst_row = g.dst_row0[b] + (j - g.idx0[b]);
     if (i == 0) cache_pos[dst_row] = g.pos_base[b] + token;
     float x[kGroup];

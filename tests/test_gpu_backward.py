@@ -361,6 +361,27 @@ def test_training_step_of_the_scorer(dodo, oracle):
     assert np.linalg.norm(_f64(dw) - ref_dw) <= 1e-5 * np.linalg.norm(ref_dw) + 1e-6
 
 
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 2), (BF, 128, 40), (BF, 64, 7), (F32, 128, 3), (F32, 128, 7), (F32, 64, 20)])
+def test_gradient_at_the_least_alignment(dodo, dtype, dh, tq):
+    """Every tensor at a multiple of 16 bytes that is not one of 32."""
+    def at16(t):
+        k = 16 // t.element_size()
+        buf = torch.empty(t.numel() + 2 * k, dtype=t.dtype, device="cuda")
+        first = k if (buf.data_ptr() + 16) % 32 else 0
+        out = buf[first:first + t.numel()].view(t.shape)
+        out.copy_(t)
+        assert out.data_ptr() % 32 == 16
+        return out
+    p = problem(("bwdalign", dh, tq), dtype, 3, dh, [tq], [600], [tq + 5])
+    d = forward(dodo, p)
+    want = backward(dodo, p, d)
+    ws = torch.empty(dodo.attend_backward_workspace_bytes(tq, 3, dh, int(p["cache_off"][-1])), dtype=torch.uint8, device="cuda")
+    moved = {n: at16(t) for n, t in d.items()}
+    got = backward(dodo, p, moved, {n: at16(t) for n, t in buffers(d).items()}, ws=at16(ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[n].nan_to_num(5.0), want[n].nan_to_num(5.0)) for n in want)
+
+
 @pytest.mark.parametrize("dtype,tq", [(BF, 2), (BF, 40), (F32, 9)])
 def test_gradient_of_rows_behind_two_to_the_31_elements(dodo, dtype, tq):
     """A region that starts behind 2^31 elements of the cache and of the local rows: the same gradients as in small arrays."""

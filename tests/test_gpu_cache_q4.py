@@ -366,6 +366,41 @@ def test_attend_q4_many_sequences(dodo, dtype, H, dh, tq):
     _check(p, *_run_q4(dodo, p))
 
 
+def _at16(t):
+    """The same tensor at an address that is a multiple of 16 and not of 32 or more."""
+    k = 16 // t.element_size()
+    buf = torch.empty(t.numel() + 2 * k, dtype=t.dtype, device="cuda")
+    first = k if (buf.data_ptr() + 16) % 32 else 0
+    out = buf[first:first + t.numel()].view(t.shape)
+    out.copy_(t)
+    assert out.data_ptr() % 32 == 16
+    return out
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+def test_q4_at_the_least_alignment(dodo, dtype, dh):
+    H, n = 3, 90
+    K, V, Q = (inputs.randn((n, H, dh), "q4align", k, dtype=dtype).cuda() for k in "KVQ")
+    idx = torch.arange(0, n, 2, dtype=torch.int32, device="cuda")
+    got = []
+    for place in (lambda t: t, _at16):
+        q4, sc, pos = (place(t) for t in _cache(45, H, dh, 0))
+        clen = np.zeros(1, np.int32)
+        dodo.gather_kv_q4(place(K), place(V), [0, n], idx, [0, 45], [0], q4, sc, pos, [0, 45], clen)
+        out = [q4, sc, pos]
+        eK, eV = place(torch.zeros((45, H, dh), dtype=dtype, device="cuda")), place(torch.zeros((45, H, dh), dtype=dtype, device="cuda"))
+        dodo.expand_kv_q4(q4, sc, [0, 45], clen, eK, eV)
+        out += [eK, eV]
+        for tq in (1, 5, 40):
+            ws = place(torch.empty(dodo.attend_q4_workspace_bytes(H, dh, 45), dtype=torch.uint8, device="cuda"))
+            O, lse = place(torch.empty((tq, H, dh), dtype=dtype, device="cuda")), torch.empty((tq, H), device="cuda")
+            dodo.attend_q4(place(Q[:tq].contiguous()), [0, tq], [n], dh ** -0.5, q4, sc, pos, [0, 45], clen, place(K), place(V), [0], [n], [n], O, lse, ws)
+            out += [O, lse]
+        torch.cuda.synchronize()
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_q4_rows_behind_two_to_the_31_elements(dodo):
     """The second sequence's region starts behind 2^31 codes: its rows, appended, expanded and attended, are those of a small cache."""
     H, dh, far, n = 128, 128, 270_000, 70
