@@ -70,9 +70,10 @@ __device__ __forceinline__ float rcp_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 32 bytes, streaming; `whole`: p is a multiple of 32, else of 16
-__device__ __forceinline__ void load32(const unsigned char* p, uint32_t* v, bool whole) {
-    if (!whole) {
+// 32 bytes, streaming; kWhole: p is a multiple of 32, else of 16
+template <bool kWhole>
+__device__ __forceinline__ void load32(const unsigned char* p, uint32_t* v) {
+    if constexpr (!kWhole) {
         const uint4 a = ld_stream16(p), b = ld_stream16(p + 16);
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
@@ -168,7 +169,7 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* codes) {
 // per feature.  8 x 205 nuggets of 32 heads of 128, bf16: 15.8 us (17.1 with one feature per instruction, 24 with an octet per
 // thread; dodo_gather_kv takes 10.1 to copy the same rows), bound by issue and by the load's latency, which a thread's single
 // group does not cover.
-template <typename T>
+template <typename T, bool kWhole>
 __global__ void __launch_bounds__(kGatherThreads, 16)
 gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __restrict__ V, int H, int dh,
                  const int32_t* __restrict__ idx, const __grid_constant__ GatherGroup g, unsigned char* __restrict__ cache_q4,
@@ -193,10 +194,9 @@ gather_q4_kernel(const unsigned char* __restrict__ K, const unsigned char* __res
     }
     const int kv = i < groups ? 0 : 1, c = i - kv * groups, h = c / per_head;
     const size_t src = ((static_cast<size_t>(g.src_row0[b]) + static_cast<size_t>(token)) * groups + c) * (kWords * 4);
-    const bool whole = (reinterpret_cast<uintptr_t>(kv == 0 ? K : V) & 31u) == 0u;      // (rows are multiples of 64 bytes)
     uint32_t raw[kWords];
 #pragma unroll
-    for (int w = 0; w < kWords; w += 8) load32((kv == 0 ? K : V) + src + 4 * w, raw + w, whole);
+    for (int w = 0; w < kWords; w += 8) load32<kWhole>((kv == 0 ? K : V) + src + 4 * w, raw + w);
     const int dst_row = g.dst_row0[b] + (j - g.idx0[b]);
     if (i == 0) cache_pos[dst_row] = g.pos_base[b] + token;
     float x[kGroup];
@@ -279,9 +279,10 @@ int dodo_launch_gather_q4(dodo_ctx* ctx, const void* K, const void* V, int dtype
     unsigned char* q4 = static_cast<unsigned char*>(cache_q4);
     const long long items = static_cast<long long>(total) * 2 * H * (dh / kGroup);
     const dim3 grid(static_cast<unsigned>((items + kGatherThreads - 1) / kGatherThreads)), block(kGatherThreads);
-    const cudaError_t e = dtype == DODO_BF16
-        ? dodo_launch_dependent(gather_q4_kernel<__nv_bfloat16>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status)
-        : dodo_launch_dependent(gather_q4_kernel<float>, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status);
+    const bool whole = ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 31u) == 0u;      // (rows are multiples of 128 bytes)
+    auto kern = dtype == DODO_BF16 ? (whole ? gather_q4_kernel<__nv_bfloat16, true> : gather_q4_kernel<__nv_bfloat16, false>)
+                                   : (whole ? gather_q4_kernel<float, true> : gather_q4_kernel<float, false>);
+    const cudaError_t e = dodo_launch_dependent(kern, grid, block, 0, st, k, v, H, dh, idx, g, q4, cache_scale, cache_pos, dev_status);
     return dodo_check_cuda(ctx, e, "4-bit gather launch");
 }
 
