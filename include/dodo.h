@@ -398,7 +398,7 @@ DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32
  * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale > 0) runs on the tensor cores when the
  * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
  * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
- * call takes the streaming kernel.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache
+ * call that has cached rows takes the streaming kernels.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache
  * by other means than dodo_gather_kv_q4 calls dodo_cache_written.  Positions of queries and local tokens lie in
  * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.  Steps s of cached values stay below 2^47 (values below
  * about 2^50 in magnitude; larger ones may come out as NaN or infinity).

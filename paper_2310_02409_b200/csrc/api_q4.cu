@@ -130,7 +130,7 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     AttendShape shp = {q_off, q_pos0, cache_off, cache_len, loc_off, loc_len, loc_pos0, B, H, dh, dtype};
     AttendPlan plan;
     AttendTotals tot;
-    dodo_attend_plan_begin(shp, ctx->attend_target_ctas, plan, tot, dodo_attend_q4_tile_queries(dtype, dh, max_tq));
+    dodo_attend_plan_begin(shp, ctx->attend_target_ctas, plan, tot, dodo_attend_q4_tile_queries(dtype, max_tq));
     // A sequence whose key list is longer than a block's share of the work is cut even when there are units enough for the
     // device (one long sequence of a ragged batch would outlast all others), but never into chunks of less than four tiles,
     // whose merge costs more than it saves (8 x 269 keys of 32 heads in two chunks each: 11.8 against 6.6 us).  The share is

@@ -18,17 +18,18 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
-// [rows, width] tensor of bf16 (box of 64 elements x box_rows rows, 128-byte swizzle) or bytes (box of box_width)
-enum MapKind { kBf16 = 0, kBytes32 = 1, kBytes128 = 2 };
+// [rows, width] tensor of bf16 (kind kBf16: boxes of 64 elements x box_rows rows, 128-byte swizzle) or of bytes (kind: the box's
+// width, 16, 32, 64 or 128; swizzled over 64 and 128 bytes)
+constexpr int kBf16 = 0;
 int encode_rows(void* fn, CUtensorMap* map, const void* base, int kind, int width, int rows, int box_rows, char* err,
                 size_t err_len) {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {dims[0] * (kind == kBf16 ? 2 : 1)};
-    const cuuint32_t box[2] = {kind == kBf16 ? 64u : kind == kBytes32 ? 32u : 128u, static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t box[2] = {kind == kBf16 ? 64u : static_cast<cuuint32_t>(kind), static_cast<cuuint32_t>(box_rows)};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult r = reinterpret_cast<EncodeTiledFn>(fn)(
         map, kind == kBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, kind == kBytes32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, kind == kBf16 || kind == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : kind == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         if (err != nullptr && err_len > 0) snprintf(err, err_len, "cuTensorMapEncodeTiled failed with %d", static_cast<int>(r));
@@ -67,7 +68,7 @@ int dodo_encode_bf16_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int
     return cached_sw128(ctx, map, base, width, rows, box_rows, ctx->err, sizeof ctx->err);
 }
 int dodo_encode_byte_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_width, int box_rows) {
-    return cached_rows(ctx, map, base, box_width == 32 ? kBytes32 : kBytes128, width, rows, box_rows, ctx->err, sizeof ctx->err);
+    return cached_rows(ctx, map, base, box_width, width, rows, box_rows, ctx->err, sizeof ctx->err);
 }
 
 int dodo_dense_encode_maps(dodo_ctx* ctx, const AttendShape& s, const void* Q, int q_rows, const void* cacheK,

@@ -7,16 +7,16 @@
 //
 // A cached key is 160 bytes a head (dh 128) where bf16 has 512, so the bound moves towards instruction issue: what counts
 // is instructions per code.  Three kernels:
-//   attend_q4_kernel        fp32, and bf16 at head size 64; tiles of 1, 2 or 4 queries: fp32 FMAs, exact codes as floats
-//   attend_q4_token_kernel  bf16 at head size 128, one query per sequence: the codes go to the matrix units as they are
-//   attend_q4_few_kernel    bf16 at head size 128, tiles of eight queries: likewise
+//   attend_q4_kernel        fp32, and single bf16 queries at head size 64: fp32 FMAs, exact codes as floats
+//   attend_q4_token_kernel  single bf16 queries at head size 128: the codes go to the matrix units as they are
+//   attend_q4_few_kernel    bf16, tiles of eight queries: likewise
 //
 // attend_q4_kernel: a lane owns a run of 16 features of a head (half a group: 8 bytes of codes, one word each of K and V
 // steps); eight lanes share a key of 128.  A code is turned into a float in place, without a shift: masking nibble i of a
 // word and or-ing in the exponent of 2^23 gives 2^23 + c 16^i exactly, one packed subtraction per two codes takes the 2^23
 // off, and the weight 16^i is folded into the query feature (for K) and divided out of the accumulator at the end (for V),
 // both powers of two and exact.  That is 2.1 instructions per code and product, and instruction issue bounds it: one bf16 query
-// over 8 x 205 cached and 64 local keys of 32 heads of 64 takes 5.2 us (four queries 12.0), fp32 of 128 8.3 (19.5).
+// over 8 x 205 cached and 64 local keys of 32 heads of 64 takes 5.2 us, one of fp32 of 128 8.3 (four queries 19.5).
 #include "dodo_internal.cuh"
 #include "sm100_ptx.cuh"
 #include <type_traits>
@@ -506,20 +506,24 @@ constexpr int kTokenWarps = 4;                // consumers; one more warp brings
 constexpr int kConsumers = 32 * kTokenWarps, kTokenThreads = kConsumers + 32;
 constexpr int kRound = 16 * kTokenWarps;       // keys of a stage: 16 per warp
 constexpr int kTokenStages = 4, kTokenBlocks = 3;
-constexpr int kCodeBytes = kRound * 128, kStageBytes = (kCodeBytes + kRound * 32 + 1023) / 1024 * 1024;
+// a stage: the codes of its keys' rows (dh bytes each, swizzled), then their group words (dh / 4 bytes)
+constexpr int code_bytes(int dh) { return kRound * dh; }
+constexpr int stage_bytes(int dh) { return (code_bytes(dh) + kRound * dh / 4 + 1023) / 1024 * 1024; }
+constexpr int kCodeBytes = code_bytes(128), kStageBytes = stage_bytes(128);
 
 // The producer's part, one thread: `rounds` stages of rows from c_row on through the ring.  Ahead of the dependency wait (see
 // attend.cu) it copies only when nothing in flight writes a cache.  False when a wait ran out.
+template <int DH>
 __device__ __forceinline__ bool bring_rows(const TokenMaps& maps, uint32_t ring, uint64_t* bar_full, uint64_t* bar_free, int h, int c_row, int rounds,
                                            int early_cache) {
     using namespace sm100;
     bool ok = true;
     auto load_round = [&](int i) {
         const int st = i % kTokenStages;
-        const uint32_t dst = ring + st * kStageBytes;
-        mbar_expect_tx(&bar_full[st], kCodeBytes + kRound * 32);
-        tma_load_2d(dst, &maps.q4, h * 128, c_row + i * kRound, &bar_full[st]);
-        tma_load_2d(dst + kCodeBytes, &maps.scale, h * 32, c_row + i * kRound, &bar_full[st]);
+        const uint32_t dst = ring + st * stage_bytes(DH);
+        mbar_expect_tx(&bar_full[st], code_bytes(DH) + kRound * DH / 4);
+        tma_load_2d(dst, &maps.q4, h * DH, c_row + i * kRound, &bar_full[st]);
+        tma_load_2d(dst + code_bytes(DH), &maps.scale, h * (DH / 4), c_row + i * kRound, &bar_full[st]);
     };
     const int ahead = min(rounds, kTokenStages);
     if (early_cache)
@@ -585,7 +589,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     __syncthreads();
     bool ok = true;
     if (warp == kTokenWarps) {
-        if (lane == 0 && !bring_rows(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+        if (lane == 0 && !bring_rows<128>(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
     } else {
     auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
         for (int i = tid; i < rows * 2; i += kConsumers)
@@ -925,7 +929,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     merge_chunks<__nv_bfloat16, DH>(sq, H, 0, h, 0, 1, nchunk, partials, tickets, &s_flag, O, lse);
 }
 
-// ---- blocks of bf16 queries, head size 128 -------------------------------------------------------------------------------
+// ---- blocks of bf16 queries ------------------------------------------------------------------------------------------------
 // The same reading of codes as bf16 numbers with up to eight queries at once: the matrix instruction's eight columns are the queries.
 // What differs from the kernel above is which codes share an instruction: one group's only, since steps and minima are a group's.
 //   Q.K   lane t of a quad takes word 4 g + t of a key's codes for group g: two instructions per group, their sums over the lanes
@@ -938,6 +942,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 // 16,384 cached and 512 local keys of 40 heads: 34.5 (the kernel above), 52, 100 us; over 8 x 205 cached and 64 local keys of 32
 // heads 7.1, 10.9, 18.3; over 4 x 717 and 1280: 29, 37, 61.  (With fp32 FMAs eight queries took 226, 35 and 118.)  Expanding the rows
 // first and attending them on the tensor cores takes 188, 21 and 49 whatever the number, which is the better from about 32 on.
+// Head size 64, the same three batches: eight queries 32, 6.9, 25 us (FMAs: four queries 58, 12.0), sixteen 64, 12, 37.
 constexpr int kFewQueries = 8;
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {       // an 8 x 8 matrix of 16-bit elements, two of row r in lane (r, t)
@@ -954,13 +959,15 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
     lo = two_bf16(a - low_half(hi), b - high_half(hi));
 }
 
+template <int DH>
 __global__ void __launch_bounds__(kTokenThreads, kTokenBlocks)
 attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant__ TokenMaps maps, const Q4Source src,
                      const __grid_constant__ AttendGroup g, const int32_t* __restrict__ cache_pos, int H, float scale_log2, int TK,
                      __nv_bfloat16* __restrict__ O, float* __restrict__ lse, float* __restrict__ partials, int* __restrict__ tickets,
                      int early_cache, int* __restrict__ dev_status) {
     using namespace sm100;
-    constexpr int DH = 128, RED = DH + 2, G = DH / DODO_Q4_GROUP;
+    constexpr int RED = DH + 2, G = DH / DODO_Q4_GROUP;
+    constexpr uint32_t kWordRow = DH / 4, kCodes = code_bytes(DH), kStage = stage_bytes(DH);
     extern __shared__ unsigned char smem_raw[];
     __shared__ float red[kTokenWarps][kFewQueries][RED];
     __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
@@ -1001,11 +1008,12 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
     }
     __syncthreads();
     if (warp == kTokenWarps) {
-        if (lane == 0 && !bring_rows(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
+        if (lane == 0 && !bring_rows<DH>(maps, ring, bar_full, bar_free, h, c_row, rounds, early_cache)) atomicOr(dev_status, DODO_DEV_WAIT_TIMEOUT);
     } else {
         auto hint_rows = [&](const __nv_bfloat16* base, int row, int rows) {
-            for (int i = tid; i < rows * 2; i += kConsumers)
-                asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(base + (static_cast<size_t>(row + i / 2) * H + h) * DH) + (i % 2) * 128));
+            constexpr int kLines = DH / 64;
+            for (int i = tid; i < rows * kLines; i += kConsumers)
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(base + (static_cast<size_t>(row + i / kLines) * H + h) * DH) + (i % kLines) * 128));
         };
         hint_rows(Q, sq.q_row0 + q_first, nq);
         hint_rows(static_cast<const __nv_bfloat16*>(src.lK), l_row, min(n_l, kHintKeys));
@@ -1013,13 +1021,25 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
         asm volatile("griddepcontrol.wait;" ::: "memory");
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-        // a warp's tile of a stage: keys 16 warp + ..., in the swizzled rows of 128 bytes.  A stage begins at a multiple of 1024, so
-        // that piece p of row j is reached by flipping bits 4 to 6 of the address of piece j & 7.
+        // a warp's tile of a stage: keys 16 warp + ..., in swizzled rows of DH bytes.  A stage begins at a multiple of 1024, so that
+        // piece p of a row is reached by flipping bits 4 to 6 (rows of 128 bytes) or 4 and 5 (of 64) of the address of the piece whose
+        // number is the row's swizzle: row & 7, or (row / 2) & 3.
         const int key0 = 16 * warp;
-        const uint32_t k_at = static_cast<uint32_t>((key0 + r) * 128 + (r << 4) + t * 4);           // row r; row r + 8 is 1024 bytes on
-        const uint32_t ks_at = static_cast<uint32_t>(kCodeBytes + (key0 + r) * 32);
-        const uint32_t v_at = static_cast<uint32_t>((key0 + 2 * t) * 128 + (2 * t << 4) + (r & 3) * 4);   // row 2 t; row 2 t + 1 is 128 + 16 on
-        const uint32_t vs_at = static_cast<uint32_t>(kCodeBytes + (key0 + 2 * t) * 32 + 16);
+        const uint32_t swz_r = DH == 128 ? r : r >> 1, swz_t = DH == 128 ? 2 * t : t;
+        const uint32_t k_at = static_cast<uint32_t>((key0 + r) * DH + t * 4) + (swz_r << 4);             // row r; row r + 8 is 8 DH bytes on
+        const uint32_t ks_at = kCodes + (key0 + r) * kWordRow;
+        const uint32_t v_at = static_cast<uint32_t>((key0 + 2 * t) * DH + (r & 3) * 4) + (swz_t << 4);   // row 2 t; the next one's swizzle is
+        constexpr uint32_t kNextRow = DH == 128 ? 128 + 16 : 64;                                         // one more, or the same
+        const uint32_t vs_at = kCodes + (key0 + 2 * t) * kWordRow + 4 * G;
+        auto words = [](uint32_t at, uint32_t* w) {       // a key's G group words
+            if constexpr (G == 4) {
+                const uint4 v = lds128(at);
+                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            } else {
+                const uint2 v = lds64(at);
+                w[0] = v.x; w[1] = v.y;
+            }
+        };
         const uint32_t sel = r < 4 ? 0x5410u : 0x7632u;            // half of the word whose nibbles are this lane's features
 
         // ---- the queries as B fragments: lane (r, t) holds query r's features 8 t .. 8 t + 7 of each group
@@ -1124,12 +1144,13 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
                 for (int c = 0; c < 2; ++c) see[i][c] = kAll || pos[i] <= qpos[c];
             float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             {
-                const uint4 w0 = lds128(base + ks_at), w1 = lds128(base + ks_at + 256u);
-                const uint32_t wa[4] = {w0.x, w0.y, w0.z, w0.w}, wb[4] = {w1.x, w1.y, w1.z, w1.w};
+                uint32_t wa[G], wb[G];
+                words(base + ks_at, wa);
+                words(base + ks_at + 8 * kWordRow, wb);
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
                     const uint32_t at = (base + k_at) ^ (16u * i);
-                    const uint32_t ka = lds32(at), kb = lds32(at + 1024u), ha = ka >> 8, hb = kb >> 8;
+                    const uint32_t ka = lds32(at), kb = lds32(at + 8u * DH), ha = ka >> 8, hb = kb >> 8;
                     float d[4] = {0.f, 0.f, 0.f, 0.f};
                     mma16816(d, ka & 0x000f000fu, kb & 0x000f000fu, ka & 0x00f000f0u, kb & 0x00f000f0u, qb[i][0][0], qb[i][0][1]);
                     mma16816(d, ha & 0x000f000fu, hb & 0x000f000fu, ha & 0x00f000f0u, hb & 0x00f000f0u, qb[i][1][0], qb[i][1][1]);
@@ -1143,8 +1164,8 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
             // minima of the values; a masked key takes no part, whatever its words hold
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint4 w = lds128(base + ks_at + 16u + 256u * i);
-                const uint32_t wv[4] = {w.x, w.y, w.z, w.w};
+                uint32_t wv[G];
+                words(base + ks_at + 4 * G + 8 * kWordRow * i, wv);
 #pragma unroll
                 for (int n = 0; n < G; ++n) {
                     const float2 v = __ffma2_rn(s[i], make_float2(high_half(wv[n]), high_half(wv[n])), accm[n]);
@@ -1164,14 +1185,13 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
                 p[2 * i] = low_half(hi) + low_half(lo);
                 p[2 * i + 1] = high_half(hi) + high_half(lo);
             }
-            uint32_t wv[4][4];
+            uint32_t wv[4][G];
             bool hid[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 hid[i] = !kAll && p[i] < 0.f;
                 p[i] *= kPScale;
-                const uint4 w = lds128(base + vs_at + 32u * (i & 1) + 256u * (i >> 1));
-                wv[i][0] = w.x; wv[i][1] = w.y; wv[i][2] = w.z; wv[i][3] = w.w;
+                words(base + vs_at + kWordRow * (i & 1) + 8 * kWordRow * (i >> 1), wv[i]);
             }
 #pragma unroll
             for (int n = 0; n < G; ++n) {
@@ -1181,7 +1201,7 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
                 for (int i = 0; i < 4; ++i) {
                     x[i] = p[i] * low_half(wv[i][n]);
                     if (!kAll) x[i] = hid[i] ? 0.f : x[i];
-                    c[i] = lds32(((base + v_at + (i & 1) * 144u) ^ (64u + 16u * n)) + 1024u * (i >> 1));
+                    c[i] = lds32(((base + v_at + (i & 1) * kNextRow) ^ (16u * (G + n))) + 8u * DH * (i >> 1));
                 }
                 split2(x[0], x[1], hi[0], lo[0]);
                 split2(x[2], x[3], hi[1], lo[1]);
@@ -1212,8 +1232,8 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
             if (i + 1 < rounds) positions(i + 1, next_pos);
             if (__all_sync(0xffffffffu, mbar_wait(&bar_full[st], static_cast<uint32_t>(i / kTokenStages) & 1u)) == 0) { ok = false; break; }
             if (i < mine) {
-                if (__all_sync(0xffffffffu, max(pos[0], pos[1]) <= qpos0)) reduce(std::true_type(), ring + st * kStageBytes, pos);
-                else reduce(std::false_type(), ring + st * kStageBytes, pos);
+                if (__all_sync(0xffffffffu, max(pos[0], pos[1]) <= qpos0)) reduce(std::true_type(), ring + st * kStage, pos);
+                else reduce(std::false_type(), ring + st * kStage, pos);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar_free[st]);
@@ -1409,19 +1429,19 @@ int launch_qt(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: query tile %d is not built", qt);
 }
 
-// the two kernels for bf16 at head size 128
-int launch_mma(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src, int cache_rows,
-                 const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
+// the kernels on the warp-level matrix units
+int launch_mma(dodo_ctx* ctx, int H, int dh, float sm_scale, int qt, const AttendGroup& g, const void* Q, const Q4Source& src, int cache_rows,
+               const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets, bool early, cudaStream_t st) {
     TokenMaps maps;
     memset(&maps, 0, sizeof maps);
     if (cache_rows > 0) {
-        int rc = dodo_encode_byte_rows(ctx, &maps.q4, src.q4, H * 128, cache_rows, 128, kRound);
-        if (rc == DODO_OK) rc = dodo_encode_byte_rows(ctx, &maps.scale, src.scale, H * 32, cache_rows, 32, kRound);
+        int rc = dodo_encode_byte_rows(ctx, &maps.q4, src.q4, H * dh, cache_rows, dh, kRound);
+        if (rc == DODO_OK) rc = dodo_encode_byte_rows(ctx, &maps.scale, src.scale, H * dh / 4, cache_rows, dh / 4, kRound);
         if (rc != DODO_OK) return rc;
     }
-    const size_t smem = static_cast<size_t>(kTokenStages) * kStageBytes + 1024;
-    auto kern = qt == 1 ? attend_q4_token_kernel : attend_q4_few_kernel;
-    bool& set = ctx->q4_attr_set[qt == 1 ? 0 : 1];
+    const size_t smem = static_cast<size_t>(kTokenStages) * stage_bytes(dh) + 1024;
+    auto kern = dh == 64 ? attend_q4_few_kernel<64> : qt == 1 ? attend_q4_token_kernel : attend_q4_few_kernel<128>;
+    bool& set = ctx->q4_attr_set[dh == 64 ? 2 : qt == 1 ? 0 : 1];
     if (!set) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "4-bit attend shared-memory attribute");
@@ -1429,7 +1449,7 @@ int launch_mma(dodo_ctx* ctx, int H, float sm_scale, int qt, const AttendGroup& 
     }
     return dodo_check_cuda(ctx, dodo_launch_dependent(kern, dim3(static_cast<unsigned>(g.cta0[g.nseq])), dim3(kTokenThreads), smem, st,
                                                       static_cast<const __nv_bfloat16*>(Q), maps, src, g, cache_pos, H, sm_scale * 1.4426950408889634f,
-                                                      dodo_attend_tile_keys(DODO_BF16, 128), static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
+                                                      dodo_attend_tile_keys(DODO_BF16, dh), static_cast<__nv_bfloat16*>(O), lse, partials, tickets, early ? 1 : 0, ctx->dev_status),
                            "4-bit attend launch");
 }
 
@@ -1441,10 +1461,10 @@ int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scal
                           float* partials, int* tickets, bool early_cache, cudaStream_t st) {
     if (g.cta0[g.nseq] == 0) return DODO_OK;
     const Q4Source src = {static_cast<const uint32_t*>(cache_q4), cache_scale, locK, locV};
-    if (dtype == DODO_BF16 && dh == 128)
-        return launch_mma(ctx, H, sm_scale, plan.qt, g, Q, src, cache_rows, cache_pos, O, lse, partials, tickets, early_cache, st);
+    if (dtype == DODO_BF16 && (dh == 128 || plan.qt > 1))
+        return launch_mma(ctx, H, dh, sm_scale, plan.qt, g, Q, src, cache_rows, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_BF16 && dh == 64)
-        return launch_qt<__nv_bfloat16, 64>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
+        return launch_t<__nv_bfloat16, 64, 1, 4>(ctx, H, sm_scale, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_F32 && dh == 128)
         return launch_qt<float, 128>(ctx, H, sm_scale, plan.qt, g, Q, src, cache_pos, O, lse, partials, tickets, early_cache, st);
     if (dtype == DODO_F32 && dh == 64)
@@ -1452,4 +1472,4 @@ int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scal
     return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "4-bit attend: dtype %d with head size %d", dtype, dh);
 }
 
-int dodo_attend_q4_tile_queries(int dtype, int dh, int max_tq) { return dtype == DODO_BF16 && dh == 128 && max_tq > 1 ? kFewQueries : 0; }
+int dodo_attend_q4_tile_queries(int dtype, int max_tq) { return dtype == DODO_BF16 && max_tq > 1 ? kFewQueries : 0; }

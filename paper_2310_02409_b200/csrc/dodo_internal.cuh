@@ -34,7 +34,7 @@ struct dodo_ctx {
     struct MapEntry { const void* base; int rows, width, box_rows, kind; CUtensorMap map; } map_cache[16];
     int map_next;               // round-robin replacement
     bool dense_attr_set[4];     // shared-memory attribute of the four forms of the tensor-core kernel
-    bool q4_attr_set[2];        // ... and of the 4-bit kernels on the warp-level matrix units
+    bool q4_attr_set[3];        // ... and of the 4-bit kernels on the warp-level matrix units
     bool backward_attr_set[4];  // ... and of the kernels of attend's gradient
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
@@ -261,7 +261,7 @@ int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendG
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
 // The streaming kernels over a 4-bit cache: launch as above, the cache (cache_rows rows) as codes and group words
 // queries per tile where the kernel of these types has only one choice, else 0
-int dodo_attend_q4_tile_queries(int dtype, int dh, int max_tq);
+int dodo_attend_q4_tile_queries(int dtype, int max_tq);
 int dodo_launch_attend_q4(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, const AttendPlan& plan,
                           const AttendGroup& g, const void* Q, const void* cache_q4, const uint32_t* cache_scale, int cache_rows,
                           const int32_t* cache_pos, const void* locK, const void* locV, void* O, float* lse,

@@ -241,6 +241,8 @@ SHAPES = [
     (BF, 3, 128, [9, 16, 5], [64, 1000, 0], [80, 16, 333]),
     (BF, 1, 128, [31], [2000], [31]),
     (BF, 2, 128, [17, 6], [0, 81], [17, 1000]),
+    (BF, 2, 64, [2, 3, 0, 8, 1], [700, 16, 33, 205, 1], [2, 40, 7, 64, 130]),
+    (BF, 3, 64, [9, 40, 5], [64, 1000, 0], [80, 40, 333]),
 ]
 
 
@@ -299,7 +301,7 @@ def test_attend_q4_visible_nan_shows(dodo, dtype, dh):
     assert bool(nan[32:64].all()) and not bool(nan[:32].any()) and not bool(nan[64:].any()) and bool(torch.isfinite(lse).all())
 
 
-@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 5), (BF, 128, 13), (BF, 64, 3), (F32, 64, 6)])
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 5), (BF, 128, 13), (BF, 64, 3), (BF, 64, 13), (F32, 64, 6)])
 def test_attend_q4_partly_visible_nan_token(dodo, dtype, dh, tq):
     """A local token, and a nugget, that only the later queries see hold NaN and infinities: earlier queries' outputs are untouched."""
     p = _problem(("q4part", dh, tq), dtype, 2, dh, [tq], [50], [tq + 3], slack=0)
@@ -321,7 +323,7 @@ def test_attend_q4_partly_visible_nan_token(dodo, dtype, dh, tq):
 
 
 # the token kernel carries codes as bf16 numbers far below 1 and weights times steps far above: both ends of its range
-@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (F32, 64, 1)])
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (BF, 64, 1), (BF, 64, 6), (F32, 64, 1)])
 @pytest.mark.parametrize("kstd,vstd", [(1.0, 1e13), (1.0, 1e-15), (1.0, 1e-20), (1e12, 1.0), (1e-12, 1.0), (1e18, 1e-10)])
 def test_attend_q4_range_of_values(dodo, dtype, dh, tq, kstd, vstd):
     p = _problem(("q4range", kstd, vstd, tq), dtype, 2, dh, [tq, tq], [300, 40], [1, 0], kstd=kstd, vstd=vstd)
