@@ -394,7 +394,8 @@ DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32
 
 /*
  * dodo_attend over a 4-bit nugget cache (local tokens, queries and outputs in `dtype`): the keys and values of cached
- * rows are those that the codes stand for, fp32 arithmetic, one rounding of O.  A block of queries whose longest part has
+ * rows are those that the codes stand for; fp32 sums, the products of weights and steps kept to 16 bits or more, one
+ * rounding of O.  A block of queries whose longest part has
  * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale > 0) runs on the tensor cores when the
  * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
  * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
