@@ -539,7 +539,10 @@ backward_dense_kernel(const __grid_constant__ BackwardMaps maps, const __grid_co
                     const float4* nd = nl + 16;
                     const int first = (u.t0 + j) * BN, rows = min(BN, sq.tq - first), q0 = sq.q_pos0 + first;
                     const bool test = edge > q0 || rows < BN;
-                    const int c_lo = my_pos - q0 - half * 32, c_hi = rows - half * 32;
+                    // the row's key is seen from column my_pos - q0 on; that difference may need 33 bits (a nugget's position is any
+                    // number), so the comparison comes first and 0 to BN is what is left of it
+                    const int from = my_pos <= q0 ? 0 : static_cast<int>(min(static_cast<unsigned>(my_pos) - static_cast<unsigned>(q0), static_cast<unsigned>(BN)));
+                    const int c_lo = from - half * 32, c_hi = rows - half * 32;
                     if (rows < BN) {   // rows behind the sequence's queries must not reach the products (both score products done with them)
                         if (!warp_wait(&sy.t[b], buf.phase())) { ok = false; break; }
                         unsigned char* y = smem + shared_int(sy.y_slot[e]) * kSlotBytes;

@@ -430,3 +430,25 @@ def test_backward_binding_refuses_wrong_tensors(dodo):
     with pytest.raises(api.DodoError) as e:
         dodo.attend_backward(**{**base, "workspace": ws[:-16]})
     assert e.value.status == api.ERR_CAPACITY
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 2), (F32, 128, 7), (F32, 128, 20), (BF, 128, 3), (BF, 64, 7), (BF, 64, 70), (BF, 128, 40), (BF, 128, 130)])
+def test_gradient_with_positions_at_the_ends_of_their_range(dodo, dtype, dh, tq):
+    """cache_pos may hold anything: nuggets at -2^31 (always seen) and 2^31 - 1 (never) among ordinary ones, for queries at positive and
+    negative positions and at both ends of what a query may have."""
+    q_pos0 = [100, -40, -2 ** 30, 2 ** 30 - tq]
+    p = problem(("bwdends", dh, tq), dtype, 2, dh, [tq] * 4, [150] * 4, [tq + 2] * 4)
+    p["q_pos0"] = np.asarray(q_pos0, np.int32)
+    p["loc_pos0"] = np.asarray([100, -60, -2 ** 30, 2 ** 30 - tq - 2], np.int32)     # some or all of the local tokens are seen
+    ends = np.array([-2 ** 31, -2 ** 31 + 1, -2 ** 30 - 1, -2 ** 30, 2 ** 30 - 1, 2 ** 30, 2 ** 31 - 2, 2 ** 31 - 1], np.int64)
+    for b, q0 in enumerate(q_pos0):
+        c0 = int(p["cache_off"][b])
+        near = np.clip(q0 + np.arange(150) - 50, -2 ** 31, 2 ** 31 - 1)              # before, among and behind the queries
+        near[::5] = np.tile(ends, 4)[:30]
+        near[64:96] = np.tile(ends, 4)                                               # (all rows of a warp)
+        p["cpos"][c0:c0 + 150] = near
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    assert dodo.device_status() == 0
+    check(p, d, out, dense=dtype == BF and tq > 4)
