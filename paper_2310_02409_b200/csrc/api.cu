@@ -603,6 +603,24 @@ int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_
     return DODO_OK;
 }
 
+// A streaming launch may read cache rows ahead of its dependency wait only when nothing this context
+// launched since its last attend has written a cache -- and, under stream capture, only when that attend
+// belongs to the same capture: a graph must not bake in what happened to precede its recording.
+unsigned long long dodo_capture_id(cudaStream_t st) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo(st, &status, &id) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return status == cudaStreamCaptureStatusActive ? id : 0;
+}
+bool dodo_cache_settled(const dodo_ctx* ctx, unsigned long long capture) { return ctx->cache_clean && ctx->clean_capture_id == capture; }
+void dodo_attend_launched(dodo_ctx* ctx, unsigned long long capture) {   // an attend never writes a cache
+    ctx->cache_clean = true;
+    ctx->clean_capture_id = capture;
+}
+
 // A call's work is launched on the caller's current device, so that has to be the context's.
 int dodo_check_device(dodo_ctx* ctx) {
     int dev = -1;
@@ -678,27 +696,16 @@ int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_
         else if (tot.tick_rows > DODO_NUM_TICKETS)
             rc = dodo_fail(ctx, DODO_ERR_CAPACITY, "too many split units (%lld)", static_cast<long long>(tot.tick_rows));
     }
-    // A streaming launch may read cache rows ahead of its dependency wait only when nothing this context
-    // launched since its last attend has written a cache -- and, under stream capture, only when that attend
-    // belongs to the same capture: a graph must not bake in what happened to precede its recording.
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaStreamCaptureStatus cap_status = cudaStreamCaptureStatusNone;
-    unsigned long long cap_id = 0;
-    if (cudaStreamGetCaptureInfo(st, &cap_status, &cap_id) != cudaSuccess) {
-        (void)cudaGetLastError();
-        cap_status = cudaStreamCaptureStatusNone;
-    }
-    if (cap_status != cudaStreamCaptureStatusActive) cap_id = 0;
+    const unsigned long long capture = dodo_capture_id(st);
     for (int gi = 0; gi < ngroups && rc == DODO_OK; ++gi) {
-        const bool early = ctx->cache_clean && ctx->clean_capture_id == cap_id;
+        if (groups[gi].cta0[groups[gi].nseq] == 0) continue;      // no query in it, nothing launched: it settles nothing
+        const bool early = dodo_cache_settled(ctx, capture);
         rc = dense ? dodo_launch_attend_dense(ctx, H, sm_scale, groups[gi], dmaps, cache_pos, O, lse, workspace, workspace_bytes,
                                               ctx->tickets, ctx->dev_status, nullptr, st)
                    : dodo_launch_attend(ctx, dtype, H, dh, sm_scale, plan, groups[gi], Q, maps, cache_pos, O, lse,
                                         static_cast<float*>(workspace), ctx->tickets, early, st);
-        if (rc == DODO_OK) {   // an attend never writes a cache
-            ctx->cache_clean = true;
-            ctx->clean_capture_id = cap_id;
-        }
+        if (rc == DODO_OK) dodo_attend_launched(ctx, capture);
     }
     if (groups != &one) free(groups);
     return rc;

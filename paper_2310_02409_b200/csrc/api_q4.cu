@@ -154,22 +154,13 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
         rc = dodo_fail(ctx, DODO_ERR_CAPACITY, "workspace of %zu bytes is too small or misaligned (need %zu)", workspace_bytes, need);
     else if (tot.tick_rows > DODO_NUM_TICKETS)
         rc = dodo_fail(ctx, DODO_ERR_CAPACITY, "too many split units (%lld)", static_cast<long long>(tot.tick_rows));
-    // cache rows ahead of the dependency wait: the rule of dodo_attend
-    cudaStreamCaptureStatus cap_status = cudaStreamCaptureStatusNone;
-    unsigned long long cap_id = 0;
-    if (cudaStreamGetCaptureInfo(st, &cap_status, &cap_id) != cudaSuccess) {
-        (void)cudaGetLastError();
-        cap_status = cudaStreamCaptureStatusNone;
-    }
-    if (cap_status != cudaStreamCaptureStatusActive) cap_id = 0;
+    const unsigned long long capture = dodo_capture_id(st);
     for (int gi = 0; gi < ngroups && rc == DODO_OK; ++gi) {
-        const bool early = ctx->cache_clean && ctx->clean_capture_id == cap_id;
+        if (groups[gi].cta0[groups[gi].nseq] == 0) continue;      // no query in it, nothing launched: it settles nothing
+        const bool early = dodo_cache_settled(ctx, capture);
         rc = dodo_launch_attend_q4(ctx, dtype, H, dh, sm_scale, plan, groups[gi], Q, cache_q4, cache_scale, cache_rows, cache_pos, locK, locV, O, lse,
                                    static_cast<float*>(workspace), ctx->tickets, early, st);
-        if (rc == DODO_OK) {
-            ctx->cache_clean = true;
-            ctx->clean_capture_id = cap_id;
-        }
+        if (rc == DODO_OK) dodo_attend_launched(ctx, capture);
     }
     if (groups != &one) free(groups);
     return rc;

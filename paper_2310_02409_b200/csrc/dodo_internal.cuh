@@ -175,6 +175,11 @@ int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_
 // that positions of queries and local tokens leave room for differences and for "never seen" (2^31 - 1)
 int dodo_check_positions(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, const int32_t* loc_len, const int32_t* loc_pos0, int B);
 int dodo_check_device(dodo_ctx* ctx);
+// Whether a streaming attend may read cache rows ahead of its dependency wait (see dodo_attend in dodo.h).  The launches of a call
+// ask for it one by one, and report themselves only when a kernel was launched: that kernel's wait is what settles an append.
+unsigned long long dodo_capture_id(cudaStream_t st);     // 0: not capturing
+bool dodo_cache_settled(const dodo_ctx* ctx, unsigned long long capture);
+void dodo_attend_launched(dodo_ctx* ctx, unsigned long long capture);
 
 struct AttendSeq {
     int q_row0;     // first query row

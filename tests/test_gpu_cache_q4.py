@@ -541,3 +541,54 @@ def test_q4_binding_refuses_wrong_tensors(dodo):
     with pytest.raises(api.DodoError) as e:
         dodo.gather_kv_q4(**args(cache_len=np.full(1, 4, np.int32)))
     assert e.value.status == api.ERR_CAPACITY
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 3), (BF, 64, 1), (F32, 128, 1)])
+def test_attend_right_behind_an_append_when_the_first_sequences_are_idle(dodo, dtype, dh, tq, four_bits):
+    """70 sequences, the first 64 of them (a whole launch group) without queries this step: the others' attention waits for the append."""
+    H, B, idle, rows_of = 8, 70, 64, 500
+    ks = [8] * idle + [rows_of] * (B - idle)
+    off = inputs.offsets(ks)
+    rows = int(off[-1])
+    K, V = (inputs.randn((rows, H, dh), "q4idle", k, dtype=dtype).cuda() for k in "KV")
+    Q = inputs.randn((tq * (B - idle), H, dh), "q4idle", "Q", dtype=dtype).cuda()
+    idx = _cuda(np.concatenate([np.arange(k, dtype=np.int32) for k in ks]))
+    q_off = np.concatenate([np.zeros(idle, np.int32), tq * np.arange(B - idle + 1)]).astype(np.int32)
+    q_pos0, pos_base = np.full(B, 10_000, np.int32), np.zeros(B, np.int32)
+    q4, sc, pos = _cache(rows, H, dh)
+    cK, cV = torch.empty_like(K), torch.empty_like(V)
+    ws = torch.empty(dodo.attend_q4_workspace_bytes(H, dh, rows), dtype=torch.uint8, device="cuda")
+    full = np.asarray(ks, np.int32)
+
+    def append():
+        clen = np.zeros(B, np.int32)
+        if four_bits:
+            dodo.gather_kv_q4(K, V, off, idx, off, pos_base, q4, sc, pos, off, clen)
+        else:
+            dodo.gather_kv(K, V, off, idx, off, pos_base, cK, cV, pos, off, clen)
+
+    def attend():
+        O = torch.full_like(Q, float("nan"))
+        torch.cuda.synchronize()
+
+        def call():
+            args = (q4, sc) if four_bits else (cK, cV)
+            fn = dodo.attend_q4 if four_bits else dodo.attend
+            fn(Q, q_off, q_pos0, dh ** -0.5, *args, pos, off, full, None, None, None, None, None, O, None, ws)
+        return O, call
+
+    append()
+    torch.cuda.synchronize()
+    want, call = attend()
+    call()
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(want.float()).all())
+    for _ in range(10):
+        for t in (q4, sc, pos, cK, cV):
+            t.zero_()
+        O, call = attend()
+        append()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(O, want)
