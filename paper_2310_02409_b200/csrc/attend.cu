@@ -79,7 +79,7 @@ attend_kernel(const T* __restrict__ Q, const AttendMaps src, const __grid_consta
     const int q_first = qtile * QT;
     const int nq = min(QT, sq.tq - q_first);
     // local rows that at least one query of the tile can see
-    const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q_first + nq - 1 - sq.l_pos0 + 1));
+    const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + q_first + nq - 1);
     // this chunk's slice of the key list [nuggets ; local], in granules of TK keys per segment
     const int nt_c = (sq.c_len + TK - 1) / TK;
     const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;

@@ -544,7 +544,7 @@ backward_tile_kernel(const BackwardArrays a, const __grid_constant__ BackwardGro
     const int chunk = r % sq.nchunk; r /= sq.nchunk;
     const int h = r % H, qt = r / H;
     const int q0 = qt * TQ, nq = min(TQ, sq.tq - q0);
-    const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q0 + nq - sq.l_pos0));
+    const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + q0 + nq - 1);
     const int nt_c = (sq.c_len + TK - 1) / TK, nt = nt_c + (l_vis + TK - 1) / TK;
     const int t0 = min(nt, chunk * sq.ctiles), t1 = min(nt, t0 + sq.ctiles);
     {

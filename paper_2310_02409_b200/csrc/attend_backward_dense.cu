@@ -180,7 +180,7 @@ __device__ __forceinline__ Unit unit_of(const BackwardGroup& g, int H, int id) {
         u.first = u.qt * BM;
         u.rows = min(BM, sq.tq - u.first);
         u.row0 = sq.q_row0 + u.first;
-        u.l_vis = max(0, min(sq.l_len, sq.q_pos0 + u.first + u.rows - sq.l_pos0));
+        u.l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + u.first + u.rows - 1);
         u.nt_c = (sq.c_len + BN - 1) / BN;
         const int nt = u.nt_c + (u.l_vis + BN - 1) / BN;
         u.t0 = min(nt, u.chunk * sq.ctiles);

@@ -101,7 +101,7 @@ struct Unit {
 };
 __device__ __forceinline__ void unit_shape(const AttendSeq& sq, Unit& u) {
     const int q_first = u.qt * BM, nq = min(BM, sq.tq - q_first);
-    u.l_vis = max(0, min(sq.l_len, sq.q_pos0 + q_first + nq - 1 - sq.l_pos0 + 1));
+    u.l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + q_first + nq - 1);
     u.nt_c = (sq.c_len + BN - 1) / BN;
     u.n = u.nt_c + (u.l_vis + BN - 1) / BN;
     u.ne = max(1, u.n);
@@ -691,9 +691,7 @@ int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendG
     // `in step` counts every (sequence, head) once, by its last query tile
     auto unit_tiles = [](const AttendSeq& sq, int qt) {
         const int q_first = qt * BM, nq = sq.tq - q_first < BM ? sq.tq - q_first : BM;
-        int l_vis = sq.q_pos0 + q_first + nq - 1 - sq.l_pos0 + 1;
-        l_vis = l_vis < sq.l_len ? l_vis : sq.l_len;
-        l_vis = l_vis > 0 ? l_vis : 0;
+        const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + q_first + nq - 1);
         return (sq.c_len + BN - 1) / BN + (l_vis + BN - 1) / BN;
     };
     long long total = 0, total_step = 0;

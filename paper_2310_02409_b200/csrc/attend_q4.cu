@@ -153,7 +153,7 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
     const int qtile = r0 / H;
     const int q_first = qtile * QT;
     const int nq = min(QT, sq.tq - q_first);
-    const int l_vis = max(0, min(sq.l_len, sq.q_pos0 + q_first + nq - 1 - sq.l_pos0 + 1));
+    const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, sq.q_pos0 + q_first + nq - 1);
     // this chunk's slice of the key list [nuggets ; local], in granules of TK keys per segment
     const int nt_c = (sq.c_len + TK - 1) / TK;
     const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
@@ -572,7 +572,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     const int r0 = bid - g.cta0[b];
     const int nchunk = sq.nchunk, chunk = r0 % nchunk, h = r0 / nchunk;    // one query: H units of nchunk blocks
     const int qpos = sq.q_pos0;
-    const int l_vis = max(0, min(sq.l_len, qpos - sq.l_pos0 + 1));
+    const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, qpos);
     const int nt_c = (sq.c_len + TK - 1) / TK;                             // planning tiles of TK keys
     const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
     const int c_begin = min(sq.c_len, t_begin * TK), c_end = min(sq.c_len, t_end * TK);
@@ -992,7 +992,7 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
     const int h = r0 % H, qtile = r0 / H;
     const int q_first = qtile * kFewQueries, nq = min(kFewQueries, sq.tq - q_first);
     const int qpos0 = sq.q_pos0 + q_first;
-    const int l_vis = max(0, min(sq.l_len, qpos0 + nq - sq.l_pos0));
+    const int l_vis = dodo_visible_local(sq.l_len, sq.l_pos0, qpos0 + nq - 1);
     const int nt_c = (sq.c_len + TK - 1) / TK;                             // planning tiles of TK keys
     const int t_begin = chunk * sq.ctiles, t_end = t_begin + sq.ctiles;
     const int c_begin = min(sq.c_len, t_begin * TK), c_end = min(sq.c_len, t_end * TK);

@@ -172,7 +172,7 @@ int dodo_launch_expand_q4(dodo_ctx* ctx, const void* cache_q4, const uint32_t* c
 int dodo_check_attend_queries(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, int dtype, int H, int dh, int B);
 int dodo_check_attend_keys(dodo_ctx* ctx, const int32_t* cache_off, const int32_t* cache_len, const int32_t* loc_off,
                            const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, bool* any_cache, bool* any_local);
-// that positions of queries and local tokens leave room for differences and for "never seen" (2^31 - 1)
+// that positions of queries and local tokens lie in [-2^30, 2^30): differences of theirs fit 32 bits, counts of rows need dodo_visible_local
 int dodo_check_positions(dodo_ctx* ctx, const int32_t* q_off, const int32_t* q_pos0, const int32_t* loc_len, const int32_t* loc_pos0, int B);
 int dodo_check_device(dodo_ctx* ctx);
 // Whether a streaming attend may read cache rows ahead of its dependency wait (see dodo_attend in dodo.h).  The launches of a call
@@ -225,6 +225,12 @@ int dodo_launch_attend(dodo_ctx* ctx, int dtype, int H, int dh, float sm_scale, 
                        const AttendGroup& g, const void* Q, const AttendMaps& maps,
                        const int32_t* cache_pos, void* O, float* lse, float* partials, int* tickets,
                        bool early_cache, cudaStream_t st);
+// How many of l_len local rows, the first at position l_pos0, a query at position `last` sees.  In 64 bits: the last query at 2^30 - 1
+// over rows from -2^30 on sees 2^31 positions, one more than an int counts.
+__host__ __device__ static inline int dodo_visible_local(int l_len, int l_pos0, int last) {
+    const long long n = static_cast<long long>(last) - l_pos0 + 1;
+    return n <= 0 ? 0 : n < l_len ? static_cast<int>(n) : l_len;
+}
 // Host view of one dodo_attend call (the caller's tables, unchanged).
 struct AttendShape {
     const int32_t *q_off, *q_pos0, *cache_off, *cache_len, *loc_off, *loc_len, *loc_pos0;

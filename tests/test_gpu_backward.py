@@ -452,3 +452,28 @@ def test_gradient_with_positions_at_the_ends_of_their_range(dodo, dtype, dh, tq)
     torch.cuda.synchronize()
     assert dodo.device_status() == 0
     check(p, d, out, dense=dtype == BF and tq > 4)
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(F32, 64, 3), (F32, 128, 20), (BF, 128, 3), (BF, 64, 70), (BF, 128, 40), (BF, 128, 300)])
+def test_attend_and_gradient_between_the_ends_of_the_positions(dodo, dtype, dh, tq):
+    """The last query at 2^30 - 1 over local tokens from -2^30 on sees them all (positions 2^31 apart, counted), and queries from -2^30
+    on none of those that end at 2^30."""
+    p = problem(("bwdcorner", dh, tq), dtype, 2, dh, [tq] * 3, [30, 30, 0], [70] * 3)
+    p["q_pos0"] = np.asarray([2 ** 30 - tq, -2 ** 30, 2 ** 30 - tq], np.int32)
+    p["loc_pos0"] = np.asarray([-2 ** 30, 2 ** 30 - 70, -2 ** 30], np.int32)
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    assert dodo.device_status() == 0
+    seen = torch.isfinite(d["lse"]).all(1)
+    assert bool(seen[:tq].all()) and not bool(seen[tq:2 * tq].any()) and bool(seen[2 * tq:].all())
+    # the forward's log-sum-exp: the error of an fp32 logit, of the exponentials and of the sum of a hundred of them
+    Q, lK, cK, lse = _f64(p["Q"]), _f64(p["lK"]), _f64(p["cK"]), _f64(d["lse"])
+    for b in (0, 2):
+        l = slice(int(p["loc_off"][b]), int(p["loc_off"][b]) + 70)
+        c = slice(int(p["cache_off"][b]), int(p["cache_off"][b]) + int(p["clen"][b]))
+        q = Q[b * tq:(b + 1) * tq]
+        k = np.concatenate([cK[c], lK[l]])
+        want = plain64.attend(q, np.zeros(tq), p["scale"], k, k, np.zeros(len(k)))[1]
+        assert np.all(np.abs(lse[b * tq:(b + 1) * tq] - want) <= plain64.logit_bound(q, k, p["scale"], dh) + 2.0 ** -20 + 100 * 2.0 ** -24 + 2.0 ** -22 * np.abs(want))
+    check(p, d, out, dense=dtype == BF and tq > 4)

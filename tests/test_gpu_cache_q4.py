@@ -592,3 +592,16 @@ def test_attend_right_behind_an_append_when_the_first_sequences_are_idle(dodo, d
         call()
         torch.cuda.synchronize()
         assert torch.equal(O, want)
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (BF, 64, 1), (BF, 64, 5), (F32, 64, 1), (F32, 128, 3), (BF, 128, 40)])
+def test_attend_q4_between_the_ends_of_the_positions(dodo, dtype, dh, tq):
+    """The last query at 2^30 - 1 over local tokens from -2^30 on sees them all (their number behind the first is 2^31), and queries
+    from -2^30 on none of those that end at 2^30."""
+    p = _problem(("q4corner", tq), dtype, 2, dh, [tq, tq, tq], [30, 30, 0], [70, 70, 70])
+    p["q_pos0"] = np.asarray([2 ** 30 - tq, -2 ** 30, 2 ** 30 - tq], np.int32)
+    p["loc_pos0"] = np.asarray([-2 ** 30, 2 ** 30 - 70, -2 ** 30], np.int32)
+    O, lse = _run_q4(dodo, p)
+    _check(p, O, lse, rounded=tq >= 32)
+    assert bool(torch.isneginf(lse[tq:2 * tq]).all()) and bool(torch.isfinite(lse[2 * tq:]).all())
+    assert dodo.device_status() == 0
