@@ -482,6 +482,7 @@ attend_q4_kernel(const T* __restrict__ Q, const Q4Source src, const __grid_const
 // rows: 25.4 against 28.4 us).  What bounds it is instruction issue next to HBM: the same kernel without the arithmetic takes 20 us
 // for 16,384 rows of 40 heads (5.4 TB/s) where this takes 25.
 constexpr int kQExp = 64;        // the query is shifted to a largest feature near 2^64
+constexpr int kMostExp = 57;     // ... where that feature is below 2^58: what undoes the shift, 2^(133 - 64 + 57), is near the largest power there is
 constexpr int kPExp = 72;        // power of two on p s, p below 2^8: fits for steps below 2^47, products are normal numbers down to p s of 2^-65
 
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -492,6 +493,10 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+
+// exponent of a number, and a power of two put together bit by bit (both for normal numbers)
+__device__ __forceinline__ int exponent_of(float x) { return static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 __device__ __forceinline__ uint2 lds64(uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; }
@@ -553,6 +558,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     constexpr int DH = 128, RED = DH + 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ float red[2 * kTokenWarps][RED];                 // a warp's cached keys, its local keys
+    __shared__ float up[kTokenWarps];                           // a huge query's power of two
     __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
     __shared__ int s_flag;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -624,19 +630,30 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
     const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0) * H + h) * DH;
     uint32_t qb[4][2][2];
     float qsum[2], q_back;      // sums of q over groups 2 (t & 1) + {0, 1}, lanes t < 2; what undoes the shifts, with the softmax scale
+    bool huge;                  // ... but for a query beyond 2^58, which leaves a power of two to its logits
     {
         float f[32], top = 0.f, mine = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 32 * t + 8 * i), f + 8 * i);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { top = fmaxf(top, fabsf(f[i])); mine += f[i]; }
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(f[i]));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // exponent of the largest feature, as powers of two put together bit by bit; a query outside 2^-62 .. 2^57 is shifted less
-        // or more, so that both powers stay normal numbers (its products still fit: codes end at 15, q at 2^128 2^7)
-        const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62), 57);
-        const float shift = __uint_as_float(static_cast<uint32_t>(kQExp - e + 127) << 23);
-        q_back = __uint_as_float(static_cast<uint32_t>(133 - kQExp + e + 127) << 23) * scale_log2;
+        // exponent of the largest feature, as powers of two put together bit by bit; a query below 2^-62 is shifted less, so that both
+        // powers stay normal numbers
+        int e = max(exponent_of(top), -62);
+        huge = e > kMostExp;
+        if (huge) {
+            const float down = power_of_two(kMostExp - e);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] *= down;
+            up[warp] = power_of_two(e - kMostExp);     // (all lanes the same)
+            e = kMostExp;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mine += f[i];
+        const float shift = power_of_two(kQExp - e);
+        q_back = power_of_two(133 - kQExp + e) * scale_log2;
         const float at0 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2), at1 = __shfl_sync(0xffffffffu, mine, (t & 1) * 2 + 1);
         qsum[0] = t < 2 ? at0 * scale_log2 : 0.f;
         qsum[1] = t < 2 ? at1 * scale_log2 : 0.f;
@@ -699,6 +716,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 s[n][i] = __shfl_sync(0xffffffffu, s[n][i], lane & ~3);
+                if (huge) s[n][i] *= up[warp];
                 if (!kAll) s[n][i] = pos[n][i] <= qpos ? s[n][i] : kNeg;
                 top = fmaxf(top, s[n][i]);
             }
@@ -970,6 +988,7 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
     constexpr uint32_t kWordRow = DH / 4, kCodes = code_bytes(DH), kStage = stage_bytes(DH);
     extern __shared__ unsigned char smem_raw[];
     __shared__ float red[kTokenWarps][kFewQueries][RED];
+    __shared__ float2 up[kTokenWarps][kFewQueries / 2];         // huge queries' powers of two
     __shared__ __align__(8) uint64_t bar_full[kTokenStages], bar_free[kTokenStages];
     __shared__ int s_flag;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -1046,30 +1065,47 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
         const __nv_bfloat16* const qrow = Q + (static_cast<size_t>(sq.q_row0 + q_first + min(r, nq - 1)) * H + h) * DH + 8 * t;
         uint32_t qb[G][2][2];
         float2 qsum[G], q_back;                 // of queries 2 t, 2 t + 1
+        bool huge;                              // one of the tile's queries leaves a power of two to its logits
         {
             float f[G][8], top = 0.f, sum[G];
 #pragma unroll
             for (int i = 0; i < G; ++i) {
                 Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(qrow + 32 * i), f[i]);
-                sum[i] = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (r >= nq) f[i][e] = 0.f;
                     top = fmaxf(top, fabsf(f[i][e]));
-                    sum[i] += f[i][e];
                 }
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // (shifts as in the kernel above, a query's own)
+            int e = max(exponent_of(top), -62);
+            huge = __any_sync(0xffffffffu, e > kMostExp) != 0;
+            if (huge) {
+                const int over = max(e - kMostExp, 0);
+                const float down = power_of_two(-over);
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) f[i][n] *= down;
+                reinterpret_cast<float*>(up[warp])[r] = power_of_two(over);      // (a quad's lanes the same)
+                e -= over;
+                __syncwarp();
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                sum[i] = 0.f;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) sum[i] += f[i][n];
                 sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
                 sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
                 sum[i] *= scale_log2;
                 qsum[i].x = __shfl_sync(0xffffffffu, sum[i], 8 * t);
                 qsum[i].y = __shfl_sync(0xffffffffu, sum[i], 8 * t + 4);
             }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // (shifts as in the kernel above, a query's own)
-            const int e = min(max(static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127, -62), 57);
-            const float shift = __uint_as_float(static_cast<uint32_t>(kQExp - e + 127) << 23), s16 = shift * 0.0625f;
-            const float back = __uint_as_float(static_cast<uint32_t>(133 - kQExp + e + 127) << 23) * scale_log2;
+            const float shift = power_of_two(kQExp - e), s16 = shift * 0.0625f;
+            const float back = power_of_two(133 - kQExp + e) * scale_log2;
             q_back.x = __shfl_sync(0xffffffffu, back, 8 * t);
             q_back.y = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
@@ -1159,6 +1195,11 @@ attend_q4_few_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constant_
                     s[0] = __ffma2_rn(qsum[i], make_float2(high_half(wa[i]), high_half(wa[i])), s[0]);
                     s[1] = __ffma2_rn(qsum[i], make_float2(high_half(wb[i]), high_half(wb[i])), s[1]);
                 }
+            }
+            if (huge) {
+                const float2 f = up[warp][t];
+                s[0] = __fmul2_rn(s[0], f);
+                s[1] = __fmul2_rn(s[1], f);
             }
             weigh(all_seen, s, see);
             // minima of the values; a masked key takes no part, whatever its words hold

@@ -605,3 +605,16 @@ def test_attend_q4_between_the_ends_of_the_positions(dodo, dtype, dh, tq):
     _check(p, O, lse, rounded=tq >= 32)
     assert bool(torch.isneginf(lse[tq:2 * tq]).all()) and bool(torch.isfinite(lse[2 * tq:]).all())
     assert dodo.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype,dh,tq", [(BF, 128, 1), (BF, 128, 5), (BF, 64, 1), (BF, 64, 6), (F32, 128, 2)])
+@pytest.mark.parametrize("power", [-110, 60, 118, 121])
+def test_attend_q4_range_of_queries(dodo, dtype, dh, tq, power):
+    """Queries times 2^power with the softmax's scale times 2^-power have the same logits, to the bit."""
+    p = _problem(("q4qrange", tq), dtype, 2, dh, [tq, tq], [300, 40], [tq, tq + 9], kstd=0.25)
+    O, lse = _run_q4(dodo, p)
+    _check(p, O, lse)
+    q = dict(p, Q=(p["Q"].float() * 2.0 ** power).to(dtype), scale=p["scale"] * 2.0 ** -power)
+    assert bool(torch.isfinite(q["Q"].float()).all()) and torch.equal((q["Q"].double() * 2.0 ** -power).to(dtype), p["Q"])
+    O2, lse2 = _run_q4(dodo, q)
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
