@@ -140,6 +140,27 @@ def _entries(table: bytes | None, sequences: int, what: str):
         raise ValueError(f"{what} must have {sequences} entries")
 
 
+def _cache_tables(off: bytes | None, length: bytes | None, sequences: int, rows: int | None):
+    """Checks an attention call's cache tables; rows None: there is no cache tensor, but the library reads tables that it is given."""
+    if rows is not None:
+        _bound(off, sequences, rows, "cache_off")
+    elif length is None:
+        return
+    elif off is None or len(off) != 4 * (sequences + 1):
+        raise ValueError(f"cache_off must have {sequences + 1} entries")
+    _entries(length, sequences, "cache_len")
+
+
+def _local_tables(off: bytes | None, length: bytes | None, pos0: bytes | None, sequences: int, given: bool):
+    """Checks an attention call's tables of local tokens; given: there are tensors beside them."""
+    if length is None and not given:
+        return
+    _entries(length, sequences, "loc_len")
+    for table, what in ((off, "loc_off"), (pos0, "loc_pos0")):
+        if given or table is not None:
+            _entries(table, sequences, what)
+
+
 def _host_i32(a) -> np.ndarray | None:
     if a is None:
         return None
@@ -384,7 +405,7 @@ class Dodo:
         n, ptr = rows_q * row, self._ptr
         q, o, g, dq = ptr(Q, dt, n, "Q"), ptr(O, dt, n, "O"), ptr(dO, dt, n, "dO"), ptr(dQ, dt, n, "dQ")
         ls = ptr(lse, torch.float32, rows_q * H, "lse")
-        ck = cv = dk = dv = pos = ds = None
+        ck = cv = dk = dv = pos = ds = rows = None
         if cacheK is not None:
             rows = self._heads(cacheK, "cacheK")[0]
             n = rows * row
@@ -395,8 +416,7 @@ class Dodo:
             if dscore is not None:
                 ds = ptr(dscore, torch.float32, None, "dscore")
                 rows = min(rows, dscore.numel())
-            _bound(co, B, rows, "cache_off")
-            _entries(cl, B, "cache_len")
+        _cache_tables(co, cl, B, rows)
         lk = lv = dlk = dlv = None
         loc_rows = 0
         if locK is not None:
@@ -404,9 +424,7 @@ class Dodo:
             n = loc_rows * row
             lk, lv = ptr(locK, dt, n, "locK"), ptr(locV, dt, n, "locV")
             dlk, dlv = ptr(dlocK, dt, n, "dlocK"), ptr(dlocV, dt, n, "dlocV")
-            _entries(lo, B, "loc_off")
-            _entries(ll, B, "loc_len")
-            _entries(lp, B, "loc_pos0")
+        _local_tables(lo, ll, lp, B, locK is not None)
         w, ws_bytes = self._workspace(workspace)
         self._check(self._lib.dodo_attend_backward(
             self._ctx, q, qo, qp, code, H, dh, sm_scale, ck, cv, pos, co, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls, g, dq, dk, dv,
@@ -460,19 +478,17 @@ class Dodo:
         _entries(qp, B, "q_pos0")
         q, o = ptr(Q, dt, None, "Q"), ptr(O, dt, Q.numel(), "O")
         ls = None if lse is None else ptr(lse, torch.float32, rows_q * H, "lse")
-        q4 = sc = pos = lk = lv = None
+        q4 = sc = pos = lk = lv = rows = None
         if cache_q4 is not None:
             rows, q4, sc = self._q4_cache(cache_q4, cache_scale, H, dh)
             pos = ptr(cache_pos, torch.int32, None, "cache_pos")
-            _bound(co, B, min(rows, cache_pos.numel()), "cache_off")
-            _entries(cl, B, "cache_len")
+            rows = min(rows, cache_pos.numel())
+        _cache_tables(co, cl, B, rows)
         loc_rows = 0
         if locK is not None:
             loc_rows = self._heads(locK, "locK")[0]
             lk, lv = ptr(locK, dt, loc_rows * H * dh, "locK"), ptr(locV, dt, loc_rows * H * dh, "locV")
-            _entries(lo, B, "loc_off")
-            _entries(ll, B, "loc_len")
-            _entries(lp, B, "loc_pos0")
+        _local_tables(lo, ll, lp, B, locK is not None)
         w, ws_bytes = self._workspace(workspace)
         self._check(self._lib.dodo_attend_q4(self._ctx, q, qo, qp, code, H, dh, sm_scale, q4, sc, pos, co, cl, lk, lv, lo, ll, lp, loc_rows,
                                              B, o, ls, w, ws_bytes, _stream()))
