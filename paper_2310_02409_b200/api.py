@@ -427,7 +427,7 @@ class Dodo:
         _local_tables(lo, ll, lp, B, locK is not None)
         w, ws_bytes = self._workspace(workspace)
         self._check(self._lib.dodo_attend_backward(
-            self._ctx, q, qo, qp, code, H, dh, float(sm_scale), ck, cv, pos, co, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls, g, dq, dk, dv,
+            self._ctx, q, qo, qp, code, H, dh, sm_scale, ck, cv, pos, co, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls, g, dq, dk, dv,
             dlk, dlv, ds, w, ws_bytes, _stream()))
 
     # -- the 4-bit nugget cache ----------------------------------------------------------------------
@@ -490,7 +490,7 @@ class Dodo:
             lk, lv = ptr(locK, dt, loc_rows * H * dh, "locK"), ptr(locV, dt, loc_rows * H * dh, "locV")
         _local_tables(lo, ll, lp, B, locK is not None)
         w, ws_bytes = self._workspace(workspace)
-        self._check(self._lib.dodo_attend_q4(self._ctx, q, qo, qp, code, H, dh, float(sm_scale), q4, sc, pos, co, cl, lk, lv, lo, ll, lp, loc_rows,
+        self._check(self._lib.dodo_attend_q4(self._ctx, q, qo, qp, code, H, dh, sm_scale, q4, sc, pos, co, cl, lk, lv, lo, ll, lp, loc_rows,
                                              B, o, ls, w, ws_bytes, _stream()))
 
     def attend_indexed(self, Q, q_off, q_pos0, sm_scale, K, V, seq_off, idx, nug_off, pos_base,

@@ -68,9 +68,3 @@ def test_tables_are_checked_without_their_tensors_too(host, name, args, change):
 @pytest.mark.parametrize("change", [dict(), dict(cache_len=[0, 0], cache_off=[0, 0, 3]), dict(cache_off=[0]), dict(loc_len=[0, 0]), dict(loc_len=[0, 0], loc_off=[0, 0], loc_pos0=[5, 5])])
 def test_calls_without_a_segment_reach_the_library(host, name, args, change):
     getattr(host, name)(**args(**change))
-
-
-@pytest.mark.parametrize("name,args", CALLS)
-@pytest.mark.parametrize("scale", [0.125, 1, np.float32(0.125), np.float64(0.125), np.float16(0.125), torch.tensor(0.125)])
-def test_the_scale_is_any_number(host, name, args, scale):
-    getattr(host, name)(**args(sm_scale=scale))
