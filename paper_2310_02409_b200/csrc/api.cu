@@ -93,9 +93,13 @@ int score_impl(dodo_ctx* ctx, const void* X, int dtype, int d, const void* w, fl
 }
 
 size_t attend_partial_rows_bound(const dodo_ctx* ctx) {
-    // split-K only happens while (query tiles x heads) < target, and then the block count stays
+    // dodo_attend: split-K only happens while (query tiles x heads) < target, and then the block count stays
     // below 2 x target; a block writes at most 8 partial rows
-    return static_cast<size_t>(16) * static_cast<size_t>(ctx->attend_target_ctas);
+    const size_t plain = static_cast<size_t>(2) * static_cast<size_t>(ctx->attend_target_ctas) * 8;
+    // dodo_attend_q4: a unit's share x = key tiles x target / work of the blocks is rounded, and cut from 1.5 on, so that it
+    // gets at most 4/3 x; the shares of all units add up to the target
+    const size_t q4 = (static_cast<size_t>(4) * static_cast<size_t>(dodo_attend_q4_target(ctx->attend_target_ctas)) + 2) / 3 * DODO_Q4_TILE_QUERIES;
+    return plain > q4 ? plain : q4;      // (both 16 rows per block of the target)
 }
 
 }  // namespace

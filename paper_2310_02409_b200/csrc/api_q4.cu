@@ -133,11 +133,10 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     dodo_attend_plan_begin(shp, ctx->attend_target_ctas, plan, tot, dodo_attend_q4_tile_queries(dtype, max_tq));
     // A sequence whose key list is longer than a block's share of the work is cut even when there are units enough for the
     // device (one long sequence of a ragged batch would outlast all others), but never into chunks of less than four tiles,
-    // whose merge costs more than it saves (8 x 269 keys of 32 heads in two chunks each: 11.8 against 6.6 us).  The share is
-    // that of three blocks per SM by default, half more than dodo_attend's: this kernel's blocks are smaller.
+    // whose merge costs more than it saves (8 x 269 keys of 32 heads in two chunks each: 11.8 against 6.6 us).
     tot.split = tot.work > tot.units;
     tot.min_chunk = 4;
-    tot.target = ctx->attend_target_ctas + ctx->attend_target_ctas / 2;
+    tot.target = dodo_attend_q4_target(ctx->attend_target_ctas);
     const int ngroups = (B + DODO_GROUP - 1) / DODO_GROUP;
     AttendGroup one;
     AttendGroup* groups = &one;

@@ -961,7 +961,7 @@ attend_q4_token_kernel(const __nv_bfloat16* __restrict__ Q, const __grid_constan
 // heads 7.1, 10.9, 18.3; over 4 x 717 and 1280: 29, 37, 61.  (With fp32 FMAs eight queries took 226, 35 and 118.)  Expanding the rows
 // first and attending them on the tensor cores takes 188, 21 and 49 whatever the number, which is the better from about 32 on.
 // Head size 64, the same three batches: eight queries 32, 6.9, 25 us (FMAs: four queries 58, 12.0), sixteen 64, 12, 37.
-constexpr int kFewQueries = 8;
+constexpr int kFewQueries = DODO_Q4_TILE_QUERIES;
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {       // an 8 x 8 matrix of 16-bit elements, two of row r in lane (r, t)
     uint32_t d;

@@ -270,6 +270,10 @@ struct DenseGather {
 int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps,
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
+// Blocks that the streaming kernels over a 4-bit cache aim at, three per SM by default: half more than dodo_attend, as their blocks
+// are smaller.  With the most queries a tile of theirs has, this decides the partial rows that a call may need (attend_partial_rows_bound).
+static inline int dodo_attend_q4_target(int attend_target) { return attend_target + attend_target / 2; }
+#define DODO_Q4_TILE_QUERIES 8
 // The streaming kernels over a 4-bit cache: launch as above, the cache (cache_rows rows) as codes and group words
 // queries per tile where the kernel of these types has only one choice, else 0
 int dodo_attend_q4_tile_queries(int dtype, int max_tq);

@@ -618,3 +618,18 @@ def test_attend_q4_range_of_queries(dodo, dtype, dh, tq, power):
     assert bool(torch.isfinite(q["Q"].float()).all()) and torch.equal((q["Q"].double() * 2.0 ** -power).to(dtype), p["Q"])
     O2, lse2 = _run_q4(dodo, q)
     assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,tq", [(BF, 8), (BF, 1), (F32, 4)])
+def test_attend_q4_fits_the_workspace_at_its_fullest(dodo, dtype, tq):
+    """A unit's share of one and a half blocks is rounded to two: with two such units per SM the partial results take all of
+    dodo_attend's workspace, and no byte behind it."""
+    H, B, dh = torch.cuda.get_device_properties(0).multi_processor_count // 4, 8, 128
+    p = _problem(("q4full", dtype == BF, tq), dtype, H, dh, [tq] * B, [560] * B, [tq] * B)
+    n = dodo.attend_workspace_bytes(dh)
+    ws = torch.full((n + 4096,), 0xff, dtype=torch.uint8, device="cuda")
+    O, lse = _run_q4(dodo, p, ws[:n])
+    assert bool((ws[n:] == 0xff).all())
+    one = dict(p, B=1, q_off=p["q_off"][:2], Q=p["Q"][:tq], cache_off=p["cache_off"][:2])
+    _check(one, O[:tq], lse[:tq])
+    assert bool(torch.isfinite(O.float()).all())
