@@ -705,7 +705,7 @@ int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_
     for (int gi = 0; gi < ngroups && rc == DODO_OK; ++gi) {
         if (groups[gi].cta0[groups[gi].nseq] == 0) continue;      // no query in it, nothing launched: it settles nothing
         const bool early = dodo_cache_settled(ctx, capture);
-        rc = dense ? dodo_launch_attend_dense(ctx, H, sm_scale, groups[gi], dmaps, cache_pos, O, lse, workspace, workspace_bytes,
+        rc = dense ? dodo_launch_attend_dense(ctx, H, sm_scale, groups[gi], dmaps, Q, maps, cache_pos, O, lse, workspace, workspace_bytes,
                                               ctx->tickets, ctx->dev_status, nullptr, st)
                    : dodo_launch_attend(ctx, dtype, H, dh, sm_scale, plan, groups[gi], Q, maps, cache_pos, O, lse,
                                         static_cast<float*>(workspace), ctx->tickets, early, st);
@@ -781,7 +781,7 @@ int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_off, cons
             gat.n[i] = seq_off[b0 + i + 1] - seq_off[b0 + i];
             gat.pos_base[i] = pos_base[b0 + i];
         }
-        rc = dodo_launch_attend_dense(ctx, H, sm_scale, grp, dmaps, idx, O, lse, workspace, workspace_bytes, ctx->tickets,
+        rc = dodo_launch_attend_dense(ctx, H, sm_scale, grp, dmaps, Q, {K, V, locK, locV}, idx, O, lse, workspace, workspace_bytes, ctx->tickets,
                                       ctx->dev_status, &gat, static_cast<cudaStream_t>(stream));
     }
     free(k_len);

@@ -26,6 +26,9 @@
 // One round to bf16 at the end; optional log-sum-exp (from the unrounded weights).
 // V rows past the end of a segment are zeroed in shared memory before use, so that whatever lies
 // behind a sequence's region (another sequence, unused capacity) can never reach the product P V.
+// A key that some of a tile's queries do not see may hold anything as well, and in the product 0 times a NaN or an infinity of
+// its V is a NaN: outputs that are not finite are summed again at the block's end, key by key, over what their query sees
+// (sum_again; all that the tiles' loop has of it is one flag).
 // Every wait is bounded; on time-out a status word is set and the block runs on to its end, where
 // it always frees its TMEM columns.
 //
@@ -126,6 +129,20 @@ __device__ __forceinline__ TileSrc tile_src(const AttendSeq& sq, const Unit& u, 
     }
     return s;
 }
+// plain: block bid's unit
+__device__ __forceinline__ void plain_unit(const AttendGroup& g, int H, int bid, Unit& u) {
+    int b;
+    if (g.uniform_ctas > 0) {
+        b = bid / g.uniform_ctas;
+    } else {
+        b = 0;
+#pragma unroll 8
+        for (int i = 1; i < DODO_GROUP; ++i) b += (i < g.nseq && g.cta0[i] <= bid) ? 1 : 0;
+    }
+    const int r0 = bid - g.cta0[b];
+    u.i = b; u.h = r0 % H; u.qt = r0 / H;
+    unit_shape(g.seq[b], u);
+}
 // The unit after u in the order (sequence, query tile, head), heads fastest; with width > 1 the query
 // tile stays what it is and the order is (sequence, head).  False past the last one.
 __device__ __forceinline__ bool next_unit(const AttendGroup& g, int H, int width, Unit& u) {
@@ -193,13 +210,173 @@ __device__ __forceinline__ void gather_tile(uint32_t dst, const CUtensorMap* map
     tma_gather4(dst + half * kKVHalfBytes + grp * 512, map, col0 + half * 64, r[0], r[1], r[2], r[3], bar);
 }
 
+// bits 0 to 3: which of four bf16 are a NaN or an infinity
+__device__ __forceinline__ uint32_t not_finite4(uint2 w) {
+    auto one = [](uint32_t x) { return x == 0x7f800000u ? 1u : 0u; };
+    return one((w.x << 16) & 0x7f800000u) | one(w.x & 0x7f800000u) << 1 | one((w.y << 16) & 0x7f800000u) << 2 | one(w.y & 0x7f800000u) << 3;
+}
+__device__ __forceinline__ void unpack4(uint2 w, float* f) {
+    f[0] = __uint_as_float(w.x << 16); f[1] = __uint_as_float(w.x & 0xffff0000u);
+    f[2] = __uint_as_float(w.y << 16); f[3] = __uint_as_float(w.y & 0xffff0000u);
+}
+// The results of a unit that are not finite, once more on the FMA units: softmax and sums of P V over the keys that a query sees and no
+// others.  A masked key's V may have caused them or a visible one's: a tile's product cannot tell.  The block's softmax warps call it
+// together, 16 queries each, kAgain at a time: a lane owns four features, four keys at a time make 4 kAgain (query, key) pairs, whose
+// products' sums over the lanes end up with a few lanes each.  All from the call's tables and with few registers: those of a called
+// function come out of the tiles' loop (with eight queries at a time it was spilled: 8 x 128 queries over 205 + 192 keys 23.0 us, with
+// two 22.2, without this function 21.9).  4 x 256 queries over 717 + 1280 keys of 32 heads, a masked NaN row in each sequence: 5.5 ms
+// (eight at a time 3.0), where finite values take 47 us.
+struct Sources { const __nv_bfloat16 *Q, *cK, *cV, *lK, *lV; };     // what the tensor maps cover
+constexpr int kAgain = 2;
+template <bool kGathered>
+__device__ __noinline__ void sum_again(const AttendGroup& g, const Sources& from, const DenseGather& gs, int i, int qt, int h, int H,
+                                       const int32_t* __restrict__ cache_pos, float scale_log2, __nv_bfloat16* O) {
+    constexpr int kPairs = 4 * kAgain, kCopies = 32 / kPairs;       // lanes that end up with a pair's sum
+    const AttendSeq& sq = g.seq[i];
+    const int lane = threadIdx.x & 31, key = lane / kCopies & 3, query = lane / kCopies / 4;      // of the lane's pair
+    Unit u;
+    u.i = i; u.qt = qt; u.h = h;
+    unit_shape(sq, u);
+    const size_t pitch = static_cast<size_t>(H) * DH, col = static_cast<size_t>(h) * DH + lane * 4;
+    const int q_end = min(sq.tq, qt * BM + (threadIdx.x >> 5) * 16 + 16);
+#pragma unroll 1
+    for (int q0 = qt * BM + (threadIdx.x >> 5) * 16; q0 < q_end; q0 += kAgain) {
+        uint2 q[kAgain];
+        uint32_t bad = 0u;
+#pragma unroll
+        for (int k = 0; k < kAgain; ++k) {
+            q[k] = make_uint2(0u, 0u);
+            if (q0 + k < q_end) {
+                const size_t at = static_cast<size_t>(sq.q_row0 + q0 + k) * pitch + col;
+                bad |= not_finite4(*reinterpret_cast<const uint2*>(O + at)) << (4 * k);
+                q[k] = __ldg(reinterpret_cast<const uint2*>(from.Q + at));
+            }
+        }
+        if (__any_sync(0xffffffffu, bad != 0u) == 0) continue;
+        const int qpos = q0 + query < q_end ? sq.q_pos0 + q0 + query : static_cast<int>(0x80000000);
+        float acc[kAgain][4], m = kNeg, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < kAgain; ++k)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) acc[k][f] = 0.f;
+#pragma unroll 1
+        for (int t = 0; t < u.n; ++t) {
+            const TileSrc ts = tile_src(sq, u, t);
+            bool settled = true;         // they all come from values that are seen
+#pragma unroll
+            for (int e = 0; e < 4 * kAgain; ++e) settled = settled && ((bad >> e & 1u) == 0u || acc[e / 4][e % 4] != acc[e / 4][e % 4]);
+            if (__all_sync(0xffffffffu, settled)) break;
+#pragma unroll 1
+            for (int r = 0; r < ts.rows; r += 4) {
+                const int mine = ts.row0 + min(r + key, ts.rows - 1), listed = ts.cache ? __ldg(cache_pos + mine) : 0;
+                const int pos = ts.cache ? listed + (kGathered ? gs.pos_base[i] : 0) : ts.pos0 + r + key;
+                const bool sees = r + key < ts.rows && q0 + query < q_end && pos <= qpos;
+                const uint32_t seen = __ballot_sync(0xffffffffu, sees);
+                if (seen == 0u) continue;
+                const int src = kGathered && ts.cache ? gs.row0[i] + min(max(listed, 0), gs.n[i] - 1) : mine;
+                uint2 kw[4], vw[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const size_t at = static_cast<size_t>(__shfl_sync(0xffffffffu, src, e * kCopies)) * pitch + col;
+                    kw[e] = __ldg(reinterpret_cast<const uint2*>((ts.cache ? from.cK : from.lK) + at));
+                    vw[e] = __ldg(reinterpret_cast<const uint2*>((ts.cache ? from.cV : from.lV) + at));
+                }
+                float part[kPairs];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float kf[4], qf[4];
+                    unpack4(kw[e], kf);
+#pragma unroll
+                    for (int k = 0; k < kAgain; ++k) {
+                        unpack4(q[k], qf);
+                        part[4 * k + e] = fmaf(qf[0], kf[0], fmaf(qf[1], kf[1], fmaf(qf[2], kf[2], qf[3] * kf[3])));
+                    }
+                }
+                // halving exchanges: at each step a lane gives away one half of its sums and adds up the other
+#pragma unroll
+                for (int o = 16, n = kPairs / 2; o > 0; o >>= 1, n >>= 1) {
+                    if (n == 0) {
+                        part[0] += __shfl_xor_sync(0xffffffffu, part[0], o);
+                    } else {
+                        const bool upper = (lane & o) != 0;
+#pragma unroll
+                        for (int j = 0; j < n; ++j) {
+                            const float give = upper ? part[j] : part[j + n], keep = upper ? part[j + n] : part[j];
+                            part[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                        }
+                    }
+                }
+                const float s = part[0] * scale_log2;
+                float top = fmaxf(m, sees ? s : kNeg);
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, kCopies));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2 * kCopies));
+                const float corr = ex2_approx(m - top), p = sees ? ex2_approx(s - top) : 0.f;
+                m = top;
+                l = fmaf(l, corr, p);
+                const float rounded = __bfloat162float(__float2bfloat16_rn(p));
+#pragma unroll
+                for (int k = 0; k < kAgain; ++k) {
+                    const float c = __shfl_sync(0xffffffffu, corr, 4 * k * kCopies);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) acc[k][f] *= c;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float vf[4];
+                    unpack4(vw[e], vf);
+#pragma unroll
+                    for (int k = 0; k < kAgain; ++k) {
+                        const float w = __shfl_sync(0xffffffffu, rounded, (4 * k + e) * kCopies);
+                        if ((seen >> ((4 * k + e) * kCopies) & 1u) != 0u) {
+#pragma unroll
+                            for (int f = 0; f < 4; ++f) acc[k][f] = fmaf(w, vf[f], acc[k][f]);
+                        }
+                    }
+                }
+            }
+        }
+        l += __shfl_xor_sync(0xffffffffu, l, kCopies);
+        l += __shfl_xor_sync(0xffffffffu, l, 2 * kCopies);
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int k = 0; k < kAgain; ++k) {
+            const float f_inv = __shfl_sync(0xffffffffu, inv, 4 * k * kCopies);
+            __nv_bfloat16* const out = O + static_cast<size_t>(sq.q_row0 + q0 + k) * pitch + col;
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+                if ((bad >> (4 * k + f) & 1u) != 0u) out[f] = __float2bfloat16_rn(acc[k][f] * f_inv);
+        }
+    }
+}
+
+// The balanced form's: sum_again for the units that the block has finished, all that lie in its range and cut ones (its first and its
+// last) where it arrived last; start and finished are the block's s_start and s_finished
+template <bool kGathered>
+__device__ __noinline__ void finish_again(const AttendGroup& g, const Sources& from, const DenseGather& gs, int T, int W, const int* start, const int* finished, int H,
+                                          const int32_t* __restrict__ cache_pos, float scale_log2, __nv_bfloat16* O) {
+    const int G = static_cast<int>(gridDim.x) / W, grp = static_cast<int>(blockIdx.x) / W;
+    Unit u;
+    u.i = start[0]; u.qt = start[1]; u.h = start[2];
+    unit_shape(g.seq[u.i], u, W);
+    int t0 = start[3], left = block_start(T, G, grp + 1) - block_start(T, G, grp);
+    bool first = true, more = left > 0;
+    while (more) {
+        const int t1 = min(u.ne, t0 + left);
+        if ((t0 == 0 && t1 == u.ne) || finished[first ? 0 : 1] != 0) sum_again<kGathered>(g, from, gs, u.i, u.qt, u.h, H, cache_pos, scale_log2, O);
+        first = false;
+        left -= t1 - t0;
+        t0 = 0;
+        more = left > 0 && next_unit(g, H, W, u);
+    }
+}
+
 // cache_pos: positions of the cache rows; gathered form: the selected positions idx (sequence-local), and
 // AttendSeq::c_row0 / c_len name a sequence's slots in it.
 template <bool kBalanced, bool kGathered>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSM)
 attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ AttendGroup g,
                     const int32_t* __restrict__ cache_pos, int H, float scale_log2,
-                    __nv_bfloat16* __restrict__ O, float* __restrict__ lse, const DenseWork work,
+                    __nv_bfloat16* __restrict__ O, float* __restrict__ lse, const DenseWork work, const __grid_constant__ Sources from,
                     int* __restrict__ dev_status, const __grid_constant__ DenseGather gs) {
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -209,6 +386,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
     __shared__ int first_masked[2];
     __shared__ int s_start[4];      // balanced: the block's first unit and tile (i, qt, h, t)
     __shared__ int s_last;
+    __shared__ int s_again, s_finished[2];      // a result was not finite; the first / last unit of the block's range, cut, was finished here
 
     const int tid = threadIdx.x, warp = tid >> 5;
     const int bid = static_cast<int>(blockIdx.x);
@@ -219,6 +397,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
     // ---- barriers, TMEM, where this block starts ---------------------------------------------------
     if (tid == 0) {
         first_masked[0] = first_masked[1] = 0x7fffffff;
+        s_again = s_finished[0] = s_finished[1] = 0;
         mbar_init(&bar_q, 1);
         for (int b = 0; b < 2; ++b) { mbar_init(&bar_s[b], 1); mbar_init(&bar_o[b], 1); mbar_init(&bar_pready[b], kSoftmaxThreads / 32); }
         for (int s = 0; s < kStages; ++s) { mbar_init(&bar_kfull[s], 1); mbar_init(&bar_vfull[s], 1); }
@@ -268,17 +447,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
         x = block_start(T, G, grp);                  // slot at which the segment starts
         left = block_start(T, G, grp + 1) - x;       // slots still to do
     } else {
-        int b;
-        if (g.uniform_ctas > 0) {
-            b = bid / g.uniform_ctas;
-        } else {
-            b = 0;
-#pragma unroll 8
-            for (int i = 1; i < DODO_GROUP; ++i) b += (i < g.nseq && g.cta0[i] <= bid) ? 1 : 0;
-        }
-        const int r0 = bid - g.cta0[b];
-        u.i = b; u.h = r0 % H; u.qt = r0 / H;
-        unit_shape(g.seq[b], u);
+        plain_unit(g, H, bid, u);
         left = u.ne;
     }
     int it = 0;        // key tiles this block has been through (barrier phases and ring stages run on)
@@ -579,6 +748,10 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
 #pragma unroll
                         for (int e = 0; e < 32; ++e) ov[e] = 0u;
                     }
+                    uint32_t most = 0u;      // the largest exponent
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) most = max(most, ov[e] & 0x7f800000u);
+                    if (most == 0x7f800000u) s_again = 1;
                     if (row_live) {
                         uint4* dst = reinterpret_cast<uint4*>(O + orow * DH + half * 64 + c * 32);
 #pragma unroll
@@ -636,6 +809,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
                         L = fmaf(__ldcg(pc + BM * DH + BM + row), ex2_approx(__ldcg(pc + BM * DH + row) - M), L);
                     }
                     const float inv = L > 0.f ? 1.f / L : 0.f;
+                    if (tid == 0) s_finished[first_seg ? 0 : 1] = 1;
 #pragma unroll 1
                     for (int cc = 0; cc < DH / 64; ++cc) {
                         float o[32];
@@ -648,6 +822,10 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = fmaf(__ldcg(src + e * BM), w, o[e]);
                         }
+                        uint32_t most = 0u;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) most = max(most, __float_as_uint(o[e]) & 0x7f800000u);
+                        if (most == 0x7f800000u) s_again = 1;
                         if (row_live) {
                             uint4* dst = reinterpret_cast<uint4*>(O + orow * DH + half * 64 + cc * 32);
 #pragma unroll
@@ -674,6 +852,14 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
     __syncthreads();
     if (warp == 0)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    if (warp < kSoftmaxThreads / 32 && s_again != 0) {
+        if (kBalanced) {
+            finish_again<kGathered>(g, from, gs, work.total_slots, work.width, s_start, s_finished, H, cache_pos, scale_log2, O);
+        } else {
+            plain_unit(g, H, bid, u);
+            sum_again<kGathered>(g, from, gs, u.i, u.qt, u.h, H, cache_pos, scale_log2, O);
+        }
+    }
 }
 
 }  // namespace
@@ -682,7 +868,7 @@ int dodo_dense_tile_queries() { return BM; }
 int dodo_dense_tile_keys() { return BN; }
 size_t dodo_dense_workspace_bytes(int num_sms) { return static_cast<size_t>(2) * 2 * num_sms * kPartFloats * sizeof(float); }
 
-int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps,
+int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps, const void* Q, const AttendMaps& src,
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st) {
     const int units = g.cta0[g.nseq];
@@ -721,6 +907,8 @@ int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendG
     work.total_slots = !balanced ? 0 : static_cast<int>(in_step ? total_step : total);
     work.partials = static_cast<float*>(workspace);
     work.tickets = tickets;
+    const Sources from = {static_cast<const __nv_bfloat16*>(Q), static_cast<const __nv_bfloat16*>(src.cK), static_cast<const __nv_bfloat16*>(src.cV),
+                          static_cast<const __nv_bfloat16*>(src.lK), static_cast<const __nv_bfloat16*>(src.lV)};
     int grid = units;
     if (balanced) {
         long long groups = resident / work.width;
@@ -740,6 +928,6 @@ int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendG
     DenseGather none;
     memset(&none, 0, sizeof none);
     kern<<<grid, kThreads, smem, st>>>(maps, g, cache_pos, H, sm_scale * 1.4426950408889634f,
-                                       static_cast<__nv_bfloat16*>(O), lse, work, dev_status, gathered ? *gather : none);
+                                       static_cast<__nv_bfloat16*>(O), lse, work, from, dev_status, gathered ? *gather : none);
     return dodo_check_cuda(ctx, cudaGetLastError(), "dense attend launch");
 }

@@ -266,8 +266,8 @@ struct DenseGather {
 };
 // gather == NULL: cache_pos are the positions of the cache rows and maps.cK / cV tile the cache.  Else: cache_pos
 // is the index list, AttendSeq::c_row0 / c_len name each sequence's slots in it, and maps.cK / cV have boxes one
-// row high over the uncompressed K / V.
-int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps,
+// row high over the uncompressed K / V.  Q, src: the arrays that the maps cover.
+int dodo_launch_attend_dense(dodo_ctx* ctx, int H, float sm_scale, const AttendGroup& g, const DenseMaps& maps, const void* Q, const AttendMaps& src,
                              const int32_t* cache_pos, void* O, float* lse, void* workspace, size_t workspace_bytes,
                              int* tickets, int* dev_status, const DenseGather* gather, cudaStream_t st);
 // Blocks that the streaming kernels over a 4-bit cache aim at, three per SM by default: half more than dodo_attend, as their blocks

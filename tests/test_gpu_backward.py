@@ -477,3 +477,40 @@ def test_attend_and_gradient_between_the_ends_of_the_positions(dodo, dtype, dh, 
         want = plain64.attend(q, np.zeros(tq), p["scale"], k, k, np.zeros(len(k)))[1]
         assert np.all(np.abs(lse[b * tq:(b + 1) * tq] - want) <= plain64.logit_bound(q, k, p["scale"], dh) + 2.0 ** -20 + 100 * 2.0 ** -24 + 2.0 ** -22 * np.abs(want))
     check(p, d, out, dense=dtype == BF and tq > 4)
+
+
+@pytest.mark.parametrize("balance", [0, 1, 3])
+@pytest.mark.parametrize("tq,nug", [(40, 200), (200, 4000)])
+def test_attend_of_blocks_with_anything_in_masked_rows(libdodo, tq, nug, balance):
+    """The forward that a gradient starts from, on the tensor cores: keys that some queries of a block do not see hold NaN and
+    infinities, in the first tile and in later ones, in every way of spreading the work."""
+    dodo = api.Dodo(0)
+    dodo.set_tuning(api.TUNE_DENSE_BALANCE, balance)
+    p = problem(("bwdblockany", tq), BF, 2, 128, [tq, 32], [nug, 64], [tq + 2, 32], slack=0)
+    half = int(p["q_pos0"][0]) + tq // 2
+    p["cpos"][[0, 63, 100]] = half
+    p["cpos"][[1, nug - 1]] = 10 ** 6
+    clean = forward(dodo, p)
+    torch.cuda.synchronize()
+    q = dict(p, **{n: p[n].clone() for n in ("cK", "cV", "lK", "lV")})
+    for n in ("cK", "cV"):
+        q[n][[1, nug - 1]] = float("nan")
+    q["cV"][0, 1, 3], q["cV"][63, 0, 64], q["cV"][100, 1, 127], q["lV"][tq + 1, 0, 0] = float("nan"), float("inf"), -float("inf"), float("nan")
+    out = forward(dodo, q)
+    again = forward(dodo, q)
+    torch.cuda.synchronize()
+    fixed = lambda t: t.nan_to_num(7.0, 1e30, -1e30)  # noqa: E731
+    assert torch.equal(out["lse"], clean["lse"]) and torch.equal(fixed(out["O"]), fixed(again["O"]))
+    assert torch.equal(out["O"][tq:], clean["O"][tq:])
+    Q, K, V = _f64(p["Q"][:tq]), np.concatenate([_f64(q["cK"][:nug]), _f64(q["lK"][:tq + 2])]), np.concatenate([_f64(q["cV"][:nug]), _f64(q["lV"][:tq + 2])])
+    kpos, qpos = np.concatenate([p["cpos"][:nug], p["loc_pos0"][0] + np.arange(tq + 2)]), p["q_pos0"][0] + np.arange(tq)
+    want, got = plain64.attend(Q, qpos, p["scale"], K, V, kpos)[0], _f64(out["O"][:tq])
+    # a weight's error: its logit's, its rounding to bf16 (2^-8), the exponential's and the sum's; the result is rounded once
+    keys = np.concatenate([_f64(p["cK"][:nug]), _f64(p["lK"][:tq + 2])])
+    w = 2.0 * plain64.logit_bound(Q, keys, p["scale"], 128) + 2.0 ** -8 + 2.0 ** -20 + len(K) * 2.0 ** -24
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    assert np.all(np.abs(got[fine] - want[fine]) <= 2.0 ** -8 * np.abs(want[fine]) + w * np.max(np.abs(V[np.isfinite(V)])))
+    assert fine[:tq // 2].all() and not fine[tq // 2:, 1, 3].any() and not fine[tq // 2:, 0, 64].any() and not fine[tq - 1, 0, 0]
+    assert dodo.device_status() == 0
+    dodo.close()

@@ -633,3 +633,44 @@ def test_attend_q4_fits_the_workspace_at_its_fullest(dodo, dtype, tq):
     one = dict(p, B=1, q_off=p["q_off"][:2], Q=p["Q"][:tq], cache_off=p["cache_off"][:2])
     _check(one, O[:tq], lse[:tq])
     assert bool(torch.isfinite(O.float()).all())
+
+
+@pytest.mark.parametrize("tq", [40, 130, 300])
+def test_attend_q4_block_masked_rows_may_hold_anything(dodo, tq):
+    """Blocks of queries on the tensor cores: nuggets that no query sees, and nuggets and local tokens that only some of them see, hold
+    NaN and infinities.  Queries that do not see them keep their bits; the others show them, in the features that have them."""
+    p = _problem(("q4blockany", tq), BF, 2, 128, [tq, 33], [150, 70], [tq + 3, 40])
+    late = p["q_pos0"][0] + tq // 2
+    p["cpos"][[0, 1, 70, 149]] = [late, 10 ** 6, late, 10 ** 6]        # a first tile's, a later one's; two that nobody sees
+    clean, lc = _run_q4(dodo, p)
+    _check(p, clean, lc, rounded=True)
+    _, _, tol, _ = _reference(p, rounded=True)
+
+    def check(q):
+        """Against the plain form over what each query sees, with the clean batch's tolerance; the log-sum-exp does not hang on values."""
+        O, lse = _run_q4(dodo, q)
+        want, got = _reference(q, rounded=True)[0], _f64(O)
+        fine = np.isfinite(want)
+        assert np.array_equal(np.isfinite(got), fine) and np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.all(np.abs(got[fine] - want[fine]) <= tol[fine]) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+        assert torch.equal(lse, lc)
+        O2, _ = _run_q4(dodo, q)
+        assert torch.equal(O.nan_to_num(7.0, 1e30, -1e30), O2.nan_to_num(7.0, 1e30, -1e30))
+        return fine
+
+    q = dict(p, words=p["words"].copy(), loc=[t.clone() for t in p["loc"]])
+    q["words"][[1, 149]] = 0x7fc07fc0
+    assert check(q).all()                                               # hidden: nothing to be seen of them
+    for row in (0, 70):                                                 # a value of head 1, features 32 to 63
+        w = dict(q, words=q["words"].copy())
+        w["words"][row, 1, 1, 1] = 0x7fc07fc0
+        fine = check(w)
+        assert fine[:tq // 2].all() and fine[tq:].all() and not fine[tq // 2:tq, 1, 32:64].any() and fine[:, 0].all()
+    last = int(p["loc_off"][0]) + tq + 3 - 4                            # the fourth last local token: its own query's and three more see it
+    for value in ("nan", "inf", "-inf"):
+        w = dict(q, loc=[t.clone() for t in p["loc"]])
+        w["loc"][1][last, 0, 5] = float(value)
+        w["loc"][1][last + 2, 0, 5] = -float("inf")
+        fine = check(w)
+        assert fine[:tq - 4].all() and not fine[tq - 4:tq, 0, 5].any() and fine[:, 1].all()
+    assert dodo.device_status() == 0

@@ -175,3 +175,36 @@ def test_indexed_attend_reports_bad_indices_and_refuses_other_shapes(libdodo):
         assert ctx.device_status() == 0
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_indexed_attend_with_anything_in_masked_rows(dodo, mode):
+    """Selected tokens that some queries do not see, or none, hold NaN and infinities in V: equal to gather, then attend, and the
+    queries that do not see them stay finite."""
+    from paper_2310_02409_b200 import api
+    H, dh, n, tq, ll = 2, 128, 900, 140, 50
+    K, V, Q, lK, lV = (inputs.randn((r, H, dh), "indexed-any", k, dtype=BF).cuda() for k, r in (("K", n), ("V", n), ("Q", tq), ("lK", ll), ("lV", ll)))
+    idx = np.sort(np.random.RandomState(4).choice(n, 300, replace=False)).astype(np.int32)
+    q0 = int(idx[150]) - 70                                       # queries from there on, inside the selection
+    V[idx[-40:].tolist()] = float("nan")                          # behind every query
+    V[int(idx[150]), 1, 7] = float("inf")                         # seen by the later half
+    assert int(idx[-40]) > q0 + tq
+    idx_d, k = torch.from_numpy(idx).cuda(), len(idx)
+    ws = torch.empty(dodo.attend_workspace_bytes(dh), dtype=torch.uint8, device="cuda")
+    cK, cV, cpos, clen = torch.zeros((k, H, dh), dtype=BF, device="cuda"), torch.zeros((k, H, dh), dtype=BF, device="cuda"), torch.zeros(k, dtype=torch.int32, device="cuda"), np.zeros(1, np.int32)
+    out = [(torch.empty_like(Q), torch.empty((tq, H), device="cuda")) for _ in range(2)]
+    local = (lK, lV, [0], [ll], [n])
+    dodo.set_tuning(api.TUNE_DENSE_BALANCE, mode)
+    try:
+        dodo.attend_indexed(Q, [0, tq], [q0], dh ** -0.5, K, V, [0, n], idx_d, [0, k], [0], *local, *out[0], ws)
+        dodo.gather_kv(K, V, [0, n], idx_d, [0, k], [0], cK, cV, cpos, [0, k], clen)
+        dodo.attend(Q, [0, tq], [q0], dh ** -0.5, cK, cV, cpos, [0, k], clen, *local, *out[1], ws)
+    finally:
+        dodo.set_tuning(api.TUNE_DENSE_BALANCE, 0)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and bool(torch.isfinite(out[0][1]).all())
+    inf = torch.isinf(out[0][0])
+    want = torch.zeros_like(inf)
+    want[int(idx[150]) - q0:, 1, 7] = True
+    assert torch.equal(inf, want) and not bool(torch.isnan(out[0][0]).any())
+    assert dodo.device_status() == 0
