@@ -274,7 +274,7 @@ DODO_API size_t dodo_attend_workspace_bytes(const dodo_ctx* ctx, int dh);
  * Query i of sequence b sits at position q_pos0[b] + i.  Nugget row j carries cache_pos[...];
  * local row j of sequence b sits at loc_pos0[b] + j.  A key is visible iff its position is <= the
  * query's.  A query with no visible key gets O = 0 and lse = -inf.  A key that a query does not see takes no part in its
- * result, whatever its rows hold (NaN, infinities).
+ * result, whatever its rows hold (NaN, infinities); one that it sees and whose product with it is a NaN makes O and lse NaN.
  *   Q          [device] [q_off[B], H, dh]          O  [device] same shape, written
  *   q_off      [host] int32[B+1]                   q_pos0 [host] int32[B]
  *   cacheK/V, cache_pos, cache_off  as in dodo_gather_kv; cache_len [host] int32[B] rows in use

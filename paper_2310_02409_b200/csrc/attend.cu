@@ -382,9 +382,9 @@ attend_kernel(const T* __restrict__ Q, const AttendMaps src, const __grid_consta
         }
         const size_t orow = static_cast<size_t>(qrow0 + q2) * H + h;
         if (nchunk == 1) {
-            store_out(O + orow * DH + dim, L > 0.f ? o / L : 0.f);
+            store_out(O + orow * DH + dim, L != 0.f ? o / L : 0.f);
             if (lse != nullptr && dim == 0)
-                lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+                lse[orow] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
         } else if (clustered) {
             const uint32_t rec = xred0 + static_cast<uint32_t>(((chunk * QT + q2) * RED) * sizeof(float));
             asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(rec + dim * 4u), "f"(o) : "memory");
@@ -403,9 +403,9 @@ attend_kernel(const T* __restrict__ Q, const AttendMaps src, const __grid_consta
 
     auto write_out = [&](int q2, int dim, float M, float L, float o) {
         const size_t orow = static_cast<size_t>(qrow0 + q2) * H + h;
-        store_out(O + orow * DH + dim, L > 0.f ? o / L : 0.f);
+        store_out(O + orow * DH + dim, L != 0.f ? o / L : 0.f);
         if (lse != nullptr && dim == 0)
-            lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+            lse[orow] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
     };
     if (clustered) {
         // the stores above are released by the arrival; the first block acquires them and merges.  A block

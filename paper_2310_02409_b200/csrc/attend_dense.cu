@@ -738,7 +738,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
             const bool whole = !kBalanced || (t0 == 0 && t1 == ne);
             if (whole) {
                 // ---- normalise, round once, store ----------------------------------------------------------------
-                const float inv = l > 0.f ? 1.f / l : 0.f;
+                const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll 1
                 for (int c = 0; c < DH / 64; ++c) {
                     uint32_t ov[32];
@@ -765,7 +765,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
                     }
                 }
                 if (row_live && half == 0 && lse != nullptr)
-                    lse[orow] = l > 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    lse[orow] = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
             } else {
                 // ---- a cut unit: unnormalised partial to the workspace; the last block to arrive merges --------
                 // Layout [feature][row]: a warp's lanes are consecutive rows, so they write and read consecutive floats.
@@ -808,7 +808,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
                         const float* pc = work.partials + static_cast<size_t>(2 * (c * W + bid % W) + (block_start(T, G, c) >= xu ? 0 : 1)) * kPartFloats;
                         L = fmaf(__ldcg(pc + BM * DH + BM + row), ex2_approx(__ldcg(pc + BM * DH + row) - M), L);
                     }
-                    const float inv = L > 0.f ? 1.f / L : 0.f;
+                    const float inv = L != 0.f ? 1.f / L : 0.f;
                     if (tid == 0) s_finished[first_seg ? 0 : 1] = 1;
 #pragma unroll 1
                     for (int cc = 0; cc < DH / 64; ++cc) {
@@ -835,7 +835,7 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
                         }
                     }
                     if (row_live && half == 0 && lse != nullptr)
-                        lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+                        lse[orow] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");   // s_last is free again
             }

@@ -514,3 +514,21 @@ def test_attend_of_blocks_with_anything_in_masked_rows(libdodo, tq, nug, balance
     assert fine[:tq // 2].all() and not fine[tq // 2:, 1, 3].any() and not fine[tq // 2:, 0, 64].any() and not fine[tq - 1, 0, 0]
     assert dodo.device_status() == 0
     dodo.close()
+
+
+@pytest.mark.parametrize("dtype,dh,tq,nug", [(F32, 64, 1, 40), (F32, 128, 3, 5000), (BF, 128, 1, 300), (BF, 128, 1, 6000), (BF, 64, 5, 70), (BF, 128, 40, 90), (BF, 128, 260, 6000)])
+def test_a_key_that_is_no_number_shows(dodo, dtype, dh, tq, nug):
+    """A visible key that holds a NaN: its head's output and log-sum-exp are NaN, not the 0 and -inf of a query that sees nothing, and
+    so is the query's gradient; other heads and sequences keep their bits."""
+    p = problem(("bwdnankey", dh, tq, nug), dtype, 2, dh, [tq, 2], [nug, 20], [tq + 1, 2], slack=0)
+    clean = forward(dodo, p)
+    q = dict(p, cK=p["cK"].clone())
+    q["cK"][nug // 2, 1, 5] = float("nan")
+    d = forward(dodo, q)
+    out = backward(dodo, q, d)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(d["O"][:tq, 1]).all()) and bool(torch.isnan(d["lse"][:tq, 1]).all())
+    assert torch.equal(d["O"][:tq, 0], clean["O"][:tq, 0]) and torch.equal(d["lse"][:tq, 0], clean["lse"][:tq, 0])
+    assert torch.equal(d["O"][tq:], clean["O"][tq:]) and torch.equal(d["lse"][tq:], clean["lse"][tq:])
+    assert bool(torch.isnan(out["dQ"][:tq, 1]).all()) and bool(torch.isfinite(out["dQ"][:tq, 0]).all()) and bool(torch.isfinite(out["dQ"][tq:]).all())
+    assert dodo.device_status() == 0

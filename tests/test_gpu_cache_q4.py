@@ -674,3 +674,14 @@ def test_attend_q4_block_masked_rows_may_hold_anything(dodo, tq):
         fine = check(w)
         assert fine[:tq - 4].all() and not fine[tq - 4:tq, 0, 5].any() and fine[:, 1].all()
     assert dodo.device_status() == 0
+
+
+@pytest.mark.parametrize("tq", [40, 200])
+def test_attend_q4_block_visible_nan_shows(dodo, tq):
+    p = _problem(("q4blockvis", tq), BF, 2, 128, [tq, 1], [90, 20], [tq + 1, 3])
+    clean, lc = _run_q4(dodo, p)
+    q = dict(p, words=p["words"].copy())
+    q["words"][45, 1, 0, 2] = 0x7fc07fc0                         # a group of a key that every query of the first sequence sees
+    O, lse = _run_q4(dodo, q)
+    assert bool(torch.isnan(O[:tq, 1]).all()) and bool(torch.isnan(lse[:tq, 1]).all())
+    assert torch.equal(O[:tq, 0], clean[:tq, 0]) and torch.equal(lse[:tq, 0], lc[:tq, 0]) and torch.equal(O[tq:], clean[tq:])
