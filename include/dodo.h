@@ -86,7 +86,7 @@ DODO_API int dodo_device_status(dodo_ctx* ctx, int* status);
  * per dodo_attend launch (default 2 x SM count); changes dodo_attend_workspace_bytes.
  * (Knob 2, a shared-memory stage count, belonged to an earlier kernel and is gone: it is refused.)
  * DODO_TUNE_DENSE_MIN_QUERIES: a call whose longest query block has at least this many tokens
- * (bf16, head size 128) runs on the tensor-core kernel (default 32); a very large value keeps
+ * (bf16, head size 128, sm_scale >= 1e-9) runs on the tensor-core kernel (default 32); a very large value keeps
  * everything on the streaming kernel.
  * DODO_TUNE_DENSE_BALANCE: how the tensor-core kernel spreads (sequence, query tile, head) units
  * over thread blocks: 0 (default) balances key tiles over the resident blocks when the units alone
@@ -322,7 +322,7 @@ DODO_API int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, con
  *             outside [0, n_b) is clamped into the sequence and DODO_DEV_BAD_INDEX is set
  *   seq_off, nug_off, pos_base  [host] as in dodo_gather_kv
  *   everything else as in dodo_attend (the workspace too)
- * Runs on the tensor-core kernel only: dtype DODO_BF16, dh 128, sm_scale > 0; else DODO_ERR_UNSUPPORTED.
+ * Runs on the tensor-core kernel only: dtype DODO_BF16, dh 128, sm_scale >= 1e-9; else DODO_ERR_UNSUPPORTED.
  */
 DODO_API int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int dtype,
                         int H, int dh, float sm_scale, const void* K, const void* V, const int32_t* seq_off,
@@ -397,7 +397,7 @@ DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32
  * dodo_attend over a 4-bit nugget cache (local tokens, queries and outputs in `dtype`): the keys and values of cached
  * rows are those that the codes stand for; fp32 sums, the products of weights and steps kept to 16 bits or more, one
  * rounding of O.  A block of queries whose longest part has
- * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale > 0) runs on the tensor cores when the
+ * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale >= 1e-9) runs on the tensor cores when the
  * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
  * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
  * call that has cached rows takes the streaming kernels.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache

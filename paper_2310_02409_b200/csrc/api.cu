@@ -666,8 +666,8 @@ int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_
     // shape rule: blocks of many bf16 queries at head size 128 are a contraction -> tensor cores
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
-    // (the tensor-core kernel takes row maxima before scaling, which needs a positive scale)
-    const bool dense = dtype == DODO_BF16 && dh == 128 && max_tq >= ctx->dense_min_tq && sm_scale > 0.f;
+    // (the tensor-core kernel takes row maxima and masks before scaling, which needs a positive scale that is not too small)
+    const bool dense = dtype == DODO_BF16 && dh == 128 && max_tq >= ctx->dense_min_tq && sm_scale >= DODO_DENSE_LEAST_SCALE;
     const AttendMaps maps = {any_cache ? cacheK : nullptr, any_cache ? cacheV : nullptr,
                              any_local ? locK : nullptr, any_local ? locV : nullptr};
     DenseMaps dmaps;
@@ -723,8 +723,8 @@ int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_off, cons
     if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
     if (B < 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "B = %d is negative", B);
     if (!valid_dtype(dtype)) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "dtype %d", dtype);
-    if (dtype != DODO_BF16 || dh != 128 || !(sm_scale > 0.f))
-        return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "indexed attention runs on the tensor-core kernel only: bf16, head size 128, positive scale "
+    if (dtype != DODO_BF16 || dh != 128 || !(sm_scale >= DODO_DENSE_LEAST_SCALE))
+        return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "indexed attention runs on the tensor-core kernel only: bf16, head size 128, scale of 1e-9 or more "
                          "(got dtype %d, head size %d, scale %g); gather into a cache and use dodo_attend otherwise", dtype, dh, sm_scale);
     if (H <= 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "H = %d", H);
     if (!valid_offsets(q_off, B)) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "q_off must start at 0 and be non-decreasing");

@@ -113,7 +113,7 @@ int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int
     int max_tq = 0;
     for (int b = 0; b < B; ++b) max_tq = max_tq > q_off[b + 1] - q_off[b] ? max_tq : q_off[b + 1] - q_off[b];
     const int cache_rows = any_cache ? cache_off[B] : 0;
-    if (dtype == DODO_BF16 && dh == 128 && sm_scale > 0.f && max_tq >= ctx->dense_min_tq && workspace != nullptr &&
+    if (dtype == DODO_BF16 && dh == 128 && sm_scale >= DODO_DENSE_LEAST_SCALE && max_tq >= ctx->dense_min_tq && workspace != nullptr &&
         dodo_aligned16(workspace) && workspace_bytes >= dodo_attend_q4_workspace_bytes(ctx, H, dh, cache_rows)) {
         const size_t head = round16(dodo_attend_workspace_bytes(ctx, dh));
         unsigned char* K = static_cast<unsigned char*>(workspace) + head;

@@ -250,6 +250,9 @@ void dodo_attend_plan_group(const AttendShape& s, const AttendPlan& plan, Attend
 struct DenseMaps {
     CUtensorMap Q, cK, cV, lK, lV;   // boxes of 64 elements x 128 rows, 128-byte swizzle
 };
+// Least softmax scale of the tensor-core attend: masked scores are -1e30 before the scale and must be far below the -1e20 that stands
+// for a row without a key in sight after it.  Calls below it take the streaming kernel.
+#define DODO_DENSE_LEAST_SCALE 1e-9f
 int dodo_dense_tile_queries();
 int dodo_dense_tile_keys();
 // cache_box_rows: rows of the box of the cK / cV maps (the key tile; 1 for the gathered form's row copies)

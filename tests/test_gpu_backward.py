@@ -532,3 +532,27 @@ def test_a_key_that_is_no_number_shows(dodo, dtype, dh, tq, nug):
     assert torch.equal(d["O"][tq:], clean["O"][tq:]) and torch.equal(d["lse"][tq:], clean["lse"][tq:])
     assert bool(torch.isnan(out["dQ"][:tq, 1]).all()) and bool(torch.isfinite(out["dQ"][:tq, 0]).all()) and bool(torch.isfinite(out["dQ"][tq:]).all())
     assert dodo.device_status() == 0
+
+
+@pytest.mark.parametrize("power", [20, 60])
+def test_gradient_of_a_block_with_a_tiny_scale(dodo, power):
+    p = problem(("bwdtiny", power), BF, 2, 128, [70, 40], [300, 60], [10, 40], inside=True)
+    p["q_pos0"][1] = -5                                           # the first queries see nothing
+    p["Q"], p["scale"] = (p["Q"].float() * 2.0 ** power).to(BF), p["scale"] * 2.0 ** -power
+    d = forward(dodo, p)
+    out = backward(dodo, p, d)
+    torch.cuda.synchronize()
+    lse = _f64(d["lse"])
+    for b in range(2):
+        q = slice(int(p["q_off"][b]), int(p["q_off"][b + 1]))
+        c = slice(int(p["cache_off"][b]), int(p["cache_off"][b]) + int(p["clen"][b]))
+        l = slice(int(p["loc_off"][b]), int(p["loc_off"][b]) + int(p["llen"][b]))
+        k, v = np.concatenate([_f64(p["cK"])[c], _f64(p["lK"])[l]]), np.concatenate([_f64(p["cV"])[c], _f64(p["lV"])[l]])
+        kpos = np.concatenate([p["cpos"][c], p["loc_pos0"][b] + np.arange(p["llen"][b])])
+        O, want = plain64.attend(_f64(p["Q"])[q], p["q_pos0"][b] + np.arange(q.stop - q.start), p["scale"], k, v, kpos)
+        seen = np.isfinite(want)
+        assert np.array_equal(np.isneginf(lse[q]), ~seen)
+        e = plain64.logit_bound(_f64(p["Q"])[q], k, p["scale"], 128) + 2.0 ** -20 + len(k) * 2.0 ** -24
+        assert np.all(np.abs(lse[q][seen] - want[seen]) <= e + 2.0 ** -22 * np.abs(want[seen]))
+        assert np.all(np.abs(_f64(d["O"])[q] - O) <= 2.0 ** -8 * np.abs(O) + (2 * e + 2.0 ** -8) * np.max(np.abs(v)))
+    check(p, d, out, dense=True)

@@ -685,3 +685,15 @@ def test_attend_q4_block_visible_nan_shows(dodo, tq):
     O, lse = _run_q4(dodo, q)
     assert bool(torch.isnan(O[:tq, 1]).all()) and bool(torch.isnan(lse[:tq, 1]).all())
     assert torch.equal(O[:tq, 0], clean[:tq, 0]) and torch.equal(lse[:tq, 0], lc[:tq, 0]) and torch.equal(O[tq:], clean[tq:])
+
+
+@pytest.mark.parametrize("power", [30, 60])
+def test_attend_q4_block_with_a_tiny_scale(dodo, power):
+    """Large queries and a tiny softmax scale: masked keys and rows that see nothing stay out (below a scale of 1e-9 blocks take the
+    kernels that mask behind the scale)."""
+    p = _problem(("q4tiny", power), BF, 2, 128, [70, 40], [300, 60], [10, 40], inside=True)
+    p["q_pos0"][1] = -5                                           # the first queries see nothing
+    p["Q"], p["scale"] = (p["Q"].float() * 2.0 ** power).to(BF), p["scale"] * 2.0 ** -power
+    O, lse = _run_q4(dodo, p)
+    _check(p, O, lse, rounded=p["scale"] >= 1e-9)
+    assert bool(torch.isneginf(lse).any())
