@@ -556,3 +556,52 @@ def test_gradient_of_a_block_with_a_tiny_scale(dodo, power):
         assert np.all(np.abs(lse[q][seen] - want[seen]) <= e + 2.0 ** -22 * np.abs(want[seen]))
         assert np.all(np.abs(_f64(d["O"])[q] - O) <= 2.0 ** -8 * np.abs(O) + (2 * e + 2.0 ** -8) * np.max(np.abs(v)))
     check(p, d, out, dense=True)
+
+
+def test_two_contexts_on_two_streams(libdodo):
+    """Gradients and 4-bit appends, expansions and attends of two contexts at once, each on its own stream with its own buffers: the
+    bits of one after the other."""
+    H, dh = 4, 128
+    rs = np.random.RandomState(6)
+
+    def job(i, ctx):
+        p = problem(("bwdtwo", i), BF, H, dh, [100 + 30 * i, 3], [700, 90], [130, 40])
+        few = problem(("bwdtwofew", i), F32, 2, 64, [20, 2], [300, 9], [22, 2])
+        K, V = (inputs.randn((600, H, dh), "bwdtwo", i, k, dtype=BF).cuda() for k in "KV")
+        Q = inputs.randn((40, H, dh), "bwdtwo", i, "Q", dtype=BF).cuda()
+        idx = _cuda(np.sort(rs.permutation(600)[:200]).astype(np.int32))
+        d, df = forward(ctx, p), forward(ctx, few)
+        n, nf = (ctx.attend_backward_workspace_bytes(int(x["q_off"][-1]), x["H"], x["dh"], int(x["cache_off"][-1])) for x in (p, few))
+        w, wf, w4 = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in (n, nf, ctx.attend_q4_workspace_bytes(H, dh, 200)))
+        torch.cuda.synchronize()
+
+        def run():
+            q4, sc = torch.zeros((200, H, 2, dh // 2), dtype=torch.uint8, device="cuda"), torch.zeros((200, H, 2, dh // 32), dtype=torch.int32, device="cuda")
+            pos, clen, outs = torch.zeros(200, dtype=torch.int32, device="cuda"), np.zeros(1, np.int32), []
+            for _ in range(4):
+                outs += list(backward(ctx, p, d, ws=w).values()) + list(backward(ctx, few, df, ws=wf).values())
+                clen[:] = 0
+                ctx.gather_kv_q4(K, V, [0, 600], idx, [0, 200], [0], q4, sc, pos, [0, 200], clen)
+                for t in (1, 5, 40):
+                    O = torch.empty((t, H, dh), dtype=BF, device="cuda")
+                    ctx.attend_q4(Q[:t].contiguous(), [0, t], [600], dh ** -0.5, q4, sc, pos, [0, 200], clen, K, V, [500], [100], [550], O, None, w4)
+                    outs.append(O)
+            return outs + [q4, sc, pos]
+        return run
+
+    ctxs, streams = [api.Dodo(0), api.Dodo(0)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = [job(i, c) for i, c in enumerate(ctxs)]
+    alone = []
+    for run in jobs:
+        alone.append(run())
+        torch.cuda.synchronize()
+    together = []
+    for run, s in zip(jobs, streams):
+        with torch.cuda.stream(s):
+            together.append(run())
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        assert len(a) == len(b) and all(torch.equal(x.float().nan_to_num(5.0), y.float().nan_to_num(5.0)) for x, y in zip(a, b))
+    for c in ctxs:
+        assert c.device_status() == 0
+        c.close()
