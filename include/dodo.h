@@ -296,9 +296,10 @@ DODO_API size_t dodo_attend_workspace_bytes(const dodo_ctx* ctx, int dh);
  * this context since then, and, under stream capture, that attend recorded in the same capture.
  * Sequences of dodo_* calls on one context therefore need no care (the first attend after a gather
  * reads everything after the wait).  A caller that writes a nugget cache by other means (its own
- * kernel, a copy, another context) between two dodo_attend calls on this context must call
- * dodo_cache_written(ctx) before the second.  Q, locK/locV, O, lse and the workspace are read and
+ * kernel, a copy, another context, the replay of a graph that holds an append) between two dodo_attend calls on
+ * this context must call dodo_cache_written(ctx) before the second.  Q, locK/locV, O, lse and the workspace are read and
  * written only after everything earlier on the stream has completed.
+ * Range: logits, and on the tensor cores <q, k> itself, lie above -5 * 10^29; a key below that counts as one not seen.
  * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.
  */
 DODO_API int dodo_attend(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0,
@@ -352,7 +353,8 @@ DODO_API int dodo_attend_indexed(dodo_ctx* ctx, const void* Q, const int32_t* q_
  * not overlap inputs or each other.  Results repeat bit for bit.  A nugget's gradient is that of the cache row:
  * the row of K and V that it was gathered from has the same one.  Queries, O and dO must be finite; a row of K or V that a
  * query does not see does not reach that query's gradient, whatever it holds.  Positions of queries and local tokens lie in
- * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.
+ * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.  fp32 blocks of queries take about four million cached rows
+ * in each 64 sequences (DODO_ERR_CAPACITY).
  * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}.
  */
 DODO_API size_t dodo_attend_backward_workspace_bytes(const dodo_ctx* ctx, int q_rows, int H, int dh, int cache_rows);
@@ -396,13 +398,16 @@ DODO_API int dodo_expand_kv_q4(dodo_ctx* ctx, const void* cache_q4, const uint32
 /*
  * dodo_attend over a 4-bit nugget cache (local tokens, queries and outputs in `dtype`): the keys and values of cached
  * rows are those that the codes stand for; fp32 sums, the products of weights and steps kept to 16 bits or more, one
- * rounding of O.  A block of queries whose longest part has
- * at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale >= 1e-9) runs on the tensor cores when the
- * workspace has dodo_attend_q4_workspace_bytes: the rows in use are expanded into it as bf16 once, so every cached value
- * is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp carries too.  With only dodo_attend_workspace_bytes every
- * call that has cached rows takes the streaming kernels.  Stream order, masks and empty rows as in dodo_attend; a program that writes the cache
- * by other means than dodo_gather_kv_q4 calls dodo_cache_written.  Positions of queries and local tokens lie in
- * [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache_pos may hold anything.  Steps s of cached values stay below 2^47 (values below
+ * rounding of O.
+ * A call whose longest block has at least DODO_TUNE_DENSE_MIN_QUERIES tokens (bf16, head size 128, sm_scale >= 1e-9) runs on
+ * the tensor cores, with all of its sequences, when the workspace has dodo_attend_q4_workspace_bytes: the rows in use are
+ * expanded into it as bf16 once, so every cached value is rounded to bf16 (at most 2^-8 of it), which the log-sum-exp
+ * carries too, and the weights are rounded to bf16.  The choice is the caller's: with only dodo_attend_workspace_bytes every
+ * call that has cached rows takes the streaming kernels and no value is rounded, at twice the time with 32 queries a
+ * sequence and seven times with 256.
+ * Stream order, masks, empty rows and range as in dodo_attend; a program that writes the cache by other means than
+ * dodo_gather_kv_q4 calls dodo_cache_written.  Positions of queries and local tokens lie in [-2^30, 2^30)
+ * (DODO_ERR_INVALID_ARG); cache_pos may hold anything.  Steps s of cached values stay below 2^47 (values below
  * about 2^50 in magnitude; larger ones may come out as NaN or infinity).
  *   cache_rows  cache_off[B] of the calls that the workspace is meant for
  *   everything else as in dodo_attend and dodo_gather_kv_q4

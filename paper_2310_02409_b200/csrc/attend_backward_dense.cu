@@ -33,9 +33,9 @@
 // 64 columns of S and 64 of T.
 // The heads' score gradients, and dQ of query units cut into chunks, are added up by kernels of their own (a fence and a ticket per
 // unit cost microseconds each, and the block that joined chunks held up the launch).
-// Measured: 4 x 256 queries over 717 + 1280 keys of 32 heads of 128 167 us (one set of inputs; 175 with three in rotation), 512
-// queries over 16,896 keys of 40 heads 610 to 720 (850 to 1000 TFLOP/s of the seven products; power moves the clock), 5 to 64 queries over 8
-// x 269 keys 58, over 4160 keys 76.
+// Measured: 4 x 256 queries over 717 + 1280 keys of 32 heads of 128 164 to 175 us with the inputs (power moves the clock), of 64 148
+// to 154; 512 queries over 16,896 keys of 40 heads 695 to 725, 840 to 880 TFLOP/s of the seven products made, 600 to 625 of the five
+// that a gradient needs; 5 to 64 queries over 8 x 269 keys 58, over 4160 keys 76.
 // Every wait is bounded; a role whose wait runs out reports it and leaves, and so do the others in turn.
 #include "dodo_internal.cuh"
 #include "sm100_ptx.cuh"

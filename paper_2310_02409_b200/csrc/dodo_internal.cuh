@@ -85,7 +85,7 @@ int dodo_score_mlp_reduce_rows();          // rows per block of the fused reduct
 int dodo_score_mlp_fused_max_tokens();     // longer sequences are selected by a launch of their own
 // tensor map of a [rows, width] bf16 row-major array: box of 64 elements x box_rows rows, 128-byte swizzle (cached)
 int dodo_encode_bf16_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_rows);
-// ... of a [rows, width] byte array: box of box_width (32: no swizzle, 128: 128-byte swizzle) bytes x box_rows rows (cached)
+// ... of a [rows, width] byte array: box of box_width (16, 32: no swizzle; 64, 128: swizzled over as many bytes) bytes x box_rows rows (cached)
 int dodo_encode_byte_rows(dodo_ctx* ctx, CUtensorMap* map, const void* base, int width, int rows, int box_width, int box_rows);
 
 // ---- threshold selection ----------------------------------------------------------------------
