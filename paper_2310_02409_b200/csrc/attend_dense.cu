@@ -224,7 +224,7 @@ __device__ __forceinline__ void unpack4(uint2 w, float* f) {
 // together, 16 queries each, kAgain at a time: a lane owns four features, four keys at a time make 4 kAgain (query, key) pairs, whose
 // products' sums over the lanes end up with a few lanes each.  All from the call's tables and with few registers: those of a called
 // function come out of the tiles' loop (with eight queries at a time it was spilled: 8 x 128 queries over 205 + 192 keys 23.0 us, with
-// two 22.2, without this function 21.9).  4 x 256 queries over 717 + 1280 keys of 32 heads, a masked NaN row in each sequence: 5.5 ms
+// two 21.9, without this function 21.7).  4 x 256 queries over 717 + 1280 keys of 32 heads, a masked NaN row in each sequence: 5.5 ms
 // (eight at a time 3.0), where finite values take 47 us.
 struct Sources { const __nv_bfloat16 *Q, *cK, *cV, *lK, *lV; };     // what the tensor maps cover
 constexpr int kAgain = 2;
@@ -748,10 +748,11 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
 #pragma unroll
                         for (int e = 0; e < 32; ++e) ov[e] = 0u;
                     }
-                    uint32_t most = 0u;      // the largest exponent
+                    float2 zero = make_float2(0.f, 0.f);     // ... unless a result is not finite
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) most = max(most, ov[e] & 0x7f800000u);
-                    if (most == 0x7f800000u) s_again = 1;
+                    for (int e = 0; e < 32; e += 2)
+                        zero = __ffma2_rn(make_float2(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1])), make_float2(0.f, 0.f), zero);
+                    if (!(zero.x + zero.y == 0.f)) s_again = 1;
                     if (row_live) {
                         uint4* dst = reinterpret_cast<uint4*>(O + orow * DH + half * 64 + c * 32);
 #pragma unroll
@@ -822,10 +823,10 @@ attend_dense_kernel(const __grid_constant__ DenseMaps maps, const __grid_constan
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = fmaf(__ldcg(src + e * BM), w, o[e]);
                         }
-                        uint32_t most = 0u;
+                        float2 zero = make_float2(0.f, 0.f);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) most = max(most, __float_as_uint(o[e]) & 0x7f800000u);
-                        if (most == 0x7f800000u) s_again = 1;
+                        for (int e = 0; e < 32; e += 2) zero = __ffma2_rn(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), zero);
+                        if (!(zero.x + zero.y == 0.f)) s_again = 1;
                         if (row_live) {
                             uint4* dst = reinterpret_cast<uint4*>(O + orow * DH + half * 64 + cc * 32);
 #pragma unroll
