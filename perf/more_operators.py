@@ -156,6 +156,12 @@ def _rope(case):
     return api.Rope(freq, api.ROPE_HALF if case["layout"] == "half" else api.ROPE_INTERLEAVED, _amplitude(case))
 
 
+def _cache(s):
+    """The cache's arrays and page table as a program that serves from it keeps them."""
+    from paper_2310_02409_b200 import api
+    return api.PagedCache(s["cacheK"], s["cacheV"], s["cache_pos"], s["page_table"])
+
+
 def _randn(g, shape, dtype):
     return torch.randn(shape, generator=g, device=DEV, dtype=torch.float32).to(dtype)
 
@@ -204,6 +210,8 @@ def prepare(case, seed):
         shape = (s["pool"], case["page"], s["H"], dh)
         s["cacheK"], s["cacheV"] = _randn(g, shape, dtype), _randn(g, shape, dtype)
         s["cache_pos"] = torch.full(shape[:2], -1, dtype=torch.int32, device=DEV)
+        if own:
+            s["cache"] = _cache(s)
         return s
     tq, nug, loc = _ints(case["tq"]), _ints(case["nug"]), _ints(case["loc"])
     B = len(tq)
@@ -220,6 +228,8 @@ def prepare(case, seed):
     s["cache_pos"] = torch.full((shape[0] * shape[1],), 2 ** 31 - 1, dtype=torch.int32, device=DEV)
     s["cache_pos"][s["row"]] = pos
     s["cache_pos"] = s["cache_pos"].view(shape[:2])
+    if own:
+        s["cache"] = _cache(s)
     s.update(scale=dh ** -0.5, q_off=_offsets(tq), q_pos0=np.asarray(q_pos0, np.int32), cache_len=np.asarray(nug, np.int32), loc_off=_offsets(loc),
              loc_len=np.asarray(loc, np.int32), loc_pos0=np.asarray(span, np.int32))
     s["Q"] = _randn(g, (sum(tq), s["H"], dh), dtype)
@@ -301,14 +311,13 @@ def _called(s):
         return {"Q": outQ, "K": outK}
     if s["op"] == "append":
         used = s["used"].copy()
-        dodo.gather_kv_paged(s["K"], s["V"], s["off"], s["idx"], s["nug_off"], s["pos0"], s["rope"], s["cacheK"], s["cacheV"], s["cache_pos"],
-                             s["page_table"], s["page_off"], used)
+        dodo.gather_kv_paged(s["K"], s["V"], s["off"], s["idx"], s["nug_off"], s["pos0"], s["rope"], s["cache"], s["page_off"], used)
         return {"K": s["cacheK"], "V": s["cacheV"], "cache_pos": s["cache_pos"]}
     if "workspace" not in s:
         s["workspace"] = torch.empty(dodo.attend_paged_workspace_bytes(s["dh"]), dtype=torch.uint8, device=DEV)
     O, lse = _new(s, "O", s["Q"].shape, s["dtype"]), _new(s, "lse", s["Q"].shape[:2], torch.float32)
-    dodo.attend_paged(s["Q"], s["q_off"], s["q_pos0"], s["scale"], s["cacheK"], s["cacheV"], s["cache_pos"], s["page_table"], s["page_off"],
-                      s["cache_len"], s["locK"], s["locV"], s["loc_off"][:-1], s["loc_len"], s["loc_pos0"], O, lse, s["workspace"])
+    dodo.attend_paged(s["Q"], s["q_off"], s["q_pos0"], s["scale"], s["cache"], s["page_off"], s["cache_len"], s["locK"], s["locV"],
+                      s["loc_off"][:-1], s["loc_len"], s["loc_pos0"], O, lse, s["workspace"])
     return {"O": O, "lse": lse}
 
 
