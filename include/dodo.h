@@ -426,6 +426,108 @@ DODO_API int dodo_attend_q4(dodo_ctx* ctx, const void* Q, const int32_t* q_off, 
 DODO_API int dodo_cache_written(dodo_ctx* ctx);
 
 /*
+ * Rotary positions.  Feature pairs of a head are turned by an angle that grows with the token's position (the base model's
+ * positions; the K/V rows that the calls above take carry them already):
+ *   y_a = scale (x_a cos t - x_b sin t),   y_b = scale (x_a sin t + x_b cos t),   t = position * freq[i],   0 <= i < rot / 2
+ *   DODO_ROPE_HALF         (a, b) = (i, i + rot / 2)          DODO_ROPE_INTERLEAVED  (a, b) = (2 i, 2 i + 1)
+ * Features from `rot` on are copied.  Angles are held as 64-bit fractions of a turn, so that no position loses any of them
+ * (2^-33 turns at position 2^31); fp32 arithmetic, one rounding of each result to the array's type.
+ *
+ * dodo_rope_frequencies  the frequencies of a base model, in radians per position: freq[i] = base^(-2 i / rot), and for contexts
+ *   longer than the `trained` ones
+ *     DODO_ROPE_LINEAR  freq / factor (positions interpolated)
+ *     DODO_ROPE_BASE    with base * factor^(rot / (rot - 2)): the slowest pair is slowed down by the factor, the fastest not at all
+ *     DODO_ROPE_PARTS   pairs with `high` turns or more over the trained length keep their frequency, those with `low` or fewer are
+ *                       divided by the factor, between them the two are mixed in proportion to the turns
+ *   rot even, 2 to DODO_ROPE_MAX; freq [host] double[rot / 2], written.  trained, low and high are read for DODO_ROPE_PARTS only.
+ * dodo_rope_init  makes a rotation of any frequencies (any finite ones, and any finite scale, 1 for plain rotation).  The struct is the
+ *   caller's, host memory, read during a call and not retained.
+ */
+enum { DODO_ROPE_HALF = 0, DODO_ROPE_INTERLEAVED = 1 };
+enum { DODO_ROPE_PLAIN = 0, DODO_ROPE_LINEAR = 1, DODO_ROPE_BASE = 2, DODO_ROPE_PARTS = 3 };
+enum { DODO_ROPE_MAX = 256, DODO_ROPE_ARRAYS = 4 };
+typedef struct {
+    int32_t rot, layout;
+    float scale;
+    uint32_t ready;                          /* set by dodo_rope_init */
+    uint64_t turn[DODO_ROPE_MAX / 2];        /* freq / (2 pi) modulo 1, times 2^64 */
+} dodo_rope_spec;
+DODO_API int dodo_rope_frequencies(int rot, double base, int scaling, double factor, int trained, double low, double high, double* freq);
+DODO_API int dodo_rope_init(dodo_rope_spec* rope, int rot, int layout, float scale, const double* freq);
+
+/*
+ * The rotation applied to up to DODO_ROPE_ARRAYS arrays (a layer's queries and keys) of one packed batch, in one launch per 64
+ * sequences; dodo_rope_backward is its gradient: what arrives at the outputs, turned by the opposite angle and scaled alike.
+ *   arrays   [host] n of them: `in` and `out` [device], element (row, head, feature) of `in` at row * in_row + head * in_head +
+ *            feature, in elements (dense: in_row = heads * dh, in_head = dh; slices of a fused projection have larger ones), `out`
+ *            likewise.  out = in with the same strides works in place; otherwise outputs overlap neither inputs nor each other.
+ *            Addresses are aligned to their element type, strides free (16-byte alignment of both is the fast case)
+ *   row_off  [host] int32[B+1], non-decreasing from 0: rows of sequence b      pos0 [host] int32[B]: position of its first row
+ * Rows outside row_off[0] .. row_off[B] are left as they were.  Supported: dh even, 2 to 512, rot <= dh; positions in
+ * [-2^31, 2^31).  An output may be a nugget cache: the next dodo_attend reads none of it early.
+ */
+typedef struct {
+    const void* in;
+    void* out;
+    int32_t heads, reserved;
+    int64_t in_row, in_head, out_row, out_head;
+} dodo_rope_array;
+DODO_API int dodo_rope(dodo_ctx* ctx, const dodo_rope_spec* rope, const dodo_rope_array* arrays, int n, int dtype, int dh,
+              const int32_t* row_off, const int32_t* pos0, int B, void* stream);
+DODO_API int dodo_rope_backward(dodo_ctx* ctx, const dodo_rope_spec* rope, const dodo_rope_array* arrays, int n, int dtype, int dh,
+                       const int32_t* row_off, const int32_t* pos0, int B, void* stream);
+
+/*
+ * Nugget cache in pages, for contexts whose caches grow: rows live in a pool of pages of `page` rows each, and row r of sequence b
+ * is row r % page of page table[page_off[b] + r / page].  Sequences may share pages that neither of them appends to.
+ *   K, V     [device] [pages, page, H, dh] in `dtype`, 16-byte aligned; H heads (those of K and V)
+ *   pos      [device] int32[pages, page]
+ *   table    [device] int32[page_off[B]], page numbers; page_off [host] int32[B+1], non-decreasing from 0.  A number outside
+ *            [0, pages) is never followed: appends leave its rows out, attention takes them as not seen, and DODO_DEV_BAD_INDEX is set
+ * The struct is host memory, read during a call and not retained.  pages * page < 2^31.
+ */
+typedef struct {
+    void *K, *V;
+    int32_t* pos;
+    const int32_t* table;
+    int32_t dtype, H, dh, pages, page, reserved;
+} dodo_paged_cache;
+
+/*
+ * dodo_gather_kv into a paged cache, K rotated at its position on the way (the position is recorded as there): row j of sequence b's
+ * selection becomes row cache_len[b] + j.
+ *   K, V      [device] rows of H * dh elements, 16-byte aligned, consecutive tokens kv_row elements apart (H * dh when dense; a
+ *             multiple of 16 bytes)
+ *   idx       [device] int32[nug_off[B]] as in dodo_gather_kv; NULL: every token is appended, in order, and nug_off is not read
+ *   rope      NULL: K is copied (it carries its positions already)
+ *   page_off  as above; a sequence's pages bound its rows (DODO_ERR_CAPACITY, nothing launched)
+ *   cache_len [host] int32[B], in/out
+ * No two appended rows may have the same place.  Positions pos_base[b] .. pos_base[b] + n_b - 1 lie below 2^31.
+ * Supported: dh even, 2 to 512, rot <= dh, H * dh elements a multiple of 16 bytes.
+ */
+DODO_API int dodo_gather_kv_paged(dodo_ctx* ctx, const void* K, const void* V, int64_t kv_row, const int32_t* seq_off, const int32_t* idx,
+                         const int32_t* nug_off, const int32_t* pos_base, int B, const dodo_rope_spec* rope,
+                         const dodo_paged_cache* cache, const int32_t* page_off, int32_t* cache_len, void* stream);
+
+/*
+ * dodo_attend over a paged cache: a chunk of new tokens, or single ones, over [rows in use ; local tokens].  The new tokens' own
+ * rows are local tokens, or have been appended before.  H query heads share the cache's heads evenly: query head h attends head
+ * h / (H / cache->H) of the cache and of locK / locV [loc_rows, cache->H, dh].  Masks, empty rows, O and lse as in dodo_attend;
+ * what a query does not see takes no part in its result, whatever it holds.  A key whose logit is -infinity counts as one not seen.
+ *   cache      its dtype and dh are those of Q, O and the local tokens; with no rows in use its arrays may be NULL
+ *   workspace  [device] at least dodo_attend_paged_workspace_bytes(ctx, dh) bytes, 16-byte aligned, contents free; needed only where
+ *              a key list is cut (DODO_ERR_CAPACITY when it is and the workspace is too small)
+ *   everything else as in dodo_attend, except that nothing is read ahead of what precedes the call on its stream
+ * Positions of queries and local tokens lie in [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache pos may hold anything.  bf16: weights are
+ * rounded to bf16 before their product with V.  Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}; H a multiple of cache->H.
+ */
+DODO_API size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh);
+DODO_API int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int H, float sm_scale,
+                      const dodo_paged_cache* cache, const int32_t* page_off, const int32_t* cache_len, const void* locK,
+                      const void* locV, const int32_t* loc_off, const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B,
+                      void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The whole path for one layer on HOST buffers (Eq. 6/15 -> Eq. 14 -> Eq. 5 -> Eq. 9 per decode
  * token): uploads the batch, compresses every sequence's context (fused score + TopK with k_b =
  * nug_off[b+1] - nug_off[b], then gather into an empty nugget cache), runs `steps` decode tokens per

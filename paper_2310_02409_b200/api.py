@@ -8,6 +8,7 @@ loudly when ``libdodo.so`` has not been built (``python -m paper_2310_02409_b200
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 
 import numpy as np
@@ -21,10 +22,14 @@ ACT_IDENTITY, ACT_RELU, ACT_GELU_TANH = 0, 1, 2
 TUNE_ATTEND_TARGET_BLOCKS, TUNE_DENSE_MIN_QUERIES, TUNE_DENSE_BALANCE = 1, 3, 4
 DEV_WAIT_TIMEOUT, DEV_BAD_INDEX = 1, 2
 Q4_GROUP = 32
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
+ROPE_MAX, ROPE_ARRAYS = 256, 4
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_CUDA = 0, -1, -2, -3, -4
 
 # every symbol include/dodo.h declares: name -> (restype, argtypes)
 _vp, _i, _u, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint32, ctypes.c_float, ctypes.c_size_t
+_d, _l = ctypes.c_double, ctypes.c_int64
 SIGNATURES = {
     "dodo_create": (_i, [ctypes.POINTER(_vp), _i]),
     "dodo_destroy": (_i, [_vp]),
@@ -61,6 +66,13 @@ SIGNATURES = {
     "dodo_attend_q4_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
     "dodo_attend_q4": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                             _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "dodo_rope_frequencies": (_i, [_i, _d, _i, _d, _i, _d, _d, _vp]),
+    "dodo_rope_init": (_i, [_vp, _i, _i, _f, _vp]),
+    "dodo_rope": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _i, _vp]),
+    "dodo_rope_backward": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _i, _vp]),
+    "dodo_gather_kv_paged": (_i, [_vp, _vp, _vp, _l, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "dodo_attend_paged_workspace_bytes": (_sz, [_vp, _i]),
+    "dodo_attend_paged": (_i, [_vp, _vp, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "dodo_host_arena_bytes": (_sz, [_vp, _i, _i, _i, _i, _i, _i, _i, _i, _i]),
     "dodo_compress_decode_host": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _vp, _i, _f,
                                        _vp, _vp, _sz, _vp]),
@@ -181,6 +193,65 @@ def _stream() -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_current_device())
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, trained: int = 0,
+                     low: float = 1.0, high: float = 32.0) -> np.ndarray:
+    """``dodo_rope_frequencies``: radians per position of the rot / 2 pairs, in 64 bits."""
+    freq = np.zeros(max(int(rot), 0) // 2, np.float64)
+    rc = load().dodo_rope_frequencies(int(rot), float(base), int(scaling), float(factor), int(trained), float(low), float(high), freq.ctypes.data)
+    if rc != OK:
+        raise DodoError(rc, "rot must be even, 2 to 256, base and factor positive and finite, trained positive, low below high")
+    return freq
+
+
+class Rope:
+    """A rotation (``dodo_rope_init``): frequencies in radians per position, one for each pair of features."""
+
+    def __init__(self, freq, layout: int = ROPE_HALF, scale: float = 1.0):
+        f = np.ascontiguousarray(freq, dtype=np.float64)
+        if f.ndim != 1:
+            raise ValueError("freq must be one-dimensional, one entry for each pair of features")
+        self.rot = 2 * f.size
+        self._spec = ctypes.create_string_buffer(16 + 8 * (ROPE_MAX // 2))
+        rc = load().dodo_rope_init(self._spec, self.rot, int(layout), float(scale), f.ctypes.data)
+        if rc != OK:
+            raise DodoError(rc, "1 to 128 finite frequencies, a finite scale and a layout (ROPE_HALF, ROPE_INTERLEAVED) are wanted")
+
+
+class PagedCache:
+    """A paged nugget cache (``dodo_paged_cache``): ``K``, ``V`` [pages, page, H, dh], ``pos`` int32 [pages, page] and ``table``
+    int32, the page numbers of all sequences one after the other.  The tensors are checked here and kept, not copied; a program
+    that moves its table to another tensor sets ``table``."""
+
+    def __init__(self, K, V, pos, table):
+        if K.dim() != 4:
+            raise ValueError(f"K must have shape [pages, page, H, dh], has {tuple(K.shape)}")
+        self.pages, self.page, self.H, self.dh = K.shape
+        for t, dt, n, name in ((K, K.dtype, None, "K"), (V, K.dtype, K.numel(), "V"), (pos, torch.int32, self.pages * self.page, "pos")):
+            _checked(t, dt, K.get_device(), n, name)
+        self.K, self.V, self.pos, self.dtype, self.code, self.index = K, V, pos, K.dtype, _dtype_code(K), K.get_device()
+        self.table = table
+
+    @property
+    def table(self):
+        return self._table
+
+    @table.setter
+    def table(self, t):
+        _checked(t, torch.int32, self.index, None, "table")
+        self._table, self.entries = t, t.numel()
+        self.spec = struct.pack("QQQQiiiiii", self.K.data_ptr(), self.V.data_ptr(), self.pos.data_ptr(), t.data_ptr(), self.code, self.H, self.dh,
+                                self.pages, self.page, 0)
+
+
+def _checked(t, dtype, index, numel, name):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and on the device of the others")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} must have {numel} elements, has {t.numel()} (shape {tuple(t.shape)})")
 
 
 class Dodo:
@@ -492,6 +563,100 @@ class Dodo:
         w, ws_bytes = self._workspace(workspace)
         self._check(self._lib.dodo_attend_q4(self._ctx, q, qo, qp, code, H, dh, sm_scale, q4, sc, pos, co, cl, lk, lv, lo, ll, lp, loc_rows,
                                              B, o, ls, w, ws_bytes, _stream()))
+
+    # -- rotary positions -----------------------------------------------------------------------------
+    def _rope(self, entry, rope, row_off, pos0, Q, K, outQ, outK):
+        ro, p0 = _table(row_off), _table(pos0)
+        if K is None and outK is not None:
+            raise ValueError("outK is given without K")
+        B, rows, dt, packed, n = len(ro) // 4 - 1, Q.shape[0], Q.dtype, b"", 0
+        dh = Q.shape[-1]
+        for x, y, name in ((Q, outQ, "Q"), (K, outK, "K")):
+            if x is None:
+                continue
+            y = x if y is None else y
+            if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != dh or y.shape != x.shape:
+                raise ValueError(f"{name} and its output must have shape [{rows}, heads, {dh}], have {tuple(x.shape)} and {tuple(y.shape)}")
+            if x.dtype is not dt or y.dtype is not dt:
+                raise TypeError(f"{name} and its output must be {dt}, are {x.dtype} and {y.dtype}")
+            a, b = x.stride(), y.stride()
+            if x.get_device() != self._index or y.get_device() != self._index or dh > 1 and (a[2] != 1 or b[2] != 1):
+                raise ValueError(f"{name} and its output must be tensors on {self.device} whose features lie side by side")
+            packed += struct.pack("QQiiqqqq", x.data_ptr(), y.data_ptr(), x.shape[1], 0, a[0], a[1], b[0], b[1])
+            n += 1
+        _bound(ro, B, rows, "row_off")
+        _entries(p0, B, "pos0")
+        self._check(entry(self._ctx, rope._spec, packed, n, _dtype_code(Q), dh, ro, p0, B, _stream()))
+
+    def rope(self, rope, row_off, pos0, Q, K=None, outQ=None, outK=None):
+        """``dodo_rope``: queries and keys ([rows, heads, dh], any strides between rows and heads) turned by their positions, sequence
+        b's rows from pos0[b] on; in place where no output is given."""
+        self._rope(self._lib.dodo_rope, rope, row_off, pos0, Q, K, outQ, outK)
+
+    def rope_backward(self, rope, row_off, pos0, dQ, dK=None, outQ=None, outK=None):
+        """``dodo_rope_backward``: gradients at the rotated queries and keys turned into those at the queries and keys."""
+        self._rope(self._lib.dodo_rope_backward, rope, row_off, pos0, dQ, dK, outQ, outK)
+
+    # -- the paged nugget cache -------------------------------------------------------------------------
+    def _pages(self, cache, page_off, B):
+        if cache.index != self._index:
+            raise ValueError(f"the cache must be on {self.device}")
+        _bound(page_off, B, cache.entries, "page_off")
+
+    def gather_kv_paged(self, K, V, seq_off, idx, nug_off, pos_base, rope, cache, page_off, cache_len):
+        """``dodo_gather_kv_paged``: append the selected rows (all of them where ``idx`` is None) to a ``PagedCache``, K turned by
+        ``rope`` (None: copied).  K and V may be slices of a wider row; ``cache_len`` (int32 numpy array) is updated in place."""
+        so, pb, po, cl = _table(seq_off), _table(pos_base), _table(page_off), _in_place(cache_len)
+        tokens, H, dh = self._heads(K, "K")
+        B, dt, row = len(so) // 4 - 1, cache.dtype, H * dh
+        if H != cache.H or dh != cache.dh or K.shape != V.shape:
+            raise ValueError(f"K and V must have shape [tokens, {cache.H}, {cache.dh}], have {tuple(K.shape)} and {tuple(V.shape)}")
+        stride = K.stride()
+        pitch = stride[0] if tokens > 1 else row
+        for t, name in ((K, "K"), (V, "V")):
+            s = t.stride()
+            if t.dtype is not dt:
+                raise TypeError(f"{name} must be {dt}, is {t.dtype}")
+            if t.get_device() != self._index or s[2] != 1 and dh > 1 or s[1] != dh and H > 1 or tokens > 1 and s[0] != pitch:
+                raise ValueError(f"{name} must be a tensor on {self.device} whose rows are dense and as far apart as K's")
+        ix = no = None
+        if idx is not None:
+            ix, no = self._ptr(idx, torch.int32, None, "idx"), _table(nug_off)
+            _bound(no, B, idx.numel(), "nug_off")
+        _bound(so, B, tokens, "seq_off")
+        _entries(pb, B, "pos_base")
+        if cache_len.size < B:
+            raise ValueError(f"cache_len must have {B} entries")
+        self._pages(cache, po, B)
+        self._check(self._lib.dodo_gather_kv_paged(self._ctx, K.data_ptr(), V.data_ptr(), pitch, so, ix, no, pb, B, None if rope is None else rope._spec,
+                                                   cache.spec, po, cl, _stream()))
+
+    def attend_paged_workspace_bytes(self, dh: int) -> int:
+        return int(self._lib.dodo_attend_paged_workspace_bytes(self._ctx, int(dh)))
+
+    def attend_paged(self, Q, q_off, q_pos0, sm_scale, cache, page_off, cache_len, locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):
+        """``dodo_attend_paged``: ``attend`` over a ``PagedCache`` and local tokens; Q may have several heads for each of the cache's."""
+        qo, qp, po, cl = _table(q_off), _table(q_pos0), _table(page_off), _table(cache_len)
+        lo, ll, lp = _table(loc_off), _table(loc_len), _table(loc_pos0)
+        rows_q, H, dh = self._heads(Q, "Q")
+        B, dt, ptr = len(qo) // 4 - 1, cache.dtype, self._ptr
+        if dh != cache.dh:
+            raise ValueError(f"Q has heads of {dh}, the cache of {cache.dh}")
+        _bound(qo, B, rows_q, "q_off")
+        _entries(qp, B, "q_pos0")
+        q, o = ptr(Q, dt, None, "Q"), ptr(O, dt, Q.numel(), "O")
+        ls = None if lse is None else ptr(lse, torch.float32, rows_q * H, "lse")
+        self._pages(cache, po, B)
+        _entries(cl, B, "cache_len")
+        lk = lv = None
+        loc_rows = 0
+        if locK is not None:
+            loc_rows = self._heads(locK, "locK")[0]
+            lk, lv = ptr(locK, dt, loc_rows * cache.H * dh, "locK"), ptr(locV, dt, loc_rows * cache.H * dh, "locV")
+        _local_tables(lo, ll, lp, B, locK is not None)
+        w, ws_bytes = self._workspace(workspace)
+        self._check(self._lib.dodo_attend_paged(self._ctx, q, qo, qp, H, sm_scale, cache.spec, po, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls,
+                                                w, ws_bytes, _stream()))
 
     def attend_indexed(self, Q, q_off, q_pos0, sm_scale, K, V, seq_off, idx, nug_off, pos_base,
                        locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):

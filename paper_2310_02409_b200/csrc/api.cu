@@ -351,6 +351,8 @@ int dodo_score_select(dodo_ctx* ctx, const void* X, int dtype, int d, const void
 
 }  // extern "C"
 
+bool dodo_valid_offsets(const int32_t* off, int B) { return valid_offsets(off, B); }
+
 // Checks shared by the gather entry points (everything but the K/V pointers).  row_bytes is set.
 int dodo_check_gather(dodo_ctx* ctx, int dtype, int H, int dh, const int32_t* seq_off, const int32_t* nug_off,
                       const int32_t* pos_base, int B, const int32_t* cache_off, const int32_t* cache_len,

@@ -1,0 +1,108 @@
+// C ABI entry point of attention over a paged cache: checks, tables, choice of kernel.
+#include "paged.cuh"
+
+int dodo_check_paged(dodo_ctx* ctx, const dodo_paged_cache* c, const int32_t* page_off, const int32_t* cache_len, int B, bool rows);
+
+// Chunks of each sequence's key list, blocks, partial rows and arrival counters.  A list is cut where it is longer than a block's share of
+// all the work (units times keys over the blocks to aim at), into chunks of about that share, all alike.  A cut list has more than one share,
+// so its chunks are fewer than twice its shares and the chunks of all cut units fewer than twice the target: dodo_paged_part_rows.
+void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv) {
+    auto tiles_of = [&](const PagedSeq& s) {
+        const int64_t keys = static_cast<int64_t>(s.c_len) + dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1);
+        return (keys + cut.keys - 1) / cut.keys;
+    };
+    auto units_of = [&](const PagedSeq& s) { return (static_cast<int64_t>(s.tq) * group + cut.rows - 1) / cut.rows * Hkv; };
+    int64_t work = 0;
+    for (int i = 0; i < g.nseq; ++i) work += units_of(g.seq[i]) * tiles_of(g.seq[i]);
+    int64_t share = (work + cut.target - 1) / cut.target;
+    if (share < cut.least / cut.keys) share = cut.least / cut.keys;
+    int64_t part = 0, tick = 0, cta = 0;
+    for (int i = 0; i < g.nseq; ++i) {
+        PagedSeq& s = g.seq[i];
+        const int64_t tiles = tiles_of(s), units = units_of(s);
+        const int64_t n = tiles > share ? (tiles + share - 1) / share : 1, each = (tiles + n - 1) / n;
+        s.nchunk = static_cast<int>(tiles > 0 ? (tiles + each - 1) / each : 1);
+        s.chunk_keys = static_cast<int>((tiles > 0 ? each : 1) * cut.keys);
+        s.part0 = static_cast<int>(part);
+        s.tick0 = static_cast<int>(tick);
+        if (s.nchunk > 1) { part += units * s.nchunk * cut.rows; tick += units; }
+        g.cta0[i] = static_cast<int>(cta);
+        cta += units * s.nchunk;
+    }
+    g.cta0[g.nseq] = static_cast<int>(cta);
+}
+
+extern "C" {
+
+size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh) {
+    if (ctx == nullptr || dh <= 0) return 0;
+    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, DODO_F32, 32));
+    return rows * dodo_paged_part_floats(dh) * sizeof(float);
+}
+
+int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int H, float sm_scale,
+                      const dodo_paged_cache* cache, const int32_t* page_off, const int32_t* cache_len, const void* locK, const void* locV,
+                      const int32_t* loc_off, const int32_t* loc_len, const int32_t* loc_pos0, int loc_rows, int B, void* O, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
+    if (cache == nullptr) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "cache must not be NULL");
+    const int dtype = cache->dtype, dh = cache->dh, Hkv = cache->H;
+    int rc = dodo_check_attend_queries(ctx, q_off, q_pos0, dtype, H, dh, B);
+    if (rc != DODO_OK) return rc;
+    if (Hkv <= 0 || H % Hkv != 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "%d query heads over %d heads of the cache", H, Hkv);
+    if ((rc = dodo_check_paged(ctx, cache, page_off, cache_len, B, false)) != DODO_OK) return rc;
+    bool any_cache = false, any_local = false;
+    for (int b = 0; b < B; ++b) any_cache = any_cache || cache_len[b] > 0;
+    if (any_cache && (rc = dodo_check_paged(ctx, cache, page_off, cache_len, B, true)) != DODO_OK) return rc;
+    if ((rc = dodo_check_attend_keys(ctx, nullptr, nullptr, loc_off, loc_len, loc_pos0, loc_rows, B, &any_cache, &any_local)) != DODO_OK) return rc;
+    if ((rc = dodo_check_positions(ctx, q_off, q_pos0, loc_len, loc_pos0, B)) != DODO_OK) return rc;
+    if (q_off[B] == 0) return DODO_OK;
+    if (Q == nullptr || O == nullptr || !dodo_aligned16(Q) || !dodo_aligned16(O))
+        return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "Q and O must be non-NULL and 16-byte aligned");
+    if (any_local && (locK == nullptr || locV == nullptr || !dodo_aligned16(locK) || !dodo_aligned16(locV)))
+        return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "locK and locV must be non-NULL and 16-byte aligned");
+    for (int b = 0; b < B; ++b)
+        if (static_cast<int64_t>(cache_len[b]) + (loc_len != nullptr ? loc_len[b] : 0) > 0x7ff00000)
+            return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "sequence %d: more than 2^31 - 2^20 keys", b);
+    if ((rc = dodo_check_device(ctx)) != DODO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+    PagedArrays a;
+    memset(&a, 0, sizeof a);
+    a.Q = Q; a.cK = cache->K; a.cV = cache->V; a.lK = locK; a.lV = locV;
+    a.pos = cache->pos; a.table = cache->table;
+    a.pages = cache->pages; a.page = cache->page;
+    int log2 = 0;
+    while ((int64_t{1} << log2) < cache->page) ++log2;
+    a.page_shift = 31 + log2;
+    a.page_mul = static_cast<uint32_t>(((uint64_t{1} << a.page_shift) + cache->page - 1) / cache->page);
+    a.H = H; a.Hkv = Hkv; a.group = H / Hkv;
+    a.scale_log2 = sm_scale * 1.4426950408889634f;
+    a.O = O; a.lse = lse;
+    a.part = static_cast<float*>(workspace);
+    a.tickets = ctx->tickets;
+    a.status = ctx->dev_status;
+    for (int b0 = 0; b0 < B; b0 += DODO_GROUP) {
+        PagedGroup g;
+        g.nseq = B - b0 < DODO_GROUP ? B - b0 : DODO_GROUP;
+        int64_t most = 0;
+        for (int i = 0; i < g.nseq; ++i) {
+            const int b = b0 + i, l = loc_len != nullptr ? loc_len[b] : 0;
+            g.seq[i] = {q_off[b], q_off[b + 1] - q_off[b], q_pos0[b], cache_len[b], page_off[b], l > 0 ? loc_off[b] : 0, l, l > 0 ? loc_pos0[b] : 0, 1, 1, 0, 0};
+            most = most > static_cast<int64_t>(g.seq[i].tq) * a.group ? most : static_cast<int64_t>(g.seq[i].tq) * a.group;
+        }
+        if (most == 0) continue;
+        const int max_rows = most > 0x7fffffff ? 0x7fffffff : static_cast<int>(most);
+        const PagedCut cut = dodo_paged_rows_cut(ctx, dtype, max_rows);
+        dodo_paged_plan(cut, g, a.group, Hkv);
+        bool parts = false;
+        for (int i = 0; i < g.nseq; ++i) parts = parts || (g.seq[i].nchunk > 1 && g.seq[i].tq > 0);
+        const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
+        if (parts && (workspace == nullptr || !dodo_aligned16(workspace) || workspace_bytes < need))
+            return dodo_fail(ctx, DODO_ERR_CAPACITY, "workspace of %zu bytes is too small or misaligned (need %zu)", workspace_bytes, need);
+        if ((rc = dodo_launch_paged_rows(ctx, dtype, dh, max_rows, g, a, st)) != DODO_OK) return rc;
+    }
+    return DODO_OK;
+}
+
+}  // extern "C"

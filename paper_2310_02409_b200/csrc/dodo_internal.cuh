@@ -51,6 +51,7 @@ struct dodo_ctx {
 
 int dodo_fail(dodo_ctx* ctx, int status, const char* fmt, ...);
 int dodo_check_cuda(dodo_ctx* ctx, cudaError_t e, const char* what);
+bool dodo_valid_offsets(const int32_t* off, int B);   // an offset table: from 0, never decreasing
 
 static inline size_t dodo_elem_bytes(int dtype) { return dtype == DODO_F32 ? 4u : 2u; }
 static inline bool dodo_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -1,0 +1,187 @@
+// Attention over a paged cache: tables of a launch, the walk through a sequence's key list, and how a block's results are joined.
+//
+// A unit of work is (sequence, tile of rows, KV head).  Its rows are the (query token, query head of the KV head's group) pairs of
+// the sequence, tokens first: row r is token r / group, head r % group, so that query heads which share a KV head share what is
+// read of it.  Its keys are one list: the rows in use of the cache, then the local tokens that its last query sees.  A long list is
+// cut into chunks, one block each; the blocks of a unit leave partial results in the workspace and the last to arrive joins them,
+// in the chunks' order.
+#pragma once
+
+#include "dodo_internal.cuh"
+
+struct PagedSeq {
+    int q_row0, tq, q_pos0;
+    int c_len, page0;           // rows in use; first entry in the page table
+    int l_row0, l_len, l_pos0;
+    int nchunk, chunk_keys;     // chunks of the key list and the keys of each
+    int part0, tick0;           // first partial row in the workspace, first arrival counter
+};
+struct PagedGroup {
+    int nseq;
+    int cta0[DODO_GROUP + 1];
+    PagedSeq seq[DODO_GROUP];
+};
+struct PagedArrays {
+    const void *Q, *cK, *cV, *lK, *lV;
+    const int32_t *pos, *table;
+    int pages, page;
+    uint32_t page_mul;          // n / page = n * page_mul >> page_shift for n < 2^31
+    int page_shift;
+    int H, Hkv, group;          // query heads, KV heads, H / Hkv
+    float scale_log2;
+    void* O;
+    float* lse;
+    float* part;                // partial rows: [rows][dh], then (maximum, sum) of each
+    int* tickets;
+    int* status;
+};
+// How a launch cuts its work: rows of a tile, keys a chunk is a multiple of, blocks to aim at, keys a chunk has at least
+struct PagedCut { int rows, keys, target, least; };
+void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv);
+static inline size_t dodo_paged_part_rows(const PagedCut& cut) { return static_cast<size_t>(2) * cut.target * cut.rows; }
+// floats of a partial row: dh sums, a maximum and a sum, and two more so that every row of every tile starts on 16 bytes
+static constexpr int dodo_paged_part_floats(int dh) { return dh + 4; }
+
+PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int dtype, int max_rows);
+int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+
+#ifdef __CUDACC__
+namespace dodo_paged {
+
+// where this block works: sequence, tile of rows, KV head, chunk
+struct Place { int b, tile, head, chunk; };
+__device__ __forceinline__ Place place_of(const PagedGroup& g, int Hkv, int bid) {
+    int lo = 0, hi = g.nseq;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.cta0[mid] <= bid) lo = mid; else hi = mid;
+    }
+    Place p;
+    p.b = lo;
+    const int r = bid - g.cta0[lo], n = g.seq[lo].nchunk;
+    p.chunk = r % n;
+    p.head = r / n % Hkv;
+    p.tile = r / n / Hkv;
+    return p;
+}
+
+// A key of the list: `row` of the cache's or the local tokens' arrays, its position; none: row < 0
+struct Key { int row, pos; bool local; };
+constexpr int kNoPos = 0x7fffffff;
+
+// entry of the page table that key j needs, 0 for local tokens
+__device__ __forceinline__ int page_of(const PagedArrays& a, int j) { return static_cast<int>(static_cast<uint64_t>(j) * a.page_mul >> a.page_shift); }
+__device__ __forceinline__ int page_entry(const PagedArrays& a, const PagedSeq& s, int j, int end) {
+    return j < min(end, s.c_len) ? __ldg(a.table + s.page0 + page_of(a, j)) : 0;
+}
+// the key itself, with its page's number at hand
+__device__ __forceinline__ Key key_at(const PagedArrays& a, const PagedSeq& s, int j, int end, int entry) {
+    Key k;
+    k.row = -1; k.pos = kNoPos; k.local = j >= s.c_len;
+    if (j >= end) return k;
+    if (k.local) {
+        k.row = s.l_row0 + (j - s.c_len);
+        k.pos = s.l_pos0 + (j - s.c_len);
+    } else if (static_cast<unsigned>(entry) < static_cast<unsigned>(a.pages)) {
+        k.row = entry * a.page + (j - page_of(a, j) * a.page);
+        k.pos = __ldg(a.pos + k.row);
+    } else {
+        atomicOr(a.status, DODO_DEV_BAD_INDEX);
+    }
+    return k;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// weight of a part whose maximum is m in a whole whose maximum is M
+__device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.f : exp2_fast(m - M); }
+
+template <typename T> __device__ __forceinline__ void store4(T* p, const float* f);
+template <> __device__ __forceinline__ void store4<float>(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, const float* f) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+__device__ __forceinline__ size_t out_row(const PagedArrays& a, const PagedSeq& s, int head, int r) {
+    return static_cast<size_t>(s.q_row0 + r / a.group) * a.H + head * a.group + r % a.group;
+}
+
+// The end of a block of kThreads threads: `parts` partial results of `rows` rows in shared memory (sums of weighted V [part][row][DH]
+// with pitch floats a row, maxima and sums of weights [part][row]) joined into results, or, where the unit is cut, into a partial
+// result of the workspace; the last block of the unit joins those.  Called by all threads, behind a barrier.
+template <typename T, int DH, int kThreads>
+__device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, const Place& p, int tile_rows, int rows, int parts, const float* acc,
+                                       int pitch, const float* mx, const float* sum) {
+    constexpr int kPieces = DH / 4;
+    __shared__ int s_last;
+    const int tid = static_cast<int>(threadIdx.x), r0 = p.tile * tile_rows;
+    const bool whole = s.nchunk == 1;
+    const size_t unit = static_cast<size_t>(p.tile) * a.Hkv + p.head;
+    // partial rows of a chunk: tile_rows rows of DH floats, then a pair of floats each
+    const size_t chunk_floats = static_cast<size_t>(tile_rows) * dodo_paged_part_floats(DH);
+    float* const base = a.part + static_cast<size_t>(s.part0) * dodo_paged_part_floats(DH) + unit * s.nchunk * chunk_floats;
+    float* const mine = base + p.chunk * chunk_floats;
+    for (int i = tid; i < rows * kPieces; i += kThreads) {
+        const int r = i / kPieces, c = i % kPieces * 4;
+        float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < parts; ++w) M = fmaxf(M, mx[w * tile_rows + r]);
+        for (int w = 0; w < parts; ++w) {
+            const float k = part_weight(mx[w * tile_rows + r], M);
+            if (k == 0.f) continue;
+            L = fmaf(k, sum[w * tile_rows + r], L);
+            const float4 v = *reinterpret_cast<const float4*>(acc + (static_cast<size_t>(w) * tile_rows + r) * pitch + c);
+            o[0] = fmaf(k, v.x, o[0]); o[1] = fmaf(k, v.y, o[1]); o[2] = fmaf(k, v.z, o[2]); o[3] = fmaf(k, v.w, o[3]);
+        }
+        if (whole) {
+            const size_t at = out_row(a, s, p.head, r0 + r);
+            const float inv = L != 0.f ? 1.f / L : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            store4(static_cast<T*>(a.O) + at * DH + c, o);
+            if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+        } else {
+            *reinterpret_cast<float4*>(mine + static_cast<size_t>(r) * DH + c) = make_float4(o[0], o[1], o[2], o[3]);
+            if (c == 0) *reinterpret_cast<float2*>(mine + static_cast<size_t>(tile_rows) * DH + 2 * r) = make_float2(M, L);
+        }
+    }
+    if (whole) return;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+        int* const t = a.tickets + s.tick0 + unit;
+        const int arrived = atomicAdd(t, 1);
+        s_last = arrived == s.nchunk - 1;
+        if (s_last) *t = 0;        // clean for the next launch
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    for (int i = tid; i < rows * kPieces; i += kThreads) {
+        const int r = i / kPieces, c = i % kPieces * 4;
+        const float* const ml = base + static_cast<size_t>(tile_rows) * DH + 2 * r;
+        float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int k = 0; k < s.nchunk; ++k) M = fmaxf(M, __ldcg(ml + k * chunk_floats));
+#pragma unroll 8
+        for (int k = 0; k < s.nchunk; ++k) {
+            const float2 q = __ldcg(reinterpret_cast<const float2*>(ml + k * chunk_floats));
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(base + k * chunk_floats + static_cast<size_t>(r) * DH + c));
+            const float w = part_weight(q.x, M);
+            L = fmaf(w, q.y, L);
+            o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[2] = fmaf(w, v.z, o[2]); o[3] = fmaf(w, v.w, o[3]);
+        }
+        const size_t at = out_row(a, s, p.head, r0 + r);
+        const float inv = L != 0.f ? 1.f / L : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= inv;
+        store4(static_cast<T*>(a.O) + at * DH + c, o);
+        if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+}  // namespace dodo_paged
+#endif
