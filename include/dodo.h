@@ -515,8 +515,8 @@ DODO_API int dodo_gather_kv_paged(dodo_ctx* ctx, const void* K, const void* V, i
  * h / (H / cache->H) of the cache and of locK / locV [loc_rows, cache->H, dh].  Masks, empty rows, O and lse as in dodo_attend;
  * what a query does not see takes no part in its result, whatever it holds.  A key whose logit is -infinity counts as one not seen.
  *   cache      its dtype and dh are those of Q, O and the local tokens; with no rows in use its arrays may be NULL
- *   workspace  [device] at least dodo_attend_paged_workspace_bytes(ctx, dh) bytes, 16-byte aligned, contents free; needed only where
- *              a key list is cut (DODO_ERR_CAPACITY when it is and the workspace is too small)
+ *   workspace  [device] 16-byte aligned, contents free; with dodo_attend_paged_workspace_bytes(ctx, dh) bytes long key lists are cut
+ *              into pieces for several thread blocks, with fewer (NULL, 0) none is: the same results up to the order of sums, later
  *   everything else as in dodo_attend, except that nothing is read ahead of what precedes the call on its stream
  * Positions of queries and local tokens lie in [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache pos may hold anything.  bf16: weights are
  * rounded to bf16 before their product with V.  Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}; H a multiple of cache->H.

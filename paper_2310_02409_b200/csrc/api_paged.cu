@@ -6,7 +6,8 @@ int dodo_check_paged(dodo_ctx* ctx, const dodo_paged_cache* c, const int32_t* pa
 // Chunks of each sequence's key list, blocks, partial rows and arrival counters.  A list is cut where it is longer than a block's share of
 // all the work (units times keys over the blocks to aim at), into chunks of about that share, all alike.  A cut list has more than one share,
 // so its chunks are fewer than twice its shares and the chunks of all cut units fewer than twice the target: dodo_paged_part_rows.
-void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv) {
+// Without room for partial rows no list is cut.
+void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, bool may_cut) {
     auto tiles_of = [&](const PagedSeq& s) {
         const int64_t keys = static_cast<int64_t>(s.c_len) + dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1);
         return (keys + cut.keys - 1) / cut.keys;
@@ -20,7 +21,7 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv) {
     for (int i = 0; i < g.nseq; ++i) {
         PagedSeq& s = g.seq[i];
         const int64_t tiles = tiles_of(s), units = units_of(s);
-        const int64_t n = tiles > share ? (tiles + share - 1) / share : 1, each = (tiles + n - 1) / n;
+        const int64_t n = may_cut && tiles > share ? (tiles + share - 1) / share : 1, each = (tiles + n - 1) / n;
         s.nchunk = static_cast<int>(tiles > 0 ? (tiles + each - 1) / each : 1);
         s.chunk_keys = static_cast<int>((tiles > 0 ? each : 1) * cut.keys);
         s.part0 = static_cast<int>(part);
@@ -32,12 +33,15 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv) {
     g.cta0[g.nseq] = static_cast<int>(cta);
 }
 
+namespace { constexpr int kFewRows = 16; }
+
 extern "C" {
 
 size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh) {
     if (ctx == nullptr || dh <= 0) return 0;
-    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, DODO_F32, 32));
-    return rows * dodo_paged_part_floats(dh) * sizeof(float);
+    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, DODO_F32, 32)) * dodo_paged_part_floats(dh) * sizeof(float);
+    const size_t dense = dodo_paged_dense_workspace_bytes(ctx->num_sms, dh);
+    return rows > dense ? rows : dense;
 }
 
 int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int H, float sm_scale,
@@ -51,9 +55,9 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
     if (rc != DODO_OK) return rc;
     if (Hkv <= 0 || H % Hkv != 0) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "%d query heads over %d heads of the cache", H, Hkv);
     if ((rc = dodo_check_paged(ctx, cache, page_off, cache_len, B, false)) != DODO_OK) return rc;
-    bool any_cache = false, any_local = false;
-    for (int b = 0; b < B; ++b) any_cache = any_cache || cache_len[b] > 0;
-    if (any_cache && (rc = dodo_check_paged(ctx, cache, page_off, cache_len, B, true)) != DODO_OK) return rc;
+    bool any_rows = false, any_cache = false, any_local = false;
+    for (int b = 0; b < B; ++b) any_rows = any_rows || cache_len[b] > 0;
+    if (any_rows && (rc = dodo_check_paged(ctx, cache, page_off, cache_len, B, true)) != DODO_OK) return rc;
     if ((rc = dodo_check_attend_keys(ctx, nullptr, nullptr, loc_off, loc_len, loc_pos0, loc_rows, B, &any_cache, &any_local)) != DODO_OK) return rc;
     if ((rc = dodo_check_positions(ctx, q_off, q_pos0, loc_len, loc_pos0, B)) != DODO_OK) return rc;
     if (q_off[B] == 0) return DODO_OK;
@@ -64,12 +68,15 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
     for (int b = 0; b < B; ++b)
         if (static_cast<int64_t>(cache_len[b]) + (loc_len != nullptr ? loc_len[b] : 0) > 0x7ff00000)
             return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "sequence %d: more than 2^31 - 2^20 keys", b);
+    if (!dodo_aligned16(workspace)) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     if ((rc = dodo_check_device(ctx)) != DODO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 
     PagedArrays a;
     memset(&a, 0, sizeof a);
-    a.Q = Q; a.cK = cache->K; a.cV = cache->V; a.lK = locK; a.lV = locV;
+    a.Q = Q; a.O = O;
+    a.cK = any_rows ? cache->K : nullptr; a.cV = any_rows ? cache->V : nullptr;
+    a.lK = any_local ? locK : nullptr; a.lV = any_local ? locV : nullptr;
     a.pos = cache->pos; a.table = cache->table;
     a.pages = cache->pages; a.page = cache->page;
     int log2 = 0;
@@ -78,7 +85,7 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
     a.page_mul = static_cast<uint32_t>(((uint64_t{1} << a.page_shift) + cache->page - 1) / cache->page);
     a.H = H; a.Hkv = Hkv; a.group = H / Hkv;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
-    a.O = O; a.lse = lse;
+    a.lse = lse;
     a.part = static_cast<float*>(workspace);
     a.tickets = ctx->tickets;
     a.status = ctx->dev_status;
@@ -93,13 +100,15 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
         }
         if (most == 0) continue;
         const int max_rows = most > 0x7fffffff ? 0x7fffffff : static_cast<int>(most);
+        // Many bf16 rows are a contraction: the tensor cores.  (Row maxima are taken before scaling, so the scale must be positive.)
+        if (dtype == DODO_BF16 && max_rows > kFewRows && sm_scale >= DODO_DENSE_LEAST_SCALE && workspace != nullptr &&
+            workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh)) {
+            if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
+            continue;
+        }
         const PagedCut cut = dodo_paged_rows_cut(ctx, dtype, max_rows);
-        dodo_paged_plan(cut, g, a.group, Hkv);
-        bool parts = false;
-        for (int i = 0; i < g.nseq; ++i) parts = parts || (g.seq[i].nchunk > 1 && g.seq[i].tq > 0);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
-        if (parts && (workspace == nullptr || !dodo_aligned16(workspace) || workspace_bytes < need))
-            return dodo_fail(ctx, DODO_ERR_CAPACITY, "workspace of %zu bytes is too small or misaligned (need %zu)", workspace_bytes, need);
+        dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);
         if ((rc = dodo_launch_paged_rows(ctx, dtype, dh, max_rows, g, a, st)) != DODO_OK) return rc;
     }
     return DODO_OK;

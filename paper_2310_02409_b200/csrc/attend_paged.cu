@@ -170,6 +170,7 @@ attend_paged_rows_kernel(const __grid_constant__ PagedGroup g, const __grid_cons
     }
 #pragma unroll
     for (int o = COPY; o < COPY * U; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (l != l) m = INFINITY;        // a NaN among the logits that the row sees: the whole row's, wherever its maximum stands
     constexpr int kPitch = DH + 4;
     float* const mx = smem + static_cast<size_t>(key_warps) * tile_rows * kPitch;
     float* const sum = mx + key_warps * tile_rows;

@@ -1,0 +1,738 @@
+// Attention of many rows over a paged cache on the 5th-generation tensor cores (bf16; rows = query tokens x query heads of a KV head).
+//
+// Work is counted in slots, one per tile of 128 keys of a unit (sequence, KV head, tile of rows); the units are laid end to end and
+// thread block c of G, one per SM, takes the slots [c T / G, (c+1) T / G) whatever units they fall in.  A unit that a block boundary
+// cuts is finished through partial results in the workspace; the last of its blocks to arrive joins them.  Nobody waits for anybody.
+//
+// A block holds two score streams: S = Q K^T [128 rows x 128 keys] of stream s in tensor-memory columns [128 s, 128 s + 128), its
+// P (bf16 pairs) over the first 64 of them, O at [256 + DH s, ...).  With more than 128 rows the streams are the two halves of a tile
+// of 256 rows, which share every K and V tile (half the operand traffic from L2); with fewer they take the key tiles in turn and are
+// added at the end.  While one stream's softmax runs, the tensor core works for the other.  Roles, each a warp or more:
+//   producer (warp 8)  walks the key list: 32 lanes look four keys each up (page, position), skip tiles that no query sees, write the
+//       tile's positions to shared memory, and bring K and V rows by four-row gather copies (tile::gather4) with the 128-byte swizzle.
+//       A key that no query of the tile sees, or that is not there, is replaced by one that is.
+//   matrix issuer (warp 9)  the whole warp walks the same list, one elected lane issues: every operand of an instruction then lies in
+//       uniform registers.  Per tile and stream O += P V, then S = Q K^T of the stream's next tile.
+//   softmax (warps 0-3 and 4-7)  a thread is a row: its 128 scores in registers, the running maximum and sum in 32 bits, maximum moved
+//       (and O rescaled in tensor memory) only when it grew by more than 2^8.  Weights are rounded to bf16 for P V (the sum is not): at
+//       most 2^-8 of each, the rounding of the result itself.
+// Masked scores are -infinity; in the product their weight 0 times a NaN or an infinity of V is a NaN all the same (keys that some
+// rows of a tile see and others do not), so results that are not finite are summed again on the FMA units over what their row sees.
+// Every wait is bounded: on time-out a role leaves its loop, the status word is set, tensor memory is freed.
+#include "paged.cuh"
+#include "sm100_ptx.cuh"
+
+namespace {
+
+using namespace sm100;
+using namespace dodo_paged;
+
+constexpr int BM = 128, BN = 128;
+constexpr int kSoftmaxWarps = 8, kThreads = 32 * (kSoftmaxWarps + 4);      // the last two warps only hand registers over
+// Registers of a thread: the launch's 168 a thread (384 threads), shared out anew between two warpgroups of softmax threads (a row's 128
+// scores) and the one of the others: 216 + 216 + 72 = 3 x 168
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+constexpr int kPosSlots = 4;
+constexpr float kRescaleStep = 8.f;
+enum { kFull = 0, kMasked = 1, kEnd = 2 };
+
+template <int DH, int TILES>
+struct Layout {
+    static constexpr int kHalves = DH / 64;
+    static constexpr int kTile = BN * DH * 2;                 // bytes of 128 rows
+    static constexpr int kHalf = BN * 128;                    // 64 columns of them
+    static constexpr int kKStages = TILES == 1 || DH == 64 ? 3 : 2, kVStages = TILES == 1 && DH == 128 ? 2 : kKStages;
+    static constexpr int kOffK = TILES * kTile, kOffV = kOffK + kKStages * kTile, kOffPos = kOffV + kVStages * kTile;
+    static constexpr int kOffXch = kOffPos + kPosSlots * BN * 4;      // maxima and sums that the streams of one tile of rows exchange
+    static constexpr int kBytes = kOffXch + (TILES == 1 ? 2 * 2 * BM * 4 : 0);
+    static constexpr int kRows = TILES * BM;
+    static constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (DH + 2);
+};
+
+struct DenseShare {
+    int total;                      // slots
+    int slot0[DODO_GROUP + 1];      // first slot of each sequence
+    int nt[DODO_GROUP];             // slots of a unit of the sequence
+    int tiles[DODO_GROUP];          // tiles of rows
+};
+struct Maps { CUtensorMap cK, cV, lK, lV; };
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(smem_u32(bar))
+        : "memory");
+}
+// 64 columns of this warp's 32 lanes; the wait for them is in the same statement, so that nothing reads them ahead of it
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+          "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+          "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+          "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]),
+          "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]),
+          "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]),
+          "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// a wait of the whole warp: the same answer in every lane
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+// barrier of the softmax threads that tells each whether any of them said so
+__device__ __forceinline__ bool any_softmax(bool mine) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(mine ? 1u : 0u) : "memory");
+    return r != 0u;
+}
+
+__device__ __forceinline__ int block_start(int T, int G, int c) { return static_cast<int>(static_cast<long long>(c) * T / G); }
+__device__ __forceinline__ int block_of(int T, int G, int x) {   // the block whose range holds slot x
+    return static_cast<int>(((static_cast<long long>(x) + 1) * G - 1) / T);
+}
+
+// A unit's share of a block: its rows, its key list, the tiles [t0, t1) of it
+struct Segment {
+    int b, head, tile;
+    int first_slot, nt, t0, t1;     // slot of the unit's first tile; tiles of the unit
+    int rows, r0;                   // rows of this tile of rows and the first
+    int min_pos, last_pos;          // positions of its first and last row
+    int l_vis, c_pad;               // local tokens that its last row sees; rows in use, in fours
+};
+// walks the segments of slots [x, end)
+__device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int tile_rows, int& x, int end, Segment& q) {
+    if (x >= end) return false;
+    int lo = 0, hi = g.nseq;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (w.slot0[mid] <= x) lo = mid; else hi = mid;
+    }
+    const PagedSeq& s = g.seq[lo];
+    const int off = x - w.slot0[lo], unit = off / w.nt[lo];
+    q.b = lo;
+    q.tile = unit % w.tiles[lo];
+    q.head = unit / w.tiles[lo];
+    q.nt = w.nt[lo];
+    q.t0 = off - unit * q.nt;
+    q.first_slot = x - q.t0;
+    q.t1 = min(q.nt, q.t0 + end - x);
+    q.r0 = q.tile * tile_rows;
+    q.rows = min(tile_rows, s.tq * a.group - q.r0);
+    q.min_pos = s.q_pos0 + q.r0 / a.group;
+    q.last_pos = s.q_pos0 + (q.r0 + q.rows - 1) / a.group;
+    q.c_pad = (s.c_len + 3) & ~3;
+    q.l_vis = dodo_visible_local(s.l_len, s.l_pos0, q.last_pos);
+    x += q.t1 - q.t0;
+    return true;
+}
+
+// One row again over all of the unit's keys that it sees: a warp, a key a lane for the scores, four (two) features a lane for the sums
+template <int DH>
+__device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, __nv_bfloat16* out) {
+    constexpr int F = DH / 32;
+    const int lane = static_cast<int>(threadIdx.x) & 31;
+    const size_t pitch = static_cast<size_t>(a.Hkv) * DH, at = static_cast<size_t>(head) * DH;
+    const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, head, r) * DH;
+    const int qpos = s.q_pos0 + r / a.group, end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
+    float m = -INFINITY, l = 0.f, acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = 0.f;
+#pragma unroll 1
+    for (int j0 = 0; j0 < end; j0 += 32) {
+        const Key k = key_at(a, s, j0 + lane, end, page_entry(a, s, j0 + lane, end));
+        const bool sees = k.row >= 0 && k.pos <= qpos;
+        float x = -INFINITY;
+        if (sees) {
+            const __nv_bfloat16* const kr = static_cast<const __nv_bfloat16*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
+            x = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < DH; c += 8) {
+                float kf[8], qf[8];
+                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(kr + c)), kf);
+                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(q + c)), qf);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x = fmaf(kf[e], qf[e], x);
+            }
+            x *= a.scale_log2;
+        }
+        float top = fmaxf(m, x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == -INFINITY ? 0.f : top, corr = part_weight(m, ref), w = exp2_fast(x - ref);
+        m = top;
+        l = fmaf(l, corr, w);
+        const float rounded = __bfloat162float(__float2bfloat16_rn(w));
+#pragma unroll
+        for (int f = 0; f < F; ++f) acc[f] *= corr;
+        uint32_t seen = __ballot_sync(0xffffffffu, sees);
+        while (seen != 0u) {
+            const int e = __ffs(seen) - 1;
+            seen &= seen - 1u;
+            const int row = __shfl_sync(0xffffffffu, k.row, e);
+            const bool local = __shfl_sync(0xffffffffu, k.local ? 1 : 0, e) != 0;
+            const float c = __shfl_sync(0xffffffffu, rounded, e);
+            const __nv_bfloat16* const vr = static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
+#pragma unroll
+            for (int f = 0; f < F; ++f) acc[f] = fmaf(c, __bfloat162float(vr[f]), acc[f]);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int f = 0; f < F; ++f) out[lane * F + f] = __float2bfloat16_rn(acc[f] * inv);
+}
+
+template <int DH, int TILES>
+__global__ void __launch_bounds__(kThreads, 1)
+attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
+                          const __grid_constant__ DenseShare work) {
+    using L = Layout<DH, TILES>;
+    constexpr int H2 = L::kHalves;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
+        bar_vfree[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_kkind[L::kKStages], s_kind[kPosSlots], s_last;
+    int* const s_pos = reinterpret_cast<int*>(base_ptr + L::kOffPos);
+
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const int T = work.total, G = static_cast<int>(gridDim.x), bid = static_cast<int>(blockIdx.x);
+    const int slot_end = block_start(T, G, bid + 1);
+    int x = block_start(T, G, bid);
+
+    if (tid == 0) {
+        mbar_init(&bar_q, kSoftmaxWarps);
+        mbar_init(&bar_o, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i], 4); }
+        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], 1); }
+        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], 1); }
+        for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kSoftmaxWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    bool stuck = false;
+    Segment q;
+
+    if (warp == kSoftmaxWarps) {
+        // ================================================ producer ================================================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        int ck = 0, cv = 0;            // K tiles (ends of segments among them) and V tiles so far
+        while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+            const PagedSeq& s = g.seq[q.b];
+            const int local_end = q.c_pad + q.l_vis, col = q.head * DH;
+            // a lane's four keys of tile t: page entries first, rows and positions a tile later, copies after that
+            int entry[4], row[4], pos[4];
+            bool local = false;
+            auto entries = [&](int t) {
+                const int v = t * BN + 4 * lane;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) entry[e] = t < q.t1 ? page_entry(a, s, v + e, s.c_len) : 0;
+            };
+            auto keys = [&](int t) {
+                const int v = t * BN + 4 * lane;
+                local = v >= q.c_pad;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    row[e] = -1; pos[e] = kNoPos;
+                    if (t >= q.t1) continue;
+                    if (local) {
+                        if (v + e < local_end) { row[e] = s.l_row0 + (v + e - q.c_pad); pos[e] = s.l_pos0 + (v + e - q.c_pad); }
+                    } else {
+                        const Key k = key_at(a, s, v + e, s.c_len, entry[e]);
+                        row[e] = k.row; pos[e] = k.pos;
+                    }
+                }
+            };
+            entries(q.t0);
+            keys(q.t0);
+            entries(q.t0 + 1);
+            for (int t = q.t0; t < q.t1; ++t) {
+                int r[4], p[4], lo = kNoPos, hi = static_cast<int>(0x80000000);
+                bool from_local = local;
+                int first = -1;
+#pragma unroll
+                for (int e = 3; e >= 0; --e) {
+                    const bool there = row[e] >= 0 && pos[e] <= q.last_pos;
+                    r[e] = there ? row[e] : -1;
+                    p[e] = there ? pos[e] : kNoPos;
+                    lo = min(lo, p[e]);
+                    hi = max(hi, p[e]);
+                    if (there) first = row[e];
+                }
+                if (t + 1 < q.t1) { keys(t + 1); entries(t + 2); }
+                const uint32_t has = __ballot_sync(0xffffffffu, first >= 0);
+                if (has == 0u) continue;                    // nobody sees a key of this tile
+                const bool masked = __any_sync(0xffffffffu, hi > q.min_pos);
+                const int donor = __ffs(has) - 1, spare = __shfl_sync(0xffffffffu, first, donor);
+                const bool spare_local = __shfl_sync(0xffffffffu, from_local ? 1 : 0, donor) != 0;
+                if (first < 0) { first = spare; from_local = spare_local; }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = r[e] >= 0 ? r[e] : first;
+
+                const int ks = ck % L::kKStages, vs = cv % L::kVStages, ps = ck % kPosSlots;
+                if (!warp_wait(&bar_kfree[ks], static_cast<uint32_t>(ck / L::kKStages + 1) & 1u)) { stuck = true; break; }
+                if (lane == 0) { s_kkind[ks] = kFull; mbar_expect_tx(&bar_kfull[ks], L::kTile); }
+                __syncwarp();
+                const uint32_t dk = base + L::kOffK + ks * L::kTile + lane * 512;
+#pragma unroll
+                for (int h = 0; h < H2; ++h) gather4(dk + h * L::kHalf, from_local ? &maps.lK : &maps.cK, col + 64 * h, r[0], r[1], r[2], r[3], &bar_kfull[ks]);
+                if (!warp_wait(&bar_posfree[ps], static_cast<uint32_t>(ck / kPosSlots + 1) & 1u)) { stuck = true; break; }
+                *reinterpret_cast<int4*>(s_pos + ps * BN + 4 * lane) = make_int4(p[0], p[1], p[2], p[3]);
+                if (lane == 0) s_kind[ps] = masked ? kMasked : kFull;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar_posfull[ps]);
+                if (!warp_wait(&bar_vfree[vs], static_cast<uint32_t>(cv / L::kVStages + 1) & 1u)) { stuck = true; break; }
+                if (lane == 0) mbar_expect_tx(&bar_vfull[vs], L::kTile);
+                __syncwarp();
+                const uint32_t dv = base + L::kOffV + vs * L::kTile + lane * 512;
+#pragma unroll
+                for (int h = 0; h < H2; ++h) gather4(dv + h * L::kHalf, from_local ? &maps.lV : &maps.cV, col + 64 * h, r[0], r[1], r[2], r[3], &bar_vfull[vs]);
+                ++ck;
+                ++cv;
+            }
+            if (stuck) break;
+            // the segment's end
+            const int ks = ck % L::kKStages, ps = ck % kPosSlots;
+            if (!warp_wait(&bar_kfree[ks], static_cast<uint32_t>(ck / L::kKStages + 1) & 1u) ||
+                !warp_wait(&bar_posfree[ps], static_cast<uint32_t>(ck / kPosSlots + 1) & 1u)) { stuck = true; break; }
+            if (lane == 0) {
+                s_kkind[ks] = kEnd;
+                s_kind[ps] = kEnd;
+                mbar_arrive(&bar_kfull[ks]);
+                mbar_arrive(&bar_posfull[ps]);
+            }
+            __syncwarp();
+            ++ck;
+        }
+        if (stuck) {         // copies in flight land before the block's shared memory goes
+            for (int i = max(0, ck - L::kKStages + 1); i <= ck; ++i) warp_wait(&bar_kfull[i % L::kKStages], static_cast<uint32_t>(i / L::kKStages) & 1u);
+            for (int i = max(0, cv - L::kVStages + 1); i <= cv; ++i) warp_wait(&bar_vfull[i % L::kVStages], static_cast<uint32_t>(i / L::kVStages) & 1u);
+        }
+    } else if (warp == kSoftmaxWarps + 1) {
+        // ================================================ matrix issuer ===========================================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        int ck = 0, cv = 0, np[2] = {0, 0}, segs = 0;
+        const uint32_t idesc_s = idesc_bf16(BN, false), idesc_o = idesc_bf16(DH, true);
+        auto wait_k = [&](int c) {      // kind of the K tile, kEnd when the wait ran out
+            if (!warp_wait(&bar_kfull[c % L::kKStages], static_cast<uint32_t>(c / L::kKStages) & 1u)) { stuck = true; return static_cast<int>(kEnd); }
+            const int kind = s_kkind[c % L::kKStages];
+            __syncwarp();
+            return kind;
+        };
+        auto scores = [&](int st, int qtile, int c, bool last_user) {
+            tc_fence_after();
+            const uint64_t da = desc_kmajor(base + qtile * L::kTile), db = desc_kmajor(base + L::kOffK + (c % L::kKStages) * L::kTile);
+            if (elect_one()) {
+#pragma unroll
+                for (int i = 0; i < DH / 16; ++i) {
+                    const uint64_t step = static_cast<uint64_t>(((i / 4) * L::kHalf + (i % 4) * 32) >> 4);
+                    mma_bf16(tmem + st * BN, da + step, db + step, idesc_s, i > 0);
+                }
+                mma_commit(&bar_s[st]);
+                if (last_user) mma_commit(&bar_kfree[c % L::kKStages]);
+            }
+            __syncwarp();
+        };
+        auto values = [&](int st, int c, bool add, bool last_user) {
+            tc_fence_after();
+            const uint64_t db = desc_mnmajor(base + L::kOffV + (c % L::kVStages) * L::kTile, L::kHalf);
+            if (elect_one()) {
+#pragma unroll
+                for (int i = 0; i < BN / 16; ++i)       // 16 keys of P = 8 columns of bf16 pairs
+                    mma_bf16_ts(tmem + 2 * BN + st * DH, tmem + st * BN + i * 8, db + static_cast<uint64_t>((i * 2048) >> 4), idesc_o, add || i > 0);
+                if (last_user) mma_commit(&bar_vfree[c % L::kVStages]);
+            }
+            __syncwarp();
+        };
+        auto wait_p = [&](int st) {
+            if (!warp_wait(&bar_p[st], static_cast<uint32_t>(np[st]) & 1u)) stuck = true;
+            ++np[st];
+        };
+        auto wait_v = [&](int c) { if (!warp_wait(&bar_vfull[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true; };
+        auto free_end = [&](int c) {     // nothing reads the slot of a segment's end
+            if (lane == 0) mbar_arrive(&bar_kfree[c % L::kKStages]);
+            __syncwarp();
+        };
+        while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+            if (!warp_wait(&bar_q, static_cast<uint32_t>(segs) & 1u)) { stuck = true; break; }
+            ++segs;
+            if constexpr (TILES == 2) {
+                const int streams = q.rows > BM ? 2 : 1;
+                int kind = wait_k(ck);
+                if (kind == kEnd) { free_end(ck); ++ck; continue; }
+                for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
+                bool add = false;
+                while (!stuck) {
+                    ++ck;                                  // the next tile
+                    for (int st = 0; st < streams; ++st) {
+                        wait_p(st);
+                        if (st == 0) wait_v(cv);
+                        values(st, cv, add, st == streams - 1);
+                        if (st == 0) kind = wait_k(ck);
+                        if (kind != kEnd) scores(st, st, ck, st == streams - 1);
+                    }
+                    ++cv;
+                    add = true;
+                    if (kind == kEnd) { free_end(ck); break; }
+                }
+                ++ck;
+            } else {
+                // tile i of the segment belongs to stream i & 1; scores run two tiles ahead of the values
+                int i = 0, ahead = 0;
+                bool ended = false;
+                auto next_scores = [&]() {
+                    if (ended) return;
+                    if (wait_k(ck) == kEnd) { ended = true; free_end(ck); }
+                    else { scores(ahead & 1, 0, ck, true); ++ahead; }
+                    ++ck;
+                };
+                next_scores();
+                next_scores();
+                if (ahead == 0) continue;
+                while (!stuck && i < ahead) {
+                    wait_p(i & 1);
+                    wait_v(cv);
+                    values(i & 1, cv, i >= 2, true);
+                    ++cv;
+                    ++i;
+                    next_scores();
+                }
+            }
+            if (elect_one()) mma_commit(&bar_o);
+            __syncwarp();
+        }
+    } else if (warp < kSoftmaxWarps) {
+        // ================================================ softmax =================================================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        const int st = warp >> 2, row = tid & (BM - 1);
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, t_s = tmem + st * BN + lanes, t_o = tmem + 2 * BN + lanes;
+        float* const xch = reinterpret_cast<float*>(base_ptr + L::kOffXch);
+        const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
+        int ck = 0, ns = 0, os = 0;
+        bool first_seg = true;
+        // (a wait that has run out ends the waiting, not the walk: the barriers of these warps count all of them)
+        while (next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+            const PagedSeq& s = g.seq[q.b];
+            const int my = (TILES == 2 ? st * BM : 0) + row;               // this thread's row of the tile of rows
+            const bool live = my < q.rows, stream_live = TILES == 1 || st * BM < q.rows, warp_live = (TILES == 2 ? st * BM : 0) + (row & ~31) < q.rows;
+            const int qpos = s.q_pos0 + (q.r0 + min(my, q.rows - 1)) / a.group;
+            // ---- Q, row by row, in the layout of the matrix unit's operands (128-byte rows of 64 features, 16-byte pieces swizzled)
+            {
+                constexpr int kPieces = (TILES == 2 ? DH : DH / 2) / 8;
+                const int piece0 = TILES == 2 ? 0 : st * kPieces;
+                const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, q.head, q.r0 + min(my, q.rows - 1)) * DH);
+                unsigned char* const dst = base_ptr + (TILES == 2 ? st * L::kTile : 0) + row * 128;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int c = piece0 + i;
+                    const uint4 v = live ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(dst + (c / 8) * L::kHalf + (((c % 8) ^ (row & 7)) << 4)) = v;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar_q);
+            }
+            float m = -INFINITY, l = 0.f;
+            int mine = 0, tiles = 0;         // tiles of this stream; of the segment
+            while (!stuck) {
+                const int ps = ck % kPosSlots;
+                if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(ck / kPosSlots) & 1u)) { stuck = true; break; }
+                const int kind = s_kind[ps];
+                ++ck;
+                if (kind == kEnd || !stream_live || (TILES == 1 && (tiles & 1) != st)) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar_posfree[ps]);
+                    if (kind == kEnd) break;
+                    ++tiles;
+                    continue;
+                }
+                ++tiles;
+                if (!warp_wait(&bar_s[st], static_cast<uint32_t>(ns) & 1u)) { stuck = true; break; }
+                ++ns;
+                tc_fence_after();
+                if (warp_live) {
+                    uint32_t sv[BN];
+                    tmem_ld64(t_s, sv);
+                    tmem_ld64(t_s + 64, sv + 64);
+                    if (kind == kMasked) {
+#pragma unroll
+                        for (int c = 0; c < BN; c += 4) {
+                            const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
+                            if (kp.x > qpos) sv[c] = 0xff800000u;
+                            if (kp.y > qpos) sv[c + 1] = 0xff800000u;
+                            if (kp.z > qpos) sv[c + 2] = 0xff800000u;
+                            if (kp.w > qpos) sv[c + 3] = 0xff800000u;
+                        }
+                    }
+                    float t4[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) t4[c] = fmaxf(__uint_as_float(sv[c]), __uint_as_float(sv[c + 4]));
+#pragma unroll
+                    for (int c = 8; c < BN; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) t4[e] = max3(t4[e], __uint_as_float(sv[c + e]), __uint_as_float(sv[c + 4 + e]));
+                    const float top = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * a.scale_log2;      // -infinity stays what it is: the scale is positive
+                    const bool grow = top > m + kRescaleStep;
+                    const float m_new = grow ? top : m;
+                    if (mine > 0 && __any_sync(0xffffffffu, grow)) {
+                        // P V of this stream's tile before is complete: its scores of this tile were issued behind it
+                        const float corr = grow ? part_weight(m, m_new) : 1.f;
+                        l *= corr;
+#pragma unroll 1
+                        for (int c = 0; c < DH; c += 32) {
+                            uint32_t ov[32];
+                            tmem_ld32(t_o + st * DH + c, ov);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+                            tmem_st32(t_o + st * DH + c, ov);
+                        }
+                    }
+                    m = m_new;
+                    const float nm = m == -INFINITY ? 0.f : -m;
+                    const float2 nm2 = make_float2(nm, nm);
+                    float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < BN; c += 4) {
+                        const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c2, nm2);
+                        const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), c2, nm2);
+                        const float2 p0 = make_float2(exp2_fast(x0.x), exp2_fast(x0.y));
+                        const float2 p1 = make_float2(exp2_fast(x1.x), exp2_fast(x1.y));
+                        sv[c / 2] = pack_bf16(p0.x, p0.y);
+                        sv[c / 2 + 1] = pack_bf16(p1.x, p1.y);
+                        sum0 = __fadd2_rn(sum0, p0);
+                        sum1 = __fadd2_rn(sum1, p1);
+                    }
+                    tmem_st32(t_s, sv);
+                    tmem_st32(t_s + 32, sv + 32);
+                    l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+                    tc_fence_before();
+                }
+                ++mine;
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(&bar_posfree[ps]); mbar_arrive(&bar_p[st]); }
+            }
+            if (tiles > 0) {
+                if (!stuck && !warp_wait(&bar_o, static_cast<uint32_t>(os) & 1u)) stuck = true;
+                ++os;
+                tc_fence_after();
+            }
+            if (l != l) m = INFINITY;        // a NaN among the logits that the row sees: the whole row's, wherever its maximum stands
+            // ---- a row's result: of its stream, or of both, each thread then half of the features
+            constexpr int kFeat = TILES == 2 ? DH : DH / 2;
+            const int f0 = TILES == 2 ? 0 : st * kFeat;
+            float w0 = 1.f, w1 = 0.f, M = m, S = l;        // weights of stream 0 (or the own one) and 1
+            if constexpr (TILES == 1) {
+                xch[st * 2 * BM + row] = m;
+                xch[st * 2 * BM + BM + row] = l;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const float om = xch[(st ^ 1) * 2 * BM + row], ol = xch[(st ^ 1) * 2 * BM + BM + row];
+                M = fmaxf(m, om);
+                const float a0 = part_weight(m, M), a1 = part_weight(om, M);
+                S = (a0 != 0.f ? a0 * l : 0.f) + (a1 != 0.f ? a1 * ol : 0.f);
+                w0 = st == 0 ? a0 : a1;
+                w1 = st == 0 ? a1 : a0;
+            }
+            const bool whole = q.t0 == 0 && q.t1 == q.nt;
+            const float inv = S != 0.f ? 1.f / S : 0.f;
+            const size_t at = live ? out_row(a, s, q.head, q.r0 + my) : 0;
+            float* const part = a.part + static_cast<size_t>(2 * bid + (first_seg ? 0 : 1)) * L::kPartFloats;
+            bool odd = false;                              // a result that is not finite
+#pragma unroll 1
+            for (int c = f0; c < f0 + kFeat && warp_live; c += 32) {
+                float o[32];
+                if (TILES == 2 ? mine == 0 : tiles == 0) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                } else {
+                    uint32_t ov[32];
+                    tmem_ld32(t_o + (TILES == 2 ? st * DH : 0) + c, ov);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = TILES == 2 ? __uint_as_float(ov[e]) : w0 != 0.f ? w0 * __uint_as_float(ov[e]) : 0.f;
+                    if (TILES == 1 && tiles > 1) {
+                        tmem_ld32(t_o + DH + c, ov);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = w1 != 0.f ? fmaf(w1, __uint_as_float(ov[e]), o[e]) : o[e];
+                    }
+                }
+                if (whole) {
+                    float zero = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) { o[e] *= inv; zero = fmaf(o[e], 0.f, zero); }
+                    odd = odd || !(zero == 0.f);
+                    if (live) {
+                        uint4* const dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + at * DH + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            dst[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
+                                                pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) part[static_cast<size_t>(c + e) * L::kRows + my] = o[e];
+                }
+            }
+            if (TILES == 2 || st == 0) {
+                if (whole) {
+                    if (live && a.lse != nullptr) a.lse[at] = S != 0.f ? (M + log2f(S)) * 0.6931471805599453f : -INFINITY;
+                } else {
+                    part[static_cast<size_t>(DH) * L::kRows + my] = M;
+                    part[static_cast<size_t>(DH + 1) * L::kRows + my] = S;
+                }
+            }
+            bool done = whole;
+            if (!whole) {
+                const int c_first = block_of(T, G, q.first_slot), c_last = block_of(T, G, q.first_slot + q.nt - 1);
+                __threadfence();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (tid == 0) {
+                    // a block's last unit is the only one that begins in it and goes on: the block's number names it
+                    const int arrived = atomicAdd(a.tickets + c_first, 1);
+                    s_last = arrived == c_last - c_first;
+                    if (s_last) a.tickets[c_first] = 0;    // clean for the next launch
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                done = s_last != 0;
+                if (done && warp_live) {
+                    __threadfence();
+                    auto piece = [&](int c) { return a.part + static_cast<size_t>(2 * c + (block_start(T, G, c) >= q.first_slot ? 0 : 1)) * L::kPartFloats + my; };
+                    float MM = -INFINITY, SS = 0.f;
+                    for (int c = c_first; c <= c_last; ++c) MM = fmaxf(MM, __ldcg(piece(c) + static_cast<size_t>(DH) * L::kRows));
+                    for (int c = c_first; c <= c_last; ++c) {
+                        const float* const pc = piece(c);
+                        const float w = part_weight(__ldcg(pc + static_cast<size_t>(DH) * L::kRows), MM);
+                        if (w != 0.f) SS = fmaf(w, __ldcg(pc + static_cast<size_t>(DH + 1) * L::kRows), SS);
+                    }
+                    const float sinv = SS != 0.f ? 1.f / SS : 0.f;
+#pragma unroll 1
+                    for (int f = f0; f < f0 + kFeat; f += 32) {
+                        float o[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                        for (int c = c_first; c <= c_last; ++c) {
+                            const float* const pc = piece(c);
+                            const float w = part_weight(__ldcg(pc + static_cast<size_t>(DH) * L::kRows), MM);
+                            if (w == 0.f) continue;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = fmaf(w, __ldcg(pc + static_cast<size_t>(f + e) * L::kRows), o[e]);
+                        }
+                        float zero = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) { o[e] *= sinv; zero = fmaf(o[e], 0.f, zero); }
+                        odd = odd || !(zero == 0.f);
+                        if (live) {
+                            uint4* const dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + at * DH + f);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                dst[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
+                                                    pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+                        }
+                    }
+                    if (live && a.lse != nullptr && (TILES == 2 || st == 0)) a.lse[at] = SS != 0.f ? (MM + log2f(SS)) * 0.6931471805599453f : -INFINITY;
+                }
+            }
+            // ---- results that are not finite, once more over what their rows see
+            if (any_softmax(odd && live && done)) {            // (behind it, both streams' O are read too)
+                for (int r = warp; r < q.rows; r += kSoftmaxWarps) {
+                    __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + r) * DH;
+                    bool bad = false;
+                    for (int f = lane; f < DH; f += 32) bad = bad || !isfinite(__bfloat162float(out[f]));
+                    if (__any_sync(0xffffffffu, bad)) sum_again<DH>(a, s, q.head, q.r0 + r, out);
+                }
+            }
+            first_seg = false;
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    }
+    if (stuck && lane == 0) atomicOr(a.status, DODO_DEV_WAIT_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+template <int DH, int TILES>
+int launch(dodo_ctx* ctx, const Maps& maps, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
+    auto kern = attend_paged_dense_kernel<DH, TILES>;
+    const int smem = Layout<DH, TILES>::kBytes + 1024;
+    bool& set = ctx->paged_attr_set[(DH == 128 ? 2 : 0) + TILES - 1];
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "paged dense attend shared-memory attribute");
+        set = true;
+    }
+    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w);
+    return dodo_check_cuda(ctx, cudaGetLastError(), "paged dense attend launch");
+}
+
+}  // namespace
+
+size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh) { return static_cast<size_t>(2) * num_sms * 2 * BM * (dh + 2) * sizeof(float); }
+
+int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
+    const int tiles = max_rows > BM ? 2 : 1, tile_rows = tiles * BM;
+    DenseShare w;
+    int64_t total = 0, units = 0;
+    for (int i = 0; i < g.nseq; ++i) {
+        const PagedSeq& s = g.seq[i];
+        const int64_t rows = static_cast<int64_t>(s.tq) * a.group, rt = (rows + tile_rows - 1) / tile_rows;
+        const int64_t keys = ((static_cast<int64_t>(s.c_len) + 3) & ~int64_t{3}) + (s.tq > 0 ? dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) : 0);
+        w.slot0[i] = static_cast<int>(total);
+        w.nt[i] = static_cast<int>(keys > 0 ? (keys + BN - 1) / BN : 1);
+        w.tiles[i] = static_cast<int>(rt > 0 ? rt : 1);
+        total += rt * a.Hkv * w.nt[i];
+        units += rt * a.Hkv;
+        if (total > 0x7fffffff) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "more than 2^31 tiles of keys in 64 sequences");
+    }
+    w.slot0[g.nseq] = static_cast<int>(total);
+    w.total = static_cast<int>(total);
+    if (total == 0) return DODO_OK;
+    // one block per SM, but none for less than four tiles or a unit
+    const int64_t most = (total + 3) / 4 > units ? (total + 3) / 4 : units;
+    const int grid = most < ctx->num_sms ? static_cast<int>(most) : ctx->num_sms;
+    Maps maps;
+    memset(&maps, 0, sizeof maps);
+    int rc = DODO_OK;
+    const int width = a.Hkv * dh, rows = a.pages * a.page;
+    if (a.cK != nullptr && rows > 0) {
+        rc = dodo_encode_bf16_rows(ctx, &maps.cK, a.cK, width, rows, 1);
+        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.cV, a.cV, width, rows, 1);
+    }
+    if (rc == DODO_OK && a.lK != nullptr && loc_rows > 0) {
+        rc = dodo_encode_bf16_rows(ctx, &maps.lK, a.lK, width, loc_rows, 1);
+        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.lV, a.lV, width, loc_rows, 1);
+    }
+    if (rc != DODO_OK) return rc;
+    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, g, a, w, grid, st) : launch<128, 1>(ctx, maps, g, a, w, grid, st);
+    return tiles == 2 ? launch<64, 2>(ctx, maps, g, a, w, grid, st) : launch<64, 1>(ctx, maps, g, a, w, grid, st);
+}

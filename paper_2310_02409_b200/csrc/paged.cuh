@@ -37,12 +37,15 @@ struct PagedArrays {
 };
 // How a launch cuts its work: rows of a tile, keys a chunk is a multiple of, blocks to aim at, keys a chunk has at least
 struct PagedCut { int rows, keys, target, least; };
-void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv);
+void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, bool may_cut);
 static inline size_t dodo_paged_part_rows(const PagedCut& cut) { return static_cast<size_t>(2) * cut.target * cut.rows; }
 // floats of a partial row: dh sums, a maximum and a sum, and two more so that every row of every tile starts on 16 bytes
 static constexpr int dodo_paged_part_floats(int dh) { return dh + 4; }
 
 PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int dtype, int max_rows);
+// many bf16 rows, on the tensor cores; scale of DODO_DENSE_LEAST_SCALE or more
+size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh);
+int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
