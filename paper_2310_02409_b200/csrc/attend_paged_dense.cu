@@ -8,9 +8,11 @@
 // P (bf16 pairs) over the first 64 of them, O at [256 + DH s, ...).  With more than 128 rows the streams are the two halves of a tile
 // of 256 rows, which share every K and V tile (half the operand traffic from L2); with fewer they take the key tiles in turn and are
 // added at the end.  While one stream's softmax runs, the tensor core works for the other.  Roles, each a warp or more:
-//   producer (warp 8)  walks the key list: 32 lanes look four keys each up (page, position), skip tiles that no query sees, write the
-//       tile's positions to shared memory, and bring K and V rows by four-row gather copies (tile::gather4) with the 128-byte swizzle.
-//       A key that no query of the tile sees, or that is not there, is replaced by one that is.
+//   scout (warp 8)  walks the key list: 32 lanes look four keys each up (page, position), skip tiles that no query sees, and leave a
+//       tile's rows and positions in shared memory.
+//   copiers (warps 10 and 11)  bring the K and the V rows that the scout found, 16 bytes a lane, to where the 128-byte swizzle of the
+//       matrix unit's operands wants them; keys that no query of the tile sees, or that are not there, come as zeros.  (Four-row gather
+//       copies of the tensor copy unit took 11,000 cycles for a tile's 64 KB, five times what the rest of the tile takes.)
 //   matrix issuer (warp 9)  the whole warp walks the same list, one elected lane issues: every operand of an instruction then lies in
 //       uniform registers.  Per tile and stream O += P V, then S = Q K^T of the stream's next tile.
 //   softmax (warps 0-3 and 4-7)  a thread is a row: its 128 scores in registers, the running maximum and sum in 32 bits, maximum moved
@@ -28,22 +30,22 @@ using namespace sm100;
 using namespace dodo_paged;
 
 constexpr int BM = 128, BN = 128;
-constexpr int kSoftmaxWarps = 8, kThreads = 32 * (kSoftmaxWarps + 4);      // the last two warps only hand registers over
+constexpr int kSoftmaxWarps = 8, kThreads = 32 * (kSoftmaxWarps + 4);
+constexpr int kPosReaders = kSoftmaxWarps + 3;      // softmax, issuer, copiers
 // Registers of a thread: the launch's 168 a thread (384 threads), shared out anew between two warpgroups of softmax threads (a row's 128
 // scores) and the one of the others: 216 + 216 + 72 = 3 x 168
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 constexpr int kPosSlots = 4;
 constexpr float kRescaleStep = 8.f;
-enum { kFull = 0, kMasked = 1, kEnd = 2 };
+enum { kMasked = 1, kEnd = 2, kLocal = 4 };     // of a tile
 
 template <int DH, int TILES>
 struct Layout {
-    static constexpr int kHalves = DH / 64;
     static constexpr int kTile = BN * DH * 2;                 // bytes of 128 rows
     static constexpr int kHalf = BN * 128;                    // 64 columns of them
     static constexpr int kKStages = TILES == 1 || DH == 64 ? 3 : 2, kVStages = TILES == 1 && DH == 128 ? 2 : kKStages;
     static constexpr int kOffK = TILES * kTile, kOffV = kOffK + kKStages * kTile, kOffPos = kOffV + kVStages * kTile;
-    static constexpr int kOffXch = kOffPos + kPosSlots * BN * 4;      // maxima and sums that the streams of one tile of rows exchange
+    static constexpr int kOffXch = kOffPos + 2 * kPosSlots * BN * 4;      // maxima and sums that the streams of one tile of rows exchange
     static constexpr int kBytes = kOffXch + (TILES == 1 ? 2 * 2 * BM * 4 : 0);
     static constexpr int kRows = TILES * BM;
     static constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (DH + 2);
@@ -55,18 +57,19 @@ struct DenseShare {
     int nt[DODO_GROUP];             // slots of a unit of the sequence
     int tiles[DODO_GROUP];          // tiles of rows
 };
-struct Maps { CUtensorMap cK, cV, lK, lV; };
 
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
     return p != 0;
 }
-__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(smem_u32(bar))
-        : "memory");
+// 16 bytes from global to shared memory, zeros where there is nothing to copy
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// arrives at the barrier once this thread's copies so far have landed
+__device__ __forceinline__ void arrive_with_copies(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // 64 columns of this warp's 32 lanes; the wait for them is in the same statement, so that nothing reads them ahead of it
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* v) {
@@ -117,7 +120,7 @@ struct Segment {
     int first_slot, nt, t0, t1;     // slot of the unit's first tile; tiles of the unit
     int rows, r0;                   // rows of this tile of rows and the first
     int min_pos, last_pos;          // positions of its first and last row
-    int l_vis, c_pad;               // local tokens that its last row sees; rows in use, in fours
+    int l_vis, c_tiles;             // local tokens that its last row sees; tiles of the cache's rows, which the local ones follow
 };
 // walks the segments of slots [x, end)
 __device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int tile_rows, int& x, int end, Segment& q) {
@@ -140,7 +143,7 @@ __device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArr
     q.rows = min(tile_rows, s.tq * a.group - q.r0);
     q.min_pos = s.q_pos0 + q.r0 / a.group;
     q.last_pos = s.q_pos0 + (q.r0 + q.rows - 1) / a.group;
-    q.c_pad = (s.c_len + 3) & ~3;
+    q.c_tiles = (s.c_len + BN - 1) / BN;
     q.l_vis = dodo_visible_local(s.l_len, s.l_pos0, q.last_pos);
     x += q.t1 - q.t0;
     return true;
@@ -205,18 +208,17 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
 
 template <int DH, int TILES>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
-                          const __grid_constant__ DenseShare work) {
+attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a, const __grid_constant__ DenseShare work) {
     using L = Layout<DH, TILES>;
-    constexpr int H2 = L::kHalves;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
         bar_vfree[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_kkind[L::kKStages], s_kind[kPosSlots], s_last;
+    __shared__ int s_kind[kPosSlots], s_last;
     int* const s_pos = reinterpret_cast<int*>(base_ptr + L::kOffPos);
+    int* const s_row = s_pos + kPosSlots * BN;
 
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int T = work.total, G = static_cast<int>(gridDim.x), bid = static_cast<int>(blockIdx.x);
@@ -227,9 +229,9 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i], 4); }
-        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], 1); }
-        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], 1); }
-        for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kSoftmaxWarps); }
+        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 32); mbar_init(&bar_kfree[i], 1); }
+        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 32); mbar_init(&bar_vfree[i], 1); }
+        for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kPosReaders); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -245,29 +247,26 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
     Segment q;
 
     if (warp == kSoftmaxWarps) {
-        // ================================================ producer ================================================
+        // ================================================ scout ===================================================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        int ck = 0, cv = 0;            // K tiles (ends of segments among them) and V tiles so far
+        int c = 0;                     // tiles and ends of segments so far
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
             const PagedSeq& s = g.seq[q.b];
-            const int local_end = q.c_pad + q.l_vis, col = q.head * DH;
-            // a lane's four keys of tile t: page entries first, rows and positions a tile later, copies after that
+            // a lane's four keys of tile t: page entries first, rows and positions a tile later
             int entry[4], row[4], pos[4];
-            bool local = false;
             auto entries = [&](int t) {
                 const int v = t * BN + 4 * lane;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) entry[e] = t < q.t1 ? page_entry(a, s, v + e, s.c_len) : 0;
+                for (int e = 0; e < 4; ++e) entry[e] = t < q.t1 && t < q.c_tiles ? page_entry(a, s, v + e, s.c_len) : 0;
             };
             auto keys = [&](int t) {
-                const int v = t * BN + 4 * lane;
-                local = v >= q.c_pad;
+                const int v = t * BN + 4 * lane, j = v - q.c_tiles * BN;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     row[e] = -1; pos[e] = kNoPos;
                     if (t >= q.t1) continue;
-                    if (local) {
-                        if (v + e < local_end) { row[e] = s.l_row0 + (v + e - q.c_pad); pos[e] = s.l_pos0 + (v + e - q.c_pad); }
+                    if (t >= q.c_tiles) {
+                        if (j + e < q.l_vis) { row[e] = s.l_row0 + j + e; pos[e] = s.l_pos0 + j + e; }
                     } else {
                         const Key k = key_at(a, s, v + e, s.c_len, entry[e]);
                         row[e] = k.row; pos[e] = k.pos;
@@ -277,78 +276,92 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
             entries(q.t0);
             keys(q.t0);
             entries(q.t0 + 1);
-            for (int t = q.t0; t < q.t1; ++t) {
-                int r[4], p[4], lo = kNoPos, hi = static_cast<int>(0x80000000);
-                bool from_local = local;
-                int first = -1;
+            for (int t = q.t0; t <= q.t1; ++t) {           // q.t1: the segment's end
+                int r[4], p[4], hi = static_cast<int>(0x80000000);
+                bool any = false;
 #pragma unroll
-                for (int e = 3; e >= 0; --e) {
+                for (int e = 0; e < 4; ++e) {
                     const bool there = row[e] >= 0 && pos[e] <= q.last_pos;
                     r[e] = there ? row[e] : -1;
                     p[e] = there ? pos[e] : kNoPos;
-                    lo = min(lo, p[e]);
                     hi = max(hi, p[e]);
-                    if (there) first = row[e];
+                    any = any || there;
                 }
-                if (t + 1 < q.t1) { keys(t + 1); entries(t + 2); }
-                const uint32_t has = __ballot_sync(0xffffffffu, first >= 0);
-                if (has == 0u) continue;                    // nobody sees a key of this tile
+                if (t < q.t1) {
+                    keys(t + 1);
+                    entries(t + 2);
+                    if (!__any_sync(0xffffffffu, any)) continue;                // nobody sees a key of this tile
+                }
                 const bool masked = __any_sync(0xffffffffu, hi > q.min_pos);
-                const int donor = __ffs(has) - 1, spare = __shfl_sync(0xffffffffu, first, donor);
-                const bool spare_local = __shfl_sync(0xffffffffu, from_local ? 1 : 0, donor) != 0;
-                if (first < 0) { first = spare; from_local = spare_local; }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = r[e] >= 0 ? r[e] : first;
-
-                const int ks = ck % L::kKStages, vs = cv % L::kVStages, ps = ck % kPosSlots;
-                if (!warp_wait(&bar_kfree[ks], static_cast<uint32_t>(ck / L::kKStages + 1) & 1u)) { stuck = true; break; }
-                if (lane == 0) { s_kkind[ks] = kFull; mbar_expect_tx(&bar_kfull[ks], L::kTile); }
-                __syncwarp();
-                const uint32_t dk = base + L::kOffK + ks * L::kTile + lane * 512;
-#pragma unroll
-                for (int h = 0; h < H2; ++h) gather4(dk + h * L::kHalf, from_local ? &maps.lK : &maps.cK, col + 64 * h, r[0], r[1], r[2], r[3], &bar_kfull[ks]);
-                if (!warp_wait(&bar_posfree[ps], static_cast<uint32_t>(ck / kPosSlots + 1) & 1u)) { stuck = true; break; }
+                const int ps = c % kPosSlots;
+                if (!warp_wait(&bar_posfree[ps], static_cast<uint32_t>(c / kPosSlots + 1) & 1u)) { stuck = true; break; }
                 *reinterpret_cast<int4*>(s_pos + ps * BN + 4 * lane) = make_int4(p[0], p[1], p[2], p[3]);
-                if (lane == 0) s_kind[ps] = masked ? kMasked : kFull;
+                *reinterpret_cast<int4*>(s_row + ps * BN + 4 * lane) = make_int4(r[0], r[1], r[2], r[3]);
+                if (lane == 0) s_kind[ps] = t == q.t1 ? kEnd : (masked ? kMasked : 0) | (t >= q.c_tiles ? kLocal : 0);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar_posfull[ps]);
-                if (!warp_wait(&bar_vfree[vs], static_cast<uint32_t>(cv / L::kVStages + 1) & 1u)) { stuck = true; break; }
-                if (lane == 0) mbar_expect_tx(&bar_vfull[vs], L::kTile);
+                ++c;
+            }
+        }
+    } else if (warp >= kSoftmaxWarps + 2) {
+        // ================================================ copiers: K (warp 10), V (warp 11) =======================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        const bool is_k = warp == kSoftmaxWarps + 2;
+        constexpr int kPieces = DH / 8, kRowsAtOnce = 32 / kPieces;      // 16-byte pieces of a row, rows of an instruction
+        const int stages = is_k ? L::kKStages : L::kVStages, piece = lane % kPieces, sub = lane / kPieces;
+        uint64_t* const full = is_k ? bar_kfull : bar_vfull;
+        uint64_t* const free = is_k ? bar_kfree : bar_vfree;
+        const uint32_t ring = base + (is_k ? L::kOffK : L::kOffV) + (piece / 8) * L::kHalf;
+        const size_t pitch = static_cast<size_t>(a.Hkv) * DH;
+        int c = 0, stage = 0;          // tiles and ends so far; the tile's stage
+        uint32_t phase = 1;
+        while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+            const size_t col = static_cast<size_t>(q.head) * DH + piece * 8;
+            const __nv_bfloat16* const from_cache = static_cast<const __nv_bfloat16*>(is_k ? a.cK : a.cV) + col;
+            const __nv_bfloat16* const from_local = static_cast<const __nv_bfloat16*>(is_k ? a.lK : a.lV) + col;
+            while (true) {
+                const int ps = c % kPosSlots;
+                if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c / kPosSlots) & 1u)) { stuck = true; break; }
+                const int kind = s_kind[ps];
+                ++c;
+                if (kind == kEnd) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar_posfree[ps]);
+                    break;
+                }
+                if (!warp_wait(&free[stage], phase)) { stuck = true; break; }
+                const __nv_bfloat16* const from = (kind & kLocal) != 0 ? from_local : from_cache;
+                const uint32_t dst = ring + stage * L::kTile;
+                const int* const rows = s_row + ps * BN + sub;
+#pragma unroll 8
+                for (int i = 0; i < BN; i += kRowsAtOnce) {
+                    const int r = i + sub, src = rows[i];
+                    copy16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + static_cast<size_t>(max(src, 0)) * pitch, src >= 0);
+                }
+                arrive_with_copies(&full[stage]);
                 __syncwarp();
-                const uint32_t dv = base + L::kOffV + vs * L::kTile + lane * 512;
-#pragma unroll
-                for (int h = 0; h < H2; ++h) gather4(dv + h * L::kHalf, from_local ? &maps.lV : &maps.cV, col + 64 * h, r[0], r[1], r[2], r[3], &bar_vfull[vs]);
-                ++ck;
-                ++cv;
+                if (lane == 0) mbar_arrive(&bar_posfree[ps]);
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
-            if (stuck) break;
-            // the segment's end
-            const int ks = ck % L::kKStages, ps = ck % kPosSlots;
-            if (!warp_wait(&bar_kfree[ks], static_cast<uint32_t>(ck / L::kKStages + 1) & 1u) ||
-                !warp_wait(&bar_posfree[ps], static_cast<uint32_t>(ck / kPosSlots + 1) & 1u)) { stuck = true; break; }
-            if (lane == 0) {
-                s_kkind[ks] = kEnd;
-                s_kind[ps] = kEnd;
-                mbar_arrive(&bar_kfull[ks]);
-                mbar_arrive(&bar_posfull[ps]);
-            }
-            __syncwarp();
-            ++ck;
         }
-        if (stuck) {         // copies in flight land before the block's shared memory goes
-            for (int i = max(0, ck - L::kKStages + 1); i <= ck; ++i) warp_wait(&bar_kfull[i % L::kKStages], static_cast<uint32_t>(i / L::kKStages) & 1u);
-            for (int i = max(0, cv - L::kVStages + 1); i <= cv; ++i) warp_wait(&bar_vfull[i % L::kVStages], static_cast<uint32_t>(i / L::kVStages) & 1u);
-        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == kSoftmaxWarps + 1) {
         // ================================================ matrix issuer ===========================================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        int ck = 0, cv = 0, np[2] = {0, 0}, segs = 0;
+        int c_pos = 0, ck = 0, cv = 0, np[2] = {0, 0}, segs = 0;     // tiles and ends; K tiles; V tiles; P of the streams
+        // the copies' writes are ordinary ones: a fence between their barrier and the matrix unit's reads
         const uint32_t idesc_s = idesc_bf16(BN, false), idesc_o = idesc_bf16(DH, true);
-        auto wait_k = [&](int c) {      // kind of the K tile, kEnd when the wait ran out
-            if (!warp_wait(&bar_kfull[c % L::kKStages], static_cast<uint32_t>(c / L::kKStages) & 1u)) { stuck = true; return static_cast<int>(kEnd); }
-            const int kind = s_kkind[c % L::kKStages];
+        auto wait_k = [&]() {           // the next tile's K rows: false at the segment's end (or when a wait ran out)
+            const int ps = c_pos % kPosSlots;
+            if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c_pos / kPosSlots) & 1u)) { stuck = true; return false; }
+            const int kind = s_kind[ps];
             __syncwarp();
-            return kind;
+            if (lane == 0) mbar_arrive(&bar_posfree[ps]);
+            ++c_pos;
+            if (kind == kEnd) return false;
+            if (!warp_wait(&bar_kfull[ck % L::kKStages], static_cast<uint32_t>(ck / L::kKStages) & 1u)) { stuck = true; return false; }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            return true;
         };
         auto scores = [&](int st, int qtile, int c, bool last_user) {
             tc_fence_after();
@@ -379,42 +392,41 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
             if (!warp_wait(&bar_p[st], static_cast<uint32_t>(np[st]) & 1u)) stuck = true;
             ++np[st];
         };
-        auto wait_v = [&](int c) { if (!warp_wait(&bar_vfull[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true; };
-        auto free_end = [&](int c) {     // nothing reads the slot of a segment's end
-            if (lane == 0) mbar_arrive(&bar_kfree[c % L::kKStages]);
-            __syncwarp();
+        auto wait_v = [&](int c) {
+            if (!warp_wait(&bar_vfull[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         };
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
             if (!warp_wait(&bar_q, static_cast<uint32_t>(segs) & 1u)) { stuck = true; break; }
             ++segs;
             if constexpr (TILES == 2) {
                 const int streams = q.rows > BM ? 2 : 1;
-                int kind = wait_k(ck);
-                if (kind == kEnd) { free_end(ck); ++ck; continue; }
+                bool more = wait_k();
+                if (!more) continue;
                 for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
+                ++ck;
                 bool add = false;
-                while (!stuck) {
-                    ++ck;                                  // the next tile
+                while (more && !stuck) {
                     for (int st = 0; st < streams; ++st) {
                         wait_p(st);
                         if (st == 0) wait_v(cv);
                         values(st, cv, add, st == streams - 1);
-                        if (st == 0) kind = wait_k(ck);
-                        if (kind != kEnd) scores(st, st, ck, st == streams - 1);
+                        if (st == 0) more = wait_k();
+                        if (more) scores(st, st, ck, st == streams - 1);
                     }
                     ++cv;
+                    ck += more ? 1 : 0;
                     add = true;
-                    if (kind == kEnd) { free_end(ck); break; }
                 }
-                ++ck;
             } else {
                 // tile i of the segment belongs to stream i & 1; scores run two tiles ahead of the values
                 int i = 0, ahead = 0;
                 bool ended = false;
                 auto next_scores = [&]() {
                     if (ended) return;
-                    if (wait_k(ck) == kEnd) { ended = true; free_end(ck); }
-                    else { scores(ahead & 1, 0, ck, true); ++ahead; }
+                    if (!wait_k()) { ended = true; return; }
+                    scores(ahead & 1, 0, ck, true);
+                    ++ahead;
                     ++ck;
                 };
                 next_scores();
@@ -432,7 +444,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
             if (elect_one()) mma_commit(&bar_o);
             __syncwarp();
         }
-    } else if (warp < kSoftmaxWarps) {
+    } else {
         // ================================================ softmax =================================================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int st = warp >> 2, row = tid & (BM - 1);
@@ -485,7 +497,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                     uint32_t sv[BN];
                     tmem_ld64(t_s, sv);
                     tmem_ld64(t_s + 64, sv + 64);
-                    if (kind == kMasked) {
+                    if ((kind & kMasked) != 0) {
 #pragma unroll
                         for (int c = 0; c < BN; c += 4) {
                             const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
@@ -672,8 +684,6 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
             }
             first_seg = false;
         }
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     }
     if (stuck && lane == 0) atomicOr(a.status, DODO_DEV_WAIT_TIMEOUT);
     tc_fence_before();
@@ -682,7 +692,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
 }
 
 template <int DH, int TILES>
-int launch(dodo_ctx* ctx, const Maps& maps, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
+int launch(dodo_ctx* ctx, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
     auto kern = attend_paged_dense_kernel<DH, TILES>;
     const int smem = Layout<DH, TILES>::kBytes + 1024;
     bool& set = ctx->paged_attr_set[(DH == 128 ? 2 : 0) + TILES - 1];
@@ -691,7 +701,7 @@ int launch(dodo_ctx* ctx, const Maps& maps, const PagedGroup& g, const PagedArra
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "paged dense attend shared-memory attribute");
         set = true;
     }
-    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w);
+    kern<<<grid, kThreads, smem, st>>>(g, a, w);
     return dodo_check_cuda(ctx, cudaGetLastError(), "paged dense attend launch");
 }
 
@@ -699,16 +709,16 @@ int launch(dodo_ctx* ctx, const Maps& maps, const PagedGroup& g, const PagedArra
 
 size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh) { return static_cast<size_t>(2) * num_sms * 2 * BM * (dh + 2) * sizeof(float); }
 
-int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
+int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
     const int tiles = max_rows > BM ? 2 : 1, tile_rows = tiles * BM;
     DenseShare w;
     int64_t total = 0, units = 0;
     for (int i = 0; i < g.nseq; ++i) {
         const PagedSeq& s = g.seq[i];
         const int64_t rows = static_cast<int64_t>(s.tq) * a.group, rt = (rows + tile_rows - 1) / tile_rows;
-        const int64_t keys = ((static_cast<int64_t>(s.c_len) + 3) & ~int64_t{3}) + (s.tq > 0 ? dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) : 0);
+        const int l_vis = s.tq > 0 ? dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) : 0, nt = (s.c_len + BN - 1) / BN + (l_vis + BN - 1) / BN;
         w.slot0[i] = static_cast<int>(total);
-        w.nt[i] = static_cast<int>(keys > 0 ? (keys + BN - 1) / BN : 1);
+        w.nt[i] = nt > 0 ? nt : 1;
         w.tiles[i] = static_cast<int>(rt > 0 ? rt : 1);
         total += rt * a.Hkv * w.nt[i];
         units += rt * a.Hkv;
@@ -720,19 +730,6 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     // one block per SM, but none for less than four tiles or a unit
     const int64_t most = (total + 3) / 4 > units ? (total + 3) / 4 : units;
     const int grid = most < ctx->num_sms ? static_cast<int>(most) : ctx->num_sms;
-    Maps maps;
-    memset(&maps, 0, sizeof maps);
-    int rc = DODO_OK;
-    const int width = a.Hkv * dh, rows = a.pages * a.page;
-    if (a.cK != nullptr && rows > 0) {
-        rc = dodo_encode_bf16_rows(ctx, &maps.cK, a.cK, width, rows, 1);
-        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.cV, a.cV, width, rows, 1);
-    }
-    if (rc == DODO_OK && a.lK != nullptr && loc_rows > 0) {
-        rc = dodo_encode_bf16_rows(ctx, &maps.lK, a.lK, width, loc_rows, 1);
-        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.lV, a.lV, width, loc_rows, 1);
-    }
-    if (rc != DODO_OK) return rc;
-    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, g, a, w, grid, st) : launch<128, 1>(ctx, maps, g, a, w, grid, st);
-    return tiles == 2 ? launch<64, 2>(ctx, maps, g, a, w, grid, st) : launch<64, 1>(ctx, maps, g, a, w, grid, st);
+    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, g, a, w, grid, st) : launch<128, 1>(ctx, g, a, w, grid, st);
+    return tiles == 2 ? launch<64, 2>(ctx, g, a, w, grid, st) : launch<64, 1>(ctx, g, a, w, grid, st);
 }
