@@ -30,11 +30,11 @@ using namespace sm100;
 using namespace dodo_paged;
 
 constexpr int BM = 128, BN = 128;
-constexpr int kSoftmaxWarps = 8, kThreads = 32 * (kSoftmaxWarps + 4);
-constexpr int kPosReaders = kSoftmaxWarps + 3;      // softmax, issuer, copiers
+constexpr int kSoftmaxWarps = 8, kFirstCopier = 10, kCopiers = 6, kThreads = 32 * (kFirstCopier + kCopiers);
+constexpr int kPosReaders = kSoftmaxWarps + 1 + kCopiers;      // softmax, issuer, copiers
 // Registers of a thread: the launch's 168 a thread (384 threads), shared out anew between two warpgroups of softmax threads (a row's 128
 // scores) and the one of the others: 216 + 216 + 72 = 3 x 168
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
 constexpr int kPosSlots = 4;
 constexpr float kRescaleStep = 8.f;
 enum { kMasked = 1, kEnd = 2, kLocal = 4 };     // of a tile
@@ -229,8 +229,8 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i], 4); }
-        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 32); mbar_init(&bar_kfree[i], 1); }
-        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 32); mbar_init(&bar_vfree[i], 1); }
+        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 32 * kCopiers); mbar_init(&bar_kfree[i], 1); }
+        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 32 * kCopiers); mbar_init(&bar_vfree[i], 1); }
         for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kPosReaders); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -303,45 +303,43 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 ++c;
             }
         }
-    } else if (warp >= kSoftmaxWarps + 2) {
-        // ================================================ copiers: K (warp 10), V (warp 11) =======================
+    } else if (warp >= kFirstCopier) {
+        // ================================================ copiers =================================================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        const bool is_k = warp == kSoftmaxWarps + 2;
         constexpr int kPieces = DH / 8, kRowsAtOnce = 32 / kPieces;      // 16-byte pieces of a row, rows of an instruction
-        const int stages = is_k ? L::kKStages : L::kVStages, piece = lane % kPieces, sub = lane / kPieces;
-        uint64_t* const full = is_k ? bar_kfull : bar_vfull;
-        uint64_t* const free = is_k ? bar_kfree : bar_vfree;
-        const uint32_t ring = base + (is_k ? L::kOffK : L::kOffV) + (piece / 8) * L::kHalf;
+        const int piece = lane % kPieces, sub = (warp - kFirstCopier) * kRowsAtOnce + lane / kPieces;
         const size_t pitch = static_cast<size_t>(a.Hkv) * DH;
-        int c = 0, stage = 0;          // tiles and ends so far; the tile's stage
-        uint32_t phase = 1;
+        int c = 0, n = 0;              // tiles and ends so far; tiles
+        auto copy = [&](uint32_t ring, uint64_t* full, uint64_t* free, int stages, const __nv_bfloat16* from, const int* rows) {
+            const int stage = n % stages;
+            if (!warp_wait(&free[stage], static_cast<uint32_t>(n / stages + 1) & 1u)) return false;
+            const uint32_t dst = ring + stage * L::kTile;
+#pragma unroll 8
+            for (int r = sub; r < BN; r += kRowsAtOnce * kCopiers) {
+                const int src = rows[r];
+                copy16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + static_cast<size_t>(max(src, 0)) * pitch, src >= 0);
+            }
+            arrive_with_copies(&full[stage]);
+            return true;
+        };
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
             const size_t col = static_cast<size_t>(q.head) * DH + piece * 8;
-            const __nv_bfloat16* const from_cache = static_cast<const __nv_bfloat16*>(is_k ? a.cK : a.cV) + col;
-            const __nv_bfloat16* const from_local = static_cast<const __nv_bfloat16*>(is_k ? a.lK : a.lV) + col;
             while (true) {
                 const int ps = c % kPosSlots;
                 if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c / kPosSlots) & 1u)) { stuck = true; break; }
                 const int kind = s_kind[ps];
                 ++c;
-                if (kind == kEnd) {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bar_posfree[ps]);
-                    break;
+                if (kind != kEnd) {
+                    const bool local = (kind & kLocal) != 0;
+                    const int* const rows = s_row + ps * BN;
+                    const uint32_t half = base + (piece / 8) * L::kHalf;
+                    if (!copy(half + L::kOffK, bar_kfull, bar_kfree, L::kKStages, static_cast<const __nv_bfloat16*>(local ? a.lK : a.cK) + col, rows) ||
+                        !copy(half + L::kOffV, bar_vfull, bar_vfree, L::kVStages, static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + col, rows)) { stuck = true; break; }
+                    ++n;
                 }
-                if (!warp_wait(&free[stage], phase)) { stuck = true; break; }
-                const __nv_bfloat16* const from = (kind & kLocal) != 0 ? from_local : from_cache;
-                const uint32_t dst = ring + stage * L::kTile;
-                const int* const rows = s_row + ps * BN + sub;
-#pragma unroll 8
-                for (int i = 0; i < BN; i += kRowsAtOnce) {
-                    const int r = i + sub, src = rows[i];
-                    copy16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + static_cast<size_t>(max(src, 0)) * pitch, src >= 0);
-                }
-                arrive_with_copies(&full[stage]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar_posfree[ps]);
-                if (++stage == stages) { stage = 0; phase ^= 1u; }
+                if (kind == kEnd) break;
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
