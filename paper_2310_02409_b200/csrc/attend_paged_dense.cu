@@ -213,7 +213,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
+    __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2][2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
         bar_vfree[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
     __shared__ uint32_t s_tmem;
     __shared__ int s_kind[kPosSlots], s_last;
@@ -228,7 +228,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
     if (tid == 0) {
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i], 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i][0], 4); mbar_init(&bar_p[i][1], 4); }
         for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 32 * kCopiers); mbar_init(&bar_kfree[i], 1); }
         for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 32 * kCopiers); mbar_init(&bar_vfree[i], 1); }
         for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kPosReaders); }
@@ -375,19 +375,21 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
             }
             __syncwarp();
         };
+        // the product of a tile's weights and values, in halves of 64 keys as the softmax publishes them
         auto values = [&](int st, int c, bool add, bool last_user) {
-            tc_fence_after();
             const uint64_t db = desc_mnmajor(base + L::kOffV + (c % L::kVStages) * L::kTile, L::kHalf);
-            if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < BN / 16; ++i)       // 16 keys of P = 8 columns of bf16 pairs
-                    mma_bf16_ts(tmem + 2 * BN + st * DH, tmem + st * BN + i * 8, db + static_cast<uint64_t>((i * 2048) >> 4), idesc_o, add || i > 0);
-                if (last_user) mma_commit(&bar_vfree[c % L::kVStages]);
+            for (int h = 0; h < 2; ++h) {
+                if (!warp_wait(&bar_p[st][h], static_cast<uint32_t>(np[st]) & 1u)) stuck = true;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int i = h * BN / 32; i < (h + 1) * BN / 32; ++i)       // 16 keys of P = 8 columns of bf16 pairs
+                        mma_bf16_ts(tmem + 2 * BN + st * DH, tmem + st * BN + i * 8, db + static_cast<uint64_t>((i * 2048) >> 4), idesc_o, add || i > 0);
+                    if (h == 1 && last_user) mma_commit(&bar_vfree[c % L::kVStages]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
-        };
-        auto wait_p = [&](int st) {
-            if (!warp_wait(&bar_p[st], static_cast<uint32_t>(np[st]) & 1u)) stuck = true;
             ++np[st];
         };
         auto wait_v = [&](int c) {
@@ -405,11 +407,10 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 ++ck;
                 bool add = false;
                 while (more && !stuck) {
+                    wait_v(cv);            // (both are there by the time the first weights are)
+                    more = wait_k();
                     for (int st = 0; st < streams; ++st) {
-                        wait_p(st);
-                        if (st == 0) wait_v(cv);
                         values(st, cv, add, st == streams - 1);
-                        if (st == 0) more = wait_k();
                         if (more) scores(st, st, ck, st == streams - 1);
                     }
                     ++cv;
@@ -431,7 +432,6 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 next_scores();
                 if (ahead == 0) continue;
                 while (!stuck && i < ahead) {
-                    wait_p(i & 1);
                     wait_v(cv);
                     values(i & 1, cv, i >= 2, true);
                     ++cv;
@@ -533,24 +533,31 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                     const float2 nm2 = make_float2(nm, nm);
                     float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int c = 0; c < BN; c += 4) {
-                        const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c2, nm2);
-                        const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), c2, nm2);
-                        const float2 p0 = make_float2(exp2_fast(x0.x), exp2_fast(x0.y));
-                        const float2 p1 = make_float2(exp2_fast(x1.x), exp2_fast(x1.y));
-                        sv[c / 2] = pack_bf16(p0.x, p0.y);
-                        sv[c / 2 + 1] = pack_bf16(p1.x, p1.y);
-                        sum0 = __fadd2_rn(sum0, p0);
-                        sum1 = __fadd2_rn(sum1, p1);
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int c = h * BN / 2; c < (h + 1) * BN / 2; c += 4) {
+                            const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c2, nm2);
+                            const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), c2, nm2);
+                            const float2 p0 = make_float2(exp2_fast(x0.x), exp2_fast(x0.y));
+                            const float2 p1 = make_float2(exp2_fast(x1.x), exp2_fast(x1.y));
+                            sv[c / 2] = pack_bf16(p0.x, p0.y);
+                            sv[c / 2 + 1] = pack_bf16(p1.x, p1.y);
+                            sum0 = __fadd2_rn(sum0, p0);
+                            sum1 = __fadd2_rn(sum1, p1);
+                        }
+                        tmem_st32(t_s + h * 32, sv + h * 32);
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bar_p[st][h]);
                     }
-                    tmem_st32(t_s, sv);
-                    tmem_st32(t_s + 32, sv + 32);
                     l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
-                    tc_fence_before();
+                } else if (lane == 0) {
+                    mbar_arrive(&bar_p[st][0]);
+                    mbar_arrive(&bar_p[st][1]);
                 }
                 ++mine;
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(&bar_posfree[ps]); mbar_arrive(&bar_p[st]); }
+                if (lane == 0) mbar_arrive(&bar_posfree[ps]);
             }
             if (tiles > 0) {
                 if (!stuck && !warp_wait(&bar_o, static_cast<uint32_t>(os) & 1u)) stuck = true;
