@@ -103,7 +103,7 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
         // Many bf16 rows are a contraction: the tensor cores.  (Row maxima are taken before scaling, so the scale must be positive.)
         if (dtype == DODO_BF16 && max_rows > kFewRows && sm_scale >= DODO_DENSE_LEAST_SCALE && workspace != nullptr &&
             workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh)) {
-            if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, g, a, st)) != DODO_OK) return rc;
+            if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
             continue;
         }
         const PagedCut cut = dodo_paged_rows_cut(ctx, dtype, max_rows);

@@ -10,9 +10,10 @@
 // added at the end.  While one stream's softmax runs, the tensor core works for the other.  Roles, each a warp or more:
 //   scout (warp 8)  walks the key list: 32 lanes look four keys each up (page, position), skip tiles that no query sees, and leave a
 //       tile's rows and positions in shared memory.
-//   copiers (warps 10 and 11)  bring the K and the V rows that the scout found, 16 bytes a lane, to where the 128-byte swizzle of the
-//       matrix unit's operands wants them; keys that no query of the tile sees, or that are not there, come as zeros.  (Four-row gather
-//       copies of the tensor copy unit took 11,000 cycles for a tile's 64 KB, five times what the rest of the tile takes.)
+//   producer (warp 10)  brings K and V by tensor copies with the 128-byte swizzle, a box as many rows high as the power of two that
+//       divides the page's (a page's rows lie side by side), up to the tile's 128; where that is less than eight, four rows at a time by
+//       gather copies (tile::gather4), which cost five times what the rest of a tile does.  Local tokens are boxes of 128.
+//   cleaner (warp 11)  writes zeros over V rows of keys that are not there or that no query of the tile sees.
 //   matrix issuer (warp 9)  the whole warp walks the same list, one elected lane issues: every operand of an instruction then lies in
 //       uniform registers.  Per tile and stream O += P V, then S = Q K^T of the stream's next tile.
 //   softmax (warps 0-3 and 4-7)  a thread is a row: its 128 scores in registers, the running maximum and sum in 32 bits, maximum moved
@@ -30,17 +31,18 @@ using namespace sm100;
 using namespace dodo_paged;
 
 constexpr int BM = 128, BN = 128;
-constexpr int kSoftmaxWarps = 8, kFirstCopier = 10, kCopiers = 6, kThreads = 32 * (kFirstCopier + kCopiers);
-constexpr int kPosReaders = kSoftmaxWarps + 1 + kCopiers;      // softmax, issuer, copiers
+constexpr int kSoftmaxWarps = 8, kThreads = 32 * (kSoftmaxWarps + 4);
+constexpr int kPosReaders = kSoftmaxWarps + 3;      // softmax, issuer, producer, cleaner
 // Registers of a thread: the launch's 168 a thread (384 threads), shared out anew between two warpgroups of softmax threads (a row's 128
 // scores) and the one of the others: 216 + 216 + 72 = 3 x 168
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 constexpr int kPosSlots = 4;
 constexpr float kRescaleStep = 8.f;
-enum { kMasked = 1, kEnd = 2, kLocal = 4 };     // of a tile
+enum { kMasked = 1, kEnd = 2, kLocal = 4, kHoles = 8 };     // of a tile; kHoles: some of its keys are not there or seen by nobody
 
 template <int DH, int TILES>
 struct Layout {
+    static constexpr int kHalves = DH / 64;
     static constexpr int kTile = BN * DH * 2;                 // bytes of 128 rows
     static constexpr int kHalf = BN * 128;                    // 64 columns of them
     static constexpr int kKStages = TILES == 1 || DH == 64 ? 3 : 2, kVStages = TILES == 1 && DH == 128 ? 2 : kKStages;
@@ -51,6 +53,7 @@ struct Layout {
     static constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (DH + 2);
 };
 
+struct Maps { CUtensorMap cK, cV, lK, lV; };
 struct DenseShare {
     int total;                      // slots
     int slot0[DODO_GROUP + 1];      // first slot of each sequence
@@ -63,23 +66,29 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
     return p != 0;
 }
-// 16 bytes from global to shared memory, zeros where there is nothing to copy
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int x, int4 r, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(smem_u32(bar))
+        : "memory");
 }
-// arrives at the barrier once this thread's copies so far have landed
-__device__ __forceinline__ void arrive_with_copies(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// 64 columns of this warp's 32 lanes; the wait for them is in the same statement, so that nothing reads them ahead of it
+#define DODO_REGS64(v) \
+    "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), \
+    "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), \
+    "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]), "+r"(v[32]), "+r"(v[33]), \
+    "+r"(v[34]), "+r"(v[35]), "+r"(v[36]), "+r"(v[37]), "+r"(v[38]), "+r"(v[39]), "+r"(v[40]), "+r"(v[41]), "+r"(v[42]), "+r"(v[43]), "+r"(v[44]), \
+    "+r"(v[45]), "+r"(v[46]), "+r"(v[47]), "+r"(v[48]), "+r"(v[49]), "+r"(v[50]), "+r"(v[51]), "+r"(v[52]), "+r"(v[53]), "+r"(v[54]), "+r"(v[55]), \
+    "+r"(v[56]), "+r"(v[57]), "+r"(v[58]), "+r"(v[59]), "+r"(v[60]), "+r"(v[61]), "+r"(v[62]), "+r"(v[63])
+// the wait for a tmem_ld64: it names the registers, so that nothing reads them ahead of it
+__device__ __forceinline__ void tmem_wait64(uint32_t* v) { asm volatile("tcgen05.wait::ld.sync.aligned;" : DODO_REGS64(v)::"memory"); }
+// 64 columns of this warp's 32 lanes
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* v) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
         "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
         "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
           "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
           "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
@@ -208,13 +217,14 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
 
 template <int DH, int TILES>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a, const __grid_constant__ DenseShare work) {
+attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
+                          const __grid_constant__ DenseShare work, int box) {
     using L = Layout<DH, TILES>;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2][2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
-        bar_vfree[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
+        bar_vfree[L::kVStages], bar_vclean[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
     __shared__ uint32_t s_tmem;
     __shared__ int s_kind[kPosSlots], s_last;
     int* const s_pos = reinterpret_cast<int*>(base_ptr + L::kOffPos);
@@ -229,8 +239,8 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i][0], 4); mbar_init(&bar_p[i][1], 4); }
-        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 32 * kCopiers); mbar_init(&bar_kfree[i], 1); }
-        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 32 * kCopiers); mbar_init(&bar_vfree[i], 1); }
+        for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], 1); }
+        for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], 1); mbar_init(&bar_vclean[i], 1); }
         for (int i = 0; i < kPosSlots; ++i) { mbar_init(&bar_posfull[i], 1); mbar_init(&bar_posfree[i], kPosReaders); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -278,11 +288,11 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
             entries(q.t0 + 1);
             for (int t = q.t0; t <= q.t1; ++t) {           // q.t1: the segment's end
                 int r[4], p[4], hi = static_cast<int>(0x80000000);
-                bool any = false;
+                bool any = false;      // rows where there are keys, positions only where somebody sees them
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool there = row[e] >= 0 && pos[e] <= q.last_pos;
-                    r[e] = there ? row[e] : -1;
+                    r[e] = row[e];
                     p[e] = there ? pos[e] : kNoPos;
                     hi = max(hi, p[e]);
                     any = any || there;
@@ -297,33 +307,59 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 if (!warp_wait(&bar_posfree[ps], static_cast<uint32_t>(c / kPosSlots + 1) & 1u)) { stuck = true; break; }
                 *reinterpret_cast<int4*>(s_pos + ps * BN + 4 * lane) = make_int4(p[0], p[1], p[2], p[3]);
                 *reinterpret_cast<int4*>(s_row + ps * BN + 4 * lane) = make_int4(r[0], r[1], r[2], r[3]);
-                if (lane == 0) s_kind[ps] = t == q.t1 ? kEnd : (masked ? kMasked : 0) | (t >= q.c_tiles ? kLocal : 0);
+                const bool holes = __any_sync(0xffffffffu, hi == kNoPos);
+                if (lane == 0) s_kind[ps] = t == q.t1 ? kEnd : (masked ? kMasked : 0) | (t >= q.c_tiles ? kLocal : 0) | (holes ? kHoles : 0);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar_posfull[ps]);
                 ++c;
             }
         }
-    } else if (warp >= kFirstCopier) {
-        // ================================================ copiers =================================================
+    } else if (warp == kSoftmaxWarps + 2) {
+        // ================================================ producer ================================================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        constexpr int kPieces = DH / 8, kRowsAtOnce = 32 / kPieces;      // 16-byte pieces of a row, rows of an instruction
-        const int piece = lane % kPieces, sub = (warp - kFirstCopier) * kRowsAtOnce + lane / kPieces;
-        const size_t pitch = static_cast<size_t>(a.Hkv) * DH;
         int c = 0, n = 0;              // tiles and ends so far; tiles
-        auto copy = [&](uint32_t ring, uint64_t* full, uint64_t* free, int stages, const __nv_bfloat16* from, const int* rows) {
+        // the rows of a tile to stage n of a ring: boxes whose first key is there
+        auto bring = [&](uint32_t ring, uint64_t* full, uint64_t* free, int stages, const CUtensorMap* cache, const CUtensorMap* loc, bool local, int col, const int* rows) {
             const int stage = n % stages;
             if (!warp_wait(&free[stage], static_cast<uint32_t>(n / stages + 1) & 1u)) return false;
+            uint64_t* const bar = &full[stage];
             const uint32_t dst = ring + stage * L::kTile;
-#pragma unroll 8
-            for (int r = sub; r < BN; r += kRowsAtOnce * kCopiers) {
-                const int src = rows[r];
-                copy16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + static_cast<size_t>(max(src, 0)) * pitch, src >= 0);
+            if (local) {
+                const int r = rows[0];
+                if (elect_one()) {
+                    mbar_expect_tx(bar, L::kTile);
+#pragma unroll
+                    for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + h * L::kHalf, loc, col + 64 * h, r, bar);
+                }
+            } else if (box >= 8) {
+                int count = 0;
+                for (int k = lane * box; k < BN; k += 32 * box) count += rows[k] >= 0 ? 1 : 0;
+                count = __reduce_add_sync(0xffffffffu, count);
+                if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(count * box * DH * 2));
+                for (int k = 0; k < BN; k += box) {
+                    const int r = rows[k];
+                    if (r >= 0 && elect_one()) {
+#pragma unroll
+                        for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + h * L::kHalf + k * 128, cache, col + 64 * h, r, bar);
+                    }
+                }
+            } else {
+                int4 r = *reinterpret_cast<const int4*>(rows + 4 * lane);
+                const int some = max(max(r.x, r.y), max(r.z, r.w));       // in the place of rows that are not there
+                const uint32_t has = __ballot_sync(0xffffffffu, some >= 0);
+                if (lane == 0) mbar_expect_tx(bar, static_cast<uint32_t>(__popc(has) * 4 * DH * 2));
+                __syncwarp();
+                if (some >= 0) {
+                    r.x = r.x < 0 ? some : r.x; r.y = r.y < 0 ? some : r.y; r.z = r.z < 0 ? some : r.z; r.w = r.w < 0 ? some : r.w;
+#pragma unroll
+                    for (int h = 0; h < L::kHalves; ++h) gather4(dst + h * L::kHalf + lane * 512, cache, col + 64 * h, r, bar);
+                }
             }
-            arrive_with_copies(&full[stage]);
+            __syncwarp();
             return true;
         };
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
-            const size_t col = static_cast<size_t>(q.head) * DH + piece * 8;
+            const int col = q.head * DH;
             while (true) {
                 const int ps = c % kPosSlots;
                 if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c / kPosSlots) & 1u)) { stuck = true; break; }
@@ -332,9 +368,8 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 if (kind != kEnd) {
                     const bool local = (kind & kLocal) != 0;
                     const int* const rows = s_row + ps * BN;
-                    const uint32_t half = base + (piece / 8) * L::kHalf;
-                    if (!copy(half + L::kOffK, bar_kfull, bar_kfree, L::kKStages, static_cast<const __nv_bfloat16*>(local ? a.lK : a.cK) + col, rows) ||
-                        !copy(half + L::kOffV, bar_vfull, bar_vfree, L::kVStages, static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + col, rows)) { stuck = true; break; }
+                    if (!bring(base + L::kOffK, bar_kfull, bar_kfree, L::kKStages, &maps.cK, &maps.lK, local, col, rows) ||
+                        !bring(base + L::kOffV, bar_vfull, bar_vfree, L::kVStages, &maps.cV, &maps.lV, local, col, rows)) { stuck = true; break; }
                     ++n;
                 }
                 __syncwarp();
@@ -342,25 +377,53 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 if (kind == kEnd) break;
             }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (stuck) {         // copies in flight land before the block's shared memory goes
+            for (int i = max(0, n - L::kKStages + 1); i <= n; ++i) mbar_wait(&bar_kfull[i % L::kKStages], static_cast<uint32_t>(i / L::kKStages) & 1u);
+            for (int i = max(0, n - L::kVStages + 1); i <= n; ++i) mbar_wait(&bar_vfull[i % L::kVStages], static_cast<uint32_t>(i / L::kVStages) & 1u);
+        }
+    } else if (warp == kSoftmaxWarps + 3) {
+        // ================================================ cleaner =================================================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        constexpr int kPieces = DH / 8;                    // 16-byte pieces of a row
+        int c = 0, n = 0;
+        while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+            while (true) {
+                const int ps = c % kPosSlots, stage = n % L::kVStages;
+                if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c / kPosSlots) & 1u)) { stuck = true; break; }
+                const int kind = s_kind[ps];
+                ++c;
+                if (kind != kEnd) {
+                    if (!warp_wait(&bar_vfull[stage], static_cast<uint32_t>(n / L::kVStages) & 1u)) { stuck = true; break; }
+                    if ((kind & kHoles) != 0) {
+                        unsigned char* const v = base_ptr + L::kOffV + stage * L::kTile + (lane % kPieces / 8) * L::kHalf + lane % 8 * 16;
+                        for (int r = lane / kPieces; r < BN; r += 32 / kPieces)
+                            if (s_pos[ps * BN + r] == kNoPos) *reinterpret_cast<uint4*>(v + r * 128) = make_uint4(0u, 0u, 0u, 0u);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar_vclean[stage]);
+                    ++n;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar_posfree[ps]);
+                if (kind == kEnd) break;
+            }
+        }
     } else if (warp == kSoftmaxWarps + 1) {
         // ================================================ matrix issuer ===========================================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         int c_pos = 0, ck = 0, cv = 0, np[2] = {0, 0}, segs = 0;     // tiles and ends; K tiles; V tiles; P of the streams
-        // the copies' writes are ordinary ones: a fence between their barrier and the matrix unit's reads
         const uint32_t idesc_s = idesc_bf16(BN, false), idesc_o = idesc_bf16(DH, true);
-        auto wait_k = [&]() {           // the next tile's K rows: false at the segment's end (or when a wait ran out)
+        auto next_tile = [&]() {        // whether the segment has another tile (or a wait ran out)
             const int ps = c_pos % kPosSlots;
             if (!warp_wait(&bar_posfull[ps], static_cast<uint32_t>(c_pos / kPosSlots) & 1u)) { stuck = true; return false; }
             const int kind = s_kind[ps];
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar_posfree[ps]);
             ++c_pos;
-            if (kind == kEnd) return false;
-            if (!warp_wait(&bar_kfull[ck % L::kKStages], static_cast<uint32_t>(ck / L::kKStages) & 1u)) { stuck = true; return false; }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            return true;
+            return kind != kEnd;
         };
+        auto wait_k = [&](int c) { if (!warp_wait(&bar_kfull[c % L::kKStages], static_cast<uint32_t>(c / L::kKStages) & 1u)) stuck = true; };
         auto scores = [&](int st, int qtile, int c, bool last_user) {
             tc_fence_after();
             const uint64_t da = desc_kmajor(base + qtile * L::kTile), db = desc_kmajor(base + L::kOffK + (c % L::kKStages) * L::kTile);
@@ -392,30 +455,32 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
             }
             ++np[st];
         };
-        auto wait_v = [&](int c) {
-            if (!warp_wait(&bar_vfull[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        };
+        auto wait_v = [&](int c) { if (!warp_wait(&bar_vclean[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true; };
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
             if (!warp_wait(&bar_q, static_cast<uint32_t>(segs) & 1u)) { stuck = true; break; }
             ++segs;
             if constexpr (TILES == 2) {
                 const int streams = q.rows > BM ? 2 : 1;
-                bool more = wait_k();
+                bool more = next_tile();
                 if (!more) continue;
+                wait_k(ck);
                 for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
                 ++ck;
-                bool add = false;
-                while (more && !stuck) {
-                    wait_v(cv);            // (both are there by the time the first weights are)
-                    more = wait_k();
+                more = next_tile();
+                bool add = false, ended = false;
+                while (!ended && !stuck) {
+                    const bool now = more;             // a tile follows this one
+                    wait_v(cv);                        // (both are there by the time the first weights are)
+                    if (now) wait_k(ck);
                     for (int st = 0; st < streams; ++st) {
                         values(st, cv, add, st == streams - 1);
-                        if (more) scores(st, st, ck, st == streams - 1);
+                        if (now) scores(st, st, ck, st == streams - 1);
+                        if (now && st == 0) more = next_tile();      // looked up while the matrix unit has work
                     }
                     ++cv;
-                    ck += more ? 1 : 0;
+                    ck += now ? 1 : 0;
                     add = true;
+                    ended = !now;
                 }
             } else {
                 // tile i of the segment belongs to stream i & 1; scores run two tiles ahead of the values
@@ -423,7 +488,8 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 bool ended = false;
                 auto next_scores = [&]() {
                     if (ended) return;
-                    if (!wait_k()) { ended = true; return; }
+                    if (!next_tile()) { ended = true; return; }
+                    wait_k(ck);
                     scores(ahead & 1, 0, ck, true);
                     ++ahead;
                     ++ck;
@@ -493,25 +559,29 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
                 tc_fence_after();
                 if (warp_live) {
                     uint32_t sv[BN];
+                    // the second half is on its way while the first one's maximum is found
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     tmem_ld64(t_s, sv);
+                    tmem_wait64(sv);
                     tmem_ld64(t_s + 64, sv + 64);
-                    if ((kind & kMasked) != 0) {
 #pragma unroll
-                        for (int c = 0; c < BN; c += 4) {
-                            const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
-                            if (kp.x > qpos) sv[c] = 0xff800000u;
-                            if (kp.y > qpos) sv[c + 1] = 0xff800000u;
-                            if (kp.z > qpos) sv[c + 2] = 0xff800000u;
-                            if (kp.w > qpos) sv[c + 3] = 0xff800000u;
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) tmem_wait64(sv + 64);
+                        if ((kind & kMasked) != 0) {
+#pragma unroll
+                            for (int c = h * 64; c < h * 64 + 64; c += 4) {
+                                const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
+                                if (kp.x > qpos) sv[c] = 0xff800000u;
+                                if (kp.y > qpos) sv[c + 1] = 0xff800000u;
+                                if (kp.z > qpos) sv[c + 2] = 0xff800000u;
+                                if (kp.w > qpos) sv[c + 3] = 0xff800000u;
+                            }
                         }
+#pragma unroll
+                        for (int c = h * 64; c < h * 64 + 64; c += 8)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) t4[e] = max3(t4[e], __uint_as_float(sv[c + e]), __uint_as_float(sv[c + 4 + e]));
                     }
-                    float t4[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) t4[c] = fmaxf(__uint_as_float(sv[c]), __uint_as_float(sv[c + 4]));
-#pragma unroll
-                    for (int c = 8; c < BN; c += 8)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) t4[e] = max3(t4[e], __uint_as_float(sv[c + e]), __uint_as_float(sv[c + 4 + e]));
                     const float top = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * a.scale_log2;      // -infinity stays what it is: the scale is positive
                     const bool grow = top > m + kRescaleStep;
                     const float m_new = grow ? top : m;
@@ -697,7 +767,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedGroup g, const __grid_con
 }
 
 template <int DH, int TILES>
-int launch(dodo_ctx* ctx, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
+int launch(dodo_ctx* ctx, const Maps& maps, int box, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
     auto kern = attend_paged_dense_kernel<DH, TILES>;
     const int smem = Layout<DH, TILES>::kBytes + 1024;
     bool& set = ctx->paged_attr_set[(DH == 128 ? 2 : 0) + TILES - 1];
@@ -706,7 +776,7 @@ int launch(dodo_ctx* ctx, const PagedGroup& g, const PagedArrays& a, const Dense
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "paged dense attend shared-memory attribute");
         set = true;
     }
-    kern<<<grid, kThreads, smem, st>>>(g, a, w);
+    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w, box);
     return dodo_check_cuda(ctx, cudaGetLastError(), "paged dense attend launch");
 }
 
@@ -714,7 +784,7 @@ int launch(dodo_ctx* ctx, const PagedGroup& g, const PagedArrays& a, const Dense
 
 size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh) { return static_cast<size_t>(2) * num_sms * 2 * BM * (dh + 2) * sizeof(float); }
 
-int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
+int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
     const int tiles = max_rows > BM ? 2 : 1, tile_rows = tiles * BM;
     DenseShare w;
     int64_t total = 0, units = 0;
@@ -735,6 +805,21 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, const PagedGrou
     // one block per SM, but none for less than four tiles or a unit
     const int64_t most = (total + 3) / 4 > units ? (total + 3) / 4 : units;
     const int grid = most < ctx->num_sms ? static_cast<int>(most) : ctx->num_sms;
-    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, g, a, w, grid, st) : launch<128, 1>(ctx, g, a, w, grid, st);
-    return tiles == 2 ? launch<64, 2>(ctx, g, a, w, grid, st) : launch<64, 1>(ctx, g, a, w, grid, st);
+    Maps maps;
+    memset(&maps, 0, sizeof maps);
+    int rc = DODO_OK, box = 1;
+    while (box < BN && a.page % (2 * box) == 0) box *= 2;
+    if (box < 8) box = 1;
+    const int width = a.Hkv * dh, rows = a.pages * a.page;
+    if (a.cK != nullptr) {
+        rc = dodo_encode_bf16_rows(ctx, &maps.cK, a.cK, width, rows, box);
+        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.cV, a.cV, width, rows, box);
+    }
+    if (rc == DODO_OK && a.lK != nullptr) {
+        rc = dodo_encode_bf16_rows(ctx, &maps.lK, a.lK, width, loc_rows, BN);
+        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.lV, a.lV, width, loc_rows, BN);
+    }
+    if (rc != DODO_OK) return rc;
+    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, box, g, a, w, grid, st) : launch<128, 1>(ctx, maps, box, g, a, w, grid, st);
+    return tiles == 2 ? launch<64, 2>(ctx, maps, box, g, a, w, grid, st) : launch<64, 1>(ctx, maps, box, g, a, w, grid, st);
 }

@@ -45,7 +45,7 @@ static constexpr int dodo_paged_part_floats(int dh) { return dh + 4; }
 PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int dtype, int max_rows);
 // many bf16 rows, on the tensor cores; scale of DODO_DENSE_LEAST_SCALE or more
 size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh);
-int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
