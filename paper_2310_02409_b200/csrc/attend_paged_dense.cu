@@ -158,6 +158,15 @@ __device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArr
     return true;
 }
 
+// a hint to L2 for row r of the segment's Q
+template <int DH>
+__device__ __forceinline__ void hint_row(const PagedArrays& a, const PagedSeq& s, const Segment& q, int r) {
+    if (r >= q.rows) return;
+    const __nv_bfloat16* const p = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, q.head, q.r0 + r) * DH;
+#pragma unroll
+    for (int c = 0; c < DH; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + c));
+}
+
 // One row again over all of the unit's keys that it sees: a warp, a key a lane for the scores, four (two) features a lane for the sums
 template <int DH>
 __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, __nv_bfloat16* out) {
@@ -234,7 +243,13 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
     const int T = work.total, G = static_cast<int>(gridDim.x), bid = static_cast<int>(blockIdx.x);
     const int slot_end = block_start(T, G, bid + 1);
     int x = block_start(T, G, bid);
+    Segment q;
 
+    // The first rows of Q are asked for ahead of everything else: behind the first keys of all blocks they would come late.
+    if (warp < kSoftmaxWarps) {
+        int ahead = x;
+        if (next_segment(g, a, work, L::kRows, ahead, slot_end, q)) hint_row<DH>(a, g.seq[q.b], q, tid);
+    }
     if (tid == 0) {
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
@@ -254,7 +269,6 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     bool stuck = false;
-    Segment q;
 
     if (warp == kSoftmaxWarps) {
         // ================================================ scout ===================================================
@@ -283,6 +297,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                     }
                 }
             };
+            for (int r = lane; r < q.rows; r += 32) hint_row<DH>(a, s, q, r);     // the segment's Q, while others are at the one before
             entries(q.t0);
             keys(q.t0);
             entries(q.t0 + 1);
@@ -515,6 +530,11 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, t_s = tmem + st * BN + lanes, t_o = tmem + 2 * BN + lanes;
         float* const xch = reinterpret_cast<float*>(base_ptr + L::kOffXch);
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
+        // a warp's part of Q's tile in shared memory, which takes the results on their way out: its 32 rows, in 16-byte pieces
+        constexpr int kPieces = (TILES == 2 ? DH : DH / 2) / 8, kAtOnce = 32 / kPieces;
+        const int warp_row = (TILES == 2 ? st * BM : 0) + (row & ~31), piece = (TILES == 2 ? 0 : st * kPieces) + lane % kPieces;
+        unsigned char* const warp_tile = base_ptr + (TILES == 2 ? st * L::kTile : 0) + (row & ~31) * 128;
+        auto tile_at = [&](int r, int c) { return warp_tile + (c / 8) * L::kHalf + r * 128 + (((c % 8) ^ (r & 7)) << 4); };
         int ck = 0, ns = 0, os = 0;
         bool first_seg = true;
         // (a wait that has run out ends the waiting, not the walk: the barriers of these warps count all of them)
@@ -523,18 +543,17 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
             const int my = (TILES == 2 ? st * BM : 0) + row;               // this thread's row of the tile of rows
             const bool live = my < q.rows, stream_live = TILES == 1 || st * BM < q.rows, warp_live = (TILES == 2 ? st * BM : 0) + (row & ~31) < q.rows;
             const int qpos = s.q_pos0 + (q.r0 + min(my, q.rows - 1)) / a.group;
-            // ---- Q, row by row, in the layout of the matrix unit's operands (128-byte rows of 64 features, 16-byte pieces swizzled)
+            // ---- Q in the layout of the matrix unit's operands (128-byte rows of 64 features, 16-byte pieces swizzled): a warp brings its
+            // rows (with one tile of rows, its stream's half of their features), neighbouring lanes neighbouring pieces
             {
-                constexpr int kPieces = (TILES == 2 ? DH : DH / 2) / 8;
-                const int piece0 = TILES == 2 ? 0 : st * kPieces;
-                const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, q.head, q.r0 + min(my, q.rows - 1)) * DH);
-                unsigned char* const dst = base_ptr + (TILES == 2 ? st * L::kTile : 0) + row * 128;
+                uint4 v[32 / kAtOnce];
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int c = piece0 + i;
-                    const uint4 v = live ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4*>(dst + (c / 8) * L::kHalf + (((c % 8) ^ (row & 7)) << 4)) = v;
+                for (int i = 0; i < 32 / kAtOnce; ++i) {        // (rows behind the last are the last one again)
+                    const int r = min(warp_row + i * kAtOnce + lane / kPieces, q.rows - 1);
+                    v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, q.head, q.r0 + r) * DH) + piece);
                 }
+#pragma unroll
+                for (int i = 0; i < 32 / kAtOnce; ++i) *reinterpret_cast<uint4*>(tile_at(i * kAtOnce + lane / kPieces, piece)) = v[i];
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar_q);
@@ -650,103 +669,111 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                 w0 = st == 0 ? a0 : a1;
                 w1 = st == 0 ? a1 : a0;
             }
-            const bool whole = q.t0 == 0 && q.t1 == q.nt;
-            const float inv = S != 0.f ? 1.f / S : 0.f;
-            const size_t at = live ? out_row(a, s, q.head, q.r0 + my) : 0;
-            float* const part = a.part + static_cast<size_t>(2 * bid + (first_seg ? 0 : 1)) * L::kPartFloats;
-            bool odd = false;                              // a result that is not finite
-#pragma unroll 1
-            for (int c = f0; c < f0 + kFeat && warp_live; c += 32) {
-                float o[32];
+            auto own = [&](int c, float* o) {              // 32 features of this block's piece, not divided by the sum
                 if (TILES == 2 ? mine == 0 : tiles == 0) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                } else {
-                    uint32_t ov[32];
-                    tmem_ld32(t_o + (TILES == 2 ? st * DH : 0) + c, ov);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = TILES == 2 ? __uint_as_float(ov[e]) : w0 != 0.f ? w0 * __uint_as_float(ov[e]) : 0.f;
-                    if (TILES == 1 && tiles > 1) {
-                        tmem_ld32(t_o + DH + c, ov);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = w1 != 0.f ? fmaf(w1, __uint_as_float(ov[e]), o[e]) : o[e];
-                    }
+                    return;
                 }
-                if (whole) {
+                uint32_t ov[32];
+                tmem_ld32(t_o + (TILES == 2 ? st * DH : 0) + c, ov);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = TILES == 2 ? __uint_as_float(ov[e]) : w0 != 0.f ? w0 * __uint_as_float(ov[e]) : 0.f;
+                if (TILES == 1 && tiles > 1) {
+                    tmem_ld32(t_o + DH + c, ov);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = w1 != 0.f ? fmaf(w1, __uint_as_float(ov[e]), o[e]) : o[e];
+                }
+            };
+            // A unit that is cut: whoever finds all other pieces there joins them with its own, which stays in tensor memory; the
+            // others write theirs.  Pieces: four features of a row side by side, then maxima and sums.
+            int c_first = bid, c_last = bid;
+            bool done = true;
+            if (q.t0 != 0 || q.t1 != q.nt) {
+                c_first = block_of(T, G, q.first_slot);
+                c_last = block_of(T, G, q.first_slot + q.nt - 1);
+                // a block's last unit is the only one that begins in it and goes on: the block's number names it
+                int* const ticket = a.tickets + c_first;
+                if (tid == 0) s_last = ld_acquire_gpu(ticket) == c_last - c_first;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                done = s_last != 0;
+                if (!done) {
+                    float* const part = a.part + static_cast<size_t>(2 * bid + (first_seg ? 0 : 1)) * L::kPartFloats;
+#pragma unroll 1
+                    for (int c = f0; c < f0 + kFeat && warp_live; c += 32) {
+                        float o[32];
+                        own(c, o);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            reinterpret_cast<float4*>(part)[static_cast<size_t>((c + e) / 4) * L::kRows + my] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                    if (TILES == 2 || st == 0) reinterpret_cast<float2*>(part + static_cast<size_t>(DH) * L::kRows)[my] = make_float2(M, S);
+                    __threadfence();
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    if (tid == 0) s_last = atomicAdd(ticket, 1) == c_last - c_first;
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    done = s_last != 0;
+                }
+                if (done) {
+                    if (tid == 0) *ticket = 0;             // clean for the next launch
+                    __threadfence();
+                }
+            }
+            bool odd = false;                              // a result that is not finite
+            if (done && warp_live) {
+                // the unit is the first of every block but the one that it begins in
+                const int begun = c_first < c_last && block_start(T, G, c_first) < q.first_slot ? 1 : 0;
+                auto part_of = [&](int c) { return a.part + static_cast<size_t>(2 * c + (c == c_first ? begun : 0)) * L::kPartFloats; };
+                auto max_sum = [&](int c) { return c == bid ? make_float2(M, S) : __ldcg(reinterpret_cast<const float2*>(part_of(c) + static_cast<size_t>(DH) * L::kRows) + my); };
+                float MM = -INFINITY, SS = 0.f;
+                for (int c = c_first; c <= c_last; ++c) {
+                    const float2 ms = max_sum(c);
+                    const float top = fmaxf(MM, ms.x), k0 = part_weight(MM, top), k1 = part_weight(ms.x, top);
+                    SS = (k0 != 0.f ? k0 * SS : 0.f) + (k1 != 0.f ? k1 * ms.y : 0.f);
+                    MM = top;
+                }
+                const float inv = SS != 0.f ? 1.f / SS : 0.f;
+#pragma unroll 1
+                for (int f = f0; f < f0 + kFeat; f += 32) {
+                    float o[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 1
+                    for (int c = c_first; c <= c_last; ++c) {
+                        const float w = part_weight(max_sum(c).x, MM);
+                        float v[32];
+                        if (c == bid) {
+                            own(f, v);
+                        } else {
+                            const float4* const src = reinterpret_cast<const float4*>(part_of(c)) + static_cast<size_t>(f / 4) * L::kRows + my;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 x4 = __ldcg(src + static_cast<size_t>(e / 4) * L::kRows);
+                                v[e] = x4.x; v[e + 1] = x4.y; v[e + 2] = x4.z; v[e + 3] = x4.w;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = w != 0.f ? fmaf(w, v[e], o[e]) : o[e];
+                    }
                     float zero = 0.f;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) { o[e] *= inv; zero = fmaf(o[e], 0.f, zero); }
                     odd = odd || !(zero == 0.f);
-                    if (live) {
-                        uint4* const dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + at * DH + c);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            dst[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
-                                                pack_bf16(o[8 * e + 6], o[8 * e + 7]));
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) part[static_cast<size_t>(c + e) * L::kRows + my] = o[e];
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint4*>(tile_at(lane, f / 8 + e)) = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                                                                         pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7]));
                 }
-            }
-            if (TILES == 2 || st == 0) {
-                if (whole) {
-                    if (live && a.lse != nullptr) a.lse[at] = S != 0.f ? (M + log2f(S)) * 0.6931471805599453f : -INFINITY;
-                } else {
-                    part[static_cast<size_t>(DH) * L::kRows + my] = M;
-                    part[static_cast<size_t>(DH + 1) * L::kRows + my] = S;
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 32 / kAtOnce; ++i) {
+                    const int r = i * kAtOnce + lane / kPieces;
+                    if (warp_row + r < q.rows)
+                        reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + warp_row + r) * DH)[piece] =
+                            *reinterpret_cast<const uint4*>(tile_at(r, piece));
                 }
-            }
-            bool done = whole;
-            if (!whole) {
-                const int c_first = block_of(T, G, q.first_slot), c_last = block_of(T, G, q.first_slot + q.nt - 1);
-                __threadfence();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (tid == 0) {
-                    // a block's last unit is the only one that begins in it and goes on: the block's number names it
-                    const int arrived = atomicAdd(a.tickets + c_first, 1);
-                    s_last = arrived == c_last - c_first;
-                    if (s_last) a.tickets[c_first] = 0;    // clean for the next launch
-                }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                done = s_last != 0;
-                if (done && warp_live) {
-                    __threadfence();
-                    auto piece = [&](int c) { return a.part + static_cast<size_t>(2 * c + (block_start(T, G, c) >= q.first_slot ? 0 : 1)) * L::kPartFloats + my; };
-                    float MM = -INFINITY, SS = 0.f;
-                    for (int c = c_first; c <= c_last; ++c) MM = fmaxf(MM, __ldcg(piece(c) + static_cast<size_t>(DH) * L::kRows));
-                    for (int c = c_first; c <= c_last; ++c) {
-                        const float* const pc = piece(c);
-                        const float w = part_weight(__ldcg(pc + static_cast<size_t>(DH) * L::kRows), MM);
-                        if (w != 0.f) SS = fmaf(w, __ldcg(pc + static_cast<size_t>(DH + 1) * L::kRows), SS);
-                    }
-                    const float sinv = SS != 0.f ? 1.f / SS : 0.f;
-#pragma unroll 1
-                    for (int f = f0; f < f0 + kFeat; f += 32) {
-                        float o[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                        for (int c = c_first; c <= c_last; ++c) {
-                            const float* const pc = piece(c);
-                            const float w = part_weight(__ldcg(pc + static_cast<size_t>(DH) * L::kRows), MM);
-                            if (w == 0.f) continue;
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = fmaf(w, __ldcg(pc + static_cast<size_t>(f + e) * L::kRows), o[e]);
-                        }
-                        float zero = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) { o[e] *= sinv; zero = fmaf(o[e], 0.f, zero); }
-                        odd = odd || !(zero == 0.f);
-                        if (live) {
-                            uint4* const dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + at * DH + f);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                dst[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
-                                                    pack_bf16(o[8 * e + 6], o[8 * e + 7]));
-                        }
-                    }
-                    if (live && a.lse != nullptr && (TILES == 2 || st == 0)) a.lse[at] = SS != 0.f ? (MM + log2f(SS)) * 0.6931471805599453f : -INFINITY;
-                }
+                __syncwarp();
+                if (live && a.lse != nullptr && (TILES == 2 || st == 0)) a.lse[out_row(a, s, q.head, q.r0 + my)] = SS != 0.f ? (MM + log2f(SS)) * 0.6931471805599453f : -INFINITY;
             }
             // ---- results that are not finite, once more over what their rows see
             if (any_softmax(odd && live && done)) {            // (behind it, both streams' O are read too)
@@ -802,9 +829,23 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     w.slot0[g.nseq] = static_cast<int>(total);
     w.total = static_cast<int>(total);
     if (total == 0) return DODO_OK;
-    // one block per SM, but none for less than four tiles or a unit
+    // One block per SM, but none for less than four tiles or a unit.  Where all units are alike there is also the share of a k-th of a
+    // unit each: no block then works for two units.  By the count of tiles' times of the slowest block: a unit begun and ended costs about
+    // three (Q, a pipeline filled and emptied, results), pieces joined another three.
     const int64_t most = (total + 3) / 4 > units ? (total + 3) / 4 : units;
-    const int grid = most < ctx->num_sms ? static_cast<int>(most) : ctx->num_sms;
+    int64_t grid = most < ctx->num_sms ? most : ctx->num_sms;
+    bool alike = true;
+    int nt = 0;
+    for (int i = 0; i < g.nseq; ++i)
+        if (g.seq[i].tq > 0) { alike = alike && (nt == 0 || nt == w.nt[i]); nt = w.nt[i]; }
+    if (alike && units <= ctx->num_sms) {
+        const int64_t each = (total + grid - 1) / grid;
+        int64_t cost = each + 3 * ((each + nt - 1) / nt + 1) + 3;
+        for (int64_t k = 1; k <= ctx->num_sms / units && k <= (nt + 3) / 4; ++k) {
+            const int64_t c = (nt + k - 1) / k + 3 + (k > 1 ? 3 : 0);
+            if (c < cost) { cost = c; grid = units * k; }
+        }
+    }
     Maps maps;
     memset(&maps, 0, sizeof maps);
     int rc = DODO_OK, box = 1;
@@ -820,6 +861,6 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
         if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.lV, a.lV, width, loc_rows, BN);
     }
     if (rc != DODO_OK) return rc;
-    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, box, g, a, w, grid, st) : launch<128, 1>(ctx, maps, box, g, a, w, grid, st);
-    return tiles == 2 ? launch<64, 2>(ctx, maps, box, g, a, w, grid, st) : launch<64, 1>(ctx, maps, box, g, a, w, grid, st);
+    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, box, g, a, w, static_cast<int>(grid), st) : launch<128, 1>(ctx, maps, box, g, a, w, static_cast<int>(grid), st);
+    return tiles == 2 ? launch<64, 2>(ctx, maps, box, g, a, w, static_cast<int>(grid), st) : launch<64, 1>(ctx, maps, box, g, a, w, static_cast<int>(grid), st);
 }
