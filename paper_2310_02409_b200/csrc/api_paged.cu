@@ -33,7 +33,15 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, boo
     g.cta0[g.nseq] = static_cast<int>(cta);
 }
 
-namespace { constexpr int kFewRows = 16; }
+namespace {
+constexpr int kFewRows = 16;
+// n / d = n * mul >> shift for 0 <= n < 2^31: mul = ceil(2^shift / d) with 2^(shift - 31) >= d is at most d / 2^shift too large
+void divide_by(int d, uint32_t& mul, int& shift) {
+    shift = 31;
+    while ((int64_t{1} << (shift - 31)) < d) ++shift;
+    mul = static_cast<uint32_t>(((uint64_t{1} << shift) + d - 1) / d);
+}
+}  // namespace
 
 extern "C" {
 
@@ -79,11 +87,9 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
     a.lK = any_local ? locK : nullptr; a.lV = any_local ? locV : nullptr;
     a.pos = cache->pos; a.table = cache->table;
     a.pages = cache->pages; a.page = cache->page;
-    int log2 = 0;
-    while ((int64_t{1} << log2) < cache->page) ++log2;
-    a.page_shift = 31 + log2;
-    a.page_mul = static_cast<uint32_t>(((uint64_t{1} << a.page_shift) + cache->page - 1) / cache->page);
     a.H = H; a.Hkv = Hkv; a.group = H / Hkv;
+    divide_by(cache->page, a.page_mul, a.page_shift);
+    divide_by(a.group, a.group_mul, a.group_shift);
     a.scale_log2 = sm_scale * 1.4426950408889634f;
     a.lse = lse;
     a.part = static_cast<float*>(workspace);

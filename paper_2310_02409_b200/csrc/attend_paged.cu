@@ -32,7 +32,7 @@ attend_paged_rows_kernel(const __grid_constant__ PagedGroup g, const __grid_cons
     const int R = s.tq * a.group, r0 = p.tile * tile_rows, rows = min(tile_rows, R - r0);
     const int wr = warp % row_warps, wk = warp / row_warps, w0 = r0 + wr * QR;          // this warp's first row
     const int live = min(QR, R - w0);                                                   // its rows, none where <= 0
-    const int last_pos = s.q_pos0 + (min(r0 + rows, R) - 1) / a.group;
+    const int last_pos = s.q_pos0 + token_of(a, min(r0 + rows, R) - 1);
     const int end_all = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, last_pos);
     const int begin = p.chunk * s.chunk_keys, end = min(begin + s.chunk_keys, end_all);
     const size_t pitch = static_cast<size_t>(a.Hkv) * DH;
@@ -47,9 +47,9 @@ attend_paged_rows_kernel(const __grid_constant__ PagedGroup g, const __grid_cons
         for (int e = 0; e < E; ++e) { q[r][e] *= a.scale_log2; acc[r][e] = 0.f; }
     }
     const int my_pair = lane % LK / COPY, my_row = my_pair / U, my_u = my_pair % U;
-    const int my_qpos = s.q_pos0 + (w0 + my_row) / a.group;
+    const int my_qpos = s.q_pos0 + token_of(a, w0 + my_row);
     const bool my_live = my_row < live;
-    const int most_pos = live > 0 ? s.q_pos0 + (w0 + live - 1) / a.group : static_cast<int>(0x80000000);
+    const int most_pos = live > 0 ? s.q_pos0 + token_of(a, w0 + live - 1) : static_cast<int>(0x80000000);
     float m = -INFINITY, l = 0.f;
 
     // step t of this warp: keys first(t) .. first(t) + KS - 1, key first(t) + i with lane i

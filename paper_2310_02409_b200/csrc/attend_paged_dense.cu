@@ -37,7 +37,8 @@ constexpr int kPosReaders = kSoftmaxWarps + 3;      // softmax, issuer, producer
 // scores) and the one of the others: 216 + 216 + 72 = 3 x 168
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 constexpr int kPosSlots = 4;
-constexpr float kRescaleStep = 8.f;
+// A row's reference maximum moves only when a score passes it by this many octaves: weights of up to 2^24 cost no digit in bf16 or fp32
+constexpr float kRescaleStep = 24.f;
 enum { kMasked = 1, kEnd = 2, kLocal = 4, kHoles = 8 };     // of a tile; kHoles: some of its keys are not there or seen by nobody
 
 template <int DH, int TILES>
@@ -48,7 +49,8 @@ struct Layout {
     static constexpr int kKStages = TILES == 1 || DH == 64 ? 3 : 2, kVStages = TILES == 1 && DH == 128 ? 2 : kKStages;
     static constexpr int kOffK = TILES * kTile, kOffV = kOffK + kKStages * kTile, kOffPos = kOffV + kVStages * kTile;
     static constexpr int kOffXch = kOffPos + 2 * kPosSlots * BN * 4;      // maxima and sums that the streams of one tile of rows exchange
-    static constexpr int kBytes = kOffXch + (TILES == 1 ? 2 * 2 * BM * 4 : 0);
+    static constexpr int kOffOut = kOffXch + (TILES == 1 ? 2 * 2 * BM * 4 : 0);      // results on their way out: 32 rows x 32 features a warp
+    static constexpr int kBytes = kOffOut + kSoftmaxWarps * 2048;
     static constexpr int kRows = TILES * BM;
     static constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (DH + 2);
 };
@@ -150,8 +152,8 @@ __device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArr
     q.t1 = min(q.nt, q.t0 + end - x);
     q.r0 = q.tile * tile_rows;
     q.rows = min(tile_rows, s.tq * a.group - q.r0);
-    q.min_pos = s.q_pos0 + q.r0 / a.group;
-    q.last_pos = s.q_pos0 + (q.r0 + q.rows - 1) / a.group;
+    q.min_pos = s.q_pos0 + token_of(a, q.r0);
+    q.last_pos = s.q_pos0 + token_of(a, q.r0 + q.rows - 1);
     q.c_tiles = (s.c_len + BN - 1) / BN;
     q.l_vis = dodo_visible_local(s.l_len, s.l_pos0, q.last_pos);
     x += q.t1 - q.t0;
@@ -174,7 +176,7 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
     const int lane = static_cast<int>(threadIdx.x) & 31;
     const size_t pitch = static_cast<size_t>(a.Hkv) * DH, at = static_cast<size_t>(head) * DH;
     const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, head, r) * DH;
-    const int qpos = s.q_pos0 + r / a.group, end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
+    const int qpos = s.q_pos0 + token_of(a, r), end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
     float m = -INFINITY, l = 0.f, acc[F];
 #pragma unroll
     for (int f = 0; f < F; ++f) acc[f] = 0.f;
@@ -530,34 +532,38 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, t_s = tmem + st * BN + lanes, t_o = tmem + 2 * BN + lanes;
         float* const xch = reinterpret_cast<float*>(base_ptr + L::kOffXch);
         const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
-        // a warp's part of Q's tile in shared memory, which takes the results on their way out: its 32 rows, in 16-byte pieces
+        // Q in the layout of the matrix unit's operands (128-byte rows of 64 features, 16-byte pieces swizzled): a warp brings its 32 rows
+        // (with one tile of rows, its stream's half of their features), neighbouring lanes neighbouring pieces
         constexpr int kPieces = (TILES == 2 ? DH : DH / 2) / 8, kAtOnce = 32 / kPieces;
         const int warp_row = (TILES == 2 ? st * BM : 0) + (row & ~31), piece = (TILES == 2 ? 0 : st * kPieces) + lane % kPieces;
-        unsigned char* const warp_tile = base_ptr + (TILES == 2 ? st * L::kTile : 0) + (row & ~31) * 128;
-        auto tile_at = [&](int r, int c) { return warp_tile + (c / 8) * L::kHalf + r * 128 + (((c % 8) ^ (r & 7)) << 4); };
+        unsigned char* const q_tile = base_ptr + (TILES == 2 ? st * L::kTile : 0) + (piece / 8) * L::kHalf + (row & ~31) * 128;
+        auto bring_q = [&](const Segment& u) {
+            uint4 v[32 / kAtOnce];
+#pragma unroll
+            for (int i = 0; i < 32 / kAtOnce; ++i) {        // (rows behind the last are the last one again)
+                const int r = min(warp_row + i * kAtOnce + lane / kPieces, u.rows - 1);
+                v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, g.seq[u.b], u.head, u.r0 + r) * DH) + piece);
+            }
+#pragma unroll
+            for (int i = 0; i < 32 / kAtOnce; ++i) {
+                const int r = i * kAtOnce + lane / kPieces;
+                *reinterpret_cast<uint4*>(q_tile + r * 128 + (((piece % 8) ^ (r & 7)) << 4)) = v[i];
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar_q);
+        };
+        unsigned char* const out_tile = base_ptr + L::kOffOut + warp * 2048;
         int ck = 0, ns = 0, os = 0;
         bool first_seg = true;
         // (a wait that has run out ends the waiting, not the walk: the barriers of these warps count all of them)
-        while (next_segment(g, a, work, L::kRows, x, slot_end, q)) {
+        bool more = next_segment(g, a, work, L::kRows, x, slot_end, q);
+        if (more) bring_q(q);
+        while (more) {
             const PagedSeq& s = g.seq[q.b];
             const int my = (TILES == 2 ? st * BM : 0) + row;               // this thread's row of the tile of rows
             const bool live = my < q.rows, stream_live = TILES == 1 || st * BM < q.rows, warp_live = (TILES == 2 ? st * BM : 0) + (row & ~31) < q.rows;
-            const int qpos = s.q_pos0 + (q.r0 + min(my, q.rows - 1)) / a.group;
-            // ---- Q in the layout of the matrix unit's operands (128-byte rows of 64 features, 16-byte pieces swizzled): a warp brings its
-            // rows (with one tile of rows, its stream's half of their features), neighbouring lanes neighbouring pieces
-            {
-                uint4 v[32 / kAtOnce];
-#pragma unroll
-                for (int i = 0; i < 32 / kAtOnce; ++i) {        // (rows behind the last are the last one again)
-                    const int r = min(warp_row + i * kAtOnce + lane / kPieces, q.rows - 1);
-                    v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, q.head, q.r0 + r) * DH) + piece);
-                }
-#pragma unroll
-                for (int i = 0; i < 32 / kAtOnce; ++i) *reinterpret_cast<uint4*>(tile_at(i * kAtOnce + lane / kPieces, piece)) = v[i];
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar_q);
-            }
+            const int qpos = s.q_pos0 + token_of(a, q.r0 + min(my, q.rows - 1));
             float m = -INFINITY, l = 0.f;
             int mine = 0, tiles = 0;         // tiles of this stream; of the segment
             while (!stuck) {
@@ -578,67 +584,84 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                 tc_fence_after();
                 if (warp_live) {
                     uint32_t sv[BN];
-                    // the second half is on its way while the first one's maximum is found
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    tmem_ld64(t_s, sv);
+                    auto load_half = [&](int h) {
+                        if (h == 0) tmem_ld64(t_s, sv);
+                        else tmem_ld64(t_s + 64, sv + 64);
+                    };
+                    auto mask_half = [&](int h) {
+#pragma unroll
+                        for (int c = h * 64; c < h * 64 + 64; c += 4) {
+                            const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
+                            if (kp.x > qpos) sv[c] = 0xff800000u;
+                            if (kp.y > qpos) sv[c + 1] = 0xff800000u;
+                            if (kp.z > qpos) sv[c + 2] = 0xff800000u;
+                            if (kp.w > qpos) sv[c + 3] = 0xff800000u;
+                        }
+                    };
+                    load_half(0);
                     tmem_wait64(sv);
-                    tmem_ld64(t_s + 64, sv + 64);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (h == 1) tmem_wait64(sv + 64);
-                        if ((kind & kMasked) != 0) {
-#pragma unroll
-                            for (int c = h * 64; c < h * 64 + 64; c += 4) {
-                                const int4 kp = *reinterpret_cast<const int4*>(s_pos + ps * BN + c);
-                                if (kp.x > qpos) sv[c] = 0xff800000u;
-                                if (kp.y > qpos) sv[c + 1] = 0xff800000u;
-                                if (kp.z > qpos) sv[c + 2] = 0xff800000u;
-                                if (kp.w > qpos) sv[c + 3] = 0xff800000u;
-                            }
-                        }
-#pragma unroll
-                        for (int c = h * 64; c < h * 64 + 64; c += 8)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) t4[e] = max3(t4[e], __uint_as_float(sv[c + e]), __uint_as_float(sv[c + 4 + e]));
-                    }
-                    const float top = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * a.scale_log2;      // -infinity stays what it is: the scale is positive
-                    const bool grow = top > m + kRescaleStep;
-                    const float m_new = grow ? top : m;
-                    if (mine > 0 && __any_sync(0xffffffffu, grow)) {
-                        // P V of this stream's tile before is complete: its scores of this tile were issued behind it
-                        const float corr = grow ? part_weight(m, m_new) : 1.f;
-                        l *= corr;
-#pragma unroll 1
-                        for (int c = 0; c < DH; c += 32) {
-                            uint32_t ov[32];
-                            tmem_ld32(t_o + st * DH + c, ov);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-                            tmem_st32(t_o + st * DH + c, ov);
-                        }
-                    }
-                    m = m_new;
-                    const float nm = m == -INFINITY ? 0.f : -m;
-                    const float2 nm2 = make_float2(nm, nm);
+                    load_half(1);
+                    if ((kind & kMasked) != 0) mask_half(0);
+                    tmem_wait64(sv + 64);
+                    if ((kind & kMasked) != 0) mask_half(1);
                     float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                        for (int c = h * BN / 2; c < (h + 1) * BN / 2; c += 4) {
-                            const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c2, nm2);
-                            const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), c2, nm2);
-                            const float2 p0 = make_float2(exp2_fast(x0.x), exp2_fast(x0.y));
-                            const float2 p1 = make_float2(exp2_fast(x1.x), exp2_fast(x1.y));
-                            sv[c / 2] = pack_bf16(p0.x, p0.y);
-                            sv[c / 2 + 1] = pack_bf16(p1.x, p1.y);
-                            sum0 = __fadd2_rn(sum0, p0);
-                            sum1 = __fadd2_rn(sum1, p1);
-                        }
+                    float2 nm2 = make_float2(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m);
+                    // weights of scores c to c + 3, packed where scores have been read
+                    auto weights = [&](int c) {
+                        const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c2, nm2);
+                        const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), c2, nm2);
+                        const float2 p0 = make_float2(exp2_fast(x0.x), exp2_fast(x0.y));
+                        const float2 p1 = make_float2(exp2_fast(x1.x), exp2_fast(x1.y));
+                        sv[c / 2] = pack_bf16(p0.x, p0.y);
+                        sv[c / 2 + 1] = pack_bf16(p1.x, p1.y);
+                        sum0 = __fadd2_rn(sum0, p0);
+                        sum1 = __fadd2_rn(sum1, p1);
+                    };
+                    auto publish = [&](int h) {
                         tmem_st32(t_s + h * 32, sv + h * 32);
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&bar_p[st][h]);
+                    };
+                    // The first half's weights by the reference maximum that there is; the tile's own is found beside them, and only where
+                    // it has grown too far (the first tile among these) is the tile begun again.
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 4) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) t4[e] = max3(t4[e], __uint_as_float(sv[c + e]), __uint_as_float(sv[BN / 2 + c + e]));
+                        weights(c);
                     }
+                    float top = fmaxf(max3(t4[0], t4[1], t4[2]), t4[3]) * a.scale_log2;      // -infinity stays what it is: the scale is positive
+                    const bool grow = top > m + kRescaleStep;
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float m_new = grow ? top : m;
+                        if (mine > 0) {
+                            // P V of this stream's tile before is complete: its scores of this tile were issued behind it
+                            const float corr = grow ? part_weight(m, m_new) : 1.f;
+                            l *= corr;
+#pragma unroll 1
+                            for (int c = 0; c < DH; c += 32) {
+                                uint32_t ov[32];
+                                tmem_ld32(t_o + st * DH + c, ov);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+                                tmem_st32(t_o + st * DH + c, ov);
+                            }
+                        }
+                        m = m_new;
+                        nm2.x = nm2.y = m == -INFINITY ? 0.f : -m;
+                        sum0 = sum1 = make_float2(0.f, 0.f);
+                        load_half(0);
+                        tmem_wait64(sv);
+                        if ((kind & kMasked) != 0) mask_half(0);
+#pragma unroll
+                        for (int c = 0; c < BN / 2; c += 4) weights(c);
+                    }
+                    publish(0);
+#pragma unroll
+                    for (int c = BN / 2; c < BN; c += 4) weights(c);
+                    publish(1);
                     l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 } else if (lane == 0) {
                     mbar_arrive(&bar_p[st][0]);
@@ -654,6 +677,10 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                 tc_fence_after();
             }
             if (l != l) m = INFINITY;        // a NaN among the logits that the row sees: the whole row's, wherever its maximum stands
+            // The matrix unit is through with Q: it gets the next segment's now, and has work while this one's results go out.
+            Segment next;
+            more = next_segment(g, a, work, L::kRows, x, slot_end, next);
+            if (more) bring_q(next);
             // ---- a row's result: of its stream, or of both, each thread then half of the features
             constexpr int kFeat = TILES == 2 ? DH : DH / 2;
             const int f0 = TILES == 2 ? 0 : st * kFeat;
@@ -733,19 +760,19 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                     MM = top;
                 }
                 const float inv = SS != 0.f ? 1.f / SS : 0.f;
-#pragma unroll 1
-                for (int f = f0; f < f0 + kFeat; f += 32) {
-                    float o[32];
+                float o[kFeat];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                for (int e = 0; e < kFeat; ++e) o[e] = 0.f;
 #pragma unroll 1
-                    for (int c = c_first; c <= c_last; ++c) {
-                        const float w = part_weight(max_sum(c).x, MM);
+                for (int c = c_first; c <= c_last; ++c) {
+                    const float w = part_weight(max_sum(c).x, MM);
+#pragma unroll
+                    for (int f = 0; f < kFeat; f += 32) {
                         float v[32];
                         if (c == bid) {
-                            own(f, v);
+                            own(f0 + f, v);
                         } else {
-                            const float4* const src = reinterpret_cast<const float4*>(part_of(c)) + static_cast<size_t>(f / 4) * L::kRows + my;
+                            const float4* const src = reinterpret_cast<const float4*>(part_of(c)) + static_cast<size_t>((f0 + f) / 4) * L::kRows + my;
 #pragma unroll
                             for (int e = 0; e < 32; e += 4) {
                                 const float4 x4 = __ldcg(src + static_cast<size_t>(e / 4) * L::kRows);
@@ -753,26 +780,31 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                             }
                         }
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = w != 0.f ? fmaf(w, v[e], o[e]) : o[e];
+                        for (int e = 0; e < 32; ++e) o[f + e] = w != 0.f ? fmaf(w, v[e], o[f + e]) : o[f + e];
                     }
-                    float zero = 0.f;
+                }
+                float zero = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) { o[e] *= inv; zero = fmaf(o[e], 0.f, zero); }
-                    odd = odd || !(zero == 0.f);
+                for (int e = 0; e < kFeat; ++e) { o[e] *= inv; zero = fmaf(o[e], 0.f, zero); }
+                odd = !(zero == 0.f);
+                // out through shared memory, 32 features at a time: four lanes a row, eight rows an instruction
+#pragma unroll
+                for (int f = 0; f < kFeat; f += 32) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint4*>(tile_at(lane, f / 8 + e)) = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
-                                                                                         pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7]));
-                }
-                __syncwarp();
+                        *reinterpret_cast<uint4*>(out_tile + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4)) =
+                            make_uint4(pack_bf16(o[f + 8 * e], o[f + 8 * e + 1]), pack_bf16(o[f + 8 * e + 2], o[f + 8 * e + 3]),
+                                       pack_bf16(o[f + 8 * e + 4], o[f + 8 * e + 5]), pack_bf16(o[f + 8 * e + 6], o[f + 8 * e + 7]));
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32 / kAtOnce; ++i) {
-                    const int r = i * kAtOnce + lane / kPieces;
-                    if (warp_row + r < q.rows)
-                        reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + warp_row + r) * DH)[piece] =
-                            *reinterpret_cast<const uint4*>(tile_at(r, piece));
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 8 + lane / 4, e = lane % 4;
+                        if (warp_row + r < q.rows)
+                            reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + warp_row + r) * DH + f0 + f)[e] =
+                                *reinterpret_cast<const uint4*>(out_tile + r * 64 + ((e ^ (r >> 1 & 3)) << 4));
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 if (live && a.lse != nullptr && (TILES == 2 || st == 0)) a.lse[out_row(a, s, q.head, q.r0 + my)] = SS != 0.f ? (MM + log2f(SS)) * 0.6931471805599453f : -INFINITY;
             }
             // ---- results that are not finite, once more over what their rows see
@@ -785,6 +817,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
                 }
             }
             first_seg = false;
+            q = next;
         }
     }
     if (stuck && lane == 0) atomicOr(a.status, DODO_DEV_WAIT_TIMEOUT);

@@ -28,6 +28,8 @@ struct PagedArrays {
     uint32_t page_mul;          // n / page = n * page_mul >> page_shift for n < 2^31
     int page_shift;
     int H, Hkv, group;          // query heads, KV heads, H / Hkv
+    uint32_t group_mul;         // n / group = n * group_mul >> group_shift for n < 2^31
+    int group_shift;
     float scale_log2;
     void* O;
     float* lse;
@@ -109,8 +111,11 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16*
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// token of row r, and the row of Q and O that it is
+__device__ __forceinline__ int token_of(const PagedArrays& a, int r) { return static_cast<int>(static_cast<uint64_t>(r) * a.group_mul >> a.group_shift); }
 __device__ __forceinline__ size_t out_row(const PagedArrays& a, const PagedSeq& s, int head, int r) {
-    return static_cast<size_t>(s.q_row0 + r / a.group) * a.H + head * a.group + r % a.group;
+    const int t = token_of(a, r);
+    return static_cast<size_t>(s.q_row0 + t) * a.H + head * a.group + (r - t * a.group);
 }
 
 // The end of a block of kThreads threads: `parts` partial results of `rows` rows in shared memory (sums of weighted V [part][row][DH]
