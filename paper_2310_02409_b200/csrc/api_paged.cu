@@ -9,14 +9,26 @@ int dodo_check_paged(dodo_ctx* ctx, const dodo_paged_cache* c, const int32_t* pa
 // Without room for partial rows no list is cut.
 void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, bool may_cut) {
     auto tiles_of = [&](const PagedSeq& s) {
-        const int64_t keys = static_cast<int64_t>(s.c_len) + dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1);
-        return (keys + cut.keys - 1) / cut.keys;
+        // (tiles of cached rows, then tiles of local tokens: one more than there are keys for, at most)
+        return (static_cast<int64_t>(s.c_len) + cut.keys - 1) / cut.keys + (dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) + cut.keys - 1) / cut.keys;
     };
     auto units_of = [&](const PagedSeq& s) { return (static_cast<int64_t>(s.tq) * group + cut.rows - 1) / cut.rows * Hkv; };
     int64_t work = 0;
     for (int i = 0; i < g.nseq; ++i) work += units_of(g.seq[i]) * tiles_of(g.seq[i]);
     int64_t share = (work + cut.target - 1) / cut.target;
     if (share < cut.least / cut.keys) share = cut.least / cut.keys;
+    // chunks of whole tiles may come to a few blocks more than the device holds at once, whose turn would come behind all others:
+    // larger chunks then, unless the units alone are that many
+    for (int round = 0; round < 16; ++round) {
+        int64_t blocks = 0, units = 0;
+        for (int i = 0; i < g.nseq; ++i) {
+            const int64_t u = units_of(g.seq[i]), n = tiles_of(g.seq[i]);
+            units += u;
+            blocks += u * (n > share ? (n + share - 1) / share : 1);
+        }
+        if (blocks <= cut.target || units >= cut.target) break;
+        share += 1 + (blocks - cut.target) * share / (4 * blocks);
+    }
     int64_t part = 0, tick = 0, cta = 0;
     for (int i = 0; i < g.nseq; ++i) {
         PagedSeq& s = g.seq[i];
@@ -47,7 +59,7 @@ extern "C" {
 
 size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh) {
     if (ctx == nullptr || dh <= 0) return 0;
-    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, DODO_F32, 32)) * dodo_paged_part_floats(dh) * sizeof(float);
+    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, 32)) * dodo_paged_part_floats(dh) * sizeof(float);
     const size_t dense = dodo_paged_dense_workspace_bytes(ctx->num_sms, dh);
     return rows > dense ? rows : dense;
 }
@@ -112,10 +124,12 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
             if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
             continue;
         }
-        const PagedCut cut = dodo_paged_rows_cut(ctx, dtype, max_rows);
+        const bool token = dtype == DODO_BF16 && dodo_paged_box(cache->page, 8) > 0;
+        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, max_rows);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
         dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);
-        if ((rc = dodo_launch_paged_rows(ctx, dtype, dh, max_rows, g, a, st)) != DODO_OK) return rc;
+        rc = token ? dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st) : dodo_launch_paged_rows(ctx, dtype, dh, max_rows, g, a, st);
+        if (rc != DODO_OK) return rc;
     }
     return DODO_OK;
 }

@@ -209,8 +209,7 @@ cudaError_t launch(const Shape& sh, const PagedGroup& g, const PagedArrays& a, c
 
 }  // namespace
 
-PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int dtype, int max_rows) {
-    (void)dtype;
+PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int max_rows) {
     const Shape sh = shape_for(max_rows);
     return {sh.rows * sh.row_warps, 32, 4 * ctx->num_sms, 128};
 }

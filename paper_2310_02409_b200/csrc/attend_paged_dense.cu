@@ -55,7 +55,6 @@ struct Layout {
     static constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (DH + 2);
 };
 
-struct Maps { CUtensorMap cK, cV, lK, lV; };
 struct DenseShare {
     int total;                      // slots
     int slot0[DODO_GROUP + 1];      // first slot of each sequence
@@ -169,67 +168,10 @@ __device__ __forceinline__ void hint_row(const PagedArrays& a, const PagedSeq& s
     for (int c = 0; c < DH; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + c));
 }
 
-// One row again over all of the unit's keys that it sees: a warp, a key a lane for the scores, four (two) features a lane for the sums
-template <int DH>
-__device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, __nv_bfloat16* out) {
-    constexpr int F = DH / 32;
-    const int lane = static_cast<int>(threadIdx.x) & 31;
-    const size_t pitch = static_cast<size_t>(a.Hkv) * DH, at = static_cast<size_t>(head) * DH;
-    const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, head, r) * DH;
-    const int qpos = s.q_pos0 + token_of(a, r), end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
-    float m = -INFINITY, l = 0.f, acc[F];
-#pragma unroll
-    for (int f = 0; f < F; ++f) acc[f] = 0.f;
-#pragma unroll 1
-    for (int j0 = 0; j0 < end; j0 += 32) {
-        const Key k = key_at(a, s, j0 + lane, end, page_entry(a, s, j0 + lane, end));
-        const bool sees = k.row >= 0 && k.pos <= qpos;
-        float x = -INFINITY;
-        if (sees) {
-            const __nv_bfloat16* const kr = static_cast<const __nv_bfloat16*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
-            x = 0.f;
-#pragma unroll 4
-            for (int c = 0; c < DH; c += 8) {
-                float kf[8], qf[8];
-                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(kr + c)), kf);
-                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(q + c)), qf);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x = fmaf(kf[e], qf[e], x);
-            }
-            x *= a.scale_log2;
-        }
-        float top = fmaxf(m, x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ref = top == -INFINITY ? 0.f : top, corr = part_weight(m, ref), w = exp2_fast(x - ref);
-        m = top;
-        l = fmaf(l, corr, w);
-        const float rounded = __bfloat162float(__float2bfloat16_rn(w));
-#pragma unroll
-        for (int f = 0; f < F; ++f) acc[f] *= corr;
-        uint32_t seen = __ballot_sync(0xffffffffu, sees);
-        while (seen != 0u) {
-            const int e = __ffs(seen) - 1;
-            seen &= seen - 1u;
-            const int row = __shfl_sync(0xffffffffu, k.row, e);
-            const bool local = __shfl_sync(0xffffffffu, k.local ? 1 : 0, e) != 0;
-            const float c = __shfl_sync(0xffffffffu, rounded, e);
-            const __nv_bfloat16* const vr = static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
-#pragma unroll
-            for (int f = 0; f < F; ++f) acc[f] = fmaf(c, __bfloat162float(vr[f]), acc[f]);
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int f = 0; f < F; ++f) out[lane * F + f] = __float2bfloat16_rn(acc[f] * inv);
-}
-
 template <int DH, int TILES>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
-                          const __grid_constant__ DenseShare work, int box) {
+attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
+                          const __grid_constant__ DenseShare work) {
     using L = Layout<DH, TILES>;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -348,7 +290,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
 #pragma unroll
                     for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + h * L::kHalf, loc, col + 64 * h, r, bar);
                 }
-            } else if (box >= 8) {
+            } else if (const int box = maps.rows; box >= 8) {
                 int count = 0;
                 for (int k = lane * box; k < BN; k += 32 * box) count += rows[k] >= 0 ? 1 : 0;
                 count = __reduce_add_sync(0xffffffffu, count);
@@ -827,7 +769,7 @@ attend_paged_dense_kernel(const __grid_constant__ Maps maps, const __grid_consta
 }
 
 template <int DH, int TILES>
-int launch(dodo_ctx* ctx, const Maps& maps, int box, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
+int launch(dodo_ctx* ctx, const PagedBoxes& maps, const PagedGroup& g, const PagedArrays& a, const DenseShare& w, int grid, cudaStream_t st) {
     auto kern = attend_paged_dense_kernel<DH, TILES>;
     const int smem = Layout<DH, TILES>::kBytes + 1024;
     bool& set = ctx->paged_attr_set[(DH == 128 ? 2 : 0) + TILES - 1];
@@ -836,7 +778,7 @@ int launch(dodo_ctx* ctx, const Maps& maps, int box, const PagedGroup& g, const 
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "paged dense attend shared-memory attribute");
         set = true;
     }
-    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w, box);
+    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w);
     return dodo_check_cuda(ctx, cudaGetLastError(), "paged dense attend launch");
 }
 
@@ -879,21 +821,9 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
             if (c < cost) { cost = c; grid = units * k; }
         }
     }
-    Maps maps;
-    memset(&maps, 0, sizeof maps);
-    int rc = DODO_OK, box = 1;
-    while (box < BN && a.page % (2 * box) == 0) box *= 2;
-    if (box < 8) box = 1;
-    const int width = a.Hkv * dh, rows = a.pages * a.page;
-    if (a.cK != nullptr) {
-        rc = dodo_encode_bf16_rows(ctx, &maps.cK, a.cK, width, rows, box);
-        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.cV, a.cV, width, rows, box);
-    }
-    if (rc == DODO_OK && a.lK != nullptr) {
-        rc = dodo_encode_bf16_rows(ctx, &maps.lK, a.lK, width, loc_rows, BN);
-        if (rc == DODO_OK) rc = dodo_encode_bf16_rows(ctx, &maps.lV, a.lV, width, loc_rows, BN);
-    }
+    PagedBoxes maps;
+    const int box = dodo_paged_box(a.page, BN), rc = dodo_paged_boxes(ctx, a, dh, loc_rows, box > 0 ? box : 1, BN, maps);
     if (rc != DODO_OK) return rc;
-    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, box, g, a, w, static_cast<int>(grid), st) : launch<128, 1>(ctx, maps, box, g, a, w, static_cast<int>(grid), st);
-    return tiles == 2 ? launch<64, 2>(ctx, maps, box, g, a, w, static_cast<int>(grid), st) : launch<64, 1>(ctx, maps, box, g, a, w, static_cast<int>(grid), st);
+    if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, g, a, w, static_cast<int>(grid), st) : launch<128, 1>(ctx, maps, g, a, w, static_cast<int>(grid), st);
+    return tiles == 2 ? launch<64, 2>(ctx, maps, g, a, w, static_cast<int>(grid), st) : launch<64, 1>(ctx, maps, g, a, w, static_cast<int>(grid), st);
 }

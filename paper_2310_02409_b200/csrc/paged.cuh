@@ -44,10 +44,16 @@ static inline size_t dodo_paged_part_rows(const PagedCut& cut) { return static_c
 // floats of a partial row: dh sums, a maximum and a sum, and two more so that every row of every tile starts on 16 bytes
 static constexpr int dodo_paged_part_floats(int dh) { return dh + 4; }
 
-PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int dtype, int max_rows);
+PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int max_rows);
 // many bf16 rows, on the tensor cores; scale of DODO_DENSE_LEAST_SCALE or more
 size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh);
 int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+// few bf16 rows, on the warp-level matrix units; pages that are multiples of eight rows
+struct PagedBoxes { int rows; CUtensorMap cK, cV, lK, lV; };     // tensor maps of 64 features x `rows` rows, of local tokens as many as a tile has
+int dodo_paged_box(int page, int most);       // rows that a tensor copy may take at once: the power of two that divides the page's, 0 below 8
+int dodo_paged_boxes(dodo_ctx* ctx, const PagedArrays& a, int dh, int loc_rows, int box, int local_box, PagedBoxes& m);
+PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows);
+int dodo_launch_paged_token(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
@@ -118,10 +124,69 @@ __device__ __forceinline__ size_t out_row(const PagedArrays& a, const PagedSeq& 
     return static_cast<size_t>(s.q_row0 + t) * a.H + head * a.group + (r - t * a.group);
 }
 
+// One row's bf16 result again over all of the unit's keys that it sees, whatever the others hold: a warp, a key a lane for the scores, four
+// (two) features a lane for the sums.  For results of matrix products that are not finite, where a weight of 0 may have met a NaN.
+template <int DH>
+__device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, __nv_bfloat16* out) {
+    constexpr int F = DH / 32;
+    const int lane = static_cast<int>(threadIdx.x) & 31;
+    const size_t pitch = static_cast<size_t>(a.Hkv) * DH, at = static_cast<size_t>(head) * DH;
+    const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, head, r) * DH;
+    const int qpos = s.q_pos0 + token_of(a, r), end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
+    float m = -INFINITY, l = 0.f, acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = 0.f;
+#pragma unroll 1
+    for (int j0 = 0; j0 < end; j0 += 32) {
+        const Key k = key_at(a, s, j0 + lane, end, page_entry(a, s, j0 + lane, end));
+        const bool sees = k.row >= 0 && k.pos <= qpos;
+        float x = -INFINITY;
+        if (sees) {
+            const __nv_bfloat16* const kr = static_cast<const __nv_bfloat16*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
+            x = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < DH; c += 8) {
+                float kf[8], qf[8];
+                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(kr + c)), kf);
+                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(q + c)), qf);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x = fmaf(kf[e], qf[e], x);
+            }
+            x *= a.scale_log2;
+        }
+        float top = fmaxf(m, x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == -INFINITY ? 0.f : top, corr = part_weight(m, ref), w = exp2_fast(x - ref);
+        m = top;
+        l = fmaf(l, corr, w);
+        const float rounded = __bfloat162float(__float2bfloat16_rn(w));
+#pragma unroll
+        for (int f = 0; f < F; ++f) acc[f] *= corr;
+        uint32_t seen = __ballot_sync(0xffffffffu, sees);
+        while (seen != 0u) {
+            const int e = __ffs(seen) - 1;
+            seen &= seen - 1u;
+            const int row = __shfl_sync(0xffffffffu, k.row, e);
+            const bool local = __shfl_sync(0xffffffffu, k.local ? 1 : 0, e) != 0;
+            const float c = __shfl_sync(0xffffffffu, rounded, e);
+            const __nv_bfloat16* const vr = static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
+#pragma unroll
+            for (int f = 0; f < F; ++f) acc[f] = fmaf(c, __bfloat162float(vr[f]), acc[f]);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int f = 0; f < F; ++f) out[lane * F + f] = __float2bfloat16_rn(acc[f] * inv);
+}
+
 // The end of a block of kThreads threads: `parts` partial results of `rows` rows in shared memory (sums of weighted V [part][row][DH]
 // with pitch floats a row, maxima and sums of weights [part][row]) joined into results, or, where the unit is cut, into a partial
-// result of the workspace; the last block of the unit joins those.  Called by all threads, behind a barrier.
-template <typename T, int DH, int kThreads>
+// result of the workspace; the last block of the unit joins those.  Called by all threads, behind a barrier.  kMixed: the sums may hold
+// what some rows do not see; results that are not finite are then summed again.
+template <typename T, int DH, int kThreads, bool kMixed = false>
 __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, const Place& p, int tile_rows, int rows, int parts, const float* acc,
                                        int pitch, const float* mx, const float* sum) {
     constexpr int kPieces = DH / 4;
@@ -133,6 +198,7 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
     const size_t chunk_floats = static_cast<size_t>(tile_rows) * dodo_paged_part_floats(DH);
     float* const base = a.part + static_cast<size_t>(s.part0) * dodo_paged_part_floats(DH) + unit * s.nchunk * chunk_floats;
     float* const mine = base + p.chunk * chunk_floats;
+    bool odd = false;
     for (int i = tid; i < rows * kPieces; i += kThreads) {
         const int r = i / kPieces, c = i % kPieces * 4;
         float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -148,7 +214,7 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
             const size_t at = out_row(a, s, p.head, r0 + r);
             const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            for (int e = 0; e < 4; ++e) { o[e] *= inv; odd = odd || !(o[e] * 0.f == 0.f); }
             store4(static_cast<T*>(a.O) + at * DH + c, o);
             if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
         } else {
@@ -156,19 +222,20 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
             if (c == 0) *reinterpret_cast<float2*>(mine + static_cast<size_t>(tile_rows) * DH + 2 * r) = make_float2(M, L);
         }
     }
-    if (whole) return;
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
-        int* const t = a.tickets + s.tick0 + unit;
-        const int arrived = atomicAdd(t, 1);
-        s_last = arrived == s.nchunk - 1;
-        if (s_last) *t = 0;        // clean for the next launch
+    if (!whole) {
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            int* const t = a.tickets + s.tick0 + unit;
+            const int arrived = atomicAdd(t, 1);
+            s_last = arrived == s.nchunk - 1;
+            if (s_last) *t = 0;        // clean for the next launch
+        }
+        __syncthreads();
+        if (!s_last) return;
+        __threadfence();
     }
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    for (int i = tid; i < rows * kPieces; i += kThreads) {
+    for (int i = tid; !whole && i < rows * kPieces; i += kThreads) {
         const int r = i / kPieces, c = i % kPieces * 4;
         const float* const ml = base + static_cast<size_t>(tile_rows) * DH + 2 * r;
         float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -185,9 +252,18 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
         const size_t at = out_row(a, s, p.head, r0 + r);
         const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= inv;
+        for (int e = 0; e < 4; ++e) { o[e] *= inv; odd = odd || !(o[e] * 0.f == 0.f); }
         store4(static_cast<T*>(a.O) + at * DH + c, o);
         if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+    }
+    if constexpr (kMixed) {
+        if (__syncthreads_or(odd ? 1 : 0) == 0) return;
+        for (int r = tid / 32; r < rows; r += kThreads / 32) {
+            __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, p.head, r0 + r) * DH;
+            bool bad = false;
+            for (int f = tid % 32; f < DH; f += 32) bad = bad || !isfinite(__bfloat162float(out[f]));
+            if (__any_sync(0xffffffffu, bad)) sum_again<DH>(a, s, p.head, r0 + r, out);
+        }
     }
 }
 
