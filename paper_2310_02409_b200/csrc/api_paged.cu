@@ -59,7 +59,7 @@ extern "C" {
 
 size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh) {
     if (ctx == nullptr || dh <= 0) return 0;
-    const size_t rows = dodo_paged_part_rows(dodo_paged_rows_cut(ctx, 32)) * dodo_paged_part_floats(dh) * sizeof(float);
+    const size_t rows = dodo_paged_part_rows({kPagedRowsMost, 0, dodo_paged_rows_blocks(ctx), 0, 0}) * dodo_paged_part_floats(dh) * sizeof(float);
     const size_t dense = dodo_paged_dense_workspace_bytes(ctx->num_sms, dh);
     return rows > dense ? rows : dense;
 }
@@ -125,10 +125,10 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
             continue;
         }
         const bool token = dtype == DODO_BF16 && dodo_paged_box(cache->page, 8) > 0;
-        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, max_rows);
+        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
         dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);
-        rc = token ? dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st) : dodo_launch_paged_rows(ctx, dtype, dh, max_rows, g, a, st);
+        rc = token ? dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st) : dodo_launch_paged_rows(ctx, dtype, dh, cut, g, a, st);
         if (rc != DODO_OK) return rc;
     }
     return DODO_OK;

@@ -190,34 +190,43 @@ attend_paged_rows_kernel(const __grid_constant__ PagedGroup g, const __grid_cons
     finish<T, DH, kThreads>(a, s, p, tile_rows, rows, key_warps, smem, kPitch, mx, sum);
 }
 
-struct Shape { int rows, row_warps; };      // rows of a warp, warps with rows of their own
-// Rows for the longest block of the batch: as many a warp as there are (a row's keys are then read once), up to eight
-Shape shape_for(int max_rows) {
-    if (max_rows == 1) return {1, 1};
-    if (max_rows <= 4) return {4, 1};
-    return {8, max_rows <= 8 ? 1 : max_rows <= 16 ? 2 : 4};
-}
 
 template <typename T, int DH>
-cudaError_t launch(const Shape& sh, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
-    const size_t smem = sizeof(float) * static_cast<size_t>(kWarps) * sh.rows * (DH + 4 + 2);
+cudaError_t launch(const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
+    const size_t smem = sizeof(float) * static_cast<size_t>(kWarps) * cut.warp_rows * (DH + 4 + 2);
     const dim3 grid(static_cast<unsigned>(g.cta0[g.nseq])), block(kThreads);
-    if (sh.rows == 1) return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 1>, grid, block, smem, st, g, a, sh.row_warps);
-    if (sh.rows == 4) return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 4>, grid, block, smem, st, g, a, sh.row_warps);
-    return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 8>, grid, block, smem, st, g, a, sh.row_warps);
+    const int row_warps = cut.rows / cut.warp_rows;
+    if (cut.warp_rows == 1) return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 1>, grid, block, smem, st, g, a, row_warps);
+    if (cut.warp_rows == 4) return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 4>, grid, block, smem, st, g, a, row_warps);
+    return dodo_launch_dependent(attend_paged_rows_kernel<T, DH, 8>, grid, block, smem, st, g, a, row_warps);
 }
 
 }  // namespace
 
-PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int max_rows) {
-    const Shape sh = shape_for(max_rows);
-    return {sh.rows * sh.row_warps, 32, 4 * ctx->num_sms, 128};
+// As many rows a warp and a block as there are (their keys are then read once), up to eight and 32, while that leaves blocks enough for the
+// device; a small batch takes fewer, down to a row a warp, and its keys are split over more warps and blocks instead (16 queries over 52 + 16
+// keys of 4 heads: 11.2 us with 16 rows a block, TINY with one).
+PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, const PagedGroup& g, int group, int Hkv, int max_rows) {
+    static const int shapes[][2] = {{8, 32}, {8, 16}, {8, 8}, {4, 4}, {1, 1}};
+    PagedCut cut = {1, 32, dodo_paged_rows_blocks(ctx), 128, 1};
+    for (const auto& s : shapes) {
+        if (s[1] > 1 && 2 * max_rows <= s[1]) continue;
+        cut.warp_rows = s[0];
+        cut.rows = s[1];
+        int64_t blocks = 0;
+        for (int i = 0; i < g.nseq; ++i) {
+            const PagedSeq& q = g.seq[i];
+            const int64_t units = (static_cast<int64_t>(q.tq) * group + cut.rows - 1) / cut.rows * Hkv, chunks = (static_cast<int64_t>(q.c_len) + q.l_len) / cut.least;
+            blocks += units * (chunks > 1 ? chunks : 1);
+        }
+        if (blocks >= ctx->num_sms) break;
+    }
+    return cut;
 }
 
-int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
-    const Shape sh = shape_for(max_rows);
+int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
     cudaError_t e;
-    if (dtype == DODO_F32) e = dh == 64 ? launch<float, 64>(sh, g, a, st) : launch<float, 128>(sh, g, a, st);
-    else e = dh == 64 ? launch<__nv_bfloat16, 64>(sh, g, a, st) : launch<__nv_bfloat16, 128>(sh, g, a, st);
+    if (dtype == DODO_F32) e = dh == 64 ? launch<float, 64>(cut, g, a, st) : launch<float, 128>(cut, g, a, st);
+    else e = dh == 64 ? launch<__nv_bfloat16, 64>(cut, g, a, st) : launch<__nv_bfloat16, 128>(cut, g, a, st);
     return dodo_check_cuda(ctx, e, "paged attend launch");
 }

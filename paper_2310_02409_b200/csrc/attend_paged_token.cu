@@ -328,7 +328,7 @@ int dodo_paged_boxes(dodo_ctx* ctx, const PagedArrays& a, int dh, int loc_rows, 
     return rc;
 }
 
-PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows) { return {max_rows <= 8 ? 8 : 16, BN, 2 * ctx->num_sms, 4 * BN}; }
+PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows) { return {max_rows <= 8 ? 8 : 16, BN, 2 * ctx->num_sms, 4 * BN, 0}; }
 
 int dodo_launch_paged_token(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st) {
     PagedBoxes m;

@@ -23,8 +23,8 @@ __device__ __forceinline__ int pool_row(const int32_t* table, int page0, int pag
     return static_cast<unsigned>(p) < static_cast<unsigned>(pages) ? p * page + r % page : -1;
 }
 
-constexpr int kThreads = 256;
-constexpr int kAhead = 2;       // pieces of K and of V that a thread requests before anything else
+constexpr int kThreads = 128;
+constexpr int kAhead = 2;       // slots of K (a piece or two each) and twice as many pieces of V that a thread requests before anything else
 
 template <typename T, int VEC, bool INTER>
 __global__ void __launch_bounds__(512)
@@ -55,21 +55,25 @@ gather_paged_kernel(const T* __restrict__ K, const T* __restrict__ V, long long 
     const int pos = g.pos_base[b] + token;
 
     Slot<T, VEC, INTER> k[kAhead];
-    uint4 v[kAhead];
+    uint4 v[2 * kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-        const int h = lane + u * lanes, c = tid + u * threads;
+        const int h = lane + u * lanes;
         if (lane < lanes && h < H) k[u].load(sk + h * dh, slot, p.half);
+    }
+#pragma unroll
+    for (int u = 0; u < 2 * kAhead; ++u) {
+        const int c = tid + u * threads;
         if (c < vecs) v[u] = ld_stream16(sv + c);
     }
     for (int i = tid; i < p.half; i += threads) cs[i] = cos_sin(p, i, pos);
     if (tid == 0) cache_pos[row] = pos;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+    for (int u = 0; u < 2 * kAhead; ++u) {
         const int c = tid + u * threads;
         if (c < vecs) dv[c] = v[u];
     }
-    for (int c = tid + kAhead * threads; c < vecs; c += threads) dv[c] = ld_stream16(sv + c);
+    for (int c = tid + 2 * kAhead * threads; c < vecs; c += threads) dv[c] = ld_stream16(sv + c);
     __syncthreads();
     if (lane >= lanes) return;
 #pragma unroll

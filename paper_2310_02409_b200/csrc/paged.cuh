@@ -37,14 +37,16 @@ struct PagedArrays {
     int* tickets;
     int* status;
 };
-// How a launch cuts its work: rows of a tile, keys a chunk is a multiple of, blocks to aim at, keys a chunk has at least
-struct PagedCut { int rows, keys, target, least; };
+// How a launch cuts its work: rows of a tile, keys a chunk is a multiple of, blocks to aim at, keys a chunk has at least, rows of a warp
+struct PagedCut { int rows, keys, target, least, warp_rows; };
 void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, bool may_cut);
 static inline size_t dodo_paged_part_rows(const PagedCut& cut) { return static_cast<size_t>(2) * cut.target * cut.rows; }
 // floats of a partial row: dh sums, a maximum and a sum, and two more so that every row of every tile starts on 16 bytes
 static constexpr int dodo_paged_part_floats(int dh) { return dh + 4; }
 
-PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, int max_rows);
+constexpr int kPagedRowsMost = 32;          // rows of a tile of the kernel on the FMA units, at most
+static inline int dodo_paged_rows_blocks(const dodo_ctx* ctx) { return 4 * ctx->num_sms; }      // blocks that it aims at
+PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, const PagedGroup& g, int group, int Hkv, int max_rows);
 // many bf16 rows, on the tensor cores; scale of DODO_DENSE_LEAST_SCALE or more
 size_t dodo_paged_dense_workspace_bytes(int num_sms, int dh);
 int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
@@ -54,7 +56,7 @@ int dodo_paged_box(int page, int most);       // rows that a tensor copy may tak
 int dodo_paged_boxes(dodo_ctx* ctx, const PagedArrays& a, int dh, int loc_rows, int box, int local_box, PagedBoxes& m);
 PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows);
 int dodo_launch_paged_token(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
-int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
 namespace dodo_paged {

@@ -43,6 +43,7 @@ rope_kernel(const __grid_constant__ RopeArrays a, const __grid_constant__ Rotati
     const int step = lanes * static_cast<int>(gridDim.y), head0 = lane < lanes ? lane + lanes * static_cast<int>(blockIdx.y) : a.heads;
     const int per_row = head0 < a.heads ? (a.heads - head0 + step - 1) / step : 0;      // this thread's pieces of a row
     const int items = per_row * (row_end - row_first);
+    constexpr int kBatch = INTER ? 4 : 2;        // pieces (of one or two loads) on their way at a time
 
     auto array_of = [&](int head) {
         int k = 0;
@@ -51,28 +52,35 @@ rope_kernel(const __grid_constant__ RopeArrays a, const __grid_constant__ Rotati
         return k;
     };
     int load_row = row_first, load_head = head0, row = row_first, head = head0;
-    Slot<T, VEC, INTER> next;
-    auto fetch = [&]() {
-        const int k = array_of(load_head);
-        next.load(static_cast<const T*>(a.in[k]) + load_row * a.in_row[k] + (load_head - a.first[k]) * a.in_head[k], slot, p.half);
-        load_head += step;
-        if (load_head >= a.heads) { load_head = head0; ++load_row; }
+    Slot<T, VEC, INTER> piece[kBatch];
+    auto fetch = [&](int first) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (first + u >= items) return;
+            const int k = array_of(load_head);
+            piece[u].load(static_cast<const T*>(a.in[k]) + load_row * a.in_row[k] + (load_head - a.first[k]) * a.in_head[k], slot, p.half);
+            load_head += step;
+            if (load_head >= a.heads) { load_head = head0; ++load_row; }
+        }
     };
     dodo_grid_dependency_sync();
-    if (items > 0) fetch();
+    fetch(0);
     for (int i = tid; i < (row_end - row_first) * p.half; i += static_cast<int>(blockDim.x)) {
         const int r = row_first + i / p.half, b = sequence_of(g.row0, g.nseq, r);
         cs[i] = cos_sin(p, i % p.half, g.pos0[b] + (r - g.row0[b]));
     }
     __syncthreads();
-    for (int it = 0; it < items; ++it) {
-        const Slot<T, VEC, INTER> now = next;
-        if (it + 1 < items) fetch();
-        const int k = array_of(head);
-        now.store(static_cast<T*>(a.out[k]) + row * a.out_row[k] + (head - a.first[k]) * a.out_head[k], slot, p.half,
-                  cs + static_cast<size_t>(row - row_first) * p.half);
-        head += step;
-        if (head >= a.heads) { head = head0; ++row; }
+    for (int it = 0; it < items; it += kBatch) {
+        if (it > 0) fetch(it);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (it + u >= items) return;
+            const int k = array_of(head);
+            piece[u].store(static_cast<T*>(a.out[k]) + row * a.out_row[k] + (head - a.first[k]) * a.out_head[k], slot, p.half,
+                           cs + static_cast<size_t>(row - row_first) * p.half);
+            head += step;
+            if (head >= a.heads) { head = head0; ++row; }
+        }
     }
 }
 
