@@ -22,6 +22,7 @@ using namespace dodo_paged;
 constexpr int BN = 64;                        // keys of a stage
 constexpr int kConsumers = 4, kThreads = 32 * (kConsumers + 1);
 constexpr float kRescaleStep = 24.f;
+constexpr int kAhead = 4;                     // stages whose keys are looked up at once
 enum { kMasked = 1, kEnd = 2, kLocal = 4, kHoles = 8 };      // of a stage; kHoles: some of its keys are not there or seen by nobody
 
 template <int DH>
@@ -79,66 +80,68 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
     const int c_stages = (s.c_len + BN - 1) / BN, t_end = min((p.chunk + 1) * (s.chunk_keys / BN), c_stages + (l_vis + BN - 1) / BN);
     const int t_begin = p.chunk * (s.chunk_keys / BN);
     bool stuck = false;
+    // ahead of the dependency wait, hints to L2 only: the first page entries, the rows of Q
+    if (warp == kConsumers) {
+        const int first = t_begin * BN + 16 * lane;
+        if (first < s.c_len) asm volatile("prefetch.global.L2 [%0];" ::"l"(a.table + s.page0 + page_of(a, first)));
+    } else if (tid < rows) {
+        const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, p.head, r0 + tid) * DH;
+#pragma unroll
+        for (int c = 0; c < DH; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + c));
+    }
     __syncthreads();
     dodo_grid_dependency_sync();
 
     if (warp == kConsumers) {
         // ================================================ producer ================================================
         const int col = p.head * DH;
-        int entry[2], row[2], pos[2];
+        // Look-ups go ahead by fours: the page entries of four stages at once, then their positions, while the four before are brought.
+        // (One stage at a time, a short list would take a round trip to memory for each.)
+        int entry[kAhead][2], row[kAhead][2], pos[kAhead][2];
         auto entries = [&](int t) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) entry[e] = t < t_end && t < c_stages ? page_entry(a, s, t * BN + 2 * lane + e, s.c_len) : 0;
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) entry[u][e] = t + u < t_end && t + u < c_stages ? page_entry(a, s, (t + u) * BN + 2 * lane + e, s.c_len) : 0;
         };
         auto keys = [&](int t) {
-            const int v = t * BN + 2 * lane, j = v - c_stages * BN;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                row[e] = -1; pos[e] = kNoPos;
-                if (t >= t_end) continue;
-                if (t >= c_stages) {
-                    if (j + e < l_vis) { row[e] = s.l_row0 + j + e; pos[e] = s.l_pos0 + j + e; }
-                } else {
-                    const Key k = key_at(a, s, v + e, s.c_len, entry[e]);
-                    row[e] = k.row; pos[e] = k.pos;
+            for (int u = 0; u < kAhead; ++u) {
+                const int v = (t + u) * BN + 2 * lane, j = v - c_stages * BN;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    row[u][e] = -1; pos[u][e] = kNoPos;
+                    if (t + u >= t_end) continue;
+                    if (t + u >= c_stages) {
+                        if (j + e < l_vis) { row[u][e] = s.l_row0 + j + e; pos[u][e] = s.l_pos0 + j + e; }
+                    } else {
+                        const Key k = key_at(a, s, v + e, s.c_len, entry[u][e]);
+                        row[u][e] = k.row; pos[u][e] = k.pos;
+                    }
                 }
             }
         };
         entries(t_begin);
         keys(t_begin);
-        entries(t_begin + 1);
+        entries(t_begin + kAhead);
         int n = 0;                     // stages filled so far
-        for (int t = t_begin; t <= max(t_begin, t_end); ++t) {       // the last is the chunk's end
-            const bool end = t >= t_end;
-            int q[2], hi = static_cast<int>(0x80000000), my_row = row[0];
-            bool any = false;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const bool there = row[e] >= 0 && pos[e] <= last_pos;
-                q[e] = there ? pos[e] : kNoPos;
-                hi = max(hi, q[e]);
-                any = any || there;
-            }
-            if (!end) {
-                keys(t + 1);
-                entries(t + 2);
-                if (!__any_sync(0xffffffffu, any)) continue;          // nobody sees a key of this stage
-            }
+        auto fill = [&](int t, int r0, int p0, int p1, bool end) {      // false: a wait ran out
+            const int hi = max(p0, p1);
             const bool masked = __any_sync(0xffffffffu, hi > first_pos), holes = __any_sync(0xffffffffu, hi == kNoPos);
             const int st = n % L::kStages;
-            if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], static_cast<uint32_t>(n / L::kStages + 1) & 1u))) { stuck = true; break; }
-            *reinterpret_cast<int2*>(&s_pos[st][2 * lane]) = make_int2(q[0], q[1]);
+            if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], static_cast<uint32_t>(n / L::kStages + 1) & 1u))) return false;
+            *reinterpret_cast<int2*>(&s_pos[st][2 * lane]) = make_int2(p0, p1);
             const bool local = t >= c_stages;
             if (lane == 0) s_kind[st] = end ? kEnd : (masked ? kMasked : 0) | (holes ? kHoles : 0);
             __syncwarp();
             ++n;
             if (end) {
                 if (lane == 0) mbar_arrive(&full[st]);
-                break;
+                return true;
             }
             // a box starts with an even key: the lane that holds it copies it, if its first row is there
             const int box = local ? BN : boxes.rows;
-            const bool mine = 2 * lane % box == 0 && my_row >= 0;
+            const bool mine = 2 * lane % box == 0 && r0 >= 0;
             const uint32_t have = __popc(__ballot_sync(0xffffffffu, mine));
             if (lane == 0) mbar_expect_tx(&full[st], have * box * DH * 4);
             __syncwarp();
@@ -147,11 +150,29 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
                 const CUtensorMap* const mv = local ? &boxes.lV : &boxes.cV;
                 const uint32_t dst = base + st * L::kStage + 2 * lane * 128;
 #pragma unroll
-                for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + h * L::kHalf, mk, col + 64 * h, my_row, &full[st]);
+                for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + h * L::kHalf, mk, col + 64 * h, r0, &full[st]);
 #pragma unroll
-                for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + L::kTile + h * L::kHalf, mv, col + 64 * h, my_row, &full[st]);
+                for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + L::kTile + h * L::kHalf, mv, col + 64 * h, r0, &full[st]);
+            }
+            return true;
+        };
+        for (int t = t_begin; t < t_end && !stuck; t += kAhead) {
+            int r0[kAhead], q[kAhead][2];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                r0[u] = row[u][0];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) q[u][e] = row[u][e] >= 0 && pos[u][e] <= last_pos ? pos[u][e] : kNoPos;
+            }
+            keys(t + kAhead);
+            entries(t + 2 * kAhead);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (stuck || t + u >= t_end || !__any_sync(0xffffffffu, min(q[u][0], q[u][1]) != kNoPos)) continue;      // nobody sees a key of this stage
+                stuck = !fill(t + u, r0[u], q[u][0], q[u][1], false);
             }
         }
+        if (!stuck) stuck = !fill(0, -1, kNoPos, kNoPos, true);
         if (stuck)          // copies in flight land before the block's shared memory goes
             for (int i = max(0, n - L::kStages); i < n; ++i) mbar_wait(&full[i % L::kStages], static_cast<uint32_t>(i / L::kStages) & 1u);
     } else {
