@@ -397,8 +397,9 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
             }
             __syncwarp();
         };
-        // the product of a tile's weights and values, in halves of 64 keys as the softmax publishes them
-        auto values = [&](int st, int c, bool add, bool last_user) {
+        // the product of a tile's weights and values, in halves of 64 keys as the softmax publishes them; `between` runs while the first is
+        // being worked on
+        auto values = [&](int st, int c, bool add, bool last_user, auto between) {
             const uint64_t db = desc_mnmajor(base + L::kOffV + (c % L::kVStages) * L::kTile, L::kHalf);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -411,6 +412,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                     if (h == 1 && last_user) mma_commit(&bar_vfree[c % L::kVStages]);
                 }
                 __syncwarp();
+                if (h == 0) between();
             }
             ++np[st];
         };
@@ -426,15 +428,19 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
                 ++ck;
                 more = next_tile();
+                wait_v(cv);
                 bool add = false, ended = false;
                 while (!ended && !stuck) {
                     const bool now = more;             // a tile follows this one
-                    wait_v(cv);                        // (both are there by the time the first weights are)
-                    if (now) wait_k(ck);
                     for (int st = 0; st < streams; ++st) {
-                        values(st, cv, add, st == streams - 1);
+                        values(st, cv, add, st == streams - 1, [&] {
+                            if (now && st == 0) wait_k(ck);
+                            if (now && st == streams - 1) {
+                                more = next_tile();
+                                wait_v(cv + 1);
+                            }
+                        });
                         if (now) scores(st, st, ck, st == streams - 1);
-                        if (now && st == 0) more = next_tile();      // looked up while the matrix unit has work
                     }
                     ++cv;
                     ck += now ? 1 : 0;
@@ -458,7 +464,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 if (ahead == 0) continue;
                 while (!stuck && i < ahead) {
                     wait_v(cv);
-                    values(i & 1, cv, i >= 2, true);
+                    values(i & 1, cv, i >= 2, true, [] {});
                     ++cv;
                     ++i;
                     next_scores();
