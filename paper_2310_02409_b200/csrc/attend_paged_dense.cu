@@ -168,6 +168,26 @@ __device__ __forceinline__ void hint_row(const PagedArrays& a, const PagedSeq& s
     for (int c = 0; c < DH; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + c));
 }
 
+// hints for the positions, K and V rows of the segment's first tile: a warp, four keys a lane
+template <int DH>
+__device__ __forceinline__ void hint_keys(const PagedArrays& a, const PagedSeq& s, const Segment& q, int lane) {
+    const size_t pitch = static_cast<size_t>(a.Hkv) * DH;
+    const int v = q.t0 * BN + 4 * lane;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int entry = page_entry(a, s, v + e, s.c_len);
+        if (q.t0 >= q.c_tiles || v + e >= s.c_len || static_cast<unsigned>(entry) >= static_cast<unsigned>(a.pages)) continue;
+        const int row = entry * a.page + (v + e - page_of(a, v + e) * a.page);
+        const size_t at = static_cast<size_t>(row) * pitch + static_cast<size_t>(q.head) * DH;
+        if (e == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(a.pos + row));
+#pragma unroll
+        for (int c = 0; c < DH; c += 64) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const __nv_bfloat16*>(a.cK) + at + c));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const __nv_bfloat16*>(a.cV) + at + c));
+        }
+    }
+}
+
 template <int DH, int TILES>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_constant__ PagedGroup g, const __grid_constant__ PagedArrays a,
@@ -189,10 +209,19 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
     int x = block_start(T, G, bid);
     Segment q;
 
-    // The first rows of Q are asked for ahead of everything else: behind the first keys of all blocks they would come late.
-    if (warp < kSoftmaxWarps) {
+    // Hints to L2 while the block sets itself up: the rows of Q that it begins with (behind the first keys of all blocks they would come
+    // late), and, as their look-up is a chain of reads from memory, positions and rows of the first keys.
+    if (warp <= kSoftmaxWarps) {
         int ahead = x;
-        if (next_segment(g, a, work, L::kRows, ahead, slot_end, q)) hint_row<DH>(a, g.seq[q.b], q, tid);
+        if (next_segment(g, a, work, L::kRows, ahead, slot_end, q)) {
+            const PagedSeq& s = g.seq[q.b];
+            if (warp < kSoftmaxWarps) {
+                hint_row<DH>(a, s, q, tid);
+            } else {
+                dodo_grid_dependency_sync();
+                hint_keys<DH>(a, s, q, lane);
+            }
+        }
     }
     if (tid == 0) {
         mbar_init(&bar_q, kSoftmaxWarps);
@@ -208,6 +237,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (warp != kSoftmaxWarps || x >= slot_end) dodo_grid_dependency_sync();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -355,8 +385,15 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                     if (!warp_wait(&bar_vfull[stage], static_cast<uint32_t>(n / L::kVStages) & 1u)) { stuck = true; break; }
                     if ((kind & kHoles) != 0) {
                         unsigned char* const v = base_ptr + L::kOffV + stage * L::kTile + (lane % kPieces / 8) * L::kHalf + lane % 8 * 16;
-                        for (int r = lane / kPieces; r < BN; r += 32 / kPieces)
-                            if (s_pos[ps * BN + r] == kNoPos) *reinterpret_cast<uint4*>(v + r * 128) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                        for (int r0 = 0; r0 < BN; r0 += 32) {
+                            // bit r: row r0 + r; as many rows at a time as lanes hold pieces for
+                            uint32_t holes = __ballot_sync(0xffffffffu, s_pos[ps * BN + r0 + lane] == kNoPos);
+                            holes >>= lane / kPieces;
+#pragma unroll
+                            for (int r = 0; r < 32; r += 32 / kPieces)
+                                if ((holes >> r & 1u) != 0u) *reinterpret_cast<uint4*>(v + (r0 + r + lane / kPieces) * 128) = make_uint4(0u, 0u, 0u, 0u);
+                        }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     __syncwarp();
@@ -428,16 +465,16 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
                 ++ck;
                 more = next_tile();
-                wait_v(cv);
-                bool add = false, ended = false;
+                bool add = false, ended = false, v_there = false;
                 while (!ended && !stuck) {
                     const bool now = more;             // a tile follows this one
+                    if (!v_there) wait_v(cv);
                     for (int st = 0; st < streams; ++st) {
                         values(st, cv, add, st == streams - 1, [&] {
                             if (now && st == 0) wait_k(ck);
                             if (now && st == streams - 1) {
                                 more = next_tile();
-                                wait_v(cv + 1);
+                                v_there = __all_sync(0xffffffffu, mbar_try_wait(&bar_vclean[(cv + 1) % L::kVStages], static_cast<uint32_t>((cv + 1) / L::kVStages) & 1u));
                             }
                         });
                         if (now) scores(st, st, ck, st == streams - 1);
@@ -784,8 +821,8 @@ int launch(dodo_ctx* ctx, const PagedBoxes& maps, const PagedGroup& g, const Pag
         if (e != cudaSuccess) return dodo_check_cuda(ctx, e, "paged dense attend shared-memory attribute");
         set = true;
     }
-    kern<<<grid, kThreads, smem, st>>>(maps, g, a, w);
-    return dodo_check_cuda(ctx, cudaGetLastError(), "paged dense attend launch");
+    return dodo_check_cuda(ctx, dodo_launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(kThreads), static_cast<size_t>(smem), st, maps, g, a, w),
+                           "paged dense attend launch");
 }
 
 }  // namespace
