@@ -43,7 +43,7 @@ rope_kernel(const __grid_constant__ RopeArrays a, const __grid_constant__ Rotati
     const int step = lanes * static_cast<int>(gridDim.y), head0 = lane < lanes ? lane + lanes * static_cast<int>(blockIdx.y) : a.heads;
     const int per_row = head0 < a.heads ? (a.heads - head0 + step - 1) / step : 0;      // this thread's pieces of a row
     const int items = per_row * (row_end - row_first);
-    constexpr int kBatch = INTER ? 4 : 2;        // pieces (of one or two loads) on their way at a time
+    constexpr int kBatch = INTER ? 8 : 2;        // pieces (of one or two loads) on their way at a time
 
     auto array_of = [&](int head) {
         int k = 0;
@@ -87,10 +87,12 @@ rope_kernel(const __grid_constant__ RopeArrays a, const __grid_constant__ Rotati
 template <typename T, int VEC, bool INTER>
 cudaError_t launch(const dodo_ctx* ctx, const RopeArrays& a, const Rotation& p, const RopeRows& g, int dh, cudaStream_t st) {
     const int slots = slots_of<VEC, INTER>(dh, p.half), rows = g.row0[g.nseq] - g.row0[0];
-    const int lanes = slots >= 256 ? 1 : min(256 / slots, a.heads);
-    // Four tokens a block once there are blocks enough for the device that way, else one, its heads spread over blocks as well
-    const int tokens = rows >= 4 * 8 * ctx->num_sms ? 4 : 1;
-    const int split = tokens > 1 ? 1 : (a.heads + lanes - 1) / lanes;
+    const int lanes = slots >= 128 ? 1 : min(128 / slots, a.heads);
+    // Two tokens a block of 128 threads once there are blocks enough for the device that way, so that sines and cosines are made while the
+    // first rows are on their way (16,384 tokens of 40 + 40 heads: 110 us; one token 140, four 113); else one, and where tokens are few
+    // their heads are spread over blocks as well
+    const int tokens = rows >= 2 * 8 * ctx->num_sms ? 2 : 1;
+    const int split = rows >= 4 * ctx->num_sms ? 1 : (a.heads + lanes - 1) / lanes;
     const int threads = (slots * lanes + 31) / 32 * 32;
     return dodo_launch_dependent(rope_kernel<T, VEC, INTER>, dim3(static_cast<unsigned>((rows + tokens - 1) / tokens), static_cast<unsigned>(split)),
                                  dim3(static_cast<unsigned>(threads)), sizeof(float2) * tokens * p.half, st, a, p, g, dh, slots, lanes, tokens);
