@@ -308,7 +308,7 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
     }
     if (stuck && lane == 0) atomicOr(a.status, DODO_DEV_WAIT_TIMEOUT);
     __syncthreads();
-    finish<__nv_bfloat16, DH, kThreads, true>(a, s, p, kRows, rows, kConsumers, reinterpret_cast<const float*>(base_ptr), DH + 4, s_max, s_sum);
+    finish<__nv_bfloat16, DH, kThreads, true>(a, s, p, kRows, rows, kConsumers, reinterpret_cast<float*>(base_ptr), DH + 4, s_max, s_sum);
 }
 
 template <int DH, int NQ>

@@ -189,42 +189,42 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
 // result of the workspace; the last block of the unit joins those.  Called by all threads, behind a barrier.  kMixed: the sums may hold
 // what some rows do not see; results that are not finite are then summed again.
 template <typename T, int DH, int kThreads, bool kMixed = false>
-__device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, const Place& p, int tile_rows, int rows, int parts, const float* acc,
-                                       int pitch, const float* mx, const float* sum) {
+__device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, const Place& p, int tile_rows, int rows, int parts, float* acc,
+                                       int pitch, float* mx, float* sum) {
     constexpr int kPieces = DH / 4;
     __shared__ int s_last;
     const int tid = static_cast<int>(threadIdx.x), r0 = p.tile * tile_rows;
-    const bool whole = s.nchunk == 1;
     const size_t unit = static_cast<size_t>(p.tile) * a.Hkv + p.head;
     // partial rows of a chunk: tile_rows rows of DH floats, then a pair of floats each
     const size_t chunk_floats = static_cast<size_t>(tile_rows) * dodo_paged_part_floats(DH);
     float* const base = a.part + static_cast<size_t>(s.part0) * dodo_paged_part_floats(DH) + unit * s.nchunk * chunk_floats;
     float* const mine = base + p.chunk * chunk_floats;
-    bool odd = false;
-    for (int i = tid; i < rows * kPieces; i += kThreads) {
-        const int r = i / kPieces, c = i % kPieces * 4;
-        float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < parts; ++w) M = fmaxf(M, mx[w * tile_rows + r]);
-        for (int w = 0; w < parts; ++w) {
-            const float k = part_weight(mx[w * tile_rows + r], M);
-            if (k == 0.f) continue;
-            L = fmaf(k, sum[w * tile_rows + r], L);
-            const float4 v = *reinterpret_cast<const float4*>(acc + (static_cast<size_t>(w) * tile_rows + r) * pitch + c);
-            o[0] = fmaf(k, v.x, o[0]); o[1] = fmaf(k, v.y, o[1]); o[2] = fmaf(k, v.z, o[2]); o[3] = fmaf(k, v.w, o[3]);
-        }
-        if (whole) {
-            const size_t at = out_row(a, s, p.head, r0 + r);
-            const float inv = L != 0.f ? 1.f / L : 0.f;
+    bool whole = s.nchunk == 1, odd = false;
+    for (;;) {
+        for (int i = tid; i < rows * kPieces; i += kThreads) {
+            const int r = i / kPieces, c = i % kPieces * 4;
+            float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < parts; ++w) M = fmaxf(M, mx[w * tile_rows + r]);
+            for (int w = 0; w < parts; ++w) {
+                const float k = part_weight(mx[w * tile_rows + r], M);
+                if (k == 0.f) continue;
+                L = fmaf(k, sum[w * tile_rows + r], L);
+                const float4 v = *reinterpret_cast<const float4*>(acc + (static_cast<size_t>(w) * tile_rows + r) * pitch + c);
+                o[0] = fmaf(k, v.x, o[0]); o[1] = fmaf(k, v.y, o[1]); o[2] = fmaf(k, v.z, o[2]); o[3] = fmaf(k, v.w, o[3]);
+            }
+            if (whole) {
+                const size_t at = out_row(a, s, p.head, r0 + r);
+                const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { o[e] *= inv; odd = odd || !(o[e] * 0.f == 0.f); }
-            store4(static_cast<T*>(a.O) + at * DH + c, o);
-            if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
-        } else {
-            *reinterpret_cast<float4*>(mine + static_cast<size_t>(r) * DH + c) = make_float4(o[0], o[1], o[2], o[3]);
-            if (c == 0) *reinterpret_cast<float2*>(mine + static_cast<size_t>(tile_rows) * DH + 2 * r) = make_float2(M, L);
+                for (int e = 0; e < 4; ++e) { o[e] *= inv; odd = odd || !(o[e] * 0.f == 0.f); }
+                store4(static_cast<T*>(a.O) + at * DH + c, o);
+                if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+            } else {
+                *reinterpret_cast<float4*>(mine + static_cast<size_t>(r) * DH + c) = make_float4(o[0], o[1], o[2], o[3]);
+                if (c == 0) *reinterpret_cast<float2*>(mine + static_cast<size_t>(tile_rows) * DH + 2 * r) = make_float2(M, L);
+            }
         }
-    }
-    if (!whole) {
+        if (whole) break;
         __threadfence();
         __syncthreads();
         if (tid == 0) {
@@ -236,27 +236,59 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
         __syncthreads();
         if (!s_last) return;
         __threadfence();
-    }
-    for (int i = tid; !whole && i < rows * kPieces; i += kThreads) {
-        const int r = i / kPieces, c = i % kPieces * 4;
-        const float* const ml = base + static_cast<size_t>(tile_rows) * DH + 2 * r;
-        float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int k = 0; k < s.nchunk; ++k) M = fmaxf(M, __ldcg(ml + k * chunk_floats));
-#pragma unroll 8
-        for (int k = 0; k < s.nchunk; ++k) {
-            const float2 q = __ldcg(reinterpret_cast<const float2*>(ml + k * chunk_floats));
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(base + k * chunk_floats + static_cast<size_t>(r) * DH + c));
-            const float w = part_weight(q.x, M);
-            L = fmaf(w, q.y, L);
-            o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[2] = fmaf(w, v.z, o[2]); o[3] = fmaf(w, v.w, o[3]);
-        }
-        const size_t at = out_row(a, s, p.head, r0 + r);
-        const float inv = L != 0.f ? 1.f / L : 0.f;
+        // The chunks' partial rows, back to where the parts were: of as many parts as leave each about eight chunks, part w takes every
+        // parts-th, in order.  Warps share parts and rows out (kLanes lanes a row, four features each); two rows of four chunks each are
+        // on their way at a time.
+        constexpr int kLanes = kPieces, kRowsAtOnce = 32 / kLanes, kWarps = kThreads / 32;
+        parts = min(parts, (s.nchunk + 7) / 8);
+        const int warp = tid >> 5, lane = tid & 31, teams = kWarps / parts;       // warps of a part
+        if (warp < teams * parts) {
+            const int w = warp % parts, c = lane % kLanes * 4, step = teams * kRowsAtOnce;
+            for (int first = warp / parts * kRowsAtOnce + lane / kLanes; first < rows; first += 2 * step) {
+                float M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f}, o[2][4] = {};
+                for (int k = w; k < s.nchunk; k += 4 * parts) {
+                    float2 q[2][4];
+                    float4 v[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { o[e] *= inv; odd = odd || !(o[e] * 0.f == 0.f); }
-        store4(static_cast<T*>(a.O) + at * DH + c, o);
-        if (c == 0 && a.lse != nullptr) a.lse[at] = L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int r = min(first + h * step, rows - 1);
+                            const float* const from = base + static_cast<size_t>(min(k + u * parts, s.nchunk - 1)) * chunk_floats;
+                            q[h][u] = __ldcg(reinterpret_cast<const float2*>(from + static_cast<size_t>(tile_rows) * DH + 2 * r));
+                            v[h][u] = __ldcg(reinterpret_cast<const float4*>(from + static_cast<size_t>(r) * DH + c));
+                        }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float top = M[h];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) top = k + u * parts < s.nchunk ? fmaxf(top, q[h][u].x) : top;
+                        const float old = part_weight(M[h], top);
+                        M[h] = top;
+                        L[h] = old != 0.f ? L[h] * old : 0.f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[h][e] = old != 0.f ? o[h][e] * old : 0.f;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const float x = k + u * parts < s.nchunk ? part_weight(q[h][u].x, top) : 0.f;
+                            if (x == 0.f) continue;
+                            L[h] = fmaf(x, q[h][u].y, L[h]);
+                            o[h][0] = fmaf(x, v[h][u].x, o[h][0]); o[h][1] = fmaf(x, v[h][u].y, o[h][1]);
+                            o[h][2] = fmaf(x, v[h][u].z, o[h][2]); o[h][3] = fmaf(x, v[h][u].w, o[h][3]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (first + h * step >= rows) continue;
+                    const int at = w * tile_rows + first + h * step;
+                    *reinterpret_cast<float4*>(acc + static_cast<size_t>(at) * pitch + c) = make_float4(o[h][0], o[h][1], o[h][2], o[h][3]);
+                    if (c == 0) { mx[at] = M[h]; sum[at] = L[h]; }
+                }
+            }
+        }
+        __syncthreads();
+        whole = true;
     }
     if constexpr (kMixed) {
         if (__syncthreads_or(odd ? 1 : 0) == 0) return;
