@@ -46,7 +46,22 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, boo
 }
 
 namespace {
-constexpr int kFewRows = 16;
+// Whether a batch is worth the tensor cores' kernel, whose blocks take longer to begin and to end, or the one for few rows takes it in
+// tiles of 16.  By what both take for stages of keys per SM: about 6 us and 1.6 us for each 64 keys of 16 rows that two blocks of an SM have,
+// against 14 us and 2.4 us for each 128 keys of a tile of rows.  (16 queries of four heads a KV head, 4 x 4000 keys, 8 KV heads: 46 us there,
+// 32 here; 6 queries over 2000 keys of one sequence: 19 there, 22 here.)  Up to 16 rows there is nothing to gain here.
+bool is_contraction(const PagedGroup& g, int group, int Hkv, int max_rows, int num_sms) {
+    const int tile_rows = max_rows > 128 ? 256 : 128;
+    int64_t few = 0, many = 0;
+    for (int i = 0; i < g.nseq; ++i) {
+        const PagedSeq& s = g.seq[i];
+        if (s.tq == 0) continue;
+        const int64_t rows = static_cast<int64_t>(s.tq) * group, local = dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1);
+        few += (rows + 15) / 16 * Hkv * ((s.c_len + 63) / 64 + (local + 63) / 64);
+        many += (rows + tile_rows - 1) / tile_rows * Hkv * ((s.c_len + 127) / 128 + (local + 127) / 128);
+    }
+    return 1.6 * few / (2.0 * num_sms) > 8.0 + 2.4 * many / num_sms;
+}
 // n / d = n * mul >> shift for 0 <= n < 2^31: mul = ceil(2^shift / d) with 2^(shift - 31) >= d is at most d / 2^shift too large
 void divide_by(int d, uint32_t& mul, int& shift) {
     shift = 31;
@@ -118,13 +133,15 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
         }
         if (most == 0) continue;
         const int max_rows = most > 0x7fffffff ? 0x7fffffff : static_cast<int>(most);
+        const bool boxes = dodo_paged_box(cache->page, 8) > 0;       // pages that tensor copies can take by boxes
         // Many bf16 rows are a contraction: the tensor cores.  (Row maxima are taken before scaling, so the scale must be positive.)
-        if (dtype == DODO_BF16 && max_rows > kFewRows && sm_scale >= DODO_DENSE_LEAST_SCALE && workspace != nullptr &&
-            workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh)) {
+        if (dtype == DODO_BF16 && sm_scale >= DODO_DENSE_LEAST_SCALE && workspace != nullptr &&
+            workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh) && max_rows > 16 &&
+            (!boxes || is_contraction(g, a.group, Hkv, max_rows, ctx->num_sms))) {
             if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
             continue;
         }
-        const bool token = dtype == DODO_BF16 && dodo_paged_box(cache->page, 8) > 0;
+        const bool token = dtype == DODO_BF16 && boxes;
         const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
         dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);

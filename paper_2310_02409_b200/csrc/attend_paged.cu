@@ -213,6 +213,9 @@ PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, const PagedGroup& g, int group
         if (s[1] > 1 && 2 * max_rows <= s[1]) continue;
         cut.warp_rows = s[0];
         cut.rows = s[1];
+        // blocks: as many as registers let an SM hold, but with eight rows a warp, bound by arithmetic, twice as many (256 fp32 queries over
+        // 2256 keys: 265 us, with half as many blocks 327; four rows over 8 x 4001 keys 64 us, with a third more blocks 85)
+        cut.target = s[0] == 4 ? 3 * ctx->num_sms : dodo_paged_rows_blocks(ctx);
         int64_t blocks = 0;
         for (int i = 0; i < g.nseq; ++i) {
             const PagedSeq& q = g.seq[i];
