@@ -125,25 +125,15 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
         keys(t_begin);
         entries(t_begin + kAhead);
         int n = 0;                     // stages filled so far
-        auto fill = [&](int t, int r0, int p0, int p1, bool end) {      // false: a wait ran out
-            const int hi = max(p0, p1);
-            const bool masked = __any_sync(0xffffffffu, hi > first_pos), holes = __any_sync(0xffffffffu, hi == kNoPos);
-            const int st = n % L::kStages;
-            if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], static_cast<uint32_t>(n / L::kStages + 1) & 1u))) return false;
-            *reinterpret_cast<int2*>(&s_pos[st][2 * lane]) = make_int2(p0, p1);
-            const bool local = t >= c_stages;
-            if (lane == 0) s_kind[st] = end ? kEnd : (masked ? kMasked : 0) | (holes ? kHoles : 0);
-            __syncwarp();
-            ++n;
-            if (end) {
-                if (lane == 0) mbar_arrive(&full[st]);
-                return true;
-            }
+        // A stage's copies need its rows alone; what the consumers wait for beside them are its positions, and the word that they are there.
+        auto copy = [&](int st, int t, int r0) {
             // a box starts with an even key: the lane that holds it copies it, if its first row is there
+            const bool local = t >= c_stages;
             const int box = local ? BN : boxes.rows;
             const bool mine = 2 * lane % box == 0 && r0 >= 0;
             const uint32_t have = __popc(__ballot_sync(0xffffffffu, mine));
-            if (lane == 0) mbar_expect_tx(&full[st], have * box * DH * 4);
+            if (lane == 0)
+                asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&full[st])), "r"(have * box * DH * 4) : "memory");
             __syncwarp();
             if (mine) {
                 const CUtensorMap* const mk = local ? &boxes.lK : &boxes.cK;
@@ -154,8 +144,22 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
 #pragma unroll
                 for (int h = 0; h < L::kHalves; ++h) tma_load_2d(dst + L::kTile + h * L::kHalf, mv, col + 64 * h, r0, &full[st]);
             }
-            return true;
         };
+        auto publish = [&](int st, int p0, int p1, bool end) {
+            const int hi = max(p0, p1);
+            const bool masked = __any_sync(0xffffffffu, hi > first_pos), holes = __any_sync(0xffffffffu, hi == kNoPos);
+            *reinterpret_cast<int2*>(&s_pos[st][2 * lane]) = make_int2(p0, p1);
+            if (lane == 0) s_kind[st] = end ? kEnd : (masked ? kMasked : 0) | (holes ? kHoles : 0);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[st]);
+            ++n;
+        };
+        auto wait_empty = [&]() { return __all_sync(0xffffffffu, mbar_wait(&empty[n % L::kStages], static_cast<uint32_t>(n / L::kStages + 1) & 1u)); };
+        // the first stages go out ahead of their positions
+        constexpr int kFirst = L::kStages < kAhead ? L::kStages : kAhead;
+#pragma unroll
+        for (int u = 0; u < kFirst; ++u)
+            if (t_begin + u < t_end) copy(u, t_begin + u, row[u][0]);
         for (int t = t_begin; t < t_end && !stuck; t += kAhead) {
             int r0[kAhead], q[kAhead][2];
 #pragma unroll
@@ -168,11 +172,19 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
             entries(t + 2 * kAhead);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (stuck || t + u >= t_end || !__any_sync(0xffffffffu, min(q[u][0], q[u][1]) != kNoPos)) continue;      // nobody sees a key of this stage
-                stuck = !fill(t + u, r0[u], q[u][0], q[u][1], false);
+                if (stuck || t + u >= t_end) continue;
+                if (u < kFirst && t == t_begin) {
+                    publish(u, q[u][0], q[u][1], false);
+                } else if (__any_sync(0xffffffffu, min(q[u][0], q[u][1]) != kNoPos)) {      // (else nobody sees a key of this stage)
+                    if (!wait_empty()) { stuck = true; continue; }
+                    const int st = n % L::kStages;
+                    copy(st, t + u, r0[u]);
+                    publish(st, q[u][0], q[u][1], false);
+                }
             }
         }
-        if (!stuck) stuck = !fill(0, -1, kNoPos, kNoPos, true);
+        if (!stuck && !wait_empty()) stuck = true;
+        if (!stuck) publish(n % L::kStages, kNoPos, kNoPos, true);
         if (stuck)          // copies in flight land before the block's shared memory goes
             for (int i = max(0, n - L::kStages); i < n; ++i) mbar_wait(&full[i % L::kStages], static_cast<uint32_t>(i / L::kStages) & 1u);
     } else {

@@ -128,6 +128,7 @@ int rope_impl(dodo_ctx* ctx, const dodo_rope_spec* rope, const dodo_rope_array* 
         a.in[a.n] = v.in; a.out[a.n] = v.out;
         a.first[a.n] = a.heads;
         a.in_row[a.n] = v.in_row; a.in_head[a.n] = v.in_head; a.out_row[a.n] = v.out_row; a.out_head[a.n] = v.out_head;
+        if (v.heads > 65535 - a.heads) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "more than 65,535 heads");
         a.heads += v.heads;
         ++a.n;
     }
