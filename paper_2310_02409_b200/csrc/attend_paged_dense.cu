@@ -847,10 +847,11 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     w.slot0[g.nseq] = static_cast<int>(total);
     w.total = static_cast<int>(total);
     if (total == 0) return DODO_OK;
-    // One block per SM, but none for less than four tiles or a unit.  Where all units are alike there is also the share of a k-th of a
+    // One block per SM, but none for less than four tiles (with one tile of rows two: the streams take them side by side; 7 x 12 to 16
+    // queries of eight heads a KV head over up to 2296 keys took 29 us with four, 25 with two) or a unit.  Where all units are alike there is also the share of a k-th of a
     // unit each: no block then works for two units.  By the count of tiles' times of the slowest block: a unit begun and ended costs about
     // three (Q, a pipeline filled and emptied, results), pieces joined another three.
-    const int64_t most = (total + 3) / 4 > units ? (total + 3) / 4 : units;
+    const int64_t shares = tiles == 1 ? (total + 1) / 2 : (total + 3) / 4, most = shares > units ? shares : units;
     int64_t grid = most < ctx->num_sms ? most : ctx->num_sms;
     bool alike = true;
     int nt = 0;
