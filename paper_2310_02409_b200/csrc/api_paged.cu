@@ -110,7 +110,8 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
     PagedArrays a;
     memset(&a, 0, sizeof a);
     a.Q = Q; a.O = O;
-    a.cK = any_rows ? cache->K : nullptr; a.cV = any_rows ? cache->V : nullptr;
+    const bool any_page = any_rows && cache->pages > 0;      // (a pool of no pages: no entry of the table is one)
+    a.cK = any_page ? cache->K : nullptr; a.cV = any_page ? cache->V : nullptr;
     a.lK = any_local ? locK : nullptr; a.lV = any_local ? locV : nullptr;
     a.pos = cache->pos; a.table = cache->table;
     a.pages = cache->pages; a.page = cache->page;

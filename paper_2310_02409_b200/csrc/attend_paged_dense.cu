@@ -196,7 +196,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    __shared__ __align__(8) uint64_t bar_q, bar_o, bar_s[2], bar_p[2][2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
+    __shared__ __align__(8) uint64_t bar_q, bar_o, bar_drain, bar_s[2], bar_p[2][2], bar_kfull[L::kKStages], bar_kfree[L::kKStages], bar_vfull[L::kVStages],
         bar_vfree[L::kVStages], bar_vclean[L::kVStages], bar_posfull[kPosSlots], bar_posfree[kPosSlots];
     __shared__ uint32_t s_tmem;
     __shared__ int s_kind[kPosSlots], s_last;
@@ -226,6 +226,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
     if (tid == 0) {
         mbar_init(&bar_q, kSoftmaxWarps);
         mbar_init(&bar_o, 1);
+        mbar_init(&bar_drain, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_s[i], 1); mbar_init(&bar_p[i][0], 4); mbar_init(&bar_p[i][1], 4); }
         for (int i = 0; i < L::kKStages; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], 1); }
         for (int i = 0; i < L::kVStages; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], 1); mbar_init(&bar_vclean[i], 1); }
@@ -454,13 +455,18 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
             ++np[st];
         };
         auto wait_v = [&](int c) { if (!warp_wait(&bar_vclean[c % L::kVStages], static_cast<uint32_t>(c / L::kVStages) & 1u)) stuck = true; };
+        // nobody sees a key of the segment: the softmax warps, which bring the next Q behind this, come no further ahead than that
+        auto empty = [&]() {
+            if (lane == 0) mbar_arrive(&bar_o);
+            __syncwarp();
+        };
         while (!stuck && next_segment(g, a, work, L::kRows, x, slot_end, q)) {
             if (!warp_wait(&bar_q, static_cast<uint32_t>(segs) & 1u)) { stuck = true; break; }
             ++segs;
             if constexpr (TILES == 2) {
                 const int streams = q.rows > BM ? 2 : 1;
                 bool more = next_tile();
-                if (!more) continue;
+                if (!more) { empty(); continue; }
                 wait_k(ck);
                 for (int st = 0; st < streams; ++st) scores(st, st, ck, st == streams - 1);
                 ++ck;
@@ -498,7 +504,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 };
                 next_scores();
                 next_scores();
-                if (ahead == 0) continue;
+                if (ahead == 0) { empty(); continue; }
                 while (!stuck && i < ahead) {
                     wait_v(cv);
                     values(i & 1, cv, i >= 2, true, [] {});
@@ -509,6 +515,11 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
             }
             if (elect_one()) mma_commit(&bar_o);
             __syncwarp();
+        }
+        if (stuck) {         // products in flight end before the block's tensor and shared memory go
+            if (elect_one()) mma_commit(&bar_drain);
+            __syncwarp();
+            mbar_wait(&bar_drain, 0u);
         }
     } else {
         // ================================================ softmax =================================================
@@ -656,11 +667,9 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar_posfree[ps]);
             }
-            if (tiles > 0) {
-                if (!stuck && !warp_wait(&bar_o, static_cast<uint32_t>(os) & 1u)) stuck = true;
-                ++os;
-                tc_fence_after();
-            }
+            if (!stuck && !warp_wait(&bar_o, static_cast<uint32_t>(os) & 1u)) stuck = true;
+            ++os;
+            tc_fence_after();
             if (l != l) m = INFINITY;        // a NaN among the logits that the row sees: the whole row's, wherever its maximum stands
             // The matrix unit is through with Q: it gets the next segment's now, and has work while this one's results go out.
             Segment next;
@@ -848,9 +857,9 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     w.total = static_cast<int>(total);
     if (total == 0) return DODO_OK;
     // One block per SM, but none for less than four tiles (with one tile of rows two: the streams take them side by side; 7 x 12 to 16
-    // queries of eight heads a KV head over up to 2296 keys took 29 us with four, 25 with two) or a unit.  Where all units are alike there is also the share of a k-th of a
-    // unit each: no block then works for two units.  By the count of tiles' times of the slowest block: a unit begun and ended costs about
-    // three (Q, a pipeline filled and emptied, results), pieces joined another three.
+    // queries of eight heads a KV head over up to 2296 keys took 29 us with four, 25 with two) or a unit.  Where all units are alike there
+    // is also the share of a k-th of a unit each: no block then works for two units.  By the count of tiles' times of the slowest block: a
+    // unit begun and ended costs about three (Q, a pipeline filled and emptied, results), pieces joined another three.
     const int64_t shares = tiles == 1 ? (total + 1) / 2 : (total + 3) / 4, most = shares > units ? shares : units;
     int64_t grid = most < ctx->num_sms ? most : ctx->num_sms;
     bool alike = true;

@@ -1,5 +1,7 @@
 """The paged nugget cache on the GPU: appends with the rotation on the way, attention over it by chunks and single tokens, against plain
 forms in 64 bits; masks, bad pages, shared pages, strides, cuts, captures and streams."""
+import struct
+
 import numpy as np
 import pytest
 import torch
@@ -567,3 +569,46 @@ def test_without_a_workspace_no_list_is_cut(dodo, dtype, H, Hkv, tq):
     s = _batch(dtype, H, Hkv, 128, [tq], [3000], [tq], 16)
     O, L = _run(dodo, s, workspace=False)
     _check(s, O, L)
+
+
+@pytest.mark.parametrize("tq,H,Hkv,dh", [(20, 16, 4, 64), (70, 16, 4, 128), (1, 8, 8, 128)])
+@pytest.mark.parametrize("page", [5, 16])
+def test_sequences_that_see_nothing_between_others(dodo, tq, H, Hkv, dh, page):
+    """Every key of most sequences lies ahead of their queries: blocks with several pieces of work that have no key to read."""
+    B = 48
+    s = _batch(BF, H, Hkv, dh, [tq] * B, [300 + 7 * (b % 5) for b in range(B)], [0] * B, page)
+    s["q_pos0"][:] = 10 ** 5
+    for b in range(B):
+        if b % 4 != 1:
+            s["pos"][s["rows"][b]] = 10 ** 6
+    O, L = _run(dodo, s)
+    _check(s, O, L, only=[0, 1, 2, 3, 5, 45, 47])
+    for b in range(B):
+        if b % 4 != 1:
+            q = slice(s["q_off"][b], s["q_off"][b + 1])
+            assert not O[q].any() and torch.isneginf(L[q]).all()
+
+
+@pytest.mark.parametrize("dtype,tq", [(BF, 1), (BF, 60), (F32, 3)])
+def test_pool_of_no_pages(libdodo, dtype, tq):
+    """No entry of the table is a page then: what is cached is not seen, the local tokens are."""
+    own = api.Dodo(0)
+    s = _batch(dtype, 4, 2, 64, [tq, tq], [40, 24], [tq, tq + 3], 8)
+    s["pages"] = 0
+    s["cK"], s["cV"] = s["cK"][:0], s["cV"][:0]
+    shape = (0, 8, 2, 64)
+    held = torch.zeros(64, device="cuda")         # an address to give: empty tensors have none
+    cache = api.PagedCache(torch.empty(shape, dtype=dtype, device="cuda"), torch.empty(shape, dtype=dtype, device="cuda"),
+                           torch.empty(0, dtype=torch.int32, device="cuda"), _cuda(s["table"]))
+    at = held.data_ptr()
+    cache.spec = struct.pack("QQQQiiiiii", at, at, at, cache.table.data_ptr(), cache.code, 2, 64, 0, 8, 0)
+    O, L = torch.full(s["Q"].shape, 7.0, dtype=dtype, device="cuda"), torch.full(s["Q"].shape[:2], 7.0, device="cuda")
+    ws = torch.empty(own.attend_paged_workspace_bytes(64), dtype=torch.uint8, device="cuda")
+    own.attend_paged(s["Q"].cuda(), s["q_off"], s["q_pos0"], s["scale"], cache, s["page_off"], s["nug"], s["lK"].cuda(), s["lV"].cuda(), s["loc_off"][:-1],
+                     s["loc"], s["loc_pos0"], O, L, ws)
+    torch.cuda.synchronize()
+    assert own.device_status() == api.DEV_BAD_INDEX
+    s["rows"], s["nug"] = [r[:0] for r in s["rows"]], np.zeros(2, np.int32)
+    _check(s, O, L)
+    own.reset()
+    own.close()
