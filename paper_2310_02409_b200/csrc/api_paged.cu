@@ -49,18 +49,21 @@ namespace {
 // Whether a batch is worth the tensor cores' kernel, whose blocks take longer to begin and to end, or the one for few rows takes it in
 // tiles of 16.  By what both take for stages of keys per SM: about 6 us and 1.6 us for each 64 keys of 16 rows that two blocks of an SM have,
 // against 14 us and 2.4 us for each 128 keys of a tile of rows.  (16 queries of four heads a KV head, 4 x 4000 keys, 8 KV heads: 46 us there,
-// 32 here; 6 queries over 2000 keys of one sequence: 19 there, 22 here.)  Up to 16 rows there is nothing to gain here.
+// 32 here; 6 queries over 2000 keys of one sequence: 19 there, 22 here.)  More tiles of 16 rows than blocks at a time take turns: four
+// sequences of 64 rows and 264 keys, 32 KV heads, 25 us there and 15 here.  Up to 16 rows there is nothing to gain here.
 bool is_contraction(const PagedGroup& g, int group, int Hkv, int max_rows, int num_sms) {
     const int tile_rows = max_rows > 128 ? 256 : 128;
-    int64_t few = 0, many = 0;
+    int64_t few = 0, many = 0, units = 0;
     for (int i = 0; i < g.nseq; ++i) {
         const PagedSeq& s = g.seq[i];
         if (s.tq == 0) continue;
         const int64_t rows = static_cast<int64_t>(s.tq) * group, local = dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1);
+        units += (rows + 15) / 16 * Hkv;
         few += (rows + 15) / 16 * Hkv * ((s.c_len + 63) / 64 + (local + 63) / 64);
         many += (rows + tile_rows - 1) / tile_rows * Hkv * ((s.c_len + 127) / 128 + (local + 127) / 128);
     }
-    return 1.6 * few / (2.0 * num_sms) > 8.0 + 2.4 * many / num_sms;
+    const double turns = units > 2 * num_sms ? static_cast<double>((units + 2 * num_sms - 1) / (2 * num_sms)) / units : 0.5 / num_sms;
+    return 1.6 * few * turns > 8.0 + 2.4 * many / num_sms;
 }
 // n / d = n * mul >> shift for 0 <= n < 2^31: mul = ceil(2^shift / d) with 2^(shift - 31) >= d is at most d / 2^shift too large
 void divide_by(int d, uint32_t& mul, int& shift) {

@@ -57,6 +57,7 @@ struct Layout {
 
 struct DenseShare {
     int total;                      // slots
+    int whole;                      // slots that a block takes or leaves together: 1, or a unit's where blocks take whole units
     int slot0[DODO_GROUP + 1];      // first slot of each sequence
     int nt[DODO_GROUP];             // slots of a unit of the sequence
     int tiles[DODO_GROUP];          // tiles of rows
@@ -119,10 +120,9 @@ __device__ __forceinline__ bool any_softmax(bool mine) {
     return r != 0u;
 }
 
-__device__ __forceinline__ int block_start(int T, int G, int c) { return static_cast<int>(static_cast<long long>(c) * T / G); }
-__device__ __forceinline__ int block_of(int T, int G, int x) {   // the block whose range holds slot x
-    return static_cast<int>(((static_cast<long long>(x) + 1) * G - 1) / T);
-}
+// the first slot of block c of G, and, where shares are single slots, the block whose range holds slot x
+__device__ __forceinline__ int block_start(const DenseShare& w, int G, int c) { return static_cast<int>(static_cast<long long>(c) * (w.total / w.whole) / G) * w.whole; }
+__device__ __forceinline__ int block_of(int T, int G, int x) { return static_cast<int>(((static_cast<long long>(x) + 1) * G - 1) / T); }
 
 // A unit's share of a block: its rows, its key list, the tiles [t0, t1) of it
 struct Segment {
@@ -205,8 +205,8 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
 
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int T = work.total, G = static_cast<int>(gridDim.x), bid = static_cast<int>(blockIdx.x);
-    const int slot_end = block_start(T, G, bid + 1);
-    int x = block_start(T, G, bid);
+    const int slot_end = block_start(work, G, bid + 1);
+    int x = block_start(work, G, bid);
     Segment q;
 
     // Hints to L2 while the block sets itself up: the rows of Q that it begins with (behind the first keys of all blocks they would come
@@ -742,63 +742,96 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
             }
             bool odd = false;                              // a result that is not finite
             if (done && warp_live) {
-                // the unit is the first of every block but the one that it begins in
-                const int begun = c_first < c_last && block_start(T, G, c_first) < q.first_slot ? 1 : 0;
-                auto part_of = [&](int c) { return a.part + static_cast<size_t>(2 * c + (c == c_first ? begun : 0)) * L::kPartFloats; };
-                auto max_sum = [&](int c) { return c == bid ? make_float2(M, S) : __ldcg(reinterpret_cast<const float2*>(part_of(c) + static_cast<size_t>(DH) * L::kRows) + my); };
-                float MM = -INFINITY, SS = 0.f;
-                for (int c = c_first; c <= c_last; ++c) {
-                    const float2 ms = max_sum(c);
-                    const float top = fmaxf(MM, ms.x), k0 = part_weight(MM, top), k1 = part_weight(ms.x, top);
-                    SS = (k0 != 0.f ? k0 * SS : 0.f) + (k1 != 0.f ? k1 * ms.y : 0.f);
-                    MM = top;
-                }
-                const float inv = SS != 0.f ? 1.f / SS : 0.f;
-                float o[kFeat];
-#pragma unroll
-                for (int e = 0; e < kFeat; ++e) o[e] = 0.f;
-#pragma unroll 1
-                for (int c = c_first; c <= c_last; ++c) {
-                    const float w = part_weight(max_sum(c).x, MM);
-#pragma unroll
-                    for (int f = 0; f < kFeat; f += 32) {
-                        float v[32];
-                        if (c == bid) {
-                            own(f0 + f, v);
-                        } else {
-                            const float4* const src = reinterpret_cast<const float4*>(part_of(c)) + static_cast<size_t>((f0 + f) / 4) * L::kRows + my;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 x4 = __ldcg(src + static_cast<size_t>(e / 4) * L::kRows);
-                                v[e] = x4.x; v[e + 1] = x4.y; v[e + 2] = x4.z; v[e + 3] = x4.w;
-                            }
-                        }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[f + e] = w != 0.f ? fmaf(w, v[e], o[f + e]) : o[f + e];
-                    }
-                }
-                float zero = 0.f;
-#pragma unroll
-                for (int e = 0; e < kFeat; ++e) { o[e] *= inv; zero = fmaf(o[e], 0.f, zero); }
-                odd = !(zero == 0.f);
                 // out through shared memory, 32 features at a time: four lanes a row, eight rows an instruction
+                uint4* at[4];
 #pragma unroll
-                for (int f = 0; f < kFeat; f += 32) {
+                for (int i = 0; i < 4; ++i) {
+                    const int r = min(warp_row + i * 8 + lane / 4, q.rows - 1);
+                    at[i] = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + r) * DH + f0) + lane % 4;
+                }
+                float2 zero = make_float2(0.f, 0.f);
+                auto emit = [&](int f, const float2* o) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        zero = __ffma2_rn(o[e], make_float2(0.f, 0.f), zero);
+                        w[e] = pack_bf16(o[e].x, o[e].y);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint4*>(out_tile + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4)) =
-                            make_uint4(pack_bf16(o[f + 8 * e], o[f + 8 * e + 1]), pack_bf16(o[f + 8 * e + 2], o[f + 8 * e + 3]),
-                                       pack_bf16(o[f + 8 * e + 4], o[f + 8 * e + 5]), pack_bf16(o[f + 8 * e + 6], o[f + 8 * e + 7]));
+                        *reinterpret_cast<uint4*>(out_tile + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = i * 8 + lane / 4, e = lane % 4;
-                        if (warp_row + r < q.rows)
-                            reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + warp_row + r) * DH + f0 + f)[e] =
-                                *reinterpret_cast<const uint4*>(out_tile + r * 64 + ((e ^ (r >> 1 & 3)) << 4));
+                        const int r = i * 8 + lane / 4;
+                        if (warp_row + r < q.rows) at[i][f / 8] = *reinterpret_cast<const uint4*>(out_tile + r * 64 + ((lane % 4 ^ (r >> 1 & 3)) << 4));
                     }
                     __syncwarp();
+                };
+                float MM = M, SS = S;
+                if (c_first == c_last) {
+                    const float inv = S != 0.f ? 1.f / S : 0.f;
+                    const float2 k0 = make_float2(w0 * inv, w0 * inv), k1 = make_float2(w1 * inv, w1 * inv);
+                    const bool some = TILES == 2 ? mine > 0 : tiles > 0;
+#pragma unroll
+                    for (int f = 0; f < kFeat; f += 32) {
+                        uint32_t ov[32];
+                        float2 o[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = make_float2(0.f, 0.f);
+                        if (some) {
+                            tmem_ld32(t_o + (TILES == 2 ? st * DH : 0) + f0 + f, ov);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __fmul2_rn(k0, make_float2(__uint_as_float(ov[2 * e]), __uint_as_float(ov[2 * e + 1])));
+                        }
+                        if (TILES == 1 && tiles > 1) {
+                            tmem_ld32(t_o + DH + f0 + f, ov);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __ffma2_rn(k1, make_float2(__uint_as_float(ov[2 * e]), __uint_as_float(ov[2 * e + 1])), o[e]);
+                        }
+                        emit(f, o);
+                    }
+                } else {
+                    // the unit is the first of every block but the one that it begins in
+                    const int begun = block_start(work, G, c_first) < q.first_slot ? 1 : 0;
+                    auto part_of = [&](int c) { return a.part + static_cast<size_t>(2 * c + (c == c_first ? begun : 0)) * L::kPartFloats; };
+                    auto max_sum = [&](int c) { return c == bid ? make_float2(M, S) : __ldcg(reinterpret_cast<const float2*>(part_of(c) + static_cast<size_t>(DH) * L::kRows) + my); };
+                    MM = -INFINITY, SS = 0.f;
+                    for (int c = c_first; c <= c_last; ++c) {
+                        const float2 ms = max_sum(c);
+                        const float top = fmaxf(MM, ms.x), a0 = part_weight(MM, top), a1 = part_weight(ms.x, top);
+                        SS = (a0 != 0.f ? a0 * SS : 0.f) + (a1 != 0.f ? a1 * ms.y : 0.f);
+                        MM = top;
+                    }
+                    const float inv = SS != 0.f ? 1.f / SS : 0.f;
+                    float2 o[kFeat / 2];
+#pragma unroll
+                    for (int e = 0; e < kFeat / 2; ++e) o[e] = make_float2(0.f, 0.f);
+#pragma unroll 1
+                    for (int c = c_first; c <= c_last; ++c) {
+                        const float w = part_weight(max_sum(c).x, MM);
+                        const float2 k = make_float2(w * inv, w * inv);
+#pragma unroll
+                        for (int f = 0; f < kFeat; f += 32) {
+                            float v[32];
+                            if (c == bid) {
+                                own(f0 + f, v);
+                            } else {
+                                const float4* const src = reinterpret_cast<const float4*>(part_of(c)) + static_cast<size_t>((f0 + f) / 4) * L::kRows + my;
+#pragma unroll
+                                for (int e = 0; e < 32; e += 4) {
+                                    const float4 x4 = __ldcg(src + static_cast<size_t>(e / 4) * L::kRows);
+                                    v[e] = x4.x; v[e + 1] = x4.y; v[e + 2] = x4.z; v[e + 3] = x4.w;
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[f / 2 + e] = __ffma2_rn(k, make_float2(v[2 * e], v[2 * e + 1]), o[f / 2 + e]);
+                        }
+                    }
+#pragma unroll
+                    for (int f = 0; f < kFeat; f += 32) emit(f, o + f / 2);
                 }
+                odd = !(zero.x + zero.y == 0.f);
                 if (live && a.lse != nullptr && (TILES == 2 || st == 0)) a.lse[out_row(a, s, q.head, q.r0 + my)] = SS != 0.f ? (MM + log2f(SS)) * 0.6931471805599453f : -INFINITY;
             }
             // ---- results that are not finite, once more over what their rows see
@@ -858,17 +891,20 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     if (total == 0) return DODO_OK;
     // One block per SM, but none for less than four tiles (with one tile of rows two: the streams take them side by side; 7 x 12 to 16
     // queries of eight heads a KV head over up to 2296 keys took 29 us with four, 25 with two) or a unit.  Where all units are alike there
-    // is also the share of a k-th of a unit each: no block then works for two units.  By the count of tiles' times of the slowest block: a
-    // unit begun and ended costs about three (Q, a pipeline filled and emptied, results), pieces joined another three.
+    // is also the share of a k-th of a unit each (no block then works for two units) and that of whole units (none is joined: 256 units of
+    // 64 rows over 264 keys took 36 us with equal shares, 26 so).  By the count of tiles' times of the slowest block: a unit begun and ended
+    // costs about three (Q, a pipeline filled and emptied, results), pieces joined another three.
     const int64_t shares = tiles == 1 ? (total + 1) / 2 : (total + 3) / 4, most = shares > units ? shares : units;
     int64_t grid = most < ctx->num_sms ? most : ctx->num_sms;
     bool alike = true;
     int nt = 0;
     for (int i = 0; i < g.nseq; ++i)
         if (g.seq[i].tq > 0) { alike = alike && (nt == 0 || nt == w.nt[i]); nt = w.nt[i]; }
-    if (alike && units <= ctx->num_sms) {
-        const int64_t each = (total + grid - 1) / grid;
+    w.whole = 1;
+    if (alike) {
+        const int64_t each = (total + grid - 1) / grid, most_units = (units + ctx->num_sms - 1) / ctx->num_sms;
         int64_t cost = each + 3 * ((each + nt - 1) / nt + 1) + 3;
+        if (units > ctx->num_sms && most_units * (nt + 3) < cost) { grid = ctx->num_sms; w.whole = nt; }
         for (int64_t k = 1; k <= ctx->num_sms / units && k <= (nt + 3) / 4; ++k) {
             const int64_t c = (nt + k - 1) / k + 3 + (k > 1 ? 3 : 0);
             if (c < cost) { cost = c; grid = units * k; }
