@@ -65,6 +65,18 @@ bool is_contraction(const PagedGroup& g, int group, int Hkv, int max_rows, int n
     const double turns = units > 2 * num_sms ? static_cast<double>((units + 2 * num_sms - 1) / (2 * num_sms)) / units : 0.5 / num_sms;
     return 1.6 * few * turns > 8.0 + 2.4 * many / num_sms;
 }
+// Whether fp32 rows are taken in tiles: where tiles of 128 keys and up to 64 rows are blocks enough for the device.  Fewer are spread over more
+// blocks by the kernel for few rows (64 rows over 124 keys of 8 heads: 9 us there, 27 in tiles; four times 64 rows over 1064 keys: 111, 70).
+bool is_tiled(const PagedGroup& g, int group, int Hkv, int max_rows, int num_sms) {
+    const int tile_rows = max_rows <= 32 ? 32 : 64;
+    int64_t blocks = 0;
+    for (int i = 0; i < g.nseq; ++i) {
+        const PagedSeq& s = g.seq[i];
+        const int64_t chunks = (static_cast<int64_t>(s.c_len) + s.l_len) / 128;
+        blocks += (static_cast<int64_t>(s.tq) * group + tile_rows - 1) / tile_rows * Hkv * (chunks > 1 ? chunks : 1);
+    }
+    return blocks >= num_sms;
+}
 // n / d = n * mul >> shift for 0 <= n < 2^31: mul = ceil(2^shift / d) with 2^(shift - 31) >= d is at most d / 2^shift too large
 void divide_by(int d, uint32_t& mul, int& shift) {
     shift = 31;
@@ -145,11 +157,13 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
             if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
             continue;
         }
-        const bool token = dtype == DODO_BF16 && boxes;
-        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
+        const bool token = dtype == DODO_BF16 && boxes, tile = dtype == DODO_F32 && max_rows > 16 && is_tiled(g, a.group, Hkv, max_rows, ctx->num_sms);
+        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : tile ? dodo_paged_tile_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
         dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);
-        rc = token ? dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st) : dodo_launch_paged_rows(ctx, dtype, dh, cut, g, a, st);
+        if (token) rc = dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st);
+        else if (tile) rc = dodo_launch_paged_tile(ctx, dh, max_rows, g, a, st);
+        else rc = dodo_launch_paged_rows(ctx, dtype, dh, cut, g, a, st);
         if (rc != DODO_OK) return rc;
     }
     return DODO_OK;

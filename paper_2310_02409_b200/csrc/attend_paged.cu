@@ -1,9 +1,11 @@
-// Attention over a paged cache on the FMA units: a warp holds a few rows (their queries and running results in registers, spread over
+// Attention of few rows over a paged cache on the FMA units (fp32, and bf16 in pages that tensor copies cannot take): a warp holds a few rows (their queries and running results in registers, spread over
 // the lanes by features) and streams the keys from memory straight into registers, a key's K and V row as one coalesced access.
 // Per step it takes U keys a group of lanes: partial products of all (row, key) pairs, summed over the lanes by halving exchanges so
 // that each lane ends up with one pair's logit, one exponential a lane, and the weights handed back by shuffles.  Table entries,
 // positions and rows of the following steps are on their way meanwhile (three steps deep, as each needs the one before).  A block's
 // four warps share the keys where there are rows for all of them (the rows they read then come from L1) and split them where not.
+// Bound by memory's latency for a row or two (16 fp32 queries over 68 keys of 4 heads: 5.4 us), by HBM for long lists, by the FMA units and
+// the exchanges between lanes from four rows a KV head on (four over 8 x 4001 keys of 8 heads: 64 us, 4.1 TB/s of K and V).
 #include "paged.cuh"
 
 namespace {
@@ -205,7 +207,7 @@ cudaError_t launch(const PagedCut& cut, const PagedGroup& g, const PagedArrays& 
 
 // As many rows a warp and a block as there are (their keys are then read once), up to eight and 32, while that leaves blocks enough for the
 // device; a small batch takes fewer, down to a row a warp, and its keys are split over more warps and blocks instead (16 queries over 52 + 16
-// keys of 4 heads: 11.2 us with 16 rows a block, TINY with one).
+// keys of 4 heads: 11.2 us with 16 rows a block, 5.4 with one).
 PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, const PagedGroup& g, int group, int Hkv, int max_rows) {
     static const int shapes[][2] = {{8, 32}, {8, 16}, {8, 8}, {4, 4}, {1, 1}};
     PagedCut cut = {1, 32, dodo_paged_rows_blocks(ctx), 128, 1};
@@ -214,7 +216,7 @@ PagedCut dodo_paged_rows_cut(const dodo_ctx* ctx, const PagedGroup& g, int group
         cut.warp_rows = s[0];
         cut.rows = s[1];
         // blocks: as many as registers let an SM hold, but with eight rows a warp, bound by arithmetic, twice as many (256 fp32 queries over
-        // 2256 keys: 265 us, with half as many blocks 327; four rows over 8 x 4001 keys 64 us, with a third more blocks 85)
+        // 2256 keys, in tiles of 64 rows by now: 265 us, with half as many blocks 327; four rows over 8 x 4001 keys 64 us, with a third more blocks 85)
         cut.target = s[0] == 4 ? 3 * ctx->num_sms : dodo_paged_rows_blocks(ctx);
         int64_t blocks = 0;
         for (int i = 0; i < g.nseq; ++i) {

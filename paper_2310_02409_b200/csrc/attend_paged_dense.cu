@@ -840,7 +840,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                     __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, q.head, q.r0 + r) * DH;
                     bool bad = false;
                     for (int f = lane; f < DH; f += 32) bad = bad || !isfinite(__bfloat162float(out[f]));
-                    if (__any_sync(0xffffffffu, bad)) sum_again<DH>(a, s, q.head, q.r0 + r, out);
+                    if (__any_sync(0xffffffffu, bad)) sum_again<__nv_bfloat16, DH>(a, s, q.head, q.r0 + r, out);
                 }
             }
             first_seg = false;

@@ -37,7 +37,7 @@ struct dodo_ctx {
     bool q4_attr_set[3];        // ... and of the 4-bit kernels on the warp-level matrix units
     bool backward_attr_set[4];  // ... and of the kernels of attend's gradient
     bool paged_attr_set[4];     // ... and of the tensor-core attend over a paged cache
-    bool paged_token_attr_set[4];
+    bool paged_token_attr_set[4], paged_tile_attr_set[4];
     bool mlp_attr_set;          // ... and of the two-layer Scorer's kernel
     bool select_attr_set;       // ... and of the select / estimate kernels, with the keys they may cache
     int select_key_cap;

@@ -56,6 +56,9 @@ int dodo_paged_box(int page, int most);       // rows that a tensor copy may tak
 int dodo_paged_boxes(dodo_ctx* ctx, const PagedArrays& a, int dh, int loc_rows, int box, int local_box, PagedBoxes& m);
 PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows);
 int dodo_launch_paged_token(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+// many fp32 rows, on the FMA units
+PagedCut dodo_paged_tile_cut(const dodo_ctx* ctx, int max_rows);
+int dodo_launch_paged_tile(dodo_ctx* ctx, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
@@ -126,14 +129,14 @@ __device__ __forceinline__ size_t out_row(const PagedArrays& a, const PagedSeq& 
     return static_cast<size_t>(s.q_row0 + t) * a.H + head * a.group + (r - t * a.group);
 }
 
-// One row's bf16 result again over all of the unit's keys that it sees, whatever the others hold: a warp, a key a lane for the scores, four
-// (two) features a lane for the sums.  For results of matrix products that are not finite, where a weight of 0 may have met a NaN.
-template <int DH>
-__device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, __nv_bfloat16* out) {
-    constexpr int F = DH / 32;
+// One row's result again over all of the unit's keys that it sees, whatever the others hold: a warp, a key a lane for the scores, four (two)
+// features a lane for the sums.  For results of products of tiles that are not finite, where a weight of 0 may have met a NaN.
+template <typename T, int DH>
+__device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, int head, int r, T* out) {
+    constexpr int F = DH / 32, E = 16 / static_cast<int>(sizeof(T));
     const int lane = static_cast<int>(threadIdx.x) & 31;
     const size_t pitch = static_cast<size_t>(a.Hkv) * DH, at = static_cast<size_t>(head) * DH;
-    const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.Q) + out_row(a, s, head, r) * DH;
+    const T* const q = static_cast<const T*>(a.Q) + out_row(a, s, head, r) * DH;
     const int qpos = s.q_pos0 + token_of(a, r), end = s.c_len + dodo_visible_local(s.l_len, s.l_pos0, qpos);
     float m = -INFINITY, l = 0.f, acc[F];
 #pragma unroll
@@ -144,15 +147,15 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
         const bool sees = k.row >= 0 && k.pos <= qpos;
         float x = -INFINITY;
         if (sees) {
-            const __nv_bfloat16* const kr = static_cast<const __nv_bfloat16*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
+            const T* const kr = static_cast<const T*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
             x = 0.f;
 #pragma unroll 4
-            for (int c = 0; c < DH; c += 8) {
-                float kf[8], qf[8];
-                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(kr + c)), kf);
-                Vec16<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(q + c)), qf);
+            for (int c = 0; c < DH; c += E) {
+                float kf[E], qf[E];
+                Vec16<T>::unpack(__ldg(reinterpret_cast<const uint4*>(kr + c)), kf);
+                Vec16<T>::unpack(__ldg(reinterpret_cast<const uint4*>(q + c)), qf);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x = fmaf(kf[e], qf[e], x);
+                for (int e = 0; e < E; ++e) x = fmaf(kf[e], qf[e], x);
             }
             x *= a.scale_log2;
         }
@@ -162,7 +165,7 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
         const float ref = top == -INFINITY ? 0.f : top, corr = part_weight(m, ref), w = exp2_fast(x - ref);
         m = top;
         l = fmaf(l, corr, w);
-        const float rounded = __bfloat162float(__float2bfloat16_rn(w));
+        const float rounded = sizeof(T) == 2 ? __bfloat162float(__float2bfloat16_rn(w)) : w;      // as the product has it
 #pragma unroll
         for (int f = 0; f < F; ++f) acc[f] *= corr;
         uint32_t seen = __ballot_sync(0xffffffffu, sees);
@@ -172,16 +175,16 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
             const int row = __shfl_sync(0xffffffffu, k.row, e);
             const bool local = __shfl_sync(0xffffffffu, k.local ? 1 : 0, e) != 0;
             const float c = __shfl_sync(0xffffffffu, rounded, e);
-            const __nv_bfloat16* const vr = static_cast<const __nv_bfloat16*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
+            const T* const vr = static_cast<const T*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
 #pragma unroll
-            for (int f = 0; f < F; ++f) acc[f] = fmaf(c, __bfloat162float(vr[f]), acc[f]);
+            for (int f = 0; f < F; ++f) acc[f] = fmaf(c, static_cast<float>(vr[f]), acc[f]);
         }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int f = 0; f < F; ++f) out[lane * F + f] = __float2bfloat16_rn(acc[f] * inv);
+    for (int f = 0; f < F; ++f) out[lane * F + f] = static_cast<T>(acc[f] * inv);
 }
 
 // The end of a block of kThreads threads: `parts` partial results of `rows` rows in shared memory (sums of weighted V [part][row][DH]
@@ -293,10 +296,10 @@ __device__ __forceinline__ void finish(const PagedArrays& a, const PagedSeq& s, 
     if constexpr (kMixed) {
         if (__syncthreads_or(odd ? 1 : 0) == 0) return;
         for (int r = tid / 32; r < rows; r += kThreads / 32) {
-            __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.O) + out_row(a, s, p.head, r0 + r) * DH;
+            T* const out = static_cast<T*>(a.O) + out_row(a, s, p.head, r0 + r) * DH;
             bool bad = false;
-            for (int f = tid % 32; f < DH; f += 32) bad = bad || !isfinite(__bfloat162float(out[f]));
-            if (__any_sync(0xffffffffu, bad)) sum_again<DH>(a, s, p.head, r0 + r, out);
+            for (int f = tid % 32; f < DH; f += 32) bad = bad || !isfinite(static_cast<float>(out[f]));
+            if (__any_sync(0xffffffffu, bad)) sum_again<T, DH>(a, s, p.head, r0 + r, out);
         }
     }
 }

@@ -612,3 +612,60 @@ def test_pool_of_no_pages(libdodo, dtype, tq):
     _check(s, O, L)
     own.reset()
     own.close()
+
+
+@pytest.mark.parametrize("H,Hkv,tq,dh", [(16, 8, 12, 128), (16, 8, 40, 128), (24, 8, 11, 64), (8, 8, 70, 64)])
+@pytest.mark.parametrize("kind", ["plain", "nan", "inf", "unseen", "seen nan", "long", "alone"])
+def test_many_f32_rows(dodo, H, Hkv, tq, dh, kind):
+    """Batches of fp32 rows that fill the device: rows of a tile that see different keys, tiles that end inside a page, cut lists."""
+    B = 3 if kind in ("long", "alone") else 24
+    nug = [1300, 1999, 771] if kind == "long" else [900, 0, 700] if kind == "alone" else [(53 * b) % 190 for b in range(B)]
+    s = _batch(F32, H, Hkv, dh, [tq - b % 3 for b in range(B)], nug, [tq - b % 3 + b % 4 for b in range(B)], 24, span=3,
+               fill=float("nan") if kind == "nan" else None)
+    some = [0, 1, 2] if B == 3 else [0, 1, 5, 13, 14, 23]
+    if kind in ("nan", "inf"):      # in keys that the last token of a sequence alone sees, and behind it
+        for b in range(B):
+            at = s["loc_off"][b] + max(int(s["q_off"][b + 1] - s["q_off"][b]) - 1, 0)
+            s["lV"][at], s["lK"][at] = float(kind), 1.0
+    if kind == "unseen":
+        s["q_pos0"][::2] = -5 * tq
+        s["pos"][s["rows"][1]] = 10 ** 6
+    if kind == "seen nan":
+        s["lK"][s["loc_off"][5] + 3] = float("nan")
+    O, L = _run(dodo, s)
+    if kind == "seen nan":
+        q = slice(s["q_off"][5], s["q_off"][6])
+        assert torch.isfinite(O[q][:2]).all() and torch.isnan(O[q][4:]).all()
+        some.remove(5)
+    if kind in ("nan", "inf"):
+        for b in some:
+            q, l = slice(s["q_off"][b], s["q_off"][b + 1]), s["loc_off"][b]
+            n = q.stop - q.start - 1
+            first = int(s["loc_pos0"][b] + n - s["q_pos0"][b])       # the first token that sees it
+            assert torch.isfinite(O[q][:first]).all() and not torch.isfinite(O[q][first:]).any()
+            s["lV"][l + n] = 0.0
+            O[q][first:] = 0.0
+            qq, Q, qpos, K, V, kpos = _sequence(s, b)
+            o, lse = paged64.attend(Q, qpos, s["scale"], K, V, kpos)
+            tO, _ = paged64.attend_bounds(Q, qpos, s["scale"], K, V, kpos, o, lse, plain64.HALF["f32"], 0.0)
+            assert (np.abs(_f64(O[q]) - o) <= tO)[:first].all()
+        return
+    _check(s, O, L, only=some)
+    if kind == "long":
+        O2, L2 = _run(dodo, s, workspace=False)
+        _check(s, O2, L2, only=some)
+
+
+def test_many_f32_rows_behind_bad_pages_and_again(libdodo):
+    own = api.Dodo(0)
+    s = _batch(F32, 16, 8, 64, [20] * 20, [100] * 20, [20] * 20, 16)
+    s["table"][1], s["table"][4], s["table"][8] = -1, s["pages"], 2 ** 31 - 1
+    O, L = _run(own, s)
+    assert own.device_status() == api.DEV_BAD_INDEX
+    for b, gone in ((0, (1, 4)), (1, (1,))):
+        keep = np.array([r // 16 not in gone for r in range(100)])
+        s["rows"][b] = s["rows"][b][keep]
+        s["nug"][b] = keep.sum()
+    _check(s, O, L, only=[0, 1, 2, 19])
+    own.reset()
+    own.close()
