@@ -77,7 +77,9 @@ DODO_API int dodo_reset(dodo_ctx* ctx, void* stream);
  *                          (tensor-core kernels), or on a sequence's selection flag (dodo_compress);
  *                          results of that launch are invalid, call dodo_reset before reusing the context
  *   DODO_DEV_BAD_INDEX     a gather met an index outside [0, n_b) of its sequence; that nugget's cache
- *                          row and position were left as they were, every other row is correct */
+ *                          row and position were left as they were, every other row is correct.  Or a call met
+ *                          an entry of a page table that is no page: its rows were left out of the append, or
+ *                          taken as not seen */
 enum { DODO_DEV_WAIT_TIMEOUT = 1, DODO_DEV_BAD_INDEX = 2 };
 DODO_API int dodo_device_status(dodo_ctx* ctx, int* status);
 
@@ -464,7 +466,8 @@ DODO_API int dodo_rope_init(dodo_rope_spec* rope, int rot, int layout, float sca
  *            Addresses are aligned to their element type, strides free (16-byte alignment of both is the fast case)
  *   row_off  [host] int32[B+1], non-decreasing from 0: rows of sequence b      pos0 [host] int32[B]: position of its first row
  * Rows outside row_off[0] .. row_off[B] are left as they were.  Supported: dh even, 2 to 512, rot <= dh; positions in
- * [-2^31, 2^31).  An output may be a nugget cache: the next dodo_attend reads none of it early.
+ * [-2^31, 2^31); 65,535 heads in all arrays (DODO_ERR_UNSUPPORTED).  An output may be a nugget cache: the next dodo_attend reads
+ * none of it early.
  */
 typedef struct {
     const void* in;

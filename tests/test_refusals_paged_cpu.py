@@ -221,3 +221,9 @@ def test_binding_refuses_shapes_and_tables(host):
                 dict(locK=torch.zeros(3, 2, 64), locV=torch.zeros(3, 2, 64)), dict(loc_len=[])):
         with pytest.raises(ValueError):
             host.attend_paged(**{**a, **bad})
+
+
+@pytest.mark.parametrize("heads,status", [((65536,), UNSUP), ((40000, 40000), UNSUP), ((2 ** 31 - 1, 2 ** 31 - 1), UNSUP)])
+def test_rope_refuses_more_heads_than_a_launch_counts(ctx, heads, status):
+    arrays = b"".join(_array(heads=h) for h in heads)
+    assert _call(ctx, "dodo_rope", **_rope(arrays=arrays, n=len(heads))) == status
