@@ -691,7 +691,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                 const float om = xch[(st ^ 1) * 2 * BM + row], ol = xch[(st ^ 1) * 2 * BM + BM + row];
                 M = fmaxf(m, om);
                 const float a0 = part_weight(m, M), a1 = part_weight(om, M);
-                S = (a0 != 0.f ? a0 * l : 0.f) + (a1 != 0.f ? a1 * ol : 0.f);
+                S = __fadd_rn(a0 != 0.f ? __fmul_rn(a0, l) : 0.f, a1 != 0.f ? __fmul_rn(a1, ol) : 0.f);      // the same number in both
                 w0 = st == 0 ? a0 : a1;
                 w1 = st == 0 ? a1 : a0;
             }

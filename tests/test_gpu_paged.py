@@ -669,3 +669,13 @@ def test_many_f32_rows_behind_bad_pages_and_again(libdodo):
     _check(s, O, L, only=[0, 1, 2, 19])
     own.reset()
     own.close()
+
+
+@pytest.mark.parametrize("H,Hkv,tq,dh,nug", [(4, 4, 140, 64, 9001), (4, 2, 64, 128, 9001), (8, 8, 128, 128, 16000), (8, 2, 100, 64, 5000), (8, 4, 9, 128, 7000)])
+def test_the_same_bits_every_time(dodo, H, Hkv, tq, dh, nug):
+    """Lists that many blocks share: whichever of them comes last, the order of every sum is the same."""
+    s = _batch(BF, H, Hkv, dh, [tq, 1], [nug, 40], [tq + 100, 1], 32, span=2)
+    O, L = _run(dodo, s)
+    for _ in range(20):
+        O2, L2 = _run(dodo, s)
+        assert torch.equal(O, O2) and torch.equal(L, L2)
