@@ -121,6 +121,7 @@ def _dev(t: torch.Tensor | None):
 
 
 _I32 = np.dtype(np.int32)
+_ROPE_ARRAY = struct.Struct("QQiiqqqq")
 
 
 def _table(a) -> bytes | None:
@@ -565,28 +566,33 @@ class Dodo:
                                              B, o, ls, w, ws_bytes, _stream()))
 
     # -- rotary positions -----------------------------------------------------------------------------
+    # (These calls and those of the paged cache are short on the device: they look at every argument once, without helpers in between.)
+    def _rope_array(self, x, y, rows, dh, dt, name):
+        shape, a = x.shape, x.stride()
+        if len(shape) != 3 or shape[0] != rows or shape[2] != dh or y is not None and y.shape != shape:
+            raise ValueError(f"{name} and its output must have shape [{rows}, heads, {dh}], have {tuple(shape)} and {tuple((x if y is None else y).shape)}")
+        if x.dtype is not dt or y is not None and y.dtype is not dt:
+            raise TypeError(f"{name} and its output must be {dt}, are {x.dtype} and {(x if y is None else y).dtype}")
+        out, b = (x, a) if y is None else (y, y.stride())
+        if x.get_device() != self._index or y is not None and y.get_device() != self._index or dh > 1 and (a[2] != 1 or b[2] != 1):
+            raise ValueError(f"{name} and its output must be tensors on {self.device} whose features lie side by side")
+        at = x.data_ptr()
+        return _ROPE_ARRAY.pack(at, at if y is None else out.data_ptr(), shape[1], 0, a[0], a[1], b[0], b[1])
+
     def _rope(self, entry, rope, row_off, pos0, Q, K, outQ, outK):
         ro, p0 = _table(row_off), _table(pos0)
         if K is None and outK is not None:
             raise ValueError("outK is given without K")
-        B, rows, dt, packed, n = len(ro) // 4 - 1, Q.shape[0], Q.dtype, b"", 0
-        dh = Q.shape[-1]
-        for x, y, name in ((Q, outQ, "Q"), (K, outK, "K")):
-            if x is None:
-                continue
-            y = x if y is None else y
-            if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != dh or y.shape != x.shape:
-                raise ValueError(f"{name} and its output must have shape [{rows}, heads, {dh}], have {tuple(x.shape)} and {tuple(y.shape)}")
-            if x.dtype is not dt or y.dtype is not dt:
-                raise TypeError(f"{name} and its output must be {dt}, are {x.dtype} and {y.dtype}")
-            a, b = x.stride(), y.stride()
-            if x.get_device() != self._index or y.get_device() != self._index or dh > 1 and (a[2] != 1 or b[2] != 1):
-                raise ValueError(f"{name} and its output must be tensors on {self.device} whose features lie side by side")
-            packed += struct.pack("QQiiqqqq", x.data_ptr(), y.data_ptr(), x.shape[1], 0, a[0], a[1], b[0], b[1])
-            n += 1
+        rows, dt = Q.shape[0], Q.dtype
+        dh, B = Q.shape[-1], len(ro) // 4 - 1
+        packed, n = self._rope_array(Q, outQ, rows, dh, dt, "Q"), 1
+        if K is not None:
+            packed, n = packed + self._rope_array(K, outK, rows, dh, dt, "K"), 2
         _bound(ro, B, rows, "row_off")
         _entries(p0, B, "pos0")
-        self._check(entry(self._ctx, rope._spec, packed, n, _dtype_code(Q), dh, ro, p0, B, _stream()))
+        rc = entry(self._ctx, rope._spec, packed, n, _dtype_code(Q), dh, ro, p0, B, _stream())
+        if rc != OK:
+            self._check(rc)
 
     def rope(self, rope, row_off, pos0, Q, K=None, outQ=None, outK=None):
         """``dodo_rope``: queries and keys ([rows, heads, dh], any strides between rows and heads) turned by their positions, sequence
@@ -598,27 +604,20 @@ class Dodo:
         self._rope(self._lib.dodo_rope_backward, rope, row_off, pos0, dQ, dK, outQ, outK)
 
     # -- the paged nugget cache -------------------------------------------------------------------------
-    def _pages(self, cache, page_off, B):
-        if cache.index != self._index:
-            raise ValueError(f"the cache must be on {self.device}")
-        _bound(page_off, B, cache.entries, "page_off")
-
     def gather_kv_paged(self, K, V, seq_off, idx, nug_off, pos_base, rope, cache, page_off, cache_len):
         """``dodo_gather_kv_paged``: append the selected rows (all of them where ``idx`` is None) to a ``PagedCache``, K turned by
         ``rope`` (None: copied).  K and V may be slices of a wider row; ``cache_len`` (int32 numpy array) is updated in place."""
         so, pb, po, cl = _table(seq_off), _table(pos_base), _table(page_off), _in_place(cache_len)
-        tokens, H, dh = self._heads(K, "K")
-        B, dt, row = len(so) // 4 - 1, cache.dtype, H * dh
-        if H != cache.H or dh != cache.dh or K.shape != V.shape:
-            raise ValueError(f"K and V must have shape [tokens, {cache.H}, {cache.dh}], have {tuple(K.shape)} and {tuple(V.shape)}")
-        stride = K.stride()
-        pitch = stride[0] if tokens > 1 else row
-        for t, name in ((K, "K"), (V, "V")):
-            s = t.stride()
-            if t.dtype is not dt:
-                raise TypeError(f"{name} must be {dt}, is {t.dtype}")
-            if t.get_device() != self._index or s[2] != 1 and dh > 1 or s[1] != dh and H > 1 or tokens > 1 and s[0] != pitch:
-                raise ValueError(f"{name} must be a tensor on {self.device} whose rows are dense and as far apart as K's")
+        shape, dt, index = K.shape, cache.dtype, self._index
+        if len(shape) != 3 or shape[1] != cache.H or shape[2] != cache.dh or V.shape != shape:
+            raise ValueError(f"K and V must have shape [tokens, {cache.H}, {cache.dh}], have {tuple(shape)} and {tuple(V.shape)}")
+        tokens, H, dh = shape
+        B, k, v = len(so) // 4 - 1, K.stride(), V.stride()
+        if K.dtype is not dt or V.dtype is not dt:
+            raise TypeError(f"K and V must be {dt}, are {K.dtype} and {V.dtype}")
+        if K.get_device() != index or V.get_device() != index or dh > 1 and (k[2] != 1 or v[2] != 1) or H > 1 and (k[1] != dh or v[1] != dh) or \
+                tokens > 1 and k[0] != v[0]:
+            raise ValueError(f"K and V must be tensors on {self.device} whose rows are dense and equally far apart")
         ix = no = None
         if idx is not None:
             ix, no = self._ptr(idx, torch.int32, None, "idx"), _table(nug_off)
@@ -627,9 +626,13 @@ class Dodo:
         _entries(pb, B, "pos_base")
         if cache_len.size < B:
             raise ValueError(f"cache_len must have {B} entries")
-        self._pages(cache, po, B)
-        self._check(self._lib.dodo_gather_kv_paged(self._ctx, K.data_ptr(), V.data_ptr(), pitch, so, ix, no, pb, B, None if rope is None else rope._spec,
-                                                   cache.spec, po, cl, _stream()))
+        if cache.index != index:
+            raise ValueError(f"the cache must be on {self.device}")
+        _bound(po, B, cache.entries, "page_off")
+        rc = self._lib.dodo_gather_kv_paged(self._ctx, K.data_ptr(), V.data_ptr(), k[0] if tokens > 1 else H * dh, so, ix, no, pb, B,
+                                            None if rope is None else rope._spec, cache.spec, po, cl, _stream())
+        if rc != OK:
+            self._check(rc)
 
     def attend_paged_workspace_bytes(self, dh: int) -> int:
         return int(self._lib.dodo_attend_paged_workspace_bytes(self._ctx, int(dh)))
@@ -638,25 +641,33 @@ class Dodo:
         """``dodo_attend_paged``: ``attend`` over a ``PagedCache`` and local tokens; Q may have several heads for each of the cache's."""
         qo, qp, po, cl = _table(q_off), _table(q_pos0), _table(page_off), _table(cache_len)
         lo, ll, lp = _table(loc_off), _table(loc_len), _table(loc_pos0)
-        rows_q, H, dh = self._heads(Q, "Q")
-        B, dt, ptr = len(qo) // 4 - 1, cache.dtype, self._ptr
-        if dh != cache.dh:
-            raise ValueError(f"Q has heads of {dh}, the cache of {cache.dh}")
-        _bound(qo, B, rows_q, "q_off")
-        _entries(qp, B, "q_pos0")
-        q, o = ptr(Q, dt, None, "Q"), ptr(O, dt, Q.numel(), "O")
+        shape, index, dt, ptr = Q.shape, self._index, cache.dtype, self._ptr
+        if len(shape) != 3 or shape[2] != cache.dh:
+            raise ValueError(f"Q must have shape [rows, H, {cache.dh}], has {tuple(shape)}")
+        rows_q, H, dh = shape
+        entries = len(qo) - 4            # bytes of a table with one for each sequence
+        B, last, little = entries // 4, int.from_bytes, "little"
+        if qp is None or cl is None or len(qp) < entries or len(cl) < entries or len(po) != entries + 4 or \
+                last(qo[-4:], little, signed=True) > rows_q or last(po[-4:], little, signed=True) > cache.entries:
+            _entries(qp, B, "q_pos0")
+            _entries(cl, B, "cache_len")
+            _bound(qo, B, rows_q, "q_off")
+            _bound(po, B, cache.entries, "page_off")
+        q, o = ptr(Q, dt, None, "Q"), ptr(O, dt, rows_q * H * dh, "O")
         ls = None if lse is None else ptr(lse, torch.float32, rows_q * H, "lse")
-        self._pages(cache, po, B)
-        _entries(cl, B, "cache_len")
+        if cache.index != index:
+            raise ValueError(f"the cache must be on {self.device}")
         lk = lv = None
         loc_rows = 0
         if locK is not None:
             loc_rows = self._heads(locK, "locK")[0]
             lk, lv = ptr(locK, dt, loc_rows * cache.H * dh, "locK"), ptr(locV, dt, loc_rows * cache.H * dh, "locV")
-        _local_tables(lo, ll, lp, B, locK is not None)
-        w, ws_bytes = self._workspace(workspace)
-        self._check(self._lib.dodo_attend_paged(self._ctx, q, qo, qp, H, sm_scale, cache.spec, po, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls,
-                                                w, ws_bytes, _stream()))
+        if lo is None or ll is None or lp is None or len(lo) < entries or len(ll) < entries or len(lp) < entries:
+            _local_tables(lo, ll, lp, B, locK is not None)
+        w, ws_bytes = (None, 0) if workspace is None else (ptr(workspace, workspace.dtype, None, "workspace"), workspace.nbytes)
+        rc = self._lib.dodo_attend_paged(self._ctx, q, qo, qp, H, sm_scale, cache.spec, po, cl, lk, lv, lo, ll, lp, loc_rows, B, o, ls, w, ws_bytes, _stream())
+        if rc != OK:
+            self._check(rc)
 
     def attend_indexed(self, Q, q_off, q_pos0, sm_scale, K, V, seq_off, idx, nug_off, pos_base,
                        locK, locV, loc_off, loc_len, loc_pos0, O, lse, workspace):
