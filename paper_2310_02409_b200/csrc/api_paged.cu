@@ -1,4 +1,6 @@
 // C ABI entry point of attention over a paged cache: checks, tables, choice of kernel.
+#include <algorithm>
+
 #include "paged.cuh"
 
 int dodo_check_paged(dodo_ctx* ctx, const dodo_paged_cache* c, const int32_t* page_off, const int32_t* cache_len, int B, bool rows);
@@ -18,17 +20,26 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, boo
     int64_t share = (work + cut.target - 1) / cut.target;
     if (share < cut.least / cut.keys) share = cut.least / cut.keys;
     // chunks of whole tiles may come to a few blocks more than the device holds at once, whose turn would come behind all others:
-    // larger chunks then, unless the units alone are that many
-    for (int round = 0; round < 16; ++round) {
-        int64_t blocks = 0, units = 0;
+    // larger chunks then, unless the whole units alone are that many.  Lists shorter than a share count as the part of one that they are, and
+    // come last, where they fill what the others leave (7 x 4 or 5
+    // tokens of 34 heads of 64 over lists of 10 to 3976 keys: 56 us where they counted whole, 36 so).
+    int64_t blocks = 0;
+    for (int turn = 0; turn < 16; ++turn) {
+        int64_t parts = 0, whole = 0;      // sixteenths of a share's block
+        blocks = 0;
         for (int i = 0; i < g.nseq; ++i) {
-            const int64_t u = units_of(g.seq[i]), n = tiles_of(g.seq[i]);
-            units += u;
+            const int64_t u = units_of(g.seq[i]), n = tiles_of(g.seq[i]), of = n > share ? 16 * ((n + share - 1) / share) : 1 + 15 * n / share;
+            parts += u * of;
+            whole += u * (of < 16 ? of : 16);
             blocks += u * (n > share ? (n + share - 1) / share : 1);
         }
-        if (blocks <= cut.target || units >= cut.target) break;
-        share += 1 + (blocks - cut.target) * share / (4 * blocks);
+        if (parts <= 16 * static_cast<int64_t>(cut.target) || whole >= 16 * static_cast<int64_t>(cut.target)) break;
+        share += 1 + (parts - 16 * static_cast<int64_t>(cut.target)) * share / (4 * parts);
     }
+    if (blocks > cut.target)
+        std::stable_sort(g.seq, g.seq + g.nseq, [](const PagedSeq& a, const PagedSeq& b) {
+            return static_cast<int64_t>(a.c_len) + a.l_len > static_cast<int64_t>(b.c_len) + b.l_len;
+        });
     int64_t part = 0, tick = 0, cta = 0;
     for (int i = 0; i < g.nseq; ++i) {
         PagedSeq& s = g.seq[i];
@@ -158,11 +169,11 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
             continue;
         }
         const bool token = dtype == DODO_BF16 && boxes, tile = dtype == DODO_F32 && max_rows > 16 && is_tiled(g, a.group, Hkv, max_rows, ctx->num_sms);
-        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : tile ? dodo_paged_tile_cut(ctx, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
+        const PagedCut cut = token ? dodo_paged_token_cut(ctx, max_rows) : tile ? dodo_paged_tile_cut(ctx, g, a.group, Hkv, max_rows) : dodo_paged_rows_cut(ctx, g, a.group, Hkv, max_rows);
         const size_t need = dodo_paged_part_rows(cut) * dodo_paged_part_floats(dh) * sizeof(float);
         dodo_paged_plan(cut, g, a.group, Hkv, workspace != nullptr && workspace_bytes >= need);
         if (token) rc = dodo_launch_paged_token(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st);
-        else if (tile) rc = dodo_launch_paged_tile(ctx, dh, max_rows, g, a, st);
+        else if (tile) rc = dodo_launch_paged_tile(ctx, dh, cut, g, a, st);
         else rc = dodo_launch_paged_rows(ctx, dtype, dh, cut, g, a, st);
         if (rc != DODO_OK) return rc;
     }

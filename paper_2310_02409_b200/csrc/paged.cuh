@@ -57,8 +57,8 @@ int dodo_paged_boxes(dodo_ctx* ctx, const PagedArrays& a, int dh, int loc_rows, 
 PagedCut dodo_paged_token_cut(const dodo_ctx* ctx, int max_rows);
 int dodo_launch_paged_token(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 // many fp32 rows, on the FMA units
-PagedCut dodo_paged_tile_cut(const dodo_ctx* ctx, int max_rows);
-int dodo_launch_paged_tile(dodo_ctx* ctx, int dh, int max_rows, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
+PagedCut dodo_paged_tile_cut(const dodo_ctx* ctx, const PagedGroup& g, int group, int Hkv, int max_rows);
+int dodo_launch_paged_tile(dodo_ctx* ctx, int dh, const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 int dodo_launch_paged_rows(dodo_ctx* ctx, int dtype, int dh, const PagedCut& cut, const PagedGroup& g, const PagedArrays& a, cudaStream_t st);
 
 #ifdef __CUDACC__
