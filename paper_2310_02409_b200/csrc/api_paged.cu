@@ -21,8 +21,8 @@ void dodo_paged_plan(const PagedCut& cut, PagedGroup& g, int group, int Hkv, boo
     if (share < cut.least / cut.keys) share = cut.least / cut.keys;
     // chunks of whole tiles may come to a few blocks more than the device holds at once, whose turn would come behind all others:
     // larger chunks then, unless the whole units alone are that many.  Lists shorter than a share count as the part of one that they are, and
-    // come last, where they fill what the others leave (7 x 4 or 5
-    // tokens of 34 heads of 64 over lists of 10 to 3976 keys: 56 us where they counted whole, 36 so).
+    // come last, where they fill what the others leave (7 x 4 or 5 tokens of 34 heads of 64 over lists of 10 to 3976 keys: 56 us where they
+    // counted whole, 36 so).
     int64_t blocks = 0;
     for (int turn = 0; turn < 16; ++turn) {
         int64_t parts = 0, whole = 0;      // sixteenths of a share's block

@@ -3,7 +3,8 @@
 // 179 us by the clock, 0.98 to 1.06 PFLOP/s.  Bound by a tile's round, scores -> softmax -> weights -> values: about 3000 cycles for 128
 // keys of 256 rows, of which the matrix products are 2048; short lists by a unit's begin and end, about three rounds.
 //
-// Work is counted in slots, one per tile of 128 keys of a unit (sequence, KV head, tile of rows); the units are laid end to end and
+// Work is counted in slots, one per tile of 128 keys of a unit (sequence, KV head, tile of rows) and, where units differ, a few ahead of
+// them for the unit's begin and end; the units are laid end to end and
 // thread block c of G, one per SM, takes the slots [c T / G, (c+1) T / G) whatever units they fall in.  A unit that a block boundary
 // cuts is finished through partial results in the workspace; the last of its blocks to arrive joins them.  Nobody waits for anybody.
 //
@@ -62,9 +63,10 @@ struct Layout {
 
 struct DenseShare {
     int total;                      // slots
+    int ahead;                      // slots of a unit ahead of its tiles', for what its begin and end cost
     int whole;                      // slots that a block takes or leaves together: 1, or a unit's where blocks take whole units
     int slot0[DODO_GROUP + 1];      // first slot of each sequence
-    int nt[DODO_GROUP];             // slots of a unit of the sequence
+    int nt[DODO_GROUP];             // tiles of a unit of the sequence
     int tiles[DODO_GROUP];          // tiles of rows
 };
 
@@ -146,21 +148,22 @@ __device__ __forceinline__ bool next_segment(const PagedGroup& g, const PagedArr
         if (w.slot0[mid] <= x) lo = mid; else hi = mid;
     }
     const PagedSeq& s = g.seq[lo];
-    const int off = x - w.slot0[lo], unit = off / w.nt[lo];
+    const int off = x - w.slot0[lo], unit = off / (w.nt[lo] + w.ahead), begin = x - (off - unit * (w.nt[lo] + w.ahead));
+    if (end - begin <= w.ahead) return false;       // the next block has its first tile
     q.b = lo;
     q.tile = unit % w.tiles[lo];
     q.head = unit / w.tiles[lo];
     q.nt = w.nt[lo];
-    q.t0 = off - unit * q.nt;
-    q.first_slot = x - q.t0;
-    q.t1 = min(q.nt, q.t0 + end - x);
+    q.first_slot = begin + w.ahead;
+    q.t0 = max(0, x - q.first_slot);
+    q.t1 = min(q.nt, end - q.first_slot);
     q.r0 = q.tile * tile_rows;
     q.rows = min(tile_rows, s.tq * a.group - q.r0);
     q.min_pos = s.q_pos0 + token_of(a, q.r0);
     q.last_pos = s.q_pos0 + token_of(a, q.r0 + q.rows - 1);
     q.c_tiles = (s.c_len + BN - 1) / BN;
     q.l_vis = dodo_visible_local(s.l_len, s.l_pos0, q.last_pos);
-    x += q.t1 - q.t0;
+    x = q.first_slot + q.t1;
     return true;
 }
 
@@ -798,7 +801,7 @@ attend_paged_dense_kernel(const __grid_constant__ PagedBoxes maps, const __grid_
                     }
                 } else {
                     // the unit is the first of every block but the one that it begins in
-                    const int begun = block_start(work, G, c_first) < q.first_slot ? 1 : 0;
+                    const int begun = block_start(work, G, c_first) < q.first_slot - work.ahead ? 1 : 0;
                     auto part_of = [&](int c) { return a.part + static_cast<size_t>(2 * c + (c == c_first ? begun : 0)) * L::kPartFloats; };
                     auto max_sum = [&](int c) { return c == bid ? make_float2(M, S) : __ldcg(reinterpret_cast<const float2*>(part_of(c) + static_cast<size_t>(DH) * L::kRows) + my); };
                     MM = -INFINITY, SS = 0.f;
@@ -880,43 +883,52 @@ int dodo_launch_paged_dense(dodo_ctx* ctx, int dh, int max_rows, int loc_rows, c
     const int tiles = max_rows > BM ? 2 : 1, tile_rows = tiles * BM;
     DenseShare w;
     int64_t total = 0, units = 0;
+    bool alike = true;
+    int nt = 0;
     for (int i = 0; i < g.nseq; ++i) {
         const PagedSeq& s = g.seq[i];
         const int64_t rows = static_cast<int64_t>(s.tq) * a.group, rt = (rows + tile_rows - 1) / tile_rows;
-        const int l_vis = s.tq > 0 ? dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) : 0, nt = (s.c_len + BN - 1) / BN + (l_vis + BN - 1) / BN;
-        w.slot0[i] = static_cast<int>(total);
-        w.nt[i] = nt > 0 ? nt : 1;
+        const int l_vis = s.tq > 0 ? dodo_visible_local(s.l_len, s.l_pos0, s.q_pos0 + s.tq - 1) : 0, n = (s.c_len + BN - 1) / BN + (l_vis + BN - 1) / BN;
+        w.nt[i] = n > 0 ? n : 1;
         w.tiles[i] = static_cast<int>(rt > 0 ? rt : 1);
         total += rt * a.Hkv * w.nt[i];
         units += rt * a.Hkv;
-        if (total > 0x7fffffff) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "more than 2^31 tiles of keys in 64 sequences");
+        if (s.tq > 0) { alike = alike && (nt == 0 || nt == w.nt[i]); nt = w.nt[i]; }
     }
-    w.slot0[g.nseq] = static_cast<int>(total);
-    w.total = static_cast<int>(total);
     if (total == 0) return DODO_OK;
+    // A unit begun and ended costs about three tiles' times (Q, a pipeline filled and emptied, results), pieces joined another three.  Where
+    // units differ in length they count so much longer, or blocks with many short ones would work longest (8 x 18 to 26 queries of two heads a
+    // KV head over lists of 30 to 3178 keys, 27 KV heads: 58 us, 38 so).  Not with four-row gather copies, whose tiles take as long as that.
     // One block per SM, but none for less than four tiles (with one tile of rows two: the streams take them side by side; 7 x 12 to 16
     // queries of eight heads a KV head over up to 2296 keys took 29 us with four, 25 with two) or a unit.  Where all units are alike there
     // is also the share of a k-th of a unit each (no block then works for two units) and that of whole units (none is joined: 256 units of
-    // 64 rows over 264 keys took 36 us with equal shares, 26 so).  By the count of tiles' times of the slowest block: a unit begun and ended
-    // costs about three (Q, a pipeline filled and emptied, results), pieces joined another three.
+    // 64 rows over 264 keys took 36 us with equal shares, 26 so), by the slowest block's count of tiles' times.
+    constexpr int kUnit = 3;
     const int64_t shares = tiles == 1 ? (total + 1) / 2 : (total + 3) / 4, most = shares > units ? shares : units;
     int64_t grid = most < ctx->num_sms ? most : ctx->num_sms;
-    bool alike = true;
-    int nt = 0;
-    for (int i = 0; i < g.nseq; ++i)
-        if (g.seq[i].tq > 0) { alike = alike && (nt == 0 || nt == w.nt[i]); nt = w.nt[i]; }
     w.whole = 1;
+    const int box = dodo_paged_box(a.page, BN);
+    w.ahead = alike || box == 0 ? 0 : kUnit;
     if (alike) {
         const int64_t each = (total + grid - 1) / grid, most_units = (units + ctx->num_sms - 1) / ctx->num_sms;
-        int64_t cost = each + 3 * ((each + nt - 1) / nt + 1) + 3;
-        if (units > ctx->num_sms && most_units * (nt + 3) < cost) { grid = ctx->num_sms; w.whole = nt; }
+        int64_t cost = each + kUnit * ((each + nt - 1) / nt + 1) + kUnit;
+        if (units > ctx->num_sms && most_units * (nt + kUnit) < cost) { grid = ctx->num_sms; w.whole = nt; }
         for (int64_t k = 1; k <= ctx->num_sms / units && k <= (nt + 3) / 4; ++k) {
-            const int64_t c = (nt + k - 1) / k + 3 + (k > 1 ? 3 : 0);
+            const int64_t c = (nt + k - 1) / k + kUnit + (k > 1 ? kUnit : 0);
             if (c < cost) { cost = c; grid = units * k; }
         }
     }
+    int64_t slots = 0;
+    for (int i = 0; i < g.nseq; ++i) {
+        const int64_t rows = static_cast<int64_t>(g.seq[i].tq) * a.group;
+        w.slot0[i] = static_cast<int>(slots);
+        slots += (rows + tile_rows - 1) / tile_rows * a.Hkv * (w.nt[i] + w.ahead);
+        if (slots > 0x7fffffff) return dodo_fail(ctx, DODO_ERR_UNSUPPORTED, "more than 2^31 tiles of keys in 64 sequences");
+    }
+    w.slot0[g.nseq] = static_cast<int>(slots);
+    w.total = static_cast<int>(slots);
     PagedBoxes maps;
-    const int box = dodo_paged_box(a.page, BN), rc = dodo_paged_boxes(ctx, a, dh, loc_rows, box > 0 ? box : 1, BN, maps);
+    const int rc = dodo_paged_boxes(ctx, a, dh, loc_rows, box > 0 ? box : 1, BN, maps);
     if (rc != DODO_OK) return rc;
     if (dh == 128) return tiles == 2 ? launch<128, 2>(ctx, maps, g, a, w, static_cast<int>(grid), st) : launch<128, 1>(ctx, maps, g, a, w, static_cast<int>(grid), st);
     return tiles == 2 ? launch<64, 2>(ctx, maps, g, a, w, static_cast<int>(grid), st) : launch<64, 1>(ctx, maps, g, a, w, static_cast<int>(grid), st);
