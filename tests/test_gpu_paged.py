@@ -679,3 +679,16 @@ def test_the_same_bits_every_time(dodo, H, Hkv, tq, dh, nug):
     for _ in range(20):
         O2, L2 = _run(dodo, s)
         assert torch.equal(O, O2) and torch.equal(L, L2)
+
+
+@pytest.mark.parametrize("H,Hkv,tq", [(1, 1, 40), (4, 2, 37), (2, 2, 140)])
+def test_ragged_batches_of_many_short_lists(dodo, H, Hkv, tq):
+    """Units of one tile and of many side by side: shares that end within a unit's begin, blocks with nothing to do, order of the short ones."""
+    B = 60
+    nug = [(97 * b) % 250 if b % 19 else 3000 for b in range(B)]
+    for page in (16, 5):
+        s = _batch(BF, H, Hkv, 64, [tq - b % 4 for b in range(B)], nug, [tq - b % 4 if b % 3 else 0 for b in range(B)], page)
+        s["q_pos0"][:] += 2000
+        _check(s, *_run(dodo, s), only=[0, 1, 2, 18, 19, 20, 38, 57, 59])
+        t = _batch(F32, H, Hkv, 64, [1 + b % 9 for b in range(B)], nug, [9] * B, page)
+        _check(t, *_run(dodo, t), only=[0, 1, 19, 20, 59])
