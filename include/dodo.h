@@ -521,8 +521,9 @@ DODO_API int dodo_gather_kv_paged(dodo_ctx* ctx, const void* K, const void* V, i
  *   workspace  [device] 16-byte aligned, contents free; with dodo_attend_paged_workspace_bytes(ctx, dh) bytes long key lists are cut
  *              into pieces for several thread blocks, with fewer (NULL, 0) none is: the same results up to the order of sums, later
  *   everything else as in dodo_attend, except that nothing is read ahead of what precedes the call on its stream
- * Positions of queries and local tokens lie in [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache pos may hold anything.  bf16: weights are
- * rounded to bf16 before their product with V.  Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}; H a multiple of cache->H.
+ * Positions of queries and local tokens lie in [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache pos may hold anything.  bf16: weights keep
+ * 16 bits or more in their product with V; on the tensor-core kernel, which batches of many rows go to, they are rounded to bf16 for it.
+ * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}; H a multiple of cache->H.
  */
 DODO_API size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh);
 DODO_API int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const int32_t* q_pos0, int H, float sm_scale,

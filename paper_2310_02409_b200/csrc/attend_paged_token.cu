@@ -1,6 +1,6 @@
 // Attention of few rows (query tokens x query heads of a KV head) over a paged cache, bf16: what a decode step asks for.  Bound by HBM:
-// every K and V row is read once, and the arithmetic has to stay out of its way.  16 tokens of 32 heads on 8 KV heads over 122,000 keys: 83 us,
-// 6.0 TB/s; one token over 16,448 keys of 40 heads: 57 us, 5.9 TB/s; 8 tokens over 269 keys of 32 heads: 10.1 us, 3.5 TB/s, of which half is
+// every K and V row is read once, and the arithmetic has to stay out of its way.  16 tokens of 32 heads on 8 KV heads over 122,000 keys: 84 us,
+// 6.0 TB/s; one token over 16,448 keys of 40 heads: 57 us, 5.9 TB/s; 8 tokens over 269 keys of 32 heads: 10.3 us, 3.4 TB/s, of which half is
 // a chain of latencies (page, rows, scores, values, results).
 //
 // A block works through a chunk of the key list in stages of 64 keys.  A producer warp looks keys up (page, position), skips stages that
@@ -10,9 +10,10 @@
 //   S^T [16 keys x 8 queries] = K Q^T      K's fragments by ldmatrix as they lie, Q's in registers from the start
 //   O^T [16 features x 8 queries] += V^T P^T      V's by ldmatrix.trans, P^T by transposing S^T's packed fragments (movmatrix)
 // Softmax: a row's reference maximum is its first stage's, and moves only when a score passes it by 2^24 (weights of up to that cost no
-// digit); sums in 32 bits; weights rounded to bf16 for V (at most 2^-8 of each, the rounding of the result itself).  V rows of keys that
-// are not there, or seen by no query, are set to zero in shared memory; what some queries of a tile see and others do not is left to the
-// check of the results at the end (finish).
+// digit); sums in 32 bits.  A weight meets V as the sum of two bf16 numbers, its rounding and the rounding of what that left: 16 bits of it
+// (at most 2^-16 of it is lost) for a second product with fragments that are there already: 0.1 to 0.5 us of the 10 to 84 us of the cases above, 1.7 %
+// at most (8 queries of 2 heads a KV head over 8 x 2064 keys, 23.2 -> 23.6 us).  V rows of keys that are not there, or seen by no query, are set
+// to zero in shared memory; what some queries of a tile see and others do not is left to the check of the results at the end (finish).
 #include "paged.cuh"
 #include "sm100_ptx.cuh"
 
@@ -54,6 +55,11 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+// two floats as bf16, and what the rounding left of them as bf16 again
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& whole, uint32_t& rest) {
+    whole = pack_bf16(a, b);
+    rest = pack_bf16(a - __uint_as_float(whole << 16), b - __uint_as_float(whole & 0xffff0000u));
 }
 
 // NQ: tiles of eight rows
@@ -273,7 +279,7 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
                         for (int k = 0; k < KK; ++k) { o[n][k][e] *= corr; o[n][k][2 + e] *= corr; }
                     }
             }
-            uint32_t pf[NQ][2];
+            uint32_t pf[NQ][2][2];     // keys 0-7 and 8-15; a weight's two pieces
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 float w[4];
@@ -281,8 +287,12 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
                 for (int e = 0; e < 4; ++e) w[e] = exp2_fast(x[n][0][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
                 l[n][0] += w[0] + w[2];
                 l[n][1] += w[1] + w[3];
-                pf[n][0] = transpose8(pack_bf16(w[0], w[1]));
-                pf[n][1] = transpose8(pack_bf16(w[2], w[3]));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    split_bf16(w[2 * h], w[2 * h + 1], pf[n][h][0], pf[n][h][1]);
+                    pf[n][h][0] = transpose8(pf[n][h][0]);
+                    pf[n][h][1] = transpose8(pf[n][h][1]);
+                }
             }
             if ((kind & kHoles) != 0) {
                 unsigned char* const v = base_ptr + st * L::kStage + L::kTile;
@@ -296,7 +306,9 @@ attend_paged_token_kernel(const __grid_constant__ PagedBoxes boxes, const __grid
                 uint32_t f[4];
                 ldmatrix4_trans(sv + (k / 4) * L::kHalf + vr * 128 + (((2 * (k % 4) + vp) ^ (vr & 7)) << 4), f);
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) mma16816(o[n][k], f, pf[n][0], pf[n][1]);
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) mma16816(o[n][k], f, pf[n][0][e], pf[n][1][e]);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty[st]);

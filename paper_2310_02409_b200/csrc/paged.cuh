@@ -165,7 +165,6 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
         const float ref = top == -INFINITY ? 0.f : top, corr = part_weight(m, ref), w = exp2_fast(x - ref);
         m = top;
         l = fmaf(l, corr, w);
-        const float rounded = sizeof(T) == 2 ? __bfloat162float(__float2bfloat16_rn(w)) : w;      // as the product has it
 #pragma unroll
         for (int f = 0; f < F; ++f) acc[f] *= corr;
         uint32_t seen = __ballot_sync(0xffffffffu, sees);
@@ -174,7 +173,7 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
             seen &= seen - 1u;
             const int row = __shfl_sync(0xffffffffu, k.row, e);
             const bool local = __shfl_sync(0xffffffffu, k.local ? 1 : 0, e) != 0;
-            const float c = __shfl_sync(0xffffffffu, rounded, e);
+            const float c = __shfl_sync(0xffffffffu, w, e);
             const T* const vr = static_cast<const T*>(local ? a.lV : a.cV) + static_cast<size_t>(row) * pitch + at + lane * F;
 #pragma unroll
             for (int f = 0; f < F; ++f) acc[f] = fmaf(c, static_cast<float>(vr[f]), acc[f]);
