@@ -83,8 +83,8 @@ DODO_API int dodo_reset(dodo_ctx* ctx, void* stream);
 enum { DODO_DEV_WAIT_TIMEOUT = 1, DODO_DEV_BAD_INDEX = 2 };
 DODO_API int dodo_device_status(dodo_ctx* ctx, int* status);
 
-/* Performance knobs (defaults are tuned for B200; results do not depend on them beyond fp32
- * summation order).  DODO_TUNE_ATTEND_TARGET_BLOCKS: split-K aims at about this many thread blocks
+/* Performance knobs (defaults are tuned for B200; results depend on them through the order of fp32 sums alone, and
+ * where they choose the kernel through its rounding of weights).  DODO_TUNE_ATTEND_TARGET_BLOCKS: split-K aims at about this many thread blocks
  * per dodo_attend launch (default 2 x SM count); changes dodo_attend_workspace_bytes.
  * (Knob 2, a shared-memory stage count, belonged to an earlier kernel and is gone: it is refused.)
  * DODO_TUNE_DENSE_MIN_QUERIES: a call whose longest query block has at least this many tokens
@@ -94,8 +94,11 @@ DODO_API int dodo_device_status(dodo_ctx* ctx, int* status);
  * over thread blocks: 0 (default) balances key tiles over the resident blocks when the units alone
  * would leave SMs idle and the key lists are long, 1 balances whenever the workspace allows (cut
  * units meet through the workspace), 2 never does (one block per unit), 3 balances like 1 but
- * never keeps the query tiles of a head in step (each block takes its own slot range). */
-enum { DODO_TUNE_ATTEND_TARGET_BLOCKS = 1, DODO_TUNE_DENSE_MIN_QUERIES = 3, DODO_TUNE_DENSE_BALANCE = 4 };
+ * never keeps the query tiles of a head in step (each block takes its own slot range).
+ * DODO_TUNE_PAGED_DENSE: which bf16 batches of dodo_attend_paged run on the tensor-core kernel, which rounds weights to bf16:
+ * 0 (default) those of more than 16 rows a KV head that it is expected to be the faster one for, 1 all that it can take
+ * (sm_scale >= 1e-9, a workspace of dodo_attend_paged_workspace_bytes), 2 none: weights then keep 16 bits or more. */
+enum { DODO_TUNE_ATTEND_TARGET_BLOCKS = 1, DODO_TUNE_DENSE_MIN_QUERIES = 3, DODO_TUNE_DENSE_BALANCE = 4, DODO_TUNE_PAGED_DENSE = 5 };
 DODO_API int dodo_set_tuning(dodo_ctx* ctx, int knob, int value);
 
 /* Number of nuggets for n context tokens at compression ratio r >= 1: k = ceil(n / r) in integer
@@ -522,7 +525,8 @@ DODO_API int dodo_gather_kv_paged(dodo_ctx* ctx, const void* K, const void* V, i
  *              into pieces for several thread blocks, with fewer (NULL, 0) none is: the same results up to the order of sums, later
  *   everything else as in dodo_attend, except that nothing is read ahead of what precedes the call on its stream
  * Positions of queries and local tokens lie in [-2^30, 2^30) (DODO_ERR_INVALID_ARG); cache pos may hold anything.  bf16: weights keep
- * 16 bits or more in their product with V; on the tensor-core kernel, which batches of many rows go to, they are rounded to bf16 for it.
+ * 16 bits or more in their product with V; on the tensor-core kernel, which batches of many rows go to, they are rounded to bf16 for it
+ * (DODO_TUNE_PAGED_DENSE keeps every batch off it).
  * Supported: dh in {64, 128}; dtype in {DODO_F32, DODO_BF16}; H a multiple of cache->H.
  */
 DODO_API size_t dodo_attend_paged_workspace_bytes(const dodo_ctx* ctx, int dh);

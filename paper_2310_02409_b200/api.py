@@ -19,7 +19,7 @@ LIB_PATH = Path(__file__).resolve().parent / "libdodo.so"
 F32, BF16 = 0, 1
 FORCE_LAST = 1
 ACT_IDENTITY, ACT_RELU, ACT_GELU_TANH = 0, 1, 2
-TUNE_ATTEND_TARGET_BLOCKS, TUNE_DENSE_MIN_QUERIES, TUNE_DENSE_BALANCE = 1, 3, 4
+TUNE_ATTEND_TARGET_BLOCKS, TUNE_DENSE_MIN_QUERIES, TUNE_DENSE_BALANCE, TUNE_PAGED_DENSE = 1, 3, 4, 5
 DEV_WAIT_TIMEOUT, DEV_BAD_INDEX = 1, 2
 Q4_GROUP = 32
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1

@@ -127,6 +127,7 @@ int dodo_create(dodo_ctx** out, int device) {
     ctx->attend_target_ctas = 2 * ctx->num_sms;
     ctx->dense_min_tq = 32;
     ctx->dense_balance = 0;
+    ctx->paged_dense = 0;
     cudaDriverEntryPointQueryResult qres;
     e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ctx->encode_tiled, cudaEnableDefault, &qres);
     if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || ctx->encode_tiled == nullptr)
@@ -179,6 +180,9 @@ int dodo_set_tuning(dodo_ctx* ctx, int knob, int value) {
     } else if (knob == DODO_TUNE_DENSE_BALANCE) {
         if (value < 0 || value > 3) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "dense balance mode %d (0 to 3)", value);
         ctx->dense_balance = value;
+    } else if (knob == DODO_TUNE_PAGED_DENSE) {
+        if (value < 0 || value > 2) return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "paged dense mode %d (0 to 2)", value);
+        ctx->paged_dense = value;
     } else {
         return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "unknown tuning knob %d", knob);
     }

@@ -163,8 +163,8 @@ int dodo_attend_paged(dodo_ctx* ctx, const void* Q, const int32_t* q_off, const 
         const bool boxes = dodo_paged_box(cache->page, 8) > 0;       // pages that tensor copies can take by boxes
         // Many bf16 rows are a contraction: the tensor cores.  (Row maxima are taken before scaling, so the scale must be positive.)
         if (dtype == DODO_BF16 && sm_scale >= DODO_DENSE_LEAST_SCALE && workspace != nullptr &&
-            workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh) && max_rows > 16 &&
-            (!boxes || is_contraction(g, a.group, Hkv, max_rows, ctx->num_sms))) {
+            workspace_bytes >= dodo_paged_dense_workspace_bytes(ctx->num_sms, dh) && ctx->paged_dense != 2 &&
+            (ctx->paged_dense == 1 || (max_rows > 16 && (!boxes || is_contraction(g, a.group, Hkv, max_rows, ctx->num_sms))))) {
             if ((rc = dodo_launch_paged_dense(ctx, dh, max_rows, any_local ? loc_rows : 0, g, a, st)) != DODO_OK) return rc;
             continue;
         }

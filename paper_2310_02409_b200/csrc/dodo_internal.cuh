@@ -29,6 +29,7 @@ struct dodo_ctx {
     int attend_target_ctas;     // split-K aims at about this many thread blocks per launch
     int dense_min_tq;           // query blocks at least this long go to the tensor-core kernel
     int dense_balance;          // 0 auto, 1 always, 2 never, 3 always but not in step: key tiles balanced over the resident blocks
+    int paged_dense;            // bf16 attend over pages on the tensor cores: 0 by its work, 1 always, 2 never
     void* encode_tiled;         // cuTensorMapEncodeTiled, fetched through the runtime
     // recently encoded tensor maps (a map depends only on these host values, so reuse is exact)
     struct MapEntry { const void* base; int rows, width, box_rows, kind; CUtensorMap map; } map_cache[16];
