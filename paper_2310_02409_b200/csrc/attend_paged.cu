@@ -123,8 +123,9 @@ attend_paged_rows_kernel(const __grid_constant__ PagedGroup g, const __grid_cons
                 }
             }
         }
-        const bool there = key_row >= 0 && my_live, sees = there && key_pos <= my_qpos;
-        const float x = sees ? part[0] : -INFINITY;
+        const bool there = key_row >= 0 && my_live;
+        const float x = there && key_pos <= my_qpos ? part[0] : -INFINITY;
+        const bool sees = x != -INFINITY;              // (a logit of -infinity is as good as none: its V may hold anything too)
         float top = fmaxf(m, x);
 #pragma unroll
         for (int o = COPY; o < COPY * U; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));

@@ -144,9 +144,8 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
 #pragma unroll 1
     for (int j0 = 0; j0 < end; j0 += 32) {
         const Key k = key_at(a, s, j0 + lane, end, page_entry(a, s, j0 + lane, end));
-        const bool sees = k.row >= 0 && k.pos <= qpos;
         float x = -INFINITY;
-        if (sees) {
+        if (k.row >= 0 && k.pos <= qpos) {
             const T* const kr = static_cast<const T*>(k.local ? a.lK : a.cK) + static_cast<size_t>(k.row) * pitch + at;
             x = 0.f;
 #pragma unroll 4
@@ -159,6 +158,7 @@ __device__ __noinline__ void sum_again(const PagedArrays& a, const PagedSeq& s, 
             }
             x *= a.scale_log2;
         }
+        const bool sees = x != -INFINITY;         // a logit of -infinity is as good as none
         float top = fmaxf(m, x);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
