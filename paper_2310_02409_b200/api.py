@@ -223,7 +223,7 @@ class Rope:
 class PagedCache:
     """A paged nugget cache (``dodo_paged_cache``): ``K``, ``V`` [pages, page, H, dh], ``pos`` int32 [pages, page] and ``table``
     int32, the page numbers of all sequences one after the other.  The tensors are checked here and kept, not copied; a program
-    that moves its table to another tensor sets ``table``."""
+    that moves its table to another tensor sets ``table``, one that moves its pool makes another PagedCache."""
 
     def __init__(self, K, V, pos, table):
         if K.dim() != 4:
@@ -231,8 +231,13 @@ class PagedCache:
         self.pages, self.page, self.H, self.dh = K.shape
         for t, dt, n, name in ((K, K.dtype, None, "K"), (V, K.dtype, K.numel(), "V"), (pos, torch.int32, self.pages * self.page, "pos")):
             _checked(t, dt, K.get_device(), n, name)
-        self.K, self.V, self.pos, self.dtype, self.code, self.index = K, V, pos, K.dtype, _dtype_code(K), K.get_device()
+        self._K, self._V, self._pos, self.dtype, self.code, self.index = K, V, pos, K.dtype, _dtype_code(K), K.get_device()
         self.table = table
+
+    # read only: the addresses in `spec` are theirs
+    K = property(lambda self: self._K)
+    V = property(lambda self: self._V)
+    pos = property(lambda self: self._pos)
 
     @property
     def table(self):
@@ -242,7 +247,7 @@ class PagedCache:
     def table(self, t):
         _checked(t, torch.int32, self.index, None, "table")
         self._table, self.entries = t, t.numel()
-        self.spec = struct.pack("QQQQiiiiii", self.K.data_ptr(), self.V.data_ptr(), self.pos.data_ptr(), t.data_ptr(), self.code, self.H, self.dh,
+        self.spec = struct.pack("QQQQiiiiii", self._K.data_ptr(), self._V.data_ptr(), self._pos.data_ptr(), t.data_ptr(), self.code, self.H, self.dh,
                                 self.pages, self.page, 0)
 
 
