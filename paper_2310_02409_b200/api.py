@@ -221,16 +221,17 @@ class Rope:
 
 
 class PagedCache:
-    """A paged nugget cache (``dodo_paged_cache``): ``K``, ``V`` [pages, page, H, dh], ``pos`` int32 [pages, page] and ``table``
-    int32, the page numbers of all sequences one after the other.  The tensors are checked here and kept, not copied; a program
+    """A paged nugget cache (``dodo_paged_cache``): ``K``, ``V`` [pages, page, H, dh], ``pos`` int32 [pages, page] (or flat) and
+    ``table`` int32, the page numbers of all sequences one after the other.  The tensors are checked here and kept, not copied; a program
     that moves its table to another tensor sets ``table``, one that moves its pool makes another PagedCache."""
 
     def __init__(self, K, V, pos, table):
         if K.dim() != 4:
             raise ValueError(f"K must have shape [pages, page, H, dh], has {tuple(K.shape)}")
         self.pages, self.page, self.H, self.dh = K.shape
-        for t, dt, n, name in ((K, K.dtype, None, "K"), (V, K.dtype, K.numel(), "V"), (pos, torch.int32, self.pages * self.page, "pos")):
-            _checked(t, dt, K.get_device(), n, name)
+        rows = (self.pages, self.page)
+        for t, dt, shapes, name in ((K, K.dtype, (K.shape,), "K"), (V, K.dtype, (K.shape,), "V"), (pos, torch.int32, (rows, (rows[0] * rows[1],)), "pos")):
+            _checked(t, dt, K.get_device(), shapes, name)
         self._K, self._V, self._pos, self.dtype, self.code, self.index = K, V, pos, K.dtype, _dtype_code(K), K.get_device()
         self.table = table
 
@@ -245,19 +246,19 @@ class PagedCache:
 
     @table.setter
     def table(self, t):
-        _checked(t, torch.int32, self.index, None, "table")
+        _checked(t, torch.int32, self.index, (t.shape,), "table")
         self._table, self.entries = t, t.numel()
         self.spec = struct.pack("QQQQiiiiii", self._K.data_ptr(), self._V.data_ptr(), self._pos.data_ptr(), t.data_ptr(), self.code, self.H, self.dh,
                                 self.pages, self.page, 0)
 
 
-def _checked(t, dtype, index, numel, name):
+def _checked(t, dtype, index, shapes, name):
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
     if t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and on the device of the others")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"{name} must have {numel} elements, has {t.numel()} (shape {tuple(t.shape)})")
+    if tuple(t.shape) not in [tuple(s) for s in shapes]:
+        raise ValueError(f"{name} must have shape {' or '.join(str(list(s)) for s in shapes)}, has {list(t.shape)}")
 
 
 class Dodo:
@@ -665,8 +666,10 @@ class Dodo:
         lk = lv = None
         loc_rows = 0
         if locK is not None:
-            loc_rows = self._heads(locK, "locK")[0]
-            lk, lv = ptr(locK, dt, loc_rows * cache.H * dh, "locK"), ptr(locV, dt, loc_rows * cache.H * dh, "locV")
+            loc_rows, loc_H, loc_dh = locK.shape if locK.dim() == 3 else (-1, 0, 0)
+            if loc_H != cache.H or loc_dh != dh:
+                raise ValueError(f"locK must have shape [rows, {cache.H}, {dh}], has {tuple(locK.shape)}")
+            lk, lv = ptr(locK, dt, None, "locK"), ptr(locV, dt, loc_rows * loc_H * dh, "locV")
         if lo is None or ll is None or lp is None or len(lo) < entries or len(ll) < entries or len(lp) < entries:
             _local_tables(lo, ll, lp, B, locK is not None)
         w, ws_bytes = (None, 0) if workspace is None else (ptr(workspace, workspace.dtype, None, "workspace"), workspace.nbytes)
