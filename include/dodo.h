@@ -435,8 +435,9 @@ DODO_API int dodo_cache_written(dodo_ctx* ctx);
  * positions; the K/V rows that the calls above take carry them already):
  *   y_a = scale (x_a cos t - x_b sin t),   y_b = scale (x_a sin t + x_b cos t),   t = position * freq[i],   0 <= i < rot / 2
  *   DODO_ROPE_HALF         (a, b) = (i, i + rot / 2)          DODO_ROPE_INTERLEAVED  (a, b) = (2 i, 2 i + 1)
- * Features from `rot` on are copied.  Angles are held as 64-bit fractions of a turn, so that no position loses any of them
- * (2^-33 turns at position 2^31); fp32 arithmetic, one rounding of each result to the array's type.
+ * Features from `rot` on are copied.  Angles are made as 64-bit fractions of a turn and rounded to 32
+ * bits of it, for frequencies of up to a radian within 2^-33 + |position| 2^-64 turns of the exact ones (below 2^-32 everywhere); fp32 arithmetic,
+ * one rounding of each result to the array's type.
  *
  * dodo_rope_frequencies  the frequencies of a base model, in radians per position: freq[i] = base^(-2 i / rot), and for contexts
  *   longer than the `trained` ones

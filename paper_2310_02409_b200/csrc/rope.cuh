@@ -1,9 +1,9 @@
 // Rotary positions: the device side shared by the rotation of whole arrays and by the paged append.
 //
 // The angle of a pair at a position is kept as a fraction of a turn in 64 bits: position x turn[i] modulo 2^64 is one integer
-// product, exact whatever the position (two's complement covers negative ones), where a float angle has lost 17 bits at 100,000
-// tokens.  Its top 32 bits give the quarter turn and a remainder within an eighth of a turn, whose sine and cosine are their
-// Taylor series (degrees 9 and 10 on [-pi/4, pi/4]: 2e-9 off, below fp32's rounding).
+// product that loses nothing but what the frequency's rounding to 64 bits did (two's complement covers negative positions), where a float angle
+// has lost 17 bits at 100,000 tokens.  Rounded to 32 bits (2^-33 turns) it gives the quarter turn and a remainder within an eighth of a turn,
+// whose sine and cosine are their Taylor series (degrees 9 and 10 on [-pi/4, pi/4]: 2e-9 off, below fp32's rounding).
 #pragma once
 
 #include "dodo_internal.cuh"
@@ -20,7 +20,7 @@ struct Rotation {
 // (cos, sin) of the angle of pair i at a position, times the scale
 __device__ __forceinline__ float2 cos_sin(const Rotation& p, int i, int pos) {
     const unsigned long long phase = static_cast<unsigned long long>(static_cast<long long>(pos)) * p.turn[i];
-    const uint32_t t = static_cast<uint32_t>(phase >> 32), q = (t + 0x20000000u) >> 30;
+    const uint32_t t = static_cast<uint32_t>((phase + 0x80000000ull) >> 32), q = (t + 0x20000000u) >> 30;      // rounded; a whole turn is none
     const float a = static_cast<float>(static_cast<int>(t - (q << 30))) * 1.46291807926715968e-9f;    // 2 pi / 2^32
     const float b = a * a;
     const float s = fmaf(a * b, fmaf(b, fmaf(b, fmaf(b, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), a);
