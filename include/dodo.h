@@ -467,7 +467,8 @@ DODO_API int dodo_rope_init(dodo_rope_spec* rope, int rot, int layout, float sca
  *   arrays   [host] n of them: `in` and `out` [device], element (row, head, feature) of `in` at row * in_row + head * in_head +
  *            feature, in elements (dense: in_row = heads * dh, in_head = dh; slices of a fused projection have larger ones), `out`
  *            likewise.  out = in with the same strides works in place; otherwise outputs overlap neither inputs nor each other.
- *            Addresses are aligned to their element type, strides free (16-byte alignment of both is the fast case)
+ *            Addresses are aligned to their element type, strides free (16-byte alignment of both is the fast case) as long as no two
+ *            heads of an output share an element (DODO_ERR_INVALID_ARG); those of an input may
  *   row_off  [host] int32[B+1], non-decreasing from 0: rows of sequence b      pos0 [host] int32[B]: position of its first row
  * Rows outside row_off[0] .. row_off[B] are left as they were.  Supported: dh even, 2 to 512, rot <= dh; positions in
  * [-2^31, 2^31); 65,535 heads in all arrays (DODO_ERR_UNSUPPORTED).  An output may be a nugget cache: the next dodo_attend reads

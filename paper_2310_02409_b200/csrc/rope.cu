@@ -99,6 +99,19 @@ cudaError_t launch(const dodo_ctx* ctx, const RopeArrays& a, const Rotation& p, 
                                  dim3(static_cast<unsigned>(threads)), sizeof(float2) * tokens * p.half, st, a, p, g, dh, slots, lanes, tokens);
 }
 
+// Whether two heads of dh elements each, of `rows` rows and `heads` heads at these distances, share an element
+bool lie_over_one_another(int rows, int heads, int64_t row, int64_t head, int dh) {
+    const __int128 r = row < 0 ? -static_cast<__int128>(row) : row, h = head < 0 ? -static_cast<__int128>(head) : head;
+    if (heads > 0 && ((rows > 1 && r < dh) || (heads > 1 && h < dh))) return true;
+    if (rows <= 1 || heads <= 1 || r >= h * (heads - 1) + dh || h >= r * (rows - 1) + dh) return false;
+    // neither lies whole within a step of the other: heads k apart against the rows next to them
+    for (int k = 1; k < heads; ++k) {
+        const __int128 at = h * k, n = at / r;
+        if ((n < rows && at - n * r < dh) || (n + 1 < rows && (n + 1) * r - at < dh)) return true;
+    }
+    return false;
+}
+
 int rope_impl(dodo_ctx* ctx, const dodo_rope_spec* rope, const dodo_rope_array* arrays, int n, int dtype, int dh, const int32_t* row_off,
               const int32_t* pos0, int B, bool back, cudaStream_t st) {
     if (ctx == nullptr) return DODO_ERR_INVALID_ARG;
@@ -134,6 +147,9 @@ int rope_impl(dodo_ctx* ctx, const dodo_rope_spec* rope, const dodo_rope_array* 
         ++a.n;
     }
     if (a.heads == 0) return DODO_OK;
+    for (int i = 0; i < n; ++i)
+        if (lie_over_one_another(row_off[B], arrays[i].heads, arrays[i].out_row, arrays[i].out_head, dh))
+            return dodo_fail(ctx, DODO_ERR_INVALID_ARG, "array %d: rows and heads of the output lie over one another", i);
     if ((rc = dodo_check_device(ctx)) != DODO_OK) return rc;
     const Rotation p = dodo_rotation(rope, back);
     const bool inter = rope->layout == DODO_ROPE_INTERLEAVED;
