@@ -40,7 +40,7 @@ rope_kernel(const __grid_constant__ RopeArrays a, const __grid_constant__ Rotati
             int lanes, int tokens) {
     extern __shared__ float2 cs[];               // [tokens][half]
     const int tid = static_cast<int>(threadIdx.x), slot = tid % slots, lane = tid / slots;
-    const int row_first = g.row0[0] + static_cast<int>(blockIdx.x) * tokens, row_end = min(row_first + tokens, g.row0[g.nseq]);
+    const int row_first = g.row0[0] + static_cast<int>(blockIdx.x) * tokens, row_end = row_first + min(tokens, g.row0[g.nseq] - row_first);
     const int step = lanes * static_cast<int>(gridDim.y), head0 = lane < lanes ? lane + lanes * static_cast<int>(blockIdx.y) : a.heads;
     const int per_row = head0 < a.heads ? (a.heads - head0 + step - 1) / step : 0;      // this thread's pieces of a row
     const int items = per_row * (row_end - row_first);
@@ -95,7 +95,7 @@ cudaError_t launch(const dodo_ctx* ctx, const RopeArrays& a, const Rotation& p, 
     const int tokens = rows >= 2 * 8 * ctx->num_sms ? 2 : 1;
     const int split = rows >= 4 * ctx->num_sms ? 1 : (a.heads + lanes - 1) / lanes;
     const int threads = (slots * lanes + 31) / 32 * 32;
-    return dodo_launch_dependent(rope_kernel<T, VEC, INTER>, dim3(static_cast<unsigned>((rows + tokens - 1) / tokens), static_cast<unsigned>(split)),
+    return dodo_launch_dependent(rope_kernel<T, VEC, INTER>, dim3(static_cast<unsigned>((rows - 1) / tokens + 1), static_cast<unsigned>(split)),
                                  dim3(static_cast<unsigned>(threads)), sizeof(float2) * tokens * p.half, st, a, p, g, dh, slots, lanes, tokens);
 }
 
