@@ -61,7 +61,8 @@ namespace {
 // tiles of 16.  By what both take for stages of keys per SM: about 6 us and 1.6 us for each 64 keys of 16 rows that two blocks of an SM have,
 // against 14 us and 2.4 us for each 128 keys of a tile of rows.  (16 queries of four heads a KV head, 4 x 4000 keys, 8 KV heads: 46 us there,
 // 32 here; 6 queries over 2000 keys of one sequence: 19 there, 22 here.)  More tiles of 16 rows than blocks at a time take turns: four
-// sequences of 64 rows and 264 keys, 32 KV heads, 25 us there and 15 here.  Up to 16 rows there is nothing to gain here.
+// sequences of 64 rows and 264 keys, 32 KV heads, 25 us there and 15 here.  Up to 16 rows there is nothing to gain here.  Pages that are no
+// multiple of eight rows are not weighed: the other kernel does not take them, and the FMA units would have to, so more than 16 rows go here.
 bool is_contraction(const PagedGroup& g, int group, int Hkv, int max_rows, int num_sms) {
     const int tile_rows = max_rows > 128 ? 256 : 128;
     int64_t few = 0, many = 0, units = 0;

@@ -1,6 +1,7 @@
 // Attention of many rows over a paged cache on the 5th-generation tensor cores (bf16; rows = query tokens x query heads of a KV head).
 // 4 x 256 queries of 32 heads on 8 KV heads over 717 + 1280 keys: 43.7 us, 718 TFLOP/s; 512 queries of 40 heads over 16,896 keys: 164 to
-// 179 us by the clock, 0.98 to 1.06 PFLOP/s.  Bound by a tile's round, scores -> softmax -> weights -> values: about 3000 cycles for 128
+// 179 us by the clock, 0.98 to 1.06 PFLOP/s (call after call, at the power limit, 214: 0.81); with heads of 64 the two take 36 us (435 TFLOP/s)
+// and 132 (661): the same rounds for half the products.  Bound by a tile's round, scores -> softmax -> weights -> values: about 3000 cycles for 128
 // keys of 256 rows, of which the matrix products are 2048; short lists by a unit's begin and end, about three rounds.
 //
 // Work is counted in slots, one per tile of 128 keys of a unit (sequence, KV head, tile of rows) and, where units differ, a few ahead of
@@ -16,7 +17,8 @@
 //       tile's rows and positions in shared memory.
 //   producer (warp 10)  brings K and V by tensor copies with the 128-byte swizzle, a box as many rows high as the power of two that
 //       divides the page's (a page's rows lie side by side), up to the tile's 128; where that is less than eight, four rows at a time by
-//       gather copies (tile::gather4), 11,000 cycles a tile.  Local tokens are boxes of 128.
+//       gather copies (tile::gather4), about 10,000 cycles a tile: the 512 queries in pages of one row 367 us, the four
+//       chunks in pages of five 59.  Local tokens are boxes of 128.
 //   cleaner (warp 11)  writes zeros over V rows of keys that are not there or that no query of the tile sees.
 //   matrix issuer (warp 9)  the whole warp walks the same list, one elected lane issues: every operand of an instruction then lies in
 //       uniform registers.  Per tile and stream O += P V, in halves of 64 keys, then S = Q K^T of the stream's next tile.

@@ -1,6 +1,7 @@
-// Attention of many fp32 rows (query tokens x query heads of a KV head) over a paged cache, on the FMA units: bound by them and by the
-// reads of shared memory that feed them.  Four sequences of 128 queries over 1128 keys, 8 heads of 128: 98 us, 24 TFLOP/s (a row or a few
-// rows a warp, as for few rows: 204 us).
+// Attention of many fp32 rows (query tokens x query heads of a KV head) over a paged cache, on the FMA units.  Four sequences
+// of 128 queries over 1128 keys, 8 heads of 128: 98 us, 24 TFLOP/s, a third of the units' rate (a row or a few rows a warp, as for few rows: 204
+// us).  What stands between: two blocks an SM are two warps a scheduler, which meet at four barriers of the block a step, and the softmax between
+// the two products has nothing beside it.  By their counts neither the FMA units nor shared memory's reads are full.
 //
 // A block takes a tile of 64 (or 32) rows through a chunk of the key list, 48 (64) keys a step: as many as let an SM hold two blocks (four
 // sequences of 64 rows over 1064 keys: 70 us, with 64 keys and one block 81).  Scores and results are made by 8 x 16 threads

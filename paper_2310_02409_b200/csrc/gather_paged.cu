@@ -1,7 +1,10 @@
 // Append to a paged nugget cache: the selected tokens' K and V rows (or all tokens') copied to the rows that the page table names, K
-// rotated at its position on the way.  Bound by HBM: a thread block per appended row, every load of the row (K, V) requested before
-// the block makes the sines and cosines of its one position.  205 of 2048 tokens of each of 8 sequences, 32 heads: 11.2 us, 4.8 TB/s, bound by the
-// chain index -> row -> loads -> stores in the 1.4 waves that the blocks make (V by bulk copies: 10.95); a token of each: 2.5 us, the launch.
+// rotated at its position on the way.  Bound by HBM: a thread block of 128 threads per appended row, whose first two pieces of K and four of V a
+// thread are requested before the block makes the sines and cosines of its one position: the whole row up to 8 KB of K and 8 KB of V (32 heads of
+// 128 in bf16).  What a longer row has beyond comes piece by piece behind that.  205 of 2048 tokens of each of 8 sequences, 32 heads of 128: 11.2 us,
+// 4.8 TB/s, bound by the chain index -> row -> loads -> stores in the 1.4 waves that the blocks make (V by bulk copies: 10.95); 40 heads 14.9 us,
+// 4.5 TB/s; 32 fp32 heads 20.1 us, 5.3 TB/s; a token of each: 2.5 us, the launch.  K of rotations whose halves are no multiple of 16 bytes goes element
+// by element: 32 bf16 heads of 96 with 24 features turned 34 us, where their bytes take 6.
 #include "rope.cuh"
 
 namespace {

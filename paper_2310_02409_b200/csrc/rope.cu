@@ -2,7 +2,9 @@
 // by HBM (16,384 tokens of 40 + 40 heads: 110 us, 6.1 TB/s; gradient of 5120 tokens of 32 + 32 interleaved heads: 34 us, 4.9 TB/s, the
 // launch's begin and end inside it; a token: 2.1 us, the launch).  A block takes a few tokens; its threads make the sines and cosines of the tokens' pairs once, in shared memory (made by
 // every head they would cost as much as the copy), and then run over the heads of all arrays, 16 bytes of each half of a head at
-// a time, the next piece on its way while one is turned.
+// a time: two such pieces (eight of the interleaved layout) are requested together, then turned and stored, the first ones while sines and
+// cosines are made; what covers the others' way is the SM's other warps.  Rotations whose halves are no multiple of 16 bytes go element by element:
+// 16,384 tokens of 40 + 40 bf16 heads of 96 with 24 features turned take 487 us (0.16 of their bytes' time), of 80 with 20 as long, fp32 too.
 #include <math.h>
 
 #include "rope.cuh"
